@@ -1,0 +1,442 @@
+// iwp_tensor.cuh - products of 16-bit matrices on the tensor cores of sm_100a, for the output head of iwp_head.cuh.
+//
+// One persistent kernel template: C[M, N] = A[M, K] B[N, K]^T with fp32 accumulators in tensor memory, and what
+// becomes of a finished tile left to an epilogue class.  Either operand may lie K-contiguous or M/N-contiguous
+// in memory (the tensor cores read both), so none of the three products of a head is ever transposed.
+//
+// A CTA pair (cta_group::2) works on one 256 x 256 tile: each CTA stages its own 128 rows of A and 128 rows of B, so
+// that every byte brought into shared memory feeds twice the arithmetic of a single CTA's 128 x 256 tile
+// (64 instead of 96 bytes per SM and clock at the full tensor rate).  Roles per CTA: warp 0 issues the tile loads
+// (TMA), warp 1 of the pair's first CTA issues the products, warp 2 owns the tensor memory, warps 4..11 are the
+// epilogue (warp % 4 = the 32 lanes of tensor memory it may read, warp / 4 = its half of the columns).  Two
+// accumulator tiles of 256 columns fill the 512 columns of tensor memory, so the epilogue of one tile runs beside the
+// products of the next.
+//
+// Every wait is bounded: a wait that runs out sets the status word and marks the CTA dead; the roles then fall
+// through to the common end, which gives copies in flight time to land, frees the tensor memory and returns.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/iwp.h"
+
+namespace iwp_tc {
+
+constexpr int TILE_M = 128;    // rows of a CTA's accumulator (lanes of tensor memory)
+constexpr int TILE_N = 256;    // columns of the accumulator
+constexpr int BLOCK_K = 64;    // elements of K per stage: 128 bytes, one swizzle row
+constexpr int EPI_WARPS = 8;
+constexpr int THREADS = 128 + 32 * EPI_WARPS;
+constexpr int STAGING_PITCH = 144;                      // bytes per row of the epilogue's staging rows (128 + 16)
+constexpr int STAGING_BYTES = 32 * STAGING_PITCH;       // per epilogue warp
+constexpr uint32_t WAIT_TRIES = 1u << 18;               // x 20 us at most per try: about 5 s
+constexpr uint32_t WAIT_HINT_NS = 20000;
+
+template <int CG>
+struct Shape {
+  static constexpr int A_BYTES = TILE_M * BLOCK_K * 2;
+  static constexpr int B_ROWS = TILE_N / CG;  // rows of B that one CTA stages
+  static constexpr int B_BYTES = B_ROWS * BLOCK_K * 2;
+  static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
+  static constexpr int STAGES = CG == 2 ? 5 : 3;
+  static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * STAGING_BYTES + 256;
+};
+
+// ---- small wrappers of the instructions used ---------------------------------------------------------
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+
+// the address, in the cluster's shared window, of `addr` in the CTA `rank` of this cluster
+__device__ __forceinline__ uint32_t map_to(uint32_t addr, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity), "r"(WAIT_HINT_NS)
+      : "memory");
+  return ok != 0;
+}
+
+// Bounded wait; false = gave up (or another role of this CTA did).
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* dead, int* status) {
+  if (mbar_try(bar, parity)) return true;
+  for (uint32_t i = 0; i < WAIT_TRIES; i++) {
+    if (mbar_try(bar, parity)) return true;
+    if (*dead) return false;
+  }
+  *dead = 1;
+  atomicExch(status, IWP_ERR_TIMEOUT);
+  return false;
+}
+
+template <int CG>
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  if constexpr (CG == 2) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(bar)
+        : "memory");
+  } else {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map),
+        "r"(x), "r"(y), "r"(bar)
+        : "memory");
+  }
+}
+
+template <int CG>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  if constexpr (CG == 2) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+  } else {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+  }
+}
+
+// Arrives on the barrier at this offset in every CTA of the pair once all products issued so far are done.
+template <int CG>
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+  if constexpr (CG == 2) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+                 "h"(static_cast<uint16_t>(3))
+                 : "memory");
+  } else {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+  }
+}
+
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+
+// 32 columns of this warp's 32 lanes: v[j] = column j of the lane's row.
+__device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
+  uint32_t r[32];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+        "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+        "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(addr)
+      : "memory");
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int j = 0; j < 32; j++) v[j] = __uint_as_float(r[j]);
+}
+
+// Shared-memory operand descriptor, 128-byte swizzle.  K-contiguous operands: rows of 128 bytes, groups of 8 rows
+// every 1024 bytes.  M/N-contiguous operands: blocks of 64 rows of M/N (128 bytes) x BLOCK_K, one block after the
+// other (the leading offset), groups of 8 along K every 1024 bytes.
+template <bool K_CONTIGUOUS>
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr) {
+  constexpr uint64_t lead = K_CONTIGUOUS ? 1 : (BLOCK_K * 128) >> 4;
+  return static_cast<uint64_t>((addr & 0x3FFFF) >> 4) | (lead << 16) | (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) |
+         (2ull << 61);
+}
+
+// ---- the work list ---------------------------------------------------------------------------------
+
+struct Work {
+  int m_tiles, n_tiles;  // tiles of TILE_M * CG rows and TILE_N columns
+  int k_blocks;          // blocks of BLOCK_K along K
+  int splits;            // the K range in this many parts (each part a tile of its own)
+  uint32_t idesc;
+  int* status;
+};
+
+struct Tile {
+  int m, n, split, k0, k1;
+};
+
+// Tiles in groups of up to 16 of the shorter side, so that the tiles in flight share operands in the L2.
+__device__ __forceinline__ Tile tile_at(const Work& w, int i) {
+  const int per = w.m_tiles * w.n_tiles;
+  Tile t;
+  t.split = i / per;
+  const int r = i - t.split * per;
+  const bool m_short = w.m_tiles <= w.n_tiles;
+  const int s = m_short ? w.m_tiles : w.n_tiles, l = m_short ? w.n_tiles : w.m_tiles;
+  const int g = r / (16 * l);
+  const int size = min(16, s - 16 * g);
+  const int q = r - g * 16 * l;
+  const int a = 16 * g + q % size, b = q / size;
+  t.m = m_short ? a : b;
+  t.n = m_short ? b : a;
+  t.k0 = static_cast<int>(static_cast<int64_t>(w.k_blocks) * t.split / w.splits);
+  t.k1 = static_cast<int>(static_cast<int64_t>(w.k_blocks) * (t.split + 1) / w.splits);
+  return t;
+}
+
+// Epi: device class with `struct Args` and `static void tile(const Args&, const Tile&, uint32_t tmem, int rank, int
+// warp, int lane, char* staging)`: reads its 128 columns of its 32 rows from tensor memory and disposes of them.
+template <int CG, bool A_KC, bool B_KC, class Epi>
+__global__ void __launch_bounds__(THREADS, 1)
+    k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const Work w,
+              const __grid_constant__ typename Epi::Args args) {
+  using S = Shape<CG>;
+  extern __shared__ char smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  char* const smem = smem_raw + (((raw + 1023) & ~1023u) - raw);  // the same offset in both CTAs of a pair
+  const uint32_t base = smem_u32(smem);
+  char* const staging = smem + S::STAGES * S::STAGE_BYTES;
+  char* const ctl = staging + EPI_WARPS * STAGING_BYTES;
+  const uint32_t bars = smem_u32(ctl);
+  const uint32_t full = bars, empty = bars + 8 * S::STAGES, acc_full = empty + 8 * S::STAGES, acc_empty = acc_full + 16;
+  volatile int* const dead = reinterpret_cast<volatile int*>(ctl + 8 * (2 * S::STAGES + 4));
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(ctl + 8 * (2 * S::STAGES + 4) + 4);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = CG == 2 ? cluster_rank() : 0;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S::STAGES; s++) {
+      mbar_init(full + 8 * s, 1);
+      mbar_init(empty + 8 * s, 1);
+    }
+    for (int b = 0; b < 2; b++) {
+      mbar_init(acc_full + 8 * b, 1);
+      mbar_init(acc_empty + 8 * b, CG * EPI_WARPS);
+    }
+    *dead = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 2) {
+    if constexpr (CG == 2) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_slot)) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_slot)) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    fence_before();
+  }
+  __syncthreads();
+  if constexpr (CG == 2) cluster_sync();
+  fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  const int total = w.m_tiles * w.n_tiles * w.splits;
+  const int first = blockIdx.x / CG, stride = gridDim.x / CG;
+
+  if (warp == 0 && lane == 0) {  // ---- loads
+    int s = 0;
+    uint32_t phase = 0;
+    const uint32_t full_of_pair = CG == 2 ? map_to(full, 0) : full;  // both CTAs' loads are counted by the first CTA
+    for (int i = first; i < total && !*dead; i += stride) {
+      const Tile t = tile_at(w, i);
+      const int row_a = t.m * TILE_M * CG + static_cast<int>(rank) * TILE_M;
+      const int row_b = t.n * TILE_N + static_cast<int>(rank) * S::B_ROWS;
+      for (int kb = t.k0; kb < t.k1; kb++) {
+        if (!mbar_wait(empty + 8 * s, phase ^ 1, dead, w.status)) break;
+        if (rank == 0) mbar_expect(full + 8 * s, CG * S::STAGE_BYTES);
+        const uint32_t bar = full_of_pair + 8 * s;
+        const uint32_t at_a = base + s * S::STAGE_BYTES, at_b = at_a + S::A_BYTES;
+        if constexpr (A_KC) {
+          tma_load<CG>(at_a, &map_a, kb * BLOCK_K, row_a, bar);
+        } else {
+#pragma unroll
+          for (int j = 0; j < TILE_M / 64; j++) tma_load<CG>(at_a + j * 64 * 128, &map_a, row_a + 64 * j, kb * BLOCK_K, bar);
+        }
+        if constexpr (B_KC) {
+          tma_load<CG>(at_b, &map_b, kb * BLOCK_K, row_b, bar);
+        } else {
+#pragma unroll
+          for (int j = 0; j < S::B_ROWS / 64; j++) tma_load<CG>(at_b + j * 64 * 128, &map_b, row_b + 64 * j, kb * BLOCK_K, bar);
+        }
+        if (++s == S::STAGES) {
+          s = 0;
+          phase ^= 1;
+        }
+      }
+    }
+  } else if (warp == 1 && lane == 0 && rank == 0) {  // ---- products
+    int s = 0, b = 0;
+    uint32_t phase = 0, acc_phase = 0;
+    for (int i = first; i < total && !*dead; i += stride) {
+      const Tile t = tile_at(w, i);
+      if (!mbar_wait(acc_empty + 8 * b, acc_phase ^ 1, dead, w.status)) break;
+      fence_after();
+      for (int kb = t.k0; kb < t.k1; kb++) {
+        if (!mbar_wait(full + 8 * s, phase, dead, w.status)) break;
+        fence_after();
+        const uint32_t at_a = base + s * S::STAGE_BYTES;
+        const uint64_t da = operand_desc<A_KC>(at_a), db = operand_desc<B_KC>(at_a + S::A_BYTES);
+        // 16 elements of K further: 32 bytes along a K-contiguous row, 16 rows of 128 bytes otherwise
+        constexpr uint64_t step_a = A_KC ? 2 : 128, step_b = B_KC ? 2 : 128;
+#pragma unroll
+        for (int k = 0; k < BLOCK_K / 16; k++)
+          mma<CG>(tmem + b * TILE_N, da + k * step_a, db + k * step_b, w.idesc, (kb > t.k0 || k > 0) ? 1u : 0u);
+        mma_commit<CG>(empty + 8 * s);
+        if (++s == S::STAGES) {
+          s = 0;
+          phase ^= 1;
+        }
+      }
+      mma_commit<CG>(acc_full + 8 * b);
+      if (++b == 2) {
+        b = 0;
+        acc_phase ^= 1;
+      }
+    }
+  } else if (warp >= 4) {  // ---- epilogue
+    const int e = warp - 4;
+    int b = 0;
+    uint32_t acc_phase = 0;
+    const uint32_t empty_of_pair = CG == 2 ? map_to(acc_empty, 0) : acc_empty;
+    for (int i = first; i < total; i += stride) {
+      const Tile t = tile_at(w, i);
+      const bool ok = mbar_wait(acc_full + 8 * b, acc_phase, dead, w.status);
+      if (!__all_sync(0xFFFFFFFFu, ok)) break;
+      fence_after();
+      const uint32_t at = tmem + b * TILE_N + (e / 4) * (TILE_N / 2) + (static_cast<uint32_t>(e % 4) << 21);
+      Epi::tile(args, t, at, CG * t.m + static_cast<int>(rank), e, lane, staging + e * STAGING_BYTES);
+      fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(empty_of_pair + 8 * b);
+      if (++b == 2) {
+        b = 0;
+        acc_phase ^= 1;
+      }
+    }
+  }
+  __syncwarp();
+  __syncthreads();
+  if (*dead) __nanosleep(1000000);  // copies in flight land in microseconds
+  if constexpr (CG == 2) cluster_sync();
+  if (warp == 2) {
+    fence_after();
+    if constexpr (CG == 2)
+      asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+    else
+      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+  }
+}
+
+// Writes a chunk of 32 columns (v: this lane's row) of the warp's 32 rows to a row-major matrix, through the warp's
+// staging rows so that the stores are whole 32-byte sectors; rows and columns outside are dropped.
+// TYPE: IWP_F32 / IWP_BF16 / IWP_F16.  `add`: the old contents are added first (in fp32).
+__device__ __forceinline__ uint32_t pack2(float a, float b, int type) {
+  if (type == 1) {
+    __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<uint32_t*>(&h);
+  }
+  __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<uint32_t*>(&h);
+}
+
+__device__ __forceinline__ float2 unpack2(uint32_t x, int type) {
+  if (type == 1) return __bfloat1622float2(*reinterpret_cast<__nv_bfloat162*>(&x));
+  return __half22float2(*reinterpret_cast<__half2*>(&x));
+}
+
+__device__ __forceinline__ float load_as_float(const void* p, int64_t i, int type) {
+  if (type == 0) return static_cast<const float*>(p)[i];
+  if (type == 1) return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
+  return __half2float(static_cast<const __half*>(p)[i]);
+}
+
+__device__ __forceinline__ void store_as(void* p, int64_t i, float v, int type) {
+  if (type == 0)
+    static_cast<float*>(p)[i] = v;
+  else if (type == 1)
+    static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
+  else
+    static_cast<__half*>(p)[i] = __float2half_rn(v);
+}
+
+__device__ __forceinline__ void store_chunk(const float (&v)[32], char* staging, void* out, int64_t ld, int type, bool wide, bool add,
+                                            int row0, int rows, int col0, int cols, int lane) {
+  char* mine = staging + lane * STAGING_PITCH;
+  if (type == 0 || !wide || add) {  // staged as fp32
+#pragma unroll
+    for (int j = 0; j < 32; j += 4) *reinterpret_cast<float4*>(mine + 4 * j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 32; j += 8)
+      *reinterpret_cast<uint4*>(mine + 2 * j) =
+          make_uint4(pack2(v[j], v[j + 1], type), pack2(v[j + 2], v[j + 3], type), pack2(v[j + 4], v[j + 5], type),
+                     pack2(v[j + 6], v[j + 7], type));
+  }
+  __syncwarp();
+  const bool whole = wide && col0 + 32 <= cols;
+  if (whole && type != 0 && !add) {
+    const int r = lane >> 2, c = lane & 3;  // 8 rows of 64 bytes at a time
+#pragma unroll
+    for (int i = 0; i < 32; i += 8) {
+      const uint4 x = *reinterpret_cast<const uint4*>(staging + (r + i) * STAGING_PITCH + 16 * c);
+      if (row0 + r + i < rows)
+        *reinterpret_cast<uint4*>(static_cast<char*>(out) + 2 * ((row0 + r + i) * ld + col0) + 16 * c) = x;
+    }
+  } else if (whole && type == 0) {
+    const int r = lane >> 3, c = lane & 7;  // 4 rows of 128 bytes at a time
+#pragma unroll
+    for (int i = 0; i < 32; i += 4) {
+      float4 x = *reinterpret_cast<const float4*>(staging + (r + i) * STAGING_PITCH + 16 * c);
+      if (row0 + r + i < rows) {
+        float4* p = reinterpret_cast<float4*>(static_cast<float*>(out) + (row0 + r + i) * ld + col0) + c;
+        if (add) {
+          const float4 y = *p;
+          x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+        }
+        *p = x;
+      }
+    }
+  } else {  // ragged columns, unaligned rows, or a 16-bit sum: element by element, a row at a time
+    const bool packed = type != 0 && wide && !add;
+    for (int i = 0; i < 32 && row0 + i < rows; i++) {
+      if (col0 + lane < cols) {
+        const int64_t at = (row0 + i) * ld + col0 + lane;
+        const char* from = staging + i * STAGING_PITCH;
+        float x = packed ? load_as_float(from, lane, type) : reinterpret_cast<const float*>(from)[lane];
+        if (add) x += load_as_float(out, at, type);
+        store_as(out, at, x, type);
+      }
+    }
+  }
+  __syncwarp();
+}
+
+}  // namespace iwp_tc
