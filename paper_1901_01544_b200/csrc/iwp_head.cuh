@@ -1,12 +1,16 @@
 // iwp_head.cuh - output head with its loss (cross entropy, or a teacher's top logits): what happens to the tiles of
 // the three products of iwp_tensor.cuh, and the small kernels around them.
 //
-//   logits pass   z tile -> per row and 128 columns: maximum and sum of exp (written), the logits at the targets
-//   finish        per row: lse, loss; their sum in a fixed order
-//   probability   z tile again (recomputed: 2 D operations per logit cost less than keeping T x V of them) ->
-//   pass          row_scale * (exp(z / tau - lse) - q), rounded to the operands' type, for one piece of the vocabulary
-//   dweight       P^T hidden for the piece: complete, since the piece holds every token
-//   dhidden       P weight for the piece, summed over the pieces in fp32
+//   logits pass   z tile -> per row and 32 to 128 columns: maximum and sum of exp (written), the logits at the targets
+//                 and, for one piece of the vocabulary, 16-bit codes of how far z is below that maximum
+//   finish        per row: lse, loss; codes -> row_scale * (exp(z / tau - lse) - q) in the operands' type, in place
+//   gradients     dweight = P^T hidden for the piece (complete, since the piece holds every token) and
+//                 dhidden = P weight for the piece, summed over the pieces in fp32
+//   other pieces  their probabilities come from a second logits product, in the operands' type at once
+//
+// A vocabulary that fits one piece thus costs three products of 2 T V D operations; of a larger one all but the kept
+// piece cost a fourth.  The code of an element costs 4 bytes of traffic, the product it replaces 2 D operations:
+// at D = 2048 0.6 against 3 picoseconds.
 //
 // Cross entropy and distillation differ only in the list of (column, q) that each row subtracts: one entry or top_k
 // of them, sorted by column, so that an epilogue warp meets them in the order in which it walks the columns.
@@ -19,102 +23,186 @@
 
 namespace iwp_head {
 
-using iwp_tc::Tile;
+using iwp_tc::ex2;
+using iwp_tc::Where;
 
 constexpr int MAX_TOP = 1024;
 constexpr int NO_COLUMN = 0x7FFFFFFF;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
-// First bytes of a workspace.
+// First bytes of a workspace.  The tickets wrap to zero with the last block of each launch.
 struct Header {
   int status;
   int n_rows;       // rows with targets
-  uint32_t ticket;  // blocks of the finish kernel that are done
+  uint32_t ticket;
   float gmax;       // largest |dloss_rows|
 };
 
-struct Entries {  // sorted by column within a row; unused ones are NO_COLUMN at the end.  [k][T]: lanes are rows
-  int* column;
-  float* q;
-  float* const_term;  // [T] sum of q log q; NaN for a row with a target outside the vocabulary
-  float* row_scale;   // [T] 1 for a row that gives gradients, 0 otherwise; dloss_rows / gmax where those are given
+// What the rows subtract.  `hard`: one target per row, read as the caller gave them; else lists made by k_soft_targets.
+struct Targets {
+  const int64_t* hard;
+  int64_t ignore;
+  int V;
   int k;
+  const int* column;       // [T][k] ascending, NO_COLUMN at the end
+  const float* q;          // [T][k]
+  const float* const_term; // [T] sum of q log q; NaN for a row with an id outside the vocabulary
+  const float* scale;      // [T] dloss_rows / gmax, or NULL: 1 for rows with targets
+
+  __device__ __forceinline__ int column_at(int64_t row, int i) const {
+    if (!hard) return column[row * k + i];
+    const int64_t y = hard[row];
+    return y != ignore && y >= 0 && y < V ? static_cast<int>(y) : NO_COLUMN;
+  }
+  __device__ __forceinline__ float q_at(int64_t row, int i) const { return hard ? 1.f : q[row * k + i]; }
+  // the first entry at or after col0
+  __device__ __forceinline__ int first(int64_t row, int col0) const {
+    if (hard) return column_at(row, 0) >= col0 ? 0 : 1;
+    int lo = 0, hi = k;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (column[row * k + mid] < col0)
+        lo = mid + 1;
+      else
+        hi = mid;
+    }
+    return lo;
+  }
+  // -1 a target outside the vocabulary, 0 none, 1 some
+  __device__ __forceinline__ int state(int64_t row) const {
+    if (hard) {
+      const int64_t y = hard[row];
+      return y == ignore ? 0 : y >= 0 && y < V ? 1 : -1;
+    }
+    const float c = const_term[row];
+    return column[row * k] != NO_COLUMN ? 1 : c != c ? -1 : 0;
+  }
+  __device__ __forceinline__ float row_scale(int64_t row) const { return state(row) == 1 ? (scale ? scale[row] : 1.f) : 0.f; }
 };
 
-__device__ __forceinline__ int first_entry(const Entries& en, int64_t T, int row, int col0) {
-  int lo = 0, hi = en.k;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (en.column[mid * T + row] < col0)
-      lo = mid + 1;
-    else
-      hi = mid;
+// The next targets of a row, in the order of their columns, a few of them fetched ahead.
+struct Upcoming {
+  int pos, next, after[3];
+  __device__ __forceinline__ void none(const Targets& en) {
+    pos = en.k;
+    next = after[0] = after[1] = after[2] = NO_COLUMN;
   }
-  return lo;
+  __device__ __forceinline__ void from(const Targets& en, int64_t row, int col0) {
+    pos = en.first(row, col0);
+    next = pos < en.k ? en.column_at(row, pos) : NO_COLUMN;
+#pragma unroll
+    for (int i = 0; i < 3; i++) after[i] = pos + 1 + i < en.k ? en.column_at(row, pos + 1 + i) : NO_COLUMN;
+  }
+  __device__ __forceinline__ void advance(const Targets& en, int64_t row) {
+    pos++;
+    next = after[0];
+    after[0] = after[1];
+    after[1] = after[2];
+    after[2] = pos + 3 < en.k ? en.column_at(row, pos + 3) : NO_COLUMN;
+  }
+};
+
+// How the logits pass leaves an element of the kept piece behind in 16 bits, with x = (z - maximum) log2(e) / tau <= 0:
+//   bf16 factors: fp16 of 2^(x + 15).  It is the summand at hand anyway, and right to 2^-11 of itself down to 2^-29 of
+//     the maximum (0 below 2^-40); the factor is rounded to bf16, eight times as coarse, afterwards.
+//   fp16 factors: the float 8 - x with its mantissa rounded to 15 bits, less the bits of 8: steps of 2^-12 in log2
+//     above 2^-8 of the maximum, of 2^-11 to 2^-24, 0 below; a probability is right to 8.5e-5 of itself, where
+//     fp16 of it would be as coarse (2.4e-4 at worst) as the rounding to the factor's type that follows.
+constexpr float SUM_SCALE = 3.0517578125e-5f;  // 2^-15
+constexpr uint32_t EIGHT = 0x41000000u;
+__device__ __forceinline__ uint32_t log_code(float x) {
+  return min((__float_as_uint(8.f - fminf(x, 0.f)) - (EIGHT - 128u)) >> 8, 0xFFFFu);
 }
+__device__ __forceinline__ float log_value(uint32_t code) { return code == 0xFFFFu ? -CUDART_INF_F : 8.f - __uint_as_float((code << 8) + EIGHT); }
 
 // ---- epilogue of the logits pass --------------------------------------------------------------------
 
 struct Logits {
+  static constexpr bool SUMS = true;
   struct Args {
-    Entries en;
+    Targets en;
     int64_t T;
     int V;
     float c;          // log2(e) / tau
-    float2* part;     // [2 * n_tiles][T]: maximum (of z * c) and sum of 2^(z c - maximum)
-    float* z_at;      // [k][T] logits at the targets
+    float2* part;     // [T][parts]: maximum (of z c) and sum of 2^(z c - maximum)
+    int parts;
+    float* z_at;      // [T][k] logits at the targets
+    uint16_t* codes;  // [T][ld] of columns v0 .. v0 + width, or width = 0
+    int64_t ld;
+    int v0, width;
+    int log_codes;
   };
-  static __device__ __forceinline__ void tile(const Args& a, const Tile& t, uint32_t tmem, int row_block, int e, int lane,
-                                              char* staging) {
-    const int row = row_block * iwp_tc::TILE_M + (e % 4) * 32 + lane;
+  static __device__ __forceinline__ Upcoming begin(const Args& a, const Where& w) {
+    Upcoming u;
+    u.none(a.en);
+    if (w.row0 + w.lane < a.T) u.from(a.en, w.row0 + w.lane, w.col0);
+    return u;
+  }
+  static __device__ __forceinline__ void tile(const Args& a, const Where& w, Upcoming& up, float (&acc)[iwp_tc::TILE_N / 2]) {
+    constexpr int CHUNKS = iwp_tc::TILE_N / 64;
+    const int row = w.row0 + w.lane;
     const bool live = row < a.T;
-    const int part = 2 * t.n + e / 4, col0 = part * (iwp_tc::TILE_N / 2);
-    int pos = 0, next = NO_COLUMN;
-    if (live) {
-      pos = first_entry(a.en, a.T, row, col0);
-      if (pos < a.en.k) next = a.en.column[pos * a.T + row];
-    }
-    float m = -CUDART_INF_F, s = 0.f;
-#pragma unroll 1
-    for (int c0 = col0; c0 < min(col0 + iwp_tc::TILE_N / 2, a.V); c0 += 32) {
-      float v[32];
-      iwp_tc::tmem_load32(tmem + (c0 - col0), v);
-      if (__any_sync(0xFFFFFFFFu, next < c0 + 32)) {  // some row has a target here
-        float* mine = reinterpret_cast<float*>(staging + lane * iwp_tc::STAGING_PITCH);
+    float top = -CUDART_INF_F;
 #pragma unroll
-        for (int j = 0; j < 32; j += 4) *reinterpret_cast<float4*>(mine + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-        while (next < c0 + 32) {
-          a.z_at[pos * a.T + row] = mine[next - c0];
-          pos++;
-          next = pos < a.en.k ? a.en.column[pos * a.T + row] : NO_COLUMN;
+    for (int c = 0; c < CHUNKS; c++) {
+      const int c0 = w.col0 + 32 * c;
+      if (32 * c >= w.width) break;
+      if (__any_sync(0xFFFFFFFFu, up.next < c0 + 32)) {  // some row has a target here
+        float* mine = reinterpret_cast<float*>(w.staging + w.lane * iwp_tc::STAGING_PITCH);
+#pragma unroll
+        for (int j = 0; j < 32; j += 4)
+          *reinterpret_cast<float4*>(mine + j) = make_float4(acc[32 * c + j], acc[32 * c + j + 1], acc[32 * c + j + 2], acc[32 * c + j + 3]);
+        while (up.next < c0 + 32) {
+          a.z_at[static_cast<int64_t>(row) * a.en.k + up.pos] = mine[up.next - c0];
+          up.advance(a.en, row);
         }
         __syncwarp();
       }
       if (c0 + 32 > a.V) {
 #pragma unroll
         for (int j = 0; j < 32; j++)
-          if (c0 + j >= a.V) v[j] = -CUDART_INF_F;
+          if (c0 + j >= a.V) acc[32 * c + j] = -CUDART_INF_F;
       }
-      float top = v[0];
 #pragma unroll
-      for (int j = 1; j < 32; j++) top = fmaxf(top, v[j]);
-      const float m_new = fmaxf(m, top * a.c);
-      const float ref = m_new == -CUDART_INF_F ? 0.f : m_new;
-      float add = 0.f;
-#pragma unroll
-      for (int j = 0; j < 32; j++) add += exp2f(fmaf(v[j], a.c, -ref));
-      s = s * exp2f(m - ref) + add;
-      m = m_new;
+      for (int j = 0; j < 32; j++) top = fmaxf(top, acc[32 * c + j]);
     }
-    if (live) a.part[part * a.T + row] = make_float2(m, s);
+    const float m = top * a.c;
+    const float ref = m == -CUDART_INF_F ? 0.f : m;  // nothing but -inf: sums of 0, not of NaN
+    float s = 0.f;
+    const bool keep = w.col0 >= a.v0 && w.col0 < a.v0 + a.width;
+    const float less = 15.f - ref;
+#pragma unroll
+    for (int c = 0; c < CHUNKS; c++) {
+      if (32 * c >= w.width) break;
+      uint32_t packed[16];
+      if (a.log_codes) {
+#pragma unroll
+        for (int j = 0; j < 32; j += 2) {
+          const float x = fmaf(acc[32 * c + j], a.c, -ref), y = fmaf(acc[32 * c + j + 1], a.c, -ref);
+          s += ex2(x + 15.f) + ex2(y + 15.f);
+          packed[j / 2] = log_code(x) | (log_code(y) << 16);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 32; j += 2) {
+          const float x = ex2(fmaf(acc[32 * c + j], a.c, less)), y = ex2(fmaf(acc[32 * c + j + 1], a.c, less));
+          s += x + y;
+          packed[j / 2] = iwp_tc::pack2(x, y, IWP_F16);
+        }
+      }
+      if (keep)
+        iwp_tc::store_packed(packed, w.staging, a.codes, a.ld, w.row0, static_cast<int>(a.T), w.col0 + 32 * c - a.v0, w.lane);
+    }
+    if (live) a.part[static_cast<int64_t>(row) * a.parts + w.col0 / w.width] = make_float2(m, s * SUM_SCALE);
   }
 };
 
 // ---- epilogue of the probability pass -----------------------------------------------------------------
 
 struct Probs {
+  static constexpr bool SUMS = false;
   struct Args {
-    Entries en;
+    Targets en;
     const float* lse;
     void* out;       // [T][ld] of `type`: this piece's columns
     int64_t T, ld;
@@ -123,36 +211,41 @@ struct Probs {
     float up;        // power of two that keeps small probabilities above the smallest fp16 (1 for bf16)
     int type;
   };
-  static __device__ __forceinline__ void tile(const Args& a, const Tile& t, uint32_t tmem, int row_block, int e, int lane,
-                                              char* staging) {
-    const int row0 = row_block * iwp_tc::TILE_M + (e % 4) * 32, row = row0 + lane;
-    const int col0 = t.n * iwp_tc::TILE_N + (e / 4) * (iwp_tc::TILE_N / 2);
-    int pos = 0, next = NO_COLUMN;
-    float scale = 0.f, lse2 = 0.f;
+  struct Begun {
+    Upcoming up;
+    float scale, lse2;
+  };
+  static __device__ __forceinline__ Begun begin(const Args& a, const Where& w) {
+    const int row = w.row0 + w.lane;
+    Begun b;
+    b.up.none(a.en);
+    b.scale = b.lse2 = 0.f;
     if (row < a.T) {
-      scale = a.en.row_scale[row] * a.up;
-      lse2 = a.lse[row] * LOG2E;
-      if (scale != 0.f) {
-        pos = first_entry(a.en, a.T, row, a.v0 + col0);
-        if (pos < a.en.k) next = a.en.column[pos * a.T + row];
-      }
+      b.scale = a.en.row_scale(row) * a.up;
+      b.lse2 = a.lse[row] * LOG2E;
+      if (b.scale != 0.f) b.up.from(a.en, row, a.v0 + w.col0);
     }
+    return b;
+  }
+  static __device__ __forceinline__ void tile(const Args& a, const Where& w, Begun& begun, uint32_t tmem) {
+    const int row = w.row0 + w.lane;
+    Upcoming& up = begun.up;
+    const float scale = begun.scale, lse2 = begun.lse2;
 #pragma unroll 1
-    for (int c0 = col0; c0 < min(col0 + iwp_tc::TILE_N / 2, a.width); c0 += 32) {
+    for (int c0 = w.col0; c0 < min(w.col0 + w.width, a.width); c0 += 32) {
       float v[32];
-      iwp_tc::tmem_load32(tmem + (c0 - col0), v);
+      iwp_tc::tmem_load32(tmem + (c0 - w.col0), v);
       // a row that gives nothing writes zeros whatever its logits are
 #pragma unroll
-      for (int j = 0; j < 32; j++) v[j] = scale == 0.f ? 0.f : exp2f(fmaf(v[j], a.c, -lse2));
+      for (int j = 0; j < 32; j++) v[j] = scale == 0.f ? 0.f : ex2(fmaf(v[j], a.c, -lse2));
       const int end = a.v0 + c0 + 32;
-      if (__any_sync(0xFFFFFFFFu, next < end)) {
-        float* mine = reinterpret_cast<float*>(staging + lane * iwp_tc::STAGING_PITCH);
+      if (__any_sync(0xFFFFFFFFu, up.next < end)) {
+        float* mine = reinterpret_cast<float*>(w.staging + w.lane * iwp_tc::STAGING_PITCH);
 #pragma unroll
         for (int j = 0; j < 32; j += 4) *reinterpret_cast<float4*>(mine + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-        while (next < end) {
-          mine[next - (a.v0 + c0)] -= a.en.q[pos * a.T + row];
-          pos++;
-          next = pos < a.en.k ? a.en.column[pos * a.T + row] : NO_COLUMN;
+        while (up.next < end) {
+          mine[up.next - (a.v0 + c0)] -= a.en.q_at(row, up.pos);
+          up.advance(a.en, row);
         }
 #pragma unroll
         for (int j = 0; j < 32; j += 4) {
@@ -163,7 +256,7 @@ struct Probs {
       }
 #pragma unroll
       for (int j = 0; j < 32; j++) v[j] *= scale;
-      iwp_tc::store_chunk(v, staging, a.out, a.ld, a.type, true, false, row0, static_cast<int>(a.T), c0, a.width, lane);
+      iwp_tc::store_chunk(v, w.staging, a.out, a.ld, a.type, true, false, w.row0, static_cast<int>(a.T), c0, a.width, w.lane);
     }
   }
 };
@@ -186,61 +279,67 @@ struct Factor {
 };
 
 struct Out {
-  struct Args {
-    Factor f;
+  static constexpr bool SUMS = false;
+  struct Matrix {
     void* out;
     int64_t ld, split_stride;  // elements
     int rows, cols, type, wide, add, raw;  // raw: partial sums, the factor is applied later
   };
-  static __device__ __forceinline__ void tile(const Args& a, const Tile& t, uint32_t tmem, int row_block, int e, int lane,
-                                              char* staging) {
-    const int row0 = row_block * iwp_tc::TILE_M + (e % 4) * 32;
-    const int col0 = t.n * iwp_tc::TILE_N + (e / 4) * (iwp_tc::TILE_N / 2);
-    const float f = a.raw ? 1.f : a.f.get();
-    char* const out = static_cast<char*>(a.out) + t.split * a.split_stride * (a.type == IWP_F32 ? 4 : 2);
+  struct Args {
+    Factor f;
+    Matrix m[2];
+  };
+  static __device__ __forceinline__ float begin(const Args& args, const Where& w) { return args.m[w.p].raw ? 1.f : args.f.get(); }
+  static __device__ __forceinline__ void tile(const Args& args, const Where& w, float f, uint32_t tmem) {
+    const Matrix& a = args.m[w.p];
+    char* const out = static_cast<char*>(a.out) + w.split * a.split_stride * (a.type == IWP_F32 ? 4 : 2);
 #pragma unroll 1
-    for (int c0 = col0; c0 < min(col0 + iwp_tc::TILE_N / 2, a.cols); c0 += 32) {
+    for (int c0 = w.col0; c0 < min(w.col0 + w.width, a.cols); c0 += 32) {
       float v[32];
-      iwp_tc::tmem_load32(tmem + (c0 - col0), v);
+      iwp_tc::tmem_load32(tmem + (c0 - w.col0), v);
 #pragma unroll
       for (int j = 0; j < 32; j++) v[j] *= f;
-      iwp_tc::store_chunk(v, staging, out, a.ld, a.type, a.wide, a.add, row0, a.rows, c0, a.cols, lane);
+      iwp_tc::store_chunk(v, w.staging, out, a.ld, a.type, a.wide, a.add, w.row0, a.rows, c0, a.cols, w.lane);
     }
   }
 };
 
-// dhidden = factor * sum over the splits (in order), rounded once.
-__global__ void k_join(Factor f, const float* part, int splits, int64_t rows, int cols, void* out, int64_t ld, int type, int add) {
+// dhidden = factor * sum over the splits (in order), rounded once.  Four columns per thread where rows allow it.
+__global__ void __launch_bounds__(256) k_join(Factor f, const float* part, int splits, int64_t rows, int cols, void* out, int64_t ld, int type,
+                                              int add, int wide) {
+  iwp_tc::launch_next();
+  iwp_tc::wait_previous();
   const float k = f.get();
   const int64_t n = rows * cols;
-  for (int64_t i = blockIdx.x * int64_t(blockDim.x) + threadIdx.x; i < n; i += int64_t(gridDim.x) * blockDim.x) {
-    float x = 0.f;
-    for (int s = 0; s < splits; s++) x += part[s * n + i];
-    x *= k;
-    const int64_t at = (i / cols) * ld + i % cols;
-    if (add) x += iwp_tc::load_as_float(out, at, type);
-    iwp_tc::store_as(out, at, x, type);
-  }
+  const int per = wide ? 4 : 1, groups = cols / per;
+  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
+    for (int g = threadIdx.x; g < groups; g += blockDim.x) {
+      const int64_t i = r * cols + g * per, at = r * ld + g * per;
+      if (wide) {
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int s = 0; s < splits; s++) {
+          const float4 y = __ldcs(reinterpret_cast<const float4*>(part + s * n + i));
+          x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
+        }
+        float v[4] = {x.x * k, x.y * k, x.z * k, x.w * k};
+        if (add)
+          for (int j = 0; j < 4; j++) v[j] += iwp_tc::load_as_float(out, at + j, type);
+        if (type == IWP_F32)
+          *reinterpret_cast<float4*>(static_cast<float*>(out) + at) = make_float4(v[0], v[1], v[2], v[3]);
+        else
+          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at) =
+              make_uint2(iwp_tc::pack2(v[0], v[1], type), iwp_tc::pack2(v[2], v[3], type));
+      } else {
+        float x = 0.f;
+        for (int s = 0; s < splits; s++) x += part[s * n + i];
+        x *= k;
+        if (add) x += iwp_tc::load_as_float(out, at, type);
+        iwp_tc::store_as(out, at, x, type);
+      }
+    }
 }
 
-// ---- targets -> entries -----------------------------------------------------------------------------------
-
-__global__ void k_hard_targets(Header* hdr, Entries en, const int64_t* targets, int64_t ignore, int64_t T, int64_t V) {
-  const int64_t t = blockIdx.x * int64_t(blockDim.x) + threadIdx.x;
-  bool has = false;
-  if (t < T) {
-    const int64_t y = targets[t];
-    const bool ignored = y == ignore, good = !ignored && y >= 0 && y < V;
-    en.column[t] = good ? static_cast<int>(y) : NO_COLUMN;
-    en.q[t] = good ? 1.f : 0.f;
-    en.const_term[t] = ignored || good ? 0.f : CUDART_NAN_F;
-    en.row_scale[t] = good ? 1.f : 0.f;
-    if (!ignored && !good) atomicExch(&hdr->status, IWP_ERR_INVALID);
-    has = !ignored;
-  }
-  const unsigned b = __ballot_sync(0xFFFFFFFFu, has);
-  if ((threadIdx.x & 31) == 0 && b) atomicAdd(&hdr->n_rows, __popc(b));
-}
+// ---- targets -----------------------------------------------------------------------------------------------
 
 __device__ __forceinline__ int64_t load_id(const void* ids, int64_t i, int bytes) {
   return bytes == 8 ? static_cast<const int64_t*>(ids)[i] : static_cast<const int32_t*>(ids)[i];
@@ -257,14 +356,18 @@ __device__ __forceinline__ float warp_sum(float x) {
   return x;
 }
 
-// One warp per row: softmax over the row's teacher logits, entries ordered by column (by counting the smaller ones).
-__global__ void k_soft_targets(Header* hdr, Entries en, const void* ids, int64_t ids_ld, int ids_bytes, const void* logits,
-                               int64_t logits_ld, int type, float inv_tau, int64_t T, int64_t V) {
-  extern __shared__ int sh_col[];
-  const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, K = en.k;
+// One warp per row: softmax over the row's teacher logits; entries ordered by column (by counting the smaller ones),
+// equal ids joined into one.
+__global__ void k_soft_targets(int* column, float* q_out, float* const_term, const void* ids, int64_t ids_ld, int ids_bytes,
+                               const void* logits, int64_t logits_ld, int type, int K, float inv_tau, int64_t T, int64_t V) {
+  extern __shared__ int sh[];
+  iwp_tc::launch_next();
+  iwp_tc::wait_previous();
+  const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t t = blockIdx.x * int64_t(warps) + warp;
   if (t >= T) return;
-  int* col = sh_col + warp * K;
+  int* col = sh + warp * 2 * K;
+  float* q = reinterpret_cast<float*>(col + K);
   float top = -CUDART_INF_F;
   bool bad = false, nan = false;
   for (int k = lane; k < K; k += 32) {
@@ -273,6 +376,7 @@ __global__ void k_soft_targets(Header* hdr, Entries en, const void* ids, int64_t
     bad |= id >= V;
     const bool used = id >= 0 && id < V && x != -CUDART_INF_F;  // NaN takes part
     col[k] = used ? static_cast<int>(id) : NO_COLUMN;
+    q[k] = x;
     if (used) {
       nan |= x != x;
       top = fmaxf(top, x);
@@ -284,123 +388,242 @@ __global__ void k_soft_targets(Header* hdr, Entries en, const void* ids, int64_t
   __syncwarp();
   float sum = 0.f;
   for (int k = lane; k < K; k += 32)
-    if (col[k] != NO_COLUMN) sum += expf(iwp_tc::load_as_float(logits, t * logits_ld + k, type) * inv_tau - top);
+    if (col[k] != NO_COLUMN) sum += expf(q[k] - top);
   sum = warp_sum(sum);
   const bool has = top != -CUDART_INF_F || nan;
   const float log_sum = logf(sum);
   float term = 0.f;
   for (int k = lane; k < K; k += 32) {
-    const int c = col[k];
-    int rank = 0;
-    for (int j = 0; j < K; j++) rank += col[j] < c || (col[j] == c && j < k);
-    float q = 0.f;
-    if (c != NO_COLUMN) {
-      const float lq = iwp_tc::load_as_float(logits, t * logits_ld + k, type) * inv_tau - top - log_sum;
-      q = expf(lq);
-      if (q != 0.f) term += q * lq;
+    float p = 0.f;
+    if (col[k] != NO_COLUMN) {
+      const float lq = q[k] - top - log_sum;
+      p = expf(lq);
+      if (p != 0.f) term += p * lq;
     }
-    en.column[rank * T + t] = bad ? NO_COLUMN : c;
-    en.q[rank * T + t] = q;
+    q[k] = p;
   }
   term = warp_sum(term);
-  if (lane == 0) {
-    en.const_term[t] = bad ? CUDART_NAN_F : has ? term : 0.f;
-    en.row_scale[t] = has && !bad ? 1.f : 0.f;
-    if (bad) atomicExch(&hdr->status, IWP_ERR_INVALID);
-    if (has || bad) atomicAdd(&hdr->n_rows, 1);
+  __syncwarp();
+  for (int k = lane; k < K; k += 32) {
+    const int c = col[k];
+    int rank = 0, before = 0;
+    float p = 0.f;
+    for (int j = 0; j < K; j++) {
+      const int o = col[j];
+      rank += o < c || (o == c && j < k);
+      before += o == c && j < k;
+      if (o == c) p += q[j];
+    }
+    // of equal ids the first carries the sum, the others stay in place with nothing: the order is kept
+    const bool drop = c == NO_COLUMN;
+    column[t * K + rank] = bad || drop ? NO_COLUMN : c;
+    q_out[t * K + rank] = drop || before ? 0.f : p;
   }
+  if (lane == 0) const_term[t] = bad ? CUDART_NAN_F : has ? term : 0.f;
 }
 
 // ---- per-row upstream gradients: their largest magnitude, and the rows relative to it ------------------------
 
-__global__ void k_row_scales(Header* hdr, float* row_scale, const float* dloss_rows, int64_t T) {
+__global__ void __launch_bounds__(1024) k_row_scales(Header* hdr, Targets en, float* scale, const float* dloss_rows, int64_t T) {
   __shared__ float sh[32];
+  iwp_tc::launch_next();
+  iwp_tc::wait_previous();
   float m = 0.f;
   for (int64_t t = threadIdx.x; t < T; t += blockDim.x)
-    if (row_scale[t] != 0.f) m = fmaxf(m, fabsf(dloss_rows[t]));
+    if (en.state(t) == 1) m = fmaxf(m, fabsf(dloss_rows[t]));
   m = warp_max(m);
   if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = m;
   __syncthreads();
-  m = warp_max((threadIdx.x & 31) < (blockDim.x >> 5) ? sh[threadIdx.x & 31] : 0.f);
+  m = warp_max(sh[threadIdx.x & 31]);
   if (threadIdx.x == 0) hdr->gmax = m;
-  for (int64_t t = threadIdx.x; t < T; t += blockDim.x)
-    if (row_scale[t] != 0.f) row_scale[t] = m > 0.f ? dloss_rows[t] / m : dloss_rows[t];
+  for (int64_t t = threadIdx.x; t < T; t += blockDim.x) scale[t] = m > 0.f ? dloss_rows[t] / m : dloss_rows[t];
+}
+
+// Number of rows with targets, for backward passes on their own (k_finish counts them otherwise).
+__global__ void __launch_bounds__(1024) k_count_rows(Header* hdr, Targets en, int64_t T) {
+  __shared__ int sh[32];
+  iwp_tc::launch_next();
+  iwp_tc::wait_previous();
+  int n = 0;
+  for (int64_t t = threadIdx.x; t < T; t += blockDim.x) n += en.state(t) != 0;
+  n = __reduce_add_sync(0xFFFFFFFFu, n);
+  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = n;
+  __syncthreads();
+  n = __reduce_add_sync(0xFFFFFFFFu, sh[threadIdx.x & 31]);
+  if (threadIdx.x == 0) hdr->n_rows = n;
 }
 
 // ---- finish of the forward pass --------------------------------------------------------------------------
 
-// Blocks of 32 warps take 32 rows (lane = row): each warp joins every 32nd part, the first warp joins the warps.
-// The last block to finish adds the blocks' sums in order.
-__global__ void __launch_bounds__(1024) k_finish(Header* hdr, Entries en, const float2* part, int parts, const float* z_at, float tau,
-                                                 int64_t T, float* rows, float* lse, float* loss, int mean, float* block_sum) {
-  __shared__ float2 sh[32][33];
+struct Finish {
+  Header* hdr;
+  Targets en;
+  const float2* part;
+  const float* z_at;
+  float* rows;  // the caller's, or scratch
+  float* lse;
+  float* loss;
+  uint16_t* codes;  // codes -> factors, in place; NULL: losses only
+  int64_t T, ld;
+  int parts, part_shift, v0, width, chunk;  // a block takes `chunk` columns of one row
+  int chunks, mean, type;
+  float tau, up;
+  int log_codes;
+};
+
+constexpr int FINISH_THREADS = 256;
+
+__device__ __forceinline__ float2 join(float2 a, float2 b) {  // (maximum, sum of 2^(x - maximum))
+  const float m = fmaxf(a.x, b.x), ref = m == -CUDART_INF_F ? 0.f : m;
+  return make_float2(m, a.y * ex2(a.x - ref) + b.y * ex2(b.x - ref));
+}
+
+// A block joins the parts of its row (in a fixed order), and turns one chunk of the row's codes into factors.  The
+// first chunk's block writes lse and loss; the last block to finish adds the rows' losses in a fixed order.
+__global__ void __launch_bounds__(FINISH_THREADS, 4) k_finish(const Finish a) {
+  constexpr int DEEP = 4, BATCH = DEEP * 8 * FINISH_THREADS;  // columns a block has in flight
+  constexpr int WARPS = FINISH_THREADS / 32, MINE = (MAX_TOP + FINISH_THREADS - 1) / FINISH_THREADS;
+  __shared__ float2 sh[WARPS];
+  __shared__ float sh_sum[WARPS];
+  __shared__ int sh_n[WARPS];
   __shared__ bool last;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t row = blockIdx.x * 32ll + lane;
-  float m = -CUDART_INF_F, s = 0.f;
-  if (row < T) {
-#pragma unroll 4
-    for (int p = warp; p < parts; p += 32) {
-      const float2 x = part[p * T + row];
-      const float mn = fmaxf(m, x.x), ref = mn == -CUDART_INF_F ? 0.f : mn;
-      s = s * exp2f(m - ref) + x.y * exp2f(x.x - ref);
-      m = mn;
-    }
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  iwp_tc::launch_next();
+  iwp_tc::wait_previous();
+  const int64_t row = blockIdx.x / a.chunks;
+  const int chunk = static_cast<int>(blockIdx.x - row * a.chunks);
+  const float2* const part = a.part + row * a.parts;
+  // the first columns are fetched while the row's statistics are joined
+  uint16_t* const codes = a.codes + row * a.ld;
+  const int c0 = chunk * a.chunk, c1 = min(c0 + a.chunk, a.width);  // within the piece
+  uint4 ahead[DEEP];
+#pragma unroll
+  for (int i = 0; i < DEEP; i++) {
+    const int o = c0 + 8 * tid + i * 8 * FINISH_THREADS;
+    if (o < c1) ahead[i] = *reinterpret_cast<const uint4*>(codes + o);
   }
-  sh[warp][lane] = make_float2(m, s);
+  float2 x = make_float2(-CUDART_INF_F, 0.f);
+  for (int p = tid; p < a.parts; p += FINISH_THREADS) x = join(x, part[p]);
+#pragma unroll
+  for (int o = 16; o; o >>= 1) x = join(x, make_float2(__shfl_xor_sync(0xFFFFFFFFu, x.x, o), __shfl_xor_sync(0xFFFFFFFFu, x.y, o)));
+  if (lane == 0) sh[warp] = x;
   __syncthreads();
-  if (warp == 0) {
-    float r = 0.f;
-    if (row < T) {
-      for (int w = 1; w < 32; w++) {
-        const float2 x = sh[w][lane];
-        const float mn = fmaxf(m, x.x), ref = mn == -CUDART_INF_F ? 0.f : mn;
-        s = s * exp2f(m - ref) + x.y * exp2f(x.x - ref);
-        m = mn;
+  x = sh[0];
+#pragma unroll
+  for (int w = 1; w < WARPS; w++) x = join(x, sh[w]);
+  const float lse2 = x.x + log2f(x.y), lse = lse2 * LN2;
+  const int state = a.en.state(row);
+  if (chunk == 0) {
+    // q (lse - z / tau) entry by entry, so that a confident row keeps its small loss
+    float below = 0.f;
+    if (state == 1)
+      for (int k = tid; k < a.en.k; k += FINISH_THREADS) {
+        if (a.en.column_at(row, k) == NO_COLUMN) continue;
+        const float q = a.en.q_at(row, k);
+        if (q != 0.f) below += q * (lse - a.z_at[row * a.en.k + k] / a.tau);
       }
-      const float l = (m + log2f(s)) * LN2;
-      lse[row] = l;
-      if (rows || loss) {
-        // sum of q (z / tau) in units of the row's lse, so that a confident row keeps its small loss
-        const float c = en.const_term[row];
-        float below = 0.f;
-        if (en.row_scale[row] != 0.f || c != 0.f) {
-          for (int k = 0; k < en.k; k++) {
-            if (en.column[k * T + row] == NO_COLUMN) break;
-            const float q = en.q[k * T + row];
-            if (q != 0.f) below += q * (l - z_at[k * T + row] / tau);
-          }
-          r = tau * tau * (c + below);
-        }
-        if (rows) rows[row] = r;
-      }
-    }
-    r = warp_sum(r);
-    if (lane == 0) {
-      block_sum[blockIdx.x] = r;
-      __threadfence();
-      last = atomicAdd(&hdr->ticket, 1u) == gridDim.x - 1;
-    }
-  }
-  __syncthreads();
-  if (last && loss) {
-    __threadfence();
-    float x = 0.f;
-    for (int b = threadIdx.x; b < static_cast<int>(gridDim.x); b += 1024) x += __ldcg(block_sum + b);
-    x = warp_sum(x);
-    __shared__ float sums[32];
-    if (lane == 0) sums[warp] = x;
+    below = warp_sum(below);
+    if (lane == 0) sh_sum[warp] = below;
     __syncthreads();
-    if (warp == 0) {
-      x = warp_sum(sums[lane]);
-      const int n = hdr->n_rows;
-      if (lane == 0) *loss = n == 0 ? 0.f : mean ? x / static_cast<float>(n) : x;
+    if (tid == 0) {
+      below = 0.f;
+      for (int w = 0; w < WARPS; w++) below += sh_sum[w];
+      const float c = a.en.hard ? 0.f : a.en.const_term[row];
+      a.lse[row] = lse;
+      a.rows[row] = state == 0 ? 0.f : state < 0 ? CUDART_NAN_F : a.tau * a.tau * (c + below);
+      if (state < 0) atomicExch(&a.hdr->status, IWP_ERR_INVALID);
     }
+  }
+  if (a.codes) {
+    const float scale = a.en.row_scale(row) * a.up;
+    auto probability = [&](int col, uint32_t code) {  // m = the part's maximum less lse2, in log2
+      const float m = part[(a.v0 + col) >> a.part_shift].x - lse2;
+      return a.log_codes ? ex2(m + log_value(code)) : __half2float(__ushort_as_half(static_cast<uint16_t>(code))) * ex2(m - 15.f);
+    };
+    int at[MINE];
+    float to[MINE];
+#pragma unroll
+    for (int i = 0; i < MINE; i++) {
+      const int k = tid + i * FINISH_THREADS;
+      at[i] = -1;
+      if (k < a.en.k && scale != 0.f) {
+        const int col = a.en.column_at(row, k);
+        const float q = a.en.q_at(row, k);
+        if (col != NO_COLUMN && q != 0.f && col >= a.v0 + c0 && col < a.v0 + c1) {
+          at[i] = col - a.v0;
+          to[i] = (probability(at[i], codes[at[i]]) - q) * scale;
+        }
+      }
+    }
+    __syncthreads();
+    for (int c = c0 + 8 * tid; c < c1; c += BATCH) {
+      uint4 u[DEEP];
+      float m[DEEP];
+#pragma unroll
+      for (int i = 0; i < DEEP; i++) {
+        const int o = c + i * 8 * FINISH_THREADS;
+        if (o < c1) {
+          u[i] = c == c0 + 8 * tid ? ahead[i] : *reinterpret_cast<const uint4*>(codes + o);
+          m[i] = part[(a.v0 + o) >> a.part_shift].x - lse2;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < DEEP; i++) {
+        const int o = c + i * 8 * FINISH_THREADS;
+        if (o >= c1) break;
+        uint32_t* const e = reinterpret_cast<uint32_t*>(&u[i]);
+        if (scale == 0.f) {  // a row that gives nothing, whatever its logits are
+          u[i] = make_uint4(0u, 0u, 0u, 0u);
+        } else if (a.log_codes) {
+#pragma unroll
+          for (int j = 0; j < 4; j++)
+            e[j] = iwp_tc::pack2(ex2(m[i] + log_value(e[j] & 0xFFFFu)) * scale, ex2(m[i] + log_value(e[j] >> 16)) * scale, IWP_F16);
+        } else {
+          const float f = ex2(m[i] - 15.f) * scale;
+#pragma unroll
+          for (int j = 0; j < 4; j++) {
+            const float2 x = iwp_tc::unpack2(e[j], IWP_F16);
+            e[j] = iwp_tc::pack2(x.x * f, x.y * f, IWP_BF16);
+          }
+        }
+        *reinterpret_cast<uint4*>(codes + o) = u[i];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < MINE; i++)
+      if (at[i] >= 0) iwp_tc::store_as(codes, at[i], to[i], a.type);
+  }
+  __syncthreads();
+  if (tid == 0) {
+    __threadfence();
+    last = atomicInc(&a.hdr->ticket, gridDim.x - 1) == gridDim.x - 1;
+  }
+  __syncthreads();
+  if (!last) return;
+  __threadfence();
+  float sum = 0.f;
+  int n = 0;
+  for (int64_t t = tid; t < a.T; t += FINISH_THREADS) {
+    sum += __ldcg(a.rows + t);
+    n += a.en.state(t) != 0;
+  }
+  sum = warp_sum(sum);
+  n = __reduce_add_sync(0xFFFFFFFFu, n);
+  if (lane == 0) sh_sum[warp] = sum, sh_n[warp] = n;
+  __syncthreads();
+  if (tid == 0) {
+    sum = 0.f, n = 0;
+    for (int w = 0; w < WARPS; w++) sum += sh_sum[w], n += sh_n[w];
+    a.hdr->n_rows = n;
+    if (a.loss) *a.loss = n == 0 ? 0.f : a.mean ? sum / static_cast<float>(n) : sum;
   }
 }
 
 // Rows of `cols` 16-bit elements to rows of `ld_to` (a multiple of 8), for operands TMA cannot address.
 __global__ void k_align_rows(const uint16_t* from, int64_t ld_from, uint16_t* to, int64_t ld_to, int64_t rows, int cols) {
+  iwp_tc::launch_next();
+  iwp_tc::wait_previous();
   for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
     for (int c = threadIdx.x; c < cols; c += blockDim.x) to[r * ld_to + c] = from[r * ld_from + c];
 }

@@ -1,13 +1,12 @@
 // iwp_loss.cu - C entries of the losses (include/iwp_loss.h): argument checks, workspace layout, launches.
 #include <cmath>
 #include <cstring>
+#include <utility>
 
 #include "iwp_balance.cuh"
 #include "iwp_head.cuh"
 
 namespace {
-
-using iwp_tc::Work;
 
 #define LOSS_CUDA(expr)            \
   do {                             \
@@ -18,18 +17,13 @@ using iwp_tc::Work;
   } while (0)
 
 constexpr int64_t MAX_SIZE = 0x7FFFFFFF;
-constexpr int64_t DEFAULT_PIECE = int64_t(512) << 20;
+constexpr int64_t DEFAULT_PIECE = int64_t(1) << 30;
+constexpr int FEW_TILES = 296;           // four per CTA pair: above this a product takes its widest tiles
 constexpr int64_t JOIN_TILES = 2 * 148;  // a split dhidden has at most this many partial tiles
 
 inline int64_t up_to(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 inline int64_t tiles_of(int64_t x, int64_t t) { return (x + t - 1) / t; }
 inline bool aligned(const void* p, int64_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
-int sm_count() {
-  int dev = 0, n = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
-  return n;
-}
 
 // cuTensorMapEncodeTiled through the runtime, so that the library links against no driver stub.
 using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -61,21 +55,47 @@ bool make_map(CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int64
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// How many clusters of CG CTAs of this kernel the device holds at once: the persistent grid (a cluster that had to wait
-// for another to end would double the time).  Looked up once per device.
-template <class Kernel>
-int resident_clusters(Kernel kernel, int cg, int smem, int* cached) {
+constexpr int MAX_DEVICES = 64;
+
+int device() {
   int dev = -1;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
-  if (cached[dev]) return cached[dev];
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return 0;
+  return cudaGetDevice(&dev) == cudaSuccess && dev < MAX_DEVICES ? dev : -1;
+}
+
+// Launches with programmatic serialisation: the kernel may start while the one before it drains.
+template <class... Params, class... Args>
+cudaError_t launch(void (*kernel)(Params...), int64_t grid, int block, size_t smem, int cluster, cudaStream_t st, Args&&... args) {
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(static_cast<unsigned>(cg));
-  cfg.blockDim = dim3(iwp_tc::THREADS);
+  cfg.gridDim = dim3(static_cast<unsigned>(grid));
+  cfg.blockDim = dim3(static_cast<unsigned>(block));
   cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = static_cast<unsigned>(cluster);
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
+}
+
+// How many CTA pairs of a product kernel the device holds at once: the persistent grid (a pair that had to wait for
+// another to end would double the time).  Looked up once per device, with the kernel's shared memory limit.
+template <class Kernel>
+int resident_pairs(Kernel kernel, int* cached) {
+  const int dev = device();
+  if (dev < 0) return 0;
+  if (cached[dev]) return cached[dev];
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, iwp_tc::SMEM) != cudaSuccess) return 0;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(iwp_tc::CG);
+  cfg.blockDim = dim3(iwp_tc::THREADS);
+  cfg.dynamicSmemBytes = iwp_tc::SMEM;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = cg;
+  at[0].val.clusterDim.x = iwp_tc::CG;
   at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
@@ -89,46 +109,103 @@ struct Matrix {
   int64_t rows, cols, ld;
 };
 
-// C[M, N] = A B^T with M, N, K taken from the operands: a K-contiguous operand is [M or N][K], the other [K][M or N].
-template <int CG, bool A_KC, bool B_KC, class Epi>
-int launch_product(const Matrix& A, const Matrix& B, int dtype, int splits, const typename Epi::Args& args, int* status,
-                   cudaStream_t st) {
-  using S = iwp_tc::Shape<CG>;
-  CUtensorMap ma, mb;
-  if (!make_map(&ma, A.p, A.rows, A.cols, A.ld, A_KC ? iwp_tc::TILE_M : iwp_tc::BLOCK_K, dtype) ||
-      !make_map(&mb, B.p, B.rows, B.cols, B.ld, B_KC ? S::B_ROWS : iwp_tc::BLOCK_K, dtype))
-    return IWP_ERR_CUDA;
-  const int64_t M = A_KC ? A.rows : A.cols, N = B_KC ? B.rows : B.cols, K = A_KC ? A.cols : A.rows;
-  Work w;
-  w.m_tiles = static_cast<int>(tiles_of(M, iwp_tc::TILE_M * CG));
-  w.n_tiles = static_cast<int>(tiles_of(N, iwp_tc::TILE_N));
-  w.k_blocks = static_cast<int>(tiles_of(K, iwp_tc::BLOCK_K));
-  w.splits = splits;
-  // f32 accumulator; operand types; which operands are M/N-contiguous; N / 8; M / 16
-  w.idesc = (1u << 4) | ((dtype == IWP_BF16 ? 1u : 0u) << 7) | ((dtype == IWP_BF16 ? 1u : 0u) << 10) | ((A_KC ? 0u : 1u) << 15) |
-            ((B_KC ? 0u : 1u) << 16) | ((iwp_tc::TILE_N / 8u) << 17) | ((iwp_tc::TILE_M * CG / 16u) << 24);
-  w.status = status;
-  const int64_t total = int64_t(w.m_tiles) * w.n_tiles * splits;
-  if (total > MAX_SIZE) return IWP_ERR_INVALID;
-  auto kernel = iwp_tc::k_product<CG, A_KC, B_KC, Epi>;
-  static int resident[64] = {};
-  const int clusters = resident_clusters(kernel, CG, S::SMEM, resident);
-  if (clusters < 1) {
-    cudaGetLastError();
-    return IWP_ERR_CUDA;
+struct Shape {
+  int64_t m, n, k;
+  int64_t m_tiles() const { return tiles_of(m, iwp_tc::CG * iwp_tc::TILE_M); }
+  int64_t k_blocks() const { return tiles_of(k, iwp_tc::BLOCK_K); }
+  int64_t tiles(int n_cols) const { return m_tiles() * tiles_of(n, n_cols); }
+  // clocks of a tile with its K in `splits` parts, about: per block of K the products or the loads, whichever takes
+  // longer (32, 28, 24 or 20 KB per CTA), but no less than an epilogue
+  double clocks(int n_cols, int splits) const {
+    const double block = n_cols == 256 ? 520 : n_cols == 192 ? 450 : n_cols == 128 ? 385 : 320;
+    const double products = static_cast<double>(tiles_of(k_blocks(), splits)) * block, epilogue = 1000 + 12.0 * n_cols;
+    return (products > epilogue ? products : epilogue) + 300;
   }
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(static_cast<unsigned>(CG * (total < clusters ? total : clusters)));
-  cfg.blockDim = dim3(iwp_tc::THREADS);
-  cfg.dynamicSmemBytes = S::SMEM;
-  cfg.stream = st;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = CG;
-  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  LOSS_CUDA(cudaLaunchKernelEx(&cfg, kernel, ma, mb, w, args));
+};
+
+// Width of a single product's tiles: 256 where there are tiles enough for all pairs, less where the narrower tiles'
+// shorter time wins over their poorer use of the loads.
+int pick_tile_n(const Shape& s, int pairs) {
+  if (s.tiles(256) > FEW_TILES) return 256;
+  int best = 256;
+  double least = 0;
+  for (int n : {256, 128, 64}) {
+    const double time = static_cast<double>(tiles_of(s.tiles(n), pairs)) * s.clocks(n, 1);
+    if (n == 256 || time < 0.95 * least) best = n, least = time;
+  }
+  return best;
+}
+
+// Plan of the two gradient products of a piece in one launch: the width of the tiles, the number of parts of dhidden's
+// K (the vocabulary), and how its tiles and dweight's are dealt to the pairs (Problems).
+struct Deal {
+  int tile_n, splits, rounds, rest, fill;
+};
+
+Deal deal_gradients(const Shape* dh, const Shape* dw, int pairs, int fixed_splits) {
+  Deal best{256, 1, 0, 0, 0};
+  double least = -1;
+  for (int n : {256, 192, 128, 64}) {
+    const int64_t one = dh ? dh->tiles(n) : 0, w = dw ? dw->tiles(n) : 0;
+    if (n < 192 && one + w > FEW_TILES) break;
+    int64_t most = dh ? dh->k_blocks() / 4 : 1;
+    if (dh && most > JOIN_TILES / one) most = JOIN_TILES / one;
+    if (most < 1) most = 1;
+    for (int64_t s = fixed_splits ? fixed_splits : 1; s <= (fixed_splits ? fixed_splits : most); s++) {
+      const double ch = dh ? dh->clocks(n, static_cast<int>(s)) : 0, cw = dw ? dw->clocks(n, 1) : 1;
+      const int64_t tiles = one * s;
+      Deal d{n, static_cast<int>(s), static_cast<int>(tiles / pairs), static_cast<int>(tiles % pairs), 0};
+      double time = d.rounds * ch;
+      int64_t left = w;
+      if (d.rest) {
+        int64_t fill = static_cast<int64_t>(ch / cw);
+        if (fill > w / (pairs - d.rest)) fill = w / (pairs - d.rest);
+        d.fill = static_cast<int>(fill);
+        left -= fill * (pairs - d.rest);
+        time += ch;
+      }
+      time += static_cast<double>(tiles_of(left, pairs)) * cw;
+      // parts are joined by a launch of its own: its start, and each part written and read once at about 2500 bytes per clock
+      if (s > 1) time += 5000 + static_cast<double>(dh->m) * static_cast<double>(dh->n) * 8 * static_cast<double>(s) / 2500;
+      if (least < 0 || time < least) least = time, best = d;
+    }
+  }
+  return best;
+}
+
+// C[M, N] = A B^T: a K-contiguous operand is [M or N][K], the other [K][M or N].
+bool make_problem(iwp_tc::Problem* q, const Matrix& A, bool a_kc, const Matrix& B, bool b_kc, int dtype, int tile_n, int splits) {
+  const Shape s{a_kc ? A.rows : A.cols, b_kc ? B.rows : B.cols, a_kc ? A.cols : A.rows};
+  if (!make_map(&q->a, A.p, A.rows, A.cols, A.ld, a_kc ? iwp_tc::TILE_M : iwp_tc::BLOCK_K, dtype) ||
+      !make_map(&q->b, B.p, B.rows, B.cols, B.ld, b_kc ? tile_n / iwp_tc::CG : iwp_tc::BLOCK_K, dtype))
+    return false;
+  q->m_tiles = static_cast<int>(s.m_tiles());
+  q->n_tiles = static_cast<int>(tiles_of(s.n, tile_n));
+  q->tile_n = tile_n;
+  q->k_blocks = static_cast<int>(s.k_blocks());
+  q->splits = splits;
+  // f32 accumulator; operand types; which operands are M/N-contiguous; N / 8; M / 16
+  const uint32_t type = dtype == IWP_BF16 ? 1u : 0u;
+  q->idesc = (1u << 4) | (type << 7) | (type << 10) | ((a_kc ? 0u : 1u) << 15) | ((b_kc ? 0u : 1u) << 16) |
+             (static_cast<uint32_t>(tile_n / 8) << 17) | ((iwp_tc::TILE_M * iwp_tc::CG / 16u) << 24);
+  q->a_kc = a_kc;
+  q->b_kc = b_kc;
+  return true;
+}
+
+template <class Epi, int N>
+int pairs_of() {
+  static int cached[MAX_DEVICES] = {};
+  return resident_pairs(iwp_tc::k_product<N, Epi>, cached);
+}
+
+template <class Epi, int N>
+int launch_product(const iwp_tc::Problems<N>& w, const typename Epi::Args& args, cudaStream_t st) {
+  const int pairs = pairs_of<Epi, N>();
+  int64_t total = 0;
+  for (const auto& q : w.p) total += int64_t(q.m_tiles) * q.n_tiles * q.splits;
+  if (total > MAX_SIZE) return IWP_ERR_INVALID;
+  LOSS_CUDA(launch(iwp_tc::k_product<N, Epi>, iwp_tc::CG * (total < pairs ? total : pairs), iwp_tc::THREADS, iwp_tc::SMEM, iwp_tc::CG, st, w, args));
   return IWP_OK;
 }
 
@@ -136,11 +213,9 @@ int launch_product(const Matrix& A, const Matrix& B, int dtype, int splits, cons
 
 struct HeadPlan {
   bool grad, pack_hidden, pack_weight;
-  int64_t k, parts, piece, p_ld, pieces;
-  int splits;
-  int64_t d_pad;
+  int64_t k, piece, pieces, d_pad;
   // offsets into the workspace
-  int64_t column, q, const_term, row_scale, z_at, block_sum, hidden, weight, big, join, bytes;
+  int64_t column, q, const_term, row_scale, rows, z_at, part, hidden, weight, probs, join, bytes;
 };
 
 bool needs_copy(const void* p, int64_t ld) { return !aligned(p, 16) || ld % 8 != 0; }
@@ -160,7 +235,6 @@ HeadPlan head_plan(const iwp_head_args* a) {
   const int64_t T = a->tokens, V = a->vocab, D = a->dim;
   p.grad = a->dhidden || a->dweight;
   p.k = a->targets ? 1 : a->top_k;
-  p.parts = 2 * tiles_of(V, iwp_tc::TILE_N);
   p.d_pad = up_to(D, 8);
   p.pack_hidden = needs_copy(a->hidden, a->hidden_ld);
   p.pack_weight = needs_copy(a->weight, a->weight_ld);
@@ -170,16 +244,22 @@ HeadPlan head_plan(const iwp_head_args* a) {
     at += up_to(n, 256);
     return o;
   };
-  p.column = take(4 * p.k * T);
-  p.q = take(4 * p.k * T);
-  p.const_term = take(4 * T);
+  if (!a->targets) {
+    p.column = take(4 * p.k * T);
+    p.q = take(4 * p.k * T);
+    p.const_term = take(4 * T);
+  }
   p.row_scale = take(4 * T);
-  p.z_at = take(4 * p.k * T);
-  p.block_sum = take(4 * tiles_of(T, 32));
+  p.rows = take(4 * T);
+  if (!a->have_lse) {
+    p.z_at = take(4 * p.k * T);
+    // a part is half a tile of at least 64 columns; narrow tiles are taken where those of 256 columns would be few
+    // (FEW_TILES), i.e. at most 8 parts of 8 bytes for each of a tile's 256 rows
+    const int64_t wide = 8 * T * 2 * tiles_of(V, 256), narrow = 8 * T * 2 * tiles_of(V, 64), most = int64_t(FEW_TILES) * 256 * 64;
+    p.part = take(wide > most ? wide : narrow < most ? narrow : most);
+  }
   if (p.pack_hidden) p.hidden = take(2 * T * p.d_pad);
   if (p.pack_weight) p.weight = take(2 * V * p.d_pad);
-  // one region for the partial statistics of the logits pass and, afterwards, the probabilities of a piece
-  int64_t big = a->have_lse ? 0 : 8 * p.parts * T;
   if (p.grad) {
     const int64_t limit = a->piece_bytes ? a->piece_bytes : DEFAULT_PIECE;
     const int64_t v_pad = up_to(V, iwp_tc::TILE_N), t = T > 0 ? T : 1;
@@ -188,19 +268,12 @@ HeadPlan head_plan(const iwp_head_args* a) {
     if (width > v_pad) width = v_pad;
     p.pieces = tiles_of(v_pad, width);
     p.piece = up_to(tiles_of(v_pad, p.pieces), iwp_tc::TILE_N);
-    p.p_ld = p.piece;
+    p.pieces = tiles_of(v_pad, p.piece);
     const int64_t most = 2 * t * v_pad < limit ? 2 * t * v_pad : limit, least = 2 * t * iwp_tc::TILE_N;
-    const int64_t bound = most > least ? most : least;
-    if (bound > big) big = bound;
-    // dhidden: few tiles and a long K are split, so that every SM pair has one; more than one piece is summed in fp32
-    const int64_t tiles = tiles_of(t, 2 * iwp_tc::TILE_M) * tiles_of(D, iwp_tc::TILE_N), k_blocks = tiles_of(p.piece, iwp_tc::BLOCK_K);
-    int64_t s = 74 / tiles;
-    if (s > k_blocks / 8) s = k_blocks / 8;
-    p.splits = s < 1 ? 1 : static_cast<int>(s);
+    p.probs = take(most > least ? most : least);
   }
-  p.big = take(big);
   if (a->dhidden) {
-    const int64_t one = 4 * T * D, split = JOIN_TILES * 4 * 2 * iwp_tc::TILE_M * iwp_tc::TILE_N;
+    const int64_t one = 4 * T * D, split = JOIN_TILES * 4 * iwp_tc::CG * iwp_tc::TILE_M * iwp_tc::TILE_N;
     p.join = take(one > split ? one : split);
   }
   p.bytes = at;
@@ -212,9 +285,13 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
   const int64_t T = a->tokens, V = a->vocab, D = a->dim;
   char* const ws = static_cast<char*>(a->workspace);
   auto* hdr = reinterpret_cast<H::Header*>(ws);
-  const int sms = sm_count();
-  if (sms < 2) return IWP_ERR_CUDA;
-  const float tau = a->targets ? 1.f : a->temperature;
+  const int pairs = pairs_of<H::Logits, 1>();
+  if (pairs < 1 || pairs_of<H::Probs, 1>() < 1 || pairs_of<H::Out, 2>() < 1) {
+    cudaGetLastError();
+    return IWP_ERR_CUDA;
+  }
+  const int sms = 2 * pairs;
+  const float tau = a->targets ? 1.f : a->temperature, c = H::LOG2E / tau;
   if (T == 0) {
     if (a->loss && !a->have_lse) LOSS_CUDA(cudaMemsetAsync(a->loss, 0, 4, st));
     if (a->dweight && !a->accumulate) {
@@ -223,118 +300,182 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
     }
     return IWP_OK;
   }
-  LOSS_CUDA(cudaMemsetAsync(ws + 4, 0, 12, st));  // counters; the status word stays
-  H::Entries en;
-  en.column = reinterpret_cast<int*>(ws + p.column);
-  en.q = reinterpret_cast<float*>(ws + p.q);
-  en.const_term = reinterpret_cast<float*>(ws + p.const_term);
-  en.row_scale = reinterpret_cast<float*>(ws + p.row_scale);
+  H::Targets en{};
+  en.hard = a->targets;
+  en.ignore = a->ignore_index;
+  en.V = static_cast<int>(V);
   en.k = static_cast<int>(p.k);
-  if (a->targets) {
-    H::k_hard_targets<<<static_cast<unsigned>(tiles_of(T, 256)), 256, 0, st>>>(hdr, en, a->targets, a->ignore_index, T, V);
-  } else {
-    H::k_soft_targets<<<static_cast<unsigned>(tiles_of(T, 4)), 128, 4 * 4 * p.k, st>>>(hdr, en, a->top_ids, a->top_ids_ld, a->ids_bytes,
-                                                                                   a->top_logits, a->top_logits_ld, a->top_type, 1.f / tau, T, V);
+  if (!a->targets) {
+    int* const column = reinterpret_cast<int*>(ws + p.column);
+    float* const q = reinterpret_cast<float*>(ws + p.q);
+    float* const term = reinterpret_cast<float*>(ws + p.const_term);
+    LOSS_CUDA(launch(H::k_soft_targets, tiles_of(T, 4), 128, 4 * 8 * p.k, 1, st, column, q, term, a->top_ids, a->top_ids_ld, a->ids_bytes,
+                     a->top_logits, a->top_logits_ld, a->top_type, en.k, 1.f / tau, T, V));
+    en.column = column;
+    en.q = q;
+    en.const_term = term;
   }
-  LOSS_CUDA(cudaGetLastError());
   if (p.grad && a->dloss_rows) {
-    H::k_row_scales<<<1, 1024, 0, st>>>(hdr, en.row_scale, a->dloss_rows, T);
-    LOSS_CUDA(cudaGetLastError());
+    float* const scale = reinterpret_cast<float*>(ws + p.row_scale);
+    LOSS_CUDA(launch(H::k_row_scales, 1, 1024, 0, 1, st, hdr, en, scale, a->dloss_rows, T));
+    en.scale = scale;
   }
+  if (a->have_lse) LOSS_CUDA(launch(H::k_count_rows, 1, 1024, 0, 1, st, hdr, en, T));
   Matrix h{a->hidden, T, D, a->hidden_ld}, w{a->weight, V, D, a->weight_ld};
-  if (p.pack_hidden) {
-    H::k_align_rows<<<static_cast<unsigned>(T < 8 * sms ? T : 8 * sms), 256, 0, st>>>(static_cast<const uint16_t*>(a->hidden), a->hidden_ld,
-                                                                                  reinterpret_cast<uint16_t*>(ws + p.hidden), p.d_pad, T, static_cast<int>(D));
-    h.p = ws + p.hidden, h.ld = p.d_pad;
-  }
-  if (p.pack_weight) {
-    H::k_align_rows<<<static_cast<unsigned>(V < 8 * sms ? V : 8 * sms), 256, 0, st>>>(static_cast<const uint16_t*>(a->weight), a->weight_ld,
-                                                                                  reinterpret_cast<uint16_t*>(ws + p.weight), p.d_pad, V, static_cast<int>(D));
-    w.p = ws + p.weight, w.ld = p.d_pad;
-  }
-  LOSS_CUDA(cudaGetLastError());
-  const float c = H::LOG2E / tau;
+  auto align_rows = [&](Matrix& m, int64_t at) {
+    const int64_t blocks = m.rows < 8 * sms ? m.rows : 8 * sms;
+    const cudaError_t e = launch(H::k_align_rows, blocks, 256, 0, 1, st, static_cast<const uint16_t*>(m.p), m.ld, reinterpret_cast<uint16_t*>(ws + at),
+                                 p.d_pad, m.rows, static_cast<int>(D));
+    m.p = ws + at, m.ld = p.d_pad;
+    return e;
+  };
+  if (p.pack_hidden) LOSS_CUDA(align_rows(h, p.hidden));
+  if (p.pack_weight) LOSS_CUDA(align_rows(w, p.weight));
+
+  const float up = a->dtype == IWP_F16 ? 8192.f : 1.f;
+  uint16_t* const probs = reinterpret_cast<uint16_t*>(ws + p.probs);
+  const int64_t kept = p.grad && !a->have_lse ? p.pieces - 1 : -1;  // the piece whose codes the logits pass leaves behind
   if (!a->have_lse) {
+    const Shape shape{T, V, D};
+    const int tile_n = pick_tile_n(shape, pairs);
+    iwp_tc::Problems<1> work;
+    if (!make_problem(&work.p[0], h, true, w, true, a->dtype, tile_n, 1)) return IWP_ERR_CUDA;
+    // Tensor cores cut what a term loses against the running sum, so long sums drift: segments of at most 1024
+    // elements of K, added up in fp32 registers, keep the logits within 3e-7 of their size (1.2e-6 at K = 4096 without).
+    const int blocks = work.p[0].k_blocks;
+    work.seg = static_cast<int>(tiles_of(blocks, tiles_of(blocks, 16)));
+    work.status = &hdr->status;
     H::Logits::Args la{};
     la.en = en;
     la.T = T;
     la.V = static_cast<int>(V);
     la.c = c;
-    la.part = reinterpret_cast<float2*>(ws + p.big);
+    la.part = reinterpret_cast<float2*>(ws + p.part);
+    la.parts = 2 * work.p[0].n_tiles;
     la.z_at = reinterpret_cast<float*>(ws + p.z_at);
-    if (int e = launch_product<2, true, true, H::Logits>(h, w, a->dtype, 1, la, &hdr->status, st)) return e;
-    H::k_finish<<<static_cast<unsigned>(tiles_of(T, 32)), 1024, 0, st>>>(hdr, en, la.part, static_cast<int>(p.parts), la.z_at, tau, T, a->rows,
-                                                                     a->lse, a->loss, a->mean, reinterpret_cast<float*>(ws + p.block_sum));
-    LOSS_CUDA(cudaGetLastError());
+    la.codes = probs;
+    la.ld = p.piece;
+    la.v0 = static_cast<int>(kept >= 0 ? kept * p.piece : 0);
+    la.width = static_cast<int>(kept >= 0 ? p.piece : 0);
+    la.log_codes = a->dtype == IWP_F16;
+    if (int e = launch_product<H::Logits, 1>(work, la, st)) return e;
+    H::Finish fa{};
+    fa.hdr = hdr;
+    fa.en = en;
+    fa.part = la.part;
+    fa.z_at = la.z_at;
+    fa.rows = a->rows ? a->rows : reinterpret_cast<float*>(ws + p.rows);
+    fa.lse = a->lse;
+    fa.loss = a->loss;
+    fa.T = T;
+    fa.parts = la.parts;
+    fa.part_shift = tile_n == 256 ? 7 : tile_n == 128 ? 6 : 5;
+    fa.mean = a->mean;
+    fa.tau = tau;
+    fa.chunks = 1;
+    if (kept >= 0) {
+      fa.codes = probs;
+      fa.ld = p.piece;
+      fa.v0 = la.v0;
+      fa.width = static_cast<int>(V - fa.v0 < p.piece ? V - fa.v0 : p.piece);
+      // a few thousand columns per block, less where the rows alone do not fill the device
+      int64_t chunk = up_to(tiles_of(T * fa.width, 8 * sms), 2048);
+      fa.chunk = static_cast<int>(chunk > 32768 ? 32768 : chunk);
+      fa.chunks = static_cast<int>(tiles_of(fa.width, fa.chunk));
+      fa.type = a->dtype;
+      fa.up = up;
+      fa.log_codes = la.log_codes;
+    }
+    LOSS_CUDA(launch(H::k_finish, T * fa.chunks, H::FINISH_THREADS, 0, 1, st, fa));
   }
   if (!p.grad) return IWP_OK;
 
-  H::Factor f{};
-  const float up = a->dtype == IWP_F16 ? 8192.f : 1.f;
-  f.hdr = hdr;
-  f.dloss = a->dloss;
-  f.factor = a->scale * tau / up;
-  f.mean = a->mean;
-  f.by_rows = a->dloss_rows != nullptr;
-  for (int64_t i = 0; i < p.pieces; i++) {
+  H::Out::Args oa{};
+  oa.f.hdr = hdr;
+  oa.f.dloss = a->dloss;
+  oa.f.factor = a->scale * tau / up;
+  oa.f.mean = a->mean;
+  oa.f.by_rows = a->dloss_rows != nullptr;
+  int splits = 1;
+  for (int64_t done = 0; done < p.pieces; done++) {
+    const int64_t i = p.pieces - 1 - done;  // the kept piece first
     const int64_t v0 = i * p.piece, width = V - v0 < p.piece ? V - v0 : p.piece;
     const Matrix wp{static_cast<const char*>(w.p) + 2 * v0 * w.ld, width, D, w.ld};
-    const Matrix probs{ws + p.big, T, width, p.p_ld};
-    H::Probs::Args pa{};
-    pa.en = en;
-    pa.lse = a->lse;
-    pa.out = ws + p.big;
-    pa.T = T;
-    pa.ld = p.p_ld;
-    pa.v0 = static_cast<int>(v0);
-    pa.width = static_cast<int>(width);
-    pa.c = c;
-    pa.up = up;
-    pa.type = a->dtype;
-    if (int e = launch_product<2, true, true, H::Probs>(h, wp, a->dtype, 1, pa, &hdr->status, st)) return e;
-    if (a->dweight) {
-      H::Out::Args oa{};
-      const int size = a->dweight_type == IWP_F32 ? 4 : 2;
-      oa.f = f;
-      oa.out = static_cast<char*>(a->dweight) + size * v0 * a->dweight_ld;
-      oa.ld = a->dweight_ld;
-      oa.rows = static_cast<int>(width);
-      oa.cols = static_cast<int>(D);
-      oa.type = a->dweight_type;
-      oa.wide = aligned(oa.out, 16) && a->dweight_ld * size % 16 == 0;
-      oa.add = a->accumulate;
-      if (int e = launch_product<2, false, false, H::Out>(probs, h, a->dtype, 1, oa, &hdr->status, st)) return e;
+    const Matrix pm{probs, T, width, p.piece};
+    if (i != kept) {
+      const Shape shape{T, width, D};
+      iwp_tc::Problems<1> work;
+      if (!make_problem(&work.p[0], h, true, wp, true, a->dtype, pick_tile_n(shape, pairs), 1)) return IWP_ERR_CUDA;
+      work.seg = 1 << 30;
+      work.status = &hdr->status;
+      H::Probs::Args pa{};
+      pa.en = en;
+      pa.lse = a->lse;
+      pa.out = probs;
+      pa.T = T;
+      pa.ld = p.piece;
+      pa.v0 = static_cast<int>(v0);
+      pa.width = static_cast<int>(width);
+      pa.c = c;
+      pa.up = up;
+      pa.type = a->dtype;
+      if (int e = launch_product<H::Probs, 1>(work, pa, st)) return e;
     }
+    // both gradients of the piece in one launch, dhidden (the longer tiles) first
+    iwp_tc::Problems<2> work;
+    work.p[0].m_tiles = work.p[0].n_tiles = work.p[0].splits = 0;
+    work.p[1].m_tiles = work.p[1].n_tiles = work.p[1].splits = 0;
+    work.seg = 1 << 30;
+    work.status = &hdr->status;
+    const Shape dh{T, D, width}, dw{width, D, T};
+    const Deal deal = deal_gradients(a->dhidden ? &dh : nullptr, a->dweight ? &dw : nullptr, pairs, done == 0 ? 0 : splits);
+    work.rounds = deal.rounds;
+    work.rest = deal.rest;
+    work.fill = deal.fill;
+    splits = deal.splits;
+    const int tile_n = deal.tile_n;
     if (a->dhidden) {
-      H::Out::Args oa{};
-      oa.f = f;
-      oa.rows = static_cast<int>(T);
-      oa.cols = static_cast<int>(D);
-      const bool direct = p.pieces == 1 && p.splits == 1;
+      const bool direct = p.pieces == 1 && splits == 1;
+      H::Out::Matrix& o = oa.m[0];
+      o.rows = static_cast<int>(T);
+      o.cols = static_cast<int>(D);
       if (direct) {
         const int size = a->dhidden_type == IWP_F32 ? 4 : 2;
-        oa.out = a->dhidden;
-        oa.ld = a->dhidden_ld;
-        oa.type = a->dhidden_type;
-        oa.wide = aligned(oa.out, 16) && oa.ld * size % 16 == 0;
-        oa.add = a->accumulate;
+        o.out = a->dhidden;
+        o.ld = a->dhidden_ld;
+        o.type = a->dhidden_type;
+        o.wide = aligned(o.out, 16) && o.ld * size % 16 == 0;
+        o.add = a->accumulate;
       } else {
-        oa.out = ws + p.join;
-        oa.ld = D;
-        oa.split_stride = T * D;
-        oa.type = IWP_F32;
-        oa.wide = D % 4 == 0;
-        oa.add = i > 0;
-        oa.raw = 1;
+        o.out = ws + p.join;
+        o.ld = D;
+        o.split_stride = T * D;
+        o.type = IWP_F32;
+        o.wide = D % 4 == 0;
+        o.add = done > 0;
+        o.raw = 1;
       }
-      if (int e = launch_product<2, true, false, H::Out>(probs, wp, a->dtype, p.splits, oa, &hdr->status, st)) return e;
+      if (!make_problem(&work.p[0], pm, true, wp, false, a->dtype, tile_n, splits)) return IWP_ERR_CUDA;
     }
+    if (a->dweight) {
+      H::Out::Matrix& o = oa.m[1];
+      const int size = a->dweight_type == IWP_F32 ? 4 : 2;
+      o.out = static_cast<char*>(a->dweight) + size * v0 * a->dweight_ld;
+      o.ld = a->dweight_ld;
+      o.rows = static_cast<int>(width);
+      o.cols = static_cast<int>(D);
+      o.type = a->dweight_type;
+      o.wide = aligned(o.out, 16) && o.ld * size % 16 == 0;
+      o.add = a->accumulate;
+      if (!make_problem(&work.p[1], pm, false, h, false, a->dtype, tile_n, 1)) return IWP_ERR_CUDA;
+    }
+    if (int e = launch_product<H::Out, 2>(work, oa, st)) return e;
   }
-  if (a->dhidden && (p.pieces > 1 || p.splits > 1)) {
-    const int64_t blocks = tiles_of(T * D, 1024);
-    H::k_join<<<static_cast<unsigned>(blocks < 16 * sms ? blocks : 16 * sms), 256, 0, st>>>(
-        f, reinterpret_cast<const float*>(ws + p.join), p.splits, T, static_cast<int>(D), a->dhidden, a->dhidden_ld, a->dhidden_type, a->accumulate);
-    LOSS_CUDA(cudaGetLastError());
+  if (a->dhidden && (p.pieces > 1 || splits > 1)) {
+    const int size = a->dhidden_type == IWP_F32 ? 4 : 2;
+    const int wide = D % 4 == 0 && aligned(a->dhidden, 16) && a->dhidden_ld * size % 16 == 0;
+    LOSS_CUDA(launch(H::k_join, T < 16 * sms ? T : 16 * sms, 256, 0, 1, st, oa.f, reinterpret_cast<const float*>(ws + p.join), splits, T,
+                     static_cast<int>(D), a->dhidden, a->dhidden_ld, a->dhidden_type, a->accumulate, wide));
   }
   return IWP_OK;
 }
@@ -347,28 +488,62 @@ bool balance_args_ok(const iwp_balance_args* a) {
   return a->type == IWP_F32 || a->type == IWP_BF16 || a->type == IWP_F16;
 }
 
-constexpr int BALANCE_BLOCKS = 148 * 2;
+constexpr int BALANCE_BLOCKS = 148;  // at most, of the rows kernel
+// Up to this many bytes of logits and ids one cluster serves: it saves the second launch and its 16 SMs keep up.
+constexpr int64_t CLUSTER_BYTES = int64_t(3) << 20;
 
-template <int TYPE, int VEC>
-int balance_rows(const iwp_balance::Rows& r, cudaStream_t st) {
-  int G = 1;
-  while (G < 32 && G * VEC < r.E) G *= 2;
-  const int need = static_cast<int>(tiles_of(r.E, int64_t(G) * VEC));
-  const int64_t steps = tiles_of(r.T, iwp_balance::ROW_THREADS / G);
-  const unsigned grid = static_cast<unsigned>(steps < 1 ? 1 : steps < BALANCE_BLOCKS ? steps : BALANCE_BLOCKS);
-  const int B = iwp_balance::ROW_THREADS;
-  if (need <= 1)
-    iwp_balance::k_balance_rows<TYPE, VEC, 1><<<grid, B, 0, st>>>(r, G);
-  else if (need <= 2)
-    iwp_balance::k_balance_rows<TYPE, VEC, 2><<<grid, B, 0, st>>>(r, G);
-  else if (need <= 4)
-    iwp_balance::k_balance_rows<TYPE, VEC, 4><<<grid, B, 0, st>>>(r, G);
-  else if (need <= 8)
-    iwp_balance::k_balance_rows<TYPE, VEC, 8><<<grid, B, 0, st>>>(r, G);
-  else if constexpr (VEC == 1)
-    iwp_balance::k_balance_rows<TYPE, VEC, 32><<<grid, B, 0, st>>>(r, G);
-  LOSS_CUDA(cudaGetLastError());
+int64_t balance_part_counts_bytes(int E) { return up_to(int64_t(iwp_balance::COUNT_BLOCKS) * (E + 1) * 4, 256); }
+
+template <int TYPE, int VEC, int N>
+int balance_launch(iwp_balance::Args a, int G, cudaStream_t st) {
+  namespace B = iwp_balance;
+  constexpr int threads = B::threads_of(VEC * N);
+  auto kernel = B::k_balance_rows<TYPE, VEC, N>;
+  const int64_t steps = tiles_of(a.T, threads / G);
+  const int64_t bytes = a.T * (a.E * (TYPE == IWP_F32 ? 4 : 2) + a.k * a.ids_bytes);
+  if (bytes <= CLUSTER_BYTES) {
+    // CTAs for about two rounds of rows each; 16 need the opt-in to clusters above the portable size
+    int ctas = 1;
+    while (ctas < 16 && 2 * ctas < steps) ctas *= 2;
+    a.part_counts = nullptr;
+    static bool opted[MAX_DEVICES] = {};
+    const int dev = device();
+    if (dev < 0) return IWP_ERR_CUDA;
+    if (!opted[dev]) {
+      LOSS_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+      opted[dev] = true;
+    }
+    LOSS_CUDA(launch(kernel, ctas, threads, 0, ctas, st, a, G));
+    return IWP_OK;
+  }
+  LOSS_CUDA(launch(B::k_balance_counts, B::COUNT_BLOCKS, B::COUNT_THREADS, 0, 1, st, a));
+  LOSS_CUDA(launch(kernel, steps < BALANCE_BLOCKS ? steps : BALANCE_BLOCKS, threads, 0, 1, st, a, G));
   return IWP_OK;
+}
+
+// A lane holds VEC neighbouring columns at a time (as many as rows are aligned for, up to 16 bytes), N times.
+template <int TYPE, int VEC>
+int balance_rows(const iwp_balance::Args& a, cudaStream_t st) {
+  int G = 1;
+  while (G < 32 && G * VEC < a.E) G *= 2;
+  const int64_t need = tiles_of(a.E, int64_t(G) * VEC);
+  constexpr int MIDDLE = VEC >= 8 ? 1 : 8 / VEC, MOST = iwp_balance::MAX_EXPERTS / 32 / VEC;
+  if (need <= 1) return balance_launch<TYPE, VEC, 1>(a, G, st);
+  if (need <= MIDDLE) return balance_launch<TYPE, VEC, MIDDLE>(a, G, st);
+  return balance_launch<TYPE, VEC, MOST>(a, G, st);
+}
+
+template <int TYPE>
+int balance_type(const iwp_balance::Args& a, cudaStream_t st) {
+  constexpr int size = TYPE == IWP_F32 ? 4 : 2;
+  auto fits = [&](int vec) {
+    return a.E % vec == 0 && a.logits_ld % vec == 0 && a.dlogits_ld % vec == 0 && aligned(a.logits, vec * size) && aligned(a.dlogits, vec * size);
+  };
+  if constexpr (size == 2)
+    if (fits(8)) return balance_rows<TYPE, 8>(a, st);
+  if (fits(4)) return balance_rows<TYPE, 4>(a, st);
+  if (fits(2)) return balance_rows<TYPE, 2>(a, st);
+  return balance_rows<TYPE, 1>(a, st);
 }
 
 }  // namespace
@@ -412,7 +587,7 @@ extern "C" int iwp_head_loss(const iwp_head_args* a, void* cuda_stream) {
 
 extern "C" int64_t iwp_balance_workspace(const iwp_balance_args* a) {
   if (!balance_args_ok(a)) return -1;
-  return 256 + up_to(int64_t(BALANCE_BLOCKS) * a->experts * 4, 256);
+  return 256 + balance_part_counts_bytes(a->experts) + up_to(int64_t(BALANCE_BLOCKS) * a->experts * 4, 256);
 }
 
 extern "C" int iwp_balance_loss(const iwp_balance_args* a, void* cuda_stream) {
@@ -424,39 +599,30 @@ extern "C" int iwp_balance_loss(const iwp_balance_args* a, void* cuda_stream) {
   if (!aligned(a->logits, size) || (a->dlogits && !aligned(a->dlogits, size)) || !aligned(a->ids, a->ids_bytes)) return IWP_ERR_INVALID;
   if (!std::isfinite(a->coef) || !std::isfinite(a->scale)) return IWP_ERR_INVALID;
   if (a->workspace_bytes < iwp_balance_workspace(a)) return IWP_ERR_CAPACITY;
-  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  auto* hdr = static_cast<iwp_balance::Header*>(a->workspace);
-  const int E = a->experts;
-  LOSS_CUDA(cudaMemsetAsync(static_cast<char*>(a->workspace) + 4, 0, 12, st));
-  LOSS_CUDA(cudaMemsetAsync(a->counts, 0, 4 * E, st));
-  const int64_t pairs = a->tokens * a->top_k;
-  if (pairs > 0) {
-    const int64_t blocks = tiles_of(pairs, 1024);
-    iwp_balance::k_balance_counts<<<static_cast<unsigned>(blocks < 148 ? blocks : 148), 512, 0, st>>>(hdr, a->counts, a->ids, a->ids_ld, a->ids_bytes,
-                                                                                              a->mask, a->tokens, a->top_k, E);
-    LOSS_CUDA(cudaGetLastError());
-  }
-  iwp_balance::Rows r{};
-  r.hdr = hdr;
+  char* const ws = static_cast<char*>(a->workspace);
+  iwp_balance::Args r{};
+  r.hdr = reinterpret_cast<iwp_balance::Header*>(ws);
   r.counts = a->counts;
   r.logits = a->logits;
+  r.ids = a->ids;
   r.mask = a->mask;
   r.dloss = a->dloss;
   r.dlogits = a->dlogits;
-  r.part = reinterpret_cast<float*>(static_cast<char*>(a->workspace) + 256);
+  r.part_counts = reinterpret_cast<int*>(ws + 256);
+  r.part = reinterpret_cast<float*>(ws + 256 + balance_part_counts_bytes(a->experts));
   r.loss = a->loss;
   r.mean_prob = a->mean_prob;
   r.logits_ld = a->logits_ld;
   r.dlogits_ld = a->dlogits ? a->dlogits_ld : a->logits_ld;
+  r.ids_ld = a->ids_ld;
   r.T = a->tokens;
-  r.E = E;
+  r.E = a->experts;
   r.k = a->top_k;
+  r.ids_bytes = a->ids_bytes;
   r.coef = a->coef;
   r.scale = a->scale;
-  // whole 16-byte words where every row starts on one and holds whole ones
-  const int vec = 16 / size;
-  const bool wide = E % vec == 0 && r.logits_ld % vec == 0 && r.dlogits_ld % vec == 0 && aligned(r.logits, 16) && aligned(r.dlogits, 16);
-  if (a->type == IWP_F32) return wide ? balance_rows<IWP_F32, 4>(r, st) : balance_rows<IWP_F32, 1>(r, st);
-  if (a->type == IWP_BF16) return wide ? balance_rows<IWP_BF16, 8>(r, st) : balance_rows<IWP_BF16, 1>(r, st);
-  return wide ? balance_rows<IWP_F16, 8>(r, st) : balance_rows<IWP_F16, 1>(r, st);
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (a->type == IWP_F32) return balance_type<IWP_F32>(r, st);
+  if (a->type == IWP_BF16) return balance_type<IWP_BF16>(r, st);
+  return balance_type<IWP_F16>(r, st);
 }

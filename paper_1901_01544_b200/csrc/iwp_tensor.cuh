@@ -2,15 +2,16 @@
 //
 // One persistent kernel template: C[M, N] = A[M, K] B[N, K]^T with fp32 accumulators in tensor memory, and what
 // becomes of a finished tile left to an epilogue class.  Either operand may lie K-contiguous or M/N-contiguous
-// in memory (the tensor cores read both), so none of the three products of a head is ever transposed.
+// in memory (the tensor cores read both), so none of the three products of a head is ever transposed, and the two
+// gradients, which need nothing of each other, are one launch with two problems.
 //
 // A CTA pair (cta_group::2) works on one 256 x 256 tile: each CTA stages its own 128 rows of A and 128 rows of B, so
 // that every byte brought into shared memory feeds twice the arithmetic of a single CTA's 128 x 256 tile
-// (64 instead of 96 bytes per SM and clock at the full tensor rate).  Roles per CTA: warp 0 issues the tile loads
-// (TMA), warp 1 of the pair's first CTA issues the products, warp 2 owns the tensor memory, warps 4..11 are the
-// epilogue (warp % 4 = the 32 lanes of tensor memory it may read, warp / 4 = its half of the columns).  Two
-// accumulator tiles of 256 columns fill the 512 columns of tensor memory, so the epilogue of one tile runs beside the
-// products of the next.
+// (64 instead of 96 bytes per SM and clock at the full tensor rate).  Problems with few tiles take tiles of 128 or
+// 64 columns instead (pick_tile_n).  Roles per CTA: warp 0 issues the tile loads (TMA), warp 1 of the pair's first
+// CTA issues the products, warp 2 owns the tensor memory, warps 4..11 are the epilogue (warp % 4 = the 32 lanes of
+// tensor memory it may read, the other half of the columns for warps 8..11).  Two accumulator tiles of 256 columns
+// fill the 512 columns of tensor memory, so the epilogue of one tile runs beside the products of the next.
 //
 // Every wait is bounded: a wait that runs out sets the status word and marks the CTA dead; the roles then fall
 // through to the common end, which gives copies in flight time to land, frees the tensor memory and returns.
@@ -36,15 +37,12 @@ constexpr int STAGING_BYTES = 32 * STAGING_PITCH;       // per epilogue warp
 constexpr uint32_t WAIT_TRIES = 1u << 18;               // x 20 us at most per try: about 5 s
 constexpr uint32_t WAIT_HINT_NS = 20000;
 
-template <int CG>
-struct Shape {
-  static constexpr int A_BYTES = TILE_M * BLOCK_K * 2;
-  static constexpr int B_ROWS = TILE_N / CG;  // rows of B that one CTA stages
-  static constexpr int B_BYTES = B_ROWS * BLOCK_K * 2;
-  static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
-  static constexpr int STAGES = CG == 2 ? 5 : 3;
-  static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * STAGING_BYTES + 256;
-};
+constexpr int CG = 2;                               // CTAs per tile
+constexpr int A_BYTES = TILE_M * BLOCK_K * 2;
+constexpr int B_BYTES = TILE_N / CG * BLOCK_K * 2;  // of the widest tile
+constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
+constexpr int STAGES = 5;
+constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * STAGING_BYTES + 256;
 
 // ---- small wrappers of the instructions used ---------------------------------------------------------
 
@@ -103,64 +101,48 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
   return false;
 }
 
-template <int CG>
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
-  if constexpr (CG == 2) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-        "l"(map), "r"(x), "r"(y), "r"(bar)
-        : "memory");
-  } else {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map),
-        "r"(x), "r"(y), "r"(bar)
-        : "memory");
-  }
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(y), "r"(bar)
+      : "memory");
 }
 
-template <int CG>
 __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-  if constexpr (CG == 2) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
-        : "memory");
-  } else {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
-        : "memory");
-  }
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
 }
 
-// Arrives on the barrier at this offset in every CTA of the pair once all products issued so far are done.
-template <int CG>
+// Arrives on the barrier at this offset in both CTAs of the pair once all products issued so far are done.
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
-  if constexpr (CG == 2) {
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
-                 "h"(static_cast<uint16_t>(3))
-                 : "memory");
-  } else {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-  }
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+               "h"(static_cast<uint16_t>(3))
+               : "memory");
+}
+
+// Programmatic launches: a kernel may start while the one before it drains, and touches memory only after wait().
+__device__ __forceinline__ void launch_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// 2^x, denormal results flushed (their weight in any sum here is below its last bit)
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 
-// 32 columns of this warp's 32 lanes: v[j] = column j of the lane's row.
+// 32 or 16 columns of this warp's 32 lanes: v[j] = column j of the lane's row.
 __device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
   uint32_t r[32];
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
-        "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
-        "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(addr)
       : "memory");
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
@@ -168,71 +150,139 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
   for (int j = 0; j < 32; j++) v[j] = __uint_as_float(r[j]);
 }
 
+__device__ __forceinline__ void tmem_load16(uint32_t addr, float (&v)[16]) {
+  uint32_t r[16];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(addr)
+      : "memory");
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int j = 0; j < 16; j++) v[j] = __uint_as_float(r[j]);
+}
+
 // Shared-memory operand descriptor, 128-byte swizzle.  K-contiguous operands: rows of 128 bytes, groups of 8 rows
 // every 1024 bytes.  M/N-contiguous operands: blocks of 64 rows of M/N (128 bytes) x BLOCK_K, one block after the
 // other (the leading offset), groups of 8 along K every 1024 bytes.
-template <bool K_CONTIGUOUS>
-__device__ __forceinline__ uint64_t operand_desc(uint32_t addr) {
-  constexpr uint64_t lead = K_CONTIGUOUS ? 1 : (BLOCK_K * 128) >> 4;
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr, bool k_contiguous) {
+  const uint64_t lead = k_contiguous ? 1 : (BLOCK_K * 128) >> 4;
   return static_cast<uint64_t>((addr & 0x3FFFF) >> 4) | (lead << 16) | (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) |
          (2ull << 61);
 }
 
 // ---- the work list ---------------------------------------------------------------------------------
 
-struct Work {
-  int m_tiles, n_tiles;  // tiles of TILE_M * CG rows and TILE_N columns
+struct Problem {
+  CUtensorMap a, b;
+  int m_tiles, n_tiles;  // tiles of CG * TILE_M rows and tile_n columns
+  int tile_n;            // 256, 192, 128 or 64
   int k_blocks;          // blocks of BLOCK_K along K
   int splits;            // the K range in this many parts (each part a tile of its own)
   uint32_t idesc;
+  int a_kc, b_kc;        // which operands are K-contiguous
+};
+
+// Up to two problems over the pairs of a launch.  Every pair first takes `rounds` tiles of problem 0; the first `rest`
+// pairs take one more each, and the others meanwhile `fill` tiles of problem 1 each; what is left of problem 1 is dealt
+// round by round.  (The tiles of one problem all cost the same, so the host can balance this without a counter.)
+template <int N>
+struct Problems {
+  Problem p[N];
+  int rounds, rest, fill;
+  int seg;  // k blocks per accumulator tile (epilogues that add up segments), or a large number
   int* status;
 };
 
 struct Tile {
-  int m, n, split, k0, k1;
+  int p, m, n, split, k0, k1;
 };
 
-// Tiles in groups of up to 16 of the shorter side, so that the tiles in flight share operands in the L2.
-__device__ __forceinline__ Tile tile_at(const Work& w, int i) {
-  const int per = w.m_tiles * w.n_tiles;
-  Tile t;
-  t.split = i / per;
-  const int r = i - t.split * per;
-  const bool m_short = w.m_tiles <= w.n_tiles;
-  const int s = m_short ? w.m_tiles : w.n_tiles, l = m_short ? w.n_tiles : w.m_tiles;
-  const int g = r / (16 * l);
-  const int size = min(16, s - 16 * g);
-  const int q = r - g * 16 * l;
-  const int a = 16 * g + q % size, b = q / size;
-  t.m = m_short ? a : b;
-  t.n = m_short ? b : a;
-  t.k0 = static_cast<int>(static_cast<int64_t>(w.k_blocks) * t.split / w.splits);
-  t.k1 = static_cast<int>(static_cast<int64_t>(w.k_blocks) * (t.split + 1) / w.splits);
-  return t;
+template <int N>
+__device__ __forceinline__ void deal(const Problems<N>& w, int pair, int pairs, int step, int& p, int& i) {
+  p = 0;
+  if constexpr (N == 1) {
+    i = step * pairs + pair;
+    return;
+  }
+  if (step < w.rounds) {
+    i = step * pairs + pair;
+    return;
+  }
+  step -= w.rounds;
+  if (w.rest > 0) {
+    if (pair < w.rest) {
+      if (step == 0) {
+        i = w.rounds * pairs + pair;
+        return;
+      }
+      step -= 1;
+    } else {
+      p = 1;
+      i = step * (pairs - w.rest) + pair - w.rest;
+      if (step < w.fill) return;
+      step -= w.fill;
+    }
+  }
+  p = 1;
+  i = step * pairs + pair;
+  if (w.rest > 0) i += w.fill * (pairs - w.rest) - w.rest + (pair < w.rest ? pairs : 0);  // the pairs without one go first
 }
 
-// Epi: device class with `struct Args` and `static void tile(const Args&, const Tile&, uint32_t tmem, int rank, int
-// warp, int lane, char* staging)`: reads its 128 columns of its 32 rows from tensor memory and disposes of them.
-template <int CG, bool A_KC, bool B_KC, class Epi>
+// The tile of a pair's step; false = it has no more.  Tiles of one problem in groups of up to 16 of the shorter side, so
+// that the tiles in flight share operands in the L2.
+template <int N>
+__device__ __forceinline__ bool tile_at(const Problems<N>& w, int pair, int pairs, int step, Tile& t) {
+  int i;
+  deal(w, pair, pairs, step, t.p, i);
+  const Problem& q = w.p[t.p];
+  const int per = q.m_tiles * q.n_tiles;
+  if (i >= per * q.splits) return false;
+  t.split = i / per;
+  const int r = i - t.split * per;
+  const bool m_short = q.m_tiles <= q.n_tiles;
+  const int s = m_short ? q.m_tiles : q.n_tiles, l = m_short ? q.n_tiles : q.m_tiles;
+  const int g = r / (16 * l);
+  const int size = min(16, s - 16 * g);
+  const int o = r - g * 16 * l;
+  const int x = 16 * g + o % size, y = o / size;
+  t.m = m_short ? x : y;
+  t.n = m_short ? y : x;
+  t.k0 = static_cast<int>(static_cast<int64_t>(q.k_blocks) * t.split / q.splits);
+  t.k1 = static_cast<int>(static_cast<int64_t>(q.k_blocks) * (t.split + 1) / q.splits);
+  return true;
+}
+
+// Epi (device class): `Args`; begin(args, where), before the tile is there; tile(args, where, begun, accumulator), in which an epilogue warp disposes of its 32 rows and
+// half of the tile's columns.  SUMS: the tensor memory is emptied into registers every `seg` blocks of K and added up
+// there (the accumulator is then an array); otherwise it is an address in tensor memory.
+struct Where {
+  int row0;     // first of the warp's 32 rows; the lane's row is row0 + lane
+  int col0;     // first of the warp's columns
+  int width;    // number of them: half a tile
+  int lane, p, split;
+  char* staging;
+};
+
+template <int N, class Epi>
 __global__ void __launch_bounds__(THREADS, 1)
-    k_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const Work w,
-              const __grid_constant__ typename Epi::Args args) {
-  using S = Shape<CG>;
+    k_product(const __grid_constant__ Problems<N> w, const __grid_constant__ typename Epi::Args args) {
   extern __shared__ char smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   char* const smem = smem_raw + (((raw + 1023) & ~1023u) - raw);  // the same offset in both CTAs of a pair
   const uint32_t base = smem_u32(smem);
-  char* const staging = smem + S::STAGES * S::STAGE_BYTES;
+  char* const staging = smem + STAGES * STAGE_BYTES;
   char* const ctl = staging + EPI_WARPS * STAGING_BYTES;
   const uint32_t bars = smem_u32(ctl);
-  const uint32_t full = bars, empty = bars + 8 * S::STAGES, acc_full = empty + 8 * S::STAGES, acc_empty = acc_full + 16;
-  volatile int* const dead = reinterpret_cast<volatile int*>(ctl + 8 * (2 * S::STAGES + 4));
-  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(ctl + 8 * (2 * S::STAGES + 4) + 4);
+  const uint32_t full = bars, empty = bars + 8 * STAGES, acc_full = empty + 8 * STAGES, acc_empty = acc_full + 16;
+  volatile int* const dead = reinterpret_cast<volatile int*>(ctl + 8 * (2 * STAGES + 4));
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(ctl + 8 * (2 * STAGES + 4) + 4);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t rank = CG == 2 ? cluster_rank() : 0;
+  const uint32_t rank = cluster_rank();
+  launch_next();
   if (threadIdx.x == 0) {
-    for (int s = 0; s < S::STAGES; s++) {
+    for (int s = 0; s < STAGES; s++) {
       mbar_init(full + 8 * s, 1);
       mbar_init(empty + 8 * s, 1);
     }
@@ -244,95 +294,103 @@ __global__ void __launch_bounds__(THREADS, 1)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 2) {
-    if constexpr (CG == 2) {
-      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_slot)) : "memory");
-      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
-    } else {
-      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_slot)) : "memory");
-      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
-    }
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_slot)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
     fence_before();
   }
   __syncthreads();
-  if constexpr (CG == 2) cluster_sync();
+  cluster_sync();
   fence_after();
   const uint32_t tmem = *tmem_slot;
+  wait_previous();
 
-  const int total = w.m_tiles * w.n_tiles * w.splits;
-  const int first = blockIdx.x / CG, stride = gridDim.x / CG;
+  const int pair = blockIdx.x / CG, pairs = gridDim.x / CG;
+  Tile t;
 
-  if (warp == 0 && lane == 0) {  // ---- loads
-    int s = 0;
-    uint32_t phase = 0;
-    const uint32_t full_of_pair = CG == 2 ? map_to(full, 0) : full;  // both CTAs' loads are counted by the first CTA
-    for (int i = first; i < total && !*dead; i += stride) {
-      const Tile t = tile_at(w, i);
-      const int row_a = t.m * TILE_M * CG + static_cast<int>(rank) * TILE_M;
-      const int row_b = t.n * TILE_N + static_cast<int>(rank) * S::B_ROWS;
-      for (int kb = t.k0; kb < t.k1; kb++) {
-        if (!mbar_wait(empty + 8 * s, phase ^ 1, dead, w.status)) break;
-        if (rank == 0) mbar_expect(full + 8 * s, CG * S::STAGE_BYTES);
-        const uint32_t bar = full_of_pair + 8 * s;
-        const uint32_t at_a = base + s * S::STAGE_BYTES, at_b = at_a + S::A_BYTES;
-        if constexpr (A_KC) {
-          tma_load<CG>(at_a, &map_a, kb * BLOCK_K, row_a, bar);
-        } else {
-#pragma unroll
-          for (int j = 0; j < TILE_M / 64; j++) tma_load<CG>(at_a + j * 64 * 128, &map_a, row_a + 64 * j, kb * BLOCK_K, bar);
-        }
-        if constexpr (B_KC) {
-          tma_load<CG>(at_b, &map_b, kb * BLOCK_K, row_b, bar);
-        } else {
-#pragma unroll
-          for (int j = 0; j < S::B_ROWS / 64; j++) tma_load<CG>(at_b + j * 64 * 128, &map_b, row_b + 64 * j, kb * BLOCK_K, bar);
-        }
-        if (++s == S::STAGES) {
-          s = 0;
-          phase ^= 1;
+  // An epilogue that sums holds 128 columns per thread: 88 registers for each thread of the first four warps, 208 for
+  // the eight epilogue warps, of the 384 x 168 that the block was launched with.
+  if (warp < 4) {
+    if constexpr (Epi::SUMS) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if (warp == 0 && lane == 0) {  // ---- loads
+      int s = 0;
+      uint32_t phase = 0;
+      const uint32_t full_of_pair = map_to(full, 0);  // both CTAs' loads are counted by the first CTA
+      for (int i = 0; !*dead && tile_at(w, pair, pairs, i, t); i++) {
+        const Problem& q = w.p[t.p];
+        const int rows_b = q.tile_n / CG;
+        const int row_a = t.m * TILE_M * CG + static_cast<int>(rank) * TILE_M;
+        const int row_b = t.n * q.tile_n + static_cast<int>(rank) * rows_b;
+        const bool a_kc = q.a_kc, b_kc = q.b_kc;
+        // M/N-contiguous boxes are 64 columns wide even where a CTA needs 32 of them
+        const uint32_t bytes = CG * (A_BYTES + (b_kc ? rows_b : (rows_b + 63) / 64 * 64) * BLOCK_K * 2);
+        for (int kb = t.k0; kb < t.k1; kb++) {
+          if (!mbar_wait(empty + 8 * s, phase ^ 1, dead, w.status)) break;
+          if (rank == 0) mbar_expect(full + 8 * s, bytes);
+          const uint32_t bar = full_of_pair + 8 * s;
+          const uint32_t at_a = base + s * STAGE_BYTES, at_b = at_a + A_BYTES;
+          if (a_kc) {
+            tma_load(at_a, &q.a, kb * BLOCK_K, row_a, bar);
+          } else {
+            tma_load(at_a, &q.a, row_a, kb * BLOCK_K, bar);
+            tma_load(at_a + 64 * 128, &q.a, row_a + 64, kb * BLOCK_K, bar);
+          }
+          if (b_kc) {
+            tma_load(at_b, &q.b, kb * BLOCK_K, row_b, bar);
+          } else {
+            tma_load(at_b, &q.b, row_b, kb * BLOCK_K, bar);
+            if (rows_b > 64) tma_load(at_b + 64 * 128, &q.b, row_b + 64, kb * BLOCK_K, bar);
+          }
+          if (++s == STAGES) {
+            s = 0;
+            phase ^= 1;
+          }
         }
       }
-    }
-  } else if (warp == 1 && lane == 0 && rank == 0) {  // ---- products
-    int s = 0, b = 0;
-    uint32_t phase = 0, acc_phase = 0;
-    for (int i = first; i < total && !*dead; i += stride) {
-      const Tile t = tile_at(w, i);
-      if (!mbar_wait(acc_empty + 8 * b, acc_phase ^ 1, dead, w.status)) break;
-      fence_after();
-      for (int kb = t.k0; kb < t.k1; kb++) {
-        if (!mbar_wait(full + 8 * s, phase, dead, w.status)) break;
-        fence_after();
-        const uint32_t at_a = base + s * S::STAGE_BYTES;
-        const uint64_t da = operand_desc<A_KC>(at_a), db = operand_desc<B_KC>(at_a + S::A_BYTES);
+    } else if (warp == 1 && lane == 0 && rank == 0) {  // ---- products
+      int s = 0, b = 0;
+      uint32_t phase = 0, acc_phase = 0;
+      for (int i = 0; !*dead && tile_at(w, pair, pairs, i, t); i++) {
+        const Problem& q = w.p[t.p];
         // 16 elements of K further: 32 bytes along a K-contiguous row, 16 rows of 128 bytes otherwise
-        constexpr uint64_t step_a = A_KC ? 2 : 128, step_b = B_KC ? 2 : 128;
+        const bool a_kc = q.a_kc, b_kc = q.b_kc;
+        const uint64_t step_a = a_kc ? 2 : 128, step_b = b_kc ? 2 : 128;
+        const uint32_t idesc = q.idesc;
+        for (int k0 = t.k0; k0 < t.k1; k0 += w.seg) {
+          const int k1 = Epi::SUMS ? min(t.k1, k0 + w.seg) : t.k1;
+          if (!mbar_wait(acc_empty + 8 * b, acc_phase ^ 1, dead, w.status)) break;
+          fence_after();
+          for (int kb = k0; kb < k1; kb++) {
+            if (!mbar_wait(full + 8 * s, phase, dead, w.status)) break;
+            fence_after();
+            const uint32_t at_a = base + s * STAGE_BYTES;
+            const uint64_t da = operand_desc(at_a, a_kc), db = operand_desc(at_a + A_BYTES, b_kc);
 #pragma unroll
-        for (int k = 0; k < BLOCK_K / 16; k++)
-          mma<CG>(tmem + b * TILE_N, da + k * step_a, db + k * step_b, w.idesc, (kb > t.k0 || k > 0) ? 1u : 0u);
-        mma_commit<CG>(empty + 8 * s);
-        if (++s == S::STAGES) {
-          s = 0;
-          phase ^= 1;
+            for (int k = 0; k < BLOCK_K / 16; k++)
+              mma(tmem + b * TILE_N, da + k * step_a, db + k * step_b, idesc, (kb > k0 || k > 0) ? 1u : 0u);
+            mma_commit(empty + 8 * s);
+            if (++s == STAGES) {
+              s = 0;
+              phase ^= 1;
+            }
+          }
+          mma_commit(acc_full + 8 * b);
+          if (++b == 2) {
+            b = 0;
+            acc_phase ^= 1;
+          }
+          if (!Epi::SUMS) break;
         }
       }
-      mma_commit<CG>(acc_full + 8 * b);
-      if (++b == 2) {
-        b = 0;
-        acc_phase ^= 1;
-      }
     }
-  } else if (warp >= 4) {  // ---- epilogue
+  } else {  // ---- epilogue
+    if constexpr (Epi::SUMS) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     const int e = warp - 4;
     int b = 0;
     uint32_t acc_phase = 0;
-    const uint32_t empty_of_pair = CG == 2 ? map_to(acc_empty, 0) : acc_empty;
-    for (int i = first; i < total; i += stride) {
-      const Tile t = tile_at(w, i);
-      const bool ok = mbar_wait(acc_full + 8 * b, acc_phase, dead, w.status);
-      if (!__all_sync(0xFFFFFFFFu, ok)) break;
-      fence_after();
-      const uint32_t at = tmem + b * TILE_N + (e / 4) * (TILE_N / 2) + (static_cast<uint32_t>(e % 4) << 21);
-      Epi::tile(args, t, at, CG * t.m + static_cast<int>(rank), e, lane, staging + e * STAGING_BYTES);
+    const uint32_t empty_of_pair = map_to(acc_empty, 0);
+    bool ok = true;
+    // the accumulator's turn is over: the products may write it again
+    auto release = [&] {
       fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_cluster(empty_of_pair + 8 * b);
@@ -340,24 +398,58 @@ __global__ void __launch_bounds__(THREADS, 1)
         b = 0;
         acc_phase ^= 1;
       }
+    };
+    for (int i = 0; ok && tile_at(w, pair, pairs, i, t); i++) {
+      const Problem& q = w.p[t.p];
+      Where at;
+      at.width = q.tile_n / 2;
+      at.row0 = (CG * t.m + static_cast<int>(rank)) * TILE_M + (e % 4) * 32;
+      at.col0 = t.n * q.tile_n + (e / 4) * at.width;
+      at.lane = lane;
+      at.p = t.p;
+      at.split = t.split;
+      at.staging = staging + e * STAGING_BYTES;
+      const uint32_t mine = tmem + (e / 4) * at.width + (static_cast<uint32_t>(e % 4) << 21);
+      auto begun = Epi::begin(args, at);  // what the rows need from memory, fetched while the products run
+      if constexpr (Epi::SUMS) {
+        float acc[TILE_N / 2];
+#pragma unroll
+        for (int j = 0; j < TILE_N / 2; j++) acc[j] = 0.f;
+        for (int k0 = t.k0; k0 < t.k1; k0 += w.seg) {
+          ok = __all_sync(0xFFFFFFFFu, mbar_wait(acc_full + 8 * b, acc_phase, dead, w.status));
+          if (!ok) break;
+          fence_after();
+#pragma unroll
+          for (int c = 0; c < TILE_N / 32; c++) {
+            if (16 * c < at.width) {
+              float v[16];
+              tmem_load16(mine + b * TILE_N + 16 * c, v);
+#pragma unroll
+              for (int j = 0; j < 16; j++) acc[16 * c + j] += v[j];
+            }
+          }
+          release();
+        }
+        if (ok) Epi::tile(args, at, begun, acc);
+      } else {
+        ok = __all_sync(0xFFFFFFFFu, mbar_wait(acc_full + 8 * b, acc_phase, dead, w.status));
+        if (!ok) break;
+        fence_after();
+        Epi::tile(args, at, begun, mine + b * TILE_N);
+        release();
+      }
     }
   }
   __syncwarp();
   __syncthreads();
   if (*dead) __nanosleep(1000000);  // copies in flight land in microseconds
-  if constexpr (CG == 2) cluster_sync();
+  cluster_sync();
   if (warp == 2) {
     fence_after();
-    if constexpr (CG == 2)
-      asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem));
-    else
-      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem));
   }
 }
 
-// Writes a chunk of 32 columns (v: this lane's row) of the warp's 32 rows to a row-major matrix, through the warp's
-// staging rows so that the stores are whole 32-byte sectors; rows and columns outside are dropped.
-// TYPE: IWP_F32 / IWP_BF16 / IWP_F16.  `add`: the old contents are added first (in fp32).
 __device__ __forceinline__ uint32_t pack2(float a, float b, int type) {
   if (type == 1) {
     __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
@@ -387,6 +479,9 @@ __device__ __forceinline__ void store_as(void* p, int64_t i, float v, int type) 
     static_cast<__half*>(p)[i] = __float2half_rn(v);
 }
 
+// Writes a chunk of 32 columns (v: this lane's row) of the warp's 32 rows to a row-major matrix, through the warp's
+// staging rows so that the stores are whole 32-byte sectors; rows and columns outside are dropped.
+// TYPE: IWP_F32 / IWP_BF16 / IWP_F16.  `add`: the old contents are added first (in fp32).
 __device__ __forceinline__ void store_chunk(const float (&v)[32], char* staging, void* out, int64_t ld, int type, bool wide, bool add,
                                             int row0, int rows, int col0, int cols, int lane) {
   char* mine = staging + lane * STAGING_PITCH;
@@ -435,6 +530,22 @@ __device__ __forceinline__ void store_chunk(const float (&v)[32], char* staging,
         store_as(out, at, x, type);
       }
     }
+  }
+  __syncwarp();
+}
+
+// The same for 32 columns of 16 bits that are packed already; rows of 16-byte multiples, all columns inside.
+__device__ __forceinline__ void store_packed(const uint32_t (&u)[16], char* staging, uint16_t* out, int64_t ld, int row0, int rows, int col0,
+                                             int lane) {
+  char* mine = staging + lane * STAGING_PITCH;
+#pragma unroll
+  for (int j = 0; j < 4; j++) *reinterpret_cast<uint4*>(mine + 16 * j) = make_uint4(u[4 * j], u[4 * j + 1], u[4 * j + 2], u[4 * j + 3]);
+  __syncwarp();
+  const int r = lane >> 2, c = lane & 3;  // 8 rows of 64 bytes at a time
+#pragma unroll
+  for (int i = 0; i < 32; i += 8) {
+    const uint4 x = *reinterpret_cast<const uint4*>(staging + (r + i) * STAGING_PITCH + 16 * c);
+    if (row0 + r + i < rows) *reinterpret_cast<uint4*>(out + (row0 + r + i) * ld + col0 + 8 * c) = x;
   }
   __syncwarp();
 }

@@ -10,11 +10,9 @@ word that kernels set, e.g. after a target outside the vocabulary.
 from __future__ import annotations
 
 import ctypes as C
-from dataclasses import dataclass
-from typing import Any, Optional
 
 from . import binding
-from .binding import IWP_ERR_INVALID, IwpError, _check
+from .binding import IWP_ERR_CAPACITY, IWP_ERR_INVALID, IwpError, _check
 
 IWP_F32, IWP_BF16, IWP_F16 = 0, 1, 2
 EXPORTS = ["iwp_loss_reset", "iwp_loss_status", "iwp_head_workspace", "iwp_head_loss", "iwp_balance_workspace", "iwp_balance_loss"]
@@ -58,25 +56,43 @@ def lib() -> C.CDLL:
     return L
 
 
-@dataclass
 class HeadResult:
-    """loss: 0-d, rows and lse: [T], all float32; dhidden / dweight: None where they were not asked for."""
+    """loss: 0-d, rows and lse: [T], all float32 (None where no forward pass was made, lse then as given); dhidden /
+    dweight: None where they were not asked for."""
 
-    loss: Any = None
-    rows: Any = None
-    lse: Any = None
-    dhidden: Any = None
-    dweight: Any = None
+    __slots__ = ("_out", "_lse", "_tokens", "dhidden", "dweight")
+
+    def __init__(self, out, lse, tokens):
+        self._out, self._lse, self._tokens, self.dhidden, self.dweight = out, lse, tokens, None, None
+
+    @property
+    def loss(self):
+        return None if self._out is None else self._out[-1]
+
+    @property
+    def rows(self):
+        return None if self._out is None else self._out[: self._tokens]
+
+    @property
+    def lse(self):
+        return self._lse if self._out is None else self._out[self._tokens : -1]
 
 
-@dataclass
 class BalanceResult:
     """loss: 0-d float32, counts: [E] int32, mean_prob: [E] float32, dlogits: [T, E] or None."""
 
-    loss: Any = None
-    counts: Any = None
-    mean_prob: Any = None
-    dlogits: Any = None
+    __slots__ = ("_out", "counts", "dlogits")
+
+    def __init__(self, out, counts, dlogits):
+        self._out, self.counts, self.dlogits = out, counts, dlogits
+
+    @property
+    def loss(self):
+        return self._out[-1]
+
+    @property
+    def mean_prob(self):
+        return self._out[:-1]
 
 
 def _types():
@@ -85,28 +101,33 @@ def _types():
     return torch, {torch.float32: IWP_F32, torch.bfloat16: IWP_BF16, torch.float16: IWP_F16}
 
 
-def _rows_of(x, name: str, shape, dtypes, device) -> int:
-    """Checks a matrix (rows may be strided, columns not) and returns its row stride."""
+def _bad(x, name: str, shape, dtypes, device):
     if x.dtype not in dtypes:
         raise TypeError(f"{name} has dtype {x.dtype}, expected one of {[str(d) for d in dtypes]}")
     if x.device != device:
         raise ValueError(f"{name} is on {x.device}, expected {device}")
     if tuple(x.shape) != tuple(shape):
         raise ValueError(f"{name} has shape {tuple(x.shape)}, expected {tuple(shape)}")
-    if x.shape[1] > 1 and x.stride(1) != 1:
+
+
+def _rows_of(x, name: str, shape, dtypes, device) -> int:
+    """Checks a matrix (rows may be strided, columns not) and returns its row stride."""
+    if x.dtype not in dtypes or x.shape != shape or x.device != device:
+        _bad(x, name, shape, dtypes, device)
+    ld, step = x.stride()
+    rows, cols = shape
+    if step != 1 and cols > 1:
         raise ValueError(f"{name}: neighbouring columns must be neighbours in memory")
-    if x.shape[0] <= 1:
-        return x.shape[1]
-    if x.stride(0) < x.shape[1]:
+    if rows <= 1:
+        return cols
+    if ld < cols:
         raise ValueError(f"{name}: rows overlap")
-    return x.stride(0)
+    return ld
 
 
 def _vector(x, name: str, n: int, dtypes, device) -> None:
-    if x.dtype not in dtypes:
-        raise TypeError(f"{name} has dtype {x.dtype}, expected one of {[str(d) for d in dtypes]}")
-    if x.device != device:
-        raise ValueError(f"{name} is on {x.device}, expected {device}")
+    if x.dtype not in dtypes or x.device != device:
+        _bad(x, name, x.shape, dtypes, device)
     if x.numel() != n or not x.is_contiguous():
         raise ValueError(f"{name} must hold {n} contiguous elements")
 
@@ -118,18 +139,22 @@ class _Plan:
             raise RuntimeError("iwp needs a CUDA device; there is no CPU fallback")
         self._torch = torch
         self.device = torch.device("cuda", torch.cuda.current_device())
-        lib()
-        self._ws = None
+        self._lib = lib()
+        self._ws, self._ws_at, self._ws_bytes = None, None, 0
+        self._floats = tuple(self._codes)
+        self._ids = (torch.int64, torch.int32)
+        self._raw_stream = torch._C._cuda_getCurrentRawStream  # current_stream() without the object around it
 
     def _stream(self) -> int:
-        return self._torch.cuda.current_stream(self.device).cuda_stream
+        return self._raw_stream(self.device.index)
 
     def _grow(self, need: int) -> None:
         if need < 0:
             raise IwpError(IWP_ERR_INVALID, "workspace size")
-        if self._ws is None or self._ws.numel() < need:
+        if self._ws_bytes < need:
             status = 0 if self._ws is None else self.status()
             self._ws = self._torch.empty(need, dtype=self._torch.uint8, device=self.device)
+            self._ws_at, self._ws_bytes = self._ws.data_ptr(), need
             _check(lib().iwp_loss_reset(self._ws.data_ptr(), self._stream()), "iwp_loss_reset")
             if status:  # a set status word outlives a larger workspace
                 self._ws[:4].view(self._torch.int32).fill_(status)
@@ -154,7 +179,7 @@ class HeadLoss(_Plan):
     """Output head [vocab, dim] with its loss; the logits are never kept.
 
     tokens: the most rows a call will bring (more are allowed: the workspace then grows once); top_k: the most teacher
-    logits per row; piece_bytes: bound on the probabilities held at a time while gradients are formed (0 = 512 MiB)."""
+    logits per row; piece_bytes: bound on the probabilities held at a time while gradients are formed (0 = 1 GiB)."""
 
     def __init__(self, tokens: int, vocab: int, dim: int, dtype=None, top_k: int = 1, piece_bytes: int = 0):
         super().__init__()
@@ -162,6 +187,7 @@ class HeadLoss(_Plan):
         self.vocab, self.dim, self.dtype, self.piece_bytes = int(vocab), int(dim), dtype or t.bfloat16, int(piece_bytes)
         if self.dtype not in (t.bfloat16, t.float16):
             raise TypeError("HeadLoss takes bfloat16 or float16 operands")
+        self._code, self._two, self._out_types = self._codes[self.dtype], (self.dtype,), (self.dtype, t.float32)
         a = HeadArgs(tokens=int(tokens), vocab=self.vocab, dim=self.dim, dtype=self._codes[self.dtype], top_k=int(top_k),
                      piece_bytes=self.piece_bytes)
         a.hidden_ld = a.weight_ld = (self.dim + 7) // 8 * 8
@@ -175,28 +201,30 @@ class HeadLoss(_Plan):
     # one call of iwp_head_loss
     def _run(self, hidden, weight, a: HeadArgs, *, grad, ignore_index=0, reduction="mean", lse=None, dloss=None, scale=1.0, dhidden=None,
              dweight=None, accumulate=False, want=("hidden", "weight")) -> HeadResult:
-        t, dev = self._torch, self.device
-        if hidden.dim() != 2 or weight.dim() != 2:
-            raise ValueError("hidden and weight are matrices")
-        T, two = hidden.shape[0], (self.dtype,)
-        a.tokens, a.vocab, a.dim, a.dtype, a.piece_bytes = T, self.vocab, self.dim, self._codes[self.dtype], self.piece_bytes
-        a.hidden_ld = _rows_of(hidden, "hidden", (T, self.dim), two, dev)
-        a.weight_ld = _rows_of(weight, "weight", (self.vocab, self.dim), two, dev)
+        t, dev, V, D = self._torch, self.device, self.vocab, self.dim
+        if hidden.dim() != 2:
+            raise ValueError("hidden is a matrix")
+        T, two = hidden.shape[0], self._two
+        a.tokens, a.vocab, a.dim, a.dtype, a.piece_bytes = T, V, D, self._code, self.piece_bytes
+        a.hidden_ld = _rows_of(hidden, "hidden", (T, D), two, dev)
+        a.weight_ld = _rows_of(weight, "weight", (V, D), two, dev)
         a.hidden, a.weight = hidden.data_ptr(), weight.data_ptr()
-        if reduction not in ("mean", "sum"):
+        if reduction == "mean":
+            a.mean = 1
+        elif reduction != "sum":
             raise ValueError("reduction is 'mean' or 'sum'")
-        a.mean, a.ignore_index, a.scale = int(reduction == "mean"), int(ignore_index), float(scale)
-        r = HeadResult()
+        a.ignore_index = ignore_index
         if lse is None:
             out = t.empty(2 * T + 1, dtype=t.float32, device=dev)
-            r.rows, r.lse, r.loss = out[:T], out[T : 2 * T], out[2 * T]
-            a.rows, a.lse, a.loss = r.rows.data_ptr(), r.lse.data_ptr(), r.loss.data_ptr()
+            r = HeadResult(out, None, T)
+            at = out.data_ptr()
+            a.rows, a.lse, a.loss = at, at + 4 * T, at + 8 * T
         else:
             _vector(lse, "lse", T, (t.float32,), dev)
-            r.lse, a.lse, a.have_lse = lse, lse.data_ptr(), 1
-        if T == 0 and lse is None:
-            a.lse = out.data_ptr()
+            r = HeadResult(None, lse, T)
+            a.lse, a.have_lse = lse.data_ptr() or 256, 1
         if grad:
+            a.scale = scale
             if dloss is not None:
                 if dloss.dim() == 0:
                     _vector(dloss, "dloss", 1, (t.float32,), dev)
@@ -204,46 +232,57 @@ class HeadLoss(_Plan):
                 else:
                     _vector(dloss, "dloss", T, (t.float32,), dev)
                     a.dloss_rows = dloss.data_ptr()
-            a.accumulate = int(accumulate)
-            for name, given, shape in (("hidden", dhidden, (T, self.dim)), ("weight", dweight, (self.vocab, self.dim))):
-                if name not in want:
-                    continue
-                if given is None:
-                    if accumulate:
-                        raise ValueError(f"accumulate needs d{name}")
-                    given = t.empty(shape, dtype=self.dtype, device=dev)
-                ld = _rows_of(given, "d" + name, shape, (self.dtype, t.float32), dev)
-                setattr(a, "d" + name, given.data_ptr() or 256)  # an empty tensor has no address
-                setattr(a, f"d{name}_ld", ld)
-                setattr(a, f"d{name}_type", self._codes[given.dtype])
-                setattr(r, "d" + name, given)
+            if accumulate:
+                a.accumulate = 1
+                if ("hidden" in want and dhidden is None) or ("weight" in want and dweight is None):
+                    raise ValueError("accumulate needs the gradients to add to")
+            if "hidden" in want:
+                if dhidden is None:
+                    dhidden, a.dhidden_ld, a.dhidden_type = t.empty((T, D), dtype=self.dtype, device=dev), D, self._code
+                else:
+                    a.dhidden_ld, a.dhidden_type = _rows_of(dhidden, "dhidden", (T, D), self._out_types, dev), self._codes[dhidden.dtype]
+                a.dhidden = dhidden.data_ptr() or 256  # an empty tensor has no address
+                r.dhidden = dhidden
+            if "weight" in want:
+                if dweight is None:
+                    dweight, a.dweight_ld, a.dweight_type = t.empty((V, D), dtype=self.dtype, device=dev), D, self._code
+                else:
+                    a.dweight_ld, a.dweight_type = _rows_of(dweight, "dweight", (V, D), self._out_types, dev), self._codes[dweight.dtype]
+                a.dweight = dweight.data_ptr()
+                r.dweight = dweight
         if T == 0:
             a.hidden = a.hidden or 256
-            a.targets = a.targets or (256 if not a.top_k else None)
-            a.top_ids, a.top_logits = a.top_ids or 256, a.top_logits or 256
-            a.lse = a.lse or 256
-        L = lib()
-        need = L.iwp_head_workspace(C.byref(a))
-        if self._ws.numel() < need or need < 0:
-            self._grow(need)
-        a.workspace, a.workspace_bytes = self._ws.data_ptr(), self._ws.numel()
-        _check(L.iwp_head_loss(C.byref(a), self._stream()), "iwp_head_loss")
+            if a.top_k:
+                a.top_ids, a.top_logits = a.top_ids or 256, a.top_logits or 256
+            else:
+                a.targets = a.targets or 256
+        a.workspace, a.workspace_bytes = self._ws_at, self._ws_bytes
+        ref = C.byref(a)
+        status = self._lib.iwp_head_loss(ref, self._raw_stream(dev.index))
+        if status == IWP_ERR_CAPACITY:  # more tokens, or rows that have to be copied, for the first time
+            self._grow(self._lib.iwp_head_workspace(ref))
+            a.workspace, a.workspace_bytes = self._ws_at, self._ws_bytes
+            status = self._lib.iwp_head_loss(ref, self._raw_stream(dev.index))
+        if status:
+            raise IwpError(status, "iwp_head_loss")
         return r
 
     def _hard(self, hidden, targets) -> HeadArgs:
-        _vector(targets, "targets", hidden.shape[0], (self._torch.int64,), self.device)
-        return HeadArgs(targets=targets.data_ptr(), temperature=1.0)
+        _vector(targets, "targets", hidden.shape[0], self._ids[:1], self.device)
+        a = HeadArgs()
+        a.targets, a.temperature = targets.data_ptr(), 1.0
+        return a
 
     def _soft(self, hidden, top_ids, top_logits, temperature) -> HeadArgs:
-        t = self._torch
         if top_ids.dim() != 2:
             raise ValueError("top_ids is a matrix")
         shape = (hidden.shape[0], top_ids.shape[1])
-        a = HeadArgs(temperature=float(temperature), top_k=shape[1])
-        a.top_ids_ld = _rows_of(top_ids, "top_ids", shape, (t.int64, t.int32), self.device)
-        a.top_logits_ld = _rows_of(top_logits, "top_logits", shape, tuple(self._codes), self.device)
+        a = HeadArgs()
+        a.temperature, a.top_k = temperature, shape[1]
+        a.top_ids_ld = _rows_of(top_ids, "top_ids", shape, self._ids, self.device)
+        a.top_logits_ld = _rows_of(top_logits, "top_logits", shape, self._floats, self.device)
         a.top_ids, a.top_logits = top_ids.data_ptr(), top_logits.data_ptr()
-        a.ids_bytes, a.top_type = (8 if top_ids.dtype == t.int64 else 4), self._codes[top_logits.dtype]
+        a.ids_bytes, a.top_type = (8 if top_ids.dtype is self._ids[0] else 4), self._codes[top_logits.dtype]
         return a
 
     def cross_entropy(self, hidden, weight, targets, *, ignore_index: int = -100, reduction: str = "mean") -> HeadResult:
@@ -286,28 +325,34 @@ class ExpertBalance(_Plan):
         if logits.dim() != 2 or ids.dim() != 2:
             raise ValueError("logits and ids are matrices")
         T, k = logits.shape[0], ids.shape[1]
-        a = BalanceArgs(tokens=T, experts=E, top_k=k, coef=float(coef), scale=float(scale))
-        a.logits_ld = _rows_of(logits, "logits", (T, E), tuple(self._codes), dev)
-        a.ids_ld = _rows_of(ids, "ids", (T, k), (t.int64, t.int32), dev)
-        a.logits, a.ids, a.type, a.ids_bytes = logits.data_ptr(), ids.data_ptr(), self._codes[logits.dtype], (8 if ids.dtype == t.int64 else 4)
+        a = BalanceArgs()
+        a.tokens, a.experts, a.top_k, a.coef, a.scale = T, E, k, coef, scale
+        a.logits_ld = _rows_of(logits, "logits", (T, E), self._floats, dev)
+        a.ids_ld = _rows_of(ids, "ids", (T, k), self._ids, dev)
+        a.logits, a.ids, a.type, a.ids_bytes = logits.data_ptr(), ids.data_ptr(), self._codes[logits.dtype], (8 if ids.dtype is self._ids[0] else 4)
         if mask is not None:
             _vector(mask, "mask", T, (t.bool, t.uint8), dev)
             a.mask = mask.data_ptr()
         out = t.empty(E + 1, dtype=t.float32, device=dev)
-        r = BalanceResult(loss=out[E], mean_prob=out[:E], counts=t.empty(E, dtype=t.int32, device=dev))
-        a.loss, a.mean_prob, a.counts = r.loss.data_ptr(), r.mean_prob.data_ptr(), r.counts.data_ptr()
+        counts = t.empty(E, dtype=t.int32, device=dev)
+        at = out.data_ptr()
+        a.mean_prob, a.loss, a.counts = at, at + 4 * E, counts.data_ptr()
         if grad:
             if dloss is not None:
                 _vector(dloss, "dloss", 1, (t.float32,), dev)
                 a.dloss = dloss.data_ptr()
-            r.dlogits = t.empty((T, E), dtype=logits.dtype, device=dev) if dlogits is None else dlogits
-            a.dlogits_ld = _rows_of(r.dlogits, "dlogits", (T, E), (logits.dtype,), dev)
-            a.dlogits = r.dlogits.data_ptr()
+            if dlogits is None:
+                dlogits, a.dlogits_ld = t.empty((T, E), dtype=logits.dtype, device=dev), E
+            else:
+                a.dlogits_ld = _rows_of(dlogits, "dlogits", (T, E), (logits.dtype,), dev)
+            a.dlogits = dlogits.data_ptr()
         if T == 0:
             a.logits, a.ids = a.logits or 256, a.ids or 256
-        a.workspace, a.workspace_bytes = self._ws.data_ptr(), self._ws.numel()
-        _check(lib().iwp_balance_loss(C.byref(a), self._stream()), "iwp_balance_loss")
-        return r
+        a.workspace, a.workspace_bytes = self._ws_at, self._ws_bytes
+        status = self._lib.iwp_balance_loss(C.byref(a), self._raw_stream(dev.index))
+        if status:
+            raise IwpError(status, "iwp_balance_loss")
+        return BalanceResult(out, counts, dlogits)
 
     def loss(self, logits, ids, mask=None, *, coef: float = 0.01) -> BalanceResult:
         """Loss, counts and mean probabilities of router logits [T, E] and chosen experts ids [T, k]."""
