@@ -19,7 +19,8 @@ namespace iwp_balance {
 namespace cg = cooperative_groups;
 
 constexpr int MAX_EXPERTS = 1024;
-constexpr int COUNT_BLOCKS = 32, COUNT_THREADS = 1024;
+constexpr int COUNT_BLOCKS = 128, COUNT_CLUSTER = 8, COUNT_THREADS = 512;  // 16 histograms come out of the 128 blocks
+constexpr int COUNT_PARTS = COUNT_BLOCKS / COUNT_CLUSTER, MAX_CLUSTER = 16;
 
 struct Header {
   int status;
@@ -34,7 +35,7 @@ struct Args {
   const uint8_t* mask;
   const float* dloss;
   void* dlogits;
-  int* part_counts;  // [COUNT_BLOCKS][E + 1]: counts, tokens; NULL: the cluster counts for itself
+  int* part_counts;  // [COUNT_PARTS][E + 1]: counts, tokens; NULL: the cluster counts for itself
   float* part;       // [gridDim.x][E]
   float* loss;
   float* mean_prob;
@@ -44,17 +45,31 @@ struct Args {
 };
 
 // Adds the ids of tokens [t0, t1) to a histogram in shared memory (cleared by the caller) and returns this thread's share
-// of the number of tokens.
+// of the number of tokens.  L lanes (a power of two) share a token, four tokens are in flight per lane.
 __device__ __forceinline__ int count_ids(const Args& a, int64_t t0, int64_t t1, int* hist) {
+  int L = 1;
+  while (L < 32 && L < a.k) L *= 2;
+  const int j0 = threadIdx.x & (L - 1);
+  const int64_t stride = blockDim.x / L;
   int n = 0;
-  for (int64_t i = t0 * a.k + threadIdx.x; i < t1 * a.k; i += blockDim.x) {
-    const int64_t t = i / a.k;
-    const int j = static_cast<int>(i - t * a.k);
-    if (a.mask && !a.mask[t]) continue;
-    n += j == 0;
-    const int64_t at = t * a.ids_ld + j;
-    const int64_t e = a.ids_bytes == 8 ? static_cast<const int64_t*>(a.ids)[at] : static_cast<const int32_t*>(a.ids)[at];
-    if (e >= 0 && e < a.E) atomicAdd(&hist[e], 1);
+  for (int64_t t = t0 + threadIdx.x / L; t < t1; t += 4 * stride) {
+    bool on[4];
+#pragma unroll
+    for (int u = 0; u < 4; u++) {
+      on[u] = t + u * stride < t1 && (!a.mask || a.mask[t + u * stride]);
+      n += on[u] && j0 == 0;
+    }
+    for (int j = j0; j < a.k; j += L) {
+      int64_t e[4];
+#pragma unroll
+      for (int u = 0; u < 4; u++) {
+        const int64_t at = (t + u * stride) * a.ids_ld + j;
+        e[u] = !on[u] ? -1 : a.ids_bytes == 8 ? static_cast<const int64_t*>(a.ids)[at] : static_cast<const int32_t*>(a.ids)[at];
+      }
+#pragma unroll
+      for (int u = 0; u < 4; u++)
+        if (e[u] >= 0 && e[u] < a.E) atomicAdd(&hist[e[u]], 1);
+    }
   }
   return n;
 }
@@ -68,8 +83,16 @@ __global__ void __launch_bounds__(COUNT_THREADS) k_balance_counts(const Args a) 
   const int64_t per = (a.T + gridDim.x - 1) / gridDim.x, t0 = blockIdx.x * per, t1 = min(a.T, t0 + per);
   const int n = __reduce_add_sync(0xFFFFFFFFu, count_ids(a, t0, t1, hist));
   if ((threadIdx.x & 31) == 0 && n) atomicAdd(&hist[a.E], n);
-  __syncthreads();
-  for (int e = threadIdx.x; e <= a.E; e += blockDim.x) a.part_counts[blockIdx.x * (a.E + 1) + e] = hist[e];
+  cg::cluster_group cluster = cg::this_cluster();
+  cluster.sync();
+  // the blocks of a cluster share out the experts
+  for (int e = cluster.block_rank() * blockDim.x + threadIdx.x; e <= a.E; e += COUNT_CLUSTER * blockDim.x) {
+    int c = 0;
+#pragma unroll
+    for (int b = 0; b < COUNT_CLUSTER; b++) c += cluster.map_shared_rank(hist, b)[e];
+    a.part_counts[blockIdx.x / COUNT_CLUSTER * (a.E + 1) + e] = c;
+  }
+  cluster.sync();  // nobody leaves while its counts are read
 }
 
 template <int TYPE>
@@ -85,6 +108,34 @@ struct Elem<IWP_F16> {
   using T = __half;
 };
 
+// Two floats at a time (sm_100's packed arithmetic): this kernel is bound by issue slots as much as by memory.
+using f2 = unsigned long long;
+__device__ __forceinline__ f2 pack(float a, float b) {
+  f2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 unpack(f2 x) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+  return r;
+}
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+  f2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ f2 add2(f2 a, f2 b) {
+  f2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+  f2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
 // Threads of a block, by the number of columns a lane holds (about five registers each).
 __host__ __device__ constexpr int threads_of(int columns) { return columns <= 8 ? 1024 : columns <= 16 ? 512 : 256; }
 
@@ -92,31 +143,35 @@ __host__ __device__ constexpr int threads_of(int columns) { return columns <= 8 
 template <int TYPE, int VEC, int N>
 __global__ void __launch_bounds__(threads_of(VEC* N), 1) k_balance_rows(const Args a, int G) {
   using E_t = typename Elem<TYPE>::T;
-  constexpr int THREADS = threads_of(VEC * N), WARPS = THREADS / 32;
+  constexpr int M = VEC * N, THREADS = threads_of(M), WARPS = THREADS / 32;
+  static_assert(M % 2 == 0, "columns go in pairs");
   struct alignas(sizeof(E_t) * VEC) Pack {
     E_t x[VEC];
   };
   __shared__ int sh_count[MAX_EXPERTS + 1];
   __shared__ float sh_f[MAX_EXPERTS];
   __shared__ float sh_sum[MAX_EXPERTS];
-  __shared__ float sh_warp[8192];  // [WARPS][E]: E <= 32 VEC N, so at most 8192
+  __shared__ float sh_warp[8192];  // [WARPS][E]: E <= 32 M, so at most 8192
   __shared__ float sh_loss[32];
   __shared__ bool last;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane & (G - 1);
   const bool alone = a.part_counts == nullptr;
 
-  // rows of this block's step s: from (s * gridDim.x + blockIdx.x) * rows on
+  // rows of this block's step s: from s * rows on
   const int rows = THREADS / G;
   const int64_t steps = (a.T + rows - 1) / rows;
-  Pack next[N];
+  union Next {
+    Pack p[N];
+    E_t x[M];
+  } next;
   bool next_on = false;
   auto fetch = [&](int64_t step) {
     const int64_t t = step * rows + tid / G;
     next_on = step < steps && t < a.T && (!a.mask || a.mask[t]);
+    const E_t* const from = static_cast<const E_t*>(a.logits) + t * a.logits_ld + g * VEC;
 #pragma unroll
     for (int n = 0; n < N; n++) {
-      const int e = (n * G + g) * VEC;
-      if (next_on && e < a.E) next[n] = *reinterpret_cast<const Pack*>(static_cast<const E_t*>(a.logits) + t * a.logits_ld + e);
+      if (next_on && (n * G + g) * VEC < a.E) next.p[n] = *reinterpret_cast<const Pack*>(from + n * G * VEC);
     }
   };
 
@@ -140,8 +195,11 @@ __global__ void __launch_bounds__(threads_of(VEC* N), 1) k_balance_rows(const Ar
       for (int i = 0; i < (MAX_EXPERTS + THREADS) / THREADS; i++) {
         total[i] = 0;
         const int e = tid + i * THREADS;
-        if (e <= a.E)
-          for (int b = 0; b < blocks; b++) total[i] += cluster.map_shared_rank(sh_count, b)[e];
+        if (e <= a.E) {
+#pragma unroll
+          for (int b = 0; b < MAX_CLUSTER; b++)
+            if (b < blocks) total[i] += cluster.map_shared_rank(sh_count, b)[e];
+        }
       }
       cluster.sync();  // everybody has read everybody's
 #pragma unroll
@@ -156,8 +214,8 @@ __global__ void __launch_bounds__(threads_of(VEC* N), 1) k_balance_rows(const Ar
     iwp_tc::wait_previous();
     for (int e = tid; e <= a.E; e += THREADS) {
       int c = 0;
-#pragma unroll 8
-      for (int b = 0; b < COUNT_BLOCKS; b++) c += __ldcg(a.part_counts + b * (a.E + 1) + e);
+#pragma unroll
+      for (int b = 0; b < COUNT_PARTS; b++) c += __ldcg(a.part_counts + b * (a.E + 1) + e);
       sh_count[e] = c;
     }
   }
@@ -173,69 +231,75 @@ __global__ void __launch_bounds__(threads_of(VEC* N), 1) k_balance_rows(const Ar
   __syncthreads();
 
   // ---- rows
-  float f[N][VEC], sum[N][VEC];
+  f2 cf[M / 2], sum[M / 2];  // c f_e
 #pragma unroll
-  for (int n = 0; n < N; n++)
-#pragma unroll
-    for (int v = 0; v < VEC; v++) {
-      const int e = (n * G + g) * VEC + v;
-      f[n][v] = e < a.E ? sh_f[e] : 0.f;
-      sum[n][v] = 0.f;
-    }
+  for (int i = 0; i < M; i += 2) {
+    const int e = (i / VEC * G + g) * VEC + i % VEC, e1 = ((i + 1) / VEC * G + g) * VEC + (i + 1) % VEC;
+    cf[i / 2] = pack(e < a.E ? c * sh_f[e] : 0.f, e1 < a.E ? c * sh_f[e1] : 0.f);
+    sum[i / 2] = pack(0.f, 0.f);
+  }
+  constexpr float LOG2E = 1.4426950408889634f;
+  const f2 log2e = pack(LOG2E, LOG2E);
   for (int64_t step = blockIdx.x; step < steps; step += gridDim.x) {
     const int64_t t = step * rows + tid / G;
     const bool on = next_on;
-    float x[N][VEC];
+    f2 x[M / 2];
     float top = -CUDART_INF_F;
 #pragma unroll
-    for (int n = 0; n < N; n++)
-#pragma unroll
-      for (int v = 0; v < VEC; v++) {
-        x[n][v] = on && (n * G + g) * VEC < a.E ? static_cast<float>(next[n].x[v]) : -CUDART_INF_F;
-        top = fmaxf(top, x[n][v]);
-      }
+    for (int i = 0; i < M; i += 2) {
+      const bool in0 = on && (i / VEC * G + g) * VEC < a.E, in1 = on && ((i + 1) / VEC * G + g) * VEC < a.E;
+      const float y0 = in0 ? static_cast<float>(next.x[i]) : -CUDART_INF_F, y1 = in1 ? static_cast<float>(next.x[i + 1]) : -CUDART_INF_F;
+      top = fmaxf(top, fmaxf(y0, y1));
+      x[i / 2] = pack(y0, y1);
+    }
     fetch(step + gridDim.x);
     for (int o = G >> 1; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-    const float ref = top == -CUDART_INF_F ? 0.f : top;
-    float s = 0.f, sf = 0.f;
+    const float ref = top == -CUDART_INF_F ? 0.f : -top;  // subtracted before the scaling, which lowest values would not survive
+    const f2 ref2 = pack(ref, ref);
+    f2 s2 = pack(0.f, 0.f), sf2 = s2;
 #pragma unroll
-    for (int n = 0; n < N; n++)
-#pragma unroll
-      for (int v = 0; v < VEC; v++) {
-        x[n][v] = __expf(x[n][v] - ref);
-        s += x[n][v];
-        sf = fmaf(x[n][v], f[n][v], sf);
-      }
+    for (int i = 0; i < M / 2; i++) {
+      const float2 y = unpack(mul2(add2(x[i], ref2), log2e));
+      x[i] = pack(iwp_tc::ex2(y.x), iwp_tc::ex2(y.y));
+      s2 = add2(s2, x[i]);
+      sf2 = fma2(x[i], cf[i], sf2);
+    }
+    float s = unpack(s2).x + unpack(s2).y, sf = unpack(sf2).x + unpack(sf2).y;
     for (int o = G >> 1; o; o >>= 1) {
       s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
       sf += __shfl_xor_sync(0xFFFFFFFFu, sf, o);
     }
     const float r = s == 0.f ? 0.f : 1.f / s;  // a row of nothing but -inf (or masked out): p = 0
-    sf *= r;
+    const f2 r2 = pack(r, r), minus = pack(-sf * r, -sf * r);
+    E_t* const to = static_cast<E_t*>(a.dlogits) + t * a.dlogits_ld + g * VEC;
+    const bool write = t < a.T && a.dlogits;
+#pragma unroll
+    for (int i = 0; i < M / 2; i++) {
+      x[i] = mul2(x[i], r2);
+      sum[i] = add2(sum[i], x[i]);
+      x[i] = mul2(x[i], add2(cf[i], minus));
+    }
 #pragma unroll
     for (int n = 0; n < N; n++) {
-      const int e = (n * G + g) * VEC;
       Pack p;
 #pragma unroll
       for (int v = 0; v < VEC; v++) {
-        const float prob = x[n][v] * r;
-        sum[n][v] += prob;
-        p.x[v] = static_cast<E_t>(on ? c * prob * (f[n][v] - sf) : 0.f);
+        const int i = n * VEC + v;
+        const float2 y = unpack(x[i / 2]);
+        p.x[v] = static_cast<E_t>(i % 2 ? y.y : y.x);
       }
-      if (t < a.T && a.dlogits && e < a.E) *reinterpret_cast<Pack*>(static_cast<E_t*>(a.dlogits) + t * a.dlogits_ld + e) = p;
+      if (write && (n * G + g) * VEC < a.E) *reinterpret_cast<Pack*>(to + n * G * VEC) = p;
     }
   }
 
   // ---- column sums: lanes of a warp, warps of the block, blocks; each in a fixed order
 #pragma unroll
-  for (int n = 0; n < N; n++)
-#pragma unroll
-    for (int v = 0; v < VEC; v++) {
-      float y = sum[n][v];
-      for (int o = G; o < 32; o <<= 1) y += __shfl_xor_sync(0xFFFFFFFFu, y, o);
-      const int e = (n * G + g) * VEC + v;
-      if (lane < G && e < a.E) sh_warp[warp * a.E + e] = y;
-    }
+  for (int i = 0; i < M; i++) {
+    float y = i % 2 ? unpack(sum[i / 2]).y : unpack(sum[i / 2]).x;
+    for (int o = G; o < 32; o <<= 1) y += __shfl_xor_sync(0xFFFFFFFFu, y, o);
+    const int e = (i / VEC * G + g) * VEC + i % VEC;
+    if (lane < G && e < a.E) sh_warp[warp * a.E + e] = y;
+  }
   __syncthreads();
   for (int e = tid; e < a.E; e += THREADS) {
     float y = 0.f;
@@ -253,7 +317,9 @@ __global__ void __launch_bounds__(threads_of(VEC* N), 1) k_balance_rows(const Ar
     if (blockIdx.x == 0)
       for (int e = tid; e < a.E; e += THREADS) {
         float y = 0.f;
-        for (int b = 0; b < static_cast<int>(gridDim.x); b++) y += gridDim.x > 1 ? cluster.map_shared_rank(sh_sum, b)[e] : sh_sum[e];
+#pragma unroll
+        for (int b = 0; b < MAX_CLUSTER; b++)
+          if (b < static_cast<int>(gridDim.x)) y += gridDim.x > 1 ? cluster.map_shared_rank(sh_sum, b)[e] : sh_sum[e];
         sh_warp[e] = y;
       }
     if (gridDim.x > 1) cluster.sync();  // nobody leaves while its sums are read

@@ -3,7 +3,8 @@
 //
 //   logits pass   z tile -> per row and 32 to 128 columns: maximum and sum of exp (written), the logits at the targets
 //                 and, for one piece of the vocabulary, 16-bit codes of how far z is below that maximum
-//   finish        per row: lse, loss; codes -> row_scale * (exp(z / tau - lse) - q) in the operands' type, in place
+//   rows          per row: lse, loss
+//   factors       codes -> row_scale * (exp(z / tau - lse) - q) in the operands' type, in place
 //   gradients     dweight = P^T hidden for the piece (complete, since the piece holds every token) and
 //                 dhidden = P weight for the piece, summed over the pieces in fp32
 //   other pieces  their probabilities come from a second logits product, in the operands' type at once
@@ -439,7 +440,7 @@ __global__ void __launch_bounds__(1024) k_row_scales(Header* hdr, Targets en, fl
   for (int64_t t = threadIdx.x; t < T; t += blockDim.x) scale[t] = m > 0.f ? dloss_rows[t] / m : dloss_rows[t];
 }
 
-// Number of rows with targets, for backward passes on their own (k_finish counts them otherwise).
+// Number of rows with targets, for backward passes on their own (k_rows counts them otherwise).
 __global__ void __launch_bounds__(1024) k_count_rows(Header* hdr, Targets en, int64_t T) {
   __shared__ int sh[32];
   iwp_tc::launch_next();
@@ -455,156 +456,95 @@ __global__ void __launch_bounds__(1024) k_count_rows(Header* hdr, Targets en, in
 
 // ---- finish of the forward pass --------------------------------------------------------------------------
 
-struct Finish {
+struct Rows {
   Header* hdr;
   Targets en;
-  const float2* part;
+  const float2* part;  // [T][parts]
   const float* z_at;
   float* rows;  // the caller's, or scratch
   float* lse;
   float* loss;
-  uint16_t* codes;  // codes -> factors, in place; NULL: losses only
-  int64_t T, ld;
-  int parts, part_shift, v0, width, chunk;  // a block takes `chunk` columns of one row
-  int chunks, mean, type;
-  float tau, up;
-  int log_codes;
+  int64_t T;
+  int parts, lanes, mean;
+  float tau;
 };
 
-constexpr int FINISH_THREADS = 256;
+constexpr int ROW_THREADS = 256;
 
 __device__ __forceinline__ float2 join(float2 a, float2 b) {  // (maximum, sum of 2^(x - maximum))
   const float m = fmaxf(a.x, b.x), ref = m == -CUDART_INF_F ? 0.f : m;
   return make_float2(m, a.y * ex2(a.x - ref) + b.y * ex2(b.x - ref));
 }
 
-// A block joins the parts of its row (in a fixed order), and turns one chunk of the row's codes into factors.  The
-// first chunk's block writes lse and loss; the last block to finish adds the rows' losses in a fixed order.
-__global__ void __launch_bounds__(FINISH_THREADS, 4) k_finish(const Finish a) {
-  constexpr int DEEP = 4, BATCH = DEEP * 8 * FINISH_THREADS;  // columns a block has in flight
-  constexpr int WARPS = FINISH_THREADS / 32, MINE = (MAX_TOP + FINISH_THREADS - 1) / FINISH_THREADS;
+// lse and loss of a row by a warp (lanes = 32), or by the block where there are few rows (lanes = 256); the last block to
+// finish adds the rows' losses in a fixed order.
+__global__ void __launch_bounds__(ROW_THREADS) k_rows(const Rows a) {
+  constexpr int WARPS = ROW_THREADS / 32;
   __shared__ float2 sh[WARPS];
   __shared__ float sh_sum[WARPS];
   __shared__ int sh_n[WARPS];
   __shared__ bool last;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  iwp_tc::launch_next();
   iwp_tc::wait_previous();
-  const int64_t row = blockIdx.x / a.chunks;
-  const int chunk = static_cast<int>(blockIdx.x - row * a.chunks);
-  const float2* const part = a.part + row * a.parts;
-  // the first columns are fetched while the row's statistics are joined
-  uint16_t* const codes = a.codes + row * a.ld;
-  const int c0 = chunk * a.chunk, c1 = min(c0 + a.chunk, a.width);  // within the piece
-  uint4 ahead[DEEP];
+  iwp_tc::launch_next();  // after the wait: whoever runs beside this kernel may read what the logits pass left
+  const int64_t row = a.lanes == 32 ? blockIdx.x * int64_t(WARPS) + warp : blockIdx.x;
+  const int me = a.lanes == 32 ? lane : tid;
+  if (row < a.T) {
+    // the row's target of this lane, fetched beside the parts
+    int column = NO_COLUMN;
+    float q = 0.f, z = 0.f;
+    if (me < a.en.k) {
+      column = a.en.column_at(row, me);
+      q = a.en.q_at(row, me);
+      if (column != NO_COLUMN) z = a.z_at[row * a.en.k + me];
+    }
+    const int state = a.en.state(row);
+    const float2* const part = a.part + row * a.parts;
+    float2 x = make_float2(-CUDART_INF_F, 0.f);
+#pragma unroll 4
+    for (int p = me; p < a.parts; p += a.lanes) x = join(x, part[p]);
 #pragma unroll
-  for (int i = 0; i < DEEP; i++) {
-    const int o = c0 + 8 * tid + i * 8 * FINISH_THREADS;
-    if (o < c1) ahead[i] = *reinterpret_cast<const uint4*>(codes + o);
-  }
-  float2 x = make_float2(-CUDART_INF_F, 0.f);
-  for (int p = tid; p < a.parts; p += FINISH_THREADS) x = join(x, part[p]);
+    for (int o = 16; o; o >>= 1) x = join(x, make_float2(__shfl_xor_sync(0xFFFFFFFFu, x.x, o), __shfl_xor_sync(0xFFFFFFFFu, x.y, o)));
+    if (a.lanes != 32) {
+      if (lane == 0) sh[warp] = x;
+      __syncthreads();
+      x = sh[0];
 #pragma unroll
-  for (int o = 16; o; o >>= 1) x = join(x, make_float2(__shfl_xor_sync(0xFFFFFFFFu, x.x, o), __shfl_xor_sync(0xFFFFFFFFu, x.y, o)));
-  if (lane == 0) sh[warp] = x;
-  __syncthreads();
-  x = sh[0];
-#pragma unroll
-  for (int w = 1; w < WARPS; w++) x = join(x, sh[w]);
-  const float lse2 = x.x + log2f(x.y), lse = lse2 * LN2;
-  const int state = a.en.state(row);
-  if (chunk == 0) {
+      for (int w = 1; w < WARPS; w++) x = join(x, sh[w]);
+    }
+    const float lse = (x.x + log2f(x.y)) * LN2;
     // q (lse - z / tau) entry by entry, so that a confident row keeps its small loss
-    float below = 0.f;
-    if (state == 1)
-      for (int k = tid; k < a.en.k; k += FINISH_THREADS) {
-        if (a.en.column_at(row, k) == NO_COLUMN) continue;
-        const float q = a.en.q_at(row, k);
-        if (q != 0.f) below += q * (lse - a.z_at[row * a.en.k + k] / a.tau);
-      }
+    float below = column != NO_COLUMN && q != 0.f ? q * (lse - z / a.tau) : 0.f;
+    for (int k = me + a.lanes; k < a.en.k; k += a.lanes) {
+      if (a.en.column_at(row, k) == NO_COLUMN) break;
+      const float qk = a.en.q_at(row, k);
+      if (qk != 0.f) below += qk * (lse - a.z_at[row * a.en.k + k] / a.tau);
+    }
     below = warp_sum(below);
-    if (lane == 0) sh_sum[warp] = below;
-    __syncthreads();
-    if (tid == 0) {
+    if (a.lanes != 32) {
+      if (lane == 0) sh_sum[warp] = below;
+      __syncthreads();
       below = 0.f;
       for (int w = 0; w < WARPS; w++) below += sh_sum[w];
+      __syncthreads();
+    }
+    if (me == 0) {
       const float c = a.en.hard ? 0.f : a.en.const_term[row];
       a.lse[row] = lse;
       a.rows[row] = state == 0 ? 0.f : state < 0 ? CUDART_NAN_F : a.tau * a.tau * (c + below);
       if (state < 0) atomicExch(&a.hdr->status, IWP_ERR_INVALID);
+      __threadfence();
     }
-  }
-  if (a.codes) {
-    const float scale = a.en.row_scale(row) * a.up;
-    auto probability = [&](int col, uint32_t code) {  // m = the part's maximum less lse2, in log2
-      const float m = part[(a.v0 + col) >> a.part_shift].x - lse2;
-      return a.log_codes ? ex2(m + log_value(code)) : __half2float(__ushort_as_half(static_cast<uint16_t>(code))) * ex2(m - 15.f);
-    };
-    int at[MINE];
-    float to[MINE];
-#pragma unroll
-    for (int i = 0; i < MINE; i++) {
-      const int k = tid + i * FINISH_THREADS;
-      at[i] = -1;
-      if (k < a.en.k && scale != 0.f) {
-        const int col = a.en.column_at(row, k);
-        const float q = a.en.q_at(row, k);
-        if (col != NO_COLUMN && q != 0.f && col >= a.v0 + c0 && col < a.v0 + c1) {
-          at[i] = col - a.v0;
-          to[i] = (probability(at[i], codes[at[i]]) - q) * scale;
-        }
-      }
-    }
-    __syncthreads();
-    for (int c = c0 + 8 * tid; c < c1; c += BATCH) {
-      uint4 u[DEEP];
-      float m[DEEP];
-#pragma unroll
-      for (int i = 0; i < DEEP; i++) {
-        const int o = c + i * 8 * FINISH_THREADS;
-        if (o < c1) {
-          u[i] = c == c0 + 8 * tid ? ahead[i] : *reinterpret_cast<const uint4*>(codes + o);
-          m[i] = part[(a.v0 + o) >> a.part_shift].x - lse2;
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < DEEP; i++) {
-        const int o = c + i * 8 * FINISH_THREADS;
-        if (o >= c1) break;
-        uint32_t* const e = reinterpret_cast<uint32_t*>(&u[i]);
-        if (scale == 0.f) {  // a row that gives nothing, whatever its logits are
-          u[i] = make_uint4(0u, 0u, 0u, 0u);
-        } else if (a.log_codes) {
-#pragma unroll
-          for (int j = 0; j < 4; j++)
-            e[j] = iwp_tc::pack2(ex2(m[i] + log_value(e[j] & 0xFFFFu)) * scale, ex2(m[i] + log_value(e[j] >> 16)) * scale, IWP_F16);
-        } else {
-          const float f = ex2(m[i] - 15.f) * scale;
-#pragma unroll
-          for (int j = 0; j < 4; j++) {
-            const float2 x = iwp_tc::unpack2(e[j], IWP_F16);
-            e[j] = iwp_tc::pack2(x.x * f, x.y * f, IWP_BF16);
-          }
-        }
-        *reinterpret_cast<uint4*>(codes + o) = u[i];
-      }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < MINE; i++)
-      if (at[i] >= 0) iwp_tc::store_as(codes, at[i], to[i], a.type);
   }
   __syncthreads();
-  if (tid == 0) {
-    __threadfence();
-    last = atomicInc(&a.hdr->ticket, gridDim.x - 1) == gridDim.x - 1;
-  }
+  if (tid == 0) last = atomicInc(&a.hdr->ticket, gridDim.x - 1) == gridDim.x - 1;
   __syncthreads();
   if (!last) return;
   __threadfence();
   float sum = 0.f;
   int n = 0;
-  for (int64_t t = tid; t < a.T; t += FINISH_THREADS) {
+#pragma unroll 4
+  for (int64_t t = tid; t < a.T; t += ROW_THREADS) {
     sum += __ldcg(a.rows + t);
     n += a.en.state(t) != 0;
   }
@@ -620,12 +560,209 @@ __global__ void __launch_bounds__(FINISH_THREADS, 4) k_finish(const Finish a) {
   }
 }
 
-// Rows of `cols` 16-bit elements to rows of `ld_to` (a multiple of 8), for operands TMA cannot address.
+// ---- codes of the kept piece -> factors ------------------------------------------------------------------------
+
+struct Factors {
+  Targets en;
+  const float2* part;  // [T][parts]
+  const float* lse;
+  uint16_t* codes;  // [T][ld], in place
+  int64_t ld;
+  int parts, part_shift, v0, width, chunks, log_codes;
+  float up;
+};
+
+constexpr int FACTOR_THREADS = 256, FACTOR_DEEP = 4, FACTOR_COLUMNS = 8 * FACTOR_THREADS * FACTOR_DEEP;
+
+// A block takes FACTOR_COLUMNS columns of one row: bound by memory, 2 bytes in and 2 out per element.
+__global__ void __launch_bounds__(FACTOR_THREADS) k_factors(const Factors a) {
+  constexpr int MINE = (MAX_TOP + FACTOR_THREADS - 1) / FACTOR_THREADS;
+  const int tid = threadIdx.x;
+  const int64_t row = blockIdx.x / a.chunks;
+  uint16_t* const codes = a.codes + row * a.ld;
+  const float2* const part = a.part + row * a.parts;
+  const int c0 = static_cast<int>(blockIdx.x - row * a.chunks) * FACTOR_COLUMNS, c1 = min(c0 + FACTOR_COLUMNS, a.width);
+  iwp_tc::launch_next();
+  // what the logits pass and the targets' kernel left is complete: k_rows started after them, and this kernel after that
+  uint4 u[FACTOR_DEEP];
+  float m[FACTOR_DEEP];
+#pragma unroll
+  for (int i = 0; i < FACTOR_DEEP; i++) {
+    const int o = c0 + 8 * tid + i * 8 * FACTOR_THREADS;
+    if (o < c1) {
+      u[i] = *reinterpret_cast<const uint4*>(codes + o);
+      m[i] = part[(a.v0 + o) >> a.part_shift].x;
+    }
+  }
+  const float scale = a.en.row_scale(row) * a.up;
+  auto probability = [&](float top, uint32_t code) {  // top = the part's maximum less lse, in log2
+    return a.log_codes ? ex2(top + log_value(code)) : __half2float(__ushort_as_half(static_cast<uint16_t>(code))) * ex2(top - 15.f);
+  };
+  int at[MINE];
+  uint32_t code[MINE];
+  bool any = false;
+#pragma unroll
+  for (int i = 0; i < MINE; i++) {
+    const int k = tid + i * FACTOR_THREADS;
+    at[i] = -1;
+    if (k < a.en.k) {
+      const int col = a.en.column_at(row, k);
+      if (col >= a.v0 + c0 && col < a.v0 + c1 && a.en.q_at(row, k) != 0.f) {
+        at[i] = col - a.v0;
+        code[i] = codes[at[i]];
+        any = true;
+      }
+    }
+  }
+  iwp_tc::wait_previous();
+  const float lse2 = a.lse[row] * LOG2E;
+  any = __syncthreads_or(any);  // and nobody's code is overwritten before it was read
+#pragma unroll
+  for (int i = 0; i < FACTOR_DEEP; i++) {
+    const int o = c0 + 8 * tid + i * 8 * FACTOR_THREADS;
+    if (o >= c1) break;
+    uint32_t* const e = reinterpret_cast<uint32_t*>(&u[i]);
+    const float top = m[i] - lse2;
+    if (scale == 0.f) {  // a row that gives nothing, whatever its logits are
+      u[i] = make_uint4(0u, 0u, 0u, 0u);
+    } else if (a.log_codes) {
+#pragma unroll
+      for (int j = 0; j < 4; j++)
+        e[j] = iwp_tc::pack2(ex2(top + log_value(e[j] & 0xFFFFu)) * scale, ex2(top + log_value(e[j] >> 16)) * scale, IWP_F16);
+    } else {
+      const float f = ex2(top - 15.f) * scale;
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        const float2 x = iwp_tc::unpack2(e[j], IWP_F16);
+        e[j] = iwp_tc::pack2(x.x * f, x.y * f, IWP_BF16);
+      }
+    }
+    *reinterpret_cast<uint4*>(codes + o) = u[i];
+  }
+  if (!any || scale == 0.f) return;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < MINE; i++)
+    if (at[i] >= 0) {
+      const float p = probability(part[(a.v0 + at[i]) >> a.part_shift].x - lse2, code[i]);
+      iwp_tc::store_as(codes, at[i], (p - a.en.q_at(row, tid + i * FACTOR_THREADS)) * scale, a.log_codes ? IWP_F16 : IWP_BF16);
+    }
+}
+
+// ---- forward pass of a few tokens -------------------------------------------------------------------------------
+
+struct Few {
+  Targets en;
+  const void* hidden;
+  const void* weight;
+  float2* part;  // [T][blocks]
+  float* z_at;
+  int64_t hidden_ld, weight_ld;
+  int T, V, D, type, blocks;  // the first `blocks` blocks share the vocabulary, the others take the targets' logits
+  float c;
+};
+
+constexpr int FEW_TOKENS = 4, FEW_THREADS = 512, FEW_ROWS = 4;
+
+// Four columns of weight rows per warp at a time, streamed once: a dot product with at most four tokens is bound by the
+// weights' bytes, and plain loads keep more of them in flight than the tensor cores' 128-row tiles would.  Operand rows
+// start at multiples of 16 bytes and hold whole ones (copies made by k_align_rows end in zeros).
+template <int TOKENS>
+__global__ void __launch_bounds__(FEW_THREADS) k_few_tokens(const Few a) {
+  constexpr int WARPS = FEW_THREADS / 32;
+  extern __shared__ uint4 sh_hidden[];  // [TOKENS][D / 8, rounded up]
+  __shared__ float2 sh[WARPS][TOKENS];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int groups = (a.D + 7) / 8;
+  iwp_tc::launch_next();
+  iwp_tc::wait_previous();
+  const uint16_t* const hidden = static_cast<const uint16_t*>(a.hidden);
+  const uint16_t* const weight = static_cast<const uint16_t*>(a.weight);
+  for (int i = tid; i < TOKENS * groups; i += FEW_THREADS) {
+    const int t = i / groups, g = i - t * groups;
+    const uint4 x = *reinterpret_cast<const uint4*>(hidden + t * a.hidden_ld + 8 * g);
+    sh_hidden[i] = x;
+  }
+  __syncthreads();
+  auto dot8 = [&](const uint4& w, int g, float (&acc)[TOKENS]) {
+    const uint32_t* const we = reinterpret_cast<const uint32_t*>(&w);
+    float2 y[4];
+#pragma unroll
+    for (int j = 0; j < 4; j++) y[j] = iwp_tc::unpack2(we[j], a.type);
+#pragma unroll
+    for (int t = 0; t < TOKENS; t++) {
+      const uint4 h = sh_hidden[t * groups + g];
+      const uint32_t* const he = reinterpret_cast<const uint32_t*>(&h);
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        const float2 x = iwp_tc::unpack2(he[j], a.type);
+        acc[t] = fmaf(x.x, y[j].x, fmaf(x.y, y[j].y, acc[t]));
+      }
+    }
+  };
+  auto load8 = [&](const uint16_t* row, int g) { return __ldcs(reinterpret_cast<const uint4*>(row + 8 * g)); };
+  if (static_cast<int>(blockIdx.x) >= a.blocks) {  // logits at the targets, a warp each
+    const int i = (blockIdx.x - a.blocks) * WARPS + warp;
+    if (i >= a.T * a.en.k) return;
+    const int t = i / a.en.k, col = a.en.column_at(t, i - t * a.en.k);
+    if (col == NO_COLUMN) return;
+    float acc[TOKENS] = {};
+    for (int g = lane; g < groups; g += 32) dot8(load8(weight + col * a.weight_ld, g), g, acc);
+    float z = 0.f;
+#pragma unroll
+    for (int j = 0; j < TOKENS; j++)
+      if (j == t) z = acc[j];
+    z = warp_sum(z);
+    if (lane == 0) a.z_at[i] = z;
+    return;
+  }
+  float m[TOKENS], s[TOKENS];
+#pragma unroll
+  for (int t = 0; t < TOKENS; t++) m[t] = -CUDART_INF_F, s[t] = 0.f;
+  for (int v = (blockIdx.x * WARPS + warp) * FEW_ROWS; v < a.V; v += a.blocks * WARPS * FEW_ROWS) {
+    float acc[FEW_ROWS][TOKENS] = {};
+    const uint16_t* const row = weight + v * a.weight_ld;
+    const int have = min(FEW_ROWS, a.V - v);
+#pragma unroll 2
+    for (int g = lane; g < groups; g += 32) {
+      uint4 w[FEW_ROWS];
+#pragma unroll
+      for (int r = 0; r < FEW_ROWS; r++) w[r] = load8(row + min(r, have - 1) * a.weight_ld, g);
+#pragma unroll
+      for (int r = 0; r < FEW_ROWS; r++) dot8(w[r], g, acc[r]);
+    }
+#pragma unroll
+    for (int t = 0; t < TOKENS; t++) {
+      float z[FEW_ROWS], top = m[t];
+#pragma unroll
+      for (int r = 0; r < FEW_ROWS; r++) {
+        z[r] = r < have ? warp_sum(acc[r][t]) * a.c : -CUDART_INF_F;
+        top = fmaxf(top, z[r]);
+      }
+      const float ref = top == -CUDART_INF_F ? 0.f : top;
+      s[t] *= ex2(m[t] - ref);
+#pragma unroll
+      for (int r = 0; r < FEW_ROWS; r++) s[t] += ex2(z[r] - ref);
+      m[t] = top;
+    }
+  }
+  if (lane == 0)
+#pragma unroll
+    for (int t = 0; t < TOKENS; t++) sh[warp][t] = make_float2(m[t], s[t]);
+  __syncthreads();
+  if (tid < TOKENS) {
+    float2 x = sh[0][tid];
+    for (int w = 1; w < WARPS; w++) x = join(x, sh[w][tid]);
+    a.part[tid * a.blocks + blockIdx.x] = x;
+  }
+}
+
+// Rows of `cols` 16-bit elements to rows of `ld_to` (a multiple of 8; zeros at the end), for operands TMA cannot address.
 __global__ void k_align_rows(const uint16_t* from, int64_t ld_from, uint16_t* to, int64_t ld_to, int64_t rows, int cols) {
   iwp_tc::launch_next();
   iwp_tc::wait_previous();
   for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
-    for (int c = threadIdx.x; c < cols; c += blockDim.x) to[r * ld_to + c] = from[r * ld_from + c];
+    for (int c = threadIdx.x; c < ld_to; c += blockDim.x) to[r * ld_to + c] = c < cols ? from[r * ld_from + c] : uint16_t(0);
 }
 
 }  // namespace iwp_head

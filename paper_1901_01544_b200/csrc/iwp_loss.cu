@@ -19,6 +19,8 @@ namespace {
 constexpr int64_t MAX_SIZE = 0x7FFFFFFF;
 constexpr int64_t DEFAULT_PIECE = int64_t(1) << 30;
 constexpr int FEW_TILES = 296;           // four per CTA pair: above this a product takes its widest tiles
+constexpr int FEW_BLOCKS = 296;           // of the pass over a few tokens: two per SM
+constexpr int64_t FEW_ELEMENTS = 4 * 5888;  // whose hidden rows stay in 48 KB of shared memory
 constexpr int64_t JOIN_TILES = 2 * 148;  // a split dhidden has at most this many partial tiles
 
 inline int64_t up_to(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
@@ -212,7 +214,7 @@ int launch_product(const iwp_tc::Problems<N>& w, const typename Epi::Args& args,
 // ---- output head ----------------------------------------------------------------------------------------
 
 struct HeadPlan {
-  bool grad, pack_hidden, pack_weight;
+  bool grad, few, pack_hidden, pack_weight;
   int64_t k, piece, pieces, d_pad;
   // offsets into the workspace
   int64_t column, q, const_term, row_scale, rows, z_at, part, hidden, weight, probs, join, bytes;
@@ -238,6 +240,7 @@ HeadPlan head_plan(const iwp_head_args* a) {
   p.d_pad = up_to(D, 8);
   p.pack_hidden = needs_copy(a->hidden, a->hidden_ld);
   p.pack_weight = needs_copy(a->weight, a->weight_ld);
+  p.few = !p.grad && T <= iwp_head::FEW_TOKENS && T * D <= FEW_ELEMENTS && (D % 8 == 0 || (p.pack_hidden && p.pack_weight));
   int64_t at = 256;
   auto take = [&at](int64_t n) {
     const int64_t o = at;
@@ -255,7 +258,7 @@ HeadPlan head_plan(const iwp_head_args* a) {
     p.z_at = take(4 * p.k * T);
     // a part is half a tile of at least 64 columns; narrow tiles are taken where those of 256 columns would be few
     // (FEW_TILES), i.e. at most 8 parts of 8 bytes for each of a tile's 256 rows
-    const int64_t wide = 8 * T * 2 * tiles_of(V, 256), narrow = 8 * T * 2 * tiles_of(V, 64), most = int64_t(FEW_TILES) * 256 * 64;
+    const int64_t wide = 8 * T * 2 * tiles_of(V, 256) + 8 * iwp_head::FEW_TOKENS * FEW_BLOCKS, narrow = 8 * T * 2 * tiles_of(V, 64), most = int64_t(FEW_TILES) * 256 * 64;
     p.part = take(wide > most ? wide : narrow < most ? narrow : most);
   }
   if (p.pack_hidden) p.hidden = take(2 * T * p.d_pad);
@@ -336,6 +339,47 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
   uint16_t* const probs = reinterpret_cast<uint16_t*>(ws + p.probs);
   const int64_t kept = p.grad && !a->have_lse ? p.pieces - 1 : -1;  // the piece whose codes the logits pass leaves behind
   if (!a->have_lse) {
+    H::Rows ra{};
+    ra.hdr = hdr;
+    ra.en = en;
+    ra.part = reinterpret_cast<float2*>(ws + p.part);
+    ra.z_at = reinterpret_cast<float*>(ws + p.z_at);
+    ra.rows = a->rows ? a->rows : reinterpret_cast<float*>(ws + p.rows);
+    ra.lse = a->lse;
+    ra.loss = a->loss;
+    ra.T = T;
+    ra.mean = a->mean;
+    ra.tau = tau;
+    ra.lanes = T < 4 * sms ? H::ROW_THREADS : 32;  // a block per row while that fills the device, a warp after that
+    const int64_t row_blocks = ra.lanes == 32 ? tiles_of(T, H::ROW_THREADS / 32) : T;
+    if (p.few) {
+      H::Few fa{};
+      fa.en = en;
+      fa.hidden = h.p;
+      fa.weight = w.p;
+      fa.part = reinterpret_cast<float2*>(ws + p.part);
+      fa.z_at = reinterpret_cast<float*>(ws + p.z_at);
+      fa.hidden_ld = h.ld;
+      fa.weight_ld = w.ld;
+      fa.T = static_cast<int>(T);
+      fa.V = static_cast<int>(V);
+      fa.D = static_cast<int>(D);
+      fa.type = a->dtype;
+      fa.c = c;
+      constexpr int warps = H::FEW_THREADS / 32;
+      const int64_t whole = tiles_of(V, warps * H::FEW_ROWS);
+      fa.blocks = static_cast<int>(whole < FEW_BLOCKS ? whole : FEW_BLOCKS);
+      const int64_t grid = fa.blocks + tiles_of(T * p.k, warps);
+      const size_t smem = static_cast<size_t>(16 * T * tiles_of(D, 8));
+      ra.parts = fa.blocks;
+      LOSS_CUDA(launch(T == 1   ? H::k_few_tokens<1>
+                       : T == 2 ? H::k_few_tokens<2>
+                       : T == 3 ? H::k_few_tokens<3>
+                                : H::k_few_tokens<4>,
+                       grid, H::FEW_THREADS, smem, 1, st, fa));
+      LOSS_CUDA(launch(H::k_rows, row_blocks, H::ROW_THREADS, 0, 1, st, ra));
+      return IWP_OK;
+    }
     const Shape shape{T, V, D};
     const int tile_n = pick_tile_n(shape, pairs);
     iwp_tc::Problems<1> work;
@@ -359,34 +403,24 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
     la.width = static_cast<int>(kept >= 0 ? p.piece : 0);
     la.log_codes = a->dtype == IWP_F16;
     if (int e = launch_product<H::Logits, 1>(work, la, st)) return e;
-    H::Finish fa{};
-    fa.hdr = hdr;
-    fa.en = en;
-    fa.part = la.part;
-    fa.z_at = la.z_at;
-    fa.rows = a->rows ? a->rows : reinterpret_cast<float*>(ws + p.rows);
-    fa.lse = a->lse;
-    fa.loss = a->loss;
-    fa.T = T;
-    fa.parts = la.parts;
-    fa.part_shift = tile_n == 256 ? 7 : tile_n == 128 ? 6 : 5;
-    fa.mean = a->mean;
-    fa.tau = tau;
-    fa.chunks = 1;
+    ra.parts = la.parts;
+    LOSS_CUDA(launch(H::k_rows, row_blocks, H::ROW_THREADS, 0, 1, st, ra));
     if (kept >= 0) {
+      H::Factors fa{};
+      fa.en = en;
+      fa.part = la.part;
+      fa.lse = a->lse;
       fa.codes = probs;
       fa.ld = p.piece;
+      fa.parts = la.parts;
+      fa.part_shift = tile_n == 256 ? 7 : tile_n == 128 ? 6 : 5;
       fa.v0 = la.v0;
       fa.width = static_cast<int>(V - fa.v0 < p.piece ? V - fa.v0 : p.piece);
-      // a few thousand columns per block, less where the rows alone do not fill the device
-      int64_t chunk = up_to(tiles_of(T * fa.width, 8 * sms), 2048);
-      fa.chunk = static_cast<int>(chunk > 32768 ? 32768 : chunk);
-      fa.chunks = static_cast<int>(tiles_of(fa.width, fa.chunk));
-      fa.type = a->dtype;
-      fa.up = up;
+      fa.chunks = static_cast<int>(tiles_of(fa.width, H::FACTOR_COLUMNS));
       fa.log_codes = la.log_codes;
+      fa.up = up;
+      LOSS_CUDA(launch(H::k_factors, T * fa.chunks, H::FACTOR_THREADS, 0, 1, st, fa));
     }
-    LOSS_CUDA(launch(H::k_finish, T * fa.chunks, H::FINISH_THREADS, 0, 1, st, fa));
   }
   if (!p.grad) return IWP_OK;
 
@@ -492,7 +526,7 @@ constexpr int BALANCE_BLOCKS = 148;  // at most, of the rows kernel
 // Up to this many bytes of logits and ids one cluster serves: it saves the second launch and its 16 SMs keep up.
 constexpr int64_t CLUSTER_BYTES = int64_t(3) << 20;
 
-int64_t balance_part_counts_bytes(int E) { return up_to(int64_t(iwp_balance::COUNT_BLOCKS) * (E + 1) * 4, 256); }
+int64_t balance_part_counts_bytes(int E) { return up_to(int64_t(iwp_balance::COUNT_PARTS) * (E + 1) * 4, 256); }
 
 template <int TYPE, int VEC, int N>
 int balance_launch(iwp_balance::Args a, int G, cudaStream_t st) {
@@ -504,7 +538,7 @@ int balance_launch(iwp_balance::Args a, int G, cudaStream_t st) {
   if (bytes <= CLUSTER_BYTES) {
     // CTAs for about two rounds of rows each; 16 need the opt-in to clusters above the portable size
     int ctas = 1;
-    while (ctas < 16 && 2 * ctas < steps) ctas *= 2;
+    while (ctas < B::MAX_CLUSTER && 2 * ctas < steps) ctas *= 2;
     a.part_counts = nullptr;
     static bool opted[MAX_DEVICES] = {};
     const int dev = device();
@@ -516,21 +550,23 @@ int balance_launch(iwp_balance::Args a, int G, cudaStream_t st) {
     LOSS_CUDA(launch(kernel, ctas, threads, 0, ctas, st, a, G));
     return IWP_OK;
   }
-  LOSS_CUDA(launch(B::k_balance_counts, B::COUNT_BLOCKS, B::COUNT_THREADS, 0, 1, st, a));
+  LOSS_CUDA(launch(B::k_balance_counts, B::COUNT_BLOCKS, B::COUNT_THREADS, 0, B::COUNT_CLUSTER, st, a));
   LOSS_CUDA(launch(kernel, steps < BALANCE_BLOCKS ? steps : BALANCE_BLOCKS, threads, 0, 1, st, a, G));
   return IWP_OK;
 }
 
-// A lane holds VEC neighbouring columns at a time (as many as rows are aligned for, up to 16 bytes), N times.
+// A lane holds VEC neighbouring columns at a time (as many as rows are aligned for, up to 16 bytes), N times: 16
+// columns, so that few lanes share a row and the sums over a row take few shuffles; fewer or more of them where a
+// row has at most 8 columns or more than 512.
 template <int TYPE, int VEC>
 int balance_rows(const iwp_balance::Args& a, cudaStream_t st) {
+  constexpr int LITTLE = VEC >= 8 ? 8 : 4, LARGE = iwp_balance::MAX_EXPERTS / 32;
+  const int columns = a.E <= 8 ? LITTLE : a.E <= 512 ? 16 : LARGE;
   int G = 1;
-  while (G < 32 && G * VEC < a.E) G *= 2;
-  const int64_t need = tiles_of(a.E, int64_t(G) * VEC);
-  constexpr int MIDDLE = VEC >= 8 ? 1 : 8 / VEC, MOST = iwp_balance::MAX_EXPERTS / 32 / VEC;
-  if (need <= 1) return balance_launch<TYPE, VEC, 1>(a, G, st);
-  if (need <= MIDDLE) return balance_launch<TYPE, VEC, MIDDLE>(a, G, st);
-  return balance_launch<TYPE, VEC, MOST>(a, G, st);
+  while (G * columns < a.E) G *= 2;
+  if (columns == LITTLE) return balance_launch<TYPE, VEC, LITTLE / VEC>(a, G, st);
+  if (columns == 16) return balance_launch<TYPE, VEC, 16 / VEC>(a, G, st);
+  return balance_launch<TYPE, VEC, LARGE / VEC>(a, G, st);
 }
 
 template <int TYPE>

@@ -497,3 +497,35 @@ def test_balance_refuses_wrong_tensors():
         plan.loss(x, torch.zeros(20, 17, dtype=torch.int64, device=DEV))
     with pytest.raises(losses.IwpError):
         losses.ExpertBalance(20, 1025)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("T,V,D", [(1, 32768, 1024), (1, 5, 8), (2, 1003, 520), (3, 4099, 4096), (4, 700, 24), (4, 64, 1001), (2, 129, 7), (5, 3000, 64),
+                                   (4, 300, 8192)])
+def test_forward_of_a_few_tokens(T, V, D, dtype):
+    h, w, y, g = operands(T, V, D, dtype, 100 + T + V)
+    ref = head_reference(h, w, y[:, None], torch.ones(T, 1, dtype=torch.float64, device=DEV), 1.0, True)
+    plan = losses.HeadLoss(T, V, D, dtype, top_k=5)
+    check_head(plan.cross_entropy(h, w, y), ref, grad=False)
+    K = min(5, V)
+    ids = torch.rand(T, V, generator=g, device=DEV).argsort(1)[:, :K].contiguous()
+    logits = torch.randn(T, K, generator=g, device=DEV)
+    ids[0, 0] = -1 if K > 1 else ids[0, 0]
+    ref = head_reference(h, w, ids, soft_targets(ids, logits, 3.0), 3.0, False)
+    check_head(plan.distill(h, w, ids, logits, 3.0, reduction="sum"), ref, grad=False)
+    wide = torch.zeros(V, D + 8, dtype=dtype, device=DEV)  # strided rows, and rows that end where 8 does not divide them
+    wide[:, :D] = w
+    ref = head_reference(h, w, y[:, None], torch.ones(T, 1, dtype=torch.float64, device=DEV), 1.0, True)
+    check_head(plan.cross_entropy(h, wide[:, :D], y), ref, grad=False)
+    assert plan.status() == 0
+
+
+def test_repeated_teacher_ids_add_up():
+    T, V, D, K = 50, 400, 64, 12
+    h, w, _, g = operands(T, V, D, BF, 200)
+    ids = torch.randint(0, 6, (T, K), generator=g, device=DEV)  # many equal ones
+    logits = torch.randn(T, K, generator=g, device=DEV)
+    plan = losses.HeadLoss(T, V, D, BF, top_k=K)
+    check_head(plan.distill_grad(h, w, ids, logits, 1.5), head_reference(h, w, ids, soft_targets(ids, logits, 1.5), 1.5, True))
+    small = losses.HeadLoss(T, V, D, BF, top_k=K, piece_bytes=1)
+    check_head(small.distill_grad(h, w, ids, logits, 1.5), head_reference(h, w, ids, soft_targets(ids, logits, 1.5), 1.5, True))
