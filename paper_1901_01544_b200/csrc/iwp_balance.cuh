@@ -36,7 +36,7 @@ struct Args {
   const float* dloss;
   void* dlogits;
   int* part_counts;  // [COUNT_PARTS][E + 1]: counts, tokens; NULL: the cluster counts for itself
-  float* part;       // [gridDim.x][E]
+  float* part;       // [gridDim.x][padded(E)]
   float* loss;
   float* mean_prob;
   int64_t logits_ld, dlogits_ld, ids_ld, T;
@@ -44,31 +44,40 @@ struct Args {
   float coef, scale;
 };
 
+// Row stride of the blocks' column sums.
+__host__ __device__ constexpr int padded(int E) { return (E + 3) / 4 * 4; }
+
 // Adds the ids of tokens [t0, t1) to a histogram in shared memory (cleared by the caller) and returns this thread's share
-// of the number of tokens.  L lanes (a power of two) share a token, four tokens are in flight per lane.
+// of the number of tokens.  L lanes (a power of two) share a token; `AHEAD` tokens are in flight per lane.
 __device__ __forceinline__ int count_ids(const Args& a, int64_t t0, int64_t t1, int* hist) {
+  constexpr int AHEAD = 4;
   int L = 1;
   while (L < 32 && L < a.k) L *= 2;
-  const int j0 = threadIdx.x & (L - 1);
-  const int64_t stride = blockDim.x / L;
+  const int j0 = threadIdx.x & (L - 1), stride = static_cast<int>(blockDim.x) / L;
   int n = 0;
-  for (int64_t t = t0 + threadIdx.x / L; t < t1; t += 4 * stride) {
-    bool on[4];
-#pragma unroll
-    for (int u = 0; u < 4; u++) {
-      on[u] = t + u * stride < t1 && (!a.mask || a.mask[t + u * stride]);
-      n += on[u] && j0 == 0;
-    }
+  for (int64_t t = t0 + threadIdx.x / L; t < t1; t += AHEAD * stride) {
     for (int j = j0; j < a.k; j += L) {
-      int64_t e[4];
+      int64_t e[AHEAD];
+      bool on[AHEAD];
 #pragma unroll
-      for (int u = 0; u < 4; u++) {
-        const int64_t at = (t + u * stride) * a.ids_ld + j;
-        e[u] = !on[u] ? -1 : a.ids_bytes == 8 ? static_cast<const int64_t*>(a.ids)[at] : static_cast<const int32_t*>(a.ids)[at];
+      for (int u = 0; u < AHEAD; u++) {
+        const int64_t at = min(t + u * stride, t1 - 1) * a.ids_ld + j;  // beyond the end: loaded again, not counted
+        e[u] = a.ids_bytes == 8 ? static_cast<const int64_t*>(a.ids)[at] : static_cast<const int32_t*>(a.ids)[at];
       }
 #pragma unroll
-      for (int u = 0; u < 4; u++)
-        if (e[u] >= 0 && e[u] < a.E) atomicAdd(&hist[e[u]], 1);
+      for (int u = 0; u < AHEAD; u++) on[u] = t + u * stride < t1;
+      if (a.mask) {
+        uint8_t m[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; u++) m[u] = a.mask[min(t + u * stride, t1 - 1)];
+#pragma unroll
+        for (int u = 0; u < AHEAD; u++) on[u] = on[u] && m[u];
+      }
+#pragma unroll
+      for (int u = 0; u < AHEAD; u++) {
+        n += on[u] && j == 0;
+        if (on[u] && e[u] >= 0 && e[u] < a.E) atomicAdd(&hist[e[u]], 1);
+      }
     }
   }
   return n;
@@ -139,78 +148,85 @@ __device__ __forceinline__ f2 mul2(f2 a, f2 b) {
 // Threads of a block, by the number of columns a lane holds (about five registers each).
 __host__ __device__ constexpr int threads_of(int columns) { return columns <= 8 ? 1024 : columns <= 16 ? 512 : 256; }
 
+constexpr int SLOTS = 4;
+__host__ __device__ constexpr int slot_bytes(int columns, int size) { return SLOTS * threads_of(columns) * columns * size; }
+
 // G lanes share a row; a lane holds N groups of VEC neighbouring columns: columns (n * G + lane) * VEC + v.
 template <int TYPE, int VEC, int N>
 __global__ void __launch_bounds__(threads_of(VEC* N), 1) k_balance_rows(const Args a, int G) {
   using E_t = typename Elem<TYPE>::T;
-  constexpr int M = VEC * N, THREADS = threads_of(M), WARPS = THREADS / 32;
+  constexpr int M = VEC * N, DEPTH = SLOTS, THREADS = threads_of(M), WARPS = THREADS / 32;
   static_assert(M % 2 == 0, "columns go in pairs");
   struct alignas(sizeof(E_t) * VEC) Pack {
     E_t x[VEC];
   };
-  __shared__ int sh_count[MAX_EXPERTS + 1];
+  __shared__ int sh_mine[MAX_EXPERTS + 1], sh_count[MAX_EXPERTS + 1];
   __shared__ float sh_f[MAX_EXPERTS];
   __shared__ float sh_sum[MAX_EXPERTS];
-  __shared__ float sh_warp[8192];  // [WARPS][E]: E <= 32 M, so at most 8192
   __shared__ float sh_loss[32];
   __shared__ bool last;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane & (G - 1);
   const bool alone = a.part_counts == nullptr;
 
-  // rows of this block's step s: from s * rows on
+  // rows of this block's step s: from s * rows on.  A thread copies what it will need of a later step into slots of
+  // its own (nobody else reads them, so no barrier): DEPTH - 1 steps are in flight.
   const int rows = THREADS / G;
   const int64_t steps = (a.T + rows - 1) / rows;
-  union Next {
-    Pack p[N];
-    E_t x[M];
-  } next;
-  bool next_on = false;
-  auto fetch = [&](int64_t step) {
+  extern __shared__ __align__(16) char sh_slots[];
+  auto slot = [&](int i, int n) { return reinterpret_cast<Pack*>(sh_slots) + (i * N + n) * THREADS + tid; };
+  uint32_t ons = 0;  // bit i: slot i holds a row that counts
+  auto fetch = [&](int64_t step, int i) {
     const int64_t t = step * rows + tid / G;
-    next_on = step < steps && t < a.T && (!a.mask || a.mask[t]);
+    const bool on = step < steps && t < a.T && (!a.mask || a.mask[t]);
+    ons = (ons & ~(1u << i)) | (static_cast<uint32_t>(on) << i);
     const E_t* const from = static_cast<const E_t*>(a.logits) + t * a.logits_ld + g * VEC;
 #pragma unroll
     for (int n = 0; n < N; n++) {
-      if (next_on && (n * G + g) * VEC < a.E) next.p[n] = *reinterpret_cast<const Pack*>(from + n * G * VEC);
+      if (on && (n * G + g) * VEC < a.E) {
+        if constexpr (sizeof(Pack) >= 4) {
+          asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(iwp_tc::smem_u32(slot(i, n))), "l"(from + n * G * VEC),
+                       "n"(static_cast<int>(sizeof(Pack)))
+                       : "memory");
+        } else {  // two bytes are too few for an asynchronous copy
+          *slot(i, n) = *reinterpret_cast<const Pack*>(from + n * G * VEC);
+        }
+      }
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  auto fetch_first = [&] {
+#pragma unroll
+    for (int i = 0; i < DEPTH - 1; i++) fetch(blockIdx.x + static_cast<int64_t>(i) * gridDim.x, i);
   };
 
   // ---- counts
   if (alone) {
     cg::cluster_group cluster = cg::this_cluster();
     const int blocks = gridDim.x;
-    for (int e = tid; e <= a.E; e += THREADS) sh_count[e] = 0;
+    for (int e = tid; e <= a.E; e += THREADS) sh_mine[e] = 0;
     iwp_tc::launch_next();
     iwp_tc::wait_previous();
-    fetch(blockIdx.x);
+    fetch_first();
     __syncthreads();
     const int64_t per = (a.T + blocks - 1) / blocks, t0 = blockIdx.x * per, t1 = min(a.T, t0 + per);
-    const int n = __reduce_add_sync(0xFFFFFFFFu, count_ids(a, t0, t1, sh_count));
-    if (lane == 0 && n) atomicAdd(&sh_count[a.E], n);
-    __syncthreads();
-    if (blocks > 1) {
+    const int n = __reduce_add_sync(0xFFFFFFFFu, count_ids(a, t0, t1, sh_mine));
+    if (lane == 0 && n) atomicAdd(&sh_mine[a.E], n);
+    if (blocks > 1)
       cluster.sync();
-      int total[(MAX_EXPERTS + THREADS) / THREADS];
+    else
+      __syncthreads();
+    for (int e = tid; e <= a.E; e += THREADS) {
+      int c = blocks > 1 ? 0 : sh_mine[e];
+      if (blocks > 1) {
 #pragma unroll
-      for (int i = 0; i < (MAX_EXPERTS + THREADS) / THREADS; i++) {
-        total[i] = 0;
-        const int e = tid + i * THREADS;
-        if (e <= a.E) {
-#pragma unroll
-          for (int b = 0; b < MAX_CLUSTER; b++)
-            if (b < blocks) total[i] += cluster.map_shared_rank(sh_count, b)[e];
-        }
+        for (int b = 0; b < MAX_CLUSTER; b++)
+          if (b < blocks) c += cluster.map_shared_rank(sh_mine, b)[e];
       }
-      cluster.sync();  // everybody has read everybody's
-#pragma unroll
-      for (int i = 0; i < (MAX_EXPERTS + THREADS) / THREADS; i++) {
-        const int e = tid + i * THREADS;
-        if (e <= a.E) sh_count[e] = total[i];
-      }
+      sh_count[e] = c;
     }
   } else {
     iwp_tc::launch_next();
-    fetch(blockIdx.x);  // inputs: complete before the counting kernel let this one start
+    fetch_first();  // inputs: complete before the counting kernel let this one start
     iwp_tc::wait_previous();
     for (int e = tid; e <= a.E; e += THREADS) {
       int c = 0;
@@ -240,9 +256,19 @@ __global__ void __launch_bounds__(threads_of(VEC* N), 1) k_balance_rows(const Ar
   }
   constexpr float LOG2E = 1.4426950408889634f;
   const f2 log2e = pack(LOG2E, LOG2E);
+  int at = 0;
   for (int64_t step = blockIdx.x; step < steps; step += gridDim.x) {
     const int64_t t = step * rows + tid / G;
-    const bool on = next_on;
+    const bool on = ons >> at & 1;
+    asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 2) : "memory");
+    union {
+      Pack p[N];
+      E_t x[M];
+    } next;
+#pragma unroll
+    for (int n = 0; n < N; n++) next.p[n] = *slot(at, n);
+    fetch(step + (DEPTH - 1) * static_cast<int64_t>(gridDim.x), at == 0 ? DEPTH - 1 : at - 1);
+    at = at + 1 == DEPTH ? 0 : at + 1;
     f2 x[M / 2];
     float top = -CUDART_INF_F;
 #pragma unroll
@@ -252,7 +278,6 @@ __global__ void __launch_bounds__(threads_of(VEC* N), 1) k_balance_rows(const Ar
       top = fmaxf(top, fmaxf(y0, y1));
       x[i / 2] = pack(y0, y1);
     }
-    fetch(step + gridDim.x);
     for (int o = G >> 1; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
     const float ref = top == -CUDART_INF_F ? 0.f : -top;  // subtracted before the scaling, which lowest values would not survive
     const f2 ref2 = pack(ref, ref);
@@ -293,6 +318,10 @@ __global__ void __launch_bounds__(threads_of(VEC* N), 1) k_balance_rows(const Ar
   }
 
   // ---- column sums: lanes of a warp, warps of the block, blocks; each in a fixed order
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncthreads();
+  float* const sh_warp = reinterpret_cast<float*>(sh_slots);  // [WARPS][E], at most 32 KB, as E <= 32 M
+  static_assert(slot_bytes(M, sizeof(E_t)) >= WARPS * 32 * M * 4 && slot_bytes(M, sizeof(E_t)) >= 4 * MAX_EXPERTS, "room for the sums");
 #pragma unroll
   for (int i = 0; i < M; i++) {
     float y = i % 2 ? unpack(sum[i / 2]).y : unpack(sum[i / 2]).x;
@@ -306,7 +335,7 @@ __global__ void __launch_bounds__(threads_of(VEC* N), 1) k_balance_rows(const Ar
 #pragma unroll 8
     for (int w = 0; w < WARPS; w++) y += sh_warp[w * a.E + e];
     sh_sum[e] = y;
-    if (!alone) a.part[static_cast<int64_t>(blockIdx.x) * a.E + e] = y;
+    if (!alone) a.part[static_cast<int64_t>(blockIdx.x) * padded(a.E) + e] = y;
   }
   if (alone) {
     cg::cluster_group cluster = cg::this_cluster();
@@ -332,24 +361,27 @@ __global__ void __launch_bounds__(threads_of(VEC* N), 1) k_balance_rows(const Ar
     __syncthreads();
     if (!last) return;
     __threadfence();
-    // groups of threads take every groups-th block, then the groups are added in order
-    const int width = a.E < THREADS ? a.E : THREADS, groups = min(THREADS / width, 8192 / a.E);
-    const int q = tid / width;
-    if (q < groups)
-      for (int e = tid - q * width; e < a.E; e += width) {
-        float y = 0.f;
+    // a thread takes four columns of every groups-th block, then the groups are added in order
+    const int quads = padded(a.E) / 4, groups = THREADS / quads;
+    if (tid < groups * quads) {
+      const int q = tid / quads, e = 4 * (tid - q * quads);
+      float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 8
-        for (int b = q; b < static_cast<int>(gridDim.x); b += groups) y += __ldcg(a.part + static_cast<int64_t>(b) * a.E + e);
-        sh_warp[q * a.E + e] = y;
+      for (int b = q; b < static_cast<int>(gridDim.x); b += groups) {
+        const float4 z = __ldcg(reinterpret_cast<const float4*>(a.part + static_cast<int64_t>(b) * padded(a.E) + e));
+        y.x += z.x, y.y += z.y, y.z += z.z, y.w += z.w;
       }
+      *reinterpret_cast<float4*>(sh_warp + q * padded(a.E) + e) = y;
+    }
     __syncthreads();
     for (int e = tid; e < a.E; e += THREADS) {
       float y = 0.f;
-      for (int i = 0; i < groups; i++) y += sh_warp[i * a.E + e];
+      for (int i = 0; i < groups; i++) y += sh_warp[i * padded(a.E) + e];
       sh_sum[e] = y;
     }
     __syncthreads();
     for (int e = tid; e < a.E; e += THREADS) sh_warp[e] = sh_sum[e];
+    __syncthreads();
   }
   float mine = 0.f;
   for (int e = tid; e < a.E; e += THREADS) {

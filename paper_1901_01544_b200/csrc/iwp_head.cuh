@@ -116,6 +116,11 @@ __device__ __forceinline__ uint32_t log_code(float x) {
 }
 __device__ __forceinline__ float log_value(uint32_t code) { return code == 0xFFFFu ? -CUDART_INF_F : 8.f - __uint_as_float((code << 8) + EIGHT); }
 
+// Column i of the lane's staged row.
+__device__ __forceinline__ float* staged_at(const Where& w, int i) {
+  return reinterpret_cast<float*>(iwp_tc::staged(w.staging, w.lane, i >> 2)) + (i & 3);
+}
+
 // ---- epilogue of the logits pass --------------------------------------------------------------------
 
 struct Logits {
@@ -149,12 +154,12 @@ struct Logits {
       const int c0 = w.col0 + 32 * c;
       if (32 * c >= w.width) break;
       if (__any_sync(0xFFFFFFFFu, up.next < c0 + 32)) {  // some row has a target here
-        float* mine = reinterpret_cast<float*>(w.staging + w.lane * iwp_tc::STAGING_PITCH);
 #pragma unroll
         for (int j = 0; j < 32; j += 4)
-          *reinterpret_cast<float4*>(mine + j) = make_float4(acc[32 * c + j], acc[32 * c + j + 1], acc[32 * c + j + 2], acc[32 * c + j + 3]);
+          *reinterpret_cast<float4*>(iwp_tc::staged(w.staging, w.lane, j / 4)) =
+              make_float4(acc[32 * c + j], acc[32 * c + j + 1], acc[32 * c + j + 2], acc[32 * c + j + 3]);
         while (up.next < c0 + 32) {
-          a.z_at[static_cast<int64_t>(row) * a.en.k + up.pos] = mine[up.next - c0];
+          a.z_at[static_cast<int64_t>(row) * a.en.k + up.pos] = *staged_at(w, up.next - c0);
           up.advance(a.en, row);
         }
         __syncwarp();
@@ -241,16 +246,16 @@ struct Probs {
       for (int j = 0; j < 32; j++) v[j] = scale == 0.f ? 0.f : ex2(fmaf(v[j], a.c, -lse2));
       const int end = a.v0 + c0 + 32;
       if (__any_sync(0xFFFFFFFFu, up.next < end)) {
-        float* mine = reinterpret_cast<float*>(w.staging + w.lane * iwp_tc::STAGING_PITCH);
 #pragma unroll
-        for (int j = 0; j < 32; j += 4) *reinterpret_cast<float4*>(mine + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+        for (int j = 0; j < 32; j += 4)
+          *reinterpret_cast<float4*>(iwp_tc::staged(w.staging, w.lane, j / 4)) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
         while (up.next < end) {
-          mine[up.next - (a.v0 + c0)] -= a.en.q_at(row, up.pos);
+          *staged_at(w, up.next - (a.v0 + c0)) -= a.en.q_at(row, up.pos);
           up.advance(a.en, row);
         }
 #pragma unroll
         for (int j = 0; j < 32; j += 4) {
-          const float4 x = *reinterpret_cast<const float4*>(mine + j);
+          const float4 x = *reinterpret_cast<const float4*>(iwp_tc::staged(w.staging, w.lane, j / 4));
           v[j] = x.x, v[j + 1] = x.y, v[j + 2] = x.z, v[j + 3] = x.w;
         }
         __syncwarp();
@@ -537,7 +542,7 @@ __global__ void __launch_bounds__(ROW_THREADS) k_rows(const Rows a) {
     }
   }
   __syncthreads();
-  if (tid == 0) last = atomicInc(&a.hdr->ticket, gridDim.x - 1) == gridDim.x - 1;
+  if (tid == 0) last = gridDim.x == 1 || atomicInc(&a.hdr->ticket, gridDim.x - 1) == gridDim.x - 1;
   __syncthreads();
   if (!last) return;
   __threadfence();
@@ -664,7 +669,7 @@ struct Few {
 
 constexpr int FEW_TOKENS = 4, FEW_THREADS = 512, FEW_ROWS = 4;
 
-// Four columns of weight rows per warp at a time, streamed once: a dot product with at most four tokens is bound by the
+// Four rows of the weights per warp at a time, streamed once: a dot product with at most four tokens is bound by the
 // weights' bytes, and plain loads keep more of them in flight than the tensor cores' 128-row tiles would.  Operand rows
 // start at multiples of 16 bytes and hold whole ones (copies made by k_align_rows end in zeros).
 template <int TOKENS>
@@ -675,9 +680,15 @@ __global__ void __launch_bounds__(FEW_THREADS) k_few_tokens(const Few a) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int groups = (a.D + 7) / 8;
   iwp_tc::launch_next();
-  iwp_tc::wait_previous();
   const uint16_t* const hidden = static_cast<const uint16_t*>(a.hidden);
   const uint16_t* const weight = static_cast<const uint16_t*>(a.weight);
+  // the beginning (2 KB each) of this warp's first rows is on its way to the L2 while the kernel before this one ends
+  for (int i = lane; i < FEW_ROWS * 16; i += 32) {
+    const int v = (blockIdx.x * WARPS + warp) * FEW_ROWS + i / 16;
+    if (static_cast<int>(blockIdx.x) < a.blocks && v < a.V && 8 * (i % 16) < groups)
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(weight + v * a.weight_ld + 64 * (i % 16)));
+  }
+  iwp_tc::wait_previous();
   for (int i = tid; i < TOKENS * groups; i += FEW_THREADS) {
     const int t = i / groups, g = i - t * groups;
     const uint4 x = *reinterpret_cast<const uint4*>(hidden + t * a.hidden_ld + 8 * g);

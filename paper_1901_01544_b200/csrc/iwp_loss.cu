@@ -202,11 +202,15 @@ int pairs_of() {
 }
 
 template <class Epi, int N>
-int launch_product(const iwp_tc::Problems<N>& w, const typename Epi::Args& args, cudaStream_t st) {
+int launch_product(iwp_tc::Problems<N>& w, const typename Epi::Args& args, cudaStream_t st) {
   const int pairs = pairs_of<Epi, N>();
   int64_t total = 0;
   for (const auto& q : w.p) total += int64_t(q.m_tiles) * q.n_tiles * q.splits;
   if (total > MAX_SIZE) return IWP_ERR_INVALID;
+  const int tile_n = w.p[N - 1].n_tiles ? w.p[N - 1].tile_n : w.p[0].tile_n;  // the same for both
+  w.b_bytes = static_cast<int>(up_to(tile_n / iwp_tc::CG, 64)) * iwp_tc::BLOCK_K * 2;
+  w.stages = iwp_tc::STAGE_SPACE / (iwp_tc::A_BYTES + w.b_bytes);
+  if (w.stages > iwp_tc::MAX_STAGES) w.stages = iwp_tc::MAX_STAGES;
   LOSS_CUDA(launch(iwp_tc::k_product<N, Epi>, iwp_tc::CG * (total < pairs ? total : pairs), iwp_tc::THREADS, iwp_tc::SMEM, iwp_tc::CG, st, w, args));
   return IWP_OK;
 }
@@ -371,12 +375,12 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
       fa.blocks = static_cast<int>(whole < FEW_BLOCKS ? whole : FEW_BLOCKS);
       const int64_t grid = fa.blocks + tiles_of(T * p.k, warps);
       const size_t smem = static_cast<size_t>(16 * T * tiles_of(D, 8));
-      ra.parts = fa.blocks;
       LOSS_CUDA(launch(T == 1   ? H::k_few_tokens<1>
                        : T == 2 ? H::k_few_tokens<2>
                        : T == 3 ? H::k_few_tokens<3>
                                 : H::k_few_tokens<4>,
                        grid, H::FEW_THREADS, smem, 1, st, fa));
+      ra.parts = fa.blocks;
       LOSS_CUDA(launch(H::k_rows, row_blocks, H::ROW_THREADS, 0, 1, st, ra));
       return IWP_OK;
     }
@@ -419,6 +423,7 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
       fa.chunks = static_cast<int>(tiles_of(fa.width, H::FACTOR_COLUMNS));
       fa.log_codes = la.log_codes;
       fa.up = up;
+      if (T * fa.chunks > MAX_SIZE) return IWP_ERR_INVALID;
       LOSS_CUDA(launch(H::k_factors, T * fa.chunks, H::FACTOR_THREADS, 0, 1, st, fa));
     }
   }
@@ -531,8 +536,16 @@ int64_t balance_part_counts_bytes(int E) { return up_to(int64_t(iwp_balance::COU
 template <int TYPE, int VEC, int N>
 int balance_launch(iwp_balance::Args a, int G, cudaStream_t st) {
   namespace B = iwp_balance;
-  constexpr int threads = B::threads_of(VEC * N);
+  constexpr int threads = B::threads_of(VEC * N), slots = B::slot_bytes(VEC * N, TYPE == IWP_F32 ? 4 : 2);
   auto kernel = B::k_balance_rows<TYPE, VEC, N>;
+  static bool ready[MAX_DEVICES] = {};
+  const int dev = device();
+  if (dev < 0) return IWP_ERR_CUDA;
+  if (!ready[dev]) {
+    LOSS_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, slots));
+    LOSS_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    ready[dev] = true;
+  }
   const int64_t steps = tiles_of(a.T, threads / G);
   const int64_t bytes = a.T * (a.E * (TYPE == IWP_F32 ? 4 : 2) + a.k * a.ids_bytes);
   if (bytes <= CLUSTER_BYTES) {
@@ -540,18 +553,11 @@ int balance_launch(iwp_balance::Args a, int G, cudaStream_t st) {
     int ctas = 1;
     while (ctas < B::MAX_CLUSTER && 2 * ctas < steps) ctas *= 2;
     a.part_counts = nullptr;
-    static bool opted[MAX_DEVICES] = {};
-    const int dev = device();
-    if (dev < 0) return IWP_ERR_CUDA;
-    if (!opted[dev]) {
-      LOSS_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-      opted[dev] = true;
-    }
-    LOSS_CUDA(launch(kernel, ctas, threads, 0, ctas, st, a, G));
+    LOSS_CUDA(launch(kernel, ctas, threads, slots, ctas, st, a, G));
     return IWP_OK;
   }
   LOSS_CUDA(launch(B::k_balance_counts, B::COUNT_BLOCKS, B::COUNT_THREADS, 0, B::COUNT_CLUSTER, st, a));
-  LOSS_CUDA(launch(kernel, steps < BALANCE_BLOCKS ? steps : BALANCE_BLOCKS, threads, 0, 1, st, a, G));
+  LOSS_CUDA(launch(kernel, steps < BALANCE_BLOCKS ? steps : BALANCE_BLOCKS, threads, slots, 1, st, a, G));
   return IWP_OK;
 }
 
@@ -623,7 +629,7 @@ extern "C" int iwp_head_loss(const iwp_head_args* a, void* cuda_stream) {
 
 extern "C" int64_t iwp_balance_workspace(const iwp_balance_args* a) {
   if (!balance_args_ok(a)) return -1;
-  return 256 + balance_part_counts_bytes(a->experts) + up_to(int64_t(BALANCE_BLOCKS) * a->experts * 4, 256);
+  return 256 + balance_part_counts_bytes(a->experts) + up_to(int64_t(BALANCE_BLOCKS) * iwp_balance::padded(a->experts) * 4, 256);
 }
 
 extern "C" int iwp_balance_loss(const iwp_balance_args* a, void* cuda_stream) {

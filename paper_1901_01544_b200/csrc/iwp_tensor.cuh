@@ -32,17 +32,20 @@ constexpr int TILE_N = 256;    // columns of the accumulator
 constexpr int BLOCK_K = 64;    // elements of K per stage: 128 bytes, one swizzle row
 constexpr int EPI_WARPS = 8;
 constexpr int THREADS = 128 + 32 * EPI_WARPS;
-constexpr int STAGING_PITCH = 144;                      // bytes per row of the epilogue's staging rows (128 + 16)
-constexpr int STAGING_BYTES = 32 * STAGING_PITCH;       // per epilogue warp
+constexpr int STAGING_BYTES = 32 * 128;                 // per epilogue warp: a row of 128 bytes per lane
 constexpr uint32_t WAIT_TRIES = 1u << 18;               // x 20 us at most per try: about 5 s
 constexpr uint32_t WAIT_HINT_NS = 20000;
 
 constexpr int CG = 2;                               // CTAs per tile
 constexpr int A_BYTES = TILE_M * BLOCK_K * 2;
-constexpr int B_BYTES = TILE_N / CG * BLOCK_K * 2;  // of the widest tile
-constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
-constexpr int STAGES = 5;
-constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * STAGING_BYTES + 256;
+constexpr int MAX_STAGES = 9;
+constexpr int STAGE_SPACE = 6 * (A_BYTES + TILE_N / CG * BLOCK_K * 2);  // 6 stages of the widest tiles, more of narrower ones
+constexpr int SMEM = 1024 + STAGE_SPACE + EPI_WARPS * STAGING_BYTES + 256;
+static_assert(SMEM <= 227 * 1024, "shared memory of a CTA");
+
+// The 16-byte word `word` (0..7) of staging row `row`: rotated by the row, so that neither lanes that write their own
+// rows nor lanes that read neighbouring words of a row meet in a bank.
+__device__ __forceinline__ char* staged(char* staging, int row, int word) { return staging + 128 * row + 16 * (word ^ (row & 7)); }
 
 // ---- small wrappers of the instructions used ---------------------------------------------------------
 
@@ -190,6 +193,7 @@ template <int N>
 struct Problems {
   Problem p[N];
   int rounds, rest, fill;
+  int stages, b_bytes;  // of the ring in shared memory, and B's share of a stage
   int seg;  // k blocks per accumulator tile (epilogues that add up segments), or a large number
   int* status;
 };
@@ -271,18 +275,18 @@ __global__ void __launch_bounds__(THREADS, 1)
   const uint32_t raw = smem_u32(smem_raw);
   char* const smem = smem_raw + (((raw + 1023) & ~1023u) - raw);  // the same offset in both CTAs of a pair
   const uint32_t base = smem_u32(smem);
-  char* const staging = smem + STAGES * STAGE_BYTES;
+  char* const staging = smem + STAGE_SPACE;
   char* const ctl = staging + EPI_WARPS * STAGING_BYTES;
   const uint32_t bars = smem_u32(ctl);
-  const uint32_t full = bars, empty = bars + 8 * STAGES, acc_full = empty + 8 * STAGES, acc_empty = acc_full + 16;
-  volatile int* const dead = reinterpret_cast<volatile int*>(ctl + 8 * (2 * STAGES + 4));
-  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(ctl + 8 * (2 * STAGES + 4) + 4);
+  const uint32_t full = bars, empty = bars + 8 * MAX_STAGES, acc_full = empty + 8 * MAX_STAGES, acc_empty = acc_full + 16;
+  volatile int* const dead = reinterpret_cast<volatile int*>(ctl + 8 * (2 * MAX_STAGES + 4));
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(ctl + 8 * (2 * MAX_STAGES + 4) + 4);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
   launch_next();
   if (threadIdx.x == 0) {
-    for (int s = 0; s < STAGES; s++) {
+    for (int s = 0; s < w.stages; s++) {
       mbar_init(full + 8 * s, 1);
       mbar_init(empty + 8 * s, 1);
     }
@@ -305,6 +309,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   wait_previous();
 
   const int pair = blockIdx.x / CG, pairs = gridDim.x / CG;
+  const int stages = w.stages, stage_bytes = A_BYTES + w.b_bytes;
   Tile t;
 
   // An epilogue that sums holds 128 columns per thread: 88 registers for each thread of the first four warps, 208 for
@@ -327,7 +332,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           if (!mbar_wait(empty + 8 * s, phase ^ 1, dead, w.status)) break;
           if (rank == 0) mbar_expect(full + 8 * s, bytes);
           const uint32_t bar = full_of_pair + 8 * s;
-          const uint32_t at_a = base + s * STAGE_BYTES, at_b = at_a + A_BYTES;
+          const uint32_t at_a = base + s * stage_bytes, at_b = at_a + A_BYTES;
           if (a_kc) {
             tma_load(at_a, &q.a, kb * BLOCK_K, row_a, bar);
           } else {
@@ -340,7 +345,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             tma_load(at_b, &q.b, row_b, kb * BLOCK_K, bar);
             if (rows_b > 64) tma_load(at_b + 64 * 128, &q.b, row_b + 64, kb * BLOCK_K, bar);
           }
-          if (++s == STAGES) {
+          if (++s == stages) {
             s = 0;
             phase ^= 1;
           }
@@ -362,13 +367,13 @@ __global__ void __launch_bounds__(THREADS, 1)
           for (int kb = k0; kb < k1; kb++) {
             if (!mbar_wait(full + 8 * s, phase, dead, w.status)) break;
             fence_after();
-            const uint32_t at_a = base + s * STAGE_BYTES;
+            const uint32_t at_a = base + s * stage_bytes;
             const uint64_t da = operand_desc(at_a, a_kc), db = operand_desc(at_a + A_BYTES, b_kc);
 #pragma unroll
             for (int k = 0; k < BLOCK_K / 16; k++)
               mma(tmem + b * TILE_N, da + k * step_a, db + k * step_b, idesc, (kb > k0 || k > 0) ? 1u : 0u);
             mma_commit(empty + 8 * s);
-            if (++s == STAGES) {
+            if (++s == stages) {
               s = 0;
               phase ^= 1;
             }
@@ -484,16 +489,15 @@ __device__ __forceinline__ void store_as(void* p, int64_t i, float v, int type) 
 // TYPE: IWP_F32 / IWP_BF16 / IWP_F16.  `add`: the old contents are added first (in fp32).
 __device__ __forceinline__ void store_chunk(const float (&v)[32], char* staging, void* out, int64_t ld, int type, bool wide, bool add,
                                             int row0, int rows, int col0, int cols, int lane) {
-  char* mine = staging + lane * STAGING_PITCH;
   if (type == 0 || !wide || add) {  // staged as fp32
 #pragma unroll
-    for (int j = 0; j < 32; j += 4) *reinterpret_cast<float4*>(mine + 4 * j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+    for (int j = 0; j < 8; j++) *reinterpret_cast<float4*>(staged(staging, lane, j)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
   } else {
 #pragma unroll
-    for (int j = 0; j < 32; j += 8)
-      *reinterpret_cast<uint4*>(mine + 2 * j) =
-          make_uint4(pack2(v[j], v[j + 1], type), pack2(v[j + 2], v[j + 3], type), pack2(v[j + 4], v[j + 5], type),
-                     pack2(v[j + 6], v[j + 7], type));
+    for (int j = 0; j < 4; j++)
+      *reinterpret_cast<uint4*>(staged(staging, lane, j)) =
+          make_uint4(pack2(v[8 * j], v[8 * j + 1], type), pack2(v[8 * j + 2], v[8 * j + 3], type), pack2(v[8 * j + 4], v[8 * j + 5], type),
+                     pack2(v[8 * j + 6], v[8 * j + 7], type));
   }
   __syncwarp();
   const bool whole = wide && col0 + 32 <= cols;
@@ -501,7 +505,7 @@ __device__ __forceinline__ void store_chunk(const float (&v)[32], char* staging,
     const int r = lane >> 2, c = lane & 3;  // 8 rows of 64 bytes at a time
 #pragma unroll
     for (int i = 0; i < 32; i += 8) {
-      const uint4 x = *reinterpret_cast<const uint4*>(staging + (r + i) * STAGING_PITCH + 16 * c);
+      const uint4 x = *reinterpret_cast<const uint4*>(staged(staging, r + i, c));
       if (row0 + r + i < rows)
         *reinterpret_cast<uint4*>(static_cast<char*>(out) + 2 * ((row0 + r + i) * ld + col0) + 16 * c) = x;
     }
@@ -509,7 +513,7 @@ __device__ __forceinline__ void store_chunk(const float (&v)[32], char* staging,
     const int r = lane >> 3, c = lane & 7;  // 4 rows of 128 bytes at a time
 #pragma unroll
     for (int i = 0; i < 32; i += 4) {
-      float4 x = *reinterpret_cast<const float4*>(staging + (r + i) * STAGING_PITCH + 16 * c);
+      float4 x = *reinterpret_cast<const float4*>(staged(staging, r + i, c));
       if (row0 + r + i < rows) {
         float4* p = reinterpret_cast<float4*>(static_cast<float*>(out) + (row0 + r + i) * ld + col0) + c;
         if (add) {
@@ -524,8 +528,8 @@ __device__ __forceinline__ void store_chunk(const float (&v)[32], char* staging,
     for (int i = 0; i < 32 && row0 + i < rows; i++) {
       if (col0 + lane < cols) {
         const int64_t at = (row0 + i) * ld + col0 + lane;
-        const char* from = staging + i * STAGING_PITCH;
-        float x = packed ? load_as_float(from, lane, type) : reinterpret_cast<const float*>(from)[lane];
+        float x = packed ? load_as_float(staged(staging, i, lane >> 3), lane & 7, type)
+                         : reinterpret_cast<const float*>(staged(staging, i, lane >> 2))[lane & 3];
         if (add) x += load_as_float(out, at, type);
         store_as(out, at, x, type);
       }
@@ -537,14 +541,13 @@ __device__ __forceinline__ void store_chunk(const float (&v)[32], char* staging,
 // The same for 32 columns of 16 bits that are packed already; rows of 16-byte multiples, all columns inside.
 __device__ __forceinline__ void store_packed(const uint32_t (&u)[16], char* staging, uint16_t* out, int64_t ld, int row0, int rows, int col0,
                                              int lane) {
-  char* mine = staging + lane * STAGING_PITCH;
 #pragma unroll
-  for (int j = 0; j < 4; j++) *reinterpret_cast<uint4*>(mine + 16 * j) = make_uint4(u[4 * j], u[4 * j + 1], u[4 * j + 2], u[4 * j + 3]);
+  for (int j = 0; j < 4; j++) *reinterpret_cast<uint4*>(staged(staging, lane, j)) = make_uint4(u[4 * j], u[4 * j + 1], u[4 * j + 2], u[4 * j + 3]);
   __syncwarp();
   const int r = lane >> 2, c = lane & 3;  // 8 rows of 64 bytes at a time
 #pragma unroll
   for (int i = 0; i < 32; i += 8) {
-    const uint4 x = *reinterpret_cast<const uint4*>(staging + (r + i) * STAGING_PITCH + 16 * c);
+    const uint4 x = *reinterpret_cast<const uint4*>(staged(staging, r + i, c));
     if (row0 + r + i < rows) *reinterpret_cast<uint4*>(out + (row0 + r + i) * ld + col0 + 8 * c) = x;
   }
   __syncwarp();
