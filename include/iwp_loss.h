@@ -70,7 +70,8 @@ typedef struct iwp_head_args {
   int64_t dweight_ld;
   void* workspace;                 /* 256-byte aligned */
   int64_t workspace_bytes;
-  int64_t piece_bytes;             /* bound on the probabilities of one piece of the vocabulary; 0 = 1 GiB */
+  int64_t piece_bytes;             /* bound on the probabilities of one piece of the vocabulary; 0 = 1 GiB, or what the
+                                      weights and their gradient take (4 V D bytes) where that is more */
   float temperature, scale;
   int32_t dtype;                   /* IWP_BF16 or IWP_F16: hidden and weight */
   int32_t top_k, ids_bytes, top_type; /* 1 <= top_k <= 1024 */

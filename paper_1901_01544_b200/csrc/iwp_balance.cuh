@@ -117,33 +117,12 @@ struct Elem<IWP_F16> {
   using T = __half;
 };
 
-// Two floats at a time (sm_100's packed arithmetic): this kernel is bound by issue slots as much as by memory.
-using f2 = unsigned long long;
-__device__ __forceinline__ f2 pack(float a, float b) {
-  f2 r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ float2 unpack(f2 x) {
-  float2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
-  return r;
-}
-__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
-  f2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ f2 add2(f2 a, f2 b) {
-  f2 r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
-  f2 r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
+using iwp_tc::add2;
+using iwp_tc::f2;
+using iwp_tc::fma2;
+using iwp_tc::mul2;
+using iwp_tc::pack;
+using iwp_tc::unpack;
 
 // Threads of a block, by the number of columns a lane holds (about five registers each).
 __host__ __device__ constexpr int threads_of(int columns) { return columns <= 8 ? 1024 : columns <= 16 ? 512 : 256; }

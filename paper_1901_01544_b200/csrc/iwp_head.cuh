@@ -24,7 +24,12 @@
 
 namespace iwp_head {
 
+using iwp_tc::add2;
 using iwp_tc::ex2;
+using iwp_tc::f2;
+using iwp_tc::fma2;
+using iwp_tc::pack;
+using iwp_tc::unpack;
 using iwp_tc::Where;
 
 constexpr int MAX_TOP = 1024;
@@ -106,15 +111,22 @@ struct Upcoming {
 // How the logits pass leaves an element of the kept piece behind in 16 bits, with x = (z - maximum) log2(e) / tau <= 0:
 //   bf16 factors: fp16 of 2^(x + 15).  It is the summand at hand anyway, and right to 2^-11 of itself down to 2^-29 of
 //     the maximum (0 below 2^-40); the factor is rounded to bf16, eight times as coarse, afterwards.
-//   fp16 factors: the float 8 - x with its mantissa rounded to 15 bits, less the bits of 8: steps of 2^-12 in log2
-//     above 2^-8 of the maximum, of 2^-11 to 2^-24, 0 below; a probability is right to 8.5e-5 of itself, where
-//     fp16 of it would be as coarse (2.4e-4 at worst) as the rounding to the factor's type that follows.
+//   fp16 factors: 16 bits out of the middle of the float y = 8 - x: steps of 2^-12 in log2 above 2^-8 of the maximum, of
+//     2^-11 to 2^-24, 0 below.  A probability is right to 8.5e-5 (1.7e-4) of itself, where fp16 of it would be as
+//     coarse (2.4e-4 at worst) as the rounding to the factor's type that follows.
+enum Codes { NO_CODES = 0, HALF_CODES = 1, LOG_CODES = 2 };
 constexpr float SUM_SCALE = 3.0517578125e-5f;  // 2^-15
-constexpr uint32_t EIGHT = 0x41000000u;
-__device__ __forceinline__ uint32_t log_code(float x) {
-  return min((__float_as_uint(8.f - fminf(x, 0.f)) - (EIGHT - 128u)) >> 8, 0xFFFFu);
+constexpr float HALF_STEP = 1.220703125e-4f;   // 2^-13: of the finer steps, added before the bits below are cut
+constexpr float LOG_END = 31.9998779296875f;   // 32 - 2^-13: the last code, which stands for everything below 2^-24
+__device__ __forceinline__ uint32_t log_codes(float y0, float y1) {  // y = 8 - x + HALF_STEP
+  y0 = fminf(fmaxf(y0, 8.f), LOG_END);
+  y1 = fminf(fmaxf(y1, 8.f), LOG_END);
+  return __byte_perm(__float_as_uint(y0), __float_as_uint(y1), 0x6521);
 }
-__device__ __forceinline__ float log_value(uint32_t code) { return code == 0xFFFFu ? -CUDART_INF_F : 8.f - __uint_as_float((code << 8) + EIGHT); }
+// y of a code, in the middle of its step (the coarser steps were cut a quarter of a step off)
+__device__ __forceinline__ float log_value(uint32_t code) {
+  return code == 0xFFFFu ? CUDART_INF_F : __uint_as_float(((code << 8) + 0x41000000u) | (code >> 15 << 6));
+}
 
 // Column i of the lane's staged row.
 __device__ __forceinline__ float* staged_at(const Where& w, int i) {
@@ -123,6 +135,7 @@ __device__ __forceinline__ float* staged_at(const Where& w, int i) {
 
 // ---- epilogue of the logits pass --------------------------------------------------------------------
 
+template <int CODES>
 struct Logits {
   static constexpr bool SUMS = true;
   struct Args {
@@ -133,10 +146,9 @@ struct Logits {
     float2* part;     // [T][parts]: maximum (of z c) and sum of 2^(z c - maximum)
     int parts;
     float* z_at;      // [T][k] logits at the targets
-    uint16_t* codes;  // [T][ld] of columns v0 .. v0 + width, or width = 0
+    uint16_t* codes;  // [T][ld] of columns v0 .. v0 + width
     int64_t ld;
     int v0, width;
-    int log_codes;
   };
   static __device__ __forceinline__ Upcoming begin(const Args& a, const Where& w) {
     Upcoming u;
@@ -144,7 +156,7 @@ struct Logits {
     if (w.row0 + w.lane < a.T) u.from(a.en, w.row0 + w.lane, w.col0);
     return u;
   }
-  static __device__ __forceinline__ void tile(const Args& a, const Where& w, Upcoming& up, float (&acc)[iwp_tc::TILE_N / 2]) {
+  static __device__ __forceinline__ void tile(const Args& a, const Where& w, Upcoming& up, f2 (&acc)[iwp_tc::TILE_N / 4]) {
     constexpr int CHUNKS = iwp_tc::TILE_N / 64;
     const int row = w.row0 + w.lane;
     const bool live = row < a.T;
@@ -155,9 +167,10 @@ struct Logits {
       if (32 * c >= w.width) break;
       if (__any_sync(0xFFFFFFFFu, up.next < c0 + 32)) {  // some row has a target here
 #pragma unroll
-        for (int j = 0; j < 32; j += 4)
-          *reinterpret_cast<float4*>(iwp_tc::staged(w.staging, w.lane, j / 4)) =
-              make_float4(acc[32 * c + j], acc[32 * c + j + 1], acc[32 * c + j + 2], acc[32 * c + j + 3]);
+        for (int j = 0; j < 32; j += 4) {
+          const float2 x = unpack(acc[16 * c + j / 2]), y = unpack(acc[16 * c + j / 2 + 1]);
+          *reinterpret_cast<float4*>(iwp_tc::staged(w.staging, w.lane, j / 4)) = make_float4(x.x, x.y, y.x, y.y);
+        }
         while (up.next < c0 + 32) {
           a.z_at[static_cast<int64_t>(row) * a.en.k + up.pos] = *staged_at(w, up.next - c0);
           up.advance(a.en, row);
@@ -166,40 +179,43 @@ struct Logits {
       }
       if (c0 + 32 > a.V) {
 #pragma unroll
-        for (int j = 0; j < 32; j++)
-          if (c0 + j >= a.V) acc[32 * c + j] = -CUDART_INF_F;
+        for (int j = 0; j < 32; j += 2) {
+          const float2 x = unpack(acc[16 * c + j / 2]);
+          acc[16 * c + j / 2] = pack(c0 + j < a.V ? x.x : -CUDART_INF_F, c0 + j + 1 < a.V ? x.y : -CUDART_INF_F);
+        }
       }
 #pragma unroll
-      for (int j = 0; j < 32; j++) top = fmaxf(top, acc[32 * c + j]);
+      for (int j = 0; j < 16; j++) {
+        const float2 x = unpack(acc[16 * c + j]);
+        top = fmaxf(top, fmaxf(x.x, x.y));
+      }
     }
     const float m = top * a.c;
     const float ref = m == -CUDART_INF_F ? 0.f : m;  // nothing but -inf: sums of 0, not of NaN
-    float s = 0.f;
-    const bool keep = w.col0 >= a.v0 && w.col0 < a.v0 + a.width;
-    const float less = 15.f - ref;
+    const bool keep = CODES != NO_CODES && w.col0 >= a.v0 && w.col0 < a.v0 + a.width;
+    const f2 scale = pack(a.c, a.c), less = pack(15.f - ref, 15.f - ref);
+    const f2 down = pack(-a.c, -a.c), from = pack(8.f + HALF_STEP + ref, 8.f + HALF_STEP + ref);
+    f2 sum = pack(0.f, 0.f);
 #pragma unroll
     for (int c = 0; c < CHUNKS; c++) {
       if (32 * c >= w.width) break;
       uint32_t packed[16];
-      if (a.log_codes) {
 #pragma unroll
-        for (int j = 0; j < 32; j += 2) {
-          const float x = fmaf(acc[32 * c + j], a.c, -ref), y = fmaf(acc[32 * c + j + 1], a.c, -ref);
-          s += ex2(x + 15.f) + ex2(y + 15.f);
-          packed[j / 2] = log_code(x) | (log_code(y) << 16);
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 32; j += 2) {
-          const float x = ex2(fmaf(acc[32 * c + j], a.c, less)), y = ex2(fmaf(acc[32 * c + j + 1], a.c, less));
-          s += x + y;
-          packed[j / 2] = iwp_tc::pack2(x, y, IWP_F16);
+      for (int j = 0; j < 16; j++) {
+        const f2 z = acc[16 * c + j];
+        const float2 x = unpack(fma2(z, scale, less));
+        const float2 e = make_float2(ex2(x.x), ex2(x.y));
+        sum = add2(sum, pack(e.x, e.y));
+        if constexpr (CODES == HALF_CODES) packed[j] = iwp_tc::pack2(e.x, e.y, IWP_F16);
+        if constexpr (CODES == LOG_CODES) {
+          const float2 y = unpack(fma2(z, down, from));
+          packed[j] = log_codes(y.x, y.y);
         }
       }
-      if (keep)
-        iwp_tc::store_packed(packed, w.staging, a.codes, a.ld, w.row0, static_cast<int>(a.T), w.col0 + 32 * c - a.v0, w.lane);
+      if (keep) iwp_tc::store_packed(packed, w.staging, a.codes, a.ld, w.row0, static_cast<int>(a.T), w.col0 + 32 * c - a.v0, w.lane);
     }
-    if (live) a.part[static_cast<int64_t>(row) * a.parts + w.col0 / w.width] = make_float2(m, s * SUM_SCALE);
+    const float2 s = unpack(sum);
+    if (live) a.part[static_cast<int64_t>(row) * a.parts + w.col0 / w.width] = make_float2(m, (s.x + s.y) * SUM_SCALE);
   }
 };
 
@@ -601,7 +617,7 @@ __global__ void __launch_bounds__(FACTOR_THREADS) k_factors(const Factors a) {
   }
   const float scale = a.en.row_scale(row) * a.up;
   auto probability = [&](float top, uint32_t code) {  // top = the part's maximum less lse, in log2
-    return a.log_codes ? ex2(top + log_value(code)) : __half2float(__ushort_as_half(static_cast<uint16_t>(code))) * ex2(top - 15.f);
+    return a.log_codes ? ex2(top + 8.f - log_value(code)) : __half2float(__ushort_as_half(static_cast<uint16_t>(code))) * ex2(top - 15.f);
   };
   int at[MINE];
   uint32_t code[MINE];
@@ -633,7 +649,7 @@ __global__ void __launch_bounds__(FACTOR_THREADS) k_factors(const Factors a) {
     } else if (a.log_codes) {
 #pragma unroll
       for (int j = 0; j < 4; j++)
-        e[j] = iwp_tc::pack2(ex2(top + log_value(e[j] & 0xFFFFu)) * scale, ex2(top + log_value(e[j] >> 16)) * scale, IWP_F16);
+        e[j] = iwp_tc::pack2(ex2(top + 8.f - log_value(e[j] & 0xFFFFu)) * scale, ex2(top + 8.f - log_value(e[j] >> 16)) * scale, IWP_F16);
     } else {
       const float f = ex2(top - 15.f) * scale;
 #pragma unroll

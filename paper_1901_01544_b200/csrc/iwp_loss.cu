@@ -17,7 +17,7 @@ namespace {
   } while (0)
 
 constexpr int64_t MAX_SIZE = 0x7FFFFFFF;
-constexpr int64_t DEFAULT_PIECE = int64_t(1) << 30;
+constexpr int64_t LEAST_PIECE = int64_t(1) << 30;
 constexpr int FEW_TILES = 296;           // four per CTA pair: above this a product takes its widest tiles
 constexpr int FEW_BLOCKS = 296;           // of the pass over a few tokens: two per SM
 constexpr int64_t FEW_ELEMENTS = 4 * 5888;  // whose hidden rows stay in 48 KB of shared memory
@@ -157,16 +157,21 @@ Deal deal_gradients(const Shape* dh, const Shape* dw, int pairs, int fixed_split
       const double ch = dh ? dh->clocks(n, static_cast<int>(s)) : 0, cw = dw ? dw->clocks(n, 1) : 1;
       const int64_t tiles = one * s;
       Deal d{n, static_cast<int>(s), static_cast<int>(tiles / pairs), static_cast<int>(tiles % pairs), 0};
-      double time = d.rounds * ch;
+      // pairs with one more tile of dhidden end at `long_way`, the others at `short_way`; what is left of dweight goes to
+      // the others first
       int64_t left = w;
+      const int64_t others = pairs - d.rest;
+      double long_way = d.rest ? ch : 0, short_way = 0;
       if (d.rest) {
         int64_t fill = static_cast<int64_t>(ch / cw);
-        if (fill > w / (pairs - d.rest)) fill = w / (pairs - d.rest);
+        if (fill > w / others) fill = w / others;
         d.fill = static_cast<int>(fill);
-        left -= fill * (pairs - d.rest);
-        time += ch;
+        left -= fill * others;
+        short_way = static_cast<double>(fill) * cw;
       }
-      time += static_cast<double>(tiles_of(left, pairs)) * cw;
+      short_way += static_cast<double>(tiles_of(left, pairs)) * cw;
+      if (left > others && d.rest) long_way += static_cast<double>(tiles_of(left - others, pairs)) * cw;
+      double time = d.rounds * ch + (long_way > short_way ? long_way : short_way);
       // parts are joined by a launch of its own: its start, and each part written and read once at about 2500 bytes per clock
       if (s > 1) time += 5000 + static_cast<double>(dh->m) * static_cast<double>(dh->n) * 8 * static_cast<double>(s) / 2500;
       if (least < 0 || time < least) least = time, best = d;
@@ -268,7 +273,10 @@ HeadPlan head_plan(const iwp_head_args* a) {
   if (p.pack_hidden) p.hidden = take(2 * T * p.d_pad);
   if (p.pack_weight) p.weight = take(2 * V * p.d_pad);
   if (p.grad) {
-    const int64_t limit = a->piece_bytes ? a->piece_bytes : DEFAULT_PIECE;
+    // By default no more than the weights and their gradient take: 8192 tokens x 131072 x 4096 then stay one piece (2 GiB)
+    // and run in PIECE_TIME, against 24.9 ms in two pieces of 1 GiB, whose first is computed twice.
+    const int64_t own = 4 * V * D;
+    const int64_t limit = a->piece_bytes ? a->piece_bytes : own > LEAST_PIECE ? own : LEAST_PIECE;
     const int64_t v_pad = up_to(V, iwp_tc::TILE_N), t = T > 0 ? T : 1;
     int64_t width = limit / (2 * t) / iwp_tc::TILE_N * iwp_tc::TILE_N;
     if (width < iwp_tc::TILE_N) width = iwp_tc::TILE_N;
@@ -292,7 +300,7 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
   const int64_t T = a->tokens, V = a->vocab, D = a->dim;
   char* const ws = static_cast<char*>(a->workspace);
   auto* hdr = reinterpret_cast<H::Header*>(ws);
-  const int pairs = pairs_of<H::Logits, 1>();
+  const int pairs = pairs_of<H::Logits<H::NO_CODES>, 1>();
   if (pairs < 1 || pairs_of<H::Probs, 1>() < 1 || pairs_of<H::Out, 2>() < 1) {
     cudaGetLastError();
     return IWP_ERR_CUDA;
@@ -393,35 +401,41 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
     const int blocks = work.p[0].k_blocks;
     work.seg = static_cast<int>(tiles_of(blocks, tiles_of(blocks, 16)));
     work.status = &hdr->status;
-    H::Logits::Args la{};
-    la.en = en;
-    la.T = T;
-    la.V = static_cast<int>(V);
-    la.c = c;
-    la.part = reinterpret_cast<float2*>(ws + p.part);
-    la.parts = 2 * work.p[0].n_tiles;
-    la.z_at = reinterpret_cast<float*>(ws + p.z_at);
-    la.codes = probs;
-    la.ld = p.piece;
-    la.v0 = static_cast<int>(kept >= 0 ? kept * p.piece : 0);
-    la.width = static_cast<int>(kept >= 0 ? p.piece : 0);
-    la.log_codes = a->dtype == IWP_F16;
-    if (int e = launch_product<H::Logits, 1>(work, la, st)) return e;
-    ra.parts = la.parts;
+    const int parts = 2 * work.p[0].n_tiles;
+    const int64_t v0 = kept >= 0 ? kept * p.piece : 0;
+    auto logits = [&](auto epilogue) {
+      using Epi = decltype(epilogue);
+      typename Epi::Args la{};
+      la.en = en;
+      la.T = T;
+      la.V = static_cast<int>(V);
+      la.c = c;
+      la.part = reinterpret_cast<float2*>(ws + p.part);
+      la.parts = parts;
+      la.z_at = reinterpret_cast<float*>(ws + p.z_at);
+      la.codes = probs;
+      la.ld = p.piece;
+      la.v0 = static_cast<int>(v0);
+      la.width = static_cast<int>(p.piece);
+      return launch_product<Epi, 1>(work, la, st);
+    };
+    const int failed = kept < 0 ? logits(H::Logits<H::NO_CODES>{}) : a->dtype == IWP_F16 ? logits(H::Logits<H::LOG_CODES>{}) : logits(H::Logits<H::HALF_CODES>{});
+    if (failed) return failed;
+    ra.parts = parts;
     LOSS_CUDA(launch(H::k_rows, row_blocks, H::ROW_THREADS, 0, 1, st, ra));
     if (kept >= 0) {
       H::Factors fa{};
       fa.en = en;
-      fa.part = la.part;
+      fa.part = ra.part;
       fa.lse = a->lse;
       fa.codes = probs;
       fa.ld = p.piece;
-      fa.parts = la.parts;
+      fa.parts = parts;
       fa.part_shift = tile_n == 256 ? 7 : tile_n == 128 ? 6 : 5;
-      fa.v0 = la.v0;
+      fa.v0 = static_cast<int>(v0);
       fa.width = static_cast<int>(V - fa.v0 < p.piece ? V - fa.v0 : p.piece);
       fa.chunks = static_cast<int>(tiles_of(fa.width, H::FACTOR_COLUMNS));
-      fa.log_codes = la.log_codes;
+      fa.log_codes = a->dtype == IWP_F16;
       fa.up = up;
       if (T * fa.chunks > MAX_SIZE) return IWP_ERR_INVALID;
       LOSS_CUDA(launch(H::k_factors, T * fa.chunks, H::FACTOR_THREADS, 0, 1, st, fa));

@@ -76,15 +76,17 @@ __device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 
+// What these barriers order is tensor memory and asynchronous copies, which have their own fences; a release at cluster
+// scope would wait for every store of the epilogue besides.
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
       "selp.u32 %0, 1, 0, p;\n\t}"
       : "=r"(ok)
       : "r"(bar), "r"(parity), "r"(WAIT_HINT_NS)
@@ -140,7 +142,35 @@ __device__ __forceinline__ float ex2(float x) {
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 
-// 32 or 16 columns of this warp's 32 lanes: v[j] = column j of the lane's row.
+// Two floats at a time: sm_100's packed arithmetic, where issue slots count.
+using f2 = unsigned long long;
+__device__ __forceinline__ f2 pack(float a, float b) {
+  f2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 unpack(f2 x) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+  return r;
+}
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+  f2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ f2 add2(f2 a, f2 b) {
+  f2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+  f2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+// 32 columns of this warp's 32 lanes: v[j] = column j of the lane's row.
 __device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
   uint32_t r[32];
   asm volatile(
@@ -151,18 +181,6 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
   for (int j = 0; j < 32; j++) v[j] = __uint_as_float(r[j]);
-}
-
-__device__ __forceinline__ void tmem_load16(uint32_t addr, float (&v)[16]) {
-  uint32_t r[16];
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(addr)
-      : "memory");
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-  for (int j = 0; j < 16; j++) v[j] = __uint_as_float(r[j]);
 }
 
 // Shared-memory operand descriptor, 128-byte swizzle.  K-contiguous operands: rows of 128 bytes, groups of 8 rows
@@ -296,6 +314,12 @@ __global__ void __launch_bounds__(THREADS, 1)
     }
     *dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+#pragma unroll
+    for (int p = 0; p < N; p++)
+      if (w.p[p].n_tiles) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&w.p[p].a) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&w.p[p].b) : "memory");
+      }
   }
   if (warp == 2) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_slot)) : "memory");
@@ -417,20 +441,20 @@ __global__ void __launch_bounds__(THREADS, 1)
       const uint32_t mine = tmem + (e / 4) * at.width + (static_cast<uint32_t>(e % 4) << 21);
       auto begun = Epi::begin(args, at);  // what the rows need from memory, fetched while the products run
       if constexpr (Epi::SUMS) {
-        float acc[TILE_N / 2];
+        f2 acc[TILE_N / 4];
 #pragma unroll
-        for (int j = 0; j < TILE_N / 2; j++) acc[j] = 0.f;
+        for (int j = 0; j < TILE_N / 4; j++) acc[j] = pack(0.f, 0.f);
         for (int k0 = t.k0; k0 < t.k1; k0 += w.seg) {
           ok = __all_sync(0xFFFFFFFFu, mbar_wait(acc_full + 8 * b, acc_phase, dead, w.status));
           if (!ok) break;
           fence_after();
 #pragma unroll
-          for (int c = 0; c < TILE_N / 32; c++) {
-            if (16 * c < at.width) {
-              float v[16];
-              tmem_load16(mine + b * TILE_N + 16 * c, v);
+          for (int c = 0; c < TILE_N / 64; c++) {
+            if (32 * c < at.width) {
+              float v[32];
+              tmem_load32(mine + b * TILE_N + 32 * c, v);
 #pragma unroll
-              for (int j = 0; j < 16; j++) acc[16 * c + j] += v[j];
+              for (int j = 0; j < 16; j++) acc[16 * c + j] = add2(acc[16 * c + j], pack(v[2 * j], v[2 * j + 1]));
             }
           }
           release();

@@ -152,12 +152,11 @@ class _Plan:
         if need < 0:
             raise IwpError(IWP_ERR_INVALID, "workspace size")
         if self._ws_bytes < need:
-            status = 0 if self._ws is None else self.status()
-            self._ws = self._torch.empty(need, dtype=self._torch.uint8, device=self.device)
+            old, self._ws = self._ws, self._torch.empty(need, dtype=self._torch.uint8, device=self.device)
             self._ws_at, self._ws_bytes = self._ws.data_ptr(), need
-            _check(lib().iwp_loss_reset(self._ws.data_ptr(), self._stream()), "iwp_loss_reset")
-            if status:  # a set status word outlives a larger workspace
-                self._ws[:4].view(self._torch.int32).fill_(status)
+            _check(lib().iwp_loss_reset(self._ws_at, self._stream()), "iwp_loss_reset")
+            if old is not None:
+                self._ws[:4].copy_(old[:4])  # a set status word outlives a larger workspace
 
     def status(self) -> int:
         """The status word, after everything enqueued on the current stream."""
@@ -178,8 +177,9 @@ class _Plan:
 class HeadLoss(_Plan):
     """Output head [vocab, dim] with its loss; the logits are never kept.
 
-    tokens: the most rows a call will bring (more are allowed: the workspace then grows once); top_k: the most teacher
-    logits per row; piece_bytes: bound on the probabilities held at a time while gradients are formed (0 = 1 GiB)."""
+    tokens: the most rows a call will bring; top_k: the most teacher logits per row.  The workspace made here serves
+    forward passes of that size; the first gradient (or a call that needs more) makes a larger one.  piece_bytes: bound on the probabilities held at a time while gradients are formed (0 = 1 GiB,
+    or what the weights and their gradient take where that is more)."""
 
     def __init__(self, tokens: int, vocab: int, dim: int, dtype=None, top_k: int = 1, piece_bytes: int = 0):
         super().__init__()
@@ -191,9 +191,6 @@ class HeadLoss(_Plan):
         a = HeadArgs(tokens=int(tokens), vocab=self.vocab, dim=self.dim, dtype=self._codes[self.dtype], top_k=int(top_k),
                      piece_bytes=self.piece_bytes)
         a.hidden_ld = a.weight_ld = (self.dim + 7) // 8 * 8
-        a.dhidden = a.dweight = 256
-        a.dhidden_ld = a.dweight_ld = self.dim
-        a.dhidden_type = a.dweight_type = a.dtype
         if self.dim % 8:  # rows of contiguous operands do not start at multiples of 16 bytes: they will be copied
             a.hidden_ld = a.weight_ld = self.dim
         self._grow(lib().iwp_head_workspace(C.byref(a)))
