@@ -178,8 +178,9 @@ class HeadLoss(_Plan):
     """Output head [vocab, dim] with its loss; the logits are never kept.
 
     tokens: the most rows a call will bring; top_k: the most teacher logits per row.  The workspace made here serves
-    forward passes of that size; the first gradient (or a call that needs more) makes a larger one.  piece_bytes: bound on the probabilities held at a time while gradients are formed (0 = 1 GiB,
-    or what the weights and their gradient take where that is more)."""
+    forward passes of that size; the first gradient (or a call that needs more) makes a larger one.  piece_bytes: bound
+    on the probabilities held at a time while gradients are formed (0 = 1 GiB, or what the weights and their gradient
+    take where that is more)."""
 
     def __init__(self, tokens: int, vocab: int, dim: int, dtype=None, top_k: int = 1, piece_bytes: int = 0):
         super().__init__()
@@ -358,3 +359,64 @@ class ExpertBalance(_Plan):
     def grad(self, logits, ids, mask=None, *, coef: float = 0.01, dloss=None, scale: float = 1.0, dlogits=None) -> BalanceResult:
         """The same with the gradient to the logits, times `scale` and the upstream gradient `dloss` (0-d)."""
         return self._run(logits, ids, mask, coef, dloss, scale, True, dlogits)
+
+
+# ---- differentiable forms ----------------------------------------------------------------------
+
+
+def _functions():
+    """autograd.Function classes around the plans, made on first use (importing this module does not import torch)."""
+    global _autograd
+    if _autograd is None:
+        import torch
+
+        class Head(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, hidden, weight, plan, kind, args, kwargs):
+                r = getattr(plan, kind)(hidden, weight, *args, **kwargs)
+                ctx.plan, ctx.kind, ctx.args, ctx.kwargs = plan, kind, args, kwargs
+                ctx.save_for_backward(hidden, weight, r.lse)
+                return r.loss.clone()
+
+            @staticmethod
+            def backward(ctx, dloss):
+                hidden, weight, lse = ctx.saved_tensors
+                want = tuple(n for n, need in zip(("hidden", "weight"), ctx.needs_input_grad) if need)
+                r = getattr(ctx.plan, ctx.kind + "_grad")(hidden, weight, *ctx.args, lse=lse, dloss=dloss.float(), want=want, **ctx.kwargs)
+                return r.dhidden, r.dweight, None, None, None, None
+
+        class Balance(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, logits, plan, ids, mask, coef):
+                ctx.plan, ctx.mask, ctx.coef = plan, mask, coef
+                ctx.save_for_backward(logits, ids)
+                r = plan.loss(logits, ids, mask, coef=coef)
+                ctx.mark_non_differentiable(r.counts)
+                return r.loss.clone(), r.counts
+
+            @staticmethod
+            def backward(ctx, dloss, _):
+                logits, ids = ctx.saved_tensors
+                return ctx.plan.grad(logits, ids, ctx.mask, coef=ctx.coef, dloss=dloss.float()).dlogits, None, None, None, None
+
+        _autograd = (Head, Balance)
+    return _autograd
+
+
+_autograd = None
+
+
+def cross_entropy(plan: HeadLoss, hidden, weight, targets, **kwargs):
+    """The loss of plan.cross_entropy as a differentiable function of hidden and weight.  Only lse is kept for the
+    backward pass, which forms the probabilities anew, piece by piece."""
+    return _functions()[0].apply(hidden, weight, plan, "cross_entropy", (targets,), kwargs)
+
+
+def distill(plan: HeadLoss, hidden, weight, top_ids, top_logits, temperature: float = 1.0, **kwargs):
+    """The loss of plan.distill as a differentiable function of hidden and weight (not of the teacher's logits)."""
+    return _functions()[0].apply(hidden, weight, plan, "distill", (top_ids, top_logits, temperature), kwargs)
+
+
+def balance(plan: ExpertBalance, logits, ids, mask=None, coef: float = 0.01):
+    """(loss, counts) of plan.loss, the loss a differentiable function of the router's logits."""
+    return _functions()[1].apply(logits, plan, ids, mask, coef)

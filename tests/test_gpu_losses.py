@@ -529,3 +529,51 @@ def test_repeated_teacher_ids_add_up():
     check_head(plan.distill_grad(h, w, ids, logits, 1.5), head_reference(h, w, ids, soft_targets(ids, logits, 1.5), 1.5, True))
     small = losses.HeadLoss(T, V, D, BF, top_k=K, piece_bytes=1)
     check_head(small.distill_grad(h, w, ids, logits, 1.5), head_reference(h, w, ids, soft_targets(ids, logits, 1.5), 1.5, True))
+
+
+def test_differentiable_forms():
+    T, V, D, E = 200, 900, 64, 16
+    h, w, y, g = operands(T, V, D, BF, 300)
+    plan, router = losses.HeadLoss(T, V, D, BF, top_k=6), losses.ExpertBalance(T, E)
+    ids = torch.rand(T, V, generator=g, device=DEV).argsort(1)[:, :6].contiguous()
+    logits = torch.randn(T, 6, generator=g, device=DEV)
+    h.requires_grad_(), w.requires_grad_()
+    (3.0 * losses.cross_entropy(plan, h, w, y)).backward()
+    ref = head_reference(h.detach(), w.detach(), y[:, None], torch.ones(T, 1, dtype=torch.float64, device=DEV), 1.0, True)
+    close_grad(h.grad, ref["dH"], ref["h_err"], "dhidden", 3.0)
+    close_grad(w.grad, ref["dW"], ref["w_err"], "dweight", 3.0)
+    h.grad = w.grad = None
+    w.requires_grad_(False)
+    loss = losses.distill(plan, h, w, ids, logits, 2.0, reduction="sum")
+    loss.backward()
+    ref = head_reference(h.detach(), w, ids, soft_targets(ids, logits, 2.0), 2.0, False)
+    close_grad(h.grad, ref["dH"], ref["h_err"], "dhidden")
+    assert w.grad is None
+    x = torch.randn(T, E, generator=g, device=DEV, requires_grad=True)
+    chosen = torch.topk(x.detach(), 2, dim=1).indices
+    loss, counts = losses.balance(router, x, chosen, None, 0.5)
+    (2.0 * loss).backward()
+    ref = balance_reference(x.detach(), chosen, None, 0.5)
+    assert torch.equal(counts.long(), ref["counts"])
+    assert (x.grad.double() - 2 * ref["dx"]).abs().max() <= 2.0**-16 * ref["scale_dx"].max() * 2
+
+
+def test_workspace_grows_and_keeps_the_status_word():
+    h, w, y, _ = operands(40, 500, 64, BF, 301)
+    plan = losses.HeadLoss(8, 500, 64, BF)
+    bad = y.clone()
+    bad[0] = 500
+    plan.cross_entropy(h[:8], w, bad[:8])
+    r = plan.cross_entropy_grad(h, w, y)  # more tokens, and gradients
+    ref = head_reference(h, w, y[:, None], torch.ones(40, 1, dtype=torch.float64, device=DEV), 1.0, True)
+    check_head(r, ref)
+    assert plan.status() == -1
+
+
+def test_example_trains():
+    from paper_1901_01544_b200 import train_head
+
+    history, counts = train_head.train(steps=12, workers=3, tokens=256, vocab=1003, dim=128)
+    first, last = history[0], history[-1]
+    assert last[0] < 0.8 * first[0] and last[1] < 0.8 * first[1]
+    assert sum(counts) == 3 * 256 * 2
