@@ -48,7 +48,8 @@ int iwp_loss_status(const void* workspace, int32_t* status_host, void* cuda_stre
  * The gradient's factors exp(..) - q are rounded once to the operands' type, as the tensor cores take no wider one.
  */
 typedef struct iwp_head_args {
-  int64_t tokens, vocab, dim;      /* T >= 0, 1 <= V, 1 <= D; each below 2^31 */
+  int64_t tokens, vocab, dim;      /* T >= 0, 1 <= V, 1 <= D; each below 2^31 - 1024, their products
+                                      at most 2^46 */
   const void* hidden;              /* [T][D], row stride hidden_ld elements */
   int64_t hidden_ld;
   const void* weight;              /* [V][D], row stride weight_ld elements */

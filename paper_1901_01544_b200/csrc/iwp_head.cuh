@@ -683,13 +683,15 @@ struct Few {
   float c;
 };
 
-constexpr int FEW_TOKENS = 4, FEW_THREADS = 512, FEW_ROWS = 4;
+constexpr int FEW_TOKENS = 2, FEW_THREADS = 512, FEW_ROWS = 4;
 
-// Four rows of the weights per warp at a time, streamed once: a dot product with at most four tokens is bound by the
-// weights' bytes, and plain loads keep more of them in flight than the tensor cores' 128-row tiles would.  Operand rows
-// start at multiples of 16 bytes and hold whole ones (copies made by k_align_rows end in zeros).
+// Four rows of the weights per warp at a time, streamed once: dot products with one or two tokens are bound by the weights'
+// bytes, and plain loads keep more of them in flight than the tensor cores' 128-row tiles would (131072 x 4096, one token:
+// 162 us = 6.6 TB/s, against 253 by tiles; two tokens 178 and 214; from three on, tiles are as fast).  A group of 8
+// elements is widened once per row and once per token.  Operand rows start at multiples of 16 bytes and hold whole ones
+// (copies made by k_align_rows end in zeros).
 template <int TOKENS>
-__global__ void __launch_bounds__(FEW_THREADS) k_few_tokens(const Few a) {
+__global__ void __launch_bounds__(FEW_THREADS, 2) k_few_tokens(const Few a) {
   constexpr int WARPS = FEW_THREADS / 32;
   extern __shared__ uint4 sh_hidden[];  // [TOKENS][D / 8, rounded up]
   __shared__ float2 sh[WARPS][TOKENS];
@@ -707,39 +709,32 @@ __global__ void __launch_bounds__(FEW_THREADS) k_few_tokens(const Few a) {
   iwp_tc::wait_previous();
   for (int i = tid; i < TOKENS * groups; i += FEW_THREADS) {
     const int t = i / groups, g = i - t * groups;
-    const uint4 x = *reinterpret_cast<const uint4*>(hidden + t * a.hidden_ld + 8 * g);
-    sh_hidden[i] = x;
+    sh_hidden[i] = *reinterpret_cast<const uint4*>(hidden + t * a.hidden_ld + 8 * g);
   }
   __syncthreads();
-  auto dot8 = [&](const uint4& w, int g, float (&acc)[TOKENS]) {
-    const uint32_t* const we = reinterpret_cast<const uint32_t*>(&w);
-    float2 y[4];
+  auto load8 = [&](const uint16_t* row, int g) { return __ldcs(reinterpret_cast<const uint4*>(row + 8 * g)); };
+  auto widen = [&](const uint4& x, f2 (&y)[4]) {
+    const uint32_t* const e = reinterpret_cast<const uint32_t*>(&x);
 #pragma unroll
-    for (int j = 0; j < 4; j++) y[j] = iwp_tc::unpack2(we[j], a.type);
-#pragma unroll
-    for (int t = 0; t < TOKENS; t++) {
-      const uint4 h = sh_hidden[t * groups + g];
-      const uint32_t* const he = reinterpret_cast<const uint32_t*>(&h);
-#pragma unroll
-      for (int j = 0; j < 4; j++) {
-        const float2 x = iwp_tc::unpack2(he[j], a.type);
-        acc[t] = fmaf(x.x, y[j].x, fmaf(x.y, y[j].y, acc[t]));
-      }
+    for (int j = 0; j < 4; j++) {
+      const float2 v = iwp_tc::unpack2(e[j], a.type);
+      y[j] = pack(v.x, v.y);
     }
   };
-  auto load8 = [&](const uint16_t* row, int g) { return __ldcs(reinterpret_cast<const uint4*>(row + 8 * g)); };
   if (static_cast<int>(blockIdx.x) >= a.blocks) {  // logits at the targets, a warp each
     const int i = (blockIdx.x - a.blocks) * WARPS + warp;
     if (i >= a.T * a.en.k) return;
     const int t = i / a.en.k, col = a.en.column_at(t, i - t * a.en.k);
     if (col == NO_COLUMN) return;
-    float acc[TOKENS] = {};
-    for (int g = lane; g < groups; g += 32) dot8(load8(weight + col * a.weight_ld, g), g, acc);
-    float z = 0.f;
+    f2 acc = pack(0.f, 0.f);
+    for (int g = lane; g < groups; g += 32) {
+      f2 x[4], y[4];
+      widen(load8(weight + col * a.weight_ld, g), x);
+      widen(sh_hidden[t * groups + g], y);
 #pragma unroll
-    for (int j = 0; j < TOKENS; j++)
-      if (j == t) z = acc[j];
-    z = warp_sum(z);
+      for (int j = 0; j < 4; j++) acc = fma2(x[j], y[j], acc);
+    }
+    const float z = warp_sum(unpack(acc).x + unpack(acc).y);
     if (lane == 0) a.z_at[i] = z;
     return;
   }
@@ -747,7 +742,11 @@ __global__ void __launch_bounds__(FEW_THREADS) k_few_tokens(const Few a) {
 #pragma unroll
   for (int t = 0; t < TOKENS; t++) m[t] = -CUDART_INF_F, s[t] = 0.f;
   for (int v = (blockIdx.x * WARPS + warp) * FEW_ROWS; v < a.V; v += a.blocks * WARPS * FEW_ROWS) {
-    float acc[FEW_ROWS][TOKENS] = {};
+    f2 acc[FEW_ROWS][TOKENS];
+#pragma unroll
+    for (int r = 0; r < FEW_ROWS; r++)
+#pragma unroll
+      for (int t = 0; t < TOKENS; t++) acc[r][t] = pack(0.f, 0.f);
     const uint16_t* const row = weight + v * a.weight_ld;
     const int have = min(FEW_ROWS, a.V - v);
 #pragma unroll 2
@@ -755,15 +754,27 @@ __global__ void __launch_bounds__(FEW_THREADS) k_few_tokens(const Few a) {
       uint4 w[FEW_ROWS];
 #pragma unroll
       for (int r = 0; r < FEW_ROWS; r++) w[r] = load8(row + min(r, have - 1) * a.weight_ld, g);
+      f2 y[TOKENS][4];
 #pragma unroll
-      for (int r = 0; r < FEW_ROWS; r++) dot8(w[r], g, acc[r]);
+      for (int t = 0; t < TOKENS; t++) widen(sh_hidden[t * groups + g], y[t]);
+#pragma unroll
+      for (int r = 0; r < FEW_ROWS; r++) {
+        f2 x[4];
+        widen(w[r], x);
+#pragma unroll
+        for (int t = 0; t < TOKENS; t++)
+#pragma unroll
+          for (int j = 0; j < 4; j++) acc[r][t] = fma2(x[j], y[t][j], acc[r][t]);
+      }
     }
 #pragma unroll
     for (int t = 0; t < TOKENS; t++) {
       float z[FEW_ROWS], top = m[t];
 #pragma unroll
       for (int r = 0; r < FEW_ROWS; r++) {
-        z[r] = r < have ? warp_sum(acc[r][t]) * a.c : -CUDART_INF_F;
+        const float2 both = unpack(acc[r][t]);
+        z[r] = warp_sum(both.x + both.y) * a.c;
+        if (r >= have) z[r] = -CUDART_INF_F;
         top = fmaxf(top, z[r]);
       }
       const float ref = top == -CUDART_INF_F ? 0.f : top;

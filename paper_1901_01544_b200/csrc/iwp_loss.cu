@@ -1,6 +1,8 @@
 // iwp_loss.cu - C entries of the losses (include/iwp_loss.h): argument checks, workspace layout, launches.
+#include <atomic>
 #include <cmath>
 #include <cstring>
+#include <type_traits>
 #include <utility>
 
 #include "iwp_balance.cuh"
@@ -16,11 +18,12 @@ namespace {
     }                              \
   } while (0)
 
-constexpr int64_t MAX_SIZE = 0x7FFFFFFF;
+constexpr int64_t MAX_SIZE = 0x7FFFFFFF - 1023;  // tiles may reach beyond it without leaving 32 bits
+constexpr int64_t MAX_ELEMENTS = int64_t(1) << 46;
 constexpr int64_t LEAST_PIECE = int64_t(1) << 30;
 constexpr int FEW_TILES = 296;           // four per CTA pair: above this a product takes its widest tiles
 constexpr int FEW_BLOCKS = 296;           // of the pass over a few tokens: two per SM
-constexpr int64_t FEW_ELEMENTS = 4 * 5888;  // whose hidden rows stay in 48 KB of shared memory
+constexpr int64_t FEW_ELEMENTS = 32768;   // of hidden states, which stay in 64 KB of shared memory
 constexpr int64_t JOIN_TILES = 2 * 148;  // a split dhidden has at most this many partial tiles
 
 inline int64_t up_to(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
@@ -86,7 +89,7 @@ cudaError_t launch(void (*kernel)(Params...), int64_t grid, int block, size_t sm
 // How many CTA pairs of a product kernel the device holds at once: the persistent grid (a pair that had to wait for
 // another to end would double the time).  Looked up once per device, with the kernel's shared memory limit.
 template <class Kernel>
-int resident_pairs(Kernel kernel, int* cached) {
+int resident_pairs(Kernel kernel, std::atomic<int>* cached) {
   const int dev = device();
   if (dev < 0) return 0;
   if (cached[dev]) return cached[dev];
@@ -103,7 +106,8 @@ int resident_pairs(Kernel kernel, int* cached) {
   cfg.numAttrs = 1;
   int n = 0;
   if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) return 0;
-  return cached[dev] = n;
+  cached[dev] = n;
+  return n;
 }
 
 struct Matrix {
@@ -117,16 +121,17 @@ struct Shape {
   int64_t k_blocks() const { return tiles_of(k, iwp_tc::BLOCK_K); }
   int64_t tiles(int n_cols) const { return m_tiles() * tiles_of(n, n_cols); }
   // clocks of a tile with its K in `splits` parts, about: per block of K the products or the loads, whichever takes
-  // longer (32, 28, 24 or 20 KB per CTA), but no less than an epilogue
+  // longer (32, 24 or 20 KB per CTA), but no less than an epilogue
   double clocks(int n_cols, int splits) const {
-    const double block = n_cols == 256 ? 520 : n_cols == 192 ? 450 : n_cols == 128 ? 385 : 320;
+    const double block = n_cols == 256 ? 520 : n_cols == 128 ? 385 : 320;
     const double products = static_cast<double>(tiles_of(k_blocks(), splits)) * block, epilogue = 1000 + 12.0 * n_cols;
     return (products > epilogue ? products : epilogue) + 300;
   }
 };
 
 // Width of a single product's tiles: 256 where there are tiles enough for all pairs, less where the narrower tiles'
-// shorter time wins over their poorer use of the loads.
+// shorter time wins over their poorer use of the loads.  (256 x 1000 x 2048, all of a training pass: 32.5 us with narrow
+// tiles, 36.9 with 256; 40 x 8192 x 512: 32.0 and 33.2; from a few hundred wide tiles on there is no difference.)
 int pick_tile_n(const Shape& s, int pairs) {
   if (s.tiles(256) > FEW_TILES) return 256;
   int best = 256;
@@ -147,9 +152,9 @@ struct Deal {
 Deal deal_gradients(const Shape* dh, const Shape* dw, int pairs, int fixed_splits) {
   Deal best{256, 1, 0, 0, 0};
   double least = -1;
-  for (int n : {256, 192, 128, 64}) {
+  for (int n : {256, 128, 64}) {
     const int64_t one = dh ? dh->tiles(n) : 0, w = dw ? dw->tiles(n) : 0;
-    if (n < 192 && one + w > FEW_TILES) break;
+    if (n < 256 && one + w > FEW_TILES) break;
     int64_t most = dh ? dh->k_blocks() / 4 : 1;
     if (dh && most > JOIN_TILES / one) most = JOIN_TILES / one;
     if (most < 1) most = 1;
@@ -202,7 +207,7 @@ bool make_problem(iwp_tc::Problem* q, const Matrix& A, bool a_kc, const Matrix& 
 
 template <class Epi, int N>
 int pairs_of() {
-  static int cached[MAX_DEVICES] = {};
+  static std::atomic<int> cached[MAX_DEVICES] = {};
   return resident_pairs(iwp_tc::k_product<N, Epi>, cached);
 }
 
@@ -232,10 +237,12 @@ struct HeadPlan {
 bool needs_copy(const void* p, int64_t ld) { return !aligned(p, 16) || ld % 8 != 0; }
 
 bool head_args_ok(const iwp_head_args* a) {
-  if (!a || a->tokens < 0 || a->tokens > MAX_SIZE || a->vocab < 1 || a->vocab > MAX_SIZE - 1024 || a->dim < 1 || a->dim > MAX_SIZE) return false;
+  if (!a || a->tokens < 0 || a->tokens > MAX_SIZE || a->vocab < 1 || a->vocab > MAX_SIZE || a->dim < 1 || a->dim > MAX_SIZE) return false;
+  // (what no device could hold, so that sizes in bytes stay far from the end of 64 bits)
+  if (a->tokens * a->vocab > MAX_ELEMENTS || a->tokens * a->dim > MAX_ELEMENTS || a->vocab * a->dim > MAX_ELEMENTS) return false;
   if (a->dtype != IWP_BF16 && a->dtype != IWP_F16) return false;
   if (!a->targets && (a->top_k < 1 || a->top_k > iwp_head::MAX_TOP)) return false;
-  if (a->hidden_ld < a->dim || a->weight_ld < a->dim) return false;
+  if (a->hidden_ld < a->dim || a->weight_ld < a->dim || a->hidden_ld > MAX_SIZE || a->weight_ld > MAX_SIZE) return false;
   if (a->dhidden && (a->dhidden_ld < a->dim || (a->dhidden_type != a->dtype && a->dhidden_type != IWP_F32))) return false;
   if (a->dweight && (a->dweight_ld < a->dim || (a->dweight_type != a->dtype && a->dweight_type != IWP_F32))) return false;
   return a->piece_bytes >= 0;
@@ -249,7 +256,7 @@ HeadPlan head_plan(const iwp_head_args* a) {
   p.d_pad = up_to(D, 8);
   p.pack_hidden = needs_copy(a->hidden, a->hidden_ld);
   p.pack_weight = needs_copy(a->weight, a->weight_ld);
-  p.few = !p.grad && T <= iwp_head::FEW_TOKENS && T * D <= FEW_ELEMENTS && (D % 8 == 0 || (p.pack_hidden && p.pack_weight));
+  p.few = !p.grad && T <= iwp_head::FEW_TOKENS && T * up_to(D, 8) <= FEW_ELEMENTS && (D % 8 == 0 || (p.pack_hidden && p.pack_weight));
   int64_t at = 256;
   auto take = [&at](int64_t n) {
     const int64_t o = at;
@@ -382,12 +389,20 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
       const int64_t whole = tiles_of(V, warps * H::FEW_ROWS);
       fa.blocks = static_cast<int>(whole < FEW_BLOCKS ? whole : FEW_BLOCKS);
       const int64_t grid = fa.blocks + tiles_of(T * p.k, warps);
-      const size_t smem = static_cast<size_t>(16 * T * tiles_of(D, 8));
-      LOSS_CUDA(launch(T == 1   ? H::k_few_tokens<1>
-                       : T == 2 ? H::k_few_tokens<2>
-                       : T == 3 ? H::k_few_tokens<3>
-                                : H::k_few_tokens<4>,
-                       grid, H::FEW_THREADS, smem, 1, st, fa));
+      auto few = [&](auto tokens) {
+        constexpr int N = decltype(tokens)::value;
+        auto kernel = H::k_few_tokens<N>;
+        static std::atomic<bool> ready[MAX_DEVICES] = {};
+        const int dev = device();
+        if (dev < 0) return cudaErrorInvalidDevice;
+        if (!ready[dev]) {
+          const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(2 * FEW_ELEMENTS));
+          if (e != cudaSuccess) return e;
+          ready[dev] = true;
+        }
+        return launch(kernel, grid, H::FEW_THREADS, static_cast<size_t>(16 * N * tiles_of(D, 8)), 1, st, fa);
+      };
+      LOSS_CUDA(T == 1 ? few(std::integral_constant<int, 1>{}) : few(std::integral_constant<int, 2>{}));
       ra.parts = fa.blocks;
       LOSS_CUDA(launch(H::k_rows, row_blocks, H::ROW_THREADS, 0, 1, st, ra));
       return IWP_OK;
@@ -542,30 +557,51 @@ bool balance_args_ok(const iwp_balance_args* a) {
 }
 
 constexpr int BALANCE_BLOCKS = 148;  // at most, of the rows kernel
-// Up to this many bytes of logits and ids one cluster serves: it saves the second launch and its 16 SMs keep up.
+// Up to this many bytes of logits and ids one cluster serves: it saves the second launch and its 16 SMs keep up
+// (0.7 MB: 12.6 us in one launch, 19.8 in two; 2.5 MB: 17.1 and 17.8; 5 MB: 25.8 and 15.4).
 constexpr int64_t CLUSTER_BYTES = int64_t(3) << 20;
 
 int64_t balance_part_counts_bytes(int E) { return up_to(int64_t(iwp_balance::COUNT_PARTS) * (E + 1) * 4, 256); }
+
+// 16 CTAs (above the portable size, which the kernel has opted in to) where the device can hold such a cluster, else 8.
+template <class Kernel>
+int largest_cluster(Kernel kernel, int threads, int smem) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(iwp_balance::MAX_CLUSTER);
+  cfg.blockDim = dim3(static_cast<unsigned>(threads));
+  cfg.dynamicSmemBytes = static_cast<size_t>(smem);
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = iwp_balance::MAX_CLUSTER;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  int n = 0;
+  if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) cudaGetLastError();
+  return n > 0 ? iwp_balance::MAX_CLUSTER : 8;
+}
 
 template <int TYPE, int VEC, int N>
 int balance_launch(iwp_balance::Args a, int G, cudaStream_t st) {
   namespace B = iwp_balance;
   constexpr int threads = B::threads_of(VEC * N), slots = B::slot_bytes(VEC * N, TYPE == IWP_F32 ? 4 : 2);
   auto kernel = B::k_balance_rows<TYPE, VEC, N>;
-  static bool ready[MAX_DEVICES] = {};
+  static std::atomic<bool> ready[MAX_DEVICES] = {};
+  static std::atomic<int> cluster[MAX_DEVICES] = {};
   const int dev = device();
   if (dev < 0) return IWP_ERR_CUDA;
   if (!ready[dev]) {
     LOSS_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, slots));
     LOSS_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    cluster[dev] = largest_cluster(kernel, threads, slots);
     ready[dev] = true;
   }
   const int64_t steps = tiles_of(a.T, threads / G);
   const int64_t bytes = a.T * (a.E * (TYPE == IWP_F32 ? 4 : 2) + a.k * a.ids_bytes);
   if (bytes <= CLUSTER_BYTES) {
-    // CTAs for about two rounds of rows each; 16 need the opt-in to clusters above the portable size
+    // CTAs for about two rounds of rows each
     int ctas = 1;
-    while (ctas < B::MAX_CLUSTER && 2 * ctas < steps) ctas *= 2;
+    while (ctas < cluster[dev] && 2 * ctas < steps) ctas *= 2;
     a.part_counts = nullptr;
     LOSS_CUDA(launch(kernel, ctas, threads, slots, ctas, st, a, G));
     return IWP_OK;
@@ -630,7 +666,12 @@ extern "C" int iwp_head_loss(const iwp_head_args* a, void* cuda_stream) {
   if (a->dhidden && !aligned(a->dhidden, a->dhidden_type == IWP_F32 ? 4 : 2)) return IWP_ERR_INVALID;
   if (a->dweight && !aligned(a->dweight, a->dweight_type == IWP_F32 ? 4 : 2)) return IWP_ERR_INVALID;
   if (!std::isfinite(a->scale)) return IWP_ERR_INVALID;
+  for (const void* x : {static_cast<const void*>(a->loss), static_cast<const void*>(a->rows), static_cast<const void*>(a->lse),
+                        static_cast<const void*>(a->dloss), static_cast<const void*>(a->dloss_rows)})
+    if (!aligned(x, 4)) return IWP_ERR_INVALID;
+  if (!aligned(a->targets, 8)) return IWP_ERR_INVALID;
   if (!a->targets) {
+    if (!aligned(a->top_ids, a->ids_bytes == 8 ? 8 : 4) || !aligned(a->top_logits, a->top_type == IWP_F32 ? 4 : 2)) return IWP_ERR_INVALID;
     if (!a->top_ids || !a->top_logits || a->top_ids_ld < a->top_k || a->top_logits_ld < a->top_k) return IWP_ERR_INVALID;
     if ((a->ids_bytes != 4 && a->ids_bytes != 8) || a->top_type < IWP_F32 || a->top_type > IWP_F16) return IWP_ERR_INVALID;
     if (!(a->temperature > 0.f) || !std::isfinite(a->temperature)) return IWP_ERR_INVALID;
@@ -653,6 +694,8 @@ extern "C" int iwp_balance_loss(const iwp_balance_args* a, void* cuda_stream) {
   if (a->logits_ld < a->experts || a->ids_ld < a->top_k || (a->ids_bytes != 4 && a->ids_bytes != 8)) return IWP_ERR_INVALID;
   if (a->dlogits && a->dlogits_ld < a->experts) return IWP_ERR_INVALID;
   if (!aligned(a->logits, size) || (a->dlogits && !aligned(a->dlogits, size)) || !aligned(a->ids, a->ids_bytes)) return IWP_ERR_INVALID;
+  if (!aligned(a->loss, 4) || !aligned(a->counts, 4) || !aligned(a->mean_prob, 4) || !aligned(a->dloss, 4)) return IWP_ERR_INVALID;
+  if (a->tokens * a->experts > MAX_ELEMENTS || a->logits_ld > MAX_SIZE || a->dlogits_ld > MAX_SIZE || a->ids_ld > MAX_SIZE) return IWP_ERR_INVALID;
   if (!std::isfinite(a->coef) || !std::isfinite(a->scale)) return IWP_ERR_INVALID;
   if (a->workspace_bytes < iwp_balance_workspace(a)) return IWP_ERR_CAPACITY;
   char* const ws = static_cast<char*>(a->workspace);

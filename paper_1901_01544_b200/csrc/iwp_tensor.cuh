@@ -197,7 +197,7 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t addr, bool k_contiguou
 struct Problem {
   CUtensorMap a, b;
   int m_tiles, n_tiles;  // tiles of CG * TILE_M rows and tile_n columns
-  int tile_n;            // 256, 192, 128 or 64
+  int tile_n;            // 256, 128 or 64
   int k_blocks;          // blocks of BLOCK_K along K
   int splits;            // the K range in this many parts (each part a tile of its own)
   uint32_t idesc;
@@ -350,8 +350,8 @@ __global__ void __launch_bounds__(THREADS, 1)
         const int row_a = t.m * TILE_M * CG + static_cast<int>(rank) * TILE_M;
         const int row_b = t.n * q.tile_n + static_cast<int>(rank) * rows_b;
         const bool a_kc = q.a_kc, b_kc = q.b_kc;
-        // M/N-contiguous boxes are 64 columns wide even where a CTA needs 32 of them
-        const uint32_t bytes = CG * (A_BYTES + (b_kc ? rows_b : (rows_b + 63) / 64 * 64) * BLOCK_K * 2);
+        // an M/N-contiguous box is 64 columns wide even where a CTA needs 32 of them
+        const uint32_t bytes = CG * (A_BYTES + (b_kc ? rows_b : max(rows_b, 64)) * BLOCK_K * 2);
         for (int kb = t.k0; kb < t.k1; kb++) {
           if (!mbar_wait(empty + 8 * s, phase ^ 1, dead, w.status)) break;
           if (rank == 0) mbar_expect(full + 8 * s, bytes);
