@@ -138,6 +138,7 @@ __device__ __forceinline__ float* staged_at(const Where& w, int i) {
 template <int CODES>
 struct Logits {
   static constexpr bool SUMS = true;
+  static constexpr int AREAS = 1;
   struct Args {
     Targets en;
     int64_t T;
@@ -223,6 +224,7 @@ struct Logits {
 
 struct Probs {
   static constexpr bool SUMS = false;
+  static constexpr int AREAS = 1;
   struct Args {
     Targets en;
     const float* lse;
@@ -302,18 +304,45 @@ struct Factor {
 
 struct Out {
   static constexpr bool SUMS = false;
+  static constexpr int AREAS = 2;
   struct Matrix {
     void* out;
     int64_t ld, split_stride;  // elements
     int rows, cols, type, wide, add, raw;  // raw: partial sums, the factor is applied later
+    int by_copy;                           // 16-bit rows that start at multiples of 16 bytes, nothing to add
+    CUtensorMap map;                       // of `out` then, in boxes of 32 rows and 64 columns
   };
   struct Args {
     Factor f;
     Matrix m[2];
   };
   static __device__ __forceinline__ float begin(const Args& args, const Where& w) { return args.m[w.p].raw ? 1.f : args.f.get(); }
-  static __device__ __forceinline__ void tile(const Args& args, const Where& w, float f, uint32_t tmem) {
+  static __device__ __forceinline__ void tile(const Args& args, Where& w, float f, uint32_t tmem) {
     const Matrix& a = args.m[w.p];
+    if (a.by_copy && w.width >= 64) {
+#pragma unroll 1
+      for (int c0 = w.col0; c0 < min(w.col0 + w.width, a.cols); c0 += 64) {
+        uint32_t packed[32];
+#pragma unroll
+        for (int half = 0; half < 2; half++) {
+          float v[32];
+          iwp_tc::tmem_load32(tmem + (c0 - w.col0) + 32 * half, v);
+#pragma unroll
+          for (int j = 0; j < 16; j++) packed[16 * half + j] = iwp_tc::pack2(v[2 * j] * f, v[2 * j + 1] * f, a.type);
+        }
+        if (w.row0 >= a.rows) continue;  // (the accumulator is read whole all the same: a warp's loads are collective)
+        iwp_tc::staging_free<1>(w.lane);
+        char* const area = w.staging + w.area * iwp_tc::STAGING_BYTES;
+        w.area ^= 1;
+#pragma unroll
+        for (int j = 0; j < 8; j++)
+          *reinterpret_cast<uint4*>(iwp_tc::staged(area, w.lane, j)) =
+              make_uint4(packed[4 * j], packed[4 * j + 1], packed[4 * j + 2], packed[4 * j + 3]);
+        iwp_tc::store_staged(&a.map, area, w.row0, c0, w.lane);
+      }
+      return;
+    }
+    iwp_tc::staging_free<0>(w.lane);
     char* const out = static_cast<char*>(a.out) + w.split * a.split_stride * (a.type == IWP_F32 ? 4 : 2);
 #pragma unroll 1
     for (int c0 = w.col0; c0 < min(w.col0 + w.width, a.cols); c0 += 32) {

@@ -47,7 +47,7 @@ Encode encoder() {
   return fn;
 }
 
-// A row-major matrix of 16-bit elements, read in boxes of box_rows rows and 64 elements (128 bytes, swizzled).
+// A row-major matrix of 16-bit elements, copied in boxes of box_rows rows and 64 elements (128 bytes, swizzled).
 // Elements outside read as zero.
 bool make_map(CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int64_t ld, int box_rows, int dtype) {
   Encode enc = encoder();
@@ -89,15 +89,15 @@ cudaError_t launch(void (*kernel)(Params...), int64_t grid, int block, size_t sm
 // How many CTA pairs of a product kernel the device holds at once: the persistent grid (a pair that had to wait for
 // another to end would double the time).  Looked up once per device, with the kernel's shared memory limit.
 template <class Kernel>
-int resident_pairs(Kernel kernel, std::atomic<int>* cached) {
+int resident_pairs(Kernel kernel, int smem, std::atomic<int>* cached) {
   const int dev = device();
   if (dev < 0) return 0;
   if (cached[dev]) return cached[dev];
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, iwp_tc::SMEM) != cudaSuccess) return 0;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return 0;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(iwp_tc::CG);
   cfg.blockDim = dim3(iwp_tc::THREADS);
-  cfg.dynamicSmemBytes = iwp_tc::SMEM;
+  cfg.dynamicSmemBytes = static_cast<size_t>(smem);
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
   at[0].val.clusterDim.x = iwp_tc::CG;
@@ -121,10 +121,11 @@ struct Shape {
   int64_t k_blocks() const { return tiles_of(k, iwp_tc::BLOCK_K); }
   int64_t tiles(int n_cols) const { return m_tiles() * tiles_of(n, n_cols); }
   // clocks of a tile with its K in `splits` parts, about: per block of K the products or the loads, whichever takes
-  // longer (32, 24 or 20 KB per CTA), but no less than an epilogue
+  // longer (32, 24 or 20 KB per CTA; more where the other operand is streamed for this one row of tiles), but no less
+  // than an epilogue
   double clocks(int n_cols, int splits) const {
-    const double block = n_cols == 256 ? 520 : n_cols == 128 ? 385 : 320;
-    const double products = static_cast<double>(tiles_of(k_blocks(), splits)) * block, epilogue = 1000 + 12.0 * n_cols;
+    const double block = n_cols == 256 ? (m_tiles() == 1 ? 680 : 520) : n_cols == 128 ? 385 : 320;
+    const double products = static_cast<double>(tiles_of(k_blocks(), splits)) * block, epilogue = 700 + 11.0 * n_cols;
     return (products > epilogue ? products : epilogue) + 300;
   }
 };
@@ -178,7 +179,7 @@ Deal deal_gradients(const Shape* dh, const Shape* dw, int pairs, int fixed_split
       if (left > others && d.rest) long_way += static_cast<double>(tiles_of(left - others, pairs)) * cw;
       double time = d.rounds * ch + (long_way > short_way ? long_way : short_way);
       // parts are joined by a launch of its own: its start, and each part written and read once at about 2500 bytes per clock
-      if (s > 1) time += 5000 + static_cast<double>(dh->m) * static_cast<double>(dh->n) * 8 * static_cast<double>(s) / 2500;
+      if (s > 1) time += 15000 + static_cast<double>(dh->m) * static_cast<double>(dh->n) * 8 * static_cast<double>(s) / 2500;
       if (least < 0 || time < least) least = time, best = d;
     }
   }
@@ -208,7 +209,7 @@ bool make_problem(iwp_tc::Problem* q, const Matrix& A, bool a_kc, const Matrix& 
 template <class Epi, int N>
 int pairs_of() {
   static std::atomic<int> cached[MAX_DEVICES] = {};
-  return resident_pairs(iwp_tc::k_product<N, Epi>, cached);
+  return resident_pairs(iwp_tc::k_product<N, Epi>, iwp_tc::smem_bytes(Epi::AREAS), cached);
 }
 
 template <class Epi, int N>
@@ -219,9 +220,10 @@ int launch_product(iwp_tc::Problems<N>& w, const typename Epi::Args& args, cudaS
   if (total > MAX_SIZE) return IWP_ERR_INVALID;
   const int tile_n = w.p[N - 1].n_tiles ? w.p[N - 1].tile_n : w.p[0].tile_n;  // the same for both
   w.b_bytes = static_cast<int>(up_to(tile_n / iwp_tc::CG, 64)) * iwp_tc::BLOCK_K * 2;
-  w.stages = iwp_tc::STAGE_SPACE / (iwp_tc::A_BYTES + w.b_bytes);
+  w.stages = iwp_tc::ring_bytes(Epi::AREAS) / (iwp_tc::A_BYTES + w.b_bytes);
   if (w.stages > iwp_tc::MAX_STAGES) w.stages = iwp_tc::MAX_STAGES;
-  LOSS_CUDA(launch(iwp_tc::k_product<N, Epi>, iwp_tc::CG * (total < pairs ? total : pairs), iwp_tc::THREADS, iwp_tc::SMEM, iwp_tc::CG, st, w, args));
+  LOSS_CUDA(launch(iwp_tc::k_product<N, Epi>, iwp_tc::CG * (total < pairs ? total : pairs), iwp_tc::THREADS, iwp_tc::smem_bytes(Epi::AREAS),
+                   iwp_tc::CG, st, w, args));
   return IWP_OK;
 }
 
@@ -464,6 +466,10 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
   oa.f.factor = a->scale * tau / up;
   oa.f.mean = a->mean;
   oa.f.by_rows = a->dloss_rows != nullptr;
+  auto copy_map = [](H::Out::Matrix& o) {
+    o.by_copy = o.type != IWP_F32 && o.wide && !o.add;
+    return !o.by_copy || make_map(&o.map, o.out, o.rows, o.cols, o.ld, 32, o.type);
+  };
   int splits = 1;
   for (int64_t done = 0; done < p.pieces; done++) {
     const int64_t i = p.pieces - 1 - done;  // the kept piece first
@@ -514,8 +520,10 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
         o.type = a->dhidden_type;
         o.wide = aligned(o.out, 16) && o.ld * size % 16 == 0;
         o.add = a->accumulate;
+        if (!copy_map(o)) return IWP_ERR_CUDA;
       } else {
         o.out = ws + p.join;
+        o.by_copy = 0;
         o.ld = D;
         o.split_stride = T * D;
         o.type = IWP_F32;
@@ -535,6 +543,7 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
       o.type = a->dweight_type;
       o.wide = aligned(o.out, 16) && o.ld * size % 16 == 0;
       o.add = a->accumulate;
+      if (!copy_map(o)) return IWP_ERR_CUDA;
       if (!make_problem(&work.p[1], pm, false, h, false, a->dtype, tile_n, 1)) return IWP_ERR_CUDA;
     }
     if (int e = launch_product<H::Out, 2>(work, oa, st)) return e;

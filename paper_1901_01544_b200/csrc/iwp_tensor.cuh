@@ -39,9 +39,12 @@ constexpr uint32_t WAIT_HINT_NS = 20000;
 constexpr int CG = 2;                               // CTAs per tile
 constexpr int A_BYTES = TILE_M * BLOCK_K * 2;
 constexpr int MAX_STAGES = 9;
-constexpr int STAGE_SPACE = 6 * (A_BYTES + TILE_N / CG * BLOCK_K * 2);  // 6 stages of the widest tiles, more of narrower ones
-constexpr int SMEM = 1024 + STAGE_SPACE + EPI_WARPS * STAGING_BYTES + 256;
-static_assert(SMEM <= 227 * 1024, "shared memory of a CTA");
+constexpr int WIDE_STAGE = A_BYTES + TILE_N / CG * BLOCK_K * 2;
+// Shared memory: a ring of load stages (6 of the widest tiles, 5 beside an epilogue with two staging areas per warp; more
+// of narrower tiles), the staging areas, barriers.
+__host__ __device__ constexpr int ring_bytes(int areas) { return (areas == 2 ? 5 : 6) * WIDE_STAGE; }
+__host__ __device__ constexpr int smem_bytes(int areas) { return 1024 + ring_bytes(areas) + areas * EPI_WARPS * STAGING_BYTES + 256; }
+static_assert(smem_bytes(1) <= 227 * 1024 && smem_bytes(2) <= 227 * 1024, "shared memory of a CTA");
 
 // The 16-byte word `word` (0..7) of staging row `row`: rotated by the row, so that neither lanes that write their own
 // rows nor lanes that read neighbouring words of a row meet in a bank.
@@ -275,7 +278,7 @@ __device__ __forceinline__ bool tile_at(const Problems<N>& w, int pair, int pair
   return true;
 }
 
-// Epi (device class): `Args`; begin(args, where), before the tile is there; tile(args, where, begun, accumulator), in which an epilogue warp disposes of its 32 rows and
+// Epi (device class): `Args`; AREAS, the staging areas per warp; begin(args, where), before the tile is there; tile(args, where, begun, accumulator), in which an epilogue warp disposes of its 32 rows and
 // half of the tile's columns.  SUMS: the tensor memory is emptied into registers every `seg` blocks of K and added up
 // there (the accumulator is then an array); otherwise it is an address in tensor memory.
 struct Where {
@@ -283,7 +286,8 @@ struct Where {
   int col0;     // first of the warp's columns
   int width;    // number of them: half a tile
   int lane, p, split;
-  char* staging;
+  char* staging;  // Epi::AREAS areas of STAGING_BYTES
+  int area;       // the one to use next, for epilogues that take turns
 };
 
 template <int N, class Epi>
@@ -293,8 +297,8 @@ __global__ void __launch_bounds__(THREADS, 1)
   const uint32_t raw = smem_u32(smem_raw);
   char* const smem = smem_raw + (((raw + 1023) & ~1023u) - raw);  // the same offset in both CTAs of a pair
   const uint32_t base = smem_u32(smem);
-  char* const staging = smem + STAGE_SPACE;
-  char* const ctl = staging + EPI_WARPS * STAGING_BYTES;
+  char* const staging = smem + ring_bytes(Epi::AREAS);
+  char* const ctl = staging + Epi::AREAS * EPI_WARPS * STAGING_BYTES;
   const uint32_t bars = smem_u32(ctl);
   const uint32_t full = bars, empty = bars + 8 * MAX_STAGES, acc_full = empty + 8 * MAX_STAGES, acc_empty = acc_full + 16;
   volatile int* const dead = reinterpret_cast<volatile int*>(ctl + 8 * (2 * MAX_STAGES + 4));
@@ -418,6 +422,9 @@ __global__ void __launch_bounds__(THREADS, 1)
     uint32_t acc_phase = 0;
     const uint32_t empty_of_pair = map_to(acc_empty, 0);
     bool ok = true;
+    Where at;
+    at.area = 0;
+    at.staging = staging + e * Epi::AREAS * STAGING_BYTES;
     // the accumulator's turn is over: the products may write it again
     auto release = [&] {
       fence_before();
@@ -430,14 +437,12 @@ __global__ void __launch_bounds__(THREADS, 1)
     };
     for (int i = 0; ok && tile_at(w, pair, pairs, i, t); i++) {
       const Problem& q = w.p[t.p];
-      Where at;
       at.width = q.tile_n / 2;
       at.row0 = (CG * t.m + static_cast<int>(rank)) * TILE_M + (e % 4) * 32;
       at.col0 = t.n * q.tile_n + (e / 4) * at.width;
       at.lane = lane;
       at.p = t.p;
       at.split = t.split;
-      at.staging = staging + e * STAGING_BYTES;
       const uint32_t mine = tmem + (e / 4) * at.width + (static_cast<uint32_t>(e % 4) << 21);
       auto begun = Epi::begin(args, at);  // what the rows need from memory, fetched while the products run
       if constexpr (Epi::SUMS) {
@@ -469,6 +474,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
     }
   }
+  if (warp >= 4 && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");  // the epilogue's last copies
   __syncwarp();
   __syncthreads();
   if (*dead) __nanosleep(1000000);  // copies in flight land in microseconds
@@ -506,6 +512,25 @@ __device__ __forceinline__ void store_as(void* p, int64_t i, float v, int type) 
     static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
   else
     static_cast<__half*>(p)[i] = __float2half_rn(v);
+}
+
+// The warp's staging rows (32 rows of 64 16-bit columns, swizzled as `map` expects) to a matrix, by one asynchronous copy;
+// rows and columns outside the matrix are dropped.  staging_free() waits until all but the last LEFT copies have read their
+// rows.
+template <int LEFT>
+__device__ __forceinline__ void staging_free(int lane) {
+  if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LEFT) : "memory");
+  __syncwarp();
+}
+__device__ __forceinline__ void store_staged(const CUtensorMap* map, char* staging, int row0, int col0, int lane) {
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  __syncwarp();
+  if (lane == 0) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(col0), "r"(row0),
+                 "r"(smem_u32(staging))
+                 : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+  }
 }
 
 // Writes a chunk of 32 columns (v: this lane's row) of the warp's 32 rows to a row-major matrix, through the warp's
