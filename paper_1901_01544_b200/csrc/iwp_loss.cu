@@ -371,7 +371,7 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
     ra.T = T;
     ra.mean = a->mean;
     ra.tau = tau;
-    ra.lanes = T < 4 * sms ? H::ROW_THREADS : 32;  // a block per row while that fills the device, a warp after that
+    ra.lanes = T <= 8 * sms ? H::ROW_THREADS : 32;  // a block per row while all blocks run at once, a warp after that
     const int64_t row_blocks = ra.lanes == 32 ? tiles_of(T, H::ROW_THREADS / 32) : T;
     if (p.few) {
       H::Few fa{};

@@ -236,14 +236,14 @@ class HeadLoss(_Plan):
                     raise ValueError("accumulate needs the gradients to add to")
             if "hidden" in want:
                 if dhidden is None:
-                    dhidden, a.dhidden_ld, a.dhidden_type = t.empty((T, D), dtype=self.dtype, device=dev), D, self._code
+                    dhidden, a.dhidden_ld, a.dhidden_type = t.empty(T, D, dtype=self.dtype, device=dev), D, self._code
                 else:
                     a.dhidden_ld, a.dhidden_type = _rows_of(dhidden, "dhidden", (T, D), self._out_types, dev), self._codes[dhidden.dtype]
                 a.dhidden = dhidden.data_ptr() or 256  # an empty tensor has no address
                 r.dhidden = dhidden
             if "weight" in want:
                 if dweight is None:
-                    dweight, a.dweight_ld, a.dweight_type = t.empty((V, D), dtype=self.dtype, device=dev), D, self._code
+                    dweight, a.dweight_ld, a.dweight_type = t.empty(V, D, dtype=self.dtype, device=dev), D, self._code
                 else:
                     a.dweight_ld, a.dweight_type = _rows_of(dweight, "dweight", (V, D), self._out_types, dev), self._codes[dweight.dtype]
                 a.dweight = dweight.data_ptr()
@@ -315,39 +315,45 @@ class ExpertBalance(_Plan):
     def __init__(self, tokens: int, experts: int):
         super().__init__()
         self.experts = int(experts)
-        a = BalanceArgs(tokens=int(tokens), experts=self.experts, top_k=1, type=IWP_F32)
+        self._masks = (self._torch.bool, self._torch.uint8)
+        self._args = a = BalanceArgs(tokens=int(tokens), experts=self.experts, top_k=1, type=IWP_F32)  # of every call
+        self._args_at = C.addressof(a)
         self._grow(lib().iwp_balance_workspace(C.byref(a)))
+        a.workspace, a.workspace_bytes = self._ws_at, self._ws_bytes
 
     def _run(self, logits, ids, mask, coef, dloss, scale, grad, dlogits) -> BalanceResult:
-        t, dev, E = self._torch, self.device, self.experts
+        t, dev, E, a = self._torch, self.device, self.experts, self._args
         if logits.dim() != 2 or ids.dim() != 2:
             raise ValueError("logits and ids are matrices")
         T, k = logits.shape[0], ids.shape[1]
-        a = BalanceArgs()
-        a.tokens, a.experts, a.top_k, a.coef, a.scale = T, E, k, coef, scale
-        a.logits_ld = _rows_of(logits, "logits", (T, E), self._floats, dev)
+        a.tokens, a.top_k, a.coef, a.scale = T, k, coef, scale
+        a.logits_ld = ld = _rows_of(logits, "logits", (T, E), self._floats, dev)
         a.ids_ld = _rows_of(ids, "ids", (T, k), self._ids, dev)
         a.logits, a.ids, a.type, a.ids_bytes = logits.data_ptr(), ids.data_ptr(), self._codes[logits.dtype], (8 if ids.dtype is self._ids[0] else 4)
-        if mask is not None:
-            _vector(mask, "mask", T, (t.bool, t.uint8), dev)
+        if mask is None:
+            a.mask = None
+        else:
+            _vector(mask, "mask", T, self._masks, dev)
             a.mask = mask.data_ptr()
         out = t.empty(E + 1, dtype=t.float32, device=dev)
         counts = t.empty(E, dtype=t.int32, device=dev)
         at = out.data_ptr()
-        a.mean_prob, a.loss, a.counts = at, at + 4 * E, counts.data_ptr()
+        a.mean_prob, a.loss, a.counts, a.dloss = at, at + 4 * E, counts.data_ptr(), None
         if grad:
             if dloss is not None:
-                _vector(dloss, "dloss", 1, (t.float32,), dev)
+                _vector(dloss, "dloss", 1, self._floats[:1], dev)
                 a.dloss = dloss.data_ptr()
             if dlogits is None:
-                dlogits, a.dlogits_ld = t.empty((T, E), dtype=logits.dtype, device=dev), E
+                dlogits = t.empty_like(logits) if ld == E and T > 1 else t.empty(T, E, dtype=logits.dtype, device=dev)
+                a.dlogits_ld = E
             else:
                 a.dlogits_ld = _rows_of(dlogits, "dlogits", (T, E), (logits.dtype,), dev)
             a.dlogits = dlogits.data_ptr()
+        else:
+            a.dlogits = None
         if T == 0:
             a.logits, a.ids = a.logits or 256, a.ids or 256
-        a.workspace, a.workspace_bytes = self._ws_at, self._ws_bytes
-        status = self._lib.iwp_balance_loss(C.byref(a), self._raw_stream(dev.index))
+        status = self._lib.iwp_balance_loss(self._args_at, self._raw_stream(dev.index))
         if status:
             raise IwpError(status, "iwp_balance_loss")
         return BalanceResult(out, counts, dlogits)
