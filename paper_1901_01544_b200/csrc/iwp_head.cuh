@@ -61,9 +61,8 @@ struct Targets {
     return y != ignore && y >= 0 && y < V ? static_cast<int>(y) : NO_COLUMN;
   }
   __device__ __forceinline__ float q_at(int64_t row, int i) const { return hard ? 1.f : q[row * k + i]; }
-  // the first entry at or after col0
+  // the first entry at or after col0, in a list
   __device__ __forceinline__ int first(int64_t row, int col0) const {
-    if (hard) return column_at(row, 0) >= col0 ? 0 : 1;
     int lo = 0, hi = k;
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
@@ -94,6 +93,12 @@ struct Upcoming {
     next = after[0] = after[1] = after[2] = NO_COLUMN;
   }
   __device__ __forceinline__ void from(const Targets& en, int64_t row, int col0) {
+    if (en.hard) {
+      none(en);
+      const int c = en.column_at(row, 0);
+      if (c >= col0 && c != NO_COLUMN) pos = 0, next = c;
+      return;
+    }
     pos = en.first(row, col0);
     next = pos < en.k ? en.column_at(row, pos) : NO_COLUMN;
 #pragma unroll

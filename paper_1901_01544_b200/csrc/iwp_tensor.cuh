@@ -435,21 +435,36 @@ __global__ void __launch_bounds__(THREADS, 1)
         acc_phase ^= 1;
       }
     };
-    for (int i = 0; ok && tile_at(w, pair, pairs, i, t); i++) {
+    // where the warp's part of a tile lies, and what its rows need from memory: fetched one tile ahead
+    auto locate = [&](const Tile& t, Where& at) {
       const Problem& q = w.p[t.p];
       at.width = q.tile_n / 2;
       at.row0 = (CG * t.m + static_cast<int>(rank)) * TILE_M + (e % 4) * 32;
       at.col0 = t.n * q.tile_n + (e / 4) * at.width;
-      at.lane = lane;
       at.p = t.p;
       at.split = t.split;
+    };
+    at.lane = lane;
+    bool more = tile_at(w, pair, pairs, 0, t);
+    Where coming = at;
+    locate(t, coming);
+    auto begun = Epi::begin(args, coming);
+    for (int i = 1; ok && more; i++) {
+      const int k0 = t.k0, k1 = t.k1, area = at.area;
+      at = coming;
+      at.area = area;
+      auto now = begun;
       const uint32_t mine = tmem + (e / 4) * at.width + (static_cast<uint32_t>(e % 4) << 21);
-      auto begun = Epi::begin(args, at);  // what the rows need from memory, fetched while the products run
+      more = tile_at(w, pair, pairs, i, t);
+      if (more) {
+        locate(t, coming);
+        begun = Epi::begin(args, coming);
+      }
       if constexpr (Epi::SUMS) {
         f2 acc[TILE_N / 4];
 #pragma unroll
         for (int j = 0; j < TILE_N / 4; j++) acc[j] = pack(0.f, 0.f);
-        for (int k0 = t.k0; k0 < t.k1; k0 += w.seg) {
+        for (int k = k0; k < k1; k += w.seg) {
           ok = __all_sync(0xFFFFFFFFu, mbar_wait(acc_full + 8 * b, acc_phase, dead, w.status));
           if (!ok) break;
           fence_after();
@@ -464,12 +479,12 @@ __global__ void __launch_bounds__(THREADS, 1)
           }
           release();
         }
-        if (ok) Epi::tile(args, at, begun, acc);
+        if (ok) Epi::tile(args, at, now, acc);
       } else {
         ok = __all_sync(0xFFFFFFFFu, mbar_wait(acc_full + 8 * b, acc_phase, dead, w.status));
         if (!ok) break;
         fence_after();
-        Epi::tile(args, at, begun, mine + b * TILE_N);
+        Epi::tile(args, at, now, mine + b * TILE_N);
         release();
       }
     }
