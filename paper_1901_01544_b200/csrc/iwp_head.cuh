@@ -133,6 +133,20 @@ __device__ __forceinline__ float log_value(uint32_t code) {
   return code == 0xFFFFu ? CUDART_INF_F : __uint_as_float(((code << 8) + 0x41000000u) | (code >> 15 << 6));
 }
 
+// 64 columns of 16 bits of the lane's row (two halves of 16 words) into the warp's next staging area, and from there to the
+// matrix of `map` by an asynchronous copy.
+__device__ __forceinline__ void copy_out(const CUtensorMap* map, Where& w, const uint32_t (&lo)[16], const uint32_t (&hi)[16], int col0) {
+  iwp_tc::staging_free<1>(w.lane);
+  char* const area = w.staging + w.area * iwp_tc::STAGING_BYTES;
+  w.area ^= 1;
+#pragma unroll
+  for (int j = 0; j < 4; j++) {
+    *reinterpret_cast<uint4*>(iwp_tc::staged(area, w.lane, j)) = make_uint4(lo[4 * j], lo[4 * j + 1], lo[4 * j + 2], lo[4 * j + 3]);
+    *reinterpret_cast<uint4*>(iwp_tc::staged(area, w.lane, j + 4)) = make_uint4(hi[4 * j], hi[4 * j + 1], hi[4 * j + 2], hi[4 * j + 3]);
+  }
+  iwp_tc::store_staged(map, area, w.row0, col0, w.lane);
+}
+
 // Column i of the lane's staged row.
 __device__ __forceinline__ float* staged_at(const Where& w, int i) {
   return reinterpret_cast<float*>(iwp_tc::staged(w.staging, w.lane, i >> 2)) + (i & 3);
@@ -143,7 +157,7 @@ __device__ __forceinline__ float* staged_at(const Where& w, int i) {
 template <int CODES>
 struct Logits {
   static constexpr bool SUMS = true;
-  static constexpr int AREAS = 1;
+  static constexpr int AREAS = CODES == NO_CODES ? 1 : 2;
   struct Args {
     Targets en;
     int64_t T;
@@ -155,6 +169,7 @@ struct Logits {
     uint16_t* codes;  // [T][ld] of columns v0 .. v0 + width
     int64_t ld;
     int v0, width;
+    CUtensorMap map;  // of the codes, in boxes of 32 rows and 64 columns
   };
   static __device__ __forceinline__ Upcoming begin(const Args& a, const Where& w) {
     Upcoming u;
@@ -162,7 +177,7 @@ struct Logits {
     if (w.row0 + w.lane < a.T) u.from(a.en, w.row0 + w.lane, w.col0);
     return u;
   }
-  static __device__ __forceinline__ void tile(const Args& a, const Where& w, Upcoming& up, f2 (&acc)[iwp_tc::TILE_N / 4]) {
+  static __device__ __forceinline__ void tile(const Args& a, Where& w, Upcoming& up, f2 (&acc)[iwp_tc::TILE_N / 4]) {
     constexpr int CHUNKS = iwp_tc::TILE_N / 64;
     const int row = w.row0 + w.lane;
     const bool live = row < a.T;
@@ -172,6 +187,7 @@ struct Logits {
       const int c0 = w.col0 + 32 * c;
       if (32 * c >= w.width) break;
       if (__any_sync(0xFFFFFFFFu, up.next < c0 + 32)) {  // some row has a target here
+        iwp_tc::staging_free<0>(w.lane);
 #pragma unroll
         for (int j = 0; j < 32; j += 4) {
           const float2 x = unpack(acc[16 * c + j / 2]), y = unpack(acc[16 * c + j / 2 + 1]);
@@ -202,23 +218,30 @@ struct Logits {
     const f2 scale = pack(a.c, a.c), less = pack(15.f - ref, 15.f - ref);
     const f2 down = pack(-a.c, -a.c), from = pack(8.f + HALF_STEP + ref, 8.f + HALF_STEP + ref);
     f2 sum = pack(0.f, 0.f);
+    uint32_t packed[2][16];
 #pragma unroll
     for (int c = 0; c < CHUNKS; c++) {
       if (32 * c >= w.width) break;
-      uint32_t packed[16];
 #pragma unroll
       for (int j = 0; j < 16; j++) {
         const f2 z = acc[16 * c + j];
         const float2 x = unpack(fma2(z, scale, less));
         const float2 e = make_float2(ex2(x.x), ex2(x.y));
         sum = add2(sum, pack(e.x, e.y));
-        if constexpr (CODES == HALF_CODES) packed[j] = iwp_tc::pack2(e.x, e.y, IWP_F16);
+        if constexpr (CODES == HALF_CODES) packed[c % 2][j] = iwp_tc::pack2(e.x, e.y, IWP_F16);
         if constexpr (CODES == LOG_CODES) {
           const float2 y = unpack(fma2(z, down, from));
-          packed[j] = log_codes(y.x, y.y);
+          packed[c % 2][j] = log_codes(y.x, y.y);
         }
       }
-      if (keep) iwp_tc::store_packed(packed, w.staging, a.codes, a.ld, w.row0, static_cast<int>(a.T), w.col0 + 32 * c - a.v0, w.lane);
+      if (keep && w.row0 < a.T) {
+        if (w.width == 32) {
+          iwp_tc::staging_free<0>(w.lane);
+          iwp_tc::store_packed(packed[0], w.staging, a.codes, a.ld, w.row0, static_cast<int>(a.T), w.col0 - a.v0, w.lane);
+        } else if (c % 2 == 1) {
+          copy_out(&a.map, w, packed[0], packed[1], w.col0 + 32 * (c - 1) - a.v0);
+        }
+      }
     }
     const float2 s = unpack(sum);
     if (live) a.part[static_cast<int64_t>(row) * a.parts + w.col0 / w.width] = make_float2(m, (s.x + s.y) * SUM_SCALE);
@@ -327,23 +350,16 @@ struct Out {
     if (a.by_copy && w.width >= 64) {
 #pragma unroll 1
       for (int c0 = w.col0; c0 < min(w.col0 + w.width, a.cols); c0 += 64) {
-        uint32_t packed[32];
+        uint32_t packed[2][16];
 #pragma unroll
         for (int half = 0; half < 2; half++) {
           float v[32];
           iwp_tc::tmem_load32(tmem + (c0 - w.col0) + 32 * half, v);
 #pragma unroll
-          for (int j = 0; j < 16; j++) packed[16 * half + j] = iwp_tc::pack2(v[2 * j] * f, v[2 * j + 1] * f, a.type);
+          for (int j = 0; j < 16; j++) packed[half][j] = iwp_tc::pack2(v[2 * j] * f, v[2 * j + 1] * f, a.type);
         }
-        if (w.row0 >= a.rows) continue;  // (the accumulator is read whole all the same: a warp's loads are collective)
-        iwp_tc::staging_free<1>(w.lane);
-        char* const area = w.staging + w.area * iwp_tc::STAGING_BYTES;
-        w.area ^= 1;
-#pragma unroll
-        for (int j = 0; j < 8; j++)
-          *reinterpret_cast<uint4*>(iwp_tc::staged(area, w.lane, j)) =
-              make_uint4(packed[4 * j], packed[4 * j + 1], packed[4 * j + 2], packed[4 * j + 3]);
-        iwp_tc::store_staged(&a.map, area, w.row0, c0, w.lane);
+        // (the accumulator is read whole all the same: a warp's loads are collective)
+        if (w.row0 < a.rows) copy_out(&a.map, w, packed[0], packed[1], c0);
       }
       return;
     }

@@ -310,7 +310,7 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
   char* const ws = static_cast<char*>(a->workspace);
   auto* hdr = reinterpret_cast<H::Header*>(ws);
   const int pairs = pairs_of<H::Logits<H::NO_CODES>, 1>();
-  if (pairs < 1 || pairs_of<H::Probs, 1>() < 1 || pairs_of<H::Out, 2>() < 1) {
+  if (pairs < 1 || pairs_of<H::Logits<H::HALF_CODES>, 1>() < 1 || pairs_of<H::Logits<H::LOG_CODES>, 1>() < 1 || pairs_of<H::Probs, 1>() < 1 || pairs_of<H::Out, 2>() < 1) {
     cudaGetLastError();
     return IWP_ERR_CUDA;
   }
@@ -434,6 +434,7 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
       la.ld = p.piece;
       la.v0 = static_cast<int>(v0);
       la.width = static_cast<int>(p.piece);
+      if (kept >= 0 && !make_map(&la.map, probs, T, p.piece, p.piece, 32, a->dtype)) return static_cast<int>(IWP_ERR_CUDA);
       return launch_product<Epi, 1>(work, la, st);
     };
     const int failed = kept < 0 ? logits(H::Logits<H::NO_CODES>{}) : a->dtype == IWP_F16 ? logits(H::Logits<H::LOG_CODES>{}) : logits(H::Logits<H::HALF_CODES>{});
