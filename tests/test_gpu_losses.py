@@ -577,3 +577,83 @@ def test_example_trains():
     first, last = history[0], history[-1]
     assert last[0] < 0.8 * first[0] and last[1] < 0.8 * first[1]
     assert sum(counts) == 3 * 256 * 2
+
+
+def test_offsets_beyond_32_bits():
+    """One piece of 20000 x 131072 codes: element offsets beyond 2^31.  Rows and columns at the far end are compared."""
+    T, V, D = 20000, 131072, 64
+    h, w, y, _ = operands(T, V, D, BF, 400)
+    plan = losses.HeadLoss(T, V, D, BF, piece_bytes=6 << 30)
+    r = plan.cross_entropy_grad(h, w, y, reduction="sum")
+    assert plan.status() == 0
+    far = slice(T - 40, T)
+    one = torch.ones(40, 1, dtype=torch.float64, device=DEV)
+    ref = head_reference(h[far], w, y[far, None], one, 1.0, False)
+    close(r.rows[far], ref["rows"], ref["row_err"], "rows")
+    close_grad(r.dhidden[far], ref["dH"], ref["h_err"], "dhidden")
+    lse = torch.full((T,), -math.inf, dtype=torch.float64, device=DEV)
+    for a in range(0, V, 16384):
+        lse = torch.logaddexp(lse, torch.logsumexp(h.double() @ w[a : a + 16384].double().T, 1))
+    cols = slice(V - 33, V)
+    H, W = h.double(), w[cols].double()
+    p = torch.exp(H @ W.T - lse[:, None])
+    dz = p - (y[:, None] == torch.arange(V - 33, V, device=DEV)).double()
+    dz_err = (D / 16 + 2) * 2.0**-22 * (H.abs().sum(1) * w.abs().max().double()) + 2.0**-20 * (1 + lse.abs())
+    f_err = 2 * U[BF] * dz.abs() + (2 * dz_err[:, None] + U[BF]) * p + 2.0**-23
+    w_err = f_err.T @ H.abs() + (T / 16 + 8) * 2.0**-22 * (dz.abs().T @ H.abs())
+    close_grad(r.dweight[cols], dz.T @ H, w_err, "dweight")
+
+
+def test_balance_offsets_beyond_32_bits():
+    T, E, k = 1 << 23, 260, 2
+    g = gen(401)
+    x = torch.randn(4096, E, generator=g, device=DEV).to(BF).repeat(T // 4096, 1)
+    ids = torch.randint(0, E, (T, k), generator=g, device=DEV, dtype=torch.int32)
+    plan = losses.ExpertBalance(T, E)
+    r = plan.grad(x, ids, coef=1.0, scale=float(T))
+    counts = torch.bincount(ids.flatten().long(), minlength=E)
+    assert torch.equal(r.counts.long(), counts)
+    far = x[-4096:].double()
+    p = torch.softmax(far, 1)
+    f = counts.double() / (T * k)
+    want = E * p * (f - (p * f).sum(1, keepdim=True))
+    # p is off by 2^-19 * 40 relative at most (see check_balance), on both sides of the difference
+    tol = U[BF] * 1.01 * want.abs() + 2 * 2.0**-19 * 40 * E * p * f.max() + TINY[BF]
+    assert ((r.dlogits[-4096:].double() - want).abs() <= tol).all()
+    # the same 4096 rows over and over: the mean of p is theirs, and 2^23 / (148 * 32) rows are added up per lane
+    mean = p.mean(0)
+    assert ((r.mean_prob.double() - mean).abs() <= (2.0**-19 * 40 + T * 2.0**-24 / 64) * mean).all()
+
+
+def test_captured_in_a_graph():
+    T, V, D, E = 200, 1500, 64, 16
+    h, w, y, g = operands(T, V, D, BF, 500)
+    x = torch.randn(T, E, generator=g, device=DEV)
+    ids = torch.topk(x, 2, dim=1).indices
+    plan, router = losses.HeadLoss(T, V, D, BF), losses.ExpertBalance(T, E)
+    plan.cross_entropy_grad(h, w, y), router.grad(x, ids)  # workspaces and look-ups
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        r, b = plan.cross_entropy_grad(h, w, y), router.grad(x, ids)
+    for seed in (501, 502):
+        h2, w2, y2, g = operands(T, V, D, BF, seed)
+        h.copy_(h2), w.copy_(w2), y.copy_(y2)
+        x.copy_(torch.randn(T, E, generator=g, device=DEV))
+        graph.replay()
+        want, wb = plan.cross_entropy_grad(h, w, y), router.grad(x, ids)
+        assert torch.equal(r.loss, want.loss) and torch.equal(r.dhidden, want.dhidden) and torch.equal(r.dweight, want.dweight)
+        assert torch.equal(b.dlogits, wb.dlogits) and torch.equal(b.loss, wb.loss)
+
+
+@pytest.mark.parametrize("T,V,D", [(130, 700, 72), (300, 6001, 200), (700, 70000, 136)])
+def test_strided_gradients_touch_nothing_beside_them(T, V, D):
+    """16-bit gradients in aligned strided rows leave by tile copies, which have to stop at the matrix's edges."""
+    h, w, y, _ = operands(T, V, D, BF, 600)
+    ref = head_reference(h, w, y[:, None], torch.ones(T, 1, dtype=torch.float64, device=DEV), 1.0, True)
+    dh, dw = torch.full((T + 40, D + 24), 7.0, dtype=BF, device=DEV), torch.full((V + 40, D + 24), 7.0, dtype=BF, device=DEV)
+    plan = losses.HeadLoss(T, V, D, BF)
+    r = plan.cross_entropy_grad(h, w, y, dhidden=dh[:T, 8 : 8 + D], dweight=dw[:V, 8 : 8 + D])
+    check_head(r, ref)
+    for buf, n in ((dh, T), (dw, V)):
+        assert (buf[n:] == 7).all() and (buf[:, :8] == 7).all() and (buf[:, 8 + D :] == 7).all()
