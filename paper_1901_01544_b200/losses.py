@@ -140,7 +140,8 @@ class _Plan:
         self._torch = torch
         self.device = torch.device("cuda", torch.cuda.current_device())
         self._lib = lib()
-        self._ws, self._ws_at, self._ws_bytes = None, None, 0
+        self._ws, self._ws_at, self._ws_bytes = None, None, 0  # made by the first call
+        self._planned = 0
         self._floats = tuple(self._codes)
         self._ids = (torch.int64, torch.int32)
         self._raw_stream = torch._C._cuda_getCurrentRawStream  # current_stream() without the object around it
@@ -148,9 +149,15 @@ class _Plan:
     def _stream(self) -> int:
         return self._raw_stream(self.device.index)
 
+    def _plan(self, need: int) -> None:
+        if need < 0:
+            raise IwpError(IWP_ERR_INVALID, "workspace size")
+        self._planned = need
+
     def _grow(self, need: int) -> None:
         if need < 0:
             raise IwpError(IWP_ERR_INVALID, "workspace size")
+        need = max(need, self._planned)
         if self._ws_bytes < need:
             old, self._ws = self._ws, self._torch.empty(need, dtype=self._torch.uint8, device=self.device)
             self._ws_at, self._ws_bytes = self._ws.data_ptr(), need
@@ -177,10 +184,10 @@ class _Plan:
 class HeadLoss(_Plan):
     """Output head [vocab, dim] with its loss; the logits are never kept.
 
-    tokens: the most rows a call will bring; top_k: the most teacher logits per row.  The workspace made here serves
-    forward passes of that size; the first gradient (or a call that needs more) makes a larger one.  piece_bytes: bound
-    on the probabilities held at a time while gradients are formed (0 = 1 GiB, or what the weights and their gradient
-    take where that is more)."""
+    tokens: the most rows a call will bring; top_k: the most teacher logits per row.  The first call makes a workspace
+    that serves forward passes of that size; the first gradient (or a call that needs more) makes a larger one.
+    piece_bytes: bound on the probabilities held at a time while gradients are formed (0 = 1 GiB, or what the weights and
+    their gradient take where that is more)."""
 
     def __init__(self, tokens: int, vocab: int, dim: int, dtype=None, top_k: int = 1, piece_bytes: int = 0):
         super().__init__()
@@ -194,7 +201,7 @@ class HeadLoss(_Plan):
         a.hidden_ld = a.weight_ld = (self.dim + 7) // 8 * 8
         if self.dim % 8:  # rows of contiguous operands do not start at multiples of 16 bytes: they will be copied
             a.hidden_ld = a.weight_ld = self.dim
-        self._grow(lib().iwp_head_workspace(C.byref(a)))
+        self._plan(lib().iwp_head_workspace(C.byref(a)))
 
     # one call of iwp_head_loss
     def _run(self, hidden, weight, a: HeadArgs, *, grad, ignore_index=0, reduction="mean", lse=None, dloss=None, scale=1.0, dhidden=None,
@@ -254,8 +261,10 @@ class HeadLoss(_Plan):
                 a.top_ids, a.top_logits = a.top_ids or 256, a.top_logits or 256
             else:
                 a.targets = a.targets or 256
-        a.workspace, a.workspace_bytes = self._ws_at, self._ws_bytes
         ref = C.byref(a)
+        if self._ws_at is None:
+            self._grow(self._lib.iwp_head_workspace(ref))
+        a.workspace, a.workspace_bytes = self._ws_at, self._ws_bytes
         status = self._lib.iwp_head_loss(ref, self._raw_stream(dev.index))
         if status == IWP_ERR_CAPACITY:  # more tokens, or rows that have to be copied, for the first time
             self._grow(self._lib.iwp_head_workspace(ref))
@@ -318,8 +327,7 @@ class ExpertBalance(_Plan):
         self._masks = (self._torch.bool, self._torch.uint8)
         self._args = a = BalanceArgs(tokens=int(tokens), experts=self.experts, top_k=1, type=IWP_F32)  # of every call
         self._args_at = C.addressof(a)
-        self._grow(lib().iwp_balance_workspace(C.byref(a)))
-        a.workspace, a.workspace_bytes = self._ws_at, self._ws_bytes
+        self._plan(lib().iwp_balance_workspace(C.byref(a)))
 
     def _run(self, logits, ids, mask, coef, dloss, scale, grad, dlogits) -> BalanceResult:
         t, dev, E, a = self._torch, self.device, self.experts, self._args
@@ -353,6 +361,9 @@ class ExpertBalance(_Plan):
             a.dlogits = None
         if T == 0:
             a.logits, a.ids = a.logits or 256, a.ids or 256
+        if self._ws_at is None:
+            self._grow(0)
+            a.workspace, a.workspace_bytes = self._ws_at, self._ws_bytes
         status = self._lib.iwp_balance_loss(self._args_at, self._raw_stream(dev.index))
         if status:
             raise IwpError(status, "iwp_balance_loss")
