@@ -433,8 +433,8 @@ __device__ __forceinline__ float warp_sum(float x) {
 __global__ void k_soft_targets(int* column, float* q_out, float* const_term, const void* ids, int64_t ids_ld, int ids_bytes,
                                const void* logits, int64_t logits_ld, int type, int K, float inv_tau, int64_t T, int64_t V) {
   extern __shared__ int sh[];
-  iwp_tc::launch_next();
   iwp_tc::wait_previous();
+  iwp_tc::launch_next();  // after the wait: the logits pass may load its operands beside this kernel
   const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t t = blockIdx.x * int64_t(warps) + warp;
   if (t >= T) return;

@@ -418,6 +418,7 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
     const int blocks = work.p[0].k_blocks;
     work.seg = static_cast<int>(tiles_of(blocks, tiles_of(blocks, 16)));
     work.status = &hdr->status;
+    work.early = !a->targets && !en.scale && !p.pack_hidden && !p.pack_weight;  // k_soft_targets comes right before
     const int parts = 2 * work.p[0].n_tiles;
     const int64_t v0 = kept >= 0 ? kept * p.piece : 0;
     auto logits = [&](auto epilogue) {
@@ -483,6 +484,7 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
       if (!make_problem(&work.p[0], h, true, wp, true, a->dtype, pick_tile_n(shape, pairs), 1)) return IWP_ERR_CUDA;
       work.seg = 1 << 30;
       work.status = &hdr->status;
+      work.early = 0;
       H::Probs::Args pa{};
       pa.en = en;
       pa.lse = a->lse;
@@ -502,6 +504,7 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
     work.p[1].m_tiles = work.p[1].n_tiles = work.p[1].splits = 0;
     work.seg = 1 << 30;
     work.status = &hdr->status;
+    work.early = 0;
     const Shape dh{T, D, width}, dw{width, D, T};
     const Deal deal = deal_gradients(a->dhidden ? &dh : nullptr, a->dweight ? &dw : nullptr, pairs, done == 0 ? 0 : splits);
     work.rounds = deal.rounds;

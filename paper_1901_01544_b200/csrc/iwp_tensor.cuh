@@ -215,7 +215,9 @@ struct Problems {
   Problem p[N];
   int rounds, rest, fill;
   int stages, b_bytes;  // of the ring in shared memory, and B's share of a stage
-  int seg;  // k blocks per accumulator tile (epilogues that add up segments), or a large number
+  int seg;    // k blocks per accumulator tile (epilogues that add up segments), or a large number
+  int early;  // 1: the operands were complete before the kernel in front of this one let it start, so that only the
+              // epilogue has to wait for that kernel's end
   int* status;
 };
 
@@ -334,7 +336,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   cluster_sync();
   fence_after();
   const uint32_t tmem = *tmem_slot;
-  wait_previous();
+  if (!w.early || warp >= 4) wait_previous();
 
   const int pair = blockIdx.x / CG, pairs = gridDim.x / CG;
   const int stages = w.stages, stage_bytes = A_BYTES + w.b_bytes;
