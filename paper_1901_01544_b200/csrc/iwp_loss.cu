@@ -310,7 +310,8 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
   char* const ws = static_cast<char*>(a->workspace);
   auto* hdr = reinterpret_cast<H::Header*>(ws);
   const int pairs = pairs_of<H::Logits<H::NO_CODES>, 1>();
-  if (pairs < 1 || pairs_of<H::Logits<H::HALF_CODES>, 1>() < 1 || pairs_of<H::Logits<H::LOG_CODES>, 1>() < 1 || pairs_of<H::Probs, 1>() < 1 || pairs_of<H::Out, 2>() < 1) {
+  const int out_pairs = pairs_of<H::Out, 2>();  // the deal of the gradients counts on this grid
+  if (pairs < 1 || out_pairs < 1 || pairs_of<H::Logits<H::HALF_CODES>, 1>() < 1 || pairs_of<H::Logits<H::LOG_CODES>, 1>() < 1 || pairs_of<H::Probs, 1>() < 1) {
     cudaGetLastError();
     return IWP_ERR_CUDA;
   }
@@ -506,7 +507,7 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
     work.status = &hdr->status;
     work.early = 0;
     const Shape dh{T, D, width}, dw{width, D, T};
-    const Deal deal = deal_gradients(a->dhidden ? &dh : nullptr, a->dweight ? &dw : nullptr, pairs, done == 0 ? 0 : splits);
+    const Deal deal = deal_gradients(a->dhidden ? &dh : nullptr, a->dweight ? &dw : nullptr, out_pairs, done == 0 ? 0 : splits);
     work.rounds = deal.rounds;
     work.rest = deal.rest;
     work.fill = deal.fill;

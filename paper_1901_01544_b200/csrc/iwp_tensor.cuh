@@ -38,7 +38,7 @@ constexpr uint32_t WAIT_HINT_NS = 20000;
 
 constexpr int CG = 2;                               // CTAs per tile
 constexpr int A_BYTES = TILE_M * BLOCK_K * 2;
-constexpr int MAX_STAGES = 9;
+constexpr int MAX_STAGES = 8;
 constexpr int WIDE_STAGE = A_BYTES + TILE_N / CG * BLOCK_K * 2;
 // Shared memory: a ring of load stages (6 of the widest tiles, 5 beside an epilogue with two staging areas per warp; more
 // of narrower tiles), the staging areas, barriers.
@@ -280,9 +280,10 @@ __device__ __forceinline__ bool tile_at(const Problems<N>& w, int pair, int pair
   return true;
 }
 
-// Epi (device class): `Args`; AREAS, the staging areas per warp; begin(args, where), before the tile is there; tile(args, where, begun, accumulator), in which an epilogue warp disposes of its 32 rows and
-// half of the tile's columns.  SUMS: the tensor memory is emptied into registers every `seg` blocks of K and added up
-// there (the accumulator is then an array); otherwise it is an address in tensor memory.
+// Epi (device class): `Args`; AREAS, the staging areas per warp; begin(args, where), before the tile is there; tile(args,
+// where, begun, accumulator), in which an epilogue warp disposes of its 32 rows and half of the tile's columns.  SUMS: the
+// tensor memory is emptied into registers every `seg` blocks of K and added up there (the accumulator is then an array);
+// otherwise it is an address in tensor memory.
 struct Where {
   int row0;     // first of the warp's 32 rows; the lane's row is row0 + lane
   int col0;     // first of the warp's columns
