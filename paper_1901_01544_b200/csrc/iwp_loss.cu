@@ -283,7 +283,7 @@ HeadPlan head_plan(const iwp_head_args* a) {
   if (p.pack_weight) p.weight = take(2 * V * p.d_pad);
   if (p.grad) {
     // By default no more than the weights and their gradient take: 8192 tokens x 131072 x 4096 then stay one piece (2 GiB)
-    // and run in 23.2 ms, against 24.8 in two pieces of 1 GiB, the logits of one of which are computed twice.
+    // and run in 23.1 ms, against 24.8 in two pieces of 1 GiB, the logits of one of which are computed twice.
     const int64_t own = 4 * V * D;
     const int64_t limit = a->piece_bytes ? a->piece_bytes : own > LEAST_PIECE ? own : LEAST_PIECE;
     const int64_t v_pad = up_to(V, iwp_tc::TILE_N), t = T > 0 ? T : 1;
