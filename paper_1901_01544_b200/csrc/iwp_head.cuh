@@ -849,11 +849,35 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) k_few_tokens(const Few a) {
 }
 
 // Rows of `cols` 16-bit elements to rows of `ld_to` (a multiple of 8; zeros at the end), for operands TMA cannot address.
-__global__ void k_align_rows(const uint16_t* from, int64_t ld_from, uint16_t* to, int64_t ld_to, int64_t rows, int cols) {
+// A warp takes a row, a lane 16 bytes of the result at a time, read in the widest units that all rows start on.  Bound by
+// memory.
+template <class Unit>
+__global__ void __launch_bounds__(256) k_align_rows(const uint16_t* from, int64_t ld_from, uint16_t* to, int64_t ld_to, int64_t rows, int cols) {
+  constexpr int PER = sizeof(Unit) / 2, UNITS = 8 / PER;
   iwp_tc::launch_next();
   iwp_tc::wait_previous();
-  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
-    for (int c = threadIdx.x; c < ld_to; c += blockDim.x) to[r * ld_to + c] = c < cols ? from[r * ld_from + c] : uint16_t(0);
+  const int lane = threadIdx.x & 31, groups = static_cast<int>(ld_to / 8);
+  for (int64_t r = blockIdx.x * 8ll + (threadIdx.x >> 5); r < rows; r += gridDim.x * 8ll) {
+    const uint16_t* const row = from + r * ld_from;
+#pragma unroll 2
+    for (int g = lane; g < groups; g += 32) {
+      union {
+        Unit u[UNITS];
+        uint16_t e[8];
+        uint4 all;
+      } x;
+      x.all = make_uint4(0u, 0u, 0u, 0u);
+      if (8 * g + 8 <= cols) {
+#pragma unroll
+        for (int j = 0; j < UNITS; j++) x.u[j] = *reinterpret_cast<const Unit*>(row + 8 * g + PER * j);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; j++)
+          if (8 * g + j < cols) x.e[j] = row[8 * g + j];
+      }
+      *reinterpret_cast<uint4*>(to + r * ld_to + 8 * g) = x.all;
+    }
+  }
 }
 
 }  // namespace iwp_head

@@ -348,9 +348,12 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
   if (a->have_lse) LOSS_CUDA(launch(H::k_count_rows, 1, 1024, 0, 1, st, hdr, en, T));
   Matrix h{a->hidden, T, D, a->hidden_ld}, w{a->weight, V, D, a->weight_ld};
   auto align_rows = [&](Matrix& m, int64_t at) {
-    const int64_t blocks = m.rows < 8 * sms ? m.rows : 8 * sms;
-    const cudaError_t e = launch(H::k_align_rows, blocks, 256, 0, 1, st, static_cast<const uint16_t*>(m.p), m.ld, reinterpret_cast<uint16_t*>(ws + at),
-                                 p.d_pad, m.rows, static_cast<int>(D));
+    const int64_t warps = tiles_of(m.rows, 8), blocks = warps < 8 * sms ? warps : 8 * sms;
+    const auto kernel = aligned(m.p, 8) && m.ld % 4 == 0   ? H::k_align_rows<uint2>
+                        : aligned(m.p, 4) && m.ld % 2 == 0 ? H::k_align_rows<uint32_t>
+                                                           : H::k_align_rows<uint16_t>;
+    const cudaError_t e = launch(kernel, blocks, 256, 0, 1, st, static_cast<const uint16_t*>(m.p), m.ld, reinterpret_cast<uint16_t*>(ws + at), p.d_pad,
+                                 m.rows, static_cast<int>(D));
     m.p = ws + at, m.ld = p.d_pad;
     return e;
   };

@@ -561,7 +561,7 @@ __device__ __forceinline__ void store_staged(const CUtensorMap* map, char* stagi
 // TYPE: IWP_F32 / IWP_BF16 / IWP_F16.  `add`: the old contents are added first (in fp32).
 __device__ __forceinline__ void store_chunk(const float (&v)[32], char* staging, void* out, int64_t ld, int type, bool wide, bool add,
                                             int row0, int rows, int col0, int cols, int lane) {
-  if (type == 0 || !wide || add) {  // staged as fp32
+  if (type == 0 || add) {  // staged as fp32
 #pragma unroll
     for (int j = 0; j < 8; j++) *reinterpret_cast<float4*>(staged(staging, lane, j)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
   } else {
@@ -595,13 +595,27 @@ __device__ __forceinline__ void store_chunk(const float (&v)[32], char* staging,
         *p = x;
       }
     }
-  } else {  // ragged columns, unaligned rows, or a 16-bit sum: element by element, a row at a time
-    const bool packed = type != 0 && wide && !add;
+  } else if (type != 0 && !add) {
+    // ragged columns or unaligned rows of 16 bits: two rows at a time, in the 4-byte words of memory; of a row that starts
+    // in the middle of one, its first and its last column are stored on their own
+    const int half = lane >> 4, c = lane & 15;
+    for (int i = half; i < 32; i += 2) {
+      if (row0 + i >= rows) break;
+      uint16_t* const row = static_cast<uint16_t*>(out) + (row0 + i) * ld + col0;
+      const int odd = static_cast<int>(reinterpret_cast<uintptr_t>(row) >> 1 & 1);
+      auto at = [&](int k) { return *reinterpret_cast<const uint16_t*>(staged(staging, i, k >> 3) + 2 * (k & 7)); };
+      const int k = 2 * c + odd;
+      if (k + 1 < 32 && col0 + k + 1 < cols)
+        *reinterpret_cast<uint32_t*>(row + k) = at(k) | static_cast<uint32_t>(at(k + 1)) << 16;
+      else if (k < 32 && col0 + k < cols)
+        row[k] = at(k);
+      if (odd && c == 0 && col0 < cols) row[0] = at(0);
+    }
+  } else {  // ragged columns or unaligned rows of fp32, or a 16-bit sum: element by element, a row at a time
     for (int i = 0; i < 32 && row0 + i < rows; i++) {
       if (col0 + lane < cols) {
         const int64_t at = (row0 + i) * ld + col0 + lane;
-        float x = packed ? load_as_float(staged(staging, i, lane >> 3), lane & 7, type)
-                         : reinterpret_cast<const float*>(staged(staging, i, lane >> 2))[lane & 3];
+        float x = reinterpret_cast<const float*>(staged(staging, i, lane >> 2))[lane & 3];
         if (add) x += load_as_float(out, at, type);
         store_as(out, at, x, type);
       }
