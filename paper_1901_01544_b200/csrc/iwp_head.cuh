@@ -376,38 +376,34 @@ struct Out {
   }
 };
 
-// dhidden = factor * sum over the splits (in order), rounded once.  Four columns per thread where rows allow it.  Bound by
-// latency for the sizes that are split at all (1021 x 1032 in two parts: 7 us).
+// dhidden = factor * sum over the splits (in order), rounded once.  The parts' rows hold whole groups of four columns; a
+// thread takes a group.  Bound by latency for the sizes that are split at all (1021 x 1032 in two parts: 7 us).
 __global__ void __launch_bounds__(256) k_join(Factor f, const float* part, int splits, int64_t rows, int cols, void* out, int64_t ld, int type,
                                               int add, int wide) {
   iwp_tc::launch_next();
   iwp_tc::wait_previous();
   const float k = f.get();
-  const int64_t n = rows * cols;
-  const int per = wide ? 4 : 1, groups = cols / per;
+  const int groups = (cols + 3) / 4;
+  const int64_t n = rows * groups * 4;
   for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
     for (int g = threadIdx.x; g < groups; g += blockDim.x) {
-      const int64_t i = r * cols + g * per, at = r * ld + g * per;
-      if (wide) {
-        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int s = 0; s < splits; s++) {
-          const float4 y = __ldcs(reinterpret_cast<const float4*>(part + s * n + i));
-          x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
-        }
-        float v[4] = {x.x * k, x.y * k, x.z * k, x.w * k};
-        if (add)
-          for (int j = 0; j < 4; j++) v[j] += iwp_tc::load_as_float(out, at + j, type);
-        if (type == IWP_F32)
-          *reinterpret_cast<float4*>(static_cast<float*>(out) + at) = make_float4(v[0], v[1], v[2], v[3]);
-        else
-          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at) =
-              make_uint2(iwp_tc::pack2(v[0], v[1], type), iwp_tc::pack2(v[2], v[3], type));
+      const int64_t i = (r * groups + g) * 4, at = r * ld + 4 * g;
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int s = 0; s < splits; s++) {
+        const float4 y = __ldcs(reinterpret_cast<const float4*>(part + s * n + i));
+        x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
+      }
+      float v[4] = {x.x * k, x.y * k, x.z * k, x.w * k};
+      const int have = min(4, cols - 4 * g);
+      if (add)
+        for (int j = 0; j < have; j++) v[j] += iwp_tc::load_as_float(out, at + j, type);
+      if (!wide || have < 4) {
+        for (int j = 0; j < have; j++) iwp_tc::store_as(out, at + j, v[j], type);
+      } else if (type == IWP_F32) {
+        *reinterpret_cast<float4*>(static_cast<float*>(out) + at) = make_float4(v[0], v[1], v[2], v[3]);
       } else {
-        float x = 0.f;
-        for (int s = 0; s < splits; s++) x += part[s * n + i];
-        x *= k;
-        if (add) x += iwp_tc::load_as_float(out, at, type);
-        iwp_tc::store_as(out, at, x, type);
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at) =
+            make_uint2(iwp_tc::pack2(v[0], v[1], type), iwp_tc::pack2(v[2], v[3], type));
       }
     }
 }

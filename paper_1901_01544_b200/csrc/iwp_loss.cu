@@ -297,7 +297,7 @@ HeadPlan head_plan(const iwp_head_args* a) {
     p.probs = take(most > least ? most : least);
   }
   if (a->dhidden) {
-    const int64_t one = 4 * T * D, split = JOIN_TILES * 4 * iwp_tc::CG * iwp_tc::TILE_M * iwp_tc::TILE_N;
+    const int64_t one = 4 * T * up_to(D, 4), split = JOIN_TILES * 4 * iwp_tc::CG * iwp_tc::TILE_M * iwp_tc::TILE_N;
     p.join = take(one > split ? one : split);
   }
   p.bytes = at;
@@ -532,10 +532,10 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
       } else {
         o.out = ws + p.join;
         o.by_copy = 0;
-        o.ld = D;
-        o.split_stride = T * D;
+        o.ld = up_to(D, 4);
+        o.split_stride = T * o.ld;
         o.type = IWP_F32;
-        o.wide = D % 4 == 0;
+        o.wide = 1;
         o.add = done > 0;
         o.raw = 1;
       }
@@ -558,7 +558,7 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
   }
   if (a->dhidden && (p.pieces > 1 || splits > 1)) {
     const int size = a->dhidden_type == IWP_F32 ? 4 : 2;
-    const int wide = D % 4 == 0 && aligned(a->dhidden, 16) && a->dhidden_ld * size % 16 == 0;
+    const int wide = aligned(a->dhidden, 16) && a->dhidden_ld * size % 16 == 0;
     LOSS_CUDA(launch(H::k_join, T < 16 * sms ? T : 16 * sms, 256, 0, 1, st, oa.f, reinterpret_cast<const float*>(ws + p.join), splits, T,
                      static_cast<int>(D), a->dhidden, a->dhidden_ld, a->dhidden_type, a->accumulate, wide));
   }
