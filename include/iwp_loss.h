@@ -45,7 +45,10 @@ int iwp_loss_status(const void* workspace, int32_t* status_host, void* cuda_stre
  * part, a logit of -inf has q = 0; nothing but those: no target.  A target or id at or above vocab (or a negative
  * target that is not ignore_index) sets the status word to IWP_ERR_INVALID, makes the row's loss NaN and gives no
  * gradient.  Products are of the operands' 16-bit type with fp32 accumulation; statistics and losses are fp32.
- * The gradient's factors exp(..) - q are rounded once to the operands' type, as the tensor cores take no wider one.
+ * The gradient's factors exp(..) - q are rounded to the operands' type, as the tensor cores take no wider one.  Where
+ * nothing is subtracted, exp(..) may have been held in a 16-bit code before: off by at most 2^-12 of itself (bf16
+ * operands) or 1.7e-4 (fp16), and nothing below 2^-40 (2^-24) of the largest of the row's 32 to 128 columns around it.
+ * Where q is subtracted, exp(..) is fp32: a student close to its teacher keeps the precision of one rounding.
  */
 typedef struct iwp_head_args {
   int64_t tokens, vocab, dim;      /* T >= 0, 1 <= V, 1 <= D; each below 2^31 - 1024, their products

@@ -634,11 +634,12 @@ __global__ void __launch_bounds__(ROW_THREADS) k_rows(const Rows a) {
 struct Factors {
   Targets en;
   const float2* part;  // [T][parts]
+  const float* z_at;   // [T][k] logits at the targets
   const float* lse;
   uint16_t* codes;  // [T][ld], in place
   int64_t ld;
   int parts, part_shift, v0, width, chunks, log_codes;
-  float up;
+  float c, up;  // log2(e) / tau
 };
 
 constexpr int FACTOR_THREADS = 256, FACTOR_DEEP = 4, FACTOR_COLUMNS = 8 * FACTOR_THREADS * FACTOR_DEEP;
@@ -665,11 +666,8 @@ __global__ void __launch_bounds__(FACTOR_THREADS) k_factors(const Factors a) {
     }
   }
   const float scale = a.en.row_scale(row) * a.up;
-  auto probability = [&](float top, uint32_t code) {  // top = the part's maximum less lse, in log2
-    return a.log_codes ? ex2(top + 8.f - log_value(code)) : __half2float(__ushort_as_half(static_cast<uint16_t>(code))) * ex2(top - 15.f);
-  };
   int at[MINE];
-  uint32_t code[MINE];
+  float z[MINE];
   bool any = false;
 #pragma unroll
   for (int i = 0; i < MINE; i++) {
@@ -679,14 +677,14 @@ __global__ void __launch_bounds__(FACTOR_THREADS) k_factors(const Factors a) {
       const int col = a.en.column_at(row, k);
       if (col >= a.v0 + c0 && col < a.v0 + c1 && a.en.q_at(row, k) != 0.f) {
         at[i] = col - a.v0;
-        code[i] = codes[at[i]];
+        z[i] = a.z_at[row * a.en.k + k];
         any = true;
       }
     }
   }
   iwp_tc::wait_previous();
   const float lse2 = a.lse[row] * LOG2E;
-  any = __syncthreads_or(any);  // and nobody's code is overwritten before it was read
+  any = __syncthreads_or(any);
 #pragma unroll
   for (int i = 0; i < FACTOR_DEEP; i++) {
     const int o = c0 + 8 * tid + i * 8 * FACTOR_THREADS;
@@ -710,11 +708,12 @@ __global__ void __launch_bounds__(FACTOR_THREADS) k_factors(const Factors a) {
     *reinterpret_cast<uint4*>(codes + o) = u[i];
   }
   if (!any || scale == 0.f) return;
-  __syncthreads();
+  __syncthreads();  // the factors of columns without a target are there
+  // p - q cancels where a student is close to its teacher: p of a target comes from its fp32 logit, not from its code
 #pragma unroll
   for (int i = 0; i < MINE; i++)
     if (at[i] >= 0) {
-      const float p = probability(part[(a.v0 + at[i]) >> a.part_shift].x - lse2, code[i]);
+      const float p = ex2(fmaf(z[i], a.c, -lse2));
       iwp_tc::store_as(codes, at[i], (p - a.en.q_at(row, tid + i * FACTOR_THREADS)) * scale, a.log_codes ? IWP_F16 : IWP_BF16);
     }
 }

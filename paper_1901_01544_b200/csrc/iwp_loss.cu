@@ -450,6 +450,7 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
       H::Factors fa{};
       fa.en = en;
       fa.part = ra.part;
+      fa.z_at = ra.z_at;
       fa.lse = a->lse;
       fa.codes = probs;
       fa.ld = p.piece;
@@ -459,6 +460,7 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
       fa.width = static_cast<int>(V - fa.v0 < p.piece ? V - fa.v0 : p.piece);
       fa.chunks = static_cast<int>(tiles_of(fa.width, H::FACTOR_COLUMNS));
       fa.log_codes = a->dtype == IWP_F16;
+      fa.c = c;
       fa.up = up;
       if (T * fa.chunks > MAX_SIZE) return IWP_ERR_INVALID;
       LOSS_CUDA(launch(H::k_factors, T * fa.chunks, H::FACTOR_THREADS, 0, 1, st, fa));

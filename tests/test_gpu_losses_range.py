@@ -1,0 +1,82 @@
+"""The losses where their numbers are delicate: factors that cancel, confident rows, upstream gradients of very different
+sizes, the lowest values, sums over long rows.
+
+Most cases take a head whose weights are the identity: the logits are then the hidden states (products with one and zero,
+sums of one term: exact), and the gradient to the hidden states is the factor exp(..) - q itself, times the upstream
+gradient.  With logits below 32 in magnitude a probability formed in fp32 is off by at most P = 2^-16 of itself: five
+roundings of exponents below 64 (2^-19 each, in log2), the sum's 64 additions per lane (2^-18), exp2 and log (2^-20)."""
+import math
+
+import pytest
+import torch
+from test_gpu_losses import BF, DEV, F32, HF, TINY, U, gen, soft_targets
+
+from paper_1901_01544_b200 import losses
+
+pytestmark = pytest.mark.gpu
+P = 2.0**-16
+
+
+def identity_head(T, V, D, dtype, seed, spread=3.0):
+    """Hidden states that are the logits of the first D columns (the others' logits are zero)."""
+    g = gen(seed)
+    h = (torch.randn(T, D, generator=g, device=DEV) * spread).to(dtype)
+    return h, torch.eye(V, D, device=DEV).to(dtype), g
+
+
+def within(got, want, tol, name):
+    got = got.double()
+    assert torch.isfinite(got).all(), name + " is not finite"
+    worst = ((got - want).abs() / tol).max().item()
+    assert worst <= 1.0, f"{name}: {worst:.3g} times its bound"
+
+
+def factor_error(p, q, dtype, at_target):
+    """Bound on one factor p - q: one rounding to the type (fp16 factors are kept 2^13 higher, so its smallest steps are
+    2^-38), the errors of p and of the teacher's q; where nothing is subtracted a code of p may have been rounded once more,
+    and be cut off below 2^-24 of its row's largest."""
+    f = (p - q).abs()
+    return U[dtype] * f + P * (p + q) + 2.0**-37 + torch.where(at_target, 0.0, U[dtype] * p + 2.0**-24 * p.amax(1, keepdim=True))
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("eps", [1e-1, 1e-3, 0.0])
+@pytest.mark.parametrize("T,n,tau,piece", [(70, 64, 1.0, 0), (70, 64, 2.0, 0), (33, 1024, 1.0, 1), (33, 1024, 1.0, 0), (300, 200, 1.0, 0)])
+def test_student_close_to_its_teacher(T, n, tau, piece, eps, dtype):
+    """Teacher's logits = the student's plus a little noise, for every column: p - q is `eps` of p, and keeps the relative
+    error of one rounding as far as fp32 can tell p from q."""
+    h, w, g = identity_head(T, n, n, dtype, 700 + T + n)
+    ids = torch.rand(T, n, generator=g, device=DEV).argsort(1)
+    logits = h.float().gather(1, ids) + eps * torch.randn(T, n, generator=g, device=DEV)
+    q = torch.zeros(T, n, dtype=torch.float64, device=DEV).scatter_(1, ids, soft_targets(ids, logits, tau))
+    p = torch.softmax(h.double() / tau, 1)
+    f = tau * (p - q)
+    f_err = tau * factor_error(p, q, dtype, torch.ones_like(p, dtype=torch.bool))
+    w_err = f_err.T @ h.double().abs() + (T / 16 + 8) * 2.0**-22 * (f.abs().T @ h.double().abs())
+    plan = losses.HeadLoss(T, n, n, dtype, top_k=n, piece_bytes=piece)
+    lse = plan.distill(h, w, ids, logits, tau).lse
+    for saved in (None, lse):
+        dh, dw = torch.empty(T, n, device=DEV), torch.empty(n, n, device=DEV)
+        plan.distill_grad(h, w, ids, logits, tau, reduction="sum", lse=saved, dhidden=dh, dweight=dw)
+        within(dh, f, f_err + 2.0**-23 * f.abs() + 1e-37, "dhidden")
+        within(dw, f.T @ h.double(), w_err + 2.0**-23 * (f.T @ h.double()).abs() + 1e-37, "dweight")
+    assert plan.status() == 0
+
+
+@pytest.mark.parametrize("piece", [0, 1])
+@pytest.mark.parametrize("T,V,n,K,tau", [(50, 300, 64, 9, 1.0), (150, 700, 128, 50, 2.0), (5, 1100, 72, 64, 0.5)])
+def test_distillation_in_fp16(T, V, n, K, tau, piece):
+    h, w, g = identity_head(T, V, n, HF, 720 + T)
+    ids = torch.rand(T, V, generator=g, device=DEV).argsort(1)[:, :K].contiguous()
+    logits = torch.randn(T, K, generator=g, device=DEV) * 3
+    q = torch.zeros(T, V, dtype=torch.float64, device=DEV).scatter_(1, ids, soft_targets(ids, logits, tau))
+    hit = torch.zeros(T, V, dtype=torch.bool, device=DEV).scatter_(1, ids, True)
+    z = torch.cat([h.double(), torch.zeros(T, V - n, dtype=torch.float64, device=DEV)], 1)
+    p = torch.softmax(z / tau, 1)
+    f, f_err = tau * (p - q), tau * factor_error(p, q, HF, hit)
+    plan = losses.HeadLoss(T, V, n, HF, top_k=K, piece_bytes=piece)
+    dh, dw = torch.empty(T, n, device=DEV), torch.empty(V, n, device=DEV)
+    plan.distill_grad(h, w, ids, logits, tau, reduction="sum", dhidden=dh, dweight=dw)
+    within(dh, f[:, :n], f_err[:, :n] + 2.0**-23 * f[:, :n].abs(), "dhidden")
+    want = f.T @ h.double()
+    within(dw, want, f_err.T @ h.double().abs() + (T / 16 + 8) * 2.0**-22 * (f.abs().T @ h.double().abs()) + 2.0**-23 * want.abs(), "dweight")
