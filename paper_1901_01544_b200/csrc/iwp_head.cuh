@@ -34,7 +34,7 @@ using iwp_tc::Where;
 
 constexpr int MAX_TOP = 1024;
 constexpr int NO_COLUMN = 0x7FFFFFFF;
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float LOG2E = 1.4426950408889634f;
 
 // First bytes of a workspace.  The tickets wrap to zero with the last block of each launch.
 struct Header {
@@ -163,7 +163,7 @@ struct Logits {
     int64_t T;
     int V;
     float c;          // log2(e) / tau
-    float2* part;     // [T][parts]: maximum (of z c) and sum of 2^(z c - maximum)
+    float2* part;     // [T][parts]: maximum of z and sum of 2^((z - maximum) c)
     int parts;
     float* z_at;      // [T][k] logits at the targets
     uint16_t* codes;  // [T][ld] of columns v0 .. v0 + width
@@ -212,11 +212,12 @@ struct Logits {
         top = fmaxf(top, fmaxf(x.x, x.y));
       }
     }
-    const float m = top * a.c;
-    const float ref = m == -CUDART_INF_F ? 0.f : m;  // nothing but -inf: sums of 0, not of NaN
+    // The maximum is subtracted before the scaling: its own term is then 1 exactly, and a row whose target has all the
+    // mass loses nothing, however large its logits are.  Nothing but -inf: sums of 0, not of NaN.
+    const float ref = top == -CUDART_INF_F ? 0.f : -top;
     const bool keep = CODES != NO_CODES && w.col0 >= a.v0 && w.col0 < a.v0 + a.width;
-    const f2 scale = pack(a.c, a.c), less = pack(15.f - ref, 15.f - ref);
-    const f2 down = pack(-a.c, -a.c), from = pack(8.f + HALF_STEP + ref, 8.f + HALF_STEP + ref);
+    const f2 scale = pack(a.c, a.c), less = pack(ref, ref), up_by = pack(15.f, 15.f);
+    const f2 down = pack(-a.c, -a.c), from = pack(8.f + HALF_STEP, 8.f + HALF_STEP);
     f2 sum = pack(0.f, 0.f);
     uint32_t packed[2][16];
 #pragma unroll
@@ -224,8 +225,8 @@ struct Logits {
       if (32 * c >= w.width) break;
 #pragma unroll
       for (int j = 0; j < 16; j++) {
-        const f2 z = acc[16 * c + j];
-        const float2 x = unpack(fma2(z, scale, less));
+        const f2 z = add2(acc[16 * c + j], less);
+        const float2 x = unpack(fma2(z, scale, up_by));
         const float2 e = make_float2(ex2(x.x), ex2(x.y));
         sum = add2(sum, pack(e.x, e.y));
         if constexpr (CODES == HALF_CODES) packed[c % 2][j] = iwp_tc::pack2(e.x, e.y, IWP_F16);
@@ -244,7 +245,7 @@ struct Logits {
       }
     }
     const float2 s = unpack(sum);
-    if (live) a.part[static_cast<int64_t>(row) * a.parts + w.col0 / w.width] = make_float2(m, (s.x + s.y) * SUM_SCALE);
+    if (live) a.part[static_cast<int64_t>(row) * a.parts + w.col0 / w.width] = make_float2(top, (s.x + s.y) * SUM_SCALE);
   }
 };
 
@@ -534,14 +535,14 @@ struct Rows {
   float* loss;
   int64_t T;
   int parts, lanes, mean;
-  float tau;
+  float tau, c;  // log2(e) / tau
 };
 
 constexpr int ROW_THREADS = 256;
 
-__device__ __forceinline__ float2 join(float2 a, float2 b) {  // (maximum, sum of 2^(x - maximum))
+__device__ __forceinline__ float2 join(float2 a, float2 b, float c) {  // (maximum, sum of 2^((z - maximum) c))
   const float m = fmaxf(a.x, b.x), ref = m == -CUDART_INF_F ? 0.f : m;
-  return make_float2(m, a.y * ex2(a.x - ref) + b.y * ex2(b.x - ref));
+  return make_float2(m, a.y * ex2((a.x - ref) * c) + b.y * ex2((b.x - ref) * c));
 }
 
 // lse and loss of a row by a warp (lanes = 32), or by the block where there are few rows (lanes = 256); the last block to
@@ -571,23 +572,24 @@ __global__ void __launch_bounds__(ROW_THREADS) k_rows(const Rows a) {
     const float2* const part = a.part + row * a.parts;
     float2 x = make_float2(-CUDART_INF_F, 0.f);
 #pragma unroll 4
-    for (int p = me; p < a.parts; p += a.lanes) x = join(x, part[p]);
+    for (int p = me; p < a.parts; p += a.lanes) x = join(x, part[p], a.c);
 #pragma unroll
-    for (int o = 16; o; o >>= 1) x = join(x, make_float2(__shfl_xor_sync(0xFFFFFFFFu, x.x, o), __shfl_xor_sync(0xFFFFFFFFu, x.y, o)));
+    for (int o = 16; o; o >>= 1) x = join(x, make_float2(__shfl_xor_sync(0xFFFFFFFFu, x.x, o), __shfl_xor_sync(0xFFFFFFFFu, x.y, o)), a.c);
     if (a.lanes != 32) {
       if (lane == 0) sh[warp] = x;
       __syncthreads();
       x = sh[0];
 #pragma unroll
-      for (int w = 1; w < WARPS; w++) x = join(x, sh[w]);
+      for (int w = 1; w < WARPS; w++) x = join(x, sh[w], a.c);
     }
-    const float lse = (x.x + log2f(x.y)) * LN2;
-    // q (lse - z / tau) entry by entry, so that a confident row keeps its small loss
-    float below = column != NO_COLUMN && q != 0.f ? q * (lse - z / a.tau) : 0.f;
+    // q (lse - z / tau) entry by entry and without lse, whose last bits a large logit takes: the sum is 1 or more and
+    // the maximum no less than z, so the loss of a confident row is small and never negative
+    const float log_sum = logf(x.y);
+    float below = column != NO_COLUMN && q != 0.f ? q * ((x.x - z) / a.tau + log_sum) : 0.f;
     for (int k = me + a.lanes; k < a.en.k; k += a.lanes) {
       if (a.en.column_at(row, k) == NO_COLUMN) break;
       const float qk = a.en.q_at(row, k);
-      if (qk != 0.f) below += qk * (lse - a.z_at[row * a.en.k + k] / a.tau);
+      if (qk != 0.f) below += qk * ((x.x - a.z_at[row * a.en.k + k]) / a.tau + log_sum);
     }
     below = warp_sum(below);
     if (a.lanes != 32) {
@@ -599,7 +601,7 @@ __global__ void __launch_bounds__(ROW_THREADS) k_rows(const Rows a) {
     }
     if (me == 0) {
       const float c = a.en.hard ? 0.f : a.en.const_term[row];
-      a.lse[row] = lse;
+      a.lse[row] = x.x / a.tau + log_sum;
       a.rows[row] = state == 0 ? 0.f : state < 0 ? CUDART_NAN_F : a.tau * a.tau * (c + below);
       if (state < 0) atomicExch(&a.hdr->status, IWP_ERR_INVALID);
       __threadfence();
@@ -690,7 +692,7 @@ __global__ void __launch_bounds__(FACTOR_THREADS) k_factors(const Factors a) {
     const int o = c0 + 8 * tid + i * 8 * FACTOR_THREADS;
     if (o >= c1) break;
     uint32_t* const e = reinterpret_cast<uint32_t*>(&u[i]);
-    const float top = m[i] - lse2;
+    const float top = fmaf(m[i], a.c, -lse2);  // the part's maximum less lse, in log2
     if (scale == 0.f) {  // a row that gives nothing, whatever its logits are
       u[i] = make_uint4(0u, 0u, 0u, 0u);
     } else if (a.log_codes) {
@@ -821,14 +823,14 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) k_few_tokens(const Few a) {
 #pragma unroll
       for (int r = 0; r < FEW_ROWS; r++) {
         const float2 both = unpack(acc[r][t]);
-        z[r] = warp_sum(both.x + both.y) * a.c;
+        z[r] = warp_sum(both.x + both.y);
         if (r >= have) z[r] = -CUDART_INF_F;
         top = fmaxf(top, z[r]);
       }
       const float ref = top == -CUDART_INF_F ? 0.f : top;
-      s[t] *= ex2(m[t] - ref);
+      s[t] *= ex2((m[t] - ref) * a.c);
 #pragma unroll
-      for (int r = 0; r < FEW_ROWS; r++) s[t] += ex2(z[r] - ref);
+      for (int r = 0; r < FEW_ROWS; r++) s[t] += ex2((z[r] - ref) * a.c);
       m[t] = top;
     }
   }
@@ -838,7 +840,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) k_few_tokens(const Few a) {
   __syncthreads();
   if (tid < TOKENS) {
     float2 x = sh[0][tid];
-    for (int w = 1; w < WARPS; w++) x = join(x, sh[w][tid]);
+    for (int w = 1; w < WARPS; w++) x = join(x, sh[w][tid], a.c);
     a.part[tid * a.blocks + blockIdx.x] = x;
   }
 }

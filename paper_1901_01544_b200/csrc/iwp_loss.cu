@@ -375,6 +375,7 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
     ra.T = T;
     ra.mean = a->mean;
     ra.tau = tau;
+    ra.c = c;
     ra.lanes = T <= 8 * sms ? H::ROW_THREADS : 32;  // a block per row while all blocks run at once, a warp after that
     const int64_t row_blocks = ra.lanes == 32 ? tiles_of(T, H::ROW_THREADS / 32) : T;
     if (p.few) {

@@ -80,3 +80,41 @@ def test_distillation_in_fp16(T, V, n, K, tau, piece):
     within(dh, f[:, :n], f_err[:, :n] + 2.0**-23 * f[:, :n].abs(), "dhidden")
     want = f.T @ h.double()
     within(dw, want, f_err.T @ h.double().abs() + (T / 16 + 8) * 2.0**-22 * (f.abs().T @ h.double().abs()) + 2.0**-23 * want.abs(), "dweight")
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("T,V,D", [(1, 64, 64), (2, 300, 64), (40, 64, 64), (300, 900, 128), (5000, 300, 64)])
+def test_confident_rows(T, V, D, dtype):
+    """Rows whose target has all the mass lose nothing at all, whatever the size of their logits; with a little mass
+    elsewhere the loss is log(1 + s), s of few terms: right to the last bits of fp32."""
+    w = torch.eye(V, D, device=DEV).to(dtype)
+    y = torch.arange(T, device=DEV) % D
+    top = torch.tensor([20.0, 37.5, 60.0, 300.0, 500.0], device=DEV)[torch.arange(T, device=DEV) % 5][:, None]
+    on = torch.nn.functional.one_hot(y, D).bool()
+    plan = losses.HeadLoss(T, V, D, dtype)
+    for gap in (400.0, 12.0, 4.0):
+        h = torch.where(on, top, top - gap).to(dtype)
+        if gap == 400.0:
+            h = torch.where(on, h, -200.0).to(dtype)
+        z = torch.cat([h.double(), torch.zeros(T, V - D, dtype=torch.float64, device=DEV)], 1)
+        lse = torch.logsumexp(z, 1)
+        want = torch.log1p(torch.where(torch.nn.functional.one_hot(y, V).bool(), 0.0, torch.exp(z - top.double())).sum(1)) if gap < 400 or V > D else 0 * lse
+        r = plan.cross_entropy(h, w, y)
+        # a lane adds at most 64 terms to a sum that starts at 1 or more, 20 more additions join lanes and parts; a term is
+        # off by 2^-19 of itself (its exponent is rounded below 64)
+        tol = 84 * 2.0**-24 * (1 + want) + 2.0**-19 * want
+        if gap == 400.0 and V == D:
+            assert not r.rows.any() and torch.equal(r.lse, top[:, 0]) and r.loss == 0
+        assert (r.rows >= 0).all()
+        within(r.rows, want, tol, "rows")
+        within(r.lse, lse, tol + 2.0**-23 * lse.abs(), "lse")
+
+
+def test_confident_rows_of_a_distillation():
+    T, n, tau = 60, 64, 2.0
+    w = torch.eye(n, device=DEV).to(BF)
+    y = torch.arange(T, device=DEV) % n
+    h = torch.where(torch.nn.functional.one_hot(y, n).bool(), 300.0, -100.0).to(BF)
+    plan = losses.HeadLoss(T, n, n, BF, top_k=1)
+    r = plan.distill(h, w, y[:, None], torch.zeros(T, 1, device=DEV), tau)
+    assert not r.rows.any() and r.loss == 0 and (r.lse == 150.0).all()
