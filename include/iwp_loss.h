@@ -49,6 +49,8 @@ int iwp_loss_status(const void* workspace, int32_t* status_host, void* cuda_stre
  * nothing is subtracted, exp(..) may have been held in a 16-bit code before: off by at most 2^-12 of itself (bf16
  * operands) or 1.7e-4 (fp16), and nothing below 2^-40 (2^-24) of the largest of the row's 32 to 128 columns around it.
  * Where q is subtracted, exp(..) is fp32: a student close to its teacher keeps the precision of one rounding.
+ * A row's dhidden depends on no other row's dloss_rows, neither in its precision nor by an infinity or NaN.  With fp16
+ * operands and dloss_rows, dweight sums over hidden states multiplied by powers of two of at most 1 and rounded to fp16.
  */
 typedef struct iwp_head_args {
   int64_t tokens, vocab, dim;      /* T >= 0, 1 <= V, 1 <= D; each below 2^31 - 1024, their products

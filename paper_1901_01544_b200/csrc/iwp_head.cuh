@@ -41,7 +41,7 @@ struct Header {
   int status;
   int n_rows;       // rows with targets
   uint32_t ticket;
-  float gmax;       // largest |dloss_rows|
+  float gmax;       // the largest of the rows' powers of two (k_row_scales)
 };
 
 // What the rows subtract.  `hard`: one target per row, read as the caller gave them; else lists made by k_soft_targets.
@@ -53,7 +53,7 @@ struct Targets {
   const int* column;       // [T][k] ascending, NO_COLUMN at the end
   const float* q;          // [T][k]
   const float* const_term; // [T] sum of q log q; NaN for a row with an id outside the vocabulary
-  const float* scale;      // [T] dloss_rows / gmax, or NULL: 1 for rows with targets
+  const float* scale;      // [T] what the rows' factors are multiplied with, or NULL: 1 for rows with targets
 
   __device__ __forceinline__ int column_at(int64_t row, int i) const {
     if (!hard) return column[row * k + i];
@@ -316,15 +316,14 @@ struct Probs {
 
 // ---- epilogue of the gradient products ------------------------------------------------------------------
 
-// What both gradients are multiplied with: `factor` (scale * tau / up) * gmax * dloss / n.
+// What both gradients are multiplied with: `factor` (scale * tau / up) * dloss / n.
 struct Factor {
   const Header* hdr;
   const float* dloss;
   float factor;
-  int mean, by_rows;
+  int mean;
   __device__ __forceinline__ float get() const {
     float f = factor;
-    if (by_rows) f *= hdr->gmax;
     if (dloss) f *= *dloss;
     if (mean) f /= static_cast<float>(max(hdr->n_rows, 1));
     return f;
@@ -339,13 +338,21 @@ struct Out {
     int64_t ld, split_stride;  // elements
     int rows, cols, type, wide, add, raw;  // raw: partial sums, the factor is applied later
     int by_copy;                           // 16-bit rows that start at multiples of 16 bytes, nothing to add
+    int by_gmax;                           // dweight, where the hidden states carry the rows' powers of two
+    const float* row_power;                // dhidden: [rows], or NULL
     CUtensorMap map;                       // of `out` then, in boxes of 32 rows and 64 columns
   };
   struct Args {
     Factor f;
     Matrix m[2];
   };
-  static __device__ __forceinline__ float begin(const Args& args, const Where& w) { return args.m[w.p].raw ? 1.f : args.f.get(); }
+  static __device__ __forceinline__ float begin(const Args& args, const Where& w) {
+    const Matrix& a = args.m[w.p];
+    if (a.raw) return 1.f;
+    const float f = args.f.get();
+    if (a.by_gmax) return f * args.f.hdr->gmax;
+    return a.row_power && w.row0 + w.lane < a.rows ? f * a.row_power[w.row0 + w.lane] : f;
+  }
   static __device__ __forceinline__ void tile(const Args& args, Where& w, float f, uint32_t tmem) {
     const Matrix& a = args.m[w.p];
     if (a.by_copy && w.width >= 64) {
@@ -377,16 +384,17 @@ struct Out {
   }
 };
 
-// dhidden = factor * sum over the splits (in order), rounded once.  The parts' rows hold whole groups of four columns; a
+// dhidden = factor (* the row's power of two) * sum over the splits (in order), rounded once.  The parts' rows hold whole groups of four columns; a
 // thread takes a group.  Bound by latency for the sizes that are split at all (1021 x 1032 in two parts: 7 us).
-__global__ void __launch_bounds__(256) k_join(Factor f, const float* part, int splits, int64_t rows, int cols, void* out, int64_t ld, int type,
-                                              int add, int wide) {
+__global__ void __launch_bounds__(256) k_join(Factor f, const float* row_power, const float* part, int splits, int64_t rows, int cols, void* out,
+                                              int64_t ld, int type, int add, int wide) {
   iwp_tc::launch_next();
   iwp_tc::wait_previous();
-  const float k = f.get();
+  const float all = f.get();
   const int groups = (cols + 3) / 4;
   const int64_t n = rows * groups * 4;
-  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
+  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+    const float k = row_power ? all * row_power[r] : all;
     for (int g = threadIdx.x; g < groups; g += blockDim.x) {
       const int64_t i = (r * groups + g) * 4, at = r * ld + 4 * g;
       float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -407,6 +415,7 @@ __global__ void __launch_bounds__(256) k_join(Factor f, const float* part, int s
             make_uint2(iwp_tc::pack2(v[0], v[1], type), iwp_tc::pack2(v[2], v[3], type));
       }
     }
+  }
 }
 
 // ---- targets -----------------------------------------------------------------------------------------------
@@ -492,21 +501,62 @@ __global__ void k_soft_targets(int* column, float* q_out, float* const_term, con
   if (lane == 0) const_term[t] = bad ? CUDART_NAN_F : has ? term : 0.f;
 }
 
-// ---- per-row upstream gradients: their largest magnitude, and the rows relative to it ------------------------
-
-__global__ void __launch_bounds__(1024) k_row_scales(Header* hdr, Targets en, float* scale, const float* dloss_rows, int64_t T) {
+// ---- per-row upstream gradients of fp16 operands ------------------------------------------------------------------
+//
+// bf16 factors take the rows' upstream gradients directly: they have fp32's range.  In fp16 a row far below the others'
+// would lose its small probabilities, and with them its own gradient, which does not depend on the others'.  There an
+// upstream gradient is split as r 2^e, 1 <= |r| < 2: the factors take r; dhidden's epilogue takes the row's 2^e; for
+// dweight, a sum over the rows, a copy of the hidden states takes 2^e relative to the largest of them (its small rows may
+// be rounded to fp16's smallest steps, which are 2^-24 beside the large rows' values; rows that give nothing are zero).
+__global__ void __launch_bounds__(1024) k_row_scales(Header* hdr, Targets en, float* scale, float* power, const float* dloss_rows, int64_t T) {
   __shared__ float sh[32];
   iwp_tc::launch_next();
   iwp_tc::wait_previous();
-  float m = 0.f;
-  for (int64_t t = threadIdx.x; t < T; t += blockDim.x)
-    if (en.state(t) == 1) m = fmaxf(m, fabsf(dloss_rows[t]));
-  m = warp_max(m);
-  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = m;
+  float top = 0.f;
+  for (int64_t t = threadIdx.x; t < T; t += blockDim.x) {
+    float r = en.state(t) == 1 ? dloss_rows[t] : 0.f, p = 1.f;
+    if (r != 0.f && isfinite(r)) {
+      int e;
+      r = 2.f * frexpf(r, &e);
+      p = ldexpf(1.f, e - 1);
+      top = fmaxf(top, p);
+    }
+    scale[t] = r;
+    power[t] = p;
+  }
+  top = warp_max(top);
+  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = top;
   __syncthreads();
-  m = warp_max(sh[threadIdx.x & 31]);
-  if (threadIdx.x == 0) hdr->gmax = m;
-  for (int64_t t = threadIdx.x; t < T; t += blockDim.x) scale[t] = m > 0.f ? dloss_rows[t] / m : dloss_rows[t];
+  top = warp_max(sh[threadIdx.x & 31]);
+  if (threadIdx.x == 0) hdr->gmax = top > 0.f ? top : 1.f;
+}
+
+// The copy of the hidden states for dweight; rows of both start at multiples of 16 bytes.  A warp takes a row.
+__global__ void __launch_bounds__(256) k_scaled_rows(const Header* hdr, const float* scale, const float* power, const __half* from, int64_t ld_from,
+                                                     __half* to, int64_t ld_to, int64_t rows, int cols) {
+  iwp_tc::launch_next();
+  iwp_tc::wait_previous();
+  const int lane = threadIdx.x & 31;
+  const float all = hdr->gmax;
+  for (int64_t r = blockIdx.x * 8ll + (threadIdx.x >> 5); r < rows; r += gridDim.x * 8ll) {
+    const bool gives = scale[r] != 0.f;
+    const float k = power[r] / all;
+    for (int g = 8 * lane; g < cols; g += 8 * 32) {
+      union {
+        __half e[8];
+        uint4 all;
+      } x;
+      if (g + 8 <= cols) {
+        x.all = *reinterpret_cast<const uint4*>(from + r * ld_from + g);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; j++) x.e[j] = g + j < cols ? from[r * ld_from + g + j] : __float2half_rn(0.f);
+      }
+#pragma unroll
+      for (int j = 0; j < 8; j++) x.e[j] = __float2half_rn(gives ? __half2float(x.e[j]) * k : 0.f);
+      *reinterpret_cast<uint4*>(to + r * ld_to + g) = x.all;
+    }
+  }
 }
 
 // Number of rows with targets, for backward passes on their own (k_rows counts them otherwise).

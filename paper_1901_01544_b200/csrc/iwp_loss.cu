@@ -231,9 +231,10 @@ int launch_product(iwp_tc::Problems<N>& w, const typename Epi::Args& args, cudaS
 
 struct HeadPlan {
   bool grad, few, pack_hidden, pack_weight;
+  bool split_rows;  // fp16 with an upstream gradient per row: k_row_scales
   int64_t k, piece, pieces, d_pad;
   // offsets into the workspace
-  int64_t column, q, const_term, row_scale, rows, z_at, part, hidden, weight, probs, join, bytes;
+  int64_t column, q, const_term, row_scale, row_power, rows, z_at, part, hidden, weight, scaled, probs, join, bytes;
 };
 
 bool needs_copy(const void* p, int64_t ld) { return !aligned(p, 16) || ld % 8 != 0; }
@@ -270,7 +271,12 @@ HeadPlan head_plan(const iwp_head_args* a) {
     p.q = take(4 * p.k * T);
     p.const_term = take(4 * T);
   }
-  p.row_scale = take(4 * T);
+  p.split_rows = p.grad && a->dloss_rows && a->dtype == IWP_F16;
+  if (p.split_rows) {
+    p.row_scale = take(4 * T);
+    p.row_power = take(4 * T);
+    if (a->dweight) p.scaled = take(2 * T * p.d_pad);
+  }
   p.rows = take(4 * T);
   if (!a->have_lse) {
     p.z_at = take(4 * p.k * T);
@@ -340,11 +346,10 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
     en.q = q;
     en.const_term = term;
   }
-  if (p.grad && a->dloss_rows) {
-    float* const scale = reinterpret_cast<float*>(ws + p.row_scale);
-    LOSS_CUDA(launch(H::k_row_scales, 1, 1024, 0, 1, st, hdr, en, scale, a->dloss_rows, T));
-    en.scale = scale;
-  }
+  float* const row_scale = reinterpret_cast<float*>(ws + p.row_scale);
+  float* const row_power = p.split_rows ? reinterpret_cast<float*>(ws + p.row_power) : nullptr;
+  if (p.split_rows) LOSS_CUDA(launch(H::k_row_scales, 1, 1024, 0, 1, st, hdr, en, row_scale, row_power, a->dloss_rows, T));
+  if (p.grad) en.scale = p.split_rows ? row_scale : a->dloss_rows;
   if (a->have_lse) LOSS_CUDA(launch(H::k_count_rows, 1, 1024, 0, 1, st, hdr, en, T));
   Matrix h{a->hidden, T, D, a->hidden_ld}, w{a->weight, V, D, a->weight_ld};
   auto align_rows = [&](Matrix& m, int64_t at) {
@@ -359,6 +364,13 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
   };
   if (p.pack_hidden) LOSS_CUDA(align_rows(h, p.hidden));
   if (p.pack_weight) LOSS_CUDA(align_rows(w, p.weight));
+  Matrix h_dw = h;  // of dweight's product
+  if (p.split_rows && a->dweight) {
+    h_dw.p = ws + p.scaled, h_dw.ld = p.d_pad;
+    const int64_t blocks = tiles_of(T, 8);
+    LOSS_CUDA(launch(H::k_scaled_rows, blocks < 8 * sms ? blocks : 8 * sms, 256, 0, 1, st, hdr, row_scale, row_power, static_cast<const __half*>(h.p),
+                     h.ld, reinterpret_cast<__half*>(ws + p.scaled), p.d_pad, T, static_cast<int>(D)));
+  }
 
   const float up = a->dtype == IWP_F16 ? 8192.f : 1.f;
   uint16_t* const probs = reinterpret_cast<uint16_t*>(ws + p.probs);
@@ -423,7 +435,7 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
     const int blocks = work.p[0].k_blocks;
     work.seg = static_cast<int>(tiles_of(blocks, tiles_of(blocks, 16)));
     work.status = &hdr->status;
-    work.early = !a->targets && !en.scale && !p.pack_hidden && !p.pack_weight;  // k_soft_targets comes right before
+    work.early = !a->targets && !p.split_rows && !p.pack_hidden && !p.pack_weight;  // k_soft_targets comes right before
     const int parts = 2 * work.p[0].n_tiles;
     const int64_t v0 = kept >= 0 ? kept * p.piece : 0;
     auto logits = [&](auto epilogue) {
@@ -474,7 +486,8 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
   oa.f.dloss = a->dloss;
   oa.f.factor = a->scale * tau / up;
   oa.f.mean = a->mean;
-  oa.f.by_rows = a->dloss_rows != nullptr;
+  oa.m[0].row_power = row_power;
+  oa.m[1].by_gmax = p.split_rows;
   auto copy_map = [](H::Out::Matrix& o) {
     o.by_copy = o.type != IWP_F32 && o.wide && !o.add;
     return !o.by_copy || make_map(&o.map, o.out, o.rows, o.cols, o.ld, 32, o.type);
@@ -555,14 +568,14 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
       o.wide = aligned(o.out, 16) && o.ld * size % 16 == 0;
       o.add = a->accumulate;
       if (!copy_map(o)) return IWP_ERR_CUDA;
-      if (!make_problem(&work.p[1], pm, false, h, false, a->dtype, tile_n, 1)) return IWP_ERR_CUDA;
+      if (!make_problem(&work.p[1], pm, false, h_dw, false, a->dtype, tile_n, 1)) return IWP_ERR_CUDA;
     }
     if (int e = launch_product<H::Out, 2>(work, oa, st)) return e;
   }
   if (a->dhidden && (p.pieces > 1 || splits > 1)) {
     const int size = a->dhidden_type == IWP_F32 ? 4 : 2;
     const int wide = aligned(a->dhidden, 16) && a->dhidden_ld * size % 16 == 0;
-    LOSS_CUDA(launch(H::k_join, T < 16 * sms ? T : 16 * sms, 256, 0, 1, st, oa.f, reinterpret_cast<const float*>(ws + p.join), splits, T,
+    LOSS_CUDA(launch(H::k_join, T < 16 * sms ? T : 16 * sms, 256, 0, 1, st, oa.f, row_power, reinterpret_cast<const float*>(ws + p.join), splits, T,
                      static_cast<int>(D), a->dhidden, a->dhidden_ld, a->dhidden_type, a->accumulate, wide));
   }
   return IWP_OK;

@@ -118,3 +118,77 @@ def test_confident_rows_of_a_distillation():
     plan = losses.HeadLoss(T, n, n, BF, top_k=1)
     r = plan.distill(h, w, y[:, None], torch.zeros(T, 1, device=DEV), tau)
     assert not r.rows.any() and r.loss == 0 and (r.lse == 150.0).all()
+
+
+def spread_rows(T, dtype, seed, hard=True, V=64, D=64):
+    h, w, g = identity_head(T, V, D, dtype, seed)
+    y = torch.randint(0, V, (T,), generator=g, device=DEV)
+    sign = torch.randint(0, 2, (T,), generator=g, device=DEV) * 2 - 1
+    up = sign * 10.0 ** (-9.0 * torch.arange(T, device=DEV) / max(1, T - 1))
+    return h, w, y, up.float()[torch.randperm(T, generator=g, device=DEV)].contiguous(), g
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("T,V,piece", [(48, 64, 0), (300, 900, 0), (300, 900, 1), (7, 64, 0)])
+def test_upstream_gradients_of_very_different_sizes(T, V, piece, dtype):
+    """A row's gradient to the hidden states depends on its own upstream gradient alone, and is as precise whatever the
+    others' are; the head's gradient is as precise as its largest rows allow."""
+    D = 64
+    h, w, y, up, g = spread_rows(T, dtype, 740 + T, V=V, D=D)
+    z = torch.cat([h.double(), torch.zeros(T, V - D, dtype=torch.float64, device=DEV)], 1)
+    p = torch.softmax(z, 1)
+    hot = torch.nn.functional.one_hot(y, V).bool()
+    f_err = factor_error(p, hot.double(), dtype, hot)
+    f, up64 = p - hot.double(), up.double()[:, None]
+    plan = losses.HeadLoss(T, V, D, dtype, piece_bytes=piece)
+    lse = plan.cross_entropy(h, w, y).lse
+    for saved in (None, lse):
+        dh, dw = torch.empty(T, D, device=DEV), torch.empty(V, D, device=DEV)
+        plan.cross_entropy_grad(h, w, y, reduction="sum", lse=saved, dloss=up, dhidden=dh, dweight=dw)
+        want = up64 * f
+        within(dh, want[:, :D], (up64.abs() * f_err)[:, :D] + 2.0**-22 * want[:, :D].abs() + 1e-37, "dhidden")
+        H = h.double()
+        # the rows' scales may be carried by a copy of the hidden states in their type, relative to the largest scale
+        # (a power of two up to twice it): steps of 2^-24 in fp16
+        copy = 2.0 * up64.abs().max() * 2.0**-24 * f.abs().T @ torch.ones_like(H) if dtype == HF else 0.0
+        tol = (up64.abs() * f_err).T @ H.abs() + copy + (T / 16 + 8) * 2.0**-22 * (want.abs().T @ H.abs())
+        within(dw, want.T @ H, tol + 1e-37, "dweight")
+    assert plan.status() == 0
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("T,V,D,piece", [(40, 8192, 512, 0), (200, 3001, 72, 0), (200, 3001, 33, 1), (1021, 5000, 136, 0)])
+def test_upstream_gradients_that_are_powers_of_two_scale_rows_exactly(T, V, D, piece, dtype):
+    g = gen(760 + T)
+    h = torch.randn(T, D, generator=g, device=DEV).to(dtype)
+    w = (torch.randn(V, D, generator=g, device=DEV) / math.sqrt(D)).to(dtype)
+    y = torch.randint(0, V, (T,), generator=g, device=DEV)
+    up = 2.0 ** torch.randint(-12, 13, (T,), generator=g, device=DEV).float() * (torch.randint(0, 2, (T,), generator=g, device=DEV) * 2 - 1)
+    up[3] = 0
+    plan = losses.HeadLoss(T, V, D, dtype, piece_bytes=piece)
+    for out in (F32, dtype):
+        base, got = (torch.zeros(T, D, dtype=out, device=DEV) for _ in range(2))
+        plan.cross_entropy_grad(h, w, y, reduction="sum", dloss=torch.ones(T, device=DEV), dhidden=base, accumulate=True, want=("hidden",))
+        plan.cross_entropy_grad(h, w, y, reduction="sum", dloss=up, dhidden=got, accumulate=True, want=("hidden",))
+        if out == F32:
+            # (fp16 factors that are below the normal numbers may round differently: half a step of 2^-24 / 2^13 per column)
+            slack = 2.0**-37 * w.double().abs().sum(0) if dtype == HF else 0.0
+            assert ((got.double() - base.double() * up.double()[:, None]).abs() <= slack * up.double().abs()[:, None]).all()
+        assert not got[3].any()
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_upstream_gradients_that_are_not_finite_stay_in_their_rows(dtype):
+    T = 48
+    h, w, y, up, _ = spread_rows(T, dtype, 780)
+    plan = losses.HeadLoss(T, 64, 64, dtype)
+    fine = plan.cross_entropy_grad(h, w, y, reduction="sum", dloss=up, want=("hidden",)).dhidden
+    for bad in (math.inf, -math.inf, math.nan):
+        off = up.clone()
+        off[5] = bad
+        got = plan.cross_entropy_grad(h, w, y, reduction="sum", dloss=off, want=("hidden",)).dhidden
+        rest = torch.arange(T, device=DEV) != 5
+        assert torch.equal(got[rest], fine[rest]) and not torch.isfinite(got[5]).any()
+    y[5] = -100  # a row without a target gives nothing, whatever its upstream gradient is
+    got = plan.cross_entropy_grad(h, w, y, reduction="sum", dloss=off)
+    assert not got.dhidden[5].any() and torch.equal(got.dhidden[rest], fine[rest]) and torch.isfinite(got.dweight).all()
