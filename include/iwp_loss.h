@@ -53,7 +53,7 @@ int iwp_loss_status(const void* workspace, int32_t* status_host, void* cuda_stre
  * operands and dloss_rows, dweight sums over hidden states multiplied by powers of two of at most 1 and rounded to fp16.
  */
 typedef struct iwp_head_args {
-  int64_t tokens, vocab, dim;      /* T >= 0, 1 <= V, 1 <= D; each below 2^31 - 1024, their products
+  int64_t tokens, vocab, dim;      /* T >= 0, 1 <= V, 1 <= D; each at most 2^31 - 2^16, their products
                                       at most 2^46 */
   const void* hidden;              /* [T][D], row stride hidden_ld elements */
   int64_t hidden_ld;

@@ -18,11 +18,15 @@ namespace {
     }                              \
   } while (0)
 
-constexpr int64_t MAX_SIZE = 0x7FFFFFFF - 1023;  // tiles may reach beyond it without leaving 32 bits
+constexpr int64_t ROOM = 0xFFFF;                 // how far 32-bit positions may run beyond a size
+constexpr int64_t MAX_SIZE = 0x7FFFFFFF - ROOM;  // of tokens, vocabulary, width and strides
 constexpr int64_t MAX_ELEMENTS = int64_t(1) << 46;
 constexpr int64_t LEAST_PIECE = int64_t(1) << 30;
 constexpr int FEW_TILES = 296;           // four per CTA pair: above this a product takes its widest tiles
 constexpr int FEW_BLOCKS = 296;           // of the pass over a few tokens: two per SM
+static_assert(2 * iwp_tc::TILE_N <= ROOM && iwp_head::FACTOR_COLUMNS + iwp_tc::TILE_N <= ROOM &&
+                  FEW_BLOCKS * (iwp_head::FEW_THREADS / 32) * iwp_head::FEW_ROWS + iwp_tc::TILE_N <= ROOM,
+              "positions of the kernels' last steps stay within 32 bits");
 constexpr int64_t FEW_ELEMENTS = 32768;   // of hidden states, which stay in 64 KB of shared memory
 constexpr int64_t JOIN_TILES = 2 * 148;  // a split dhidden has at most this many partial tiles
 
