@@ -5,9 +5,10 @@
  *
  * Conventions as in iwp.h: int status, nothing throws or aborts, pointers are DEVICE pointers unless named *_host,
  * the caller owns every buffer.  No call here allocates, synchronises or keeps anything between calls; all scratch is
- * the caller's `workspace` (one per stream: calls that share a workspace must not overlap on the GPU), whose first
- * word is a status word that kernels set and iwp_loss_status() reads.  A new workspace is made ready by
- * iwp_loss_reset() once.
+ * the caller's `workspace` (one per stream: calls that share a workspace must not overlap on the GPU).  What outlives a
+ * call is in the IWP_LOSS_STATE bytes of `state`, or of the workspace's beginning if `state` is NULL: a status word
+ * that kernels set and iwp_loss_status() reads, and counters.  They are made ready by iwp_loss_reset() once; the rest of
+ * a workspace needs no preparation, so with a `state` of its own a workspace may be exchanged for another at any time.
  */
 #ifndef IWP_LOSS_H_
 #define IWP_LOSS_H_
@@ -21,14 +22,15 @@ extern "C" {
 #endif
 
 enum { IWP_F32 = 0, IWP_BF16 = 1, IWP_F16 = 2 }; /* element types */
+enum { IWP_LOSS_STATE = 256 };
 
-/* Zeroes the status word of a workspace, in stream order.  Errors: IWP_ERR_INVALID (NULL), IWP_ERR_CUDA. */
-int iwp_loss_reset(void* workspace, void* cuda_stream);
+/* Zeroes a state (or the one at a workspace's beginning), in stream order.  Errors: IWP_ERR_INVALID (NULL), IWP_ERR_CUDA. */
+int iwp_loss_reset(void* state, void* cuda_stream);
 
-/* Copies a workspace's status word to *status_host behind everything enqueued on cuda_stream and waits for that
+/* Copies a state's (or a workspace's) status word to *status_host behind everything enqueued on cuda_stream and waits for that
  * stream: IWP_OK; IWP_ERR_INVALID (a target or teacher id at or above the vocabulary was met); IWP_ERR_TIMEOUT (a
  * bounded device-side wait gave up; results are undefined).  Errors: IWP_ERR_INVALID (NULL), IWP_ERR_CUDA. */
-int iwp_loss_status(const void* workspace, int32_t* status_host, void* cuda_stream);
+int iwp_loss_status(const void* state, int32_t* status_host, void* cuda_stream);
 
 /* ---- output head with its loss ---------------------------------------------------------------------
  *
@@ -76,6 +78,7 @@ typedef struct iwp_head_args {
   int64_t dweight_ld;
   void* workspace;                 /* 256-byte aligned */
   int64_t workspace_bytes;
+  void* state;                     /* IWP_LOSS_STATE bytes, 256-byte aligned, or NULL: the workspace's first */
   int64_t piece_bytes;             /* bound on the probabilities of one piece of the vocabulary; 0 = 1 GiB, or what the
                                       weights and their gradient take (4 V D bytes) where that is more */
   float temperature, scale;
@@ -121,6 +124,7 @@ typedef struct iwp_balance_args {
   int64_t dlogits_ld;
   void* workspace;                 /* 256-byte aligned */
   int64_t workspace_bytes;
+  void* state;                     /* as in iwp_head_args */
   float coef, scale;
   int32_t experts, top_k;          /* 1 <= E <= 1024, 1 <= top_k <= E */
   int32_t type, ids_bytes;

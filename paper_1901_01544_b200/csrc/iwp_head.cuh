@@ -36,7 +36,7 @@ constexpr int MAX_TOP = 1024;
 constexpr int NO_COLUMN = 0x7FFFFFFF;
 constexpr float LOG2E = 1.4426950408889634f;
 
-// First bytes of a workspace.  The tickets wrap to zero with the last block of each launch.
+// State that outlives a call (and what the kernels of one pass to each other beside it).  The tickets wrap to zero with the last block of each launch.
 struct Header {
   int status;
   int n_rows;       // rows with targets

@@ -264,7 +264,7 @@ HeadPlan head_plan(const iwp_head_args* a) {
   p.pack_hidden = needs_copy(a->hidden, a->hidden_ld);
   p.pack_weight = needs_copy(a->weight, a->weight_ld);
   p.few = !p.grad && T <= iwp_head::FEW_TOKENS && T * up_to(D, 8) <= FEW_ELEMENTS && (D % 8 == 0 || (p.pack_hidden && p.pack_weight));
-  int64_t at = 256;
+  int64_t at = IWP_LOSS_STATE;
   auto take = [&at](int64_t n) {
     const int64_t o = at;
     at += up_to(n, 256);
@@ -318,7 +318,7 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
   namespace H = iwp_head;
   const int64_t T = a->tokens, V = a->vocab, D = a->dim;
   char* const ws = static_cast<char*>(a->workspace);
-  auto* hdr = reinterpret_cast<H::Header*>(ws);
+  auto* hdr = static_cast<H::Header*>(a->state ? a->state : a->workspace);
   const int pairs = pairs_of<H::Logits<H::NO_CODES>, 1>();
   const int out_pairs = pairs_of<H::Out, 2>();  // the deal of the gradients counts on this grid
   if (pairs < 1 || out_pairs < 1 || pairs_of<H::Logits<H::HALF_CODES>, 1>() < 1 || pairs_of<H::Logits<H::LOG_CODES>, 1>() < 1 || pairs_of<H::Probs, 1>() < 1) {
@@ -677,16 +677,16 @@ int balance_type(const iwp_balance::Args& a, cudaStream_t st) {
 
 }  // namespace
 
-extern "C" int iwp_loss_reset(void* workspace, void* cuda_stream) {
-  if (!workspace) return IWP_ERR_INVALID;
-  LOSS_CUDA(cudaMemsetAsync(workspace, 0, 256, static_cast<cudaStream_t>(cuda_stream)));
+extern "C" int iwp_loss_reset(void* state, void* cuda_stream) {
+  if (!state) return IWP_ERR_INVALID;
+  LOSS_CUDA(cudaMemsetAsync(state, 0, IWP_LOSS_STATE, static_cast<cudaStream_t>(cuda_stream)));
   return IWP_OK;
 }
 
-extern "C" int iwp_loss_status(const void* workspace, int32_t* status_host, void* cuda_stream) {
-  if (!workspace || !status_host) return IWP_ERR_INVALID;
+extern "C" int iwp_loss_status(const void* state, int32_t* status_host, void* cuda_stream) {
+  if (!state || !status_host) return IWP_ERR_INVALID;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  LOSS_CUDA(cudaMemcpyAsync(status_host, workspace, sizeof(int32_t), cudaMemcpyDeviceToHost, st));
+  LOSS_CUDA(cudaMemcpyAsync(status_host, state, sizeof(int32_t), cudaMemcpyDeviceToHost, st));
   LOSS_CUDA(cudaStreamSynchronize(st));
   return IWP_OK;
 }
@@ -698,7 +698,7 @@ extern "C" int64_t iwp_head_workspace(const iwp_head_args* a) {
 
 extern "C" int iwp_head_loss(const iwp_head_args* a, void* cuda_stream) {
   if (!head_args_ok(a)) return IWP_ERR_INVALID;
-  if (!a->hidden || !a->weight || !a->lse || !a->workspace || !aligned(a->workspace, 256)) return IWP_ERR_INVALID;
+  if (!a->hidden || !a->weight || !a->lse || !a->workspace || !aligned(a->workspace, 256) || !aligned(a->state, 256)) return IWP_ERR_INVALID;
   if (!aligned(a->hidden, 2) || !aligned(a->weight, 2)) return IWP_ERR_INVALID;
   if (a->dhidden && !aligned(a->dhidden, a->dhidden_type == IWP_F32 ? 4 : 2)) return IWP_ERR_INVALID;
   if (a->dweight && !aligned(a->dweight, a->dweight_type == IWP_F32 ? 4 : 2)) return IWP_ERR_INVALID;
@@ -721,13 +721,13 @@ extern "C" int iwp_head_loss(const iwp_head_args* a, void* cuda_stream) {
 
 extern "C" int64_t iwp_balance_workspace(const iwp_balance_args* a) {
   if (!balance_args_ok(a)) return -1;
-  return 256 + balance_part_counts_bytes(a->experts) + up_to(int64_t(BALANCE_BLOCKS) * iwp_balance::padded(a->experts) * 4, 256);
+  return IWP_LOSS_STATE + balance_part_counts_bytes(a->experts) + up_to(int64_t(BALANCE_BLOCKS) * iwp_balance::padded(a->experts) * 4, 256);
 }
 
 extern "C" int iwp_balance_loss(const iwp_balance_args* a, void* cuda_stream) {
   if (!balance_args_ok(a)) return IWP_ERR_INVALID;
   const int size = a->type == IWP_F32 ? 4 : 2;
-  if (!a->logits || !a->ids || !a->counts || !a->workspace || !aligned(a->workspace, 256)) return IWP_ERR_INVALID;
+  if (!a->logits || !a->ids || !a->counts || !a->workspace || !aligned(a->workspace, 256) || !aligned(a->state, 256)) return IWP_ERR_INVALID;
   if (a->logits_ld < a->experts || a->ids_ld < a->top_k || (a->ids_bytes != 4 && a->ids_bytes != 8)) return IWP_ERR_INVALID;
   if (a->dlogits && a->dlogits_ld < a->experts) return IWP_ERR_INVALID;
   if (!aligned(a->logits, size) || (a->dlogits && !aligned(a->dlogits, size)) || !aligned(a->ids, a->ids_bytes)) return IWP_ERR_INVALID;
@@ -737,15 +737,15 @@ extern "C" int iwp_balance_loss(const iwp_balance_args* a, void* cuda_stream) {
   if (a->workspace_bytes < iwp_balance_workspace(a)) return IWP_ERR_CAPACITY;
   char* const ws = static_cast<char*>(a->workspace);
   iwp_balance::Args r{};
-  r.hdr = reinterpret_cast<iwp_balance::Header*>(ws);
+  r.hdr = static_cast<iwp_balance::Header*>(a->state ? a->state : a->workspace);
   r.counts = a->counts;
   r.logits = a->logits;
   r.ids = a->ids;
   r.mask = a->mask;
   r.dloss = a->dloss;
   r.dlogits = a->dlogits;
-  r.part_counts = reinterpret_cast<int*>(ws + 256);
-  r.part = reinterpret_cast<float*>(ws + 256 + balance_part_counts_bytes(a->experts));
+  r.part_counts = reinterpret_cast<int*>(ws + IWP_LOSS_STATE);
+  r.part = reinterpret_cast<float*>(ws + IWP_LOSS_STATE + balance_part_counts_bytes(a->experts));
   r.loss = a->loss;
   r.mean_prob = a->mean_prob;
   r.logits_ld = a->logits_ld;

@@ -6,6 +6,9 @@ current stream, torch supplies device memory, there is no CPU fallback, and erro
 `TypeError` / `ValueError` (tensors that do not fit the call).  A plan (`HeadLoss`, `ExpertBalance`) owns the
 workspace of its calls; like a `Pruner` it serves one stream and one thread at a time.  `check()` reads the status
 word that kernels set, e.g. after a target outside the vocabulary.
+
+Calls may be captured in a CUDA graph (a plan is made before the capture, and kept as long as the graph, which works in
+its workspace): from its first capture on, a plan keeps every workspace that it outgrows, for the graphs' sake.
 """
 from __future__ import annotations
 
@@ -15,6 +18,7 @@ from . import binding
 from .binding import IWP_ERR_CAPACITY, IWP_ERR_INVALID, IwpError, _check
 
 IWP_F32, IWP_BF16, IWP_F16 = 0, 1, 2
+LOSS_STATE = 256
 EXPORTS = ["iwp_loss_reset", "iwp_loss_status", "iwp_head_workspace", "iwp_head_loss", "iwp_balance_workspace", "iwp_balance_loss"]
 
 _vp, _i64, _i32, _f32 = C.c_void_p, C.c_int64, C.c_int32, C.c_float
@@ -25,7 +29,7 @@ class HeadArgs(C.Structure):
         ("tokens", _i64), ("vocab", _i64), ("dim", _i64), ("hidden", _vp), ("hidden_ld", _i64), ("weight", _vp), ("weight_ld", _i64),
         ("targets", _vp), ("ignore_index", _i64), ("top_ids", _vp), ("top_ids_ld", _i64), ("top_logits", _vp), ("top_logits_ld", _i64),
         ("loss", _vp), ("rows", _vp), ("lse", _vp), ("dloss", _vp), ("dloss_rows", _vp), ("dhidden", _vp), ("dhidden_ld", _i64),
-        ("dweight", _vp), ("dweight_ld", _i64), ("workspace", _vp), ("workspace_bytes", _i64), ("piece_bytes", _i64),
+        ("dweight", _vp), ("dweight_ld", _i64), ("workspace", _vp), ("workspace_bytes", _i64), ("state", _vp), ("piece_bytes", _i64),
         ("temperature", _f32), ("scale", _f32), ("dtype", _i32), ("top_k", _i32), ("ids_bytes", _i32), ("top_type", _i32),
         ("dhidden_type", _i32), ("dweight_type", _i32), ("mean", _i32), ("accumulate", _i32), ("have_lse", _i32),
     ]
@@ -35,6 +39,7 @@ class BalanceArgs(C.Structure):
     _fields_ = [
         ("tokens", _i64), ("logits", _vp), ("logits_ld", _i64), ("ids", _vp), ("ids_ld", _i64), ("mask", _vp), ("dloss", _vp), ("loss", _vp),
         ("counts", _vp), ("mean_prob", _vp), ("dlogits", _vp), ("dlogits_ld", _i64), ("workspace", _vp), ("workspace_bytes", _i64),
+        ("state", _vp),
         ("coef", _f32), ("scale", _f32), ("experts", _i32), ("top_k", _i32), ("type", _i32), ("ids_bytes", _i32),
     ]
 
@@ -140,14 +145,36 @@ class _Plan:
         self._torch = torch
         self.device = torch.device("cuda", torch.cuda.current_device())
         self._lib = lib()
+        self._capturing = torch._C._cuda_isCurrentStreamCapturing
+        if self._capturing():
+            raise RuntimeError(f"make the {type(self).__name__} before the capture: its state is zeroed once, not by every replay")
         self._ws, self._ws_at, self._ws_bytes = None, None, 0  # made by the first call
         self._planned = 0
+        self._captured, self._outgrown = False, []
         self._floats = tuple(self._codes)
         self._ids = (torch.int64, torch.int32)
         self._raw_stream = torch._C._cuda_getCurrentRawStream  # current_stream() without the object around it
+        self._state = torch.empty(LOSS_STATE, dtype=torch.uint8, device=self.device)
+        self._state_at, self._last = self._state.data_ptr(), self._raw_stream(self.device.index)
+        _check(self._lib.iwp_loss_reset(self._state_at, self._last), "iwp_loss_reset")
+        self._made = torch.cuda.Event()
+        self._made.record()
 
     def _stream(self) -> int:
-        return self._raw_stream(self.device.index)
+        """The stream of this call."""
+        s = self._raw_stream(self.device.index)
+        if self._capturing():
+            self._captured = True
+        elif s != self._last:
+            # another stream than last time: behind the state's zeroing, and no memory of the plan's goes back to the
+            # allocator before that stream is done with it
+            now = self._torch.cuda.current_stream(self.device)
+            now.wait_event(self._made)
+            for x in (self._state, self._ws):
+                if x is not None:
+                    x.record_stream(now)
+            self._last = s
+        return s
 
     def _plan(self, need: int) -> None:
         if need < 0:
@@ -161,24 +188,20 @@ class _Plan:
         if self._ws_bytes < need:
             old, self._ws = self._ws, self._torch.empty(need, dtype=self._torch.uint8, device=self.device)
             self._ws_at, self._ws_bytes = self._ws.data_ptr(), need
-            _check(lib().iwp_loss_reset(self._ws_at, self._stream()), "iwp_loss_reset")
-            if old is not None:
-                self._ws[:4].copy_(old[:4])  # a set status word outlives a larger workspace
+            if self._captured and old is not None:
+                self._outgrown.append(old)
 
     def status(self) -> int:
         """The status word, after everything enqueued on the current stream."""
-        if self._ws is None:
-            return 0
         v = C.c_int32()
-        _check(lib().iwp_loss_status(self._ws.data_ptr(), C.byref(v), self._stream()), "iwp_loss_status")
+        _check(lib().iwp_loss_status(self._state_at, C.byref(v), self._stream()), "iwp_loss_status")
         return int(v.value)
 
     def check(self) -> None:
         _check(self.status(), type(self).__name__)
 
     def reset(self) -> None:
-        if self._ws is not None:
-            _check(lib().iwp_loss_reset(self._ws.data_ptr(), self._stream()), "iwp_loss_reset")
+        _check(lib().iwp_loss_reset(self._state_at, self._stream()), "iwp_loss_reset")
 
 
 class HeadLoss(_Plan):
@@ -261,15 +284,15 @@ class HeadLoss(_Plan):
                 a.top_ids, a.top_logits = a.top_ids or 256, a.top_logits or 256
             else:
                 a.targets = a.targets or 256
-        ref = C.byref(a)
+        ref, stream = C.byref(a), self._stream()
         if self._ws_at is None:
             self._grow(self._lib.iwp_head_workspace(ref))
-        a.workspace, a.workspace_bytes = self._ws_at, self._ws_bytes
-        status = self._lib.iwp_head_loss(ref, self._raw_stream(dev.index))
+        a.workspace, a.workspace_bytes, a.state = self._ws_at, self._ws_bytes, self._state_at
+        status = self._lib.iwp_head_loss(ref, stream)
         if status == IWP_ERR_CAPACITY:  # more tokens, or rows that have to be copied, for the first time
             self._grow(self._lib.iwp_head_workspace(ref))
             a.workspace, a.workspace_bytes = self._ws_at, self._ws_bytes
-            status = self._lib.iwp_head_loss(ref, self._raw_stream(dev.index))
+            status = self._lib.iwp_head_loss(ref, stream)
         if status:
             raise IwpError(status, "iwp_head_loss")
         return r
@@ -361,10 +384,11 @@ class ExpertBalance(_Plan):
             a.dlogits = None
         if T == 0:
             a.logits, a.ids = a.logits or 256, a.ids or 256
+        stream = self._stream()
         if self._ws_at is None:
             self._grow(0)
-            a.workspace, a.workspace_bytes = self._ws_at, self._ws_bytes
-        status = self._lib.iwp_balance_loss(self._args_at, self._raw_stream(dev.index))
+            a.workspace, a.workspace_bytes, a.state = self._ws_at, self._ws_bytes, self._state_at
+        status = self._lib.iwp_balance_loss(self._args_at, stream)
         if status:
             raise IwpError(status, "iwp_balance_loss")
         return BalanceResult(out, counts, dlogits)
