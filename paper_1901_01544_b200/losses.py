@@ -402,7 +402,7 @@ class ExpertBalance(_Plan):
         return self._run(logits, ids, mask, coef, dloss, scale, True, dlogits)
 
 
-# ---- differentiable forms ----------------------------------------------------------------------
+# ---- differentiable forms (once: a second derivative is refused) --------------------------------------
 
 
 def _functions():
@@ -411,34 +411,53 @@ def _functions():
     if _autograd is None:
         import torch
 
+        class Once(torch.autograd.Function):
+            """make(): gradients that depend on `inputs`.  Under create_graph a derivative of them is asked for only if
+            they are differentiated again, and is refused then (they would pass for constants otherwise)."""
+
+            @staticmethod
+            def forward(ctx, make, *inputs):
+                return make()
+
+            @staticmethod
+            def backward(ctx, *_):
+                raise RuntimeError("the losses' gradients cannot be differentiated again")
+
         class Head(torch.autograd.Function):
             @staticmethod
             def forward(ctx, hidden, weight, plan, kind, args, kwargs):
                 r = getattr(plan, kind)(hidden, weight, *args, **kwargs)
-                ctx.plan, ctx.kind, ctx.args, ctx.kwargs = plan, kind, args, kwargs
-                ctx.save_for_backward(hidden, weight, r.lse)
+                tensors = [a for a in args if isinstance(a, torch.Tensor)]  # they come first
+                ctx.plan, ctx.kind, ctx.rest, ctx.kwargs = plan, kind, args[len(tensors) :], kwargs
+                ctx.save_for_backward(hidden, weight, r.lse, *tensors)
                 return r.loss.clone()
 
             @staticmethod
             def backward(ctx, dloss):
-                hidden, weight, lse = ctx.saved_tensors
+                hidden, weight, lse, *tensors = ctx.saved_tensors
                 want = tuple(n for n, need in zip(("hidden", "weight"), ctx.needs_input_grad) if need)
-                r = getattr(ctx.plan, ctx.kind + "_grad")(hidden, weight, *ctx.args, lse=lse, dloss=dloss.float(), want=want, **ctx.kwargs)
-                return r.dhidden, r.dweight, None, None, None, None
+                grad = getattr(ctx.plan, ctx.kind + "_grad")
+
+                def make():
+                    r = grad(hidden, weight, *tensors, *ctx.rest, lse=lse, dloss=dloss.float(), want=want, **ctx.kwargs)
+                    return r.dhidden, r.dweight
+
+                return *Once.apply(make, hidden, weight, dloss), None, None, None, None
 
         class Balance(torch.autograd.Function):
             @staticmethod
             def forward(ctx, logits, plan, ids, mask, coef):
-                ctx.plan, ctx.mask, ctx.coef = plan, mask, coef
-                ctx.save_for_backward(logits, ids)
+                ctx.plan, ctx.coef = plan, coef
+                ctx.save_for_backward(logits, ids, mask)
                 r = plan.loss(logits, ids, mask, coef=coef)
                 ctx.mark_non_differentiable(r.counts)
                 return r.loss.clone(), r.counts
 
             @staticmethod
             def backward(ctx, dloss, _):
-                logits, ids = ctx.saved_tensors
-                return ctx.plan.grad(logits, ids, ctx.mask, coef=ctx.coef, dloss=dloss.float()).dlogits, None, None, None, None
+                logits, ids, mask = ctx.saved_tensors
+                make = lambda: ctx.plan.grad(logits, ids, mask, coef=ctx.coef, dloss=dloss.float()).dlogits  # noqa: E731
+                return Once.apply(make, logits, dloss), None, None, None, None
 
         _autograd = (Head, Balance)
     return _autograd
