@@ -155,17 +155,16 @@ class _Plan:
         self._ids = (torch.int64, torch.int32)
         self._raw_stream = torch._C._cuda_getCurrentRawStream  # current_stream() without the object around it
         self._state = torch.empty(LOSS_STATE, dtype=torch.uint8, device=self.device)
-        self._state_at, self._last = self._state.data_ptr(), self._raw_stream(self.device.index)
+        self._index = self.device.index
+        self._state_at, self._last = self._state.data_ptr(), self._raw_stream(self._index)
         _check(self._lib.iwp_loss_reset(self._state_at, self._last), "iwp_loss_reset")
         self._made = torch.cuda.Event()
         self._made.record()
 
     def _stream(self) -> int:
         """The stream of this call."""
-        s = self._raw_stream(self.device.index)
-        if self._capturing():
-            self._captured = True
-        elif s != self._last:
+        s = self._raw_stream(self._index)
+        if s != self._last and not self._capturing():
             # another stream than last time: behind the state's zeroing, and no memory of the plan's goes back to the
             # allocator before that stream is done with it
             now = self._torch.cuda.current_stream(self.device)
@@ -285,6 +284,8 @@ class HeadLoss(_Plan):
             else:
                 a.targets = a.targets or 256
         ref, stream = C.byref(a), self._stream()
+        if self._capturing():
+            self._captured = True
         if self._ws_at is None:
             self._grow(self._lib.iwp_head_workspace(ref))
         a.workspace, a.workspace_bytes, a.state = self._ws_at, self._ws_bytes, self._state_at
