@@ -27,9 +27,9 @@ enum { IWP_LOSS_STATE = 256 };
 /* Zeroes a state (or the one at a workspace's beginning), in stream order.  Errors: IWP_ERR_INVALID (NULL), IWP_ERR_CUDA. */
 int iwp_loss_reset(void* state, void* cuda_stream);
 
-/* Copies a state's (or a workspace's) status word to *status_host behind everything enqueued on cuda_stream and waits for that
- * stream: IWP_OK; IWP_ERR_INVALID (a target or teacher id at or above the vocabulary was met); IWP_ERR_TIMEOUT (a
- * bounded device-side wait gave up; results are undefined).  Errors: IWP_ERR_INVALID (NULL), IWP_ERR_CUDA. */
+/* Copies a state's (or a workspace's) status word to *status_host behind everything enqueued on cuda_stream and waits
+ * for that stream: IWP_OK; IWP_ERR_INVALID (a target or teacher id outside the vocabulary was met); IWP_ERR_TIMEOUT
+ * (a bounded device-side wait gave up; results are undefined).  Errors: IWP_ERR_INVALID (NULL), IWP_ERR_CUDA. */
 int iwp_loss_status(const void* state, int32_t* status_host, void* cuda_stream);
 
 /* ---- output head with its loss ---------------------------------------------------------------------
@@ -46,7 +46,8 @@ int iwp_loss_status(const void* state, int32_t* status_host, void* cuda_stream);
  * (targets == NULL): q = softmax over the row's top_k teacher logits / tau; an id below 0 is padding and takes no
  * part, a logit of -inf has q = 0; nothing but those: no target.  A target or id at or above vocab (or a negative
  * target that is not ignore_index) sets the status word to IWP_ERR_INVALID, makes the row's loss NaN and gives no
- * gradient.  Products are of the operands' 16-bit type with fp32 accumulation; statistics and losses are fp32.
+ * gradient; the row still counts as one with a target.
+ * Products are of the operands' 16-bit type with fp32 accumulation; statistics and losses are fp32.
  * The gradient's factors exp(..) - q are rounded to the operands' type, as the tensor cores take no wider one.  Where
  * nothing is subtracted, exp(..) may have been held in a 16-bit code before: off by at most 2^-12 of itself (bf16
  * operands) or 1.7e-4 (fp16), and nothing below 2^-40 (2^-24) of the largest of the row's 32 to 128 columns around it.

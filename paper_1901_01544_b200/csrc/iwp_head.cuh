@@ -559,13 +559,20 @@ __global__ void __launch_bounds__(256) k_scaled_rows(const Header* hdr, const fl
   }
 }
 
-// Number of rows with targets, for backward passes on their own (k_rows counts them otherwise).
+// Number of rows with targets, and whether one is outside the vocabulary, for backward passes on their own (k_rows sees to
+// both otherwise).
 __global__ void __launch_bounds__(1024) k_count_rows(Header* hdr, Targets en, int64_t T) {
   __shared__ int sh[32];
   iwp_tc::launch_next();
   iwp_tc::wait_previous();
   int n = 0;
-  for (int64_t t = threadIdx.x; t < T; t += blockDim.x) n += en.state(t) != 0;
+  bool bad = false;
+  for (int64_t t = threadIdx.x; t < T; t += blockDim.x) {
+    const int state = en.state(t);
+    n += state != 0;
+    bad |= state < 0;
+  }
+  if (bad) atomicExch(&hdr->status, IWP_ERR_INVALID);
   n = __reduce_add_sync(0xFFFFFFFFu, n);
   if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = n;
   __syncthreads();

@@ -192,3 +192,18 @@ def test_upstream_gradients_that_are_not_finite_stay_in_their_rows(dtype):
     y[5] = -100  # a row without a target gives nothing, whatever its upstream gradient is
     got = plan.cross_entropy_grad(h, w, y, reduction="sum", dloss=off)
     assert not got.dhidden[5].any() and torch.equal(got.dhidden[rest], fine[rest]) and torch.isfinite(got.dweight).all()
+
+
+def test_an_invalid_target_is_reported_by_a_backward_pass_of_its_own():
+    T, V, D = 40, 64, 64
+    h, w, g = identity_head(T, V, D, BF, 810)
+    y = torch.randint(0, V, (T,), generator=g, device=DEV)
+    lse = losses.HeadLoss(T, V, D, BF).cross_entropy(h, w, y).lse
+    y[3] = V
+    plan = losses.HeadLoss(T, V, D, BF)
+    r = plan.cross_entropy_grad(h, w, y, lse=lse)
+    assert plan.status() == -1 and not r.dhidden[3].any() and torch.isfinite(r.dhidden.float()).all()
+    plan = losses.HeadLoss(T, V, D, BF, top_k=2)
+    ids = torch.stack([y.clamp(max=V - 1), y], 1)
+    r = plan.distill_grad(h, w, ids, torch.zeros(T, 2, device=DEV), lse=lse)
+    assert plan.status() == -1 and not r.dhidden[3].any()
