@@ -451,7 +451,7 @@ __global__ void k_soft_targets(int* column, float* q_out, float* const_term, con
   bool bad = false, nan = false;
   for (int k = lane; k < K; k += 32) {
     const int64_t id = load_id(ids, t * ids_ld + k, ids_bytes);
-    const float x = iwp_tc::load_as_float(logits, t * logits_ld + k, type) * inv_tau;
+    const float x = iwp_tc::load_as_float(logits, t * logits_ld + k, type);
     bad |= id >= V;
     const bool used = id >= 0 && id < V && x != -CUDART_INF_F;  // NaN takes part
     col[k] = used ? static_cast<int>(id) : NO_COLUMN;
@@ -467,7 +467,7 @@ __global__ void k_soft_targets(int* column, float* q_out, float* const_term, con
   __syncwarp();
   float sum = 0.f;
   for (int k = lane; k < K; k += 32)
-    if (col[k] != NO_COLUMN) sum += expf(q[k] - top);
+    if (col[k] != NO_COLUMN) sum += expf((q[k] - top) * inv_tau);  // subtracted first: a type's lowest value, over tau, leaves it
   sum = warp_sum(sum);
   const bool has = top != -CUDART_INF_F || nan;
   const float log_sum = logf(sum);
@@ -475,7 +475,7 @@ __global__ void k_soft_targets(int* column, float* q_out, float* const_term, con
   for (int k = lane; k < K; k += 32) {
     float p = 0.f;
     if (col[k] != NO_COLUMN) {
-      const float lq = q[k] - top - log_sum;
+      const float lq = (q[k] - top) * inv_tau - log_sum;
       p = expf(lq);
       if (p != 0.f) term += p * lq;
     }

@@ -207,3 +207,29 @@ def test_an_invalid_target_is_reported_by_a_backward_pass_of_its_own():
     ids = torch.stack([y.clamp(max=V - 1), y], 1)
     r = plan.distill_grad(h, w, ids, torch.zeros(T, 2, device=DEV), lse=lse)
     assert plan.status() == -1 and not r.dhidden[3].any()
+
+
+def test_teachers_lowest_logits_at_low_temperature():
+    """The type's lowest value is a logit like any other; divided by a temperature below one it leaves the type."""
+    T, n = 40, 64
+    h, w, g = identity_head(T, n, n, BF, 800)
+    for top_type in (F32, BF, HF):
+        for tau in (0.5, 0.75, 1.0):
+            ids = torch.rand(T, n, generator=g, device=DEV).argsort(1)[:, :7].contiguous()
+            logits = torch.randn(T, 7, generator=g, device=DEV).to(top_type)
+            logits[3] = torch.finfo(top_type).min  # equal ones: a uniform teacher
+            logits[4, 1:] = torch.finfo(top_type).min
+            logits[5] = torch.finfo(top_type).max
+            logits[6, 2] = torch.finfo(top_type).max
+            q = torch.zeros(T, n, dtype=torch.float64, device=DEV).scatter_(1, ids, soft_targets(ids, logits, tau))
+            hit = torch.zeros(T, n, dtype=torch.bool, device=DEV).scatter_(1, ids, True)
+            p = torch.softmax(h.double() / tau, 1)
+            f, f_err = tau * (p - q), tau * factor_error(p, q, BF, hit)
+            plan = losses.HeadLoss(T, n, n, BF, top_k=7)
+            dh = torch.empty(T, n, device=DEV)
+            r = plan.distill_grad(h, w, ids, logits, tau, reduction="sum", dhidden=dh, want=("hidden",))
+            within(dh, f, f_err + 2.0**-23 * f.abs() + 1e-37, "dhidden")
+            z = h.double() / tau
+            entropy = torch.where(q > 0, q * torch.log(q.clamp(min=1e-300)), 0.0).sum(1)
+            rows = tau * tau * (entropy - (q * z).sum(1) + torch.logsumexp(z, 1))
+            within(r.rows, rows, tau * tau * 2.0**-16 * (40 + z.abs().amax(1)), "rows")
