@@ -210,6 +210,10 @@ bool make_problem(iwp_tc::Problem* q, const Matrix& A, bool a_kc, const Matrix& 
   return true;
 }
 
+// Tensor cores cut what a term loses against the running sum, so long sums drift: segments of at most 1024 elements of K,
+// added up in fp32 registers, keep the logits within 3e-7 of their size (1.2e-6 at K = 4096 without).
+int segment(const iwp_tc::Problem& q) { return static_cast<int>(tiles_of(q.k_blocks, tiles_of(q.k_blocks, 16))); }
+
 template <class Epi, int N>
 int pairs_of() {
   static std::atomic<int> cached[MAX_DEVICES] = {};
@@ -434,10 +438,7 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
     const int tile_n = pick_tile_n(shape, pairs);
     iwp_tc::Problems<1> work;
     if (!make_problem(&work.p[0], h, true, w, true, a->dtype, tile_n, 1)) return IWP_ERR_CUDA;
-    // Tensor cores cut what a term loses against the running sum, so long sums drift: segments of at most 1024
-    // elements of K, added up in fp32 registers, keep the logits within 3e-7 of their size (1.2e-6 at K = 4096 without).
-    const int blocks = work.p[0].k_blocks;
-    work.seg = static_cast<int>(tiles_of(blocks, tiles_of(blocks, 16)));
+    work.seg = segment(work.p[0]);
     work.status = &hdr->status;
     work.early = !a->targets && !p.split_rows && !p.pack_hidden && !p.pack_weight;  // k_soft_targets comes right before
     const int parts = 2 * work.p[0].n_tiles;
@@ -506,7 +507,7 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
       const Shape shape{T, width, D};
       iwp_tc::Problems<1> work;
       if (!make_problem(&work.p[0], h, true, wp, true, a->dtype, pick_tile_n(shape, pairs), 1)) return IWP_ERR_CUDA;
-      work.seg = 1 << 30;
+      work.seg = segment(work.p[0]);
       work.status = &hdr->status;
       work.early = 0;
       H::Probs::Args pa{};
@@ -520,6 +521,7 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
       pa.c = c;
       pa.up = up;
       pa.type = a->dtype;
+      if (!make_map(&pa.map, probs, T, p.piece, p.piece, 32, a->dtype)) return IWP_ERR_CUDA;
       if (int e = launch_product<H::Probs, 1>(work, pa, st)) return e;
     }
     // both gradients of the piece in one launch, dhidden (the longer tiles) first

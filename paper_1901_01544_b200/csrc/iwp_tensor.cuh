@@ -28,6 +28,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "../../include/iwp.h"
 
 namespace iwp_tc {
@@ -470,11 +472,9 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
       if constexpr (Epi::SUMS) {
         f2 acc[TILE_N / 4];
-#pragma unroll
-        for (int j = 0; j < TILE_N / 4; j++) acc[j] = pack(0.f, 0.f);
-        for (int k = k0; k < k1; k += w.seg) {
+        auto segment = [&](auto first) {
           ok = __all_sync(0xFFFFFFFFu, mbar_wait(acc_full + 8 * b, acc_phase, dead, w.status));
-          if (!ok) break;
+          if (!ok) return;
           fence_after();
 #pragma unroll
           for (int c = 0; c < TILE_N / 64; c++) {
@@ -482,11 +482,16 @@ __global__ void __launch_bounds__(THREADS, 1)
               float v[32];
               tmem_load32(mine + b * TILE_N + 32 * c, v);
 #pragma unroll
-              for (int j = 0; j < 16; j++) acc[16 * c + j] = add2(acc[16 * c + j], pack(v[2 * j], v[2 * j + 1]));
+              for (int j = 0; j < 16; j++) {
+                const f2 x = pack(v[2 * j], v[2 * j + 1]);
+                acc[16 * c + j] = decltype(first)::value ? x : add2(acc[16 * c + j], x);
+              }
             }
           }
           release();
-        }
+        };
+        segment(std::true_type{});
+        for (int k = k0 + w.seg; ok && k < k1; k += w.seg) segment(std::false_type{});
         if (ok) Epi::tile(args, at, now, acc);
       } else {
         ok = __all_sync(0xFFFFFFFFu, mbar_wait(acc_full + 8 * b, acc_phase, dead, w.status));

@@ -233,3 +233,25 @@ def test_teachers_lowest_logits_at_low_temperature():
             entropy = torch.where(q > 0, q * torch.log(q.clamp(min=1e-300)), 0.0).sum(1)
             rows = tau * tau * (entropy - (q * z).sum(1) + torch.logsumexp(z, 1))
             within(r.rows, rows, tau * tau * 2.0**-16 * (40 + z.abs().amax(1)), "rows")
+
+
+@pytest.mark.parametrize("saved", [False, True])
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_probabilities_see_the_logits_that_lse_saw(dtype, saved):
+    """All columns of the head are one vector, with which every row's product is a sum of 4096 terms of one sign, about 1000:
+    p = 1 / V exactly.  lse is near 1031, so p is off by less than 2^-12 of itself (three exponents below 2048 rounded by
+    half a step of 2^-13, times log 2, and lse by as much), which is less than half a step of either type (2^-9, 2^-12
+    below a power of two): columns that are nobody's target get the sum of the hidden states, times 2^-10 exactly."""
+    T, V, D = 130, 1024, 4096
+    g = gen(790)
+    row = (0.5 + torch.rand(D, generator=g, device=DEV)).to(dtype)
+    h = (0.2 + 0.1 * torch.rand(T, D, generator=g, device=DEV)).to(dtype)
+    w = row.expand(V, D).contiguous()
+    y = torch.randint(0, V, (T,), generator=g, device=DEV)
+    plan = losses.HeadLoss(T, V, D, dtype, piece_bytes=1)  # pieces of 256 columns: all but one from a second product
+    lse = plan.cross_entropy(h, w, y).lse if saved else None
+    dw = torch.empty(V, D, device=DEV)
+    plan.cross_entropy_grad(h, w, y, reduction="sum", lse=lse, dweight=dw, want=("weight",))
+    cols = torch.bincount(y, minlength=V) == 0
+    want = (2.0**-10 * h.double().sum(0)).expand(int(cols.sum()), D)
+    within(dw[cols], want, (T / 16 + 8) * 2.0**-22 * want, "dweight")
