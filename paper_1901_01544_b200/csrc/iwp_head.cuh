@@ -252,9 +252,7 @@ struct Logits {
 
 // ---- epilogue of the probability pass -----------------------------------------------------------------
 
-// Its K is added up in the segments of the logits pass: lse is the sum over the same logits, to the last bit.  Summed
-// in tensor memory alone, products of 4096 terms of one sign came out about 1e-5 lower, and with logits of 1000 every
-// probability 1 to 2 % off.
+// Its K is added up in the segments of the logits pass: lse is the sum over the same logits, to the last bit.
 struct Probs {
   static constexpr bool SUMS = true;
   static constexpr int AREAS = 2;
@@ -353,56 +351,98 @@ struct Factor {
   }
 };
 
+struct OutMatrix {
+  void* out;
+  int64_t ld, split_stride;  // elements
+  int rows, cols, type, wide, add, raw;  // raw: partial sums, the factor is applied later
+  int by_copy;                           // 16-bit rows that start at multiples of 16 bytes, nothing to add
+  int by_gmax;                           // dweight, where the hidden states carry the rows' powers of two
+  const float* row_power;                // dhidden: [rows], or NULL
+  CUtensorMap map;                       // of `out` then, in boxes of 32 rows and 64 columns
+};
+
+struct OutArgs {
+  Factor f;
+  OutMatrix m[2];
+};
+
+// LONG: for K of several segments, whose sums are in registers and leave fewer of them to the stores: 300 x 8060 x 1031 takes
+// 116 us with them and 106 without, so products of one segment do without.
+template <bool LONG>
 struct Out {
-  static constexpr bool SUMS = false;
+  static constexpr bool SUMS = LONG;
   static constexpr int AREAS = 2;
-  struct Matrix {
-    void* out;
-    int64_t ld, split_stride;  // elements
-    int rows, cols, type, wide, add, raw;  // raw: partial sums, the factor is applied later
-    int by_copy;                           // 16-bit rows that start at multiples of 16 bytes, nothing to add
-    int by_gmax;                           // dweight, where the hidden states carry the rows' powers of two
-    const float* row_power;                // dhidden: [rows], or NULL
-    CUtensorMap map;                       // of `out` then, in boxes of 32 rows and 64 columns
-  };
-  struct Args {
-    Factor f;
-    Matrix m[2];
-  };
+  using Args = OutArgs;
   static __device__ __forceinline__ float begin(const Args& args, const Where& w) {
-    const Matrix& a = args.m[w.p];
+    const OutMatrix& a = args.m[w.p];
     if (a.raw) return 1.f;
     const float f = args.f.get();
     if (a.by_gmax) return f * args.f.hdr->gmax;
     return a.row_power && w.row0 + w.lane < a.rows ? f * a.row_power[w.row0 + w.lane] : f;
   }
-  static __device__ __forceinline__ void tile(const Args& args, Where& w, float f, uint32_t tmem) {
-    const Matrix& a = args.m[w.p];
+  using Sums = std::conditional_t<LONG, f2 (&)[iwp_tc::TILE_N / 4], uint32_t>;
+  // 32 of the warp's columns, from c on, times f; in registers c is a constant
+  static __device__ __forceinline__ void take(Sums sums, int c, float f, float (&v)[32]) {
+    if constexpr (LONG) {
+#pragma unroll
+      for (int j = 0; j < 16; j++) {
+        const float2 x = unpack(mul2(sums[c / 2 + j], pack(f, f)));
+        v[2 * j] = x.x, v[2 * j + 1] = x.y;
+      }
+    } else {
+      iwp_tc::tmem_load32(sums + c, v);
+#pragma unroll
+      for (int j = 0; j < 32; j++) v[j] *= f;
+    }
+  }
+  static __device__ __forceinline__ void copy64(const OutMatrix& a, Where& w, float f, Sums sums, int c) {
+    uint32_t packed[2][16];
+#pragma unroll
+    for (int half = 0; half < 2; half++) {
+      float v[32];
+      take(sums, c + 32 * half, f, v);
+#pragma unroll
+      for (int j = 0; j < 16; j++) packed[half][j] = iwp_tc::pack2(v[2 * j], v[2 * j + 1], a.type);
+    }
+    // (the accumulator is read whole all the same: a warp's loads are collective)
+    if (w.row0 < a.rows) copy_out(&a.map, w, packed[0], packed[1], w.col0 + c);
+  }
+  static __device__ __forceinline__ void tile(const Args& args, Where& w, float f, Sums sums) {
+    const OutMatrix& a = args.m[w.p];
+    const int end = min(w.width, a.cols - w.col0);
     if (a.by_copy && w.width >= 64) {
+      if constexpr (LONG) {
+#pragma unroll
+        for (int c = 0; c < iwp_tc::TILE_N / 2; c += 64)
+          if (c < end) copy64(a, w, f, sums, c);
+      } else {
 #pragma unroll 1
-      for (int c0 = w.col0; c0 < min(w.col0 + w.width, a.cols); c0 += 64) {
-        uint32_t packed[2][16];
-#pragma unroll
-        for (int half = 0; half < 2; half++) {
-          float v[32];
-          iwp_tc::tmem_load32(tmem + (c0 - w.col0) + 32 * half, v);
-#pragma unroll
-          for (int j = 0; j < 16; j++) packed[half][j] = iwp_tc::pack2(v[2 * j] * f, v[2 * j + 1] * f, a.type);
-        }
-        // (the accumulator is read whole all the same: a warp's loads are collective)
-        if (w.row0 < a.rows) copy_out(&a.map, w, packed[0], packed[1], c0);
+        for (int c = 0; c < end; c += 64) copy64(a, w, f, sums, c);
       }
       return;
     }
     iwp_tc::staging_free<0>(w.lane);
     char* const out = static_cast<char*>(a.out) + w.split * a.split_stride * (a.type == IWP_F32 ? 4 : 2);
+    // 64 columns at a time, after which the sums in registers move up: one copy of the many ways to store, and room for it
 #pragma unroll 1
-    for (int c0 = w.col0; c0 < min(w.col0 + w.width, a.cols); c0 += 32) {
-      float v[32];
-      iwp_tc::tmem_load32(tmem + (c0 - w.col0), v);
+    for (int c = 0; c < end; c += 64) {
 #pragma unroll
-      for (int j = 0; j < 32; j++) v[j] *= f;
-      iwp_tc::store_chunk(v, w.staging, out, a.ld, a.type, a.wide, a.add, w.row0, a.rows, c0, a.cols, w.lane);
+      for (int i = 0; i < 64; i += 32) {
+        if (c + i < end) {
+          float v[32];
+          take(sums, LONG ? i : c + i, f, v);
+          iwp_tc::stage_chunk(v, w.staging + i / 32 * iwp_tc::STAGING_BYTES, a.type, a.add, w.lane);
+        }
+      }
+      if constexpr (LONG) {
+#pragma unroll
+        for (int j = 0; j < 32; j++) sums[j] = sums[j + 32];
+      }
+      __syncwarp();
+#pragma unroll 1
+      for (int i = 0; i < min(64, end - c); i += 32)
+        iwp_tc::write_chunk<LONG ? 4 : 8>(w.staging + i / 32 * iwp_tc::STAGING_BYTES, out, a.ld, a.type, a.wide, a.add, w.row0, a.rows, w.col0 + c + i, a.cols, w.lane);
+      __syncwarp();
     }
   }
 };

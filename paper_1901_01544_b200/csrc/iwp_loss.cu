@@ -1,4 +1,5 @@
 // iwp_loss.cu - C entries of the losses (include/iwp_loss.h): argument checks, workspace layout, launches.
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <cstring>
@@ -63,6 +64,8 @@ bool make_map(CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int64
              strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+
+constexpr int SEGMENT = 1024 / iwp_tc::BLOCK_K;  // most blocks of K that are summed in tensor memory
 
 constexpr int MAX_DEVICES = 64;
 
@@ -201,6 +204,8 @@ bool make_problem(iwp_tc::Problem* q, const Matrix& A, bool a_kc, const Matrix& 
   q->tile_n = tile_n;
   q->k_blocks = static_cast<int>(s.k_blocks());
   q->splits = splits;
+  const int64_t part = tiles_of(s.k_blocks(), splits);
+  q->seg = static_cast<int>(tiles_of(part, tiles_of(part, SEGMENT)));  // of even length
   // f32 accumulator; operand types; which operands are M/N-contiguous; N / 8; M / 16
   const uint32_t type = dtype == IWP_BF16 ? 1u : 0u;
   q->idesc = (1u << 4) | (type << 7) | (type << 10) | ((a_kc ? 0u : 1u) << 15) | ((b_kc ? 0u : 1u) << 16) |
@@ -210,9 +215,7 @@ bool make_problem(iwp_tc::Problem* q, const Matrix& A, bool a_kc, const Matrix& 
   return true;
 }
 
-// Tensor cores cut what a term loses against the running sum, so long sums drift: segments of at most 1024 elements of K,
-// added up in fp32 registers, keep the logits within 3e-7 of their size (1.2e-6 at K = 4096 without).
-int segment(const iwp_tc::Problem& q) { return static_cast<int>(tiles_of(q.k_blocks, tiles_of(q.k_blocks, 16))); }
+int64_t segments(const iwp_tc::Problem& q) { return q.splits ? tiles_of(tiles_of(q.k_blocks, q.splits), q.seg) : 0; }
 
 template <class Epi, int N>
 int pairs_of() {
@@ -221,8 +224,7 @@ int pairs_of() {
 }
 
 template <class Epi, int N>
-int launch_product(iwp_tc::Problems<N>& w, const typename Epi::Args& args, cudaStream_t st) {
-  const int pairs = pairs_of<Epi, N>();
+int launch_product(iwp_tc::Problems<N>& w, const typename Epi::Args& args, int pairs, cudaStream_t st) {
   int64_t total = 0;
   for (const auto& q : w.p) total += int64_t(q.m_tiles) * q.n_tiles * q.splits;
   if (total > MAX_SIZE) return IWP_ERR_INVALID;
@@ -323,9 +325,10 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
   const int64_t T = a->tokens, V = a->vocab, D = a->dim;
   char* const ws = static_cast<char*>(a->workspace);
   auto* hdr = static_cast<H::Header*>(a->state ? a->state : a->workspace);
-  const int pairs = pairs_of<H::Logits<H::NO_CODES>, 1>();
-  const int out_pairs = pairs_of<H::Out, 2>();  // the deal of the gradients counts on this grid
-  if (pairs < 1 || out_pairs < 1 || pairs_of<H::Logits<H::HALF_CODES>, 1>() < 1 || pairs_of<H::Logits<H::LOG_CODES>, 1>() < 1 || pairs_of<H::Probs, 1>() < 1) {
+  // one persistent grid for all products (the deal of the gradients counts on it)
+  const int pairs = std::min({pairs_of<H::Logits<H::NO_CODES>, 1>(), pairs_of<H::Logits<H::HALF_CODES>, 1>(), pairs_of<H::Logits<H::LOG_CODES>, 1>(),
+                              pairs_of<H::Probs, 1>(), pairs_of<H::Out<false>, 2>(), pairs_of<H::Out<true>, 2>()});
+  if (pairs < 1) {
     cudaGetLastError();
     return IWP_ERR_CUDA;
   }
@@ -438,7 +441,6 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
     const int tile_n = pick_tile_n(shape, pairs);
     iwp_tc::Problems<1> work;
     if (!make_problem(&work.p[0], h, true, w, true, a->dtype, tile_n, 1)) return IWP_ERR_CUDA;
-    work.seg = segment(work.p[0]);
     work.status = &hdr->status;
     work.early = !a->targets && !p.split_rows && !p.pack_hidden && !p.pack_weight;  // k_soft_targets comes right before
     const int parts = 2 * work.p[0].n_tiles;
@@ -458,7 +460,7 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
       la.v0 = static_cast<int>(v0);
       la.width = static_cast<int>(p.piece);
       if (kept >= 0 && !make_map(&la.map, probs, T, p.piece, p.piece, 32, a->dtype)) return static_cast<int>(IWP_ERR_CUDA);
-      return launch_product<Epi, 1>(work, la, st);
+      return launch_product<Epi, 1>(work, la, pairs, st);
     };
     const int failed = kept < 0 ? logits(H::Logits<H::NO_CODES>{}) : a->dtype == IWP_F16 ? logits(H::Logits<H::LOG_CODES>{}) : logits(H::Logits<H::HALF_CODES>{});
     if (failed) return failed;
@@ -486,14 +488,14 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
   }
   if (!p.grad) return IWP_OK;
 
-  H::Out::Args oa{};
+  H::OutArgs oa{};
   oa.f.hdr = hdr;
   oa.f.dloss = a->dloss;
   oa.f.factor = a->scale * tau / up;
   oa.f.mean = a->mean;
   oa.m[0].row_power = row_power;
   oa.m[1].by_gmax = p.split_rows;
-  auto copy_map = [](H::Out::Matrix& o) {
+  auto copy_map = [](H::OutMatrix& o) {
     o.by_copy = o.type != IWP_F32 && o.wide && !o.add;
     return !o.by_copy || make_map(&o.map, o.out, o.rows, o.cols, o.ld, 32, o.type);
   };
@@ -507,7 +509,6 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
       const Shape shape{T, width, D};
       iwp_tc::Problems<1> work;
       if (!make_problem(&work.p[0], h, true, wp, true, a->dtype, pick_tile_n(shape, pairs), 1)) return IWP_ERR_CUDA;
-      work.seg = segment(work.p[0]);
       work.status = &hdr->status;
       work.early = 0;
       H::Probs::Args pa{};
@@ -522,17 +523,16 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
       pa.up = up;
       pa.type = a->dtype;
       if (!make_map(&pa.map, probs, T, p.piece, p.piece, 32, a->dtype)) return IWP_ERR_CUDA;
-      if (int e = launch_product<H::Probs, 1>(work, pa, st)) return e;
+      if (int e = launch_product<H::Probs, 1>(work, pa, pairs, st)) return e;
     }
     // both gradients of the piece in one launch, dhidden (the longer tiles) first
     iwp_tc::Problems<2> work;
     work.p[0].m_tiles = work.p[0].n_tiles = work.p[0].splits = 0;
     work.p[1].m_tiles = work.p[1].n_tiles = work.p[1].splits = 0;
-    work.seg = 1 << 30;
     work.status = &hdr->status;
     work.early = 0;
     const Shape dh{T, D, width}, dw{width, D, T};
-    const Deal deal = deal_gradients(a->dhidden ? &dh : nullptr, a->dweight ? &dw : nullptr, out_pairs, done == 0 ? 0 : splits);
+    const Deal deal = deal_gradients(a->dhidden ? &dh : nullptr, a->dweight ? &dw : nullptr, pairs, done == 0 ? 0 : splits);
     work.rounds = deal.rounds;
     work.rest = deal.rest;
     work.fill = deal.fill;
@@ -540,7 +540,7 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
     const int tile_n = deal.tile_n;
     if (a->dhidden) {
       const bool direct = p.pieces == 1 && splits == 1;
-      H::Out::Matrix& o = oa.m[0];
+      H::OutMatrix& o = oa.m[0];
       o.rows = static_cast<int>(T);
       o.cols = static_cast<int>(D);
       if (direct) {
@@ -564,7 +564,7 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
       if (!make_problem(&work.p[0], pm, true, wp, false, a->dtype, tile_n, splits)) return IWP_ERR_CUDA;
     }
     if (a->dweight) {
-      H::Out::Matrix& o = oa.m[1];
+      H::OutMatrix& o = oa.m[1];
       const int size = a->dweight_type == IWP_F32 ? 4 : 2;
       o.out = static_cast<char*>(a->dweight) + size * v0 * a->dweight_ld;
       o.ld = a->dweight_ld;
@@ -576,7 +576,8 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
       if (!copy_map(o)) return IWP_ERR_CUDA;
       if (!make_problem(&work.p[1], pm, false, h_dw, false, a->dtype, tile_n, 1)) return IWP_ERR_CUDA;
     }
-    if (int e = launch_product<H::Out, 2>(work, oa, st)) return e;
+    const bool sums = segments(work.p[0]) > 1 || segments(work.p[1]) > 1;
+    if (int e = sums ? launch_product<H::Out<true>, 2>(work, oa, pairs, st) : launch_product<H::Out<false>, 2>(work, oa, pairs, st)) return e;
   }
   if (a->dhidden && (p.pieces > 1 || splits > 1)) {
     const int size = a->dhidden_type == IWP_F32 ? 4 : 2;

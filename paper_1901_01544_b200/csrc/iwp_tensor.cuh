@@ -210,6 +210,7 @@ struct Problem {
   int tile_n;            // 256, 128 or 64
   int k_blocks;          // blocks of BLOCK_K along K
   int splits;            // the K range in this many parts (each part a tile of its own)
+  int seg;               // blocks of K per accumulator
   uint32_t idesc;
   int a_kc, b_kc;        // which operands are K-contiguous
 };
@@ -222,7 +223,6 @@ struct Problems {
   Problem p[N];
   int rounds, rest, fill;
   int stages, b_bytes;  // of the ring in shared memory, and B's share of a stage
-  int seg;    // k blocks per accumulator tile (epilogues that add up segments), or a large number
   int early;  // 1: the operands were complete before the kernel in front of this one let it start, so that only the
               // epilogue has to wait for that kernel's end
   int* status;
@@ -288,9 +288,13 @@ __device__ __forceinline__ bool tile_at(const Problems<N>& w, int pair, int pair
 }
 
 // Epi (device class): `Args`; AREAS, the staging areas per warp; begin(args, where), before the tile is there; tile(args,
-// where, begun, accumulator), in which an epilogue warp disposes of its 32 rows and half of the tile's columns.  SUMS: the
-// tensor memory is emptied into registers every `seg` blocks of K and added up there (the accumulator is then an array);
-// otherwise it is an address in tensor memory.
+// where, begun, sums), in which an epilogue warp disposes of its 32 rows and half of the tile's columns.
+//
+// Tensor cores cut what a term loses against the running sum, so long sums of one sign come out low: with K = 131072 by up to
+// 1.4e-3 of themselves, with 8192 by 1.5e-5, 1024 by 1e-6.  With SUMS the tensor memory is therefore emptied into registers
+// every `seg` blocks of K (at most 1024 elements) and added up there, in fp32 rounded to nearest, while the products go on in
+// the other accumulator; tile() gets an array of pairs of columns.  Without, for K of one segment, it gets an address in
+// tensor memory.
 struct Where {
   int row0;     // first of the warp's 32 rows; the lane's row is row0 + lane
   int col0;     // first of the warp's columns
@@ -398,8 +402,8 @@ __global__ void __launch_bounds__(THREADS, 1)
         const bool a_kc = q.a_kc, b_kc = q.b_kc;
         const uint64_t step_a = a_kc ? 2 : 128, step_b = b_kc ? 2 : 128;
         const uint32_t idesc = q.idesc;
-        for (int k0 = t.k0; k0 < t.k1; k0 += w.seg) {
-          const int k1 = Epi::SUMS ? min(t.k1, k0 + w.seg) : t.k1;
+        for (int k0 = t.k0; k0 < t.k1; k0 += q.seg) {
+          const int k1 = min(t.k1, k0 + q.seg);
           if (!mbar_wait(acc_empty + 8 * b, acc_phase ^ 1, dead, w.status)) break;
           fence_after();
           for (int kb = k0; kb < k1; kb++) {
@@ -421,7 +425,6 @@ __global__ void __launch_bounds__(THREADS, 1)
             b = 0;
             acc_phase ^= 1;
           }
-          if (!Epi::SUMS) break;
         }
       }
     }
@@ -460,7 +463,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     locate(t, coming);
     auto begun = Epi::begin(args, coming);
     for (int i = 1; ok && more; i++) {
-      const int k0 = t.k0, k1 = t.k1, area = at.area;
+      const int k0 = t.k0, k1 = t.k1, seg = w.p[t.p].seg, area = at.area;
       at = coming;
       at.area = area;
       auto now = begun;
@@ -470,12 +473,15 @@ __global__ void __launch_bounds__(THREADS, 1)
         locate(t, coming);
         begun = Epi::begin(args, coming);
       }
+      auto wait = [&] {
+        ok = __all_sync(0xFFFFFFFFu, mbar_wait(acc_full + 8 * b, acc_phase, dead, w.status));
+        if (ok) fence_after();
+        return ok;
+      };
+      if (!wait()) break;
       if constexpr (Epi::SUMS) {
         f2 acc[TILE_N / 4];
         auto segment = [&](auto first) {
-          ok = __all_sync(0xFFFFFFFFu, mbar_wait(acc_full + 8 * b, acc_phase, dead, w.status));
-          if (!ok) return;
-          fence_after();
 #pragma unroll
           for (int c = 0; c < TILE_N / 64; c++) {
             if (32 * c < at.width) {
@@ -491,12 +497,9 @@ __global__ void __launch_bounds__(THREADS, 1)
           release();
         };
         segment(std::true_type{});
-        for (int k = k0 + w.seg; ok && k < k1; k += w.seg) segment(std::false_type{});
+        for (int k = k0 + seg; k < k1 && wait(); k += seg) segment(std::false_type{});
         if (ok) Epi::tile(args, at, now, acc);
       } else {
-        ok = __all_sync(0xFFFFFFFFu, mbar_wait(acc_full + 8 * b, acc_phase, dead, w.status));
-        if (!ok) break;
-        fence_after();
         Epi::tile(args, at, now, mine + b * TILE_N);
         release();
       }
@@ -561,12 +564,10 @@ __device__ __forceinline__ void store_staged(const CUtensorMap* map, char* stagi
   }
 }
 
-// Writes a chunk of 32 columns (v: this lane's row) of the warp's 32 rows to a row-major matrix, through the warp's
-// staging rows so that the stores are whole 32-byte sectors; rows and columns outside are dropped.
-// TYPE: IWP_F32 / IWP_BF16 / IWP_F16.  `add`: the old contents are added first (in fp32).
-__device__ __forceinline__ void store_chunk(const float (&v)[32], char* staging, void* out, int64_t ld, int type, bool wide, bool add,
-                                            int row0, int rows, int col0, int cols, int lane) {
-  if (type == 0 || add) {  // staged as fp32
+// A chunk of 32 columns (v: this lane's row) into the warp's staging rows: fp32 where it is written or added to as such, else
+// of the 16-bit `type`.
+__device__ __forceinline__ void stage_chunk(const float (&v)[32], char* staging, int type, bool add, int lane) {
+  if (type == 0 || add) {
 #pragma unroll
     for (int j = 0; j < 8; j++) *reinterpret_cast<float4*>(staged(staging, lane, j)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
   } else {
@@ -576,7 +577,15 @@ __device__ __forceinline__ void store_chunk(const float (&v)[32], char* staging,
           make_uint4(pack2(v[8 * j], v[8 * j + 1], type), pack2(v[8 * j + 2], v[8 * j + 3], type), pack2(v[8 * j + 4], v[8 * j + 5], type),
                      pack2(v[8 * j + 6], v[8 * j + 7], type));
   }
-  __syncwarp();
+}
+
+// A staged chunk to a row-major matrix, in whole 32-byte sectors where rows are `wide` (start at multiples of 16 bytes); rows
+// and columns outside are dropped.  TYPE: IWP_F32 / IWP_BF16 / IWP_F16.  `add`: the old contents are added first (in fp32;
+// all of a thread's on their way at once, since the compiler cannot tell that a store does not touch them).  The
+// caller synchronises the warp before and after.
+template <int BATCH>
+__device__ __forceinline__ void write_chunk(char* staging, void* out, int64_t ld, int type, bool wide, bool add, int row0, int rows, int col0,
+                                            int cols, int lane) {
   const bool whole = wide && col0 + 32 <= cols;
   if (whole && type != 0 && !add) {
     const int r = lane >> 2, c = lane & 3;  // 8 rows of 64 bytes at a time
@@ -588,16 +597,20 @@ __device__ __forceinline__ void store_chunk(const float (&v)[32], char* staging,
     }
   } else if (whole && type == 0) {
     const int r = lane >> 3, c = lane & 7;  // 4 rows of 128 bytes at a time
+    float* p = static_cast<float*>(out) + (row0 + r) * ld + col0 + 4 * c;
+#pragma unroll 1
+    for (int h = 0; h < 32; h += 4 * BATCH, p += 4 * BATCH * ld) {
+      float4 old[BATCH];
+      if (add) {
 #pragma unroll
-    for (int i = 0; i < 32; i += 4) {
-      float4 x = *reinterpret_cast<const float4*>(staged(staging, r + i, c));
-      if (row0 + r + i < rows) {
-        float4* p = reinterpret_cast<float4*>(static_cast<float*>(out) + (row0 + r + i) * ld + col0) + c;
-        if (add) {
-          const float4 y = *p;
-          x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
-        }
-        *p = x;
+        for (int i = 0; i < BATCH; i++)
+          if (row0 + r + h + 4 * i < rows) old[i] = *reinterpret_cast<const float4*>(p + 4 * i * ld);
+      }
+#pragma unroll
+      for (int i = 0; i < BATCH; i++) {
+        float4 x = *reinterpret_cast<const float4*>(staged(staging, r + h + 4 * i, c));
+        if (add) x = make_float4(x.x + old[i].x, x.y + old[i].y, x.z + old[i].z, x.w + old[i].w);
+        if (row0 + r + h + 4 * i < rows) *reinterpret_cast<float4*>(p + 4 * i * ld) = x;
       }
     }
   } else if (type != 0 && !add) {
@@ -616,20 +629,37 @@ __device__ __forceinline__ void store_chunk(const float (&v)[32], char* staging,
         row[k] = at(k);
       if (odd && c == 0 && col0 < cols) row[0] = at(0);
     }
-  } else {  // ragged columns or unaligned rows of fp32, or a 16-bit sum: element by element, a row at a time
+  } else if (type == 0) {  // ragged columns or unaligned rows of fp32: a row at a time
+    if (col0 + lane < cols) {
+      float* p = static_cast<float*>(out) + row0 * ld + col0 + lane;
+#pragma unroll 1
+      for (int h = 0; h < 32; h += 2 * BATCH, p += 2 * BATCH * ld) {
+        float old[2 * BATCH];
+        if (add) {
+#pragma unroll
+          for (int i = 0; i < 2 * BATCH; i++)
+            if (row0 + h + i < rows) old[i] = p[i * ld];
+        }
+#pragma unroll
+        for (int i = 0; i < 2 * BATCH; i++) {
+          float x = reinterpret_cast<const float*>(staged(staging, h + i, lane >> 2))[lane & 3];
+          if (add) x += old[i];
+          if (row0 + h + i < rows) p[i * ld] = x;
+        }
+      }
+    }
+  } else {  // a 16-bit sum: element by element, a row at a time
     for (int i = 0; i < 32 && row0 + i < rows; i++) {
       if (col0 + lane < cols) {
         const int64_t at = (row0 + i) * ld + col0 + lane;
-        float x = reinterpret_cast<const float*>(staged(staging, i, lane >> 2))[lane & 3];
-        if (add) x += load_as_float(out, at, type);
-        store_as(out, at, x, type);
+        const float x = reinterpret_cast<const float*>(staged(staging, i, lane >> 2))[lane & 3];
+        store_as(out, at, x + load_as_float(out, at, type), type);
       }
     }
   }
-  __syncwarp();
 }
 
-// The same for 32 columns of 16 bits that are packed already; rows of 16-byte multiples, all columns inside.
+// 32 columns of 16 bits that are packed already, staged and written; rows of 16-byte multiples, all columns inside.
 __device__ __forceinline__ void store_packed(const uint32_t (&u)[16], char* staging, uint16_t* out, int64_t ld, int row0, int rows, int col0,
                                              int lane) {
 #pragma unroll

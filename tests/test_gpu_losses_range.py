@@ -255,3 +255,28 @@ def test_probabilities_see_the_logits_that_lse_saw(dtype, saved):
     cols = torch.bincount(y, minlength=V) == 0
     want = (2.0**-10 * h.double().sum(0)).expand(int(cols.sum()), D)
     within(dw[cols], want, (T / 16 + 8) * 2.0**-22 * want, "dweight")
+
+
+def test_long_sums_of_one_sign():
+    """Rows whose logits are all equal have p = 2^-k exactly, and a factor of -1 (rounded) at the target.  The gradients are then
+    sums of exactly known terms, here of one sign.  Sums of at most 1024 terms in the tensor cores lose (1024 / 16 + 2) 2^-22 of
+    themselves at most, adding those up in fp32 2^-24 each: below 2^-15 in all.  (Left to the tensor cores alone, 65536
+    terms came out 4e-4 low, 32768 7e-5.)"""
+    for T, V, D in ((8192, 65536, 1024), (32768, 1024, 128)):
+        g = gen(820)
+        w = (torch.rand(V, D, generator=g, device=DEV) ** 4).to(BF)
+        w[:, :64] = 1.0
+        h = torch.zeros(T, D, device=DEV, dtype=BF)
+        h[:, :64] = (torch.rand(T, 64, generator=g, device=DEV) ** 4).to(BF)
+        y = torch.randint(0, V // 2, (T,), generator=g, device=DEV)
+        plan = losses.HeadLoss(T, V, D, BF)
+        dh, dw = torch.empty(T, D, device=DEV), torch.empty(V, D, device=DEV)
+        plan.cross_entropy_grad(h, w, y, reduction="sum", dhidden=dh, dweight=dw)
+        rows = slice(T - 256, T)
+        total = sum(w[i : i + 4096, 64:].double().sum(0) for i in range(0, V, 4096)) / V
+        own = w[y[rows], 64:].double()
+        at = torch.tensor(1 / V - 1, device=DEV).to(BF).double()
+        want = total - own / V + at * own
+        within(dh[rows, 64:], want, 2.0**-15 * (total + own), "dhidden")
+        want = (h[:, :64].double().sum(0) / V).expand(V - V // 2, 64)
+        within(dw[V // 2 :, :64], want, 2.0**-15 * want, "dweight")
