@@ -41,7 +41,8 @@ int iwp_loss_status(const void* state, int32_t* status_host, void* cuda_stream);
  *   rows[t] = tau^2 * sum_k q_k (log q_k - z[t][i_k] / tau + lse[t])      (a row without targets: 0)
  *   loss    = sum_t rows[t], divided by the number of rows with targets if `mean` (0 if there is none)
  *   dz[t][v] = g_t * tau * (exp(z[t][v] / tau - lse[t]) - q of v),  g_t = dloss_rows[t] * dloss * scale (/ number)
- *   dhidden = dz weight,  dweight = dz^T hidden                            (rows without targets give nothing)
+ *   dhidden = dz weight,  dweight = dz^T hidden                            (rows without targets give nothing,
+ *                                                          whatever their hidden states hold)
  * Cross entropy (targets != NULL): q = 1 at targets[t]; targets[t] == ignore_index: no target.  Distillation
  * (targets == NULL): q = softmax over the row's top_k teacher logits / tau; an id below 0 is padding and takes no
  * part, a logit of -inf has q = 0; nothing but those: no target.  A target or id at or above vocab (or a negative

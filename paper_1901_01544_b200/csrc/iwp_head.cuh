@@ -43,6 +43,8 @@ struct Header {
   int n_rows;       // rows with targets
   uint32_t ticket;
   float gmax;       // the largest of the rows' powers of two (k_row_scales)
+  int dirty;        // a row that gives nothing has a lse that is not finite; noted while rows are walked
+  int clean;        // the same once they all were: dweight reads a copy of the hidden states (clean_rows)
 };
 
 // What the rows subtract.  `hard`: one target per row, read as the caller gave them; else lists made by k_soft_targets.
@@ -622,25 +624,59 @@ __global__ void __launch_bounds__(256) k_scaled_rows(const Header* hdr, const fl
   }
 }
 
+// dweight sums over all rows, and zero times what is not finite is not zero: where a row that gives nothing (padding, say, that
+// attended to nothing) holds NaN or infinities, which its lse tells, the product reads a copy of the hidden states in
+// which such rows are zero.  Rows of both start at multiples of 16 bytes.  A warp takes a row.
+struct Clean {
+  const uint16_t* from;
+  uint16_t* to;  // NULL: not needed
+  int64_t ld_from, ld_to, T;
+  int D;
+};
+__device__ __forceinline__ void clean_rows(const Clean& a, const Targets& en, int64_t warp, int64_t warps) {
+  const int lane = threadIdx.x & 31;
+  for (int64_t r = warp; r < a.T; r += warps) {
+    const bool gives = en.row_scale(r) != 0.f;
+    for (int g = 8 * lane; g < a.D; g += 8 * 32) {
+      union {
+        uint16_t e[8];
+        uint4 all;
+      } x;
+      x.all = make_uint4(0u, 0u, 0u, 0u);
+      if (gives && g + 8 <= a.D) {
+        x.all = *reinterpret_cast<const uint4*>(a.from + r * a.ld_from + g);
+      } else if (gives) {
+#pragma unroll
+        for (int j = 0; j < 8; j++)
+          if (g + j < a.D) x.e[j] = a.from[r * a.ld_from + g + j];
+      }
+      *reinterpret_cast<uint4*>(a.to + r * a.ld_to + g) = x.all;
+    }
+  }
+}
+
 // Number of rows with targets, and whether one is outside the vocabulary, for backward passes on their own (k_rows sees to
-// both otherwise).
-__global__ void __launch_bounds__(1024) k_count_rows(Header* hdr, Targets en, int64_t T) {
+// both otherwise); the same for clean_rows, by its one block.
+__global__ void __launch_bounds__(1024) k_count_rows(Header* hdr, Targets en, const float* lse, Clean copy, int64_t T) {
   __shared__ int sh[32];
   iwp_tc::launch_next();
   iwp_tc::wait_previous();
   int n = 0;
-  bool bad = false;
+  bool bad = false, dirty = false;
   for (int64_t t = threadIdx.x; t < T; t += blockDim.x) {
     const int state = en.state(t);
     n += state != 0;
     bad |= state < 0;
+    dirty |= !isfinite(lse[t]) && en.row_scale(t) == 0.f;
   }
   if (bad) atomicExch(&hdr->status, IWP_ERR_INVALID);
   n = __reduce_add_sync(0xFFFFFFFFu, n);
   if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = n;
   __syncthreads();
   n = __reduce_add_sync(0xFFFFFFFFu, sh[threadIdx.x & 31]);
-  if (threadIdx.x == 0) hdr->n_rows = n;
+  dirty = __syncthreads_or(dirty && copy.to);
+  if (threadIdx.x == 0) hdr->n_rows = n, hdr->clean = dirty;
+  if (dirty) clean_rows(copy, en, threadIdx.x >> 5, blockDim.x >> 5);
 }
 
 // ---- finish of the forward pass --------------------------------------------------------------------------
@@ -721,7 +757,9 @@ __global__ void __launch_bounds__(ROW_THREADS) k_rows(const Rows a) {
     }
     if (me == 0) {
       const float c = a.en.hard ? 0.f : a.en.const_term[row];
-      a.lse[row] = x.x / a.tau + log_sum;
+      const float lse = x.x / a.tau + log_sum;
+      a.lse[row] = lse;
+      if (!isfinite(lse) && a.en.row_scale(row) == 0.f) atomicExch(&a.hdr->dirty, 1);
       a.rows[row] = state == 0 ? 0.f : state < 0 ? CUDART_NAN_F : a.tau * a.tau * (c + below);
       if (state < 0) atomicExch(&a.hdr->status, IWP_ERR_INVALID);
       __threadfence();
@@ -747,6 +785,7 @@ __global__ void __launch_bounds__(ROW_THREADS) k_rows(const Rows a) {
     sum = 0.f, n = 0;
     for (int w = 0; w < WARPS; w++) sum += sh_sum[w], n += sh_n[w];
     a.hdr->n_rows = n;
+    a.hdr->clean = atomicExch(&a.hdr->dirty, 0);
     if (a.loss) *a.loss = n == 0 ? 0.f : a.mean ? sum / static_cast<float>(n) : sum;
   }
 }
@@ -762,6 +801,9 @@ struct Factors {
   int64_t ld;
   int parts, part_shift, v0, width, chunks, log_codes;
   float c, up;  // log2(e) / tau
+  const Header* hdr;
+  int64_t blocks;  // of the factors; any others clean_rows, if there is need
+  Clean copy;
 };
 
 constexpr int FACTOR_THREADS = 256, FACTOR_DEEP = 4, FACTOR_COLUMNS = 8 * FACTOR_THREADS * FACTOR_DEEP;
@@ -769,8 +811,14 @@ constexpr int FACTOR_THREADS = 256, FACTOR_DEEP = 4, FACTOR_COLUMNS = 8 * FACTOR
 // A block takes FACTOR_COLUMNS columns of one row: bound by memory, 2 bytes in and 2 out per element (4096 x 32768: 78 us =
 // 6.9 TB/s with the end of the codes still in the L2; with 64 targets per row to look through, 88 us).
 __global__ void __launch_bounds__(FACTOR_THREADS) k_factors(const Factors a) {
-  constexpr int MINE = (MAX_TOP + FACTOR_THREADS - 1) / FACTOR_THREADS;
+  constexpr int MINE = (MAX_TOP + FACTOR_THREADS - 1) / FACTOR_THREADS, WARPS = FACTOR_THREADS / 32;
   const int tid = threadIdx.x;
+  if (blockIdx.x >= a.blocks) {
+    iwp_tc::launch_next();
+    iwp_tc::wait_previous();
+    if (a.hdr->clean) clean_rows(a.copy, a.en, (blockIdx.x - a.blocks) * WARPS + tid / 32, (gridDim.x - a.blocks) * WARPS);
+    return;
+  }
   const int64_t row = blockIdx.x / a.chunks;
   uint16_t* const codes = a.codes + row * a.ld;
   const float2* const part = a.part + row * a.parts;

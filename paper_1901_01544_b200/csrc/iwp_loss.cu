@@ -208,6 +208,7 @@ bool make_problem(iwp_tc::Problem* q, const Matrix& A, bool a_kc, const Matrix& 
   q->seg = static_cast<int>(tiles_of(part, tiles_of(part, SEGMENT)));  // of even length
   // f32 accumulator; operand types; which operands are M/N-contiguous; N / 8; M / 16
   const uint32_t type = dtype == IWP_BF16 ? 1u : 0u;
+  q->use_other = nullptr;
   q->idesc = (1u << 4) | (type << 7) | (type << 10) | ((a_kc ? 0u : 1u) << 15) | ((b_kc ? 0u : 1u) << 16) |
              (static_cast<uint32_t>(tile_n / 8) << 17) | ((iwp_tc::TILE_M * iwp_tc::CG / 16u) << 24);
   q->a_kc = a_kc;
@@ -244,7 +245,7 @@ struct HeadPlan {
   bool split_rows;  // fp16 with an upstream gradient per row: k_row_scales
   int64_t k, piece, pieces, d_pad;
   // offsets into the workspace
-  int64_t column, q, const_term, row_scale, row_power, rows, z_at, part, hidden, weight, scaled, probs, join, bytes;
+  int64_t column, q, const_term, row_scale, row_power, rows, z_at, part, hidden, weight, copy, probs, join, bytes;
 };
 
 bool needs_copy(const void* p, int64_t ld) { return !aligned(p, 16) || ld % 8 != 0; }
@@ -285,8 +286,8 @@ HeadPlan head_plan(const iwp_head_args* a) {
   if (p.split_rows) {
     p.row_scale = take(4 * T);
     p.row_power = take(4 * T);
-    if (a->dweight) p.scaled = take(2 * T * p.d_pad);
   }
+  if (a->dweight) p.copy = take(2 * T * p.d_pad);
   p.rows = take(4 * T);
   if (!a->have_lse) {
     p.z_at = take(4 * p.k * T);
@@ -361,7 +362,6 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
   float* const row_power = p.split_rows ? reinterpret_cast<float*>(ws + p.row_power) : nullptr;
   if (p.split_rows) LOSS_CUDA(launch(H::k_row_scales, 1, 1024, 0, 1, st, hdr, en, row_scale, row_power, a->dloss_rows, T));
   if (p.grad) en.scale = p.split_rows ? row_scale : a->dloss_rows;
-  if (a->have_lse) LOSS_CUDA(launch(H::k_count_rows, 1, 1024, 0, 1, st, hdr, en, T));
   Matrix h{a->hidden, T, D, a->hidden_ld}, w{a->weight, V, D, a->weight_ld};
   auto align_rows = [&](Matrix& m, int64_t at) {
     const int64_t warps = tiles_of(m.rows, 8), blocks = warps < 8 * sms ? warps : 8 * sms;
@@ -375,12 +375,16 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
   };
   if (p.pack_hidden) LOSS_CUDA(align_rows(h, p.hidden));
   if (p.pack_weight) LOSS_CUDA(align_rows(w, p.weight));
-  Matrix h_dw = h;  // of dweight's product
+  // dweight's product: the hidden states; with the rows' scales; or, if the device finds that they have to be, clean
+  const Matrix h_copy{ws + p.copy, T, D, p.d_pad}, h_dw = p.split_rows ? h_copy : h;
+  const bool may_clean = a->dweight && !p.split_rows;
+  const H::Clean copy{static_cast<const uint16_t*>(h.p), may_clean ? reinterpret_cast<uint16_t*>(ws + p.copy) : nullptr, h.ld, p.d_pad, T,
+                      static_cast<int>(D)};
+  if (a->have_lse) LOSS_CUDA(launch(H::k_count_rows, 1, 1024, 0, 1, st, hdr, en, a->lse, copy, T));
   if (p.split_rows && a->dweight) {
-    h_dw.p = ws + p.scaled, h_dw.ld = p.d_pad;
     const int64_t blocks = tiles_of(T, 8);
     LOSS_CUDA(launch(H::k_scaled_rows, blocks < 8 * sms ? blocks : 8 * sms, 256, 0, 1, st, hdr, row_scale, row_power, static_cast<const __half*>(h.p),
-                     h.ld, reinterpret_cast<__half*>(ws + p.scaled), p.d_pad, T, static_cast<int>(D)));
+                     h.ld, reinterpret_cast<__half*>(ws + p.copy), p.d_pad, T, static_cast<int>(D)));
   }
 
   const float up = a->dtype == IWP_F16 ? 8192.f : 1.f;
@@ -482,8 +486,12 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
       fa.log_codes = a->dtype == IWP_F16;
       fa.c = c;
       fa.up = up;
-      if (T * fa.chunks > MAX_SIZE) return IWP_ERR_INVALID;
-      LOSS_CUDA(launch(H::k_factors, T * fa.chunks, H::FACTOR_THREADS, 0, 1, st, fa));
+      fa.hdr = hdr;
+      fa.blocks = T * fa.chunks;
+      fa.copy = copy;
+      const int64_t others = may_clean ? std::min<int64_t>(tiles_of(T, H::FACTOR_THREADS / 32), sms) : 0;
+      if (fa.blocks + others > MAX_SIZE) return IWP_ERR_INVALID;
+      LOSS_CUDA(launch(H::k_factors, fa.blocks + others, H::FACTOR_THREADS, 0, 1, st, fa));
     }
   }
   if (!p.grad) return IWP_OK;
@@ -529,6 +537,7 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
     iwp_tc::Problems<2> work;
     work.p[0].m_tiles = work.p[0].n_tiles = work.p[0].splits = 0;
     work.p[1].m_tiles = work.p[1].n_tiles = work.p[1].splits = 0;
+    work.p[1].use_other = nullptr;
     work.status = &hdr->status;
     work.early = 0;
     const Shape dh{T, D, width}, dw{width, D, T};
@@ -575,6 +584,10 @@ int head_run(const iwp_head_args* a, const HeadPlan& p, cudaStream_t st) {
       o.add = a->accumulate;
       if (!copy_map(o)) return IWP_ERR_CUDA;
       if (!make_problem(&work.p[1], pm, false, h_dw, false, a->dtype, tile_n, 1)) return IWP_ERR_CUDA;
+      if (may_clean) {
+        if (!make_map(&work.p[1].b_other, h_copy.p, T, D, p.d_pad, iwp_tc::BLOCK_K, a->dtype)) return IWP_ERR_CUDA;
+        work.p[1].use_other = &hdr->clean;
+      }
     }
     const bool sums = segments(work.p[0]) > 1 || segments(work.p[1]) > 1;
     if (int e = sums ? launch_product<H::Out<true>, 2>(work, oa, pairs, st) : launch_product<H::Out<false>, 2>(work, oa, pairs, st)) return e;

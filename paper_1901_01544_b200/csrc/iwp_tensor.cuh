@@ -213,6 +213,8 @@ struct Problem {
   int seg;               // blocks of K per accumulator
   uint32_t idesc;
   int a_kc, b_kc;        // which operands are K-contiguous
+  CUtensorMap b_other;   // what takes B's place if *use_other (on the device; NULL: never), last problem of a launch only
+  const int* use_other;
 };
 
 // Up to two problems over the pairs of a launch.  Every pair first takes `rounds` tiles of problem 0; the first `rest`
@@ -362,12 +364,14 @@ __global__ void __launch_bounds__(THREADS, 1)
       int s = 0;
       uint32_t phase = 0;
       const uint32_t full_of_pair = map_to(full, 0);  // both CTAs' loads are counted by the first CTA
+      const bool other = w.p[N - 1].use_other && __ldcg(w.p[N - 1].use_other);
       for (int i = 0; !*dead && tile_at(w, pair, pairs, i, t); i++) {
         const Problem& q = w.p[t.p];
         const int rows_b = q.tile_n / CG;
         const int row_a = t.m * TILE_M * CG + static_cast<int>(rank) * TILE_M;
         const int row_b = t.n * q.tile_n + static_cast<int>(rank) * rows_b;
         const bool a_kc = q.a_kc, b_kc = q.b_kc;
+        const CUtensorMap* const map_b = other && t.p == N - 1 ? &q.b_other : &q.b;
         // an M/N-contiguous box is 64 columns wide even where a CTA needs 32 of them
         const uint32_t bytes = CG * (A_BYTES + (b_kc ? rows_b : max(rows_b, 64)) * BLOCK_K * 2);
         for (int kb = t.k0; kb < t.k1; kb++) {
@@ -382,10 +386,10 @@ __global__ void __launch_bounds__(THREADS, 1)
             tma_load(at_a + 64 * 128, &q.a, row_a + 64, kb * BLOCK_K, bar);
           }
           if (b_kc) {
-            tma_load(at_b, &q.b, kb * BLOCK_K, row_b, bar);
+            tma_load(at_b, map_b, kb * BLOCK_K, row_b, bar);
           } else {
-            tma_load(at_b, &q.b, row_b, kb * BLOCK_K, bar);
-            if (rows_b > 64) tma_load(at_b + 64 * 128, &q.b, row_b + 64, kb * BLOCK_K, bar);
+            tma_load(at_b, map_b, row_b, kb * BLOCK_K, bar);
+            if (rows_b > 64) tma_load(at_b + 64 * 128, map_b, row_b + 64, kb * BLOCK_K, bar);
           }
           if (++s == stages) {
             s = 0;

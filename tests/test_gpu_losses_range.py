@@ -280,3 +280,45 @@ def test_long_sums_of_one_sign():
         within(dh[rows, 64:], want, 2.0**-15 * (total + own), "dhidden")
         want = (h[:, :64].double().sum(0) / V).expand(V - V // 2, 64)
         within(dw[V // 2 :, :64], want, 2.0**-15 * want, "dweight")
+
+
+@pytest.mark.parametrize("saved", [False, True])
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("T,V,D,piece", [(130, 700, 72, 0), (300, 2000, 264, 1), (40, 300, 33, 0), (1100, 500, 64, 0)])
+def test_rows_that_give_nothing_may_hold_anything(T, V, D, piece, dtype, saved):
+    """NaN and infinities in the hidden states of rows without a target, or without an upstream gradient, reach nothing:
+    all results are those of the same rows filled with zeros."""
+    g = gen(840 + T)
+    h = torch.randn(T, D, generator=g, device=DEV).to(dtype)
+    w = (torch.randn(V, D, generator=g, device=DEV) / math.sqrt(D)).to(dtype)
+    y = torch.randint(0, V, (T,), generator=g, device=DEV)
+    off = torch.rand(T, generator=g, device=DEV) < 0.2
+    off[1], off[2] = True, False
+    clean, dirty = h.clone(), h.clone()
+    clean[off] = 0
+    junk = torch.tensor([math.nan, math.inf, -math.inf, 0.0], device=DEV)[torch.randint(0, 4, (T, D), generator=g, device=DEV)].to(dtype)
+    junk[:, D // 2] = math.nan
+    junk[::2] = math.inf  # a row of nothing but infinities
+    dirty[off] = junk[off]
+    ids = torch.rand(T, V, generator=g, device=DEV).argsort(1)[:, :5].contiguous()
+    teacher = torch.randn(T, 5, generator=g, device=DEV)
+    up = torch.where(off, 0.0, torch.randn(T, generator=g, device=DEV))
+    y_off, ids_off = torch.where(off, -100, y), torch.where(off[:, None], -1, ids)
+    plan = losses.HeadLoss(T, V, D, dtype, top_k=5, piece_bytes=piece)
+    calls = [
+        (plan.cross_entropy, plan.cross_entropy_grad, (y_off,), {}),
+        (plan.distill, plan.distill_grad, (ids_off, teacher, 2.0), {}),
+        (plan.cross_entropy, plan.cross_entropy_grad, (y,), dict(dloss=up)),
+    ]
+    for forward, grad, args, kw in calls:
+        out = []
+        for hidden in (dirty, clean):
+            lse = forward(hidden, w, *args).lse.clone() if saved else None
+            r = grad(hidden, w, *args, lse=lse, reduction="sum", dweight=torch.empty(V, D, device=DEV), **kw)
+            out.append((r.dhidden, r.dweight))
+        for a, b in zip(*out):
+            assert torch.isfinite(a.float()).all() and torch.equal(a, b)
+        again = grad(clean, w, *args, reduction="sum", dweight=torch.empty(V, D, device=DEV), **kw)  # and leave nothing behind
+        if not saved:
+            assert torch.equal(again.dweight, out[1][1])
+    assert plan.status() == 0
