@@ -322,3 +322,49 @@ def test_rows_that_give_nothing_may_hold_anything(T, V, D, piece, dtype, saved):
         if not saved:
             assert torch.equal(again.dweight, out[1][1])
     assert plan.status() == 0
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("T,V,D,piece,pad", [(130, 700, 72, 0, 0), (130, 700, 72, 0, 3), (40, 8192, 512, 0, 8), (300, 2000, 33, 1, 0), (1500, 900, 200, 0, 5)])
+def test_gradients_of_16_bits_accumulate(T, V, D, piece, pad, dtype):
+    """Added to what is there in fp32 and rounded once; in rows of any alignment, and nothing beside them."""
+    g = gen(860 + T + pad)
+    h = torch.randn(T, D, generator=g, device=DEV).to(dtype)
+    w = (torch.randn(V, D, generator=g, device=DEV) / math.sqrt(D)).to(dtype)
+    ids = torch.rand(T, V, generator=g, device=DEV).argsort(1)[:, :6].contiguous()
+    teacher = torch.randn(T, 6, generator=g, device=DEV) * 2
+    plan = losses.HeadLoss(T, V, D, dtype, top_k=6, piece_bytes=piece)
+    plain = [torch.zeros(n, D, device=DEV) for n in (T, V)]
+    plan.distill_grad(h, w, ids, teacher, 1.5, reduction="sum", dhidden=plain[0], dweight=plain[1])
+    wide = [torch.randn(n, D + pad, generator=g, device=DEV).to(dtype) for n in (T, V)]
+    old = [x.clone() for x in wide]
+    views = [x[:, pad // 2 : pad // 2 + D] for x in wide]
+    plan.distill_grad(h, w, ids, teacher, 1.5, reduction="sum", dhidden=views[0], dweight=views[1], accumulate=True)
+    for x, before, got, grad in zip(wide, old, views, plain):
+        want = before[:, pad // 2 : pad // 2 + D].double() + grad.double()
+        # the fp32 gradients are the same products: only the sum's two roundings differ
+        within(got, want, 1.01 * U[dtype] * want.abs() + 2.0**-22 * (grad.double().abs() + want.abs()) + TINY[dtype], "sum")
+        x[:, pad // 2 : pad // 2 + D] = before[:, pad // 2 : pad // 2 + D]
+        assert torch.equal(x, before)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("T,V,n,K", [(50, 300, 64, 9), (150, 700, 128, 50), (33, 1100, 72, 64), (300, 2049, 64, 7)])
+def test_distillation_does_not_depend_on_the_pieces(T, V, n, K, dtype):
+    """The rows' losses are the same bits whatever the pieces; gradients differ by what a code may (see factor_error)."""
+    h, w, g = identity_head(T, V, n, dtype, 880 + T)
+    ids = torch.rand(T, V, generator=g, device=DEV).argsort(1)[:, :K].contiguous()
+    teacher = torch.randn(T, K, generator=g, device=DEV) * 3
+    q = torch.zeros(T, V, dtype=torch.float64, device=DEV).scatter_(1, ids, soft_targets(ids, teacher, 1.0))
+    hit = torch.zeros(T, V, dtype=torch.bool, device=DEV).scatter_(1, ids, True)
+    p = torch.softmax(torch.cat([h.double(), torch.zeros(T, V - n, dtype=torch.float64, device=DEV)], 1), 1)
+    f_err = factor_error(p, q, dtype, hit)[:, :n]
+    first = None
+    for piece in (0, 1, 2 * T * 512, 2 * T * 768):
+        plan = losses.HeadLoss(T, V, n, dtype, top_k=K, piece_bytes=piece)
+        dh = torch.empty(T, n, device=DEV)
+        r = plan.distill_grad(h, w, ids, teacher, reduction="sum", dhidden=dh)
+        within(dh, (p - q)[:, :n], f_err + 2.0**-23 * (p - q)[:, :n].abs(), "dhidden")
+        if first is None:
+            first = r
+        assert torch.equal(r.rows, first.rows) and torch.equal(r.lse, first.lse)
