@@ -45,7 +45,7 @@ enum {
   IWP_ERR_OOM = -2,      /* device or host allocation failed */
   IWP_ERR_CUDA = -3,     /* a CUDA runtime call or kernel launch failed */
   IWP_ERR_INTERNAL = -4, /* a device-side conservation check failed (counts do not add up) */
-  IWP_ERR_TIMEOUT = -5,  /* a bounded device-side wait gave up (unused: no kernel here waits) */
+  IWP_ERR_TIMEOUT = -5,  /* a bounded device-side wait gave up (the losses of iwp_loss.h; no kernel of the step waits) */
   IWP_ERR_CAPACITY = -6  /* threshold mode: the index set did not fit the list (see iwp_create_threshold) */
 };
 

@@ -24,8 +24,9 @@ SOURCES = [
 ]
 
 
-# The same library with every computed index range-checked and the histogram counts checked for conservation
-# (a failed check sets the status word; nothing traps).  Loaded instead of libiwp.so when IWP_LIB_VARIANT=debug.
+# The same library with every computed index of the step's kernels range-checked and the histogram counts checked for
+# conservation (a failed check sets the status word; nothing traps), and with a kernel whose bounded waits run out, for the
+# losses' tests.  The losses' kernels have no checks of their own.  Loaded instead of libiwp.so when IWP_LIB_VARIANT=debug.
 LIB_DEBUG = os.path.join(HERE, "libiwp_debug.so")
 
 

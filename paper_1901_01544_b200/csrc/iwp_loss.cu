@@ -707,6 +707,15 @@ extern "C" int iwp_loss_status(const void* state, int32_t* status_host, void* cu
   return IWP_OK;
 }
 
+#ifdef IWP_DEBUG_CHECKS
+// Checked build only: a kernel whose bounded waits run out.  gave_up: int, on the device.
+extern "C" int iwp_loss_wait_probe(void* state, int32_t* gave_up, void* cuda_stream) {
+  if (!state || !gave_up) return IWP_ERR_INVALID;
+  LOSS_CUDA(launch(iwp_tc::k_wait_probe, 1, 64, 0, 1, static_cast<cudaStream_t>(cuda_stream), static_cast<int*>(state), gave_up));
+  return IWP_OK;
+}
+#endif
+
 extern "C" int64_t iwp_head_workspace(const iwp_head_args* a) {
   if (!head_args_ok(a)) return -1;
   return head_plan(a).bytes;

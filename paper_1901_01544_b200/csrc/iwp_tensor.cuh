@@ -105,9 +105,9 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
 }
 
 // Bounded wait; false = gave up (or another role of this CTA did).
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* dead, int* status) {
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* dead, int* status, uint32_t tries = WAIT_TRIES) {
   if (mbar_try(bar, parity)) return true;
-  for (uint32_t i = 0; i < WAIT_TRIES; i++) {
+  for (uint32_t i = 0; i < tries; i++) {
     if (mbar_try(bar, parity)) return true;
     if (*dead) return false;
   }
@@ -115,6 +115,20 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
   atomicExch(status, IWP_ERR_TIMEOUT);
   return false;
 }
+
+#ifdef IWP_DEBUG_CHECKS
+// For the test of the waits: two warps wait for a barrier that nothing arrives on, one of them at most 40 ms.
+__global__ void __launch_bounds__(64) k_wait_probe(int* status, int* gave_up) {
+  __shared__ uint64_t bar;
+  __shared__ volatile int dead;
+  if (threadIdx.x == 0) {
+    mbar_init(smem_u32(&bar), 1);
+    dead = 0;
+  }
+  __syncthreads();
+  if (threadIdx.x % 32 == 0 && !mbar_wait(smem_u32(&bar), 0, &dead, status, threadIdx.x == 0 ? 2000u : WAIT_TRIES)) atomicAdd(gave_up, 1);
+}
+#endif
 
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
   asm volatile(
