@@ -34,8 +34,9 @@ int iwp_loss_status(const void* state, int32_t* status_host, void* cuda_stream);
 
 /* ---- output head with its loss ---------------------------------------------------------------------
  *
- * logits z[t][v] = <hidden[t], weight[v]>, never kept: they exist tile by tile in tensor memory, and as the
- * probabilities of one piece of the vocabulary (at most piece_bytes) while the gradients of that piece are formed.
+ * logits z[t][v] = <hidden[t], weight[v]> exist tile by tile in tensor memory; forward passes keep none of them.  While
+ * the gradients of a piece of the vocabulary are formed, its probabilities are held in 16 bits: at most piece_bytes, by
+ * default up to max(1 GiB, 4 V D bytes), which for many vocabularies is all of them.
  * Row t has sparse targets (i_k, q_k), sum of q = 1, or none.  With tau = temperature (1 for the cross entropy)
  *   lse[t]  = log sum_v exp(z[t][v] / tau)
  *   rows[t] = tau^2 * sum_k q_k (log q_k - z[t][i_k] / tau + lse[t])      (a row without targets: 0)
@@ -88,13 +89,15 @@ typedef struct iwp_head_args {
   int32_t top_k, ids_bytes, top_type; /* 1 <= top_k <= 1024 */
   int32_t dhidden_type, dweight_type; /* dtype or IWP_F32 */
   int32_t mean;                    /* 1 = mean over rows with targets, 0 = sum */
+                                   /* (outputs overlap neither inputs nor one another) */
   int32_t accumulate;              /* 1 = the gradients are added to what dhidden and dweight hold */
   int32_t have_lse;                /* 1 = lse is given: no forward pass, loss and rows are not written */
 } iwp_head_args;
 
 /* Bytes of workspace a call with these arguments needs (pointers matter only by being NULL or not, and by their
- * alignment: operands whose rows do not start at multiples of 16 bytes are first copied to rows that do).  It does
- * not shrink when tokens grow.  -1 = invalid arguments. */
+ * alignment: operands whose rows do not start at multiples of 16 bytes are first copied to rows that do): the
+ * statistics, T D elements where dweight is asked for, the probabilities of a piece, and 78 MB or 4 T D bytes for
+ * partial sums where dhidden is.  It does not shrink when tokens grow.  -1 = invalid arguments. */
 int64_t iwp_head_workspace(const iwp_head_args* args);
 
 /* Loss, and the gradients that are not NULL.  Asynchronous on cuda_stream.  Errors: IWP_ERR_INVALID (sizes, NULL,

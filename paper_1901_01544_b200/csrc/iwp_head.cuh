@@ -809,7 +809,7 @@ struct Factors {
 constexpr int FACTOR_THREADS = 256, FACTOR_DEEP = 4, FACTOR_COLUMNS = 8 * FACTOR_THREADS * FACTOR_DEEP;
 
 // A block takes FACTOR_COLUMNS columns of one row: bound by memory, 2 bytes in and 2 out per element (4096 x 32768: 78 us =
-// 6.9 TB/s with the end of the codes still in the L2; with 64 targets per row to look through, 88 us).
+// 6.9 TB/s with the end of the codes still in the L2; with 64 targets per row to look through, 90 us).
 __global__ void __launch_bounds__(FACTOR_THREADS) k_factors(const Factors a) {
   constexpr int MINE = (MAX_TOP + FACTOR_THREADS - 1) / FACTOR_THREADS, WARPS = FACTOR_THREADS / 32;
   const int tid = threadIdx.x;
@@ -905,7 +905,7 @@ constexpr int FEW_TOKENS = 2, FEW_THREADS = 512, FEW_ROWS = 4;
 
 // Four rows of the weights per warp at a time, streamed once: dot products with one or two tokens are bound by the weights'
 // bytes, and plain loads keep more of them in flight than the tensor cores' 128-row tiles would (131072 x 4096, one token:
-// 162 us = 6.6 TB/s, against 253 by tiles; two tokens 178 and 214; from three on, tiles are as fast).  A group of 8
+// 165 us = 6.5 TB/s, against 253 by tiles; two tokens 183 and 214; from three on, tiles are as fast).  A group of 8
 // elements is widened once per row and once per token.  Operand rows start at multiples of 16 bytes and hold whole ones
 // (copies made by k_align_rows end in zeros).
 template <int TOKENS>

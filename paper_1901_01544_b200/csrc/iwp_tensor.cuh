@@ -13,9 +13,9 @@
 // tensor memory it may read, the other half of the columns for warps 8..11).  Two accumulator tiles of 256 columns
 // fill the 512 columns of tensor memory, so the epilogue of one tile runs beside the products of the next.
 //
-// Bound by the tensor cores for K of about 1000 and more, and there by power: the logits of 8192 x 131072 x 4096 take 5.63 ms
-// alone (1.56 PFLOP/s), its two gradients 12.3 ms (1.43), in a loop both settle near 1.3, as a library product does
-// (1.37). 1024 x 50176 x 1024: logits 71 us (1.49 PFLOP/s, tensor pipe 69 % active), dhidden 79, dweight 85. Below K of 500
+// Bound by the tensor cores for K of about 1000 and more, and there by power: the logits of 8192 x 131072 x 4096 take 5.6 ms
+// alone (1.57 PFLOP/s), its two gradients 13.0 ms (1.35), in a loop both settle near 1.3, as a library product does
+// (1.37). 1024 x 50176 x 1024: logits 70 us (1.5 PFLOP/s; 80 with codes), dhidden 84, dweight 87. Below K of 500
 // an epilogue (7000 clocks for 256 x 256 logits with their exponentials) takes longer than a tile's products.
 //
 // Every wait is bounded: a wait that runs out sets the status word and marks the CTA dead; the roles then fall
@@ -309,8 +309,8 @@ __device__ __forceinline__ bool tile_at(const Problems<N>& w, int pair, int pair
 // Tensor cores cut what a term loses against the running sum, so long sums of one sign come out low: with K = 131072 by up to
 // 1.4e-3 of themselves, with 8192 by 1.5e-5, 1024 by 1e-6.  With SUMS the tensor memory is therefore emptied into registers
 // every `seg` blocks of K (at most 1024 elements) and added up there, in fp32 rounded to nearest, while the products go on in
-// the other accumulator; tile() gets an array of pairs of columns.  Without, for K of one segment, it gets an address in
-// tensor memory.
+// the other accumulator; tile() gets an array of pairs of columns.  (dhidden of 1024 x 50176 x 1024: 84 us, 78 without;
+// segments of 4096 take the same.)  Without, for K of one segment, it gets an address in tensor memory.
 struct Where {
   int row0;     // first of the warp's 32 rows; the lane's row is row0 + lane
   int col0;     // first of the warp's columns

@@ -204,12 +204,14 @@ class _Plan:
 
 
 class HeadLoss(_Plan):
-    """Output head [vocab, dim] with its loss; the logits are never kept.
+    """Output head [vocab, dim] with its loss.  Forward passes keep no logits; gradients hold the probabilities of a piece of
+    the vocabulary in 16 bits while they are formed, of all of it where `piece_bytes` allows.
 
     tokens: the most rows a call will bring; top_k: the most teacher logits per row.  The first call makes a workspace
     that serves forward passes of that size; the first gradient (or a call that needs more) makes a larger one.
-    piece_bytes: bound on the probabilities held at a time while gradients are formed (0 = 1 GiB, or what the weights and
-    their gradient take where that is more)."""
+    piece_bytes: bound on the probabilities held at a time (0 = 1 GiB, or 4 vocab dim bytes, what the weights and their
+    gradient take, where that is more).  A plan that has formed gradients keeps a workspace of that, the partial sums
+    (78 MB or more) and copies of the hidden states."""
 
     def __init__(self, tokens: int, vocab: int, dim: int, dtype=None, top_k: int = 1, piece_bytes: int = 0):
         super().__init__()
