@@ -368,8 +368,8 @@ struct OutArgs {
   OutMatrix m[2];
 };
 
-// LONG: for K of several segments, whose sums are in registers and leave fewer of them to the stores: 300 x 8060 x 1031 takes
-// 116 us with them and 106 without, so products of one segment do without.
+// LONG: for K of several segments, whose sums are in registers and leave fewer of them to the stores: 3001 x 8060 x 1031 takes
+// 200 us with them and 193 without, so products of one segment do without.
 template <bool LONG>
 struct Out {
   static constexpr bool SUMS = LONG;
@@ -425,6 +425,7 @@ struct Out {
     }
     iwp_tc::staging_free<0>(w.lane);
     char* const out = static_cast<char*>(a.out) + w.split * a.split_stride * (a.type == IWP_F32 ? 4 : 2);
+    const bool half = a.type != IWP_F32 && !a.add;  // staged in 16 bits
     // 64 columns at a time, after which the sums in registers move up: one copy of the many ways to store, and room for it
 #pragma unroll 1
     for (int c = 0; c < end; c += 64) {
@@ -433,7 +434,10 @@ struct Out {
         if (c + i < end) {
           float v[32];
           take(sums, LONG ? i : c + i, f, v);
-          iwp_tc::stage_chunk(v, w.staging + i / 32 * iwp_tc::STAGING_BYTES, a.type, a.add, w.lane);
+          if (half)
+            iwp_tc::stage_chunk(v, w.staging, w.lane, i / 8, a.type);
+          else
+            iwp_tc::stage_chunk(v, w.staging + i / 32 * iwp_tc::STAGING_BYTES, w.lane);
         }
       }
       if constexpr (LONG) {
@@ -441,6 +445,13 @@ struct Out {
         for (int j = 0; j < 32; j++) sums[j] = sums[j + 32];
       }
       __syncwarp();
+      if (half) {
+        if (w.row0 < a.rows)
+          iwp_tc::write_rows16(w.staging, reinterpret_cast<uint16_t*>(out) + w.row0 * a.ld + w.col0 + c, a.ld, a.wide, w.row0, a.rows, min(64, end - c),
+                               w.lane);
+        __syncwarp();
+        continue;
+      }
 #pragma unroll 1
       for (int i = 0; i < min(64, end - c); i += 32)
         iwp_tc::write_chunk<LONG ? 4 : 8>(w.staging + i / 32 * iwp_tc::STAGING_BYTES, out, a.ld, a.type, a.wide, a.add, w.row0, a.rows, w.col0 + c + i, a.cols, w.lane);

@@ -582,38 +582,65 @@ __device__ __forceinline__ void store_staged(const CUtensorMap* map, char* stagi
   }
 }
 
-// A chunk of 32 columns (v: this lane's row) into the warp's staging rows: fp32 where it is written or added to as such, else
-// of the 16-bit `type`.
-__device__ __forceinline__ void stage_chunk(const float (&v)[32], char* staging, int type, bool add, int lane) {
-  if (type == 0 || add) {
+// A chunk of 32 columns (v: this lane's row) into the warp's staging rows, in fp32, or in 16 bits from the 16-byte word `word`
+// of the row on.
+__device__ __forceinline__ void stage_chunk(const float (&v)[32], char* staging, int lane) {
 #pragma unroll
-    for (int j = 0; j < 8; j++) *reinterpret_cast<float4*>(staged(staging, lane, j)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-  } else {
+  for (int j = 0; j < 8; j++) *reinterpret_cast<float4*>(staged(staging, lane, j)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+}
+__device__ __forceinline__ void stage_chunk(const float (&v)[32], char* staging, int lane, int word, int type) {
 #pragma unroll
-    for (int j = 0; j < 4; j++)
-      *reinterpret_cast<uint4*>(staged(staging, lane, j)) =
-          make_uint4(pack2(v[8 * j], v[8 * j + 1], type), pack2(v[8 * j + 2], v[8 * j + 3], type), pack2(v[8 * j + 4], v[8 * j + 5], type),
-                     pack2(v[8 * j + 6], v[8 * j + 7], type));
-  }
+  for (int j = 0; j < 4; j++)
+    *reinterpret_cast<uint4*>(staged(staging, lane, word + j)) =
+        make_uint4(pack2(v[8 * j], v[8 * j + 1], type), pack2(v[8 * j + 2], v[8 * j + 3], type), pack2(v[8 * j + 4], v[8 * j + 5], type),
+                   pack2(v[8 * j + 6], v[8 * j + 7], type));
 }
 
-// A staged chunk to a row-major matrix, in whole 32-byte sectors where rows are `wide` (start at multiples of 16 bytes); rows
-// and columns outside are dropped.  TYPE: IWP_F32 / IWP_BF16 / IWP_F16.  `add`: the old contents are added first (in fp32;
-// all of a thread's on their way at once, since the compiler cannot tell that a store does not touch them).  The
-// caller synchronises the warp before and after.
+// n staged columns of 16 bits (at most 64) to a row-major matrix; rows outside are dropped, the caller synchronises the warp
+// before and after.  32 columns in rows that start at multiples of 16 bytes (`wide`): 8 rows of 64 bytes at a time.  Otherwise
+// one or two rows at a time in the 4-byte words of memory; of a row that starts in the middle of one, its first and its last column are
+// stored on their own.
+__device__ __forceinline__ void write_rows16(char* staging, uint16_t* out, int64_t ld, bool wide, int row0, int rows, int n, int lane) {
+  if (wide && n == 32) {
+    const int r = lane >> 2, c = lane & 3;
+#pragma unroll
+    for (int i = 0; i < 32; i += 8) {
+      const uint4 x = *reinterpret_cast<const uint4*>(staged(staging, r + i, c));
+      if (row0 + r + i < rows) *reinterpret_cast<uint4*>(out + (r + i) * ld + 8 * c) = x;
+    }
+    return;
+  }
+  auto words = [&](auto lanes) {  // of a row
+    constexpr int LANES = decltype(lanes)::value, STEP = 32 / LANES;
+    const int c = lane % LANES;
+    uint16_t* row = out + lane / LANES * ld;
+#pragma unroll 4
+    for (int i = lane / LANES; i < 32; i += STEP, row += STEP * ld) {
+      if (row0 + i >= rows) continue;
+      const int odd = static_cast<int>(reinterpret_cast<uintptr_t>(row) >> 1 & 1), k = 2 * c + odd;
+      auto at = [&](int k) { return *reinterpret_cast<const uint16_t*>(staged(staging, i, k >> 3) + 2 * (k & 7)); };
+      if (k + 1 < n)
+        *reinterpret_cast<uint32_t*>(row + k) = at(k) | static_cast<uint32_t>(at(k + 1)) << 16;
+      else if (k < n)
+        row[k] = at(k);
+      if (odd && c == 0) row[0] = at(0);
+    }
+  };
+  if (n > 32)
+    words(std::integral_constant<int, 32>{});
+  else
+    words(std::integral_constant<int, 16>{});
+}
+
+// A chunk staged in fp32 to a row-major matrix, in whole 32-byte sectors where rows are `wide`; rows and columns outside are
+// dropped.  TYPE: IWP_F32, or the 16 bits of a sum.  `add`: the old contents are added first (in fp32; all of a batch on
+// their way at once, since the compiler cannot tell that a store does not touch them).  The caller synchronises the warp before
+// and after.
 template <int BATCH>
 __device__ __forceinline__ void write_chunk(char* staging, void* out, int64_t ld, int type, bool wide, bool add, int row0, int rows, int col0,
                                             int cols, int lane) {
   const bool whole = wide && col0 + 32 <= cols;
-  if (whole && type != 0 && !add) {
-    const int r = lane >> 2, c = lane & 3;  // 8 rows of 64 bytes at a time
-#pragma unroll
-    for (int i = 0; i < 32; i += 8) {
-      const uint4 x = *reinterpret_cast<const uint4*>(staged(staging, r + i, c));
-      if (row0 + r + i < rows)
-        *reinterpret_cast<uint4*>(static_cast<char*>(out) + 2 * ((row0 + r + i) * ld + col0) + 16 * c) = x;
-    }
-  } else if (whole && type == 0) {
+  if (whole && type == 0) {
     const int r = lane >> 3, c = lane & 7;  // 4 rows of 128 bytes at a time
     float* p = static_cast<float*>(out) + (row0 + r) * ld + col0 + 4 * c;
 #pragma unroll 1
@@ -630,22 +657,6 @@ __device__ __forceinline__ void write_chunk(char* staging, void* out, int64_t ld
         if (add) x = make_float4(x.x + old[i].x, x.y + old[i].y, x.z + old[i].z, x.w + old[i].w);
         if (row0 + r + h + 4 * i < rows) *reinterpret_cast<float4*>(p + 4 * i * ld) = x;
       }
-    }
-  } else if (type != 0 && !add) {
-    // ragged columns or unaligned rows of 16 bits: two rows at a time, in the 4-byte words of memory; of a row that starts
-    // in the middle of one, its first and its last column are stored on their own
-    const int half = lane >> 4, c = lane & 15;
-    for (int i = half; i < 32; i += 2) {
-      if (row0 + i >= rows) break;
-      uint16_t* const row = static_cast<uint16_t*>(out) + (row0 + i) * ld + col0;
-      const int odd = static_cast<int>(reinterpret_cast<uintptr_t>(row) >> 1 & 1);
-      auto at = [&](int k) { return *reinterpret_cast<const uint16_t*>(staged(staging, i, k >> 3) + 2 * (k & 7)); };
-      const int k = 2 * c + odd;
-      if (k + 1 < 32 && col0 + k + 1 < cols)
-        *reinterpret_cast<uint32_t*>(row + k) = at(k) | static_cast<uint32_t>(at(k + 1)) << 16;
-      else if (k < 32 && col0 + k < cols)
-        row[k] = at(k);
-      if (odd && c == 0 && col0 < cols) row[0] = at(0);
     }
   } else if (type == 0) {  // ragged columns or unaligned rows of fp32: a row at a time
     if (col0 + lane < cols) {
