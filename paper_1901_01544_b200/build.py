@@ -11,16 +11,20 @@ LIB = os.path.join(HERE, "libiwp.so")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 STEP_DEPS = [os.path.join(CSRC, f) for f in ("iwp_api.cu", "iwp_device.cuh", "iwp_stream.cuh", "iwp_sample.cuh", "iwp_select.cuh", "iwp_reduce.cuh",
                                             "iwp_threshold.cuh", "iwp_wire.cuh", "iwp_plan.hpp")] + [os.path.join(INCLUDE, "iwp.h")]
-LOSS_DEPS = [os.path.join(CSRC, f) for f in ("iwp_loss.cu", "iwp_tensor.cuh", "iwp_head.cuh", "iwp_balance.cuh")] + [
+LOSS_DEPS = [os.path.join(CSRC, f) for f in ("iwp_loss.cu", "iwp_tensor.cuh", "iwp_head.cuh", "iwp_balance.cuh", "iwp_host.hpp")] + [
     os.path.join(INCLUDE, f) for f in ("iwp_loss.h", "iwp.h")]
-DEPS = STEP_DEPS + LOSS_DEPS
+AROUND_DEPS = [os.path.join(CSRC, f) for f in ("iwp_route.cu", "iwp_route.cuh", "iwp_exchange.cuh", "iwp_clip.cu", "iwp_clip.cuh", "iwp_elem.cuh")] + [
+    os.path.join(INCLUDE, f) for f in ("iwp_route.h", "iwp_clip.h")]
+DEPS = STEP_DEPS + LOSS_DEPS + AROUND_DEPS
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC"]
 # The step is bit-exact against its oracle: IEEE arithmetic, no FMA contraction, correctly rounded division, denormals
-# kept.  The losses are held to tolerances and use the compiler's defaults.
+# kept.  The losses, the router and the clipping are held to tolerances and use the compiler's defaults.
 SOURCES = [
     (os.path.join(CSRC, "iwp_api.cu"), ["-fmad=false", "-prec-div=true", "-prec-sqrt=true", "-ftz=false"]),
     (os.path.join(CSRC, "iwp_loss.cu"), []),
+    (os.path.join(CSRC, "iwp_route.cu"), []),
+    (os.path.join(CSRC, "iwp_clip.cu"), []),
 ]
 
 

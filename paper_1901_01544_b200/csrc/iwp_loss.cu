@@ -8,16 +8,11 @@
 
 #include "iwp_balance.cuh"
 #include "iwp_head.cuh"
+#include "iwp_host.hpp"
 
 namespace {
 
-#define LOSS_CUDA(expr)            \
-  do {                             \
-    if ((expr) != cudaSuccess) {   \
-      cudaGetLastError();          \
-      return IWP_ERR_CUDA;         \
-    }                              \
-  } while (0)
+using namespace iwp_host;
 
 constexpr int64_t ROOM = 0xFFFF;                 // how far 32-bit positions may run beyond a size
 constexpr int64_t MAX_SIZE = 0x7FFFFFFF - ROOM;  // of tokens, vocabulary, width and strides
@@ -30,10 +25,6 @@ static_assert(2 * iwp_tc::TILE_N <= ROOM && iwp_head::FACTOR_COLUMNS + iwp_tc::T
               "positions of the kernels' last steps stay within 32 bits");
 constexpr int64_t FEW_ELEMENTS = 32768;   // of hidden states, which stay in 64 KB of shared memory
 constexpr int64_t JOIN_TILES = 2 * 148;  // a split dhidden has at most this many partial tiles
-
-inline int64_t up_to(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
-inline int64_t tiles_of(int64_t x, int64_t t) { return (x + t - 1) / t; }
-inline bool aligned(const void* p, int64_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 // cuTensorMapEncodeTiled through the runtime, so that the library links against no driver stub.
 using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -66,32 +57,6 @@ bool make_map(CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int64
 }
 
 constexpr int SEGMENT = 1024 / iwp_tc::BLOCK_K;  // most blocks of K that are summed in tensor memory
-
-constexpr int MAX_DEVICES = 64;
-
-int device() {
-  int dev = -1;
-  return cudaGetDevice(&dev) == cudaSuccess && dev < MAX_DEVICES ? dev : -1;
-}
-
-// Launches with programmatic serialisation: the kernel may start while the one before it drains.
-template <class... Params, class... Args>
-cudaError_t launch(void (*kernel)(Params...), int64_t grid, int block, size_t smem, int cluster, cudaStream_t st, Args&&... args) {
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(static_cast<unsigned>(grid));
-  cfg.blockDim = dim3(static_cast<unsigned>(block));
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute at[2];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  at[1].id = cudaLaunchAttributeClusterDimension;
-  at[1].val.clusterDim.x = static_cast<unsigned>(cluster);
-  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = cluster > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
-}
 
 // How many CTA pairs of a product kernel the device holds at once: the persistent grid (a pair that had to wait for
 // another to end would double the time).  Looked up once per device, with the kernel's shared memory limit.

@@ -138,6 +138,10 @@ def _vector(x, name: str, n: int, dtypes, device) -> None:
 
 
 class _Plan:
+    """What plans share: the state and the workspace of their calls, and the streams these are used on."""
+
+    _state_bytes, _reset_entry = LOSS_STATE, "iwp_loss_reset"
+
     def __init__(self):
         torch, self._codes = _types()
         if not torch.cuda.is_available():
@@ -154,10 +158,10 @@ class _Plan:
         self._floats = tuple(self._codes)
         self._ids = (torch.int64, torch.int32)
         self._raw_stream = torch._C._cuda_getCurrentRawStream  # current_stream() without the object around it
-        self._state = torch.empty(LOSS_STATE, dtype=torch.uint8, device=self.device)
+        self._state = torch.empty(self._state_bytes, dtype=torch.uint8, device=self.device)
         self._index = self.device.index
         self._state_at, self._last = self._state.data_ptr(), self._raw_stream(self._index)
-        _check(self._lib.iwp_loss_reset(self._state_at, self._last), "iwp_loss_reset")
+        _check(getattr(self._lib, self._reset_entry)(self._state_at, self._last), self._reset_entry)
         self._made = torch.cuda.Event()
         self._made.record()
 
@@ -169,11 +173,14 @@ class _Plan:
             # allocator before that stream is done with it
             now = self._torch.cuda.current_stream(self.device)
             now.wait_event(self._made)
-            for x in (self._state, self._ws):
+            for x in self._memory():
                 if x is not None:
                     x.record_stream(now)
             self._last = s
         return s
+
+    def _memory(self):
+        return self._state, self._ws
 
     def _plan(self, need: int) -> None:
         if need < 0:
@@ -200,7 +207,7 @@ class _Plan:
         _check(self.status(), type(self).__name__)
 
     def reset(self) -> None:
-        _check(lib().iwp_loss_reset(self._state_at, self._stream()), "iwp_loss_reset")
+        _check(getattr(self._lib, self._reset_entry)(self._state_at, self._stream()), self._reset_entry)
 
 
 class HeadLoss(_Plan):
@@ -408,10 +415,10 @@ class ExpertBalance(_Plan):
 # ---- differentiable forms (once: a second derivative is refused) --------------------------------------
 
 
-def _functions():
-    """autograd.Function classes around the plans, made on first use (importing this module does not import torch)."""
-    global _autograd
-    if _autograd is None:
+def _once():
+    """The autograd.Function that refuses second derivatives, made on first use (importing this module does not import torch)."""
+    global _refuses
+    if _refuses is None:
         import torch
 
         class Once(torch.autograd.Function):
@@ -425,6 +432,21 @@ def _functions():
             @staticmethod
             def backward(ctx, *_):
                 raise RuntimeError("the losses' gradients cannot be differentiated again")
+
+        _refuses = Once
+    return _refuses
+
+
+_refuses = None
+
+
+def _functions():
+    """autograd.Function classes around the plans, made on first use."""
+    global _autograd
+    if _autograd is None:
+        import torch
+
+        Once = _once()
 
         class Head(torch.autograd.Function):
             @staticmethod
