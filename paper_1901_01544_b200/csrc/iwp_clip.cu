@@ -3,6 +3,8 @@
 #include <atomic>
 #include <cmath>
 #include <cstring>
+#include <memory>
+#include <new>
 
 #include "iwp_clip.cuh"
 #include "iwp_host.hpp"
@@ -22,12 +24,15 @@ constexpr int64_t SMALL_ELEMENTS = int64_t(1) << 18;
 int size_of(int type) { return type == IWP_F32 ? 4 : 2; }
 bool is_type(int type) { return type == IWP_F32 || type == IWP_BF16 || type == IWP_F16; }
 
-// Elements of a part: enough parts for every warp that the GPU holds at once (or that the cluster has) where that leaves
-// something to stream per lane, and not so many that adding up their sums counts.
-int64_t part_elements(int64_t total) {
-  const int64_t warps = total <= SMALL_ELEMENTS ? MAX_CLUSTER * (K::SMALL_THREADS / 32) : int64_t(SMS) * 64;
-  return std::min<int64_t>(16384, std::max<int64_t>(512, up_to(tiles_of(total, warps), 256)));
+// Warps that share the elements out: all that the two passes run at once (or that the cluster has), but with something to
+// stream for each.
+constexpr int64_t LEAST_RANGE = 512;
+int64_t warps_of(int64_t total) {
+  const int64_t most = total <= SMALL_ELEMENTS ? MAX_CLUSTER * (K::SMALL_THREADS / 32) : int64_t(4) * SMS * K::WARPS;
+  return std::min(most, tiles_of(total, LEAST_RANGE));
 }
+// Elements of a warp's range.
+int64_t range_of(int64_t total) { return total ? up_to(tiles_of(total, warps_of(total)), 64) : 0; }
 
 bool tensor_ok(const iwp_clip_tensor& t, int groups) {
   if (t.rows < 0 || t.cols < 0 || t.group < 0 || t.group >= groups || !is_type(t.in_type)) return false;
@@ -38,55 +43,86 @@ bool tensor_ok(const iwp_clip_tensor& t, int groups) {
   return is_type(t.out_type) && aligned(t.out, size_of(t.out_type)) && (t.rows == 1 || (t.out_ld >= t.cols && t.out_ld <= MAX_LD));
 }
 
-// Calls f(part) for every part of a tensor; counts them if f is a counter.
+// Walks over all elements, by group and in a group by tensor, and calls f(warp, part) for every part in that order.
 template <class F>
-void each_part(iwp_clip_tensor t, int64_t size, const F& f) {
-  if (t.rows == 0 || t.cols == 0) return;
-  if (t.rows > 1 && t.in_ld == t.cols && (!t.out || t.out_ld == t.cols)) t.cols *= t.rows, t.rows = 1;
-  const int64_t cols = std::min(t.cols, size), rows = std::max<int64_t>(1, t.cols > size ? 1 : size / t.cols);
-  for (int64_t r = 0; r < t.rows; r += rows)
-    for (int64_t c = 0; c < t.cols; c += cols) {
+void each_part(const iwp_clip_tensor* tensors, const int64_t* order, int64_t n, int64_t range, const F& f) {
+  constexpr int64_t MOST = int64_t(1) << 30;
+  int64_t at = 0;  // elements so far
+  for (int64_t o = 0; o < n; o++) {
+    iwp_clip_tensor t = tensors[order[o]];
+    if (t.rows == 0 || t.cols == 0) continue;
+    if (t.rows > 1 && t.in_ld == t.cols && (!t.out || t.out_ld == t.cols)) t.cols *= t.rows, t.rows = 1;
+    for (int64_t r = 0, c = 0; r < t.rows;) {
+      const int64_t left = std::min(MOST, range - at % range);
+      int64_t rows = 1, cols = std::min(t.cols - c, left);
+      if (c == 0 && left >= t.cols) rows = std::min(t.rows - r, left / t.cols);  // whole rows
       K::Part p{};
       p.in = static_cast<const char*>(t.in) + (r * t.in_ld + c) * size_of(t.in_type);
       p.out = t.out ? static_cast<char*>(t.out) + (r * t.out_ld + c) * size_of(t.out_type) : nullptr;
       p.in_ld = t.in_ld;
       p.out_ld = t.out ? t.out_ld : 0;
-      p.rows = static_cast<int>(std::min(rows, t.rows - r));
-      p.cols = static_cast<int>(std::min(cols, t.cols - c));
+      p.rows = static_cast<int>(rows);
+      p.cols = static_cast<int>(cols);
       p.group = t.group;
       p.in_type = static_cast<int16_t>(t.in_type);
       p.out_type = static_cast<int16_t>(t.out ? t.out_type : t.in_type);
-      f(p);
+      f(at / range, p);
+      at += rows * cols;
+      c += cols;
+      if (c == t.cols) c = 0, r += rows;
     }
+  }
 }
 
-int64_t parts_of(iwp_clip_tensor t, int64_t size) {
+// Tensors by group, in the order they are given in.
+std::unique_ptr<int64_t[]> order_of(const iwp_clip_tensor* tensors, int64_t n) {
+  std::unique_ptr<int64_t[]> order(new (std::nothrow) int64_t[n + 1]);
+  if (!order) return nullptr;
+  for (int64_t i = 0; i < n; i++) order[i] = i;
+  std::sort(order.get(), order.get() + n, [&](int64_t a, int64_t b) { return tensors[a].group != tensors[b].group ? tensors[a].group < tensors[b].group : a < b; });
+  return order;
+}
+
+// Most parts that each_part() makes of a tensor: a strided matrix is cut at the ends of rows and of ranges.
+int64_t most_parts(const iwp_clip_tensor& t, int64_t range) {
   if (t.rows == 0 || t.cols == 0) return 0;
-  if (t.rows > 1 && t.in_ld == t.cols && (!t.out || t.out_ld == t.cols)) t.cols *= t.rows, t.rows = 1;
-  return t.cols > size ? t.rows * tiles_of(t.cols, size) : tiles_of(t.rows, size / t.cols);
+  return t.rows == 1 ? 2 + t.cols / range + (t.cols >> 30) : 4 + 3 * (t.rows * t.cols / range) + (t.cols > range ? 2 * t.rows : 0) + (t.rows * t.cols >> 29);
 }
 
-int64_t firsts_at(int64_t parts) { return up_to(parts * int64_t(sizeof(K::Part)), 256); }
+struct Table {
+  int64_t parts, spans, bytes;  // offsets
+};
+Table table_of(int64_t warps, int64_t parts, int64_t groups) {
+  Table t;
+  t.parts = warps * int64_t(sizeof(K::Start));
+  t.spans = t.parts + parts * int64_t(sizeof(K::Part));
+  t.bytes = up_to(t.spans + groups * int64_t(sizeof(int2)), 256);
+  return t;
+}
 
 }  // namespace
 
 extern "C" int iwp_clip_layout(const iwp_clip_tensor* tensors, int64_t n, int32_t groups, iwp_clip_sizes* sizes) {
   if (!sizes || n < 0 || (n && !tensors) || groups < 1 || groups > MAX_GROUPS) return IWP_ERR_INVALID;
-  int64_t total = 0, parts = 0;
+  int64_t total = 0, most = 0;
   for (int64_t i = 0; i < n; i++) {
     if (!tensor_ok(tensors[i], groups)) return IWP_ERR_INVALID;
     total += tensors[i].rows * tensors[i].cols;
     if (total > MAX_ELEMENTS) return IWP_ERR_INVALID;
   }
-  const int64_t size = part_elements(total);
+  const int64_t range = range_of(total);
   for (int64_t i = 0; i < n; i++) {
-    parts += parts_of(tensors[i], size);
-    if (parts > MAX_PARTS) return IWP_ERR_INVALID;
+    most += most_parts(tensors[i], range);
+    if (most > MAX_PARTS) return IWP_ERR_INVALID;
   }
+  const auto order = order_of(tensors, n);
+  if (!order) return IWP_ERR_OOM;
+  int64_t parts = 0;
+  each_part(tensors, order.get(), n, range, [&](int64_t, const K::Part&) { parts++; });
   sizes->parts = parts;
   sizes->elements = total;
-  sizes->table_bytes = firsts_at(parts) + up_to(4 * (int64_t(groups) + 1), 256);
-  sizes->workspace_bytes = up_to(std::max<int64_t>(8 * parts, 8), 256);
+  sizes->table_bytes = table_of(warps_of(total), parts, groups).bytes;
+  sizes->workspace_bytes = up_to(8 * (warps_of(total) + groups), 256);
   return IWP_OK;
 }
 
@@ -95,16 +131,31 @@ extern "C" int iwp_clip_table(const iwp_clip_tensor* tensors, int64_t n, int32_t
   if (const int e = iwp_clip_layout(tensors, n, groups, &sizes)) return e;
   if (!table || !aligned(table, 8)) return IWP_ERR_INVALID;
   if (table_bytes < sizes.table_bytes) return IWP_ERR_CAPACITY;
+  const auto order = order_of(tensors, n);
+  if (!order) return IWP_ERR_OOM;
   std::memset(table, 0, sizes.table_bytes);
-  const int64_t size = part_elements(sizes.elements);
-  int* const first = reinterpret_cast<int*>(static_cast<char*>(table) + firsts_at(sizes.parts));
-  // by group, and in a group by tensor: first[g] counts up from the group's first part while the parts are laid out
-  for (int64_t i = 0; i < n; i++) first[tensors[i].group + 1] += static_cast<int>(parts_of(tensors[i], size));
-  for (int g = 0; g < groups; g++) first[g + 1] += first[g];
-  for (int64_t i = 0; i < n; i++)
-    each_part(tensors[i], size, [&](const K::Part& p) { std::memcpy(static_cast<char*>(table) + int64_t(first[p.group]++) * sizeof p, &p, sizeof p); });
-  for (int g = groups; g > 0; g--) first[g] = first[g - 1];  // each is now where the next begins
-  first[0] = 0;
+  const int64_t warps = warps_of(sizes.elements);
+  const Table at = table_of(warps, sizes.parts, groups);
+  char* const base = static_cast<char*>(table);
+  auto* const spans = reinterpret_cast<int2*>(base + at.spans);
+  int64_t last = -1, i = 0;
+  each_part(tensors, order.get(), n, range_of(sizes.elements), [&](int64_t w, const K::Part& p) {
+    std::memcpy(base + at.parts + i * int64_t(sizeof p), &p, sizeof p);
+    auto* const start = reinterpret_cast<K::Start*>(base) + w;
+    i++;
+    if (w != last) {
+      std::memcpy(&start->part, &p, sizeof p);
+      start->next = static_cast<int>(i);
+      last = w;
+    }
+    start->end = static_cast<int>(i);
+    int2& span = spans[p.group];
+    const int place = static_cast<int>(w) + p.group;
+    if (span.y == 0) span.x = place;
+    span.y = place + 1;
+  });
+  // (a range rounded up may leave the last warps without elements)
+  for (int64_t w = last + 1; w < warps; w++) reinterpret_cast<K::Start*>(base)[w].end = -1;
   return IWP_OK;
 }
 
@@ -114,16 +165,20 @@ extern "C" int iwp_clip(const iwp_clip_args* a, void* cuda_stream) {
   if (!aligned(a->factors, 4) || (a->write && !a->factors) || !a->state || !aligned(a->state, 256)) return IWP_ERR_INVALID;
   if (!a->workspace || !aligned(a->workspace, 256)) return IWP_ERR_INVALID;
   if (!(a->max_norm >= 0.) || !std::isfinite(a->scale) || a->scale == 0.) return IWP_ERR_INVALID;
-  if (a->workspace_bytes < 8 * a->parts) return IWP_ERR_CAPACITY;
+  const int64_t warps = warps_of(a->elements);
+  if (a->workspace_bytes < 8 * (warps + a->groups)) return IWP_ERR_CAPACITY;
+  const Table at = table_of(warps, a->parts, a->groups);
+  const char* const table = static_cast<const char*>(a->table);
   K::Args r{};
   r.hdr = static_cast<K::Header*>(a->state);
-  r.parts = static_cast<const K::Part*>(a->table);
-  r.first = reinterpret_cast<const int*>(static_cast<const char*>(a->table) + firsts_at(a->parts));
+  r.starts = reinterpret_cast<const K::Start*>(table);
+  r.parts = reinterpret_cast<const K::Part*>(table + at.parts);
+  r.spans = reinterpret_cast<const int2*>(table + at.spans);
   r.sums = static_cast<double*>(a->workspace);
+  r.warps = static_cast<int>(warps);
   r.squares = a->squares;
   r.norms = a->norms;
   r.factors = a->factors;
-  r.count = a->parts;
   r.max_norm = a->max_norm;
   r.scale = a->scale;
   r.groups = a->groups;
@@ -131,7 +186,7 @@ extern "C" int iwp_clip(const iwp_clip_args* a, void* cuda_stream) {
   r.have_squares = a->have_squares != 0;
   r.drop = a->drop_nonfinite != 0;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  if (a->elements <= SMALL_ELEMENTS && a->parts <= 4096 && a->groups <= 4096) {
+  if (a->elements <= SMALL_ELEMENTS && a->groups <= 4096) {
     static std::atomic<int> largest[MAX_DEVICES] = {};
     const int dev = device();
     if (dev < 0) return IWP_ERR_CUDA;
@@ -151,15 +206,14 @@ extern "C" int iwp_clip(const iwp_clip_args* a, void* cuda_stream) {
       largest[dev] = n > 0 ? MAX_CLUSTER : 8;
     }
     int ctas = 1;
-    while (ctas < largest[dev] && ctas * (K::SMALL_THREADS / 32) < a->parts) ctas *= 2;
+    while (ctas < largest[dev] && ctas * (K::SMALL_THREADS / 32) < warps) ctas *= 2;
     LOSS_CUDA(launch(K::k_small, ctas, K::SMALL_THREADS, 0, ctas, st, r));
     return IWP_OK;
   }
-  const int64_t blocks = std::max<int64_t>(1, tiles_of(a->parts, K::WARPS));
-  if (a->have_squares)
-    LOSS_CUDA(launch(K::k_factors, std::min<int64_t>(tiles_of(a->groups, K::THREADS), SMS), K::THREADS, 0, 1, st, r));
-  else
-    LOSS_CUDA(launch(K::k_squares, std::min<int64_t>(blocks, 8 * SMS), K::THREADS, 0, 1, st, r));
-  if (a->write && a->parts) LOSS_CUDA(launch(K::k_scale, std::min<int64_t>(blocks, 6 * SMS), K::THREADS, 0, 1, st, r));
+  const int64_t blocks = std::max<int64_t>(1, tiles_of(warps, K::WARPS));
+  if (!a->have_squares) LOSS_CUDA(launch(K::k_squares, blocks, K::THREADS, 0, 1, st, r));
+  if (a->have_squares || a->groups > K::FEW_GROUPS)
+    LOSS_CUDA(launch(K::k_groups, std::min<int64_t>(tiles_of(a->groups, K::WARPS), 8 * SMS), K::THREADS, 0, 1, st, r));
+  if (a->write && warps) LOSS_CUDA(launch(K::k_scale, blocks, K::THREADS, 0, 1, st, r));
   return IWP_OK;
 }

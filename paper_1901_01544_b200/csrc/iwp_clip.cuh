@@ -1,8 +1,9 @@
 // iwp_clip.cuh - sums of squares of many tensors in groups, and the tensors times their group's factor.
 //
-// The tensors are cut into parts of one group each, and a warp takes a part.  Both passes are bound by memory.  Squares are
-// added up eight at a time in fp32 and from there on in 64 bits: no sum of gradients that are finite overflows, and
-// eights whose squares leave fp32's range are taken in 64 bits from the start.
+// The elements are shared out evenly: a warp has one contiguous range of them, group after group and tensor after tensor, cut
+// into parts where tensors, strided rows or the range end.  Both passes are bound by memory.  Squares are added up eight
+// at a time in fp32 and from there on in 64 bits: no sum of gradients that are finite overflows, and eights whose squares
+// leave fp32's range are taken in 64 bits from the start.
 #pragma once
 
 #include <cooperative_groups.h>
@@ -28,22 +29,32 @@ struct alignas(16) Part {
 };
 static_assert(sizeof(Part) == 48, "part");
 
+// A warp's parts: one here, so that it is there after a single read, and parts [next, end) of the list.
+struct alignas(16) Start {
+  Part part;
+  int next, end;
+  int fill[2];
+};
+static_assert(sizeof(Start) == 64, "start");
+
 struct Header {
   int status;
   uint32_t ticket;  // wraps to zero with the last block of a launch
 };
 
+// Warp w leaves its sum over elements of group g at w + g: from one of its groups to the next g grows, and from one warp to
+// the next w does, so no two share a place.  A group's sums are at [span.x, span.y).
 struct Args {
   Header* hdr;
+  const Start* starts;  // [warps]
   const Part* parts;
-  const int* first;  // [groups + 1]: the first part of each group
-  double* sums;      // [parts]
+  const int2* spans;  // [groups]
+  double* sums;       // [warps + groups]
   double* squares;
   float* norms;
   float* factors;
-  int64_t count;  // of parts
   double max_norm, scale;
-  int groups, write, have_squares, drop;
+  int warps, groups, write, have_squares, drop;
 };
 
 template <int TYPE>
@@ -65,17 +76,17 @@ __device__ __forceinline__ void add_squares(const float (&x)[N], double& sum) {
   }
 }
 
-// Elements until p is at a multiple of 16 bytes, at most n.
-template <int SIZE>
+// Elements until p is at a multiple of TO bytes, at most n.
+template <int SIZE, int TO = 16>
 __device__ __forceinline__ int until_aligned(const void* p, int n) {
-  const int e = static_cast<int>((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / SIZE;
+  const int e = static_cast<int>((TO - (reinterpret_cast<uintptr_t>(p) & (TO - 1))) & (TO - 1)) / SIZE;
   return e < n ? e : n;
 }
 
 template <int TYPE>
 __device__ __forceinline__ void square_run(const void* from, int n, int lane, double& sum) {
   using T = typename Of<TYPE>::T;
-  constexpr int VEC = 16 / sizeof(T), WORDS = 8 / VEC, AHEAD = 4;  // eight elements: one or two words
+  constexpr int VEC = 16 / sizeof(T), WORDS = 8 / VEC, AHEAD = 8 / WORDS;  // eight elements: one or two words; eight words in flight
   const T* p = static_cast<const T*>(from);
   const int head = until_aligned<sizeof(T)>(p, n);
   if (lane < head) {
@@ -84,31 +95,27 @@ __device__ __forceinline__ void square_run(const void* from, int n, int lane, do
   }
   p += head, n -= head;
   const Word<TYPE, VEC>* const w = reinterpret_cast<const Word<TYPE, VEC>*>(p);
-  const int eights = n / 8;
-  int i = lane;
-  // a warp's lanes read neighbouring words: word u of an eight is 32 further
-  for (; i - lane + 32 * AHEAD <= eights; i += 32 * AHEAD) {
+  const int words = n / VEC;
+  // a warp's lanes read neighbouring words; word u of a lane's eight is 32 further
+  for (int i = lane; i < words; i += 32 * WORDS * AHEAD) {
     Word<TYPE, VEC> y[AHEAD][WORDS];
 #pragma unroll
     for (int a = 0; a < AHEAD; a++)
 #pragma unroll
-      for (int u = 0; u < WORDS; u++) y[a][u] = w[(i - lane + 32 * a) * WORDS + 32 * u + lane];
+      for (int u = 0; u < WORDS; u++) {
+        const int at = i + 32 * (a * WORDS + u);
+        y[a][u] = w[at < words ? at : 0];
+      }
 #pragma unroll
     for (int a = 0; a < AHEAD; a++) {
       float x[8];
 #pragma unroll
-      for (int v = 0; v < 8; v++) x[v] = value<TYPE>(y[a][v / VEC].x[v % VEC]);
-      add_squares<TYPE, 8>(x, sum);
+      for (int v = 0; v < 8; v++) x[v] = i + 32 * (a * WORDS + v / VEC) < words ? value<TYPE>(y[a][v / VEC].x[v % VEC]) : 0.f;
+      if (i + 32 * a * WORDS < words) add_squares<TYPE, 8>(x, sum);
     }
   }
-  for (; i < eights; i += 32) {
-    float x[8];
-#pragma unroll
-    for (int v = 0; v < 8; v++) x[v] = value<TYPE>(w[i * WORDS + v / VEC].x[v % VEC]);
-    add_squares<TYPE, 8>(x, sum);
-  }
-  if (lane < n - eights * 8) {
-    const float x[1] = {value<TYPE>(p[eights * 8 + lane])};
+  if (lane < n - words * VEC) {
+    const float x[1] = {value<TYPE>(p[words * VEC + lane])};
     add_squares<TYPE, 1>(x, sum);
   }
 }
@@ -119,9 +126,8 @@ __device__ __forceinline__ double sum_of(double x) {
 }
 
 template <int TYPE>
-__device__ __forceinline__ double square_part(const Part& q, int lane) {
+__device__ __forceinline__ void square_part(const Part& q, int lane, double& sum) {
   using T = typename Of<TYPE>::T;
-  double sum = 0;
   if (q.rows == 1 || q.cols >= 256) {
     for (int r = 0; r < q.rows; r++) square_run<TYPE>(static_cast<const T*>(q.in) + r * q.in_ld, q.cols, lane, sum);
   } else {
@@ -131,13 +137,15 @@ __device__ __forceinline__ double square_part(const Part& q, int lane) {
       add_squares<TYPE, 1>(x, sum);
     }
   }
-  return sum_of(sum);
 }
 
-__device__ __forceinline__ double square(const Part& q, int lane) {
-  if (q.in_type == IWP_F32) return square_part<IWP_F32>(q, lane);
-  if (q.in_type == IWP_BF16) return square_part<IWP_BF16>(q, lane);
-  return square_part<IWP_F16>(q, lane);
+__device__ __forceinline__ void square(const Part& q, int lane, double& sum) {
+  if (q.in_type == IWP_F32)
+    square_part<IWP_F32>(q, lane, sum);
+  else if (q.in_type == IWP_BF16)
+    square_part<IWP_BF16>(q, lane, sum);
+  else
+    square_part<IWP_F16>(q, lane, sum);
 }
 
 template <int IN, int OUT>
@@ -149,44 +157,39 @@ template <int IN, int OUT>
 __device__ __forceinline__ void scale_run(const void* from, void* to, int n, int lane, float f) {
   using T = typename Of<IN>::T;
   using U = typename Of<OUT>::T;
-  constexpr int VI = 16 / sizeof(T), VO = 16 / sizeof(U), AHEAD = 2;
-  constexpr int V = VI > VO ? VI : VO;  // elements a lane takes at a time: whole words of both
+  // elements of a lane's word: 16 bytes of the wider type, so that a warp's loads and its stores are both contiguous
+  constexpr int V = 16 / (sizeof(T) > sizeof(U) ? sizeof(T) : sizeof(U)), AHEAD = 4;
+  using WI = Word<IN, V>;
+  using WO = Word<OUT, V>;
   const T* p = static_cast<const T*>(from);
   U* q = static_cast<U*>(to);
-  const int head = until_aligned<sizeof(U)>(q, n);
-  if (until_aligned<sizeof(T)>(p + head, 1) == 0) {  // both at multiples of 16 bytes from there on
+  const int head = until_aligned<sizeof(U), sizeof(WO)>(q, n);
+  if (until_aligned<sizeof(T), sizeof(WI)>(p + head, 1) == 0) {  // both at multiples of their words from there on
     if (lane < head) q[lane] = scaled<IN, OUT>(p[lane], f);
     p += head, q += head, n -= head;
-    const int groups = n / V;
-    for (int i = lane; i < groups; i += 32 * AHEAD) {
-      Word<IN, VI> x[AHEAD][V / VI];
+    const int words = n / V;
+    const WI* const wi = reinterpret_cast<const WI*>(p);
+    WO* const wo = reinterpret_cast<WO*>(q);
+    for (int i = lane; i < words; i += 32 * AHEAD) {
+      WI x[AHEAD];
 #pragma unroll
-      for (int a = 0; a < AHEAD; a++)
-        if (i + 32 * a < groups) {
+      for (int a = 0; a < AHEAD; a++) x[a] = wi[i + 32 * a < words ? i + 32 * a : i];
 #pragma unroll
-          for (int u = 0; u < V / VI; u++) x[a][u] = reinterpret_cast<const Word<IN, VI>*>(p)[(i + 32 * a) * (V / VI) + u];
-        }
+      for (int a = 0; a < AHEAD; a++) {
+        WO y;
 #pragma unroll
-      for (int a = 0; a < AHEAD; a++)
-        if (i + 32 * a < groups) {
-#pragma unroll
-          for (int u = 0; u < V / VO; u++) {
-            Word<OUT, VO> y;
-#pragma unroll
-            for (int v = 0; v < VO; v++) y.x[v] = scaled<IN, OUT>(x[a][(u * VO + v) / VI].x[(u * VO + v) % VI], f);
-            reinterpret_cast<Word<OUT, VO>*>(q)[(i + 32 * a) * (V / VO) + u] = y;
-          }
-        }
+        for (int v = 0; v < V; v++) y.x[v] = scaled<IN, OUT>(x[a].x[v], f);
+        if (i + 32 * a < words) wo[i + 32 * a] = y;
+      }
     }
-    if (lane < n - groups * V) q[groups * V + lane] = scaled<IN, OUT>(p[groups * V + lane], f);
+    if (lane < n - words * V) q[words * V + lane] = scaled<IN, OUT>(p[words * V + lane], f);
     return;
   }
   constexpr int SINGLE = 8;
   for (int i = lane; i < n; i += 32 * SINGLE) {
     T x[SINGLE];
 #pragma unroll
-    for (int a = 0; a < SINGLE; a++)
-      if (i + 32 * a < n) x[a] = p[i + 32 * a];
+    for (int a = 0; a < SINGLE; a++) x[a] = p[i + 32 * a < n ? i + 32 * a : i];
 #pragma unroll
     for (int a = 0; a < SINGLE; a++)
       if (i + 32 * a < n) q[i + 32 * a] = scaled<IN, OUT>(x[a], f);
@@ -227,14 +230,34 @@ __device__ __forceinline__ void scale(const Part& q, int lane, float f) {
     scale_from<IWP_F16>(q, lane, f);
 }
 
-// A group's sum over its parts, by a warp: lanes take every 32nd part, then the lanes are added.
+// A group's sum, by a warp: lanes take every 32nd of the warps' sums, then the lanes are added.
 __device__ __forceinline__ double group_sum(const Args& a, int group, int lane) {
   if (a.have_squares) return a.squares[group];
   double s = 0;
-  const int end = a.first[group + 1];
+  const int2 span = a.spans[group];
 #pragma unroll 8
-  for (int i = a.first[group] + lane; i < end; i += 32) s += __ldcg(a.sums + i);
+  for (int i = span.x + lane; i < span.y; i += 32) s += __ldcg(a.sums + i);
   return sum_of(s);
+}
+
+// Sums of warp w's range.
+__device__ __forceinline__ void square_range(const Args& a, int w, int lane) {
+  const Start start = a.starts[w];
+  if (start.end < 0) return;  // nothing left for this warp
+  Part q = start.part;
+  double sum = 0;
+  for (int i = start.next;; i++) {
+    const bool more = i < start.end;
+    const Part ahead = more ? a.parts[i] : q;
+    square(q, lane, sum);
+    if (!more || ahead.group != q.group) {
+      sum = sum_of(sum);
+      if (lane == 0) __stcg(a.sums + w + q.group, sum);
+      sum = 0;
+    }
+    if (!more) return;
+    q = ahead;
+  }
 }
 
 struct Outcome {
@@ -258,16 +281,17 @@ __device__ __forceinline__ void finish_group(const Args& a, int group, double sq
   if (a.factors) a.factors[group] = o.factor;
 }
 
-// Sums, and in the last block to finish the groups' norms and factors.
-__global__ void __launch_bounds__(THREADS, 5) k_squares(const Args a) {
+// Few groups: the last block to finish adds up the warps' sums (up to FEW_GROUPS).  Many: a launch of
+// its own, a warp per group.
+constexpr int FEW_GROUPS = 8;
+
+__global__ void __launch_bounds__(THREADS, 4) k_squares(const Args a) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  launch_next();
   wait_previous();
-  const int64_t stride = static_cast<int64_t>(gridDim.x) * WARPS;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * WARPS + warp; i < a.count; i += stride) {
-    const double s = square(a.parts[i], lane);
-    if (lane == 0) a.sums[i] = s;
-  }
+  launch_next();  // after the wait: k_scale may read the table while this kernel runs
+  const int w = blockIdx.x * WARPS + warp;
+  if (w < a.warps) square_range(a, w, lane);
+  if (a.groups > FEW_GROUPS) return;
   __shared__ bool last;
   __threadfence();
   __syncthreads();
@@ -275,19 +299,12 @@ __global__ void __launch_bounds__(THREADS, 5) k_squares(const Args a) {
   __syncthreads();
   if (!last) return;
   __threadfence();
-  if (a.groups >= WARPS) {
-    for (int g = warp; g < a.groups; g += WARPS) {
-      const double s = group_sum(a, g, lane);
-      if (lane == 0) finish_group(a, g, s);
-    }
-    return;
-  }
   __shared__ double part[WARPS];
-  for (int g = 0; g < a.groups; g++) {  // few groups: the whole block sums each
+  for (int g = 0; g < a.groups; g++) {
     double s = 0;
-    const int end = a.first[g + 1];
-#pragma unroll 8
-    for (int i = a.first[g] + threadIdx.x; i < end; i += THREADS) s += __ldcg(a.sums + i);
+    const int2 span = a.spans[g];
+#pragma unroll 16
+    for (int i = span.x + threadIdx.x; i < span.y; i += THREADS) s += __ldcg(a.sums + i);
     s = sum_of(s);
     if (lane == 0) part[warp] = s;
     __syncthreads();
@@ -300,53 +317,62 @@ __global__ void __launch_bounds__(THREADS, 5) k_squares(const Args a) {
   }
 }
 
-// Norms and factors from sums that are given.
-__global__ void __launch_bounds__(THREADS) k_factors(const Args a) {
-  launch_next();
+__global__ void __launch_bounds__(THREADS) k_groups(const Args a) {
+  const int lane = threadIdx.x & 31;
   wait_previous();
-  for (int g = blockIdx.x * THREADS + threadIdx.x; g < a.groups; g += gridDim.x * THREADS) finish_group(a, g, a.squares[g]);
+  launch_next();
+  for (int g = blockIdx.x * WARPS + threadIdx.x / 32; g < a.groups; g += gridDim.x * WARPS) {
+    const double s = group_sum(a, g, lane);
+    if (lane == 0) finish_group(a, g, s);
+  }
 }
 
-// Back to front: what the sums read last is still in the L2.
-__global__ void __launch_bounds__(THREADS, 4) k_scale(const Args a) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  launch_next();
+// Each warp its range again, back to front: what the sums read last may still be in the L2.
+__device__ __forceinline__ void scale_range(const Args& a, int w, int lane) {
+  const Start start = a.starts[w];
   wait_previous();
-  const int64_t stride = static_cast<int64_t>(gridDim.x) * WARPS;
-  for (int64_t i = a.count - 1 - (static_cast<int64_t>(blockIdx.x) * WARPS + warp); i >= 0; i -= stride) {
-    const Part& q = a.parts[i];
-    scale(q, lane, __ldcg(a.factors + q.group));
+  int group = -1;
+  float f = 0.f;
+  for (int i = start.end - 1; i >= start.next - 1; i--) {
+    const Part q = i >= start.next ? a.parts[i] : start.part;
+    if (q.group != group) group = q.group, f = __ldcg(a.factors + group);
+    scale(q, lane, f);
   }
+}
+
+__global__ void __launch_bounds__(THREADS, 4) k_scale(const Args a) {
+  const int lane = threadIdx.x & 31, w = blockIdx.x * WARPS + threadIdx.x / 32;
+  launch_next();
+  if (w < a.warps)
+    scale_range(a, w, lane);
+  else
+    wait_previous();
 }
 
 // All of it in one launch of one cluster, for little work.
 __global__ void __launch_bounds__(SMALL_THREADS) k_small(const Args a) {
   const int lane = threadIdx.x & 31, warps = gridDim.x * (SMALL_THREADS / 32);
-  const int warp = (threadIdx.x >> 5) * gridDim.x + blockIdx.x;  // neighbouring parts in different CTAs
+  const int warp = (threadIdx.x >> 5) * gridDim.x + blockIdx.x;  // neighbouring ranges in different CTAs
   cg::cluster_group cluster = cg::this_cluster();
   launch_next();
   wait_previous();
-  if (!a.have_squares) {
-    for (int64_t i = warp; i < a.count; i += warps) {
-      const double s = square(a.parts[i], lane);
-      if (lane == 0) __stcg(a.sums + i, s);
-    }
-    cluster.sync();
-  }
+  if (!a.have_squares)
+    for (int w = warp; w < a.warps; w += warps) square_range(a, w, lane);
+  cluster.sync();
   for (int g = warp; g < a.groups; g += warps) {
     const double s = group_sum(a, g, lane);
     if (lane == 0) finish_group(a, g, s);
   }
   if (!a.write) return;
-  int group = -1;
+  int group = -1;  // the factors again: no second barrier
   float f = 0.f;
-  for (int64_t i = warp; i < a.count; i += warps) {
-    const Part& q = a.parts[i];
-    if (q.group != group) {
-      group = q.group;
-      f = outcome(a, group_sum(a, group, lane)).factor;
+  for (int w = warp; w < a.warps; w += warps) {
+    const Start start = a.starts[w];
+    for (int i = start.next - 1; i < start.end; i++) {
+      const Part q = i >= start.next ? a.parts[i] : start.part;
+      if (q.group != group) group = q.group, f = outcome(a, group_sum(a, group, lane)).factor;
+      scale(q, lane, f);
     }
-    scale(q, lane, f);
   }
 }
 

@@ -150,8 +150,7 @@ int exchange(const iwp_exchange_args* a, int what, cudaStream_t st) {
     const int64_t words = a->dim / VEC;
     X::RowArgs q = r;
     if (what == COMBINE_GRAD) {
-      int threads = 32;
-      while (threads < X::ROW_THREADS && threads < words) threads *= 2;
+      const int threads = static_cast<int>(std::min<int64_t>(X::ROW_THREADS, up_to(words, 32)));
       const int64_t blocks = std::min<int64_t>(a->tokens, int64_t(16) * SMS * X::ROW_THREADS / threads);
       if (a->top_k <= 8)
         LOSS_CUDA(launch(X::k_combine_grad<TYPE, VEC, 8>, blocks, threads, 0, 1, st, q));
@@ -159,14 +158,18 @@ int exchange(const iwp_exchange_args* a, int what, cudaStream_t st) {
         LOSS_CUDA(launch(X::k_combine_grad<TYPE, VEC, 32>, blocks, threads, 0, 1, st, q));
       return IWP_OK;
     }
+    if (what == COMBINE) {
+      const int threads = static_cast<int>(std::min<int64_t>(X::ROW_THREADS, up_to(words, 32)));
+      q.parts = static_cast<int>(tiles_of(words, threads));
+      const int64_t blocks = std::min<int64_t>(a->tokens * q.parts, int64_t(6) * SMS * X::ROW_THREADS / threads);
+      LOSS_CUDA(launch(X::k_combine<TYPE, VEC>, blocks, threads, 0, 1, st, q));
+      return IWP_OK;
+    }
     // few tokens: several warps share a row, down to a word per lane
     q.parts = 1;
     while (a->tokens * q.parts < int64_t(8) * SMS * X::ROW_WARPS && words / (2 * q.parts) >= 32) q.parts *= 2;
     const int64_t blocks = std::min<int64_t>(tiles_of(a->tokens * q.parts, X::ROW_WARPS), int64_t(8) * SMS);
-    if (what == DISPATCH)
-      LOSS_CUDA(launch(X::k_dispatch<TYPE, VEC>, blocks, X::ROW_THREADS, 0, 1, st, q));
-    else
-      LOSS_CUDA(launch(X::k_combine<TYPE, VEC>, blocks, X::ROW_THREADS, 0, 1, st, q));
+    LOSS_CUDA(launch(X::k_dispatch<TYPE, VEC>, blocks, X::ROW_THREADS, 0, 1, st, q));
     return IWP_OK;
   });
 }
@@ -287,9 +290,9 @@ extern "C" int iwp_order(const iwp_order_args* a, void* cuda_stream) {
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const int smem = 4 * X::ORDER_WARPS * r.E;
   static std::atomic<int> allowed[MAX_DEVICES] = {};
-  LOSS_CUDA(allow_shared(X::k_order_place, 4 * X::ORDER_WARPS * X::MAX_EXPERTS, allowed));
+  LOSS_CUDA(allow_shared(X::k_order_place<4>, 4 * X::ORDER_WARPS * X::MAX_EXPERTS, allowed));
   if (blocks > 1) LOSS_CUDA(launch(X::k_order_count, blocks, X::ORDER_THREADS, 0, 1, st, r));
-  LOSS_CUDA(launch(X::k_order_place, blocks, X::ORDER_THREADS, smem, 1, st, r));
+  LOSS_CUDA(launch(X::k_order_place<4>, blocks, X::ORDER_THREADS, smem, 1, st, r));
   return IWP_OK;
 }
 

@@ -85,6 +85,12 @@ class Order(NamedTuple):
     rows: object
 
 
+class _Made(Order):
+    """An order that a plan has made: what its tensors are is known."""
+
+    experts = 0
+
+
 class _Here(_Plan):
     """A plan whose calls are refused while another device than its own is current."""
 
@@ -192,6 +198,12 @@ class ExpertExchange(_Here):
         self._plan(self._lib.iwp_order_workspace(C.byref(a)))
         self._order_at = C.addressof(a)
 
+        def entry(name):
+            args = ExchangeArgs(experts=self.experts)  # of every call
+            return args, C.addressof(args), getattr(self._lib, name)
+
+        self._dispatch, self._combine, self._combine_grad = entry("iwp_dispatch"), entry("iwp_combine"), entry("iwp_combine_grad")
+
     def order(self, ids) -> Order:
         """Slots of the pairs (t, j) with ids [T, k]; ids outside the experts belong to none."""
         t, dev, a = self._torch, self.device, self._order_args
@@ -212,57 +224,62 @@ class ExpertExchange(_Here):
         status = self._lib.iwp_order(self._order_at, stream)
         if status:
             raise IwpError(status, "iwp_order")
-        return Order(offsets, slots, rows)
+        order = _Made(offsets, slots, rows)
+        order.experts = self.experts
+        return order
 
-    def _exchange(self, order: Order, x, by: str):
-        """Arguments of an exchange; x: [T, D] by token or [T k, D] by slot."""
-        t, dev = self._torch, self.device
-        T, k = order.slots.shape
-        _vector(order.slots, "slots", T * k, (t.int32,), dev)
-        _vector(order.offsets, "offsets", self.experts + 1, (t.int32,), dev)
-        if x.dim() != 2:
-            raise ValueError(f"{by} is a matrix")
-        a = ExchangeArgs(tokens=T, dim=x.shape[1], slots=order.slots.data_ptr(), offsets=order.offsets.data_ptr(), experts=self.experts, top_k=k)
-        return a, T, k, x.shape[1]
+    def _begin(self, a: ExchangeArgs, order: Order, x, name: str):
+        """T, k and the width of x, a matrix, in an exchange by `order`."""
+        offsets, slots, _ = order
+        if slots.dim() != 2 or x.dim() != 2:
+            raise ValueError(f"slots and {name} are matrices")
+        if type(order) is not _Made or order.experts != self.experts:
+            _vector(slots, "slots", slots.numel(), self._ids[1:], self.device)
+            _vector(offsets, "offsets", self.experts + 1, self._ids[1:], self.device)
+        T, k = slots.shape
+        a.tokens, a.top_k, a.dim, a.slots, a.offsets = T, k, x.shape[1], slots.data_ptr(), offsets.data_ptr()
+        return T, k, x.shape[1]
 
-    def _take(self, a: ExchangeArgs, field: str, x, name: str, shape, dtypes) -> None:
-        setattr(a, field + "_ld", _rows_of(x, name, shape, dtypes, self.device))
-        setattr(a, field, x.data_ptr() or 256)
-
-    def _out(self, a: ExchangeArgs, field: str, out, shape, dtype):
-        if out is None:
-            out = self._torch.empty(shape, dtype=dtype, device=self.device)
-        self._take(a, field, out, "out", shape, (dtype,))
-        return out
-
-    def _weights(self, a: ExchangeArgs, weights, T: int, k: int) -> None:
-        if weights is not None:
-            self._take(a, "weights", weights, "weights", (T, k), self._floats[:1])
-
-    def _call(self, entry: str, a: ExchangeArgs) -> None:
+    def _end(self, a: ExchangeArgs, at: int, call, entry: str) -> None:
         if a.tokens == 0 or a.dim == 0:
             return
-        status = getattr(self._lib, entry)(C.addressof(a), self._stream())
+        status = call(at, self._stream())
         if status:
             raise IwpError(status, entry)
 
     def dispatch(self, x, order: Order, *, out=None):
         """Rows [T k, D] in the order of the slots: x [T, D] of each slot's token; zero behind the last slot."""
-        a, T, k, D = self._exchange(order, x, "x")
-        self._take(a, "by_token", x, "x", (T, D), self._floats)
-        a.type = self._codes[x.dtype]
-        out = self._out(a, "by_slot_out", out, (T * k, D), x.dtype)
-        self._call("iwp_dispatch", a)
+        a, at, call = self._dispatch
+        T, k, D = self._begin(a, order, x, "x")
+        a.by_token_ld = _rows_of(x, "x", (T, D), self._floats, self.device)
+        a.by_token, a.type = x.data_ptr(), self._codes[x.dtype]
+        if out is None:
+            out = x.new_empty((T * k, D))
+            a.by_slot_out_ld = D
+        else:
+            a.by_slot_out_ld = _rows_of(out, "out", (T * k, D), (x.dtype,), self.device)
+        a.by_slot_out = out.data_ptr()
+        self._end(a, at, call, "iwp_dispatch")
         return out
 
     def combine(self, z, order: Order, weights=None, *, out=None):
         """Rows [T, D]: the sum of each token's rows of z [T k, D], times weights [T, k] float32 (1 if None)."""
-        a, T, k, D = self._exchange(order, z, "z")
-        self._take(a, "by_slot", z, "z", (T * k, D), self._floats)
-        self._weights(a, weights, T, k)
-        a.type = self._codes[z.dtype]
-        out = self._out(a, "by_token_out", out, (T, D), z.dtype)
-        self._call("iwp_combine", a)
+        a, at, call = self._combine
+        T, k, D = self._begin(a, order, z, "z")
+        a.by_slot_ld = _rows_of(z, "z", (T * k, D), self._floats, self.device)
+        a.by_slot, a.type = z.data_ptr(), self._codes[z.dtype]
+        if weights is None:
+            a.weights = None
+        else:
+            a.weights_ld = _rows_of(weights, "weights", (T, k), self._floats[:1], self.device)
+            a.weights = weights.data_ptr()
+        if out is None:
+            out = z.new_empty((T, D))
+            a.by_token_out_ld = D
+        else:
+            a.by_token_out_ld = _rows_of(out, "out", (T, D), (z.dtype,), self.device)
+        a.by_token_out = out.data_ptr()
+        self._end(a, at, call, "iwp_combine")
         return out
 
     def dispatch_grad(self, dout, order: Order, *, out=None):
@@ -271,20 +288,30 @@ class ExpertExchange(_Here):
 
     def combine_grad(self, dy, z, order: Order, weights=None, *, out=None, want=("rows", "weights")):
         """The gradients ([T k, D] to z, [T, k] float32 to the weights) of `combine`; None where `want` leaves one out."""
-        t = self._torch
-        a, T, k, D = self._exchange(order, dy, "dy")
-        self._take(a, "by_token", dy, "dy", (T, D), self._floats)
-        a.type = self._codes[dy.dtype]
-        self._weights(a, weights, T, k)
-        dz = dw = None
+        a, at, call = self._combine_grad
+        T, k, D = self._begin(a, order, dy, "dy")
+        a.by_token_ld = _rows_of(dy, "dy", (T, D), self._floats, self.device)
+        a.by_token, a.type = dy.data_ptr(), self._codes[dy.dtype]
+        if weights is None:
+            a.weights = None
+        else:
+            a.weights_ld = _rows_of(weights, "weights", (T, k), self._floats[:1], self.device)
+            a.weights = weights.data_ptr()
+        dz = dw = a.by_slot = a.by_slot_out = a.dweights = None
         if "rows" in want:
-            dz = out = self._out(a, "by_slot_out", out, (T * k, D), dy.dtype)
+            if out is None:
+                dz = dy.new_empty((T * k, D))
+                a.by_slot_out_ld = D
+            else:
+                dz = out
+                a.by_slot_out_ld = _rows_of(dz, "out", (T * k, D), (dy.dtype,), self.device)
+            a.by_slot_out = dz.data_ptr()
         if "weights" in want:
-            self._take(a, "by_slot", z, "z", (T * k, D), (dy.dtype,))
-            dw = t.empty(T, k, dtype=t.float32, device=self.device)
-            a.dweights = dw.data_ptr() or 256
+            a.by_slot_ld = _rows_of(z, "z", (T * k, D), (dy.dtype,), self.device)
+            dw = self._torch.empty(T, k, dtype=self._torch.float32, device=self.device)
+            a.by_slot, a.dweights = z.data_ptr(), dw.data_ptr()
         if dz is not None or dw is not None:
-            self._call("iwp_combine_grad", a)
+            self._end(a, at, call, "iwp_combine_grad")
         return dz, dw
 
 

@@ -120,7 +120,7 @@ def test_nothing_and_too_little(L):
     need = L.iwp_order_workspace(made(routing.OrderArgs, ORDER, {}))
     assert need > 0 and L.iwp_order_workspace(made(routing.OrderArgs, ORDER, dict(experts=0))) == -1 and L.iwp_order_workspace(None) == -1
     assert L.iwp_order(made(routing.OrderArgs, ORDER, dict(workspace_bytes=need - 1)), None) == binding.IWP_ERR_CAPACITY
-    assert L.iwp_clip(made(clipping.ClipArgs, CLIP, dict(parts=100, workspace_bytes=799)), None) == binding.IWP_ERR_CAPACITY
+    assert L.iwp_clip(made(clipping.ClipArgs, CLIP, dict(elements=100_000, workspace_bytes=8 * (-(-100_000 // 512) + 1) - 1)), None) == binding.IWP_ERR_CAPACITY
     for entry in ("iwp_route_grad", "iwp_dispatch", "iwp_combine", "iwp_combine_grad"):  # no tokens: nothing to do, no launch
         cls, base = (routing.RouteGradArgs, GRAD) if entry == "iwp_route_grad" else (routing.ExchangeArgs, ROWS)
         assert getattr(L, entry)(made(cls, base, dict(tokens=0)), None) == binding.IWP_OK
@@ -134,7 +134,12 @@ class Part(C.Structure):
                 ("group", C.c_int32), ("in_type", C.c_int16), ("out_type", C.c_int16)]
 
 
+class Start(C.Structure):
+    _fields_ = [("part", Part), ("next", C.c_int32), ("end", C.c_int32), ("fill", C.c_int32 * 2)]
+
+
 def table_of(L, tensors, groups):
+    """Parts of each warp, in order, and where each group's sums are."""
     arr = (clipping.ClipTensor * max(1, len(tensors)))(*tensors)
     sizes = clipping.ClipSizes()
     assert L.iwp_clip_layout(arr, len(tensors), groups, C.byref(sizes)) == binding.IWP_OK
@@ -142,9 +147,15 @@ def table_of(L, tensors, groups):
     assert L.iwp_clip_table(arr, len(tensors), groups, raw, sizes.table_bytes - 1) == binding.IWP_ERR_CAPACITY
     assert L.iwp_clip_table(arr, len(tensors), groups, raw, sizes.table_bytes) == binding.IWP_OK
     at = C.addressof(raw)
-    parts = [p for p in (Part * sizes.parts).from_address(at)] if sizes.parts else []
-    first = list((C.c_int32 * (groups + 1)).from_address(at + (sizes.parts * C.sizeof(Part) + 255) // 256 * 256))
-    return sizes, [Part.from_buffer_copy(p) for p in parts], first, raw
+    n = sizes.elements
+    warps = min(256 if n <= 1 << 18 else 4736, -(-n // 512))
+    starts = [Start.from_buffer_copy(s) for s in (Start * warps).from_address(at)] if warps else []
+    at += warps * C.sizeof(Start)
+    parts = [Part.from_buffer_copy(p) for p in (Part * sizes.parts).from_address(at)] if sizes.parts else []
+    at += sizes.parts * C.sizeof(Part)
+    spans = [tuple(s) for s in (C.c_int32 * 2 * groups).from_address(at)]
+    assert at + 8 * groups <= C.addressof(raw) + sizes.table_bytes
+    return sizes, [[s.part] + parts[s.next : s.end] if s.end >= 0 else [] for s in starts], spans, parts
 
 
 @pytest.mark.parametrize("total", [0, 5, 5000, 300_000, 40_000_000])
@@ -157,13 +168,19 @@ def test_every_element_is_in_one_part_of_its_group(L, total):
         tensors.append(clipping.ClipTensor(at, 2 * at, rows, cols, ld, ld, rng.choice([0, 1, 3]), rng.choice([0, 1, 2]), rng.choice([0, 1, 2])))
         at += rows * ld * 4 + 64
         left -= rows * cols
-    sizes, parts, first, _ = table_of(L, tensors, groups)
-    assert sizes.elements == sum(t.rows * t.cols for t in tensors) and len(parts) == sizes.parts and sizes.workspace_bytes >= 8 * sizes.parts
-    assert first[0] == 0 and first[-1] == len(parts) and first == sorted(first)
+    sizes, warps, spans, listed = table_of(L, tensors, groups)
+    assert sizes.elements == sum(t.rows * t.cols for t in tensors) and sizes.workspace_bytes >= 8 * (len(warps) + groups)
+    parts = [p for w in warps for p in w]
+    assert bytes(b"".join(parts)) == bytes(b"".join(listed))
+    # a warp's sum over a group has a place of its own, among the group's
+    places = [(w + p.group, w, p.group) for w, mine in enumerate(warps) for p in mine]
+    assert len({q[0] for q in places}) == len({q[1:] for q in places}) and max((q[0] for q in places), default=0) < len(warps) + groups
     for g in range(groups):
-        assert all(p.group == g for p in parts[first[g] : first[g + 1]])
+        own = {q[0] for q in places if q[2] == g}
+        assert own == set(range(*spans[g])), (g, spans[g])
+    size = [sum(p.rows * p.cols for p in mine) for mine in warps]
+    assert sum(size) == sizes.elements and max(size, default=0) <= max(512, sizes.elements // max(1, len(warps)) + 64)
     if total > 1_000_000:  # (element by element below)
-        assert sum(p.rows * p.cols for p in parts) == sizes.elements and max(p.rows * p.cols for p in parts) <= 16384
         return
     width = {0: 4, 1: 2, 2: 2}
 
