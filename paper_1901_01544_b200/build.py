@@ -13,7 +13,8 @@ STEP_DEPS = [os.path.join(CSRC, f) for f in ("iwp_api.cu", "iwp_device.cuh", "iw
                                             "iwp_threshold.cuh", "iwp_wire.cuh", "iwp_plan.hpp")] + [os.path.join(INCLUDE, "iwp.h")]
 LOSS_DEPS = [os.path.join(CSRC, f) for f in ("iwp_loss.cu", "iwp_tensor.cuh", "iwp_head.cuh", "iwp_balance.cuh", "iwp_host.hpp")] + [
     os.path.join(INCLUDE, f) for f in ("iwp_loss.h", "iwp.h")]
-AROUND_DEPS = [os.path.join(CSRC, f) for f in ("iwp_route.cu", "iwp_route.cuh", "iwp_exchange.cuh", "iwp_clip.cu", "iwp_clip.cuh", "iwp_elem.cuh")] + [
+AROUND_DEPS = [os.path.join(CSRC, f) for f in ("iwp_route.cu", "iwp_route_f32.cu", "iwp_route_bf16.cu", "iwp_route_f16.cu", "iwp_route.cuh",
+                                               "iwp_route_launch.hpp", "iwp_exchange.cuh", "iwp_clip.cu", "iwp_clip.cuh", "iwp_elem.cuh")] + [
     os.path.join(INCLUDE, f) for f in ("iwp_route.h", "iwp_clip.h")]
 DEPS = STEP_DEPS + LOSS_DEPS + AROUND_DEPS
 
@@ -24,6 +25,9 @@ SOURCES = [
     (os.path.join(CSRC, "iwp_api.cu"), ["-fmad=false", "-prec-div=true", "-prec-sqrt=true", "-ftz=false"]),
     (os.path.join(CSRC, "iwp_loss.cu"), []),
     (os.path.join(CSRC, "iwp_route.cu"), []),
+    (os.path.join(CSRC, "iwp_route_f32.cu"), []),
+    (os.path.join(CSRC, "iwp_route_bf16.cu"), []),
+    (os.path.join(CSRC, "iwp_route_f16.cu"), []),
     (os.path.join(CSRC, "iwp_clip.cu"), []),
 ]
 

@@ -14,7 +14,6 @@ namespace {
 using namespace iwp_host;
 namespace K = iwp_clipper;
 
-constexpr int SMS = 148;
 constexpr int64_t MAX_ELEMENTS = int64_t(1) << 46, MAX_PARTS = int64_t(1) << 26, MAX_LD = int64_t(1) << 46;
 constexpr int MAX_GROUPS = 1 << 20;
 constexpr int MAX_CLUSTER = 16;

@@ -3,6 +3,7 @@
 
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstddef>
 #include <cstdint>
 #include <utility>
@@ -24,10 +25,22 @@ inline int64_t tiles_of(int64_t x, int64_t t) { return (x + t - 1) / t; }
 inline bool aligned(const void* p, int64_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 constexpr int MAX_DEVICES = 64;
+constexpr int SMS = 148;
 
 inline int device() {
   int dev = -1;
   return cudaGetDevice(&dev) == cudaSuccess && dev < MAX_DEVICES ? dev : -1;
+}
+
+// Shared memory above the default limit is opted in to once per kernel and device.
+template <class Kernel>
+cudaError_t allow_shared(Kernel kernel, int bytes, std::atomic<int>* allowed) {
+  const int dev = device();
+  if (dev < 0) return cudaErrorInvalidDevice;
+  if (bytes <= 48 * 1024 || bytes <= allowed[dev]) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) allowed[dev] = bytes;
+  return e;
 }
 
 // Launches with programmatic serialisation: the kernel may start while the one before it drains.

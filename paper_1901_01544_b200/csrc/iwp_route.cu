@@ -6,7 +6,7 @@
 
 #include "iwp_exchange.cuh"
 #include "iwp_host.hpp"
-#include "iwp_route.cuh"
+#include "iwp_route_launch.hpp"
 
 namespace {
 
@@ -15,7 +15,6 @@ using namespace iwp_host;
 constexpr int64_t MAX_SIZE = 0x7FFFFFFF - 0xFFFF;  // of tokens, pairs, widths and strides
 constexpr int64_t MAX_ELEMENTS = int64_t(1) << 46;
 constexpr int64_t MAX_PAIRS = int64_t(1) << 30;  // room for the steps behind the last one
-constexpr int SMS = 148;
 
 int size_of(int type) { return type == IWP_F32 ? 4 : 2; }
 bool is_type(int type) { return type == IWP_F32 || type == IWP_BF16 || type == IWP_F16; }
@@ -39,54 +38,16 @@ int by_type_and_word(int type, const Fits& fits, const F& f) {
 
 // ---- routing ------------------------------------------------------------------------------------------
 
-// Columns per lane: 8 up to 256 experts, 32 above.
-constexpr int FEW_COLUMNS = 8, MANY_COLUMNS = 32;
-int columns_of(int E) { return E <= 32 * FEW_COLUMNS ? FEW_COLUMNS : MANY_COLUMNS; }
-int lanes_of(int E, int columns) {
-  int G = 1;
-  while (G * columns < E) G *= 2;
-  return G;
-}
-
-// Shared memory above the default limit is opted in to once per kernel and device.
-template <class Kernel>
-cudaError_t allow_shared(Kernel kernel, int bytes, std::atomic<int>* allowed) {
-  const int dev = device();
-  if (dev < 0) return cudaErrorInvalidDevice;
-  if (bytes <= 48 * 1024 || bytes <= allowed[dev]) return cudaSuccess;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e == cudaSuccess) allowed[dev] = bytes;
-  return e;
+// Elements of the widest word of up to 16 bytes that rows fit.
+template <class Fits>
+int widest_word(int type, const Fits& fits) {
+  for (int vec = 16 / size_of(type); vec > 1; vec /= 2)
+    if (fits(vec)) return vec;
+  return 1;
 }
 
 bool route_sizes_ok(int64_t T, int E, int k) {
   return T >= 0 && T <= MAX_SIZE && E >= 1 && E <= iwp_router::MAX_EXPERTS && k >= 1 && k <= iwp_router::MAX_TOP && k <= E && T * E <= MAX_ELEMENTS;
-}
-
-template <int TYPE, int VEC, int M>
-int route_launch(const iwp_router::Args& r, cudaStream_t st) {
-  namespace R = iwp_router;
-  const int G = lanes_of(r.E, M);
-  const int smem = R::shared_of(r.E, r.k, r.groups, G, M).bytes;
-  auto kernel = R::k_route<TYPE, M, VEC>;
-  static std::atomic<int> allowed[MAX_DEVICES] = {};
-  LOSS_CUDA(allow_shared(kernel, smem, allowed));
-  const int64_t steps = tiles_of(r.T, R::THREADS / G);
-  LOSS_CUDA(launch(kernel, std::max<int64_t>(1, std::min<int64_t>(steps, 8 * SMS)), R::THREADS, smem, 1, st, r, G));
-  return IWP_OK;
-}
-
-template <int TYPE, int VEC, int M>
-int route_grad_launch(const iwp_router::GradArgs& r, cudaStream_t st) {
-  namespace R = iwp_router;
-  const int G = lanes_of(r.E, M);
-  const int smem = R::THREADS / G * r.k * 8;
-  auto kernel = R::k_route_grad<TYPE, M, VEC>;
-  static std::atomic<int> allowed[MAX_DEVICES] = {};
-  LOSS_CUDA(allow_shared(kernel, smem, allowed));
-  const int64_t steps = tiles_of(r.T, R::THREADS / G);
-  LOSS_CUDA(launch(kernel, std::min<int64_t>(steps, 8 * SMS), R::THREADS, smem, 1, st, r, G));
-  return IWP_OK;
 }
 
 // ---- exchange -----------------------------------------------------------------------------------------
@@ -214,10 +175,10 @@ extern "C" int iwp_route(const iwp_route_args* a, void* cuda_stream) {
   r.ids_bytes = a->ids_bytes;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   auto fits = [&](int vec) { return a->experts % vec == 0 && (a->logits_ld % vec == 0 || a->tokens == 1) && aligned(a->logits, vec * size); };
-  return by_type_and_word(a->type, fits, [&](auto type, auto vec) -> int {
-    constexpr int TYPE = decltype(type)::value, VEC = decltype(vec)::value;
-    return columns_of(a->experts) == FEW_COLUMNS ? route_launch<TYPE, VEC, FEW_COLUMNS>(r, st) : route_launch<TYPE, VEC, MANY_COLUMNS>(r, st);
-  });
+  const int word = widest_word(a->type, fits);
+  if (a->type == IWP_F32) return iwp_router::launch_route<IWP_F32>(r, word, st);
+  if (a->type == IWP_BF16) return iwp_router::launch_route<IWP_BF16>(r, word, st);
+  return iwp_router::launch_route<IWP_F16>(r, word, st);
 }
 
 extern "C" int iwp_route_grad(const iwp_route_grad_args* a, void* cuda_stream) {
@@ -257,10 +218,10 @@ extern "C" int iwp_route_grad(const iwp_route_grad_args* a, void* cuda_stream) {
     return a->experts % vec == 0 && ((a->logits_ld % vec == 0 && a->dlogits_ld % vec == 0) || a->tokens == 1) && aligned(a->logits, vec * size) &&
            aligned(a->dlogits, vec * size);
   };
-  return by_type_and_word(a->type, fits, [&](auto type, auto vec) -> int {
-    constexpr int TYPE = decltype(type)::value, VEC = decltype(vec)::value;
-    return columns_of(a->experts) == FEW_COLUMNS ? route_grad_launch<TYPE, VEC, FEW_COLUMNS>(r, st) : route_grad_launch<TYPE, VEC, MANY_COLUMNS>(r, st);
-  });
+  const int word = widest_word(a->type, fits);
+  if (a->type == IWP_F32) return iwp_router::launch_route_grad<IWP_F32>(r, word, st);
+  if (a->type == IWP_BF16) return iwp_router::launch_route_grad<IWP_BF16>(r, word, st);
+  return iwp_router::launch_route_grad<IWP_F16>(r, word, st);
 }
 
 extern "C" int64_t iwp_order_workspace(const iwp_order_args* a) {

@@ -1,10 +1,15 @@
 // iwp_route.cuh - choice of experts from a router's logits with the weights of the chosen, and the gradient to the logits.
 //
-// A row of E logits lives in the registers of G lanes (1 to 32), M neighbouring columns per lane.  The k largest are taken
-// one after another: a maximum over the lane's columns, one over the lanes, and the lowest lane and column that hold it (so
-// ties go to the lower expert).  Only the chosen scores have to be exact to the last bits, and only they are computed that
+// A row of E logits lives in the registers of G lanes (1 to 32), M neighbouring columns per lane.  A column's key is its choice
+// value in an order-preserving 32-bit code whose low bits give way to the column's number, so that keys are distinct, ties
+// go to the lower expert, and a maximum over the lanes tells both value and place.  Every lane sorts its keys by a network;
+// then the largest head is taken k times.  Of 16-bit logits the codes lose nothing.  Where they (or the rounding of scores)
+// may have hidden an order, the row's choice is made again by a warp, in fp32 and if need be in 64 bits: a few rows in
+// a thousand where values differ.  Only the chosen scores have to be exact to the last bits, and only they are computed that
 // way, by k lanes at the end.
 #pragma once
+
+#include <type_traits>
 
 #include "../../include/iwp_route.h"
 #include "iwp_elem.cuh"
@@ -48,11 +53,11 @@ __device__ __forceinline__ float load(const void* p, int64_t at) {
   return static_cast<float>(static_cast<const typename Of<TYPE>::T*>(p)[at]);
 }
 
-// M columns from `first` on of a row; -inf outside.
+// M columns from `first` on of a row, in words of VEC; -inf outside.
 template <int TYPE, int M, int VEC>
-__device__ __forceinline__ void load_columns(float (&x)[M], const void* logits, int64_t row, int first, int E, bool in) {
+__device__ __forceinline__ void load_words(float (&x)[M], const typename Of<TYPE>::T* row, int first, int E, bool in) {
   using W = Word<TYPE, VEC>;
-  const auto* p = static_cast<const typename Of<TYPE>::T*>(logits) + row + first;
+  const auto* const p = row + first;
 #pragma unroll
   for (int n = 0; n < M / VEC; n++) {
     if (in && first + n * VEC < E) {
@@ -66,299 +71,490 @@ __device__ __forceinline__ void load_columns(float (&x)[M], const void* logits, 
   }
 }
 
-__device__ __forceinline__ float max_over(float x, int G) {
-  for (int o = G >> 1; o; o >>= 1) x = fmaxf(x, __shfl_xor_sync(ALL, x, o));
+// M columns of results, `add` to what is there.
+template <int TYPE, int M, int VEC>
+__device__ __forceinline__ void store_words(const float (&x)[M], typename Of<TYPE>::T* row, int first, int E, bool add) {
+  using T = typename Of<TYPE>::T;
+  using W = Word<TYPE, VEC>;
+  T* const p = row + first;
+#pragma unroll
+  for (int n = 0; n < M / VEC; n++) {
+    if (first + n * VEC >= E) continue;
+    W w;
+    if (add) w = *reinterpret_cast<const W*>(p + n * VEC);
+#pragma unroll
+    for (int v = 0; v < VEC; v++) w.x[v] = static_cast<T>(add ? x[n * VEC + v] + static_cast<float>(w.x[v]) : x[n * VEC + v]);
+    *reinterpret_cast<W*>(p + n * VEC) = w;
+  }
+}
+
+// Calls f with the width of a word as a constant.
+template <int TYPE, class F>
+__device__ __forceinline__ void with_word(int word, const F& f) {
+  if constexpr (TYPE != IWP_F32) {
+    if (word == 8) return f(std::integral_constant<int, 8>{});
+  }
+  if (word == 4) return f(std::integral_constant<int, 4>{});
+  if (word == 2) return f(std::integral_constant<int, 2>{});
+  f(std::integral_constant<int, 1>{});
+}
+
+template <int TYPE, int M>
+__device__ __forceinline__ void load_columns(float (&x)[M], const typename Of<TYPE>::T* row, int first, int E, bool in, int word) {
+  with_word<TYPE>(word, [&](auto v) { load_words<TYPE, M, decltype(v)::value>(x, row, first, E, in); });
+}
+
+// Over groups of G lanes.
+template <int G>
+__device__ __forceinline__ float max_over(float x) {
+#pragma unroll
+  for (int o = G / 2; o; o /= 2) x = fmaxf(x, __shfl_xor_sync(ALL, x, o));
   return x;
 }
-__device__ __forceinline__ float sum_over(float x, int G) {
-  for (int o = G >> 1; o; o >>= 1) x += __shfl_xor_sync(ALL, x, o);
+template <int G>
+__device__ __forceinline__ float sum_over(float x) {
+#pragma unroll
+  for (int o = G / 2; o; o /= 2) x += __shfl_xor_sync(ALL, x, o);
   return x;
 }
 
-// The choice of one row in 64 bits, by a whole warp.  Rows come here whose fp32 choice values lie closer than their
-// errors, a few in a thousand at most where biases differ.
-template <int TYPE>
-__device__ __noinline__ void choose_exactly(const Args& a, int64_t t, int* pick) {
-  const int lane = threadIdx.x & 31, n = (a.E + 31) / 32;
-  double c[MAX_EXPERTS / 32];
+// Choice values in fp32 are off: a softmax score by 6 2^-24 of itself and more the further it is from the top (the argument of
+// 2^x), which its own size outweighs; and all of a row by a factor from their sum, 52 2^-24 at most (4 + 2 d of each term at
+// a distance of d, 5.3 on average at most, and up to 37 additions).  Two of them are then wrong by 64 2^-24 of the largest
+// score against each other; the tolerance is 96.  A sigmoid, whose slope falls as its argument's error grows, is off by
+// 7 2^-24; the tolerance is 16.  Both sums with the bias are rounded.
+constexpr float SOFTMAX_TOLERANCE = 0x1.8p-18f, SIGMOID_TOLERANCE = 0x1p-20f;
+__device__ __forceinline__ bool apart(float high, float low, float tol) { return high - low > tol + 0x1p-21f * (fabsf(high) + fabsf(low)); }
+
+// The choice of one row by a whole warp, by choice values of type Real.  Returns whether fp32 leaves it open.
+template <int TYPE, int M, class Real>
+__device__ __noinline__ bool choose(const Args& a, int64_t t, int* pick) {
+  const int lane = threadIdx.x & 31, size = a.E / a.groups;
+  const bool softmax = a.score == IWP_SOFTMAX, by_score = a.bias || (a.groups > 1 && a.group_top == 2);
+  constexpr bool wide = sizeof(Real) == 8;
+  const Real none = -static_cast<Real>(CUDART_INF_F);
+  Real c[M];
   float top = -CUDART_INF_F;
-  for (int i = 0; i < n; i++) {
+#pragma unroll
+  for (int i = 0; i < M; i++) {
     const int e = lane + 32 * i;
     const float x = e < a.E ? load<TYPE>(a.logits, t * a.logits_ld + e) : -CUDART_INF_F;
     c[i] = x;
     top = fmaxf(top, x);
   }
-  top = max_over(top, 32);
-  double s = 0;
-  if (a.score == IWP_SOFTMAX) {
-    for (int i = 0; i < n; i++) {
-      if (c[i] > -CUDART_INF) s += exp(c[i] - top);
+  top = max_over<32>(top);
+  float tol = 0.f;
+  if (by_score) {
+    Real s = 0;
+#pragma unroll
+    for (int i = 0; i < M; i++) {
+      const Real x = c[i];
+      if (!(x > none)) continue;
+      if constexpr (wide)
+        c[i] = softmax ? exp(x - top) : 1. / (1. + exp(-x));
+      else
+        c[i] = softmax ? ex2((x - top) * LOG2E) : 1.f / (1.f + ex2(-x * LOG2E));
+      if (softmax) s += c[i];
     }
-    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(ALL, s, o);
+    if (softmax) {
+#pragma unroll
+      for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(ALL, s, o);
+    }
+    tol = softmax ? SOFTMAX_TOLERANCE / static_cast<float>(s) : SIGMOID_TOLERANCE;
+#pragma unroll
+    for (int i = 0; i < M; i++) {
+      if (!(c[i] > none)) continue;
+      if (softmax) c[i] /= s;
+      if (a.bias) c[i] += a.bias[lane + 32 * i];
+      if (!(c[i] > none)) c[i] = none;
+    }
   }
-  for (int i = 0; i < n; i++) {
-    const int e = lane + 32 * i;
-    if (!(c[i] > -CUDART_INF)) continue;
-    const double y = a.score == IWP_SOFTMAX ? exp(c[i] - top) / s : 1.0 / (1.0 + exp(-c[i]));
-    c[i] = a.bias ? y + a.bias[e] : y;
-    if (!(c[i] > -CUDART_INF)) c[i] = -CUDART_INF;
-  }
+  bool open_question = false;
   if (a.groups > 1) {
-    const int size = a.E / a.groups;
-    double mine = -CUDART_INF;  // lane q: group q's score
+    Real mine = none;  // lane q: group q's score
     for (int q = 0; q < a.groups; q++) {
-      double b1 = -CUDART_INF, b2 = -CUDART_INF;
-      for (int i = 0; i < n; i++) {
-        const int e = lane + 32 * i;
-        if (e / size != q || e >= a.E) continue;
+      Real b1 = none, b2 = none;
+#pragma unroll
+      for (int i = 0; i < M; i++) {
+        if ((lane + 32 * i) / size != q) continue;
         if (c[i] > b1)
           b2 = b1, b1 = c[i];
         else if (c[i] > b2)
           b2 = c[i];
       }
+#pragma unroll
       for (int o = 16; o; o >>= 1) {
-        const double o1 = __shfl_xor_sync(ALL, b1, o), o2 = __shfl_xor_sync(ALL, b2, o);
-        b2 = fmax(fmin(b1, o1), fmax(b2, o2));
-        b1 = fmax(b1, o1);
+        const Real o1 = __shfl_xor_sync(ALL, b1, o), o2 = __shfl_xor_sync(ALL, b2, o);
+        const Real less = b1 < o1 ? b1 : o1, second = b2 < o2 ? o2 : b2;
+        b1 = b1 < o1 ? o1 : b1;
+        b2 = less < second ? second : less;
       }
       if (lane == q) mine = a.group_top == 2 ? b1 + b2 : b1;
     }
     int ahead = 0;
     for (int q = 0; q < a.groups; q++) {
-      const double other = __shfl_sync(ALL, mine, q);
+      const Real other = __shfl_sync(ALL, mine, q);
       ahead += other > mine || (other == mine && q < lane);
     }
-    const unsigned open = __ballot_sync(ALL, lane < a.groups && ahead < a.top_groups);
-    for (int i = 0; i < n; i++) {
+    const bool is_open = lane < a.groups && ahead < a.top_groups;
+    const unsigned open = __ballot_sync(ALL, is_open);
+    if (!wide && by_score) {
+      const float least = -max_over<32>(is_open ? -static_cast<float>(mine) : -CUDART_INF_F);
+      const float most = max_over<32>(is_open ? -CUDART_INF_F : static_cast<float>(mine));
+      open_question = most > -CUDART_INF_F && least < CUDART_INF_F && !apart(least, most, 2.f * tol);
+    }
+#pragma unroll
+    for (int i = 0; i < M; i++) {
       const int e = lane + 32 * i;
-      if (e < a.E && !(open >> (e / size) & 1)) c[i] = -CUDART_INF;
+      if (e < a.E && !(open >> (e / size) & 1)) c[i] = none;
     }
   }
-  if (!a.bias) {  // the logits order the scores
-    for (int i = 0; i < n; i++)
-      if (c[i] > -CUDART_INF) c[i] = load<TYPE>(a.logits, t * a.logits_ld + lane + 32 * i);
+  if (by_score && !a.bias) {  // the logits order the scores
+#pragma unroll
+    for (int i = 0; i < M; i++)
+      if (c[i] > none) c[i] = load<TYPE>(a.logits, t * a.logits_ld + lane + 32 * i);
   }
-  for (int j = 0; j < a.k; j++) {
-    double m = -CUDART_INF;
+  // After the k-th, those that may be as good as it are looked at, too.
+  Real before = 0;
+  int e_before = -1;
+  for (int j = 0; j < a.E; j++) {
+    Real m = none;
     int at = MAX_EXPERTS;
-    for (int i = 0; i < n; i++)
+#pragma unroll
+    for (int i = 0; i < M; i++)
       if (c[i] > m) m = c[i], at = lane + 32 * i;
+#pragma unroll
     for (int o = 16; o; o >>= 1) {
-      const double om = __shfl_xor_sync(ALL, m, o);
+      const Real om = __shfl_xor_sync(ALL, m, o);
       const int oat = __shfl_xor_sync(ALL, at, o);
       if (om > m || (om == m && oat < at)) m = om, at = oat;
     }
-    if (at < MAX_EXPERTS && (at & 31) == lane) c[at / 32] = -CUDART_INF;
-    if (lane == 0) pick[j] = at < MAX_EXPERTS ? at : -1;
+#pragma unroll
+    for (int i = 0; i < M; i++)
+      if (lane + 32 * i == at) c[i] = none;
+    if (j < a.k && lane == 0) pick[j] = at < MAX_EXPERTS ? at : -1;
+    if (!wide && a.bias && j > 0 && at < MAX_EXPERTS && !apart(before, m, tol)) {
+      open_question |= load<TYPE>(a.logits, t * a.logits_ld + e_before) != load<TYPE>(a.logits, t * a.logits_ld + at) || a.bias[e_before] != a.bias[at];
+      if (j >= a.k && open_question) break;
+    } else if (j >= a.k) {
+      break;
+    }
+    if (j >= a.k - 1 && (wide || !a.bias || at >= MAX_EXPERTS)) break;
+    if (j < a.k) before = m, e_before = at;
+  }
+  return open_question;
+}
+
+// As bits that order as the values do, -inf at NONE.
+constexpr uint32_t NONE = 0x007FFFFFu;
+__device__ __forceinline__ uint32_t ordered(float x) {
+  const uint32_t u = __float_as_uint(x + 0.f);  // (-0 is 0)
+  return u ^ (static_cast<uint32_t>(static_cast<int32_t>(u) >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float unordered(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u); }
+
+// Batcher's odd-even merge sort, descending.
+template <int M>
+__device__ __forceinline__ void sort_keys(uint32_t (&x)[M]) {
+#pragma unroll
+  for (int p = 1; p < M; p *= 2)
+#pragma unroll
+    for (int k = p; k >= 1; k /= 2)
+#pragma unroll
+      for (int j = k % p; j <= M - 1 - k; j += 2 * k)
+#pragma unroll
+        for (int i = 0; i < k; i++)
+          if (i + j + k < M && (i + j) / (2 * p) == (i + j + k) / (2 * p)) {
+            const uint32_t high = max(x[i + j], x[i + j + k]), low = min(x[i + j], x[i + j + k]);
+            x[i + j] = high, x[i + j + k] = low;
+          }
+}
+
+template <int G>
+__device__ __forceinline__ uint32_t key_over(uint32_t x) {
+  if constexpr (G == 32) {
+    return __reduce_max_sync(ALL, x);
+  } else {
+#pragma unroll
+    for (int o = G / 2; o; o /= 2) x = max(x, __shfl_xor_sync(ALL, x, o));
+    return x;
   }
 }
 
-// Shared memory of a block of k_route.
+// Shared memory of a block of k_route: counts, a warp's picks made again, and for groups that no whole lanes hold a row's keys
+// and the bounds of its groups' scores.
 struct Shared {
-  int hist, pick, value, row, score, bytes;  // offsets
+  int hist, pick, row, score, bytes;  // offsets
 };
-__host__ __device__ inline Shared shared_of(int E, int k, int groups, int G, int M) {
-  const int rows = THREADS / G;
+__host__ __device__ inline bool groups_of_lanes(int E, int groups, int M) {
+  const int lanes = E / groups / M;
+  return lanes * M * groups == E && (lanes & (lanes - 1)) == 0;
+}
+__host__ __device__ inline Shared shared_of(int E, int groups, int G, int M) {
+  const bool rows = groups > 1 && !groups_of_lanes(E, groups, M);
   Shared s;
   s.hist = 0;
   s.pick = s.hist + 4 * E;
-  s.value = s.pick + 4 * rows * (k + 1);
-  s.row = s.value + 4 * rows * k;
-  s.score = s.row + (groups > 1 ? 4 * THREADS * M : 0);
-  s.bytes = s.score + (groups > 1 ? 4 * rows * groups : 0);
+  s.row = s.pick + 4 * THREADS;
+  s.score = s.row + (rows ? 4 * THREADS * M : 0);
+  s.bytes = s.score + (rows ? 8 * (THREADS / G) * groups : 0);
   return s;
 }
 
-template <int TYPE, int M, int VEC>
-__global__ void __launch_bounds__(THREADS) k_route(const Args a, int G) {
+__device__ __forceinline__ float reciprocal(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// SCORES: the choice goes by scores, or among groups; else by the logits alone.  k <= G: a lane has one pick at most.
+// word: elements that all rows are aligned for.
+template <int TYPE, int M, int G, bool SCORES>
+__global__ void __launch_bounds__(THREADS, M == 8 ? 4 : 2) k_route(const __grid_constant__ Args a, int word) {
   extern __shared__ __align__(16) char smem[];
-  const Shared at = shared_of(a.E, a.k, a.groups, G, M);
-  const int tid = threadIdx.x, lane = tid & 31, g = lane & (G - 1), rows = THREADS / G, rl = tid / G;
+  using T = typename Of<TYPE>::T;
+  constexpr uint32_t LOW = (1u << (M == 8 ? 8 : M == 16 ? 9 : 10)) - 1;  // the bits of a key that hold its column
+  constexpr bool LOSSLESS = !SCORES && TYPE != IWP_F32;
+  constexpr int ROWS = THREADS / G;
+  const Shared at = shared_of(a.E, a.groups, G, M);
+  const int tid = threadIdx.x, lane = tid & 31, g = lane & (G - 1), rl = tid / G, row0 = lane & ~(G - 1);
   int* const hist = reinterpret_cast<int*>(smem + at.hist);
-  int* const pick = reinterpret_cast<int*>(smem + at.pick) + rl * (a.k + 1);
-  float* const value = reinterpret_cast<float*>(smem + at.value) + rl * a.k;
-  float* const row = reinterpret_cast<float*>(smem + at.row) + rl * G * M;
-  float* const group_score = reinterpret_cast<float*>(smem + at.score) + rl * a.groups;
-  const unsigned of_row = (G == 32 ? ALL : (1u << G) - 1) << (lane & ~(G - 1));
+  int* const pick = reinterpret_cast<int*>(smem + at.pick) + (tid & ~31);
+  const unsigned of_row = (G == 32 ? ALL : (1u << G) - 1) << row0;
   const int first = g * M;
-  const bool softmax = a.score == IWP_SOFTMAX;
-  const bool by_score = a.bias || (a.groups > 1 && a.group_top == 2);  // else the logits decide everything
+  const bool softmax = a.score == IWP_SOFTMAX, renormalize = a.renormalize, count = a.counts != nullptr;
+  const bool by_score = SCORES && (a.bias || (a.groups > 1 && a.group_top == 2));
   launch_next();
   for (int e = tid; e < a.E; e += THREADS) hist[e] = 0;
   wait_previous();
   __syncthreads();
-  const int64_t steps = (a.T + rows - 1) / rows;
-  for (int64_t step = blockIdx.x; step < steps; step += gridDim.x) {
-    const int64_t t = step * rows + rl, from = t * a.logits_ld;
-    const bool in = t < a.T, on = in && (!a.mask || a.mask[t]);
-    float x[M], c[M];
-    load_columns<TYPE, M, VEC>(x, a.logits, from, first, a.E, on);
-    float top = -CUDART_INF_F;
-    bool odd = false;
+  float bias[M];
+  if constexpr (SCORES) {
 #pragma unroll
     for (int i = 0; i < M; i++) {
-      top = fmaxf(top, x[i]);
-      odd |= isnan(x[i]) || (softmax && x[i] == CUDART_INF_F);
+      bias[i] = a.bias && first + i < a.E ? __ldg(a.bias + first + i) : 0.f;
+      if (!(bias[i] > -CUDART_INF_F)) bias[i] = -CUDART_INF_F;  // not available
     }
-    top = max_over(top, G);
-    const bool bad = (__ballot_sync(ALL, odd) & of_row) != 0;
-    // choice values, and how far two of them may be apart and still be in the wrong order: s is off by at most
-    // (2 d + 22) 2^-24 of itself for softmax at a distance of d from the top (2^x, its argument, the sum), so by less than
-    // 2^-19 of the largest s; 4 2^-24 for sigmoid, whose slope falls as its argument's error grows
+  }
+  uint32_t column[M];  // a key's low bits
+#pragma unroll
+  for (int i = 0; i < M; i++) column[i] = LOW - first - i;
+  const int64_t steps = (a.T + ROWS - 1) / ROWS;
+  for (int64_t step = blockIdx.x; step < steps; step += gridDim.x) {
+    const int64_t t = step * ROWS + rl;
+    const T* const row = static_cast<const T*>(a.logits) + t * a.logits_ld;
+    const bool in = t < a.T, on = in && (!a.mask || a.mask[t]);
+    float x[M];
+    load_columns<TYPE, M>(x, row, first, a.E, on, word);
+    // rows that hold a NaN or an infinity are looked at again
+    float odd = 0.f;
+#pragma unroll
+    for (int i = 0; i < M; i++) odd = fmaf(x[i], 0.f, odd);
+    bool bad = false;
+    if (odd != odd) {
+#pragma unroll
+      for (int i = 0; i < M; i++) bad |= isnan(x[i]) || (softmax && x[i] == CUDART_INF_F);
+    }
+    bad = (__ballot_sync(ALL, bad) & of_row) != 0;
+    float top = -CUDART_INF_F, s = 0.f;  // of the row: largest logit, sum of exponentials below it
+    if (softmax && (SCORES || !renormalize)) {
+#pragma unroll
+      for (int i = 0; i < M; i++) top = fmaxf(top, x[i]);
+      top = max_over<G>(top);
+      if (!renormalize) {
+#pragma unroll
+        for (int i = 0; i < M; i++) s += x[i] == -CUDART_INF_F ? 0.f : expf(x[i] - top);
+        s = sum_over<G>(s);
+      }
+    }
+    uint32_t key[M];
     float tol = 0.f;
-    if (by_score) {
-      float scale = 1.f;
+    if (SCORES && by_score) {
+      float c[M], scale = 1.f;
+      tol = SIGMOID_TOLERANCE;
       if (softmax) {
-        float s = 0.f;
+        float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < M; i++) {
-          c[i] = x[i] == -CUDART_INF_F ? 0.f : ex2((x[i] - top) * LOG2E);
-          s += c[i];
+          c[i] = ex2((x[i] - top) * LOG2E);
+          if (x[i] == -CUDART_INF_F) c[i] = 0.f;
+          sum += c[i];
         }
-        s = sum_over(s, G);
-        scale = s > 0.f ? 1.f / s : 0.f;
+        sum = sum_over<G>(sum);
+        scale = sum > 0.f ? reciprocal(sum) : 0.f;
+        tol = SOFTMAX_TOLERANCE * scale;
       } else {
 #pragma unroll
-        for (int i = 0; i < M; i++) c[i] = 1.f / (1.f + ex2(-x[i] * LOG2E));
+        for (int i = 0; i < M; i++) c[i] = reciprocal(1.f + ex2(-x[i] * LOG2E));
       }
-      tol = softmax ? scale * 0x1p-18f : 0x1p-20f;
 #pragma unroll
-      for (int i = 0; i < M; i++) {
-        c[i] *= scale;
-        if (a.bias && first + i < a.E) c[i] += a.bias[first + i];
-        if (x[i] == -CUDART_INF_F || !(c[i] > -CUDART_INF_F)) c[i] = -CUDART_INF_F;
+      for (int i = 0; i < M; i++) c[i] = fmaf(c[i], scale, bias[i]);
+      if (odd != odd) {
+#pragma unroll
+        for (int i = 0; i < M; i++)
+          if (x[i] == -CUDART_INF_F) c[i] = -CUDART_INF_F;
       }
+#pragma unroll
+      for (int i = 0; i < M; i++) key[i] = (ordered(c[i]) & ~LOW) | column[i];
     } else {
 #pragma unroll
-      for (int i = 0; i < M; i++) c[i] = x[i];
+      for (int i = 0; i < M; i++) key[i] = (ordered(x[i]) & ~LOW) | column[i];
     }
-    bool again = false;  // in 64 bits
-    if (a.groups > 1) {
+    bool again = false;  // by a warp
+    if (SCORES && a.groups > 1) {
       const int size = a.E / a.groups;
-#pragma unroll
-      for (int i = 0; i < M; i++) row[first + i] = c[i];
-      __syncwarp();
-      for (int q = g; q < a.groups; q += G) {
-        float b1 = -CUDART_INF_F, b2 = -CUDART_INF_F;
-        for (int e = q * size; e < (q + 1) * size; e++) {
-          const float y = row[e];
-          b2 = fmaxf(b2, fminf(b1, y));
-          b1 = fmaxf(b1, y);
+      if (groups_of_lanes(a.E, a.groups, M)) {
+        sort_keys<M>(key);
+        const int lanes = size / M;
+        uint32_t b1 = key[0], b2 = key[1];
+        for (int o = 1; o < lanes; o *= 2) {
+          const uint32_t o1 = __shfl_xor_sync(ALL, b1, o), o2 = __shfl_xor_sync(ALL, b2, o);
+          b2 = max(min(b1, o1), max(b2, o2));
+          b1 = max(b1, o1);
         }
-        group_score[q] = a.group_top == 2 ? b1 + b2 : b1;
-      }
-      __syncwarp();
-      float least = CUDART_INF_F, most = -CUDART_INF_F;  // of the groups that are open and closed
-      unsigned open = 0;                                   // bit n: this lane's n-th group
-      for (int q = g, n = 0; q < a.groups; q += G, n++) {
-        const float mine = group_score[q];
+        // least and most that the score may be
+        const bool some = first < a.E && b1 > NONE && (a.group_top == 1 || b2 > NONE);
+        float low = -CUDART_INF_F, high = -CUDART_INF_F;
+        if (some) {
+          low = unordered(b1 & ~LOW), high = unordered(b1 | LOW);
+          if (a.group_top == 2) low += unordered(b2 & ~LOW), high += unordered(b2 | LOW);
+        }
+        const int mine = first / size;
         int ahead = 0;
-        for (int p = 0; p < a.groups; p++) {
-          const float other = group_score[p];
-          ahead += other > mine || (other == mine && p < q);
+#pragma unroll 4
+        for (int q = 0; q < a.groups; q++) {
+          const float other = __shfl_sync(ALL, low, row0 + q * lanes);
+          ahead += other > low || (other == low && q < mine);
         }
-        if (ahead < a.top_groups)
-          least = fminf(least, mine), open |= 1u << n;
-        else
-          most = fmaxf(most, mine);
-      }
-      least = -max_over(-least, G);
-      most = max_over(most, G);
-      again = by_score && most >= least - (2.f * tol + 0x1p-21f * (fabsf(least) + fabsf(most))) && most > -CUDART_INF_F && least < CUDART_INF_F;
-      __syncwarp();
-      for (int q = g, n = 0; q < a.groups; q += G, n++) group_score[q] = (open >> n & 1) ? 1.f : 0.f;
-      __syncwarp();
+        const bool is_open = ahead < a.top_groups;
+        const float least = -max_over<G>(is_open && first < a.E ? -low : -CUDART_INF_F);
+        const float most = max_over<G>(is_open ? -CUDART_INF_F : high);
+        again = most > -CUDART_INF_F && least < CUDART_INF_F && !apart(least, most, 2.f * tol);
+        if (!is_open) {
 #pragma unroll
-      for (int i = 0; i < M; i++) {
-        if (first + i < a.E && group_score[(first + i) / size] == 0.f) c[i] = -CUDART_INF_F;
-        if (!a.bias && c[i] > -CUDART_INF_F) c[i] = x[i];
+          for (int i = 0; i < M; i++) key[i] = 0;
+        }
+      } else {
+        uint32_t* const keys = reinterpret_cast<uint32_t*>(smem + at.row) + rl * G * M;
+        float* const group_score = reinterpret_cast<float*>(smem + at.score) + rl * 2 * a.groups;  // the least it may be
+        float* const group_high = group_score + a.groups;
+#pragma unroll
+        for (int i = 0; i < M; i++) keys[first + i] = key[i];
+        __syncwarp();
+        for (int q = g; q < a.groups; q += G) {
+          uint32_t b1 = 0, b2 = 0;
+          for (int e = q * size; e < (q + 1) * size; e++) {
+            const uint32_t y = keys[e];
+            b2 = max(b2, min(b1, y));
+            b1 = max(b1, y);
+          }
+          const bool some = b1 > NONE && (a.group_top == 1 || b2 > NONE);
+          group_score[q] = !some ? -CUDART_INF_F : unordered(b1 & ~LOW) + (a.group_top == 2 ? unordered(b2 & ~LOW) : 0.f);
+          group_high[q] = !some ? -CUDART_INF_F : unordered(b1 | LOW) + (a.group_top == 2 ? unordered(b2 | LOW) : 0.f);
+        }
+        __syncwarp();
+        float least = CUDART_INF_F, most = -CUDART_INF_F;
+        unsigned open = 0;  // bit n: this lane's n-th group
+        for (int q = g, n = 0; q < a.groups; q += G, n++) {
+          const float mine = group_score[q];
+          int ahead = 0;
+          for (int p = 0; p < a.groups; p++) {
+            const float other = group_score[p];
+            ahead += other > mine || (other == mine && p < q);
+          }
+          if (ahead < a.top_groups)
+            least = fminf(least, mine), open |= 1u << n;
+          else
+            most = fmaxf(most, group_high[q]);
+        }
+        least = -max_over<G>(-least);
+        most = max_over<G>(most);
+        again = most > -CUDART_INF_F && least < CUDART_INF_F && !apart(least, most, 2.f * tol);
+        __syncwarp();
+        for (int q = g, n = 0; q < a.groups; q += G, n++) group_score[q] = (open >> n & 1) ? 1.f : 0.f;
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < M; i++)
+          if (first + i < a.E && group_score[(first + i) / size] == 0.f) key[i] = 0;
+        __syncwarp();
+        sort_keys<M>(key);
       }
+    } else {
+      sort_keys<M>(key);
     }
-    // the k largest, and with a bias one more, to see how far behind it is
-    const int picks = a.bias ? a.k + 1 : a.k;
-    float before = CUDART_INF_F;
-    unsigned near = 0;  // bit j: the choice j + 1 is as good as j
+    // the k largest, and one more, to see how far behind it is: lane j's own and the next
+    uint32_t mine = 0, next = 0;
+    const int picks = LOSSLESS ? a.k : a.k + 1;
     for (int j = 0; j < picks; j++) {
-      float best = -CUDART_INF_F;
+      const uint32_t m = key_over<G>(key[0]);
+      const bool pop = key[0] == m;
 #pragma unroll
-      for (int i = 0; i < M; i++) best = fmaxf(best, c[i]);
-      const float m = max_over(best, G);
-      const unsigned holders = __ballot_sync(ALL, best == m) & of_row;
-      if (lane == __ffs(holders) - 1) {
-        int which = -1;
-        if (m > -CUDART_INF_F) {
+      for (int i = 0; i < 7; i++) key[i] = pop ? key[i + 1] : key[i];
+      if constexpr (M == 8) {
+        if (pop) key[7] = 0;
+      } else if (a.k > 7) {  // (else no lane gets that far)
 #pragma unroll
-          for (int i = 0; i < M; i++)
-            if (which < 0 && c[i] == m) which = i, c[i] = -CUDART_INF_F;
+        for (int i = 7; i < M - 1; i++) key[i] = pop ? key[i + 1] : key[i];
+        if (pop) key[M - 1] = 0;
+      }
+      if (g == j) mine = m;
+      if (!LOSSLESS && g + 1 == j) next = m;
+    }
+    int e = mine > NONE && on && g < a.k ? static_cast<int>(LOW - (mine & LOW)) : -1;
+    float y = e >= 0 ? static_cast<float>(row[e]) : -CUDART_INF_F;
+    if constexpr (!LOSSLESS) {
+      const float y2 = __shfl_down_sync(ALL, y, 1);
+      if (e >= 0 && next > NONE) {
+        const bool close = SCORES ? !apart(unordered(mine & ~LOW), unordered(next | LOW), tol) : (mine ^ next) <= LOW;
+        if (close) {
+          if (g == a.k - 1)
+            again = true;  // others may be as close
+          else if (SCORES && a.bias)
+            again |= y != y2 || a.bias[e] != a.bias[LOW - (next & LOW)];
+          else
+            again |= y < y2;
         }
-        pick[j] = which < 0 ? -1 : first + which;
       }
-      if (a.bias && j > 0 && before - m <= tol + 0x1p-21f * (fabsf(before) + fabsf(m))) near |= 1u << (j - 1);
-      before = m;
-    }
-    __syncwarp();
-    if (near) {  // equal in logit and bias is equal
-      for (int j = 0; j < a.k; j++) {
-        if (!(near >> j & 1)) continue;
-        const int e0 = pick[j], e1 = pick[j + 1];
-        if (e0 < 0 || e1 < 0) continue;
-        again |= load<TYPE>(a.logits, from + e0) != load<TYPE>(a.logits, from + e1) || a.bias[e0] != a.bias[e1];
+      unsigned todo = __ballot_sync(ALL, again && on && !bad);
+      while (todo) {
+        const int who = __ffs(todo) - 1, who0 = who & ~(G - 1);
+        todo &= ~((G == 32 ? ALL : (1u << G) - 1) << who0);
+        const int64_t which = __shfl_sync(ALL, t, who);
+        if (choose<TYPE, M, float>(a, which, pick)) choose<TYPE, M, double>(a, which, pick);
+        __syncwarp();
+        if (row0 == who0 && g < a.k) {
+          e = pick[g];
+          y = e >= 0 ? static_cast<float>(row[e]) : -CUDART_INF_F;
+        }
+        __syncwarp();
       }
     }
-    again = again && on && !bad;
-    unsigned todo = __ballot_sync(ALL, again && g == 0);
-    while (todo) {
-      const int who = __ffs(todo) - 1;
-      todo &= todo - 1;
-      choose_exactly<TYPE>(a, __shfl_sync(ALL, t, who), reinterpret_cast<int*>(smem + at.pick) + (tid - lane + who) / G * (a.k + 1));
-    }
-    __syncwarp();
     // weights
-    float most = -CUDART_INF_F;
-    for (int j = g; j < a.k; j += G) {
-      const int e = pick[j];
-      const float y = on && e >= 0 ? load<TYPE>(a.logits, from + e) : -CUDART_INF_F;
-      value[j] = y;
-      most = fmaxf(most, y);
+    float w = 0.f;
+    if (softmax) {
+      float ref = top;
+      if (renormalize) ref = SCORES ? max_over<G>(y) : __shfl_sync(ALL, y, row0);
+      if (y > -CUDART_INF_F) w = expf(y - ref);
+    } else {  // sigmoid, times e^-ref, so that scores far below one still have a ratio
+      float ref = 0.f;
+      if (renormalize) ref = fminf(SCORES ? max_over<G>(y) : __shfl_sync(ALL, y, row0), 0.f);
+      if (y > -CUDART_INF_F) w = y >= 0.f ? 1.f / (1.f + expf(-y)) : expf(y - ref) / (1.f + expf(y));
     }
-    most = max_over(most, G);
-    float s = 0.f;
-    if (softmax && !a.renormalize) {
-#pragma unroll
-      for (int i = 0; i < M; i++) s += x[i] == -CUDART_INF_F ? 0.f : expf(x[i] - top);
+    if (renormalize) s = sum_over<G>(w);
+    if (softmax || renormalize) w *= s > 0.f ? a.weight_scale / s : 0.f;
+    else w *= a.weight_scale;
+    if (bad && on) w = CUDART_NAN_F, e = -1;
+    if (in && g < a.k) {
+      const int64_t to = t * a.k + g;
+      a.weights[to] = w;
+      if (a.ids_bytes == 8)
+        static_cast<int64_t*>(a.ids)[to] = e;
+      else
+        static_cast<int32_t*>(a.ids)[to] = e;
+      if (count && e >= 0) atomicAdd(&hist[e], 1);
     }
-    const float ref = softmax ? (a.renormalize ? most : top) : a.renormalize ? fminf(most, 0.f) : 0.f;
-    for (int j = g; j < a.k; j += G) {
-      const float y = value[j];
-      float w = 0.f;
-      if (y > -CUDART_INF_F) {
-        if (softmax)
-          w = expf(y - ref);
-        else  // sigmoid, times e^-ref, so that scores far below one still have a ratio
-          w = y >= 0.f ? 1.f / (1.f + expf(-y)) : expf(y - ref) / (1.f + expf(y));
-      }
-      value[j] = w;
-      if (a.renormalize) s += w;
-    }
-    s = sum_over(s, G);
-    const float scale = a.renormalize || softmax ? (s > 0.f ? a.weight_scale / s : 0.f) : a.weight_scale;
-    for (int j = g; j < a.k; j += G) {
-      int e = pick[j];
-      if (!on || bad) e = -1;
-      const float w = on && bad ? CUDART_NAN_F : e < 0 ? 0.f : value[j] * scale;
-      if (in) {
-        const int64_t to = t * a.k + j;
-        a.weights[to] = w;
-        if (a.ids_bytes == 8)
-          static_cast<int64_t*>(a.ids)[to] = e;
-        else
-          static_cast<int32_t*>(a.ids)[to] = e;
-        if (a.counts && e >= 0) atomicAdd(&hist[e], 1);
-      }
-    }
-    __syncwarp();
   }
-  if (!a.counts) return;
+  if (!count) return;
   __syncthreads();
   if (gridDim.x == 1) {
     for (int e = tid; e < a.E; e += THREADS) a.counts[e] = hist[e];
@@ -388,88 +584,79 @@ struct GradArgs {
   int E, k, score, renormalize, ids_bytes, accumulate;
 };
 
-template <int TYPE, int M, int VEC>
-__global__ void __launch_bounds__(THREADS) k_route_grad(const GradArgs a, int G) {
-  extern __shared__ __align__(16) char smem[];
-  using E_t = typename Of<TYPE>::T;
-  using W = Word<TYPE, VEC>;
-  const int tid = threadIdx.x, lane = tid & 31, g = lane & (G - 1), rows = THREADS / G, rl = tid / G, first = g * M;
-  int* const id = reinterpret_cast<int*>(smem) + rl * 2 * a.k;
-  float* const value = reinterpret_cast<float*>(id + a.k);
-  const unsigned of_row = (G == 32 ? ALL : (1u << G) - 1) << (lane & ~(G - 1));
-  const bool softmax = a.score == IWP_SOFTMAX;
+// A row's gradient is zero (or, for softmax taken as it is, a multiple of the scores) but at the chosen experts: all of it is
+// written in words first, then the chosen ones by a lane each.
+template <int TYPE, int M, int G>
+__global__ void __launch_bounds__(THREADS, M == 8 ? 4 : 2) k_route_grad(const __grid_constant__ GradArgs a, int word) {
+  using T = typename Of<TYPE>::T;
+  constexpr int ROWS = THREADS / G;
+  const int tid = threadIdx.x, lane = tid & 31, g = lane & (G - 1), rl = tid / G, row0 = lane & ~(G - 1), first = g * M;
+  const unsigned of_row = (G == 32 ? ALL : (1u << G) - 1) << row0;
+  const bool softmax = a.score == IWP_SOFTMAX, dense = softmax && !a.renormalize;
   launch_next();
   wait_previous();
-  const int64_t steps = (a.T + rows - 1) / rows;
+  const int64_t steps = (a.T + ROWS - 1) / ROWS;
   for (int64_t step = blockIdx.x; step < steps; step += gridDim.x) {
-    const int64_t t = step * rows + rl, from = t * a.logits_ld;
+    const int64_t t = step * ROWS + rl;
     const bool in = t < a.T;
+    const T* const row = static_cast<const T*>(a.logits) + t * a.logits_ld;
+    T* const out = static_cast<T*>(a.dlogits) + t * a.dlogits_ld;
+    int e = -1;
+    float p = 0.f, y = 0.f;  // weight, and its product with the gradient
+    if (in && g < a.k) {
+      const int64_t id = load_id(a.ids, a.ids_bytes, t * a.ids_ld + g);
+      if (id >= 0 && id < a.E) {
+        e = static_cast<int>(id);
+        p = a.weights[t * a.weights_ld + g];
+        y = p * a.dweights[t * a.dweights_ld + g];
+      }
+    }
+    const float sum = sum_over<G>(y);
+    const bool some = (__ballot_sync(ALL, e >= 0) & of_row) != 0;
+    float x = 0.f, old = 0.f;
+    if (e >= 0) {
+      if (dense || !softmax) x = static_cast<float>(row[e]);
+      if (a.accumulate) old = static_cast<float>(out[e]);
+    }
     float v[M];
-    float sum = 0.f;
-    bool some = false;
-    for (int j = g; j < a.k; j += G) {
-      const int64_t e = in ? load_id(a.ids, a.ids_bytes, t * a.ids_ld + j) : -1;
-      const bool ok = e >= 0 && e < a.E;
-      const float y = ok ? a.dweights[t * a.dweights_ld + j] * a.weights[t * a.weights_ld + j] : 0.f;
-      id[j] = ok ? static_cast<int>(e) : -1;
-      value[j] = y;
-      sum += y;
-      some |= ok;
-    }
-    sum = sum_over(sum, G);
-    some = (__ballot_sync(ALL, some) & of_row) != 0;
-    for (int j = g; j < a.k; j += G) {
-      const int e = id[j];
-      if (e < 0) continue;
-      float y = value[j];
-      if (a.renormalize) y -= a.weights[t * a.weights_ld + j] * a.inv_scale * sum;
-      if (!softmax) y *= 1.f / (1.f + expf(load<TYPE>(a.logits, from + e)));
-      value[j] = y;
-    }
-    if (softmax && !a.renormalize) {
-      load_columns<TYPE, M, VEC>(v, a.logits, from, first, a.E, in && some);
+    if (dense) {
+      load_columns<TYPE, M>(v, row, first, a.E, in && some, word);
       float top = -CUDART_INF_F, s = 0.f;
 #pragma unroll
       for (int i = 0; i < M; i++) top = fmaxf(top, v[i]);
-      top = max_over(top, G);
+      top = max_over<G>(top);
 #pragma unroll
       for (int i = 0; i < M; i++) {
         v[i] = v[i] == -CUDART_INF_F ? 0.f : expf(v[i] - top);
         s += v[i];
       }
-      s = sum_over(s, G);
+      s = sum_over<G>(s);
       const float f = s > 0.f ? -sum / s : 0.f;
 #pragma unroll
-      for (int i = 0; i < M; i++) v[i] *= f;
+      for (int i = 0; i < M; i++) v[i] *= f * a.scale;
+      x = x > -CUDART_INF_F ? expf(x - top) * f : 0.f;  // what the chosen expert gets with the others
     } else {
 #pragma unroll
       for (int i = 0; i < M; i++) v[i] = 0.f;
+      if (a.renormalize) y -= p * a.inv_scale * sum;
+      if (!softmax) y *= 1.f / (1.f + expf(x));
+      x = 0.f;
     }
-    __syncwarp();
-    for (int j = 0; j < a.k; j++) {
-      const int d = id[j] - first;
-      const float y = value[j];
-      if (id[j] < 0 || d < 0 || d >= M) continue;
+    // an expert that the row names more than once gets all of it
+    const unsigned same = __match_any_sync(ALL, e >= 0 ? (row0 << 16 | e) : -1 - lane);
+    if (__any_sync(ALL, same & (same - 1))) {
+      float all = 0.f;
 #pragma unroll
-      for (int i = 0; i < M; i++)
-        if (i == d) v[i] += y;
-    }
-    __syncwarp();
-    E_t* const to = static_cast<E_t*>(a.dlogits) + t * a.dlogits_ld + first;
-#pragma unroll
-    for (int n = 0; n < M / VEC; n++) {
-      if (!in || first + n * VEC >= a.E) continue;
-      W w;
-      if (a.accumulate) {
-        w = *reinterpret_cast<const W*>(to + n * VEC);
-#pragma unroll
-        for (int i = 0; i < VEC; i++) w.x[i] = static_cast<E_t>(fmaf(v[n * VEC + i], a.scale, static_cast<float>(w.x[i])));
-      } else {
-#pragma unroll
-        for (int i = 0; i < VEC; i++) w.x[i] = static_cast<E_t>(v[n * VEC + i] * a.scale);
+      for (int i = 0; i < G; i++) {
+        const float other = __shfl_sync(ALL, y, row0 + i);
+        if (same >> (row0 + i) & 1) all += other;
       }
-      *reinterpret_cast<W*>(to + n * VEC) = w;
+      y = all;
     }
+    if (in && (dense || !a.accumulate))
+      with_word<TYPE>(word, [&](auto vec) { store_words<TYPE, M, decltype(vec)::value>(v, out, first, a.E, a.accumulate); });
+    __syncwarp();
+    if (e >= 0) out[e] = static_cast<T>(fmaf(y + x, a.scale, old));
   }
 }
 
