@@ -41,7 +41,7 @@ int iwp_route_reset(void* state, void* cuda_stream);
  * softmax, +inf) has ids -1 and weights NaN.
  */
 typedef struct iwp_route_args {
-  int64_t tokens;                  /* 0 <= T <= 2^31 - 2^16, T E <= 2^46 */
+  int64_t tokens;                  /* 0 <= T <= 2^30, T E <= 2^46 */
   const void* logits;              /* [T][E] of type, row stride logits_ld elements */
   int64_t logits_ld;
   const float* bias;               /* [E], or NULL */

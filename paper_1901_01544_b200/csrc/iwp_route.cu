@@ -47,7 +47,7 @@ int widest_word(int type, const Fits& fits) {
 }
 
 bool route_sizes_ok(int64_t T, int E, int k) {
-  return T >= 0 && T <= MAX_SIZE && E >= 1 && E <= iwp_router::MAX_EXPERTS && k >= 1 && k <= iwp_router::MAX_TOP && k <= E && T * E <= MAX_ELEMENTS;
+  return T >= 0 && T <= MAX_PAIRS && E >= 1 && E <= iwp_router::MAX_EXPERTS && k >= 1 && k <= iwp_router::MAX_TOP && k <= E && T * E <= MAX_ELEMENTS;
 }
 
 // ---- exchange -----------------------------------------------------------------------------------------
@@ -163,7 +163,7 @@ extern "C" int iwp_route(const iwp_route_args* a, void* cuda_stream) {
   r.weights = a->weights;
   r.counts = a->counts;
   r.logits_ld = a->logits_ld;
-  r.T = a->tokens;
+  r.T = static_cast<int>(a->tokens);
   r.weight_scale = a->weight_scale;
   r.E = a->experts;
   r.k = a->top_k;
@@ -204,7 +204,7 @@ extern "C" int iwp_route_grad(const iwp_route_grad_args* a, void* cuda_stream) {
   r.weights_ld = a->weights_ld;
   r.dweights_ld = a->dweights_ld;
   r.dlogits_ld = a->dlogits_ld;
-  r.T = a->tokens;
+  r.T = static_cast<int>(a->tokens);
   r.inv_scale = 1.f / a->weight_scale;
   r.scale = a->scale;
   r.E = a->experts;

@@ -1,12 +1,11 @@
 // iwp_route.cuh - choice of experts from a router's logits with the weights of the chosen, and the gradient to the logits.
 //
-// A row of E logits lives in the registers of G lanes (1 to 32), M neighbouring columns per lane.  A column's key is its choice
-// value in an order-preserving 32-bit code whose low bits give way to the column's number, so that keys are distinct, ties
-// go to the lower expert, and a maximum over the lanes tells both value and place.  Every lane sorts its keys by a network;
-// then the largest head is taken k times.  Of 16-bit logits the codes lose nothing.  Where they (or the rounding of scores)
-// may have hidden an order, the row's choice is made again by a warp, in fp32 and if need be in 64 bits: a few rows in
-// a thousand where values differ.  Only the chosen scores have to be exact to the last bits, and only they are computed that
-// way, by k lanes at the end.
+// A row of E logits lives in the registers of G lanes (2 to 32), M neighbouring columns per lane.  A column's key is its choice
+// value in an order-preserving 32-bit code whose lowest bits give way to the column's place in its lane.  Every lane sorts its
+// keys by a network; then the largest head is taken k times, the lowest lane's where several hold it: so ties go to the lower
+// expert.  Of 16-bit logits the codes lose nothing.  Where they (or the rounding of scores) may have hidden an order, a warp
+// makes the row's choice again: by the logits themselves, or by scores in 64 bits (a row in a thousand where values differ).
+// Only the chosen scores have to be exact to the last bits, and only they are computed that way, by k lanes at the end.
 #pragma once
 
 #include <type_traits>
@@ -37,8 +36,9 @@ struct Args {
   void* ids;
   float* weights;
   int* counts;
-  int64_t logits_ld, T;
+  int64_t logits_ld;
   float weight_scale;
+  int T;
   int E, k, groups, top_groups, group_top, score, renormalize, ids_bytes;
 };
 
@@ -122,16 +122,15 @@ __device__ __forceinline__ float sum_over(float x) {
 // 2^x), which its own size outweighs; and all of a row by a factor from their sum, 52 2^-24 at most (4 + 2 d of each term at
 // a distance of d, 5.3 on average at most, and up to 37 additions).  Two of them are then wrong by 64 2^-24 of the largest
 // score against each other; the tolerance is 96.  A sigmoid, whose slope falls as its argument's error grows, is off by
-// 7 2^-24; the tolerance is 16.  Both sums with the bias are rounded.
+// 7 2^-24; the tolerance is 16.  Sums with the bias are rounded by 2^-24 of themselves; the tolerance is twice that.
 constexpr float SOFTMAX_TOLERANCE = 0x1.8p-18f, SIGMOID_TOLERANCE = 0x1p-20f;
-__device__ __forceinline__ bool apart(float high, float low, float tol) { return high - low > tol + 0x1p-21f * (fabsf(high) + fabsf(low)); }
+__device__ __forceinline__ bool apart(float high, float low, float tol) { return high - low > tol + 0x1p-23f * (fabsf(high) + fabsf(low)); }
 
-// The choice of one row by a whole warp, by choice values of type Real.  Returns whether fp32 leaves it open.
+// The choice of one row by a whole warp: by the logits (Real = float), or by scores in 64 bits.
 template <int TYPE, int M, class Real>
-__device__ __noinline__ bool choose(const Args& a, int64_t t, int* pick) {
+__device__ __noinline__ void choose(const Args& a, int64_t t, int* pick) {
   const int lane = threadIdx.x & 31, size = a.E / a.groups;
-  const bool softmax = a.score == IWP_SOFTMAX, by_score = a.bias || (a.groups > 1 && a.group_top == 2);
-  constexpr bool wide = sizeof(Real) == 8;
+  constexpr bool scores = sizeof(Real) == 8;
   const Real none = -static_cast<Real>(CUDART_INF_F);
   Real c[M];
   float top = -CUDART_INF_F;
@@ -142,25 +141,18 @@ __device__ __noinline__ bool choose(const Args& a, int64_t t, int* pick) {
     c[i] = x;
     top = fmaxf(top, x);
   }
-  top = max_over<32>(top);
-  float tol = 0.f;
-  if (by_score) {
-    Real s = 0;
+  if constexpr (scores) {
+    const bool softmax = a.score == IWP_SOFTMAX;
+    top = max_over<32>(top);
+    double s = 0;
 #pragma unroll
     for (int i = 0; i < M; i++) {
-      const Real x = c[i];
-      if (!(x > none)) continue;
-      if constexpr (wide)
-        c[i] = softmax ? exp(x - top) : 1. / (1. + exp(-x));
-      else
-        c[i] = softmax ? ex2((x - top) * LOG2E) : 1.f / (1.f + ex2(-x * LOG2E));
-      if (softmax) s += c[i];
+      if (!(c[i] > none)) continue;
+      c[i] = softmax ? exp(c[i] - top) : 1. / (1. + exp(-c[i]));
+      s += c[i];
     }
-    if (softmax) {
 #pragma unroll
-      for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(ALL, s, o);
-    }
-    tol = softmax ? SOFTMAX_TOLERANCE / static_cast<float>(s) : SIGMOID_TOLERANCE;
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(ALL, s, o);
 #pragma unroll
     for (int i = 0; i < M; i++) {
       if (!(c[i] > none)) continue;
@@ -169,7 +161,6 @@ __device__ __noinline__ bool choose(const Args& a, int64_t t, int* pick) {
       if (!(c[i] > none)) c[i] = none;
     }
   }
-  bool open_question = false;
   if (a.groups > 1) {
     Real mine = none;  // lane q: group q's score
     for (int q = 0; q < a.groups; q++) {
@@ -196,28 +187,19 @@ __device__ __noinline__ bool choose(const Args& a, int64_t t, int* pick) {
       const Real other = __shfl_sync(ALL, mine, q);
       ahead += other > mine || (other == mine && q < lane);
     }
-    const bool is_open = lane < a.groups && ahead < a.top_groups;
-    const unsigned open = __ballot_sync(ALL, is_open);
-    if (!wide && by_score) {
-      const float least = -max_over<32>(is_open ? -static_cast<float>(mine) : -CUDART_INF_F);
-      const float most = max_over<32>(is_open ? -CUDART_INF_F : static_cast<float>(mine));
-      open_question = most > -CUDART_INF_F && least < CUDART_INF_F && !apart(least, most, 2.f * tol);
-    }
+    const unsigned open = __ballot_sync(ALL, lane < a.groups && ahead < a.top_groups);
 #pragma unroll
     for (int i = 0; i < M; i++) {
       const int e = lane + 32 * i;
       if (e < a.E && !(open >> (e / size) & 1)) c[i] = none;
     }
   }
-  if (by_score && !a.bias) {  // the logits order the scores
+  if (scores && !a.bias) {  // the logits order the scores
 #pragma unroll
     for (int i = 0; i < M; i++)
       if (c[i] > none) c[i] = load<TYPE>(a.logits, t * a.logits_ld + lane + 32 * i);
   }
-  // After the k-th, those that may be as good as it are looked at, too.
-  Real before = 0;
-  int e_before = -1;
-  for (int j = 0; j < a.E; j++) {
+  for (int j = 0; j < a.k; j++) {
     Real m = none;
     int at = MAX_EXPERTS;
 #pragma unroll
@@ -232,17 +214,8 @@ __device__ __noinline__ bool choose(const Args& a, int64_t t, int* pick) {
 #pragma unroll
     for (int i = 0; i < M; i++)
       if (lane + 32 * i == at) c[i] = none;
-    if (j < a.k && lane == 0) pick[j] = at < MAX_EXPERTS ? at : -1;
-    if (!wide && a.bias && j > 0 && at < MAX_EXPERTS && !apart(before, m, tol)) {
-      open_question |= load<TYPE>(a.logits, t * a.logits_ld + e_before) != load<TYPE>(a.logits, t * a.logits_ld + at) || a.bias[e_before] != a.bias[at];
-      if (j >= a.k && open_question) break;
-    } else if (j >= a.k) {
-      break;
-    }
-    if (j >= a.k - 1 && (wide || !a.bias || at >= MAX_EXPERTS)) break;
-    if (j < a.k) before = m, e_before = at;
+    if (lane == 0) pick[j] = at < MAX_EXPERTS ? at : -1;
   }
-  return open_question;
 }
 
 // As bits that order as the values do, -inf at NONE.
@@ -281,10 +254,10 @@ __device__ __forceinline__ uint32_t key_over(uint32_t x) {
   }
 }
 
-// Shared memory of a block of k_route: counts, a warp's picks made again, and for groups that no whole lanes hold a row's keys
-// and the bounds of its groups' scores.
+// Shared memory of a block of k_route: counts, rows' choices (key and expert), a warp's choices made again, and for groups that
+// no whole lanes hold a row's keys and the bounds of its groups' scores.
 struct Shared {
-  int hist, pick, row, score, bytes;  // offsets
+  int list, hist, pick, row, score, bytes;  // offsets
 };
 __host__ __device__ inline bool groups_of_lanes(int E, int groups, int M) {
   const int lanes = E / groups / M;
@@ -293,7 +266,8 @@ __host__ __device__ inline bool groups_of_lanes(int E, int groups, int M) {
 __host__ __device__ inline Shared shared_of(int E, int groups, int G, int M) {
   const bool rows = groups > 1 && !groups_of_lanes(E, groups, M);
   Shared s;
-  s.hist = 0;
+  s.list = 0;
+  s.hist = s.list + 8 * (THREADS / G) * (G + 1);
   s.pick = s.hist + 4 * E;
   s.row = s.pick + 4 * THREADS;
   s.score = s.row + (rows ? 4 * THREADS * M : 0);
@@ -307,20 +281,24 @@ __device__ __forceinline__ float reciprocal(float x) {
   return y;
 }
 
+// Blocks of k_route that an SM holds, by their registers.
+__host__ __device__ constexpr int blocks_of(int M, bool scores) { return M > 8 ? 2 : scores ? 3 : 4; }
+
 // SCORES: the choice goes by scores, or among groups; else by the logits alone.  k <= G: a lane has one pick at most.
 // word: elements that all rows are aligned for.
 template <int TYPE, int M, int G, bool SCORES>
-__global__ void __launch_bounds__(THREADS, M == 8 ? 4 : 2) k_route(const __grid_constant__ Args a, int word) {
+__global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const __grid_constant__ Args a, int word) {
   extern __shared__ __align__(16) char smem[];
   using T = typename Of<TYPE>::T;
-  constexpr uint32_t LOW = (1u << (M == 8 ? 8 : M == 16 ? 9 : 10)) - 1;  // the bits of a key that hold its column
+  constexpr uint32_t LOW = M - 1;  // the bits of a key that hold its place in the lane
   constexpr bool LOSSLESS = !SCORES && TYPE != IWP_F32;
   constexpr int ROWS = THREADS / G;
   const Shared at = shared_of(a.E, a.groups, G, M);
   const int tid = threadIdx.x, lane = tid & 31, g = lane & (G - 1), rl = tid / G, row0 = lane & ~(G - 1);
+  uint2* const list = reinterpret_cast<uint2*>(smem + at.list) + rl * (G + 1);
   int* const hist = reinterpret_cast<int*>(smem + at.hist);
   int* const pick = reinterpret_cast<int*>(smem + at.pick) + (tid & ~31);
-  const unsigned of_row = (G == 32 ? ALL : (1u << G) - 1) << row0;
+  const unsigned of_row = (G == 32 ? ALL : (1u << G) - 1) << row0, before = ((1u << lane) - 1) & of_row;
   const int first = g * M;
   const bool softmax = a.score == IWP_SOFTMAX, renormalize = a.renormalize, count = a.counts != nullptr;
   const bool by_score = SCORES && (a.bias || (a.groups > 1 && a.group_top == 2));
@@ -336,12 +314,8 @@ __global__ void __launch_bounds__(THREADS, M == 8 ? 4 : 2) k_route(const __grid_
       if (!(bias[i] > -CUDART_INF_F)) bias[i] = -CUDART_INF_F;  // not available
     }
   }
-  uint32_t column[M];  // a key's low bits
-#pragma unroll
-  for (int i = 0; i < M; i++) column[i] = LOW - first - i;
-  const int64_t steps = (a.T + ROWS - 1) / ROWS;
-  for (int64_t step = blockIdx.x; step < steps; step += gridDim.x) {
-    const int64_t t = step * ROWS + rl;
+  for (int t0 = blockIdx.x * ROWS; t0 < a.T; t0 += gridDim.x * ROWS) {
+    const int t = t0 + rl;
     const T* const row = static_cast<const T*>(a.logits) + t * a.logits_ld;
     const bool in = t < a.T, on = in && (!a.mask || a.mask[t]);
     float x[M];
@@ -395,10 +369,10 @@ __global__ void __launch_bounds__(THREADS, M == 8 ? 4 : 2) k_route(const __grid_
           if (x[i] == -CUDART_INF_F) c[i] = -CUDART_INF_F;
       }
 #pragma unroll
-      for (int i = 0; i < M; i++) key[i] = (ordered(c[i]) & ~LOW) | column[i];
+      for (int i = 0; i < M; i++) key[i] = (ordered(c[i]) & ~LOW) | (LOW - i);
     } else {
 #pragma unroll
-      for (int i = 0; i < M; i++) key[i] = (ordered(x[i]) & ~LOW) | column[i];
+      for (int i = 0; i < M; i++) key[i] = (ordered(x[i]) & ~LOW) | (LOW - i);
     }
     bool again = false;  // by a warp
     if (SCORES && a.groups > 1) {
@@ -482,12 +456,13 @@ __global__ void __launch_bounds__(THREADS, M == 8 ? 4 : 2) k_route(const __grid_
     } else {
       sort_keys<M>(key);
     }
-    // the k largest, and one more, to see how far behind it is: lane j's own and the next
-    uint32_t mine = 0, next = 0;
-    const int picks = LOSSLESS ? a.k : a.k + 1;
-    for (int j = 0; j < picks; j++) {
-      const uint32_t m = key_over<G>(key[0]);
-      const bool pop = key[0] == m;
+    // the k largest, and one more, to see how far behind it is
+    auto take = [&](int j) {
+      const uint32_t head = key[0] | LOW;  // (places in different lanes do not compare)
+      const bool hit = head == key_over<G>(head);
+      const unsigned holders = __ballot_sync(ALL, hit);
+      const bool pop = hit && !(holders & before);
+      if (pop) list[j] = make_uint2(key[0], first + LOW - (key[0] & LOW));
 #pragma unroll
       for (int i = 0; i < 7; i++) key[i] = pop ? key[i + 1] : key[i];
       if constexpr (M == 8) {
@@ -497,30 +472,55 @@ __global__ void __launch_bounds__(THREADS, M == 8 ? 4 : 2) k_route(const __grid_
         for (int i = 7; i < M - 1; i++) key[i] = pop ? key[i + 1] : key[i];
         if (pop) key[M - 1] = 0;
       }
-      if (g == j) mine = m;
-      if (!LOSSLESS && g + 1 == j) next = m;
-    }
-    int e = mine > NONE && on && g < a.k ? static_cast<int>(LOW - (mine & LOW)) : -1;
+    };
+    const int picks = LOSSLESS ? a.k : a.k + 1;
+    for (int j = 0; j < picks; j++) take(j);
+    __syncwarp();
+    const uint2 mine = list[g < a.k ? g : 0];
+    int e = mine.x > NONE && on && g < a.k ? static_cast<int>(mine.y) : -1;
     float y = e >= 0 ? static_cast<float>(row[e]) : -CUDART_INF_F;
     if constexpr (!LOSSLESS) {
-      const float y2 = __shfl_down_sync(ALL, y, 1);
-      if (e >= 0 && next > NONE) {
-        const bool close = SCORES ? !apart(unordered(mine & ~LOW), unordered(next | LOW), tol) : (mine ^ next) <= LOW;
-        if (close) {
-          if (g == a.k - 1)
-            again = true;  // others may be as close
-          else if (SCORES && a.bias)
-            again |= y != y2 || a.bias[e] != a.bias[LOW - (next & LOW)];
+      auto close = [&](uint32_t high, uint32_t low) {
+        return low > NONE && (SCORES ? !apart(unordered(high & ~LOW), unordered(low | LOW), tol) : (high ^ low) <= LOW);
+      };
+      auto differ = [&](int e1) { return y != static_cast<float>(row[e1]) || (SCORES && a.bias && a.bias[e] != a.bias[e1]); };
+      bool last = false;  // this lane's choice is the row's last, and the next is as good
+      if (e >= 0) {
+        const uint2 next = list[g + 1];
+        if (close(mine.x, next.x)) {
+          if (g < a.k - 1)
+            again |= SCORES && a.bias ? differ(next.y) : y < static_cast<float>(row[next.y]);
+          else if (differ(next.y))
+            again = true;
           else
-            again |= y < y2;
+            last = true;  // so may be others
+        }
+      }
+      for (int n = 0; __any_sync(ALL, last); n++) {
+        __syncwarp();
+        if (M == 8 && n < 4) {
+          take(a.k);
+          __syncwarp();
+        }
+        if (last) {
+          const uint2 next = list[a.k];
+          if (M > 8 || n >= 4)
+            again = true, last = false;
+          else if (!close(mine.x, next.x))
+            last = false;
+          else if (differ(next.y))
+            again = true, last = false;
         }
       }
       unsigned todo = __ballot_sync(ALL, again && on && !bad);
       while (todo) {
         const int who = __ffs(todo) - 1, who0 = who & ~(G - 1);
         todo &= ~((G == 32 ? ALL : (1u << G) - 1) << who0);
-        const int64_t which = __shfl_sync(ALL, t, who);
-        if (choose<TYPE, M, float>(a, which, pick)) choose<TYPE, M, double>(a, which, pick);
+        const int which = __shfl_sync(ALL, t, who);
+        if (by_score)
+          choose<TYPE, M, double>(a, which, pick);
+        else
+          choose<TYPE, M, float>(a, which, pick);
         __syncwarp();
         if (row0 == who0 && g < a.k) {
           e = pick[g];
@@ -538,14 +538,17 @@ __global__ void __launch_bounds__(THREADS, M == 8 ? 4 : 2) k_route(const __grid_
     } else {  // sigmoid, times e^-ref, so that scores far below one still have a ratio
       float ref = 0.f;
       if (renormalize) ref = fminf(SCORES ? max_over<G>(y) : __shfl_sync(ALL, y, row0), 0.f);
-      if (y > -CUDART_INF_F) w = y >= 0.f ? 1.f / (1.f + expf(-y)) : expf(y - ref) / (1.f + expf(y));
+      if (y > -CUDART_INF_F) {
+        const float far = expf(-fabsf(y));
+        w = (y >= 0.f ? 1.f : ref == 0.f ? far : expf(y - ref)) / (1.f + far);
+      }
     }
     if (renormalize) s = sum_over<G>(w);
     if (softmax || renormalize) w *= s > 0.f ? a.weight_scale / s : 0.f;
     else w *= a.weight_scale;
     if (bad && on) w = CUDART_NAN_F, e = -1;
     if (in && g < a.k) {
-      const int64_t to = t * a.k + g;
+      const int64_t to = static_cast<int64_t>(t) * a.k + g;
       a.weights[to] = w;
       if (a.ids_bytes == 8)
         static_cast<int64_t*>(a.ids)[to] = e;
@@ -553,6 +556,7 @@ __global__ void __launch_bounds__(THREADS, M == 8 ? 4 : 2) k_route(const __grid_
         static_cast<int32_t*>(a.ids)[to] = e;
       if (count && e >= 0) atomicAdd(&hist[e], 1);
     }
+    __syncwarp();  // the list has been read
   }
   if (!count) return;
   __syncthreads();
@@ -579,8 +583,9 @@ struct GradArgs {
   const float* weights;
   const float* dweights;
   void* dlogits;
-  int64_t logits_ld, ids_ld, weights_ld, dweights_ld, dlogits_ld, T;
+  int64_t logits_ld, ids_ld, weights_ld, dweights_ld, dlogits_ld;
   float inv_scale, scale;
+  int T;
   int E, k, score, renormalize, ids_bytes, accumulate;
 };
 
@@ -595,9 +600,8 @@ __global__ void __launch_bounds__(THREADS, M == 8 ? 4 : 2) k_route_grad(const __
   const bool softmax = a.score == IWP_SOFTMAX, dense = softmax && !a.renormalize;
   launch_next();
   wait_previous();
-  const int64_t steps = (a.T + ROWS - 1) / ROWS;
-  for (int64_t step = blockIdx.x; step < steps; step += gridDim.x) {
-    const int64_t t = step * ROWS + rl;
+  for (int t0 = blockIdx.x * ROWS; t0 < a.T; t0 += gridDim.x * ROWS) {
+    const int t = t0 + rl;
     const bool in = t < a.T;
     const T* const row = static_cast<const T*>(a.logits) + t * a.logits_ld;
     T* const out = static_cast<T*>(a.dlogits) + t * a.dlogits_ld;

@@ -42,7 +42,7 @@ int launch_route_form(const Args& r, int word, cudaStream_t st) {
   static std::atomic<int> allowed[MAX_DEVICES] = {};
   LOSS_CUDA(allow_shared(kernel, smem, allowed));
   const int64_t steps = tiles_of(r.T, THREADS / G);
-  LOSS_CUDA(launch(kernel, std::max<int64_t>(1, std::min<int64_t>(steps, (M == 8 ? 4 : 2) * SMS)), THREADS, smem, 1, st, r, word));
+  LOSS_CUDA(launch(kernel, std::max<int64_t>(1, std::min<int64_t>(steps, blocks_of(M, SCORES) * SMS)), THREADS, smem, 1, st, r, word));
   return IWP_OK;
 }
 
