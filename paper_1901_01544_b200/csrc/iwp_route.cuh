@@ -254,10 +254,11 @@ __device__ __forceinline__ uint32_t key_over(uint32_t x) {
   }
 }
 
-// Shared memory of a block of k_route: counts, rows' choices (key and expert), a warp's choices made again, and for groups that
+// Shared memory of a block of k_route: lanes' sorted keys, rows' choices (key and lane), counts, a warp's choices made again, and for groups that
 // no whole lanes hold a row's keys and the bounds of its groups' scores.
+__host__ __device__ constexpr int stride_of(int M) { return M + 4; }  // of a lane's sorted keys and a zero: no two of eight lanes share a bank
 struct Shared {
-  int list, hist, pick, row, score, bytes;  // offsets
+  int waiting, list, hist, pick, row, score, bytes;  // offsets
 };
 __host__ __device__ inline bool groups_of_lanes(int E, int groups, int M) {
   const int lanes = E / groups / M;
@@ -266,7 +267,8 @@ __host__ __device__ inline bool groups_of_lanes(int E, int groups, int M) {
 __host__ __device__ inline Shared shared_of(int E, int groups, int G, int M) {
   const bool rows = groups > 1 && !groups_of_lanes(E, groups, M);
   Shared s;
-  s.list = 0;
+  s.waiting = 0;
+  s.list = s.waiting + 4 * THREADS * stride_of(M);
   s.hist = s.list + 8 * (THREADS / G) * (G + 1);
   s.pick = s.hist + 4 * E;
   s.row = s.pick + 4 * THREADS;
@@ -295,6 +297,7 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
   constexpr int ROWS = THREADS / G;
   const Shared at = shared_of(a.E, a.groups, G, M);
   const int tid = threadIdx.x, lane = tid & 31, g = lane & (G - 1), rl = tid / G, row0 = lane & ~(G - 1);
+  uint32_t* const waiting = reinterpret_cast<uint32_t*>(smem + at.waiting) + tid * stride_of(M);
   uint2* const list = reinterpret_cast<uint2*>(smem + at.list) + rl * (G + 1);
   int* const hist = reinterpret_cast<int*>(smem + at.hist);
   int* const pick = reinterpret_cast<int*>(smem + at.pick) + (tid & ~31);
@@ -304,6 +307,7 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
   const bool by_score = SCORES && (a.bias || (a.groups > 1 && a.group_top == 2));
   launch_next();
   for (int e = tid; e < a.E; e += THREADS) hist[e] = 0;
+  waiting[M] = 0;
   wait_previous();
   __syncthreads();
   float bias[M];
@@ -456,27 +460,27 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
     } else {
       sort_keys<M>(key);
     }
-    // the k largest, and one more, to see how far behind it is
+    // the k largest, and one more, to see how far behind it is: a lane's keys wait in shared memory, behind them a zero
+#pragma unroll
+    for (int i = 0; i < M; i += 4) reinterpret_cast<uint4*>(waiting)[i / 4] = make_uint4(key[i], key[i + 1], key[i + 2], key[i + 3]);
+    uint32_t head = key[0];
+    const uint32_t* ahead_of = waiting + 1;
     auto take = [&](int j) {
-      const uint32_t head = key[0] | LOW;  // (places in different lanes do not compare)
-      const bool hit = head == key_over<G>(head);
+      const bool hit = (head | LOW) == key_over<G>(head | LOW);  // (places in different lanes do not compare)
       const unsigned holders = __ballot_sync(ALL, hit);
-      const bool pop = hit && !(holders & before);
-      if (pop) list[j] = make_uint2(key[0], first + LOW - (key[0] & LOW));
-#pragma unroll
-      for (int i = 0; i < 7; i++) key[i] = pop ? key[i + 1] : key[i];
-      if constexpr (M == 8) {
-        if (pop) key[7] = 0;
-      } else if (a.k > 7) {  // (else no lane gets that far)
-#pragma unroll
-        for (int i = 7; i < M - 1; i++) key[i] = pop ? key[i + 1] : key[i];
-        if (pop) key[M - 1] = 0;
+      if (hit && !(holders & before)) {
+        list[j] = make_uint2(head, first);
+        head = *ahead_of++;
       }
     };
     const int picks = LOSSLESS ? a.k : a.k + 1;
     for (int j = 0; j < picks; j++) take(j);
     __syncwarp();
-    const uint2 mine = list[g < a.k ? g : 0];
+    auto listed = [&](int j) {  // (key, expert)
+      const uint2 p = list[j];
+      return make_uint2(p.x, p.y + (LOW - (p.x & LOW)));
+    };
+    const uint2 mine = listed(g < a.k ? g : 0);
     int e = mine.x > NONE && on && g < a.k ? static_cast<int>(mine.y) : -1;
     float y = e >= 0 ? static_cast<float>(row[e]) : -CUDART_INF_F;
     if constexpr (!LOSSLESS) {
@@ -486,7 +490,7 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
       auto differ = [&](int e1) { return y != static_cast<float>(row[e1]) || (SCORES && a.bias && a.bias[e] != a.bias[e1]); };
       bool last = false;  // this lane's choice is the row's last, and the next is as good
       if (e >= 0) {
-        const uint2 next = list[g + 1];
+        const uint2 next = listed(g + 1);
         if (close(mine.x, next.x)) {
           if (g < a.k - 1)
             again |= SCORES && a.bias ? differ(next.y) : y < static_cast<float>(row[next.y]);
@@ -498,13 +502,13 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
       }
       for (int n = 0; __any_sync(ALL, last); n++) {
         __syncwarp();
-        if (M == 8 && n < 4) {
+        if (n < 4) {
           take(a.k);
           __syncwarp();
         }
         if (last) {
-          const uint2 next = list[a.k];
-          if (M > 8 || n >= 4)
+          const uint2 next = listed(a.k);
+          if (n >= 4)
             again = true, last = false;
           else if (!close(mine.x, next.x))
             last = false;
