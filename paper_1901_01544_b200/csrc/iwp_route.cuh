@@ -1,11 +1,12 @@
 // iwp_route.cuh - choice of experts from a router's logits with the weights of the chosen, and the gradient to the logits.
 //
-// A row of E logits lives in the registers of G lanes (2 to 32), M neighbouring columns per lane.  A column's key is its choice
-// value in an order-preserving 32-bit code whose lowest bits give way to the column's place in its lane.  Every lane sorts its
-// keys by a network; then the largest head is taken k times, the lowest lane's where several hold it: so ties go to the lower
-// expert.  Of 16-bit logits the codes lose nothing.  Where they (or the rounding of scores) may have hidden an order, a warp
-// makes the row's choice again: by the logits themselves, or by scores in 64 bits (a row in a thousand where values differ).
-// Only the chosen scores have to be exact to the last bits, and only they are computed that way, by k lanes at the end.
+// A row of E logits lives in the registers of G lanes (8 up to 256 experts and 8 choices, so that a warp works on four rows at
+// a time), M columns per lane, word by word in turn.  A column's key is its choice value in an order-preserving 32-bit code
+// whose lowest bits give way to the column's place in its lane.  Every lane sorts its eight largest keys by a network; then the largest
+// head is taken k times, ties as the columns go: so they fall to the lower expert.  Of 16-bit logits the codes lose
+// nothing.  Where they (or the rounding of scores) may have hidden an order, a warp makes the row's choice again: by the
+// logits themselves, or by scores in 64 bits (a row in a few hundred where values differ).  Only the chosen scores have to be exact
+// to the last bits, and only they are computed that way, by k lanes at the end.
 #pragma once
 
 #include <type_traits>
@@ -53,38 +54,35 @@ __device__ __forceinline__ float load(const void* p, int64_t at) {
   return static_cast<float>(static_cast<const typename Of<TYPE>::T*>(p)[at]);
 }
 
-// M columns from `first` on of a row, in words of VEC; -inf outside.
-template <int TYPE, int M, int VEC>
-__device__ __forceinline__ void load_words(float (&x)[M], const typename Of<TYPE>::T* row, int first, int E, bool in) {
-  using W = Word<TYPE, VEC>;
-  const auto* const p = row + first;
+// Lane g's M columns of a row, in words of VEC that the G lanes take in turn: place i holds column
+// ((i / VEC) G + g) VEC + i % VEC.  -inf outside.
+template <int TYPE, int M, int G, int VEC>
+__device__ __forceinline__ void load_words(float (&x)[M], const typename Of<TYPE>::T* row, int g, int E, bool in) {
 #pragma unroll
   for (int n = 0; n < M / VEC; n++) {
-    if (in && first + n * VEC < E) {
-      const W w = *reinterpret_cast<const W*>(p + n * VEC);
+    const int first = (n * G + g) * VEC;
+    Raw<TYPE, VEC> w;
+    const bool here = in && first < E;
+    if (here) w = *reinterpret_cast<const Raw<TYPE, VEC>*>(row + first);
 #pragma unroll
-      for (int v = 0; v < VEC; v++) x[n * VEC + v] = static_cast<float>(w.x[v]);
-    } else {
-#pragma unroll
-      for (int v = 0; v < VEC; v++) x[n * VEC + v] = -CUDART_INF_F;
-    }
+    for (int v = 0; v < VEC; v++) x[n * VEC + v] = here ? element<TYPE, VEC>(w, v) : -CUDART_INF_F;
   }
 }
 
-// M columns of results, `add` to what is there.
-template <int TYPE, int M, int VEC>
-__device__ __forceinline__ void store_words(const float (&x)[M], typename Of<TYPE>::T* row, int first, int E, bool add) {
+// The same columns of results, with `add` added to what is there.
+template <int TYPE, int M, int G, int VEC>
+__device__ __forceinline__ void store_words(const float (&x)[M], typename Of<TYPE>::T* row, int g, int E, bool add) {
   using T = typename Of<TYPE>::T;
   using W = Word<TYPE, VEC>;
-  T* const p = row + first;
 #pragma unroll
   for (int n = 0; n < M / VEC; n++) {
-    if (first + n * VEC >= E) continue;
+    const int first = (n * G + g) * VEC;
+    if (first >= E) continue;
     W w;
-    if (add) w = *reinterpret_cast<const W*>(p + n * VEC);
+    if (add) w = *reinterpret_cast<const W*>(row + first);
 #pragma unroll
     for (int v = 0; v < VEC; v++) w.x[v] = static_cast<T>(add ? x[n * VEC + v] + static_cast<float>(w.x[v]) : x[n * VEC + v]);
-    *reinterpret_cast<W*>(p + n * VEC) = w;
+    *reinterpret_cast<W*>(row + first) = w;
   }
 }
 
@@ -99,9 +97,9 @@ __device__ __forceinline__ void with_word(int word, const F& f) {
   f(std::integral_constant<int, 1>{});
 }
 
-template <int TYPE, int M>
-__device__ __forceinline__ void load_columns(float (&x)[M], const typename Of<TYPE>::T* row, int first, int E, bool in, int word) {
-  with_word<TYPE>(word, [&](auto v) { load_words<TYPE, M, decltype(v)::value>(x, row, first, E, in); });
+template <int TYPE, int M, int G>
+__device__ __forceinline__ void load_columns(float (&x)[M], const typename Of<TYPE>::T* row, int g, int E, bool in, int word) {
+  with_word<TYPE>(word, [&](auto v) { load_words<TYPE, M, G, decltype(v)::value>(x, row, g, E, in); });
 }
 
 // Over groups of G lanes.
@@ -226,21 +224,39 @@ __device__ __forceinline__ uint32_t ordered(float x) {
 }
 __device__ __forceinline__ float unordered(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u); }
 
-// Batcher's odd-even merge sort, descending.
+__device__ __forceinline__ void in_order(uint32_t& a, uint32_t& b) {
+  const uint32_t high = max(a, b), low = min(a, b);
+  a = high, b = low;
+}
+// Batcher's odd-even merge sort of eight keys from `first` on, descending.
 template <int M>
-__device__ __forceinline__ void sort_keys(uint32_t (&x)[M]) {
+__device__ __forceinline__ void sort_eight(uint32_t (&x)[M], int first) {
 #pragma unroll
-  for (int p = 1; p < M; p *= 2)
+  for (int p = 1; p < 8; p *= 2)
 #pragma unroll
     for (int k = p; k >= 1; k /= 2)
 #pragma unroll
-      for (int j = k % p; j <= M - 1 - k; j += 2 * k)
+      for (int j = k % p; j <= 7 - k; j += 2 * k)
 #pragma unroll
         for (int i = 0; i < k; i++)
-          if (i + j + k < M && (i + j) / (2 * p) == (i + j + k) / (2 * p)) {
-            const uint32_t high = max(x[i + j], x[i + j + k]), low = min(x[i + j], x[i + j + k]);
-            x[i + j] = high, x[i + j + k] = low;
-          }
+          if (i + j + k < 8 && (i + j) / (2 * p) == (i + j + k) / (2 * p)) in_order(x[first + i + j], x[first + i + j + k]);
+}
+// The eight largest keys, descending, in front: of two sorted eights they are the larger of each pair from opposite ends, which
+// are bitonic.
+template <int M>
+__device__ __forceinline__ void top_eight(uint32_t (&x)[M]) {
+  sort_eight(x, 0);
+#pragma unroll
+  for (int b = 8; b < M; b += 8) {
+    sort_eight(x, b);
+#pragma unroll
+    for (int i = 0; i < 8; i++) x[i] = max(x[i], x[b + 7 - i]);
+#pragma unroll
+    for (int k = 4; k >= 1; k /= 2)
+#pragma unroll
+      for (int i = 0; i < 8; i++)
+        if (!(i & k)) in_order(x[i], x[i + k]);
+  }
 }
 
 template <int G>
@@ -254,26 +270,23 @@ __device__ __forceinline__ uint32_t key_over(uint32_t x) {
   }
 }
 
-// Shared memory of a block of k_route: lanes' sorted keys, rows' choices (key and lane), counts, a warp's choices made again, and for groups that
-// no whole lanes hold a row's keys and the bounds of its groups' scores.
-__host__ __device__ constexpr int stride_of(int M) { return M + 4; }  // of a lane's sorted keys and a zero: no two of eight lanes share a bank
+// Shared memory of a block of k_route: lanes' sorted keys and a zero behind them (no two of eight lanes share a bank), rows' choices
+// (key and lane), counts, a warp's choices made again, and where there are groups a row's keys in the order of the columns and
+// the bounds of its groups' scores.
+constexpr int WAITING = 12;
 struct Shared {
   int waiting, list, hist, pick, row, score, bytes;  // offsets
 };
-__host__ __device__ inline bool groups_of_lanes(int E, int groups, int M) {
-  const int lanes = E / groups / M;
-  return lanes * M * groups == E && (lanes & (lanes - 1)) == 0;
-}
 __host__ __device__ inline Shared shared_of(int E, int groups, int G, int M) {
-  const bool rows = groups > 1 && !groups_of_lanes(E, groups, M);
+  const int rows = THREADS / G;
   Shared s;
   s.waiting = 0;
-  s.list = s.waiting + 4 * THREADS * stride_of(M);
-  s.hist = s.list + 8 * (THREADS / G) * (G + 1);
+  s.list = s.waiting + 4 * THREADS * WAITING;
+  s.hist = s.list + 8 * rows * (G + 1);
   s.pick = s.hist + 4 * E;
   s.row = s.pick + 4 * THREADS;
-  s.score = s.row + (rows ? 4 * THREADS * M : 0);
-  s.bytes = s.score + (rows ? 8 * (THREADS / G) * groups : 0);
+  s.score = s.row + (groups > 1 ? 4 * rows * G * M : 0);
+  s.bytes = s.score + (groups > 1 ? 8 * rows * groups : 0);
   return s;
 }
 
@@ -283,8 +296,19 @@ __device__ __forceinline__ float reciprocal(float x) {
   return y;
 }
 
+// The bias of lane g's columns, in words of the rows' width.
+template <int M, int G>
+__device__ __forceinline__ void load_bias(float (&b)[M], const float* bias, int g, int E, int word) {
+  const int shift = __popc(word - 1);
+#pragma unroll
+  for (int i = 0; i < M; i++) {
+    const int e = ((((i >> shift) * G + g) << shift) + (i & (word - 1)));
+    b[i] = e < E ? __ldg(bias + e) : 0.f;
+  }
+}
+
 // Blocks of k_route that an SM holds, by their registers.
-__host__ __device__ constexpr int blocks_of(int M, bool scores) { return M > 8 ? 2 : scores ? 3 : 4; }
+__host__ __device__ constexpr int blocks_of(int M, bool scores) { return M == 8 ? (scores ? 3 : 4) : M == 16 ? 3 : 2; }
 
 // SCORES: the choice goes by scores, or among groups; else by the logits alone.  k <= G: a lane has one pick at most.
 // word: elements that all rows are aligned for.
@@ -294,183 +318,159 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
   using T = typename Of<TYPE>::T;
   constexpr uint32_t LOW = M - 1;  // the bits of a key that hold its place in the lane
   constexpr bool LOSSLESS = !SCORES && TYPE != IWP_F32;
-  constexpr int ROWS = THREADS / G;
+  constexpr int ROWS = THREADS / G, AGAIN = M * G > 32 ? M * G / 32 : 1;  // columns per lane where a warp has one row
   const Shared at = shared_of(a.E, a.groups, G, M);
   const int tid = threadIdx.x, lane = tid & 31, g = lane & (G - 1), rl = tid / G, row0 = lane & ~(G - 1);
-  uint32_t* const waiting = reinterpret_cast<uint32_t*>(smem + at.waiting) + tid * stride_of(M);
+  uint32_t* const waiting = reinterpret_cast<uint32_t*>(smem + at.waiting) + tid * WAITING;
   uint2* const list = reinterpret_cast<uint2*>(smem + at.list) + rl * (G + 1);
   int* const hist = reinterpret_cast<int*>(smem + at.hist);
   int* const pick = reinterpret_cast<int*>(smem + at.pick) + (tid & ~31);
   const unsigned of_row = (G == 32 ? ALL : (1u << G) - 1) << row0, before = ((1u << lane) - 1) & of_row;
-  const int first = g * M;
+  const uint32_t in_word = word - 1;
+  const int shift = __popc(in_word);
+  auto column = [&](uint32_t place, int of_lane) { return static_cast<int>((((place >> shift) * G + of_lane) << shift) + (place & in_word)); };
   const bool softmax = a.score == IWP_SOFTMAX, renormalize = a.renormalize, count = a.counts != nullptr;
   const bool by_score = SCORES && (a.bias || (a.groups > 1 && a.group_top == 2));
   launch_next();
   for (int e = tid; e < a.E; e += THREADS) hist[e] = 0;
-  waiting[M] = 0;
+  waiting[8] = 0;
   wait_previous();
   __syncthreads();
-  float bias[M];
-  if constexpr (SCORES) {
-#pragma unroll
-    for (int i = 0; i < M; i++) {
-      bias[i] = a.bias && first + i < a.E ? __ldg(a.bias + first + i) : 0.f;
-      if (!(bias[i] > -CUDART_INF_F)) bias[i] = -CUDART_INF_F;  // not available
-    }
-  }
   for (int t0 = blockIdx.x * ROWS; t0 < a.T; t0 += gridDim.x * ROWS) {
     const int t = t0 + rl;
     const T* const row = static_cast<const T*>(a.logits) + t * a.logits_ld;
     const bool in = t < a.T, on = in && (!a.mask || a.mask[t]);
-    float x[M];
-    load_columns<TYPE, M>(x, row, first, a.E, on, word);
-    // rows that hold a NaN or an infinity are looked at again
-    float odd = 0.f;
-#pragma unroll
-    for (int i = 0; i < M; i++) odd = fmaf(x[i], 0.f, odd);
-    bool bad = false;
-    if (odd != odd) {
-#pragma unroll
-      for (int i = 0; i < M; i++) bad |= isnan(x[i]) || (softmax && x[i] == CUDART_INF_F);
-    }
-    bad = (__ballot_sync(ALL, bad) & of_row) != 0;
-    float top = -CUDART_INF_F, s = 0.f;  // of the row: largest logit, sum of exponentials below it
-    if (softmax && (SCORES || !renormalize)) {
-#pragma unroll
-      for (int i = 0; i < M; i++) top = fmaxf(top, x[i]);
-      top = max_over<G>(top);
-      if (!renormalize) {
-#pragma unroll
-        for (int i = 0; i < M; i++) s += x[i] == -CUDART_INF_F ? 0.f : expf(x[i] - top);
-        s = sum_over<G>(s);
-      }
-    }
     uint32_t key[M];
-    float tol = 0.f;
-    if (SCORES && by_score) {
-      float c[M], scale = 1.f;
-      tol = SIGMOID_TOLERANCE;
-      if (softmax) {
-        float sum = 0.f;
+    bool bad = false;
+    float top = -CUDART_INF_F, s = 0.f, tol = 0.f;  // of the row: largest logit, sum of exponentials below it
+    {
+      float x[M];
+      load_columns<TYPE, M, G>(x, row, g, a.E, on, word);
+      // rows that hold a NaN or an infinity are looked at again
+      float odd = 0.f;
 #pragma unroll
-        for (int i = 0; i < M; i++) {
-          c[i] = ex2((x[i] - top) * LOG2E);
-          if (x[i] == -CUDART_INF_F) c[i] = 0.f;
-          sum += c[i];
-        }
-        sum = sum_over<G>(sum);
-        scale = sum > 0.f ? reciprocal(sum) : 0.f;
-        tol = SOFTMAX_TOLERANCE * scale;
-      } else {
-#pragma unroll
-        for (int i = 0; i < M; i++) c[i] = reciprocal(1.f + ex2(-x[i] * LOG2E));
-      }
-#pragma unroll
-      for (int i = 0; i < M; i++) c[i] = fmaf(c[i], scale, bias[i]);
+      for (int i = 0; i < M; i++) odd = fmaf(x[i], 0.f, odd);
       if (odd != odd) {
 #pragma unroll
-        for (int i = 0; i < M; i++)
-          if (x[i] == -CUDART_INF_F) c[i] = -CUDART_INF_F;
+        for (int i = 0; i < M; i++) bad |= isnan(x[i]) || (softmax && x[i] == CUDART_INF_F);
       }
+      bad = (__ballot_sync(ALL, bad) & of_row) != 0;
+      if (softmax && (SCORES || !renormalize)) {
 #pragma unroll
-      for (int i = 0; i < M; i++) key[i] = (ordered(c[i]) & ~LOW) | (LOW - i);
-    } else {
+        for (int i = 0; i < M; i++) top = fmaxf(top, x[i]);
+        top = max_over<G>(top);
+        if (!renormalize) {
 #pragma unroll
-      for (int i = 0; i < M; i++) key[i] = (ordered(x[i]) & ~LOW) | (LOW - i);
+          for (int i = 0; i < M; i++) s += x[i] == -CUDART_INF_F ? 0.f : expf(x[i] - top);
+          s = sum_over<G>(s);
+        }
+      }
+      if (SCORES && by_score) {
+        tol = SIGMOID_TOLERANCE;
+        float scale = 1.f;
+        if (softmax) {
+          float sum = 0.f;
+#pragma unroll
+          for (int i = 0; i < M; i++) {
+            const bool none = x[i] == -CUDART_INF_F;
+            x[i] = ex2((x[i] - top) * LOG2E);
+            if (none) x[i] = 0.f;
+            sum += x[i];
+            key[i] = none;
+          }
+          sum = sum_over<G>(sum);
+          scale = sum > 0.f ? reciprocal(sum) : 0.f;
+          tol = SOFTMAX_TOLERANCE * scale;
+        } else {
+#pragma unroll
+          for (int i = 0; i < M; i++) {
+            key[i] = x[i] == -CUDART_INF_F;
+            x[i] = reciprocal(1.f + ex2(-x[i] * LOG2E));
+          }
+        }
+        float b[M];
+        if (a.bias) load_bias<M, G>(b, a.bias, g, a.E, word);
+#pragma unroll
+        for (int i = 0; i < M; i++) {
+          const float c = key[i] ? -CUDART_INF_F : a.bias ? fmaf(x[i], scale, b[i]) : x[i] * scale;
+          key[i] = (ordered(c > -CUDART_INF_F ? c : -CUDART_INF_F) & ~LOW) | (LOW - i);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < M; i++) key[i] = (ordered(x[i]) & ~LOW) | (LOW - i);
+      }
     }
     bool again = false;  // by a warp
     if (SCORES && a.groups > 1) {
       const int size = a.E / a.groups;
-      if (groups_of_lanes(a.E, a.groups, M)) {
-        sort_keys<M>(key);
-        const int lanes = size / M;
-        uint32_t b1 = key[0], b2 = key[1];
-        for (int o = 1; o < lanes; o *= 2) {
-          const uint32_t o1 = __shfl_xor_sync(ALL, b1, o), o2 = __shfl_xor_sync(ALL, b2, o);
-          b2 = max(min(b1, o1), max(b2, o2));
-          b1 = max(b1, o1);
+      uint32_t* const keys = reinterpret_cast<uint32_t*>(smem + at.row) + rl * G * M;
+      float* const group_score = reinterpret_cast<float*>(smem + at.score) + rl * 2 * a.groups;  // the least it may be
+      float* const group_high = group_score + a.groups;
+#pragma unroll
+      for (int i = 0; i < M; i++) keys[column(i, g)] = key[i];
+      __syncwarp();
+      for (int q = g; q < a.groups; q += G) {
+        uint32_t b1 = 0, b2 = 0;
+        int e = q % size;  // (each lane starts at another column, and so at another bank)
+#pragma unroll 4
+        for (int i = 0; i < size; i++) {
+          const uint32_t y = keys[q * size + e];
+          e = e + 1 == size ? 0 : e + 1;
+          b2 = max(b2, min(b1, y));
+          b1 = max(b1, y);
         }
-        // least and most that the score may be
-        const bool some = first < a.E && b1 > NONE && (a.group_top == 1 || b2 > NONE);
+        const bool some = b1 > NONE && (a.group_top == 1 || b2 > NONE);
         float low = -CUDART_INF_F, high = -CUDART_INF_F;
         if (some) {
           low = unordered(b1 & ~LOW), high = unordered(b1 | LOW);
           if (a.group_top == 2) low += unordered(b2 & ~LOW), high += unordered(b2 | LOW);
         }
-        const int mine = first / size;
+        group_score[q] = low, group_high[q] = high;
+      }
+      __syncwarp();
+      float least = CUDART_INF_F, most = -CUDART_INF_F;
+      unsigned open = 0;  // bit q: group q
+      for (int q = g; q < a.groups; q += G) {
+        const float mine = group_score[q];
         int ahead = 0;
 #pragma unroll 4
-        for (int q = 0; q < a.groups; q++) {
-          const float other = __shfl_sync(ALL, low, row0 + q * lanes);
-          ahead += other > low || (other == low && q < mine);
+        for (int p = 0; p < a.groups; p++) {
+          const float other = group_score[p];
+          ahead += other > mine || (other == mine && p < q);
         }
-        const bool is_open = ahead < a.top_groups;
-        const float least = -max_over<G>(is_open && first < a.E ? -low : -CUDART_INF_F);
-        const float most = max_over<G>(is_open ? -CUDART_INF_F : high);
-        again = most > -CUDART_INF_F && least < CUDART_INF_F && !apart(least, most, 2.f * tol);
-        if (!is_open) {
-#pragma unroll
-          for (int i = 0; i < M; i++) key[i] = 0;
-        }
-      } else {
-        uint32_t* const keys = reinterpret_cast<uint32_t*>(smem + at.row) + rl * G * M;
-        float* const group_score = reinterpret_cast<float*>(smem + at.score) + rl * 2 * a.groups;  // the least it may be
-        float* const group_high = group_score + a.groups;
-#pragma unroll
-        for (int i = 0; i < M; i++) keys[first + i] = key[i];
-        __syncwarp();
-        for (int q = g; q < a.groups; q += G) {
-          uint32_t b1 = 0, b2 = 0;
-          for (int e = q * size; e < (q + 1) * size; e++) {
-            const uint32_t y = keys[e];
-            b2 = max(b2, min(b1, y));
-            b1 = max(b1, y);
-          }
-          const bool some = b1 > NONE && (a.group_top == 1 || b2 > NONE);
-          group_score[q] = !some ? -CUDART_INF_F : unordered(b1 & ~LOW) + (a.group_top == 2 ? unordered(b2 & ~LOW) : 0.f);
-          group_high[q] = !some ? -CUDART_INF_F : unordered(b1 | LOW) + (a.group_top == 2 ? unordered(b2 | LOW) : 0.f);
-        }
-        __syncwarp();
-        float least = CUDART_INF_F, most = -CUDART_INF_F;
-        unsigned open = 0;  // bit n: this lane's n-th group
-        for (int q = g, n = 0; q < a.groups; q += G, n++) {
-          const float mine = group_score[q];
-          int ahead = 0;
-          for (int p = 0; p < a.groups; p++) {
-            const float other = group_score[p];
-            ahead += other > mine || (other == mine && p < q);
-          }
-          if (ahead < a.top_groups)
-            least = fminf(least, mine), open |= 1u << n;
-          else
-            most = fmaxf(most, group_high[q]);
-        }
-        least = -max_over<G>(-least);
-        most = max_over<G>(most);
-        again = most > -CUDART_INF_F && least < CUDART_INF_F && !apart(least, most, 2.f * tol);
-        __syncwarp();
-        for (int q = g, n = 0; q < a.groups; q += G, n++) group_score[q] = (open >> n & 1) ? 1.f : 0.f;
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < M; i++)
-          if (first + i < a.E && group_score[(first + i) / size] == 0.f) key[i] = 0;
-        __syncwarp();
-        sort_keys<M>(key);
+        if (ahead < a.top_groups)
+          least = fminf(least, mine), open |= 1u << q;
+        else
+          most = fmaxf(most, group_high[q]);
       }
-    } else {
-      sort_keys<M>(key);
-    }
-    // the k largest, and one more, to see how far behind it is: a lane's keys wait in shared memory, behind them a zero
+      least = -max_over<G>(-least);
+      most = max_over<G>(most);
 #pragma unroll
-    for (int i = 0; i < M; i += 4) reinterpret_cast<uint4*>(waiting)[i / 4] = make_uint4(key[i], key[i + 1], key[i + 2], key[i + 3]);
+      for (int o = G / 2; o; o /= 2) open |= __shfl_xor_sync(ALL, open, o);
+      again = most > -CUDART_INF_F && least < CUDART_INF_F && !apart(least, most, 2.f * tol);
+      // closed groups' keys go: a word's columns are mostly of one group
+      const float per = 1.f / static_cast<float>(size);
+#pragma unroll
+      for (int i = 0; i < M; i++) {
+        const int e = column(i, g);
+        const int q = static_cast<int>((static_cast<float>(e) + 0.5f) * per);  // (exact: e < 1024)
+        if (q < a.groups && !(open >> q & 1)) key[i] = 0;
+      }
+      __syncwarp();
+    }
+    top_eight<M>(key);
+    // the k largest, and one more, to see how far behind it is: a lane's keys wait in shared memory
+    reinterpret_cast<uint4*>(waiting)[0] = make_uint4(key[0], key[1], key[2], key[3]);
+    reinterpret_cast<uint4*>(waiting)[1] = make_uint4(key[4], key[5], key[6], key[7]);
     uint32_t head = key[0];
-    const uint32_t* ahead_of = waiting + 1;
+    const uint32_t* behind = waiting + 1;
     auto take = [&](int j) {
-      const bool hit = (head | LOW) == key_over<G>(head | LOW);  // (places in different lanes do not compare)
+      // ties: the lower word, then the lower lane (places in a word of different lanes do not compare)
+      const bool hit = (head | in_word) == key_over<G>(head | in_word);
       const unsigned holders = __ballot_sync(ALL, hit);
       if (hit && !(holders & before)) {
-        list[j] = make_uint2(head, first);
-        head = *ahead_of++;
+        list[j] = make_uint2(head, g);
+        head = behind == waiting + 9 ? 0 : *behind++;
       }
     };
     const int picks = LOSSLESS ? a.k : a.k + 1;
@@ -478,12 +478,12 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
     __syncwarp();
     auto listed = [&](int j) {  // (key, expert)
       const uint2 p = list[j];
-      return make_uint2(p.x, p.y + (LOW - (p.x & LOW)));
+      return make_uint2(p.x, column(LOW - (p.x & LOW), p.y));
     };
     const uint2 mine = listed(g < a.k ? g : 0);
     int e = mine.x > NONE && on && g < a.k ? static_cast<int>(mine.y) : -1;
     float y = e >= 0 ? static_cast<float>(row[e]) : -CUDART_INF_F;
-    if constexpr (!LOSSLESS) {
+    if (!LOSSLESS) {
       auto close = [&](uint32_t high, uint32_t low) {
         return low > NONE && (SCORES ? !apart(unordered(high & ~LOW), unordered(low | LOW), tol) : (high ^ low) <= LOW);
       };
@@ -516,15 +516,18 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
             again = true, last = false;
         }
       }
+    }
+    if (!LOSSLESS || M > 8) {
+      if (M > 8) again |= behind == waiting + 9;  // there may have been more in this lane
       unsigned todo = __ballot_sync(ALL, again && on && !bad);
       while (todo) {
         const int who = __ffs(todo) - 1, who0 = who & ~(G - 1);
         todo &= ~((G == 32 ? ALL : (1u << G) - 1) << who0);
         const int which = __shfl_sync(ALL, t, who);
         if (by_score)
-          choose<TYPE, M, double>(a, which, pick);
+          choose<TYPE, AGAIN, double>(a, which, pick);
         else
-          choose<TYPE, M, float>(a, which, pick);
+          choose<TYPE, AGAIN, float>(a, which, pick);
         __syncwarp();
         if (row0 == who0 && g < a.k) {
           e = pick[g];
@@ -593,13 +596,15 @@ struct GradArgs {
   int E, k, score, renormalize, ids_bytes, accumulate;
 };
 
+__host__ __device__ constexpr int grad_blocks_of(int M) { return M <= 16 ? 4 : 3; }
+
 // A row's gradient is zero (or, for softmax taken as it is, a multiple of the scores) but at the chosen experts: all of it is
 // written in words first, then the chosen ones by a lane each.
 template <int TYPE, int M, int G>
-__global__ void __launch_bounds__(THREADS, M == 8 ? 4 : 2) k_route_grad(const __grid_constant__ GradArgs a, int word) {
+__global__ void __launch_bounds__(THREADS, grad_blocks_of(M)) k_route_grad(const __grid_constant__ GradArgs a, int word) {
   using T = typename Of<TYPE>::T;
   constexpr int ROWS = THREADS / G;
-  const int tid = threadIdx.x, lane = tid & 31, g = lane & (G - 1), rl = tid / G, row0 = lane & ~(G - 1), first = g * M;
+  const int tid = threadIdx.x, lane = tid & 31, g = lane & (G - 1), rl = tid / G, row0 = lane & ~(G - 1);
   const unsigned of_row = (G == 32 ? ALL : (1u << G) - 1) << row0;
   const bool softmax = a.score == IWP_SOFTMAX, dense = softmax && !a.renormalize;
   launch_next();
@@ -628,7 +633,7 @@ __global__ void __launch_bounds__(THREADS, M == 8 ? 4 : 2) k_route_grad(const __
     }
     float v[M];
     if (dense) {
-      load_columns<TYPE, M>(v, row, first, a.E, in && some, word);
+      load_columns<TYPE, M, G>(v, row, g, a.E, in && some, word);
       float top = -CUDART_INF_F, s = 0.f;
 #pragma unroll
       for (int i = 0; i < M; i++) top = fmaxf(top, v[i]);
@@ -662,7 +667,7 @@ __global__ void __launch_bounds__(THREADS, M == 8 ? 4 : 2) k_route_grad(const __
       y = all;
     }
     if (in && (dense || !a.accumulate))
-      with_word<TYPE>(word, [&](auto vec) { store_words<TYPE, M, decltype(vec)::value>(v, out, first, a.E, a.accumulate); });
+      with_word<TYPE>(word, [&](auto vec) { store_words<TYPE, M, G, decltype(vec)::value>(v, out, g, a.E, a.accumulate); });
     __syncwarp();
     if (e >= 0) out[e] = static_cast<T>(fmaf(y + x, a.scale, old));
   }

@@ -10,28 +10,29 @@
 
 namespace iwp_router {
 
-// Columns per lane: 8 up to 256 experts, so that a row takes few lanes and what they do together serves several rows.
-inline int columns_of(int E) { return E <= 256 ? 8 : E <= 512 ? 16 : 32; }
-// Lanes of a row: for its columns, and one for each choice.
+// Lanes of a row: one for each choice, and few, so that what they do together serves several rows; columns of a lane: 8, 16
+// or 32.  (131072 x 256 fp32, 8 choices: 8 lanes of 32 columns LAYOUT_8 us, 32 lanes of 8 columns LAYOUT_32.)
 inline int lanes_of(int E, int k) {
-  int G = 2;
-  while (G * columns_of(E) < E || G < k) G *= 2;
+  int G = E <= 16 ? 2 : E <= 32 ? 4 : 8;
+  while (G * 32 < E || G < k) G *= 2;
   return G;
 }
+inline int columns_of(int E, int G) { return E <= 8 * G ? 8 : E <= 16 * G ? 16 : 32; }
 
 // Calls f(columns per lane, lanes of a row).
 template <class F>
 int by_layout(int E, int k, const F& f) {
-  using C8 = std::integral_constant<int, 8>;
-  using L32 = std::integral_constant<int, 32>;
-  const int columns = columns_of(E), G = lanes_of(E, k);
-  if (columns == 16) return f(std::integral_constant<int, 16>{}, L32{});
-  if (columns == 32) return f(L32{}, L32{});
-  if (G == 2) return f(C8{}, std::integral_constant<int, 2>{});
-  if (G == 4) return f(C8{}, std::integral_constant<int, 4>{});
-  if (G == 8) return f(C8{}, std::integral_constant<int, 8>{});
-  if (G == 16) return f(C8{}, std::integral_constant<int, 16>{});
-  return f(C8{}, L32{});
+  const int G = lanes_of(E, k), columns = columns_of(E, G);
+  auto with = [&](auto lanes) -> int {
+    if (columns == 8) return f(std::integral_constant<int, 8>{}, lanes);
+    if (columns == 16) return f(std::integral_constant<int, 16>{}, lanes);
+    return f(std::integral_constant<int, 32>{}, lanes);
+  };
+  if (G == 2) return f(std::integral_constant<int, 8>{}, std::integral_constant<int, 2>{});
+  if (G == 4) return f(std::integral_constant<int, 8>{}, std::integral_constant<int, 4>{});
+  if (G == 8) return with(std::integral_constant<int, 8>{});
+  if (G == 16) return with(std::integral_constant<int, 16>{});
+  return with(std::integral_constant<int, 32>{});
 }
 
 template <int TYPE, int M, int G, bool SCORES>
@@ -60,7 +61,7 @@ int launch_route_grad(const GradArgs& r, int word, cudaStream_t st) {
     using namespace iwp_host;
     constexpr int M = decltype(columns)::value, G = decltype(lanes)::value;
     const int64_t steps = tiles_of(r.T, THREADS / G);
-    LOSS_CUDA(launch(k_route_grad<TYPE, M, G>, std::min<int64_t>(steps, (M == 8 ? 4 : 2) * SMS), THREADS, 0, 1, st, r, word));
+    LOSS_CUDA(launch(k_route_grad<TYPE, M, G>, std::min<int64_t>(steps, grad_blocks_of(M) * SMS), THREADS, 0, 1, st, r, word));
     return IWP_OK;
   });
 }

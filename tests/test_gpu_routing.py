@@ -256,7 +256,9 @@ def test_strides_types_of_ids_and_bits():
     dw = torch.randn(T, 2 * k, generator=gen(15), device=DEV)[:, ::1][:, :k]
     into = torch.full((T, 2 * E), 7.0, device=DEV)
     got = plan.grad(x, r.ids.long(), r.weights, dw, dlogits=into[:, 3 : E + 3])
-    assert torch.equal(got, plan.grad(x.contiguous(), r.ids, r.weights, dw.contiguous()))
+    # words of other widths add up a row's exponentials in another order: each result is within its bound
+    _, bound = grad_bound(x, r.ids.long(), r.weights.double(), dw, dict(score="softmax", renormalize=False), F32)
+    assert ((got.double() - plan.grad(x.contiguous(), r.ids, r.weights, dw.contiguous()).double()).abs() <= 2 * bound).all()
     assert (into[:, :3] == 7).all() and (into[:, E + 3 :] == 7).all()
     again = plan.route(x)
     assert torch.equal(r.ids, again.ids) and torch.equal(r.weights, again.weights) and torch.equal(r.counts, again.counts)
