@@ -296,19 +296,60 @@ __device__ __forceinline__ float reciprocal(float x) {
   return y;
 }
 
-// The bias of lane g's columns, in words of the rows' width.
-template <int M, int G>
-__device__ __forceinline__ void load_bias(float (&b)[M], const float* bias, int g, int E, int word) {
-  const int shift = __popc(word - 1);
+// x = scale x + bias in lane g's columns.
+template <int M, int G, int VEC>
+__device__ __forceinline__ void add_bias(float (&x)[M], float scale, const float* bias, int g, int E) {
 #pragma unroll
-  for (int i = 0; i < M; i++) {
-    const int e = ((((i >> shift) * G + g) << shift) + (i & (word - 1)));
-    b[i] = e < E ? __ldg(bias + e) : 0.f;
+  for (int n = 0; n < M / VEC; n++) {
+    const int first = (n * G + g) * VEC;
+    if (first < E) {
+#pragma unroll
+      for (int v = 0; v < VEC; v++) x[n * VEC + v] = fmaf(x[n * VEC + v], scale, __ldg(bias + first + v));
+    }
+  }
+}
+
+// Lane g's keys to their columns' places in `keys`.
+template <int M, int G, int VEC>
+__device__ __forceinline__ void spread_keys(const uint32_t (&key)[M], uint32_t* keys, int g) {
+#pragma unroll
+  for (int n = 0; n < M / VEC; n++) {
+    uint32_t* const to = keys + (n * G + g) * VEC;
+    if constexpr (VEC % 4 == 0) {
+#pragma unroll
+      for (int v = 0; v < VEC; v += 4)
+        *reinterpret_cast<uint4*>(to + v) = make_uint4(key[n * VEC + v], key[n * VEC + v + 1], key[n * VEC + v + 2], key[n * VEC + v + 3]);
+    } else {
+#pragma unroll
+      for (int v = 0; v < VEC; v++) to[v] = key[n * VEC + v];
+    }
+  }
+}
+
+// Lane g's keys in groups of `size` columns that are not open become 0.
+template <int M, int G, int VEC>
+__device__ __forceinline__ void close_groups(uint32_t (&key)[M], unsigned open, int size, int groups, int g) {
+  const float per = 1.f / static_cast<float>(size);
+  auto is_open = [&](int e) {
+    const int q = static_cast<int>((static_cast<float>(e) + 0.5f) * per);  // e / size, exact for e < 1024
+    return q >= groups || (open >> q & 1);
+  };
+#pragma unroll
+  for (int n = 0; n < M / VEC; n++) {
+    const int first = (n * G + g) * VEC;
+    if (size % VEC == 0) {  // a word is of one group
+      const bool on = is_open(first);
+#pragma unroll
+      for (int v = 0; v < VEC; v++) key[n * VEC + v] = on ? key[n * VEC + v] : 0;
+    } else {
+#pragma unroll
+      for (int v = 0; v < VEC; v++) key[n * VEC + v] = is_open(first + v) ? key[n * VEC + v] : 0;
+    }
   }
 }
 
 // Blocks of k_route that an SM holds, by their registers.
-__host__ __device__ constexpr int blocks_of(int M, bool scores) { return M == 8 ? (scores ? 3 : 4) : M == 16 ? 3 : 2; }
+__host__ __device__ constexpr int blocks_of(int M, bool scores) { return M == 8 ? (scores ? 4 : 5) : M == 16 ? 4 : 3; }
 
 // SCORES: the choice goes by scores, or among groups; else by the logits alone.  k <= G: a lane has one pick at most.
 // word: elements that all rows are aligned for.
@@ -388,12 +429,12 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
             x[i] = reciprocal(1.f + ex2(-x[i] * LOG2E));
           }
         }
-        float b[M];
-        if (a.bias) load_bias<M, G>(b, a.bias, g, a.E, word);
+        if (a.bias) with_word<TYPE>(word, [&](auto v) { add_bias<M, G, decltype(v)::value>(x, scale, a.bias, g, a.E); });
 #pragma unroll
         for (int i = 0; i < M; i++) {
-          const float c = key[i] ? -CUDART_INF_F : a.bias ? fmaf(x[i], scale, b[i]) : x[i] * scale;
-          key[i] = (ordered(c > -CUDART_INF_F ? c : -CUDART_INF_F) & ~LOW) | (LOW - i);
+          // (what is not available, by its logit or its bias, is -inf; a NaN is less)
+          const float c = a.bias ? x[i] : x[i] * scale;
+          key[i] = key[i] || !(c > -CUDART_INF_F) ? 0 : (ordered(c) & ~LOW) | (LOW - i);
         }
       } else {
 #pragma unroll
@@ -406,18 +447,29 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
       uint32_t* const keys = reinterpret_cast<uint32_t*>(smem + at.row) + rl * G * M;
       float* const group_score = reinterpret_cast<float*>(smem + at.score) + rl * 2 * a.groups;  // the least it may be
       float* const group_high = group_score + a.groups;
-#pragma unroll
-      for (int i = 0; i < M; i++) keys[column(i, g)] = key[i];
+      with_word<TYPE>(word, [&](auto v) { spread_keys<M, G, decltype(v)::value>(key, keys, g); });
       __syncwarp();
       for (int q = g; q < a.groups; q += G) {
         uint32_t b1 = 0, b2 = 0;
-        int e = q % size;  // (each lane starts at another column, and so at another bank)
-#pragma unroll 4
-        for (int i = 0; i < size; i++) {
-          const uint32_t y = keys[q * size + e];
-          e = e + 1 == size ? 0 : e + 1;
+        auto see = [&](uint32_t y) {
           b2 = max(b2, min(b1, y));
           b1 = max(b1, y);
+        };
+        // (each lane starts at another column, and so at other banks)
+        if (size % 4 == 0) {
+          int u = q % (size / 4);
+#pragma unroll 4
+          for (int i = 0; i < size / 4; i++) {
+            const uint4 y = *reinterpret_cast<const uint4*>(keys + q * size + 4 * u);
+            u = u + 1 == size / 4 ? 0 : u + 1;
+            see(y.x), see(y.y), see(y.z), see(y.w);
+          }
+        } else {
+          int u = q % size;
+          for (int i = 0; i < size; i++) {
+            see(keys[q * size + u]);
+            u = u + 1 == size ? 0 : u + 1;
+          }
         }
         const bool some = b1 > NONE && (a.group_top == 1 || b2 > NONE);
         float low = -CUDART_INF_F, high = -CUDART_INF_F;
@@ -448,14 +500,7 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
 #pragma unroll
       for (int o = G / 2; o; o /= 2) open |= __shfl_xor_sync(ALL, open, o);
       again = most > -CUDART_INF_F && least < CUDART_INF_F && !apart(least, most, 2.f * tol);
-      // closed groups' keys go: a word's columns are mostly of one group
-      const float per = 1.f / static_cast<float>(size);
-#pragma unroll
-      for (int i = 0; i < M; i++) {
-        const int e = column(i, g);
-        const int q = static_cast<int>((static_cast<float>(e) + 0.5f) * per);  // (exact: e < 1024)
-        if (q < a.groups && !(open >> q & 1)) key[i] = 0;
-      }
+      with_word<TYPE>(word, [&](auto v) { close_groups<M, G, decltype(v)::value>(key, open, size, a.groups, g); });
       __syncwarp();
     }
     top_eight<M>(key);
@@ -596,7 +641,7 @@ struct GradArgs {
   int E, k, score, renormalize, ids_bytes, accumulate;
 };
 
-__host__ __device__ constexpr int grad_blocks_of(int M) { return M <= 16 ? 4 : 3; }
+__host__ __device__ constexpr int grad_blocks_of(int M) { return M <= 16 ? 5 : 4; }
 
 // A row's gradient is zero (or, for softmax taken as it is, a multiple of the scores) but at the chosen experts: all of it is
 // written in words first, then the chosen ones by a lane each.
@@ -609,21 +654,27 @@ __global__ void __launch_bounds__(THREADS, grad_blocks_of(M)) k_route_grad(const
   const bool softmax = a.score == IWP_SOFTMAX, dense = softmax && !a.renormalize;
   launch_next();
   wait_previous();
+  // a choice's expert, weight and upstream gradient are fetched a row ahead
+  int64_t next_id = -1;
+  float next_p = 0.f, next_dw = 0.f;
+  auto fetch = [&](int64_t t) {
+    next_id = -1;
+    if (t < a.T && g < a.k) {
+      next_id = load_id(a.ids, a.ids_bytes, t * a.ids_ld + g);
+      next_p = a.weights[t * a.weights_ld + g];
+      next_dw = a.dweights[t * a.dweights_ld + g];
+    }
+  };
+  fetch(static_cast<int64_t>(blockIdx.x) * ROWS + rl);
   for (int t0 = blockIdx.x * ROWS; t0 < a.T; t0 += gridDim.x * ROWS) {
     const int t = t0 + rl;
     const bool in = t < a.T;
     const T* const row = static_cast<const T*>(a.logits) + t * a.logits_ld;
     T* const out = static_cast<T*>(a.dlogits) + t * a.dlogits_ld;
-    int e = -1;
-    float p = 0.f, y = 0.f;  // weight, and its product with the gradient
-    if (in && g < a.k) {
-      const int64_t id = load_id(a.ids, a.ids_bytes, t * a.ids_ld + g);
-      if (id >= 0 && id < a.E) {
-        e = static_cast<int>(id);
-        p = a.weights[t * a.weights_ld + g];
-        y = p * a.dweights[t * a.dweights_ld + g];
-      }
-    }
+    const int e = next_id >= 0 && next_id < a.E ? static_cast<int>(next_id) : -1;
+    const float p = e >= 0 ? next_p : 0.f;  // weight, and its product with the gradient
+    float y = e >= 0 ? p * next_dw : 0.f;
+    fetch(static_cast<int64_t>(t) + static_cast<int64_t>(gridDim.x) * ROWS);
     const float sum = sum_over<G>(y);
     const bool some = (__ballot_sync(ALL, e >= 0) & of_row) != 0;
     float x = 0.f, old = 0.f;
