@@ -124,98 +124,6 @@ __device__ __forceinline__ float sum_over(float x) {
 constexpr float SOFTMAX_TOLERANCE = 0x1.8p-18f, SIGMOID_TOLERANCE = 0x1p-20f;
 __device__ __forceinline__ bool apart(float high, float low, float tol) { return high - low > tol + 0x1p-23f * (fabsf(high) + fabsf(low)); }
 
-// The choice of one row by a whole warp: by the logits (Real = float), or by scores in 64 bits.
-template <int TYPE, int M, class Real>
-__device__ __noinline__ void choose(const Args& a, int64_t t, int* pick) {
-  const int lane = threadIdx.x & 31, size = a.E / a.groups;
-  constexpr bool scores = sizeof(Real) == 8;
-  const Real none = -static_cast<Real>(CUDART_INF_F);
-  Real c[M];
-  float top = -CUDART_INF_F;
-#pragma unroll
-  for (int i = 0; i < M; i++) {
-    const int e = lane + 32 * i;
-    const float x = e < a.E ? load<TYPE>(a.logits, t * a.logits_ld + e) : -CUDART_INF_F;
-    c[i] = x;
-    top = fmaxf(top, x);
-  }
-  if constexpr (scores) {
-    const bool softmax = a.score == IWP_SOFTMAX;
-    top = max_over<32>(top);
-    double s = 0;
-#pragma unroll
-    for (int i = 0; i < M; i++) {
-      if (!(c[i] > none)) continue;
-      c[i] = softmax ? exp(c[i] - top) : 1. / (1. + exp(-c[i]));
-      s += c[i];
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(ALL, s, o);
-#pragma unroll
-    for (int i = 0; i < M; i++) {
-      if (!(c[i] > none)) continue;
-      if (softmax) c[i] /= s;
-      if (a.bias) c[i] += a.bias[lane + 32 * i];
-      if (!(c[i] > none)) c[i] = none;
-    }
-  }
-  if (a.groups > 1) {
-    Real mine = none;  // lane q: group q's score
-    for (int q = 0; q < a.groups; q++) {
-      Real b1 = none, b2 = none;
-#pragma unroll
-      for (int i = 0; i < M; i++) {
-        if ((lane + 32 * i) / size != q) continue;
-        if (c[i] > b1)
-          b2 = b1, b1 = c[i];
-        else if (c[i] > b2)
-          b2 = c[i];
-      }
-#pragma unroll
-      for (int o = 16; o; o >>= 1) {
-        const Real o1 = __shfl_xor_sync(ALL, b1, o), o2 = __shfl_xor_sync(ALL, b2, o);
-        const Real less = b1 < o1 ? b1 : o1, second = b2 < o2 ? o2 : b2;
-        b1 = b1 < o1 ? o1 : b1;
-        b2 = less < second ? second : less;
-      }
-      if (lane == q) mine = a.group_top == 2 ? b1 + b2 : b1;
-    }
-    int ahead = 0;
-    for (int q = 0; q < a.groups; q++) {
-      const Real other = __shfl_sync(ALL, mine, q);
-      ahead += other > mine || (other == mine && q < lane);
-    }
-    const unsigned open = __ballot_sync(ALL, lane < a.groups && ahead < a.top_groups);
-#pragma unroll
-    for (int i = 0; i < M; i++) {
-      const int e = lane + 32 * i;
-      if (e < a.E && !(open >> (e / size) & 1)) c[i] = none;
-    }
-  }
-  if (scores && !a.bias) {  // the logits order the scores
-#pragma unroll
-    for (int i = 0; i < M; i++)
-      if (c[i] > none) c[i] = load<TYPE>(a.logits, t * a.logits_ld + lane + 32 * i);
-  }
-  for (int j = 0; j < a.k; j++) {
-    Real m = none;
-    int at = MAX_EXPERTS;
-#pragma unroll
-    for (int i = 0; i < M; i++)
-      if (c[i] > m) m = c[i], at = lane + 32 * i;
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-      const Real om = __shfl_xor_sync(ALL, m, o);
-      const int oat = __shfl_xor_sync(ALL, at, o);
-      if (om > m || (om == m && oat < at)) m = om, at = oat;
-    }
-#pragma unroll
-    for (int i = 0; i < M; i++)
-      if (lane + 32 * i == at) c[i] = none;
-    if (lane == 0) pick[j] = at < MAX_EXPERTS ? at : -1;
-  }
-}
-
 // As bits that order as the values do, -inf at NONE.
 constexpr uint32_t NONE = 0x007FFFFFu;
 __device__ __forceinline__ uint32_t ordered(float x) {
@@ -223,6 +131,120 @@ __device__ __forceinline__ uint32_t ordered(float x) {
   return u ^ (static_cast<uint32_t>(static_cast<int32_t>(u) >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float unordered(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u); }
+
+// Codes that order as the values do, 0 for what is not available.
+__device__ __forceinline__ uint64_t code_of(float x) { return x > -CUDART_INF_F ? ordered(x) : 0; }
+__device__ __forceinline__ uint64_t code_of(double x) {
+  if (!(x > -CUDART_INF)) return 0;
+  const uint64_t u = static_cast<uint64_t>(__double_as_longlong(x + 0.));
+  return u ^ (static_cast<uint64_t>(static_cast<int64_t>(u) >> 63) | 0x8000000000000000ull);
+}
+__device__ __forceinline__ double value_of(uint64_t code) {
+  return __longlong_as_double(static_cast<int64_t>(code >> 63 ? code ^ 0x8000000000000000ull : ~code));
+}
+__device__ __forceinline__ uint64_t max_over_warp(uint64_t x) {
+  const uint32_t high = __reduce_max_sync(ALL, static_cast<uint32_t>(x >> 32));
+  const uint32_t low = __reduce_max_sync(ALL, static_cast<uint32_t>(x >> 32) == high ? static_cast<uint32_t>(x) : 0);
+  return static_cast<uint64_t>(high) << 32 | low;
+}
+
+// The choice of one row by a whole warp: by the logits, or (SCORES) by scores in 64 bits.  A few rows of a launch come here
+// and the launch waits for them, so what there is to do is laid out side by side: 64-bit codes, whose maxima take two
+// reductions, and no branches around a column's arithmetic.
+template <int TYPE, int M, bool SCORES>
+__device__ __noinline__ void choose(const Args& a, int64_t t, int* pick) {
+  const int lane = threadIdx.x & 31, size = a.E / a.groups;
+  uint64_t code[M];
+  {
+    float x[M];
+    float top = -CUDART_INF_F;
+#pragma unroll
+    for (int i = 0; i < M; i++) {
+      const int e = lane + 32 * i;
+      x[i] = e < a.E ? load<TYPE>(a.logits, t * a.logits_ld + e) : -CUDART_INF_F;
+      top = fmaxf(top, x[i]);
+    }
+    if constexpr (SCORES) {
+      const bool softmax = a.score == IWP_SOFTMAX;
+      top = softmax ? max_over<32>(top) : 0.f;
+      if (top == -CUDART_INF_F) top = 0.f;
+      double c[M], s = 0;
+#pragma unroll
+      for (int i = 0; i < M; i++) {
+        const double y = softmax ? static_cast<double>(x[i]) - top : -static_cast<double>(x[i]);
+        c[i] = exp(y);
+        s += c[i];
+      }
+      if (softmax) {
+#pragma unroll
+        for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(ALL, s, o);
+      }
+#pragma unroll
+      for (int i = 0; i < M; i++) {
+        const int e = lane + 32 * i;
+        double y = (softmax ? c[i] : 1.) / (softmax ? s : 1. + c[i]);
+        if (a.bias && e < a.E) y += a.bias[e];
+        code[i] = x[i] > -CUDART_INF_F ? code_of(y) : 0;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < M; i++) code[i] = code_of(x[i]);
+    }
+  }
+  if (a.groups > 1) {
+    uint64_t mine = 0;  // lane q: group q's score
+    for (int q = 0; q < a.groups; q++) {
+      uint64_t b1 = 0, b2 = 0;
+#pragma unroll
+      for (int i = 0; i < M; i++) {
+        const uint64_t y = (lane + 32 * i) / size == q ? code[i] : 0;
+        const uint64_t less = y < b1 ? y : b1;
+        b1 = y < b1 ? b1 : y;
+        b2 = less < b2 ? b2 : less;
+      }
+      const uint64_t first = max_over_warp(b1);
+      uint64_t score = first;
+      if (SCORES && a.group_top == 2) {
+        // the second is the largest that is left once one lane has given its first
+        const unsigned holders = __ballot_sync(ALL, b1 == first);
+        const uint64_t second = max_over_warp(lane == __ffs(holders) - 1 ? b2 : b1);
+        score = second ? code_of(value_of(first) + value_of(second)) : 0;
+      }
+      if (lane == q) mine = score;
+    }
+    int ahead = 0;
+    for (int q = 0; q < a.groups; q++) {
+      const uint64_t other = __shfl_sync(ALL, mine, q);
+      ahead += other > mine || (other == mine && q < lane);
+    }
+    const unsigned open = __ballot_sync(ALL, lane < a.groups && ahead < a.top_groups);
+#pragma unroll
+    for (int i = 0; i < M; i++) {
+      const int e = lane + 32 * i;
+      if (e < a.E && !(open >> (e / size) & 1)) code[i] = 0;
+    }
+  }
+  if (SCORES && !a.bias) {  // the logits order the scores
+#pragma unroll
+    for (int i = 0; i < M; i++)
+      if (code[i]) code[i] = code_of(load<TYPE>(a.logits, t * a.logits_ld + lane + 32 * i));
+  }
+  for (int j = 0; j < a.k; j++) {
+    uint64_t best = 0;
+#pragma unroll
+    for (int i = 0; i < M; i++) best = code[i] > best ? code[i] : best;
+    const uint64_t m = max_over_warp(best);
+    int at = MAX_EXPERTS;
+#pragma unroll
+    for (int i = M - 1; i >= 0; i--)
+      if (code[i] == m) at = lane + 32 * i;
+    at = __reduce_min_sync(ALL, at);
+#pragma unroll
+    for (int i = 0; i < M; i++)
+      if (lane + 32 * i == at) code[i] = 0;
+    if (lane == 0) pick[j] = m ? at : -1;
+  }
+}
 
 __device__ __forceinline__ void in_order(uint32_t& a, uint32_t& b) {
   const uint32_t high = max(a, b), low = min(a, b);
@@ -570,9 +592,9 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
         todo &= ~((G == 32 ? ALL : (1u << G) - 1) << who0);
         const int which = __shfl_sync(ALL, t, who);
         if (by_score)
-          choose<TYPE, AGAIN, double>(a, which, pick);
+          choose<TYPE, AGAIN, true>(a, which, pick);
         else
-          choose<TYPE, AGAIN, float>(a, which, pick);
+          choose<TYPE, AGAIN, false>(a, which, pick);
         __syncwarp();
         if (row0 == who0 && g < a.k) {
           e = pick[g];
