@@ -31,11 +31,12 @@ typedef struct iwp_clip_tensor {
 typedef struct iwp_clip_sizes {
   int64_t table_bytes;             /* of the table, 16-byte aligned on the device */
   int64_t workspace_bytes;         /* of every call's workspace */
-  int64_t parts, elements;         /* for iwp_clip_args */
+  int64_t parts, warps;            /* for iwp_clip_args */
+  int64_t range;                   /* work of a warp, for iwp_clip_table() */
 } iwp_clip_sizes;
 
-/* Errors: IWP_ERR_INVALID (NULL, sizes, types, alignment below the type's size, groups outside [0, groups), more than 2^26
- * parts, as rows of few elements make them). */
+/* Errors: IWP_ERR_INVALID (NULL, sizes, types, alignment below the type's size, groups outside [0, groups), more than 2^25
+ * rows), IWP_ERR_OOM (host memory). */
 int iwp_clip_layout(const iwp_clip_tensor* tensors_host, int64_t n, int32_t groups, iwp_clip_sizes* sizes_host);
 int iwp_clip_table(const iwp_clip_tensor* tensors_host, int64_t n, int32_t groups, void* table_host, int64_t table_bytes);
 
@@ -49,7 +50,7 @@ int iwp_clip_table(const iwp_clip_tensor* tensors_host, int64_t n, int32_t group
  * they are untouched. */
 typedef struct iwp_clip_args {
   const void* table;               /* device */
-  int64_t parts, elements;         /* of iwp_clip_layout() */
+  int64_t parts, warps;            /* of iwp_clip_layout() */
   double* squares;                 /* [groups] */
   float* norms;                    /* [groups] */
   float* factors;                  /* [groups]; may be NULL without `write` */

@@ -27,12 +27,12 @@ class ClipTensor(C.Structure):
 
 
 class ClipSizes(C.Structure):
-    _fields_ = [("table_bytes", _i64), ("workspace_bytes", _i64), ("parts", _i64), ("elements", _i64)]
+    _fields_ = [("table_bytes", _i64), ("workspace_bytes", _i64), ("parts", _i64), ("warps", _i64), ("range", _i64)]
 
 
 class ClipArgs(C.Structure):
     _fields_ = [
-        ("table", _vp), ("parts", _i64), ("elements", _i64), ("squares", _vp), ("norms", _vp), ("factors", _vp), ("workspace", _vp),
+        ("table", _vp), ("parts", _i64), ("warps", _i64), ("squares", _vp), ("norms", _vp), ("factors", _vp), ("workspace", _vp),
         ("workspace_bytes", _i64), ("state", _vp), ("max_norm", _f64), ("scale", _f64), ("groups", _i32), ("write", _i32), ("have_squares", _i32),
         ("drop_nonfinite", _i32),
     ]
@@ -157,7 +157,7 @@ class GradientClip(_Here):
         self._table = host.to(self.device)
         self._made.record()  # the table is there, too
         self._planned = sizes.workspace_bytes
-        self._args = ClipArgs(table=self._table.data_ptr(), parts=sizes.parts, elements=sizes.elements, state=self._state_at, groups=self.groups)
+        self._args = ClipArgs(table=self._table.data_ptr(), parts=sizes.parts, warps=sizes.warps, state=self._state_at, groups=self.groups)
         self._args_at = C.addressof(self._args)
 
     def _memory(self):

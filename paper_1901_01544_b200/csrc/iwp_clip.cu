@@ -16,22 +16,23 @@ namespace K = iwp_clipper;
 
 constexpr int64_t MAX_ELEMENTS = int64_t(1) << 46, MAX_PARTS = int64_t(1) << 26, MAX_LD = int64_t(1) << 46;
 constexpr int MAX_GROUPS = 1 << 20;
+constexpr int64_t MAX_WARPS = int64_t(4) * SMS * K::WARPS;
 constexpr int MAX_CLUSTER = 16;
-// Up to this many elements one cluster serves, in one launch.
-constexpr int64_t SMALL_ELEMENTS = int64_t(1) << 18;
+// A part costs a warp as much time as this many elements more: its description and its first elements are waited for.
+constexpr int64_t PART_COST = 1024;
+// Up to this cost one cluster serves, in one launch.
+constexpr int64_t SMALL_COST = int64_t(1) << 19;
+constexpr int64_t SMALL_WARPS = MAX_CLUSTER * (K::SMALL_THREADS / 32);
 
 int size_of(int type) { return type == IWP_F32 ? 4 : 2; }
 bool is_type(int type) { return type == IWP_F32 || type == IWP_BF16 || type == IWP_F16; }
 
-// Warps that share the elements out: all that the two passes run at once (or that the cluster has), but with something to
-// stream for each.
-constexpr int64_t LEAST_RANGE = 512;
-int64_t warps_of(int64_t total) {
-  const int64_t most = total <= SMALL_ELEMENTS ? MAX_CLUSTER * (K::SMALL_THREADS / 32) : int64_t(4) * SMS * K::WARPS;
-  return std::min(most, tiles_of(total, LEAST_RANGE));
+// Warps that share the work out: all that the two passes run at once (or that the cluster has), but with something to stream
+// for each.
+int64_t warps_for(int64_t cost) {
+  const int64_t most = cost <= SMALL_COST ? SMALL_WARPS : MAX_WARPS;
+  return std::min(most, tiles_of(cost, PART_COST + 512));
 }
-// Elements of a warp's range.
-int64_t range_of(int64_t total) { return total ? up_to(tiles_of(total, warps_of(total)), 64) : 0; }
 
 bool tensor_ok(const iwp_clip_tensor& t, int groups) {
   if (t.rows < 0 || t.cols < 0 || t.group < 0 || t.group >= groups || !is_type(t.in_type)) return false;
@@ -42,19 +43,22 @@ bool tensor_ok(const iwp_clip_tensor& t, int groups) {
   return is_type(t.out_type) && aligned(t.out, size_of(t.out_type)) && (t.rows == 1 || (t.out_ld >= t.cols && t.out_ld <= MAX_LD));
 }
 
-// Walks over all elements, by group and in a group by tensor, and calls f(warp, part) for every part in that order.
+// Walks over all elements, by group and in a group by tensor, and calls f(warp, part) for every part in that order; a warp's
+// parts cost `range` at most.  Returns the number of warps.
 template <class F>
-void each_part(const iwp_clip_tensor* tensors, const int64_t* order, int64_t n, int64_t range, const F& f) {
-  constexpr int64_t MOST = int64_t(1) << 30;
-  int64_t at = 0;  // elements so far
+int64_t each_part(const iwp_clip_tensor* tensors, const int64_t* order, int64_t n, int64_t range, const F& f) {
+  constexpr int64_t MOST = int64_t(1) << 30, LEAST = 64;
+  int64_t w = 0, left = range;
+  bool used = false;
   for (int64_t o = 0; o < n; o++) {
     iwp_clip_tensor t = tensors[order[o]];
     if (t.rows == 0 || t.cols == 0) continue;
     if (t.rows > 1 && t.in_ld == t.cols && (!t.out || t.out_ld == t.cols)) t.cols *= t.rows, t.rows = 1;
     for (int64_t r = 0, c = 0; r < t.rows;) {
-      const int64_t left = std::min(MOST, range - at % range);
-      int64_t rows = 1, cols = std::min(t.cols - c, left);
-      if (c == 0 && left >= t.cols) rows = std::min(t.rows - r, left / t.cols);  // whole rows
+      if (left < PART_COST + LEAST) w++, left = range;
+      const int64_t most = std::min(MOST, (left - PART_COST) / LEAST * LEAST);
+      int64_t rows = 1, cols = std::min(t.cols - c, most);
+      if (c == 0 && most >= t.cols) rows = std::min(t.rows - r, most / t.cols);  // whole rows
       K::Part p{};
       p.in = static_cast<const char*>(t.in) + (r * t.in_ld + c) * size_of(t.in_type);
       p.out = t.out ? static_cast<char*>(t.out) + (r * t.out_ld + c) * size_of(t.out_type) : nullptr;
@@ -65,12 +69,14 @@ void each_part(const iwp_clip_tensor* tensors, const int64_t* order, int64_t n, 
       p.group = t.group;
       p.in_type = static_cast<int16_t>(t.in_type);
       p.out_type = static_cast<int16_t>(t.out ? t.out_type : t.in_type);
-      f(at / range, p);
-      at += rows * cols;
+      f(w, p);
+      used = true;
+      left -= PART_COST + rows * cols;
       c += cols;
       if (c == t.cols) c = 0, r += rows;
     }
   }
+  return w + used;
 }
 
 // Tensors by group, in the order they are given in.
@@ -82,10 +88,23 @@ std::unique_ptr<int64_t[]> order_of(const iwp_clip_tensor* tensors, int64_t n) {
   return order;
 }
 
-// Most parts that each_part() makes of a tensor: a strided matrix is cut at the ends of rows and of ranges.
-int64_t most_parts(const iwp_clip_tensor& t, int64_t range) {
-  if (t.rows == 0 || t.cols == 0) return 0;
-  return t.rows == 1 ? 2 + t.cols / range + (t.cols >> 30) : 4 + 3 * (t.rows * t.cols / range) + (t.cols > range ? 2 * t.rows : 0) + (t.rows * t.cols >> 29);
+// How the work is shared out: ranges of about the least cost that the warps there are suffice for.
+struct Shares {
+  int64_t warps, range, parts;
+};
+Shares shares_of(const iwp_clip_tensor* tensors, const int64_t* order, int64_t n, int64_t total) {
+  Shares s{};
+  if (total == 0) return s;
+  auto walk = [&](int64_t range) {
+    s.range = range;
+    s.parts = 0;
+    return each_part(tensors, order, n, range, [&](int64_t, const K::Part&) { s.parts++; });
+  };
+  walk(MAX_ELEMENTS);
+  s.warps = warps_for(total + PART_COST * s.parts);
+  int64_t range = up_to(tiles_of(total + PART_COST * s.parts, s.warps), 64) + PART_COST;
+  while (walk(range) > s.warps) range += up_to(range / 64, 64);
+  return s;
 }
 
 struct Table {
@@ -103,25 +122,23 @@ Table table_of(int64_t warps, int64_t parts, int64_t groups) {
 
 extern "C" int iwp_clip_layout(const iwp_clip_tensor* tensors, int64_t n, int32_t groups, iwp_clip_sizes* sizes) {
   if (!sizes || n < 0 || (n && !tensors) || groups < 1 || groups > MAX_GROUPS) return IWP_ERR_INVALID;
-  int64_t total = 0, most = 0;
+  int64_t total = 0, rows = 0;
   for (int64_t i = 0; i < n; i++) {
     if (!tensor_ok(tensors[i], groups)) return IWP_ERR_INVALID;
     total += tensors[i].rows * tensors[i].cols;
-    if (total > MAX_ELEMENTS) return IWP_ERR_INVALID;
-  }
-  const int64_t range = range_of(total);
-  for (int64_t i = 0; i < n; i++) {
-    most += most_parts(tensors[i], range);
-    if (most > MAX_PARTS) return IWP_ERR_INVALID;
+    const iwp_clip_tensor& t = tensors[i];
+    if (t.rows > 1 && t.cols > 0 && (t.in_ld != t.cols || (t.out && t.out_ld != t.cols))) rows += t.rows;
+    if (total > MAX_ELEMENTS || rows > MAX_PARTS / 2) return IWP_ERR_INVALID;
   }
   const auto order = order_of(tensors, n);
   if (!order) return IWP_ERR_OOM;
-  int64_t parts = 0;
-  each_part(tensors, order.get(), n, range, [&](int64_t, const K::Part&) { parts++; });
-  sizes->parts = parts;
-  sizes->elements = total;
-  sizes->table_bytes = table_of(warps_of(total), parts, groups).bytes;
-  sizes->workspace_bytes = up_to(8 * (warps_of(total) + groups), 256);
+  const Shares shares = shares_of(tensors, order.get(), n, total);
+  if (shares.parts > MAX_PARTS) return IWP_ERR_INVALID;
+  sizes->parts = shares.parts;
+  sizes->warps = shares.warps;
+  sizes->range = shares.range;
+  sizes->table_bytes = table_of(shares.warps, shares.parts, groups).bytes;
+  sizes->workspace_bytes = up_to(8 * (shares.warps + groups), 256);
   return IWP_OK;
 }
 
@@ -133,12 +150,12 @@ extern "C" int iwp_clip_table(const iwp_clip_tensor* tensors, int64_t n, int32_t
   const auto order = order_of(tensors, n);
   if (!order) return IWP_ERR_OOM;
   std::memset(table, 0, sizes.table_bytes);
-  const int64_t warps = warps_of(sizes.elements);
+  const int64_t warps = sizes.warps;
   const Table at = table_of(warps, sizes.parts, groups);
   char* const base = static_cast<char*>(table);
   auto* const spans = reinterpret_cast<int2*>(base + at.spans);
   int64_t last = -1, i = 0;
-  each_part(tensors, order.get(), n, range_of(sizes.elements), [&](int64_t w, const K::Part& p) {
+  each_part(tensors, order.get(), n, sizes.range, [&](int64_t w, const K::Part& p) {
     std::memcpy(base + at.parts + i * int64_t(sizeof p), &p, sizeof p);
     auto* const start = reinterpret_cast<K::Start*>(base) + w;
     i++;
@@ -153,18 +170,18 @@ extern "C" int iwp_clip_table(const iwp_clip_tensor* tensors, int64_t n, int32_t
     if (span.y == 0) span.x = place;
     span.y = place + 1;
   });
-  // (a range rounded up may leave the last warps without elements)
+  // (the last warps may be left without elements)
   for (int64_t w = last + 1; w < warps; w++) reinterpret_cast<K::Start*>(base)[w].end = -1;
   return IWP_OK;
 }
 
 extern "C" int iwp_clip(const iwp_clip_args* a, void* cuda_stream) {
-  if (!a || a->groups < 1 || a->groups > MAX_GROUPS || a->parts < 0 || a->parts > MAX_PARTS || a->elements < 0 || a->elements > MAX_ELEMENTS) return IWP_ERR_INVALID;
+  if (!a || a->groups < 1 || a->groups > MAX_GROUPS || a->parts < 0 || a->parts > MAX_PARTS || a->warps < 0 || a->warps > MAX_WARPS) return IWP_ERR_INVALID;
   if (!a->table || !aligned(a->table, 16) || !a->squares || !aligned(a->squares, 8) || !a->norms || !aligned(a->norms, 4)) return IWP_ERR_INVALID;
   if (!aligned(a->factors, 4) || (a->write && !a->factors) || !a->state || !aligned(a->state, 256)) return IWP_ERR_INVALID;
   if (!a->workspace || !aligned(a->workspace, 256)) return IWP_ERR_INVALID;
   if (!(a->max_norm >= 0.) || !std::isfinite(a->scale) || a->scale == 0.) return IWP_ERR_INVALID;
-  const int64_t warps = warps_of(a->elements);
+  const int64_t warps = a->warps;
   if (a->workspace_bytes < 8 * (warps + a->groups)) return IWP_ERR_CAPACITY;
   const Table at = table_of(warps, a->parts, a->groups);
   const char* const table = static_cast<const char*>(a->table);
@@ -185,7 +202,7 @@ extern "C" int iwp_clip(const iwp_clip_args* a, void* cuda_stream) {
   r.have_squares = a->have_squares != 0;
   r.drop = a->drop_nonfinite != 0;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  if (a->elements <= SMALL_ELEMENTS && a->groups <= 4096) {
+  if (warps <= SMALL_WARPS && a->groups <= 4096) {
     static std::atomic<int> largest[MAX_DEVICES] = {};
     const int dev = device();
     if (dev < 0) return IWP_ERR_CUDA;

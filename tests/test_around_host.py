@@ -65,7 +65,7 @@ GRAD = dict(tokens=8, experts=16, top_k=2, type=0, ids_bytes=4, logits=256, logi
 ORDER = dict(tokens=8, experts=16, top_k=2, ids_bytes=4, ids=256, ids_ld=2, offsets=256, slots=256, rows=256, workspace=256, workspace_bytes=1 << 30)
 ROWS = dict(tokens=8, dim=16, experts=16, top_k=2, type=0, slots=256, offsets=256, by_token=256, by_token_ld=16, by_slot=256, by_slot_ld=16, weights=256,
             weights_ld=2, by_token_out=256, by_token_out_ld=16, by_slot_out=256, by_slot_out_ld=16, dweights=256)
-CLIP = dict(table=256, parts=1, elements=10, squares=256, norms=256, factors=256, workspace=256, workspace_bytes=1 << 20, state=256, max_norm=1.0, scale=1.0,
+CLIP = dict(table=256, parts=1, warps=1, squares=256, norms=256, factors=256, workspace=256, workspace_bytes=1 << 20, state=256, max_norm=1.0, scale=1.0,
             groups=1, write=1)
 
 
@@ -106,7 +106,7 @@ def test_exchange_refuses(L, entry, bad):
 
 
 @pytest.mark.parametrize("bad", [
-    dict(table=None), dict(table=264), dict(parts=-1), dict(parts=1 << 27), dict(elements=-1), dict(squares=None), dict(squares=260), dict(norms=None), dict(factors=None),
+    dict(table=None), dict(table=264), dict(parts=-1), dict(parts=1 << 27), dict(warps=-1), dict(warps=4737), dict(squares=None), dict(squares=260), dict(norms=None), dict(factors=None),
     dict(workspace=None), dict(workspace=128), dict(state=None), dict(state=64), dict(max_norm=-1.0), dict(max_norm=math.nan), dict(scale=0.0), dict(scale=math.inf),
     dict(groups=0), dict(groups=(1 << 20) + 1)])
 def test_clip_refuses(L, bad):
@@ -120,7 +120,7 @@ def test_nothing_and_too_little(L):
     need = L.iwp_order_workspace(made(routing.OrderArgs, ORDER, {}))
     assert need > 0 and L.iwp_order_workspace(made(routing.OrderArgs, ORDER, dict(experts=0))) == -1 and L.iwp_order_workspace(None) == -1
     assert L.iwp_order(made(routing.OrderArgs, ORDER, dict(workspace_bytes=need - 1)), None) == binding.IWP_ERR_CAPACITY
-    assert L.iwp_clip(made(clipping.ClipArgs, CLIP, dict(elements=100_000, workspace_bytes=8 * (-(-100_000 // 512) + 1) - 1)), None) == binding.IWP_ERR_CAPACITY
+    assert L.iwp_clip(made(clipping.ClipArgs, CLIP, dict(warps=300, workspace_bytes=8 * 301 - 1)), None) == binding.IWP_ERR_CAPACITY
     for entry in ("iwp_route_grad", "iwp_dispatch", "iwp_combine", "iwp_combine_grad"):  # no tokens: nothing to do, no launch
         cls, base = (routing.RouteGradArgs, GRAD) if entry == "iwp_route_grad" else (routing.ExchangeArgs, ROWS)
         assert getattr(L, entry)(made(cls, base, dict(tokens=0)), None) == binding.IWP_OK
@@ -147,8 +147,7 @@ def table_of(L, tensors, groups):
     assert L.iwp_clip_table(arr, len(tensors), groups, raw, sizes.table_bytes - 1) == binding.IWP_ERR_CAPACITY
     assert L.iwp_clip_table(arr, len(tensors), groups, raw, sizes.table_bytes) == binding.IWP_OK
     at = C.addressof(raw)
-    n = sizes.elements
-    warps = min(256 if n <= 1 << 18 else 4736, -(-n // 512))
+    warps = sizes.warps
     starts = [Start.from_buffer_copy(s) for s in (Start * warps).from_address(at)] if warps else []
     at += warps * C.sizeof(Start)
     parts = [Part.from_buffer_copy(p) for p in (Part * sizes.parts).from_address(at)] if sizes.parts else []
@@ -169,7 +168,8 @@ def test_every_element_is_in_one_part_of_its_group(L, total):
         at += rows * ld * 4 + 64
         left -= rows * cols
     sizes, warps, spans, listed = table_of(L, tensors, groups)
-    assert sizes.elements == sum(t.rows * t.cols for t in tensors) and sizes.workspace_bytes >= 8 * (len(warps) + groups)
+    elements = sum(t.rows * t.cols for t in tensors)
+    assert sizes.workspace_bytes >= 8 * (len(warps) + groups)
     parts = [p for w in warps for p in w]
     assert bytes(b"".join(parts)) == bytes(b"".join(listed))
     # a warp's sum over a group has a place of its own, among the group's
@@ -178,8 +178,10 @@ def test_every_element_is_in_one_part_of_its_group(L, total):
     for g in range(groups):
         own = {q[0] for q in places if q[2] == g}
         assert own == set(range(*spans[g])), (g, spans[g])
-    size = [sum(p.rows * p.cols for p in mine) for mine in warps]
-    assert sum(size) == sizes.elements and max(size, default=0) <= max(512, sizes.elements // max(1, len(warps)) + 64)
+    cost = [sum(1024 + p.rows * p.cols for p in mine) for mine in warps]
+    assert sum(cost) == elements + 1024 * len(parts)
+    if warps:  # shared out evenly: what a range cut short leaves of it, and rounding
+        assert max(cost) <= sizes.range <= 1.1 * sum(cost) / len(cost) + 2 * 1024 + 3 * 128
     if total > 1_000_000:  # (element by element below)
         return
     width = {0: 4, 1: 2, 2: 2}
