@@ -94,11 +94,11 @@ __device__ __forceinline__ void square_run(const void* from, int n, int lane, do
     add_squares<TYPE, 1>(x, sum);
   }
   p += head, n -= head;
-  const Word<TYPE, VEC>* const w = reinterpret_cast<const Word<TYPE, VEC>*>(p);
+  const auto* const w = reinterpret_cast<const Raw<TYPE, VEC>*>(p);
   const int words = n / VEC;
   // a warp's lanes read neighbouring words; word u of a lane's eight is 32 further
   for (int i = lane; i < words; i += 32 * WORDS * AHEAD) {
-    Word<TYPE, VEC> y[AHEAD][WORDS];
+    Raw<TYPE, VEC> y[AHEAD][WORDS];
 #pragma unroll
     for (int a = 0; a < AHEAD; a++)
 #pragma unroll
@@ -110,7 +110,7 @@ __device__ __forceinline__ void square_run(const void* from, int n, int lane, do
     for (int a = 0; a < AHEAD; a++) {
       float x[8];
 #pragma unroll
-      for (int v = 0; v < 8; v++) x[v] = i + 32 * (a * WORDS + v / VEC) < words ? value<TYPE>(y[a][v / VEC].x[v % VEC]) : 0.f;
+      for (int v = 0; v < 8; v++) x[v] = i + 32 * (a * WORDS + v / VEC) < words ? element<TYPE, VEC>(y[a][v / VEC], v % VEC) : 0.f;
       if (i + 32 * a * WORDS < words) add_squares<TYPE, 8>(x, sum);
     }
   }
@@ -148,9 +148,9 @@ __device__ __forceinline__ void square(const Part& q, int lane, double& sum) {
     square_part<IWP_F16>(q, lane, sum);
 }
 
-template <int IN, int OUT>
-__device__ __forceinline__ typename Of<OUT>::T scaled(typename Of<IN>::T x, float f) {
-  return static_cast<typename Of<OUT>::T>(f == 0.f ? 0.f : value<IN>(x) * f);
+template <int OUT>
+__device__ __forceinline__ typename Of<OUT>::T scaled(float x, float f) {
+  return static_cast<typename Of<OUT>::T>(f == 0.f ? 0.f : x * f);
 }
 
 template <int IN, int OUT>
@@ -159,30 +159,34 @@ __device__ __forceinline__ void scale_run(const void* from, void* to, int n, int
   using U = typename Of<OUT>::T;
   // elements of a lane's word: 16 bytes of the wider type, so that a warp's loads and its stores are both contiguous
   constexpr int V = 16 / (sizeof(T) > sizeof(U) ? sizeof(T) : sizeof(U)), AHEAD = 4;
-  using WI = Word<IN, V>;
+  using WI = Raw<IN, V>;
   using WO = Word<OUT, V>;
   const T* p = static_cast<const T*>(from);
   U* q = static_cast<U*>(to);
   const int head = until_aligned<sizeof(U), sizeof(WO)>(q, n);
   if (until_aligned<sizeof(T), sizeof(WI)>(p + head, 1) == 0) {  // both at multiples of their words from there on
-    if (lane < head) q[lane] = scaled<IN, OUT>(p[lane], f);
+    if (lane < head) q[lane] = scaled<OUT>(value<IN>(p[lane]), f);
     p += head, q += head, n -= head;
     const int words = n / V;
     const WI* const wi = reinterpret_cast<const WI*>(p);
-    WO* const wo = reinterpret_cast<WO*>(q);
-    for (int i = lane; i < words; i += 32 * AHEAD) {
-      WI x[AHEAD];
+    auto* const wo = reinterpret_cast<Raw<OUT, V>*>(q);
+    // back to front, and written past the caches: what the sums read last is read from the L2 again
+    for (int i = words ? (words - 1) / (32 * AHEAD) * (32 * AHEAD) + lane : -1; i >= 0; i -= 32 * AHEAD) {
+      Raw<IN, V> x[AHEAD];
 #pragma unroll
-      for (int a = 0; a < AHEAD; a++) x[a] = wi[i + 32 * a < words ? i + 32 * a : i];
+      for (int a = 0; a < AHEAD; a++) x[a] = wi[min(i + 32 * a, words - 1)];
 #pragma unroll
       for (int a = 0; a < AHEAD; a++) {
-        WO y;
+        union {
+          WO y;
+          Raw<OUT, V> raw;
+        };
 #pragma unroll
-        for (int v = 0; v < V; v++) y.x[v] = scaled<IN, OUT>(x[a].x[v], f);
-        if (i + 32 * a < words) wo[i + 32 * a] = y;
+        for (int v = 0; v < V; v++) y.x[v] = scaled<OUT>(element<IN, V>(x[a], v), f);
+        if (i + 32 * a < words) __stcs(wo + i + 32 * a, raw);
       }
     }
-    if (lane < n - words * V) q[words * V + lane] = scaled<IN, OUT>(p[words * V + lane], f);
+    if (lane < n - words * V) q[words * V + lane] = scaled<OUT>(value<IN>(p[words * V + lane]), f);
     return;
   }
   constexpr int SINGLE = 8;
@@ -192,7 +196,7 @@ __device__ __forceinline__ void scale_run(const void* from, void* to, int n, int
     for (int a = 0; a < SINGLE; a++) x[a] = p[i + 32 * a < n ? i + 32 * a : i];
 #pragma unroll
     for (int a = 0; a < SINGLE; a++)
-      if (i + 32 * a < n) q[i + 32 * a] = scaled<IN, OUT>(x[a], f);
+      if (i + 32 * a < n) q[i + 32 * a] = scaled<OUT>(value<IN>(x[a]), f);
   }
 }
 
@@ -206,7 +210,7 @@ __device__ __forceinline__ void scale_part(const Part& q, int lane, float f) {
   } else {
     for (int i = lane; i < q.rows * q.cols; i += 32) {
       const int r = i / q.cols, c = i - r * q.cols;
-      static_cast<U*>(q.out)[r * q.out_ld + c] = scaled<IN, OUT>(static_cast<const T*>(q.in)[r * q.in_ld + c], f);
+      static_cast<U*>(q.out)[r * q.out_ld + c] = scaled<OUT>(value<IN>(static_cast<const T*>(q.in)[r * q.in_ld + c]), f);
     }
   }
 }
@@ -327,7 +331,7 @@ __global__ void __launch_bounds__(THREADS) k_groups(const Args a) {
   }
 }
 
-// Each warp its range again, back to front: what the sums read last may still be in the L2.
+// Each warp its range again.
 __device__ __forceinline__ void scale_range(const Args& a, int w, int lane) {
   const Start start = a.starts[w];
   wait_previous();
