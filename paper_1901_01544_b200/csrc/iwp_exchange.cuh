@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(ORDER_THREADS) k_order_count(const OrderArgs a
 
 // Dynamic shared memory: ORDER_WARPS * E counters.  A warp keeps up to KEPT * 32 of its pairs' experts in registers.
 template <int KEPT>
-__global__ void __launch_bounds__(ORDER_THREADS) k_order_place(const OrderArgs a) {
+__global__ void __launch_bounds__(ORDER_THREADS, 1) k_order_place(const OrderArgs a) {
   extern __shared__ int count[];  // [warp][E]
   __shared__ int part[ORDER_THREADS], part_before[ORDER_THREADS];
   __shared__ int sums[ORDER_WARPS];
@@ -109,10 +109,15 @@ __global__ void __launch_bounds__(ORDER_THREADS) k_order_place(const OrderArgs a
   if (tid < a.E) {
     int at = offset + before;
 #pragma unroll
-    for (int w = 0; w < ORDER_WARPS; w++) {
-      const int n = count[w * a.E + tid];
-      count[w * a.E + tid] = at;
-      at += n;
+    for (int w0 = 0; w0 < ORDER_WARPS; w0 += 16) {
+      int n[16];
+#pragma unroll
+      for (int w = 0; w < 16; w++) n[w] = count[(w0 + w) * a.E + tid];
+#pragma unroll
+      for (int w = 0; w < 16; w++) {
+        count[(w0 + w) * a.E + tid] = at;
+        at += n[w];
+      }
     }
     if (blockIdx.x == 0) a.offsets[tid] = offset;
   }
