@@ -405,6 +405,7 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
     const bool in = t < a.T, on = in && (!a.mask || a.mask[t]);
     uint32_t key[M];
     bool bad = false;
+    uint32_t gone = 0;  // bit i: place i holds a logit of -inf, or no column
     float top = -CUDART_INF_F, s = 0.f, tol = 0.f;  // of the row: largest logit, sum of exponentials below it
     {
       float x[M];
@@ -415,7 +416,10 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
       for (int i = 0; i < M; i++) odd = fmaf(x[i], 0.f, odd);
       if (odd != odd) {
 #pragma unroll
-        for (int i = 0; i < M; i++) bad |= isnan(x[i]) || (softmax && x[i] == CUDART_INF_F);
+        for (int i = 0; i < M; i++) {
+          bad |= isnan(x[i]) || (softmax && x[i] == CUDART_INF_F);
+          if (x[i] == -CUDART_INF_F) gone |= 1u << i;
+        }
       }
       bad = (__ballot_sync(ALL, bad) & of_row) != 0;
       if (softmax && (SCORES || !renormalize)) {
@@ -435,28 +439,28 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
           float sum = 0.f;
 #pragma unroll
           for (int i = 0; i < M; i++) {
-            const bool none = x[i] == -CUDART_INF_F;
             x[i] = ex2((x[i] - top) * LOG2E);
-            if (none) x[i] = 0.f;
             sum += x[i];
-            key[i] = none;
           }
           sum = sum_over<G>(sum);
           scale = sum > 0.f ? reciprocal(sum) : 0.f;
           tol = SOFTMAX_TOLERANCE * scale;
         } else {
 #pragma unroll
-          for (int i = 0; i < M; i++) {
-            key[i] = x[i] == -CUDART_INF_F;
-            x[i] = reciprocal(1.f + ex2(-x[i] * LOG2E));
-          }
+          for (int i = 0; i < M; i++) x[i] = reciprocal(1.f + ex2(-x[i] * LOG2E));
         }
-        if (a.bias) with_word<TYPE>(word, [&](auto v) { add_bias<M, G, decltype(v)::value>(x, scale, a.bias, g, a.E); });
+        if (a.bias) {
+          with_word<TYPE>(word, [&](auto v) { add_bias<M, G, decltype(v)::value>(x, scale, a.bias, g, a.E); });
+        } else {
 #pragma unroll
-        for (int i = 0; i < M; i++) {
-          // (what is not available, by its logit or its bias, is -inf; a NaN is less)
-          const float c = a.bias ? x[i] : x[i] * scale;
-          key[i] = key[i] || !(c > -CUDART_INF_F) ? 0 : (ordered(c) & ~LOW) | (LOW - i);
+          for (int i = 0; i < M; i++) x[i] *= scale;
+        }
+#pragma unroll
+        for (int i = 0; i < M; i++) key[i] = (ordered(x[i]) & ~LOW) | (LOW - i);
+        if (gone) {
+#pragma unroll
+          for (int i = 0; i < M; i++)
+            if (gone >> i & 1) key[i] = 0;
         }
       } else {
 #pragma unroll
@@ -526,6 +530,7 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
       __syncwarp();
     }
     top_eight<M>(key);
+    if (SCORES) again |= key[0] > (0xFF800000u | LOW);  // a NaN in the bias
     // the k largest, and one more, to see how far behind it is: a lane's keys wait in shared memory
     reinterpret_cast<uint4*>(waiting)[0] = make_uint4(key[0], key[1], key[2], key[3]);
     reinterpret_cast<uint4*>(waiting)[1] = make_uint4(key[4], key[5], key[6], key[7]);
