@@ -60,9 +60,10 @@ typedef struct iwp_route_args {
 int iwp_route(const iwp_route_args* args, void* cuda_stream); /* Errors: IWP_ERR_INVALID (sizes, NULL, types, strides), IWP_ERR_CUDA. */
 
 /* The gradient to the logits, for an upstream gradient dweights and the ids and weights of iwp_route():
- *   a_j = dweights[t][j] weights[t][j],  A = sum_j a_j
- *   softmax: dlogits[t][e] = sum of a_j over j with ids[t][j] == e  -  q_e A,  q_e = p of e where renormalized (0 elsewhere), else s_e
- *   sigmoid: dlogits[t][e] = (1 - s_e) (sum of those a_j - p_e A if renormalized)   at the chosen experts, 0 elsewhere
+ *   renormalized: b_j = weights[t][j] sum_i p_i (dweights[t][j] - dweights[t][i]),  p_i = weights[t][i] / weight_scale
+ *   else:         b_j = weights[t][j] dweights[t][j]
+ *   softmax: dlogits[t][e] = sum of b_j over j with ids[t][j] == e,  less s_e sum_j b_j if not renormalized
+ *   sigmoid: dlogits[t][e] = (1 - s_e) (sum of those b_j)
  * ids outside [0, E) take no part and give nothing; a row of nothing else (and, without renormalization, any expert of
  * logit -inf) gets 0. */
 typedef struct iwp_route_grad_args {

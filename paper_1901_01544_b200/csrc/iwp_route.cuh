@@ -623,8 +623,8 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
       }
     }
     if (renormalize) s = sum_over<G>(w);
-    if (softmax || renormalize) w *= s > 0.f ? a.weight_scale / s : 0.f;
-    else w *= a.weight_scale;
+    if (softmax || renormalize) w = s > 0.f ? w / s : 0.f;  // (1 if it is the only one)
+    w *= a.weight_scale;
     if (bad && on) w = CUDART_NAN_F, e = -1;
     if (in && g < a.k) {
       const int64_t to = static_cast<int64_t>(t) * a.k + g;
@@ -699,10 +699,9 @@ __global__ void __launch_bounds__(THREADS, grad_blocks_of(M)) k_route_grad(const
     const T* const row = static_cast<const T*>(a.logits) + t * a.logits_ld;
     T* const out = static_cast<T*>(a.dlogits) + t * a.dlogits_ld;
     const int e = next_id >= 0 && next_id < a.E ? static_cast<int>(next_id) : -1;
-    const float p = e >= 0 ? next_p : 0.f;  // weight, and its product with the gradient
-    float y = e >= 0 ? p * next_dw : 0.f;
+    const float p = e >= 0 ? next_p : 0.f, dw = e >= 0 ? next_dw : 0.f;
     fetch(static_cast<int64_t>(t) + static_cast<int64_t>(gridDim.x) * ROWS);
-    const float sum = sum_over<G>(y);
+    float y = p * dw;
     const bool some = (__ballot_sync(ALL, e >= 0) & of_row) != 0;
     float x = 0.f, old = 0.f;
     if (e >= 0) {
@@ -722,14 +721,20 @@ __global__ void __launch_bounds__(THREADS, grad_blocks_of(M)) k_route_grad(const
         s += v[i];
       }
       s = sum_over<G>(s);
-      const float f = s > 0.f ? -sum / s : 0.f;
+      const float sum = sum_over<G>(y), f = s > 0.f ? -sum / s : 0.f;
 #pragma unroll
       for (int i = 0; i < M; i++) v[i] *= f * a.scale;
       x = x > -CUDART_INF_F ? expf(x - top) * f : 0.f;  // what the chosen expert gets with the others
     } else {
 #pragma unroll
       for (int i = 0; i < M; i++) v[i] = 0.f;
-      if (a.renormalize) y -= p * a.inv_scale * sum;
+      if (a.renormalize) {
+        // differences of the upstream gradients, so that nothing is left of a choice of one, and what is left of a sure one is exact
+        y = 0.f;
+#pragma unroll 4
+        for (int i = 0; i < a.k; i++) y = fmaf(__shfl_sync(ALL, p, row0 + i), dw - __shfl_sync(ALL, dw, row0 + i), y);
+        y *= p * a.inv_scale;
+      }
       if (!softmax) y *= 1.f / (1.f + expf(x));
       x = 0.f;
     }

@@ -221,6 +221,44 @@ def test_grad(T, E, k, dtype, form):
     assert ((sums.double() - base.double() - 0.5 * want).abs() <= bound + half(dtype) * (base.double() + 0.5 * want).abs()).all()
 
 
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_grad_of_choices_that_are_sure(score):
+    """One expert per token, or one that outweighs the others by e^12: the gradient is a sum of p_j (dw_i - dw_j), each term off by
+    the weights' errors and two roundings, and none of a choice of one."""
+    T, E = 200, 40
+    x = torch.randn(T, E, generator=gen(50), device=DEV)
+    for scale in (1.0, 2.5):
+        one = routing.ExpertRouter(E, 1, score=score, weight_scale=scale)
+        r = one.route(x)
+        assert (r.weights == scale).all() and (one.grad(x, r.ids, r.weights, torch.randn(T, 1, device=DEV)) == 0).all()
+    x -= 6.0
+    x[:, 7] += 12.0
+    plan = routing.ExpertRouter(E, 4, score="softmax")
+    r = plan.route(x)
+    dw = torch.randn(T, 4, generator=gen(51), device=DEV)
+    got = torch.gather(plan.grad(x, r.ids, r.weights, dw), 1, r.ids.long()).double()
+    ids, p, _ = plain(x, 4)
+    d = dw.double()[:, :, None] - dw.double()[:, None, :]
+    want, size = p * (p[:, None, :] * d).sum(2), p * (p[:, None, :] * d.abs()).sum(2)
+    assert ((got - want).abs() <= (2 * slack(x, ids) + 16 * U) * size).all()
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_an_expert_named_twice_gets_both(form):
+    T, E, k = 50, 20, 3
+    x = torch.randn(T, E, generator=gen(52), device=DEV)
+    ids = torch.randint(0, E, (T, k), generator=gen(53), device=DEV)
+    ids[:, 2] = ids[:, 0]
+    dw = torch.randn(T, k, generator=gen(54), device=DEV)
+    plan = routing.ExpertRouter(E, k, **form)
+    w = torch.rand(T, k, generator=gen(55), device=DEV)
+    w = form.get("weight_scale", 1.0) * w / w.sum(1, keepdim=True)
+    got = plan.grad(x, ids, w, dw)
+    want, bound = grad_bound(x, ids, w.double(), dw, form, F32)
+    # the weights' sum is 1 but for its roundings
+    assert ((got.double() - want).abs() <= bound + 8 * U * (w * dw).abs().sum(1, keepdim=True).double()).all()
+
+
 @pytest.mark.parametrize("form", FORMS)
 def test_grad_against_differences(form):
     """The plain weights in 64 bits, at x + h v and x - h v with the choice held: the difference is off by h^2 / 6 times a third
