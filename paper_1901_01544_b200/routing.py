@@ -86,9 +86,9 @@ class Order(NamedTuple):
 
 
 class _Made(Order):
-    """An order that a plan has made: what its tensors are is known."""
+    """An order that a plan has made: its experts, tokens and choices, and where slots and offsets are."""
 
-    experts = 0
+    made = ()
 
 
 class _Here(_Plan):
@@ -225,20 +225,26 @@ class ExpertExchange(_Here):
         if status:
             raise IwpError(status, "iwp_order")
         order = _Made(offsets, slots, rows)
-        order.experts = self.experts
+        order.made = (self.experts, T, k, a.slots, a.offsets)
         return order
 
     def _begin(self, a: ExchangeArgs, order: Order, x, name: str):
         """T, k and the width of x, a matrix, in an exchange by `order`."""
-        offsets, slots, _ = order
-        if slots.dim() != 2 or x.dim() != 2:
-            raise ValueError(f"slots and {name} are matrices")
-        if type(order) is not _Made or order.experts != self.experts:
+        if x.dim() != 2:
+            raise ValueError(f"{name} is a matrix")
+        D = x.shape[1]
+        if type(order) is _Made and order.made[0] == self.experts:
+            _, T, k, a.slots, a.offsets = order.made
+        else:
+            offsets, slots, _ = order
+            if slots.dim() != 2:
+                raise ValueError("slots is a matrix")
             _vector(slots, "slots", slots.numel(), self._ids[1:], self.device)
             _vector(offsets, "offsets", self.experts + 1, self._ids[1:], self.device)
-        T, k = slots.shape
-        a.tokens, a.top_k, a.dim, a.slots, a.offsets = T, k, x.shape[1], slots.data_ptr(), offsets.data_ptr()
-        return T, k, x.shape[1]
+            T, k = slots.shape
+            a.slots, a.offsets = slots.data_ptr(), offsets.data_ptr()
+        a.tokens, a.top_k, a.dim = T, k, D
+        return T, k, D
 
     def _end(self, a: ExchangeArgs, at: int, call, entry: str) -> None:
         if a.tokens == 0 or a.dim == 0:
