@@ -4,7 +4,8 @@ between tokens and experts (`ExpertExchange`).  include/iwp_route.h has the form
 Like the rest of the binding this only marshals arguments: every step runs in the library's CUDA kernels on torch's current
 stream, there is no CPU fallback, and errors are `IwpError` (status codes) or `TypeError` / `ValueError` (tensors that do not
 fit the call).  Plans are used as those of `losses`: one stream and one thread at a time, made before a CUDA graph is
-captured and kept as long as the graph.
+captured and kept as long as the graph.  The differentiable forms can be captured with their backward pass, as torch's own
+operators can: nothing of an earlier eager backward graph of the same leaves may be left then.
 """
 from __future__ import annotations
 
@@ -316,6 +317,8 @@ class ExpertExchange(_Here):
             a.by_slot_ld = _rows_of(z, "z", (T * k, D), (dy.dtype,), self.device)
             dw = self._torch.empty(T, k, dtype=self._torch.float32, device=self.device)
             a.by_slot, a.dweights = z.data_ptr(), dw.data_ptr()
+        if D == 0 and dw is not None:
+            dw.zero_()
         if dz is not None or dw is not None:
             self._end(a, at, call, "iwp_combine_grad")
         return dz, dw

@@ -313,6 +313,10 @@ def test_no_tokens():
     z = exchange.dispatch(torch.empty(0, 8, device=DEV), o)
     assert z.shape == (0, 8) and exchange.combine(z, o, r.weights).shape == (0, 8)
     assert exchange.combine_grad(torch.empty(0, 8, device=DEV), z, o, r.weights)[0].shape == (0, 8)
+    # rows without columns
+    o = exchange.order(torch.zeros(5, 2, dtype=torch.int32, device=DEV))
+    z = exchange.dispatch(torch.empty(5, 0, device=DEV), o)
+    assert z.shape == (10, 0) and (exchange.combine_grad(torch.empty(5, 0, device=DEV), z, o)[1] == 0).all()
 
 
 def test_offsets_beyond_32_bits():
