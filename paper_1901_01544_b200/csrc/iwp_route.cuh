@@ -375,6 +375,10 @@ __host__ __device__ constexpr int blocks_of(int M, bool scores) { return M == 8 
 
 // SCORES: the choice goes by scores, or among groups; else by the logits alone.  k <= G: a lane has one pick at most.
 // word: elements that all rows are aligned for.
+//
+// Bound by the integer pipe, which takes a minimum or a maximum every other cycle: 131072 x 256 fp32, 8 choices, 54 us = 2.5 TB/s
+// at 270 instructions per row, half of them the sorts'.  (The largest of a lane taken k times from unsorted columns by 32 lanes per
+// row: 333 us; sorted, 32 lanes per row: 96.)  With sigmoid scores and a bias 78 us; 16384 x 256 bf16, 8 of which 4 groups 26 us.
 template <int TYPE, int M, int G, bool SCORES>
 __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const __grid_constant__ Args a, int word) {
   extern __shared__ __align__(16) char smem[];
@@ -671,7 +675,9 @@ struct GradArgs {
 __host__ __device__ constexpr int grad_blocks_of(int M) { return M <= 16 ? 5 : 4; }
 
 // A row's gradient is zero (or, for softmax taken as it is, a multiple of the scores) but at the chosen experts: all of it is
-// written in words first, then the chosen ones by a lane each.
+// written in words first, then the chosen ones by a lane each.  Bound by the writes: 131072 x 256 fp32 30 us = 4.5 TB/s, where
+// setting the same bytes to zero takes 19 (28 without the chosen ones; 77 with every lane looking for its columns among
+// the chosen).
 template <int TYPE, int M, int G>
 __global__ void __launch_bounds__(THREADS, grad_blocks_of(M)) k_route_grad(const __grid_constant__ GradArgs a, int word) {
   using T = typename Of<TYPE>::T;

@@ -261,7 +261,7 @@ class ExpertExchange(_Here):
         a.by_token_ld = _rows_of(x, "x", (T, D), self._floats, self.device)
         a.by_token, a.type = x.data_ptr(), self._codes[x.dtype]
         if out is None:
-            out = x.new_empty((T * k, D))
+            out = self._torch.empty(T * k, D, dtype=x.dtype, device=self.device)
             a.by_slot_out_ld = D
         else:
             a.by_slot_out_ld = _rows_of(out, "out", (T * k, D), (x.dtype,), self.device)
@@ -281,7 +281,7 @@ class ExpertExchange(_Here):
             a.weights_ld = _rows_of(weights, "weights", (T, k), self._floats[:1], self.device)
             a.weights = weights.data_ptr()
         if out is None:
-            out = z.new_empty((T, D))
+            out = self._torch.empty(T, D, dtype=z.dtype, device=self.device)
             a.by_token_out_ld = D
         else:
             a.by_token_out_ld = _rows_of(out, "out", (T, D), (z.dtype,), self.device)
@@ -307,7 +307,7 @@ class ExpertExchange(_Here):
         dz = dw = a.by_slot = a.by_slot_out = a.dweights = None
         if "rows" in want:
             if out is None:
-                dz = dy.new_empty((T * k, D))
+                dz = self._torch.empty(T * k, D, dtype=dy.dtype, device=self.device)
                 a.by_slot_out_ld = D
             else:
                 dz = out
