@@ -4,9 +4,10 @@
 // a time), M columns per lane, word by word in turn.  A column's key is its choice value in an order-preserving 32-bit code
 // whose lowest bits give way to the column's place in its lane.  Every lane sorts its eight largest keys by a network; then the largest
 // head is taken k times, ties as the columns go: so they fall to the lower expert.  Of 16-bit logits the codes lose
-// nothing.  Where they (or the rounding of scores) may have hidden an order, a warp makes the row's choice again: by the
-// logits themselves, or by scores in 64 bits (a row in a few hundred where values differ).  Only the chosen scores have to be exact
-// to the last bits, and only they are computed that way, by k lanes at the end.
+// nothing.  Where they (or the rounding of scores) may have hidden an order, in a row of a few hundred where values differ, the
+// choices in question are put in order by the logits themselves or by scores in 64 bits; a warp makes the row's choice again where even
+// that is not enough.  Only the chosen scores have to be exact to the last bits, and only they are computed that way, by k lanes at
+// the end.
 #pragma once
 
 #include <type_traits>
@@ -246,6 +247,25 @@ __device__ __noinline__ void choose(const Args& a, int64_t t, int* pick) {
   }
 }
 
+// A score in 64 bits; sum: of softmax's exponentials below `top`.
+static __device__ __noinline__ double exact_score(float x, float top, double sum, bool softmax) {
+  const double y = exp(softmax ? static_cast<double>(x) - top : -static_cast<double>(x));
+  return softmax ? y / sum : 1. / (1. + y);
+}
+
+// The sum of a row's exponentials below `top`, off by 2^-22 of itself at most (two units in the last place of expf).
+template <int TYPE, int M, int G>
+__device__ __noinline__ double exact_sum(const typename Of<TYPE>::T* row, int g, int E, bool on, int word, float top) {
+  float x[M];
+  load_columns<TYPE, M, G>(x, row, g, E, on, word);
+  double s = 0;
+#pragma unroll
+  for (int i = 0; i < M; i++) s += x[i] == -CUDART_INF_F ? 0.f : expf(x[i] - top);
+#pragma unroll
+  for (int o = G / 2; o; o /= 2) s += __shfl_xor_sync(ALL, s, o);
+  return s;
+}
+
 __device__ __forceinline__ void in_order(uint32_t& a, uint32_t& b) {
   const uint32_t high = max(a, b), low = min(a, b);
   a = high, b = low;
@@ -304,9 +324,9 @@ __host__ __device__ inline Shared shared_of(int E, int groups, int G, int M) {
   Shared s;
   s.waiting = 0;
   s.list = s.waiting + 4 * THREADS * WAITING;
-  s.hist = s.list + 8 * rows * (G + 1);
+  s.hist = s.list + 8 * rows * 2 * G;
   s.pick = s.hist + 4 * E;
-  s.row = s.pick + 4 * THREADS;
+  s.row = (s.pick + 4 * THREADS + 15) / 16 * 16;
   s.score = s.row + (groups > 1 ? 4 * rows * G * M : 0);
   s.bytes = s.score + (groups > 1 ? 8 * rows * groups : 0);
   return s;
@@ -389,7 +409,7 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
   const Shared at = shared_of(a.E, a.groups, G, M);
   const int tid = threadIdx.x, lane = tid & 31, g = lane & (G - 1), rl = tid / G, row0 = lane & ~(G - 1);
   uint32_t* const waiting = reinterpret_cast<uint32_t*>(smem + at.waiting) + tid * WAITING;
-  uint2* const list = reinterpret_cast<uint2*>(smem + at.list) + rl * (G + 1);
+  uint2* const list = reinterpret_cast<uint2*>(smem + at.list) + rl * 2 * G;
   int* const hist = reinterpret_cast<int*>(smem + at.hist);
   int* const pick = reinterpret_cast<int*>(smem + at.pick) + (tid & ~31);
   const unsigned of_row = (G == 32 ? ALL : (1u << G) - 1) << row0, before = ((1u << lane) - 1) & of_row;
@@ -410,6 +430,7 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
     uint32_t key[M];
     bool bad = false;
     uint32_t gone = 0;  // bit i: place i holds a logit of -inf, or no column
+    float scale_of_row = 0.f;  // the largest softmax score
     float top = -CUDART_INF_F, s = 0.f, tol = 0.f;  // of the row: largest logit, sum of exponentials below it
     {
       float x[M];
@@ -448,6 +469,7 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
           }
           sum = sum_over<G>(sum);
           scale = sum > 0.f ? reciprocal(sum) : 0.f;
+          scale_of_row = scale;
           tol = SOFTMAX_TOLERANCE * scale;
         } else {
 #pragma unroll
@@ -529,7 +551,61 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
       most = max_over<G>(most);
 #pragma unroll
       for (int o = G / 2; o; o /= 2) open |= __shfl_xor_sync(ALL, open, o);
-      again = most > -CUDART_INF_F && least < CUDART_INF_F && !apart(least, most, 2.f * tol);
+      const bool question = on && !bad && most > -CUDART_INF_F && least < CUDART_INF_F && !apart(least, most, 2.f * tol);
+      if (__any_sync(ALL, question)) {
+        // groups' scores in 64 bits, from the columns that make them up
+        double* const exact = reinterpret_cast<double*>(group_score);
+        const double sum = softmax && by_score ? exact_sum<TYPE, M, G>(row, g, a.E, on, word, top) : 1.;
+        __syncwarp();
+        for (int q = g; q < a.groups; q += G) {
+          uint32_t b1 = 0, b2 = 0, b3 = 0;
+          int e1 = 0, e2 = 0;
+          for (int e = q * size; e < (q + 1) * size; e++) {
+            const uint32_t y = keys[e] | LOW;  // (places do not compare)
+            if (y > b1)
+              b3 = b2, b2 = b1, e2 = e1, b1 = y, e1 = e;
+            else if (y > b2)
+              b3 = b2, b2 = y, e2 = e;
+            else if (y > b3)
+              b3 = y;
+          }
+          const bool two = a.group_top == 2, some = on && b1 > NONE && (!two || b2 > NONE);
+          double score = -CUDART_INF;
+          if (some) {
+            auto value = [&](int e) {
+              const float x = static_cast<float>(row[e]);
+              if (!by_score) return static_cast<double>(x);
+              const double y = exact_score(x, top, sum, softmax);
+              return a.bias ? y + a.bias[e] : y;
+            };
+            score = value(e1);
+            if (two) {
+              const double other = value(e2);
+              score = score > other ? score + other : other + score;
+            }
+            // another column may belong in its place, by as little as the codes hide
+            const uint32_t in = two ? b2 : b1, out = two ? b3 : b2;
+            again |= question && out > NONE && !apart(unordered(in & ~LOW), unordered(out), tol);
+          }
+          exact[q] = score;
+        }
+        __syncwarp();
+        if (question) open = 0;
+        for (int q = g; q < a.groups; q += G) {
+          const double mine = exact[q];
+          int ahead = 0;
+          for (int p = 0; p < a.groups; p++) {
+            const double other = exact[p];
+            ahead += other > mine || (other == mine && p < q);
+            // (the error of softmax's sum is common to all scores, but not to the biases)
+            if (softmax && a.bias && question && other != mine && other > -CUDART_INF && mine > -CUDART_INF) again |= fabs(other - mine) <= 0x1p-20 * scale_of_row;
+          }
+          if (question && ahead < a.top_groups) open |= 1u << q;
+        }
+#pragma unroll
+        for (int o = G / 2; o; o /= 2) open |= __shfl_xor_sync(ALL, open, o);
+        again = (__ballot_sync(ALL, again) & of_row) != 0;
+      }
       with_word<TYPE>(word, [&](auto v) { close_groups<M, G, decltype(v)::value>(key, open, size, a.groups, g); });
       __syncwarp();
     }
@@ -558,41 +634,59 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
     };
     const uint2 mine = listed(g < a.k ? g : 0);
     int e = mine.x > NONE && on && g < a.k ? static_cast<int>(mine.y) : -1;
-    float y = e >= 0 ? static_cast<float>(row[e]) : -CUDART_INF_F;
     if (!LOSSLESS) {
       auto close = [&](uint32_t high, uint32_t low) {
         return low > NONE && (SCORES ? !apart(unordered(high & ~LOW), unordered(low | LOW), tol) : (high ^ low) <= LOW);
       };
-      auto differ = [&](int e1) { return y != static_cast<float>(row[e1]) || (SCORES && a.bias && a.bias[e] != a.bias[e1]); };
-      bool last = false;  // this lane's choice is the row's last, and the next is as good
-      if (e >= 0) {
-        const uint2 next = listed(g + 1);
-        if (close(mine.x, next.x)) {
-          if (g < a.k - 1)
-            again |= SCORES && a.bias ? differ(next.y) : y < static_cast<float>(row[next.y]);
-          else if (differ(next.y))
-            again = true;
-          else
-            last = true;  // so may be others
-        }
-      }
-      for (int n = 0; __any_sync(ALL, last); n++) {
-        __syncwarp();
-        if (n < 4) {
-          take(a.k);
+      const bool question = e >= 0 && !bad && close(mine.x, list[g + 1].x);
+      if (__any_sync(ALL, question)) {
+        // all that may be as good as the k-th, up to two per lane, in order of what the codes stand for
+        int n = picks;
+        auto more = [&] { return on && !bad && close(list[a.k - 1].x, list[n - 1].x); };
+        while (n < 2 * G && __any_sync(ALL, more())) {
+          take(n++);
           __syncwarp();
         }
-        if (last) {
-          const uint2 next = listed(a.k);
-          if (n >= 4)
-            again = true, last = false;
-          else if (!close(mine.x, next.x))
-            last = false;
-          else if (differ(next.y))
-            again = true, last = false;
+        again |= more();
+        const bool exact = SCORES && a.bias;
+        const double sum = exact && softmax ? exact_sum<TYPE, M, G>(row, g, a.E, on, word, top) : 1.;
+        double value[2];
+        float bias[2] = {0.f, 0.f};
+        int expert[2], rank[2] = {0, 0};
+#pragma unroll
+        for (int u = 0; u < 2; u++) {
+          const int j = g + u * G;
+          const uint2 p = listed(j < n ? j : 0);
+          const bool there = on && j < n && p.x > NONE;
+          expert[u] = there ? static_cast<int>(p.y) : MAX_EXPERTS + j;
+          value[u] = -CUDART_INF;
+          if (there) {
+            const float x = static_cast<float>(row[p.y]);
+            if (exact) bias[u] = a.bias[p.y];
+            value[u] = exact ? exact_score(x, top, sum, softmax) + bias[u] : static_cast<double>(x);
+          }
         }
+        for (int i = 0; i < n; i++) {
+          const double other = __shfl_sync(ALL, i < G ? value[0] : value[1], row0 + (i & (G - 1)));
+          const int its = __shfl_sync(ALL, i < G ? expert[0] : expert[1], row0 + (i & (G - 1)));
+          const float its_bias = __shfl_sync(ALL, i < G ? bias[0] : bias[1], row0 + (i & (G - 1)));
+#pragma unroll
+          for (int u = 0; u < 2; u++) {
+            rank[u] += other > value[u] || (other == value[u] && its < expert[u]);
+            // (the error of softmax's sum is common to all scores, but not to the biases)
+            if (exact && softmax && other != value[u] && its < MAX_EXPERTS && expert[u] < MAX_EXPERTS)
+              again |= fabs(other - value[u]) <= 0x1p-21 * fabs((other - its_bias) - (value[u] - bias[u]));
+          }
+        }
+        __syncwarp();
+#pragma unroll
+        for (int u = 0; u < 2; u++)
+          if (g + u * G < n && rank[u] < a.k) list[rank[u]].y = expert[u];
+        __syncwarp();
+        if (e >= 0) e = static_cast<int>(list[g].y);
       }
     }
+    float y = e >= 0 ? static_cast<float>(row[e]) : -CUDART_INF_F;
     if (!LOSSLESS || M > 8) {
       if (M > 8) again |= behind == waiting + 9;  // there may have been more in this lane
       unsigned todo = __ballot_sync(ALL, again && on && !bad);

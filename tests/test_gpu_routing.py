@@ -132,6 +132,43 @@ def test_choices_that_fp32_cannot_tell_apart(E, groups, score):
 
 
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("size", [2, 3, 5, 12])
+@pytest.mark.parametrize("E,k,groups", [(64, 8, 1), (64, 5, 8), (256, 8, 8), (200, 7, 5), (16, 2, 1), (512, 8, 4)])
+def test_clusters_of_choices_as_good(E, k, groups, size, score):
+    """Clusters of `size` experts whose s + b differ by the rounding of b alone, clusters 0.01 apart, some of a cluster equal in
+    every bit; wherever the k-th falls in its cluster."""
+    for seed in range(4):
+        g = gen(100 + seed)
+        x = torch.randn(1, E, generator=g, device=DEV)
+        order = torch.randperm(E, generator=g, device=DEV)
+        cluster = torch.empty(E, dtype=torch.long, device=DEV)
+        cluster[order] = torch.arange(E, device=DEV) // size
+        for c in range(0, E // size, 2):  # two of every other cluster have the same logit, and so the same bias
+            pair = (cluster == c).nonzero()[:2, 0]
+            x[0, pair[-1]] = x[0, pair[0]]
+        s = (torch.softmax(x.double(), 1) if score == "softmax" else torch.sigmoid(x.double()))[0]
+        bias = (0.01 * cluster.double() + 0.3 - s).float()
+        rows = torch.cat([x.repeat(20, 1), torch.randn(20, E, generator=g, device=DEV)])
+        for kw in (dict(score=score, groups=groups, top_groups=max(1, groups // 2)), dict(score=score, groups=groups, top_groups=max(1, groups - 1), group_top=1)):
+            if k <= E // groups * kw["top_groups"]:
+                check_route(routing.ExpertRouter(E, k, **kw), rows, bias, **kw)
+
+
+@pytest.mark.parametrize("groups", [1, 4])
+def test_clusters_of_logits_as_good(groups):
+    """fp32 logits that differ in their last bits, and some that do not."""
+    E, k = 128, 8
+    for seed in range(4):
+        g = gen(200 + seed)
+        base = torch.randint(-4, 5, (60, E), generator=g, device=DEV).float() + 0.1
+        x = base * (1 + torch.randint(0, 3, (60, E), generator=g, device=DEV) * 2.0**-23)
+        for score in ("softmax", "sigmoid"):
+            kw = dict(score=score, groups=groups, top_groups=max(1, groups // 2))
+            check_route(routing.ExpertRouter(E, k, **kw), x, **kw)
+            check_route(routing.ExpertRouter(E, k, group_top=1, **kw), x, group_top=1, **kw)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 def test_ties_go_to_the_lower_expert(score):
     T, E, k = 300, 96, 8
     x = torch.randint(-2, 3, (T, E), generator=gen(5), device=DEV).to(BF)
