@@ -439,7 +439,7 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
       float odd = 0.f;
 #pragma unroll
       for (int i = 0; i < M; i++) odd = fmaf(x[i], 0.f, odd);
-      if (odd != odd) {
+      if (on && odd != odd) {
 #pragma unroll
         for (int i = 0; i < M; i++) {
           bad |= isnan(x[i]) || (softmax && x[i] == CUDART_INF_F);
