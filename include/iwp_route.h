@@ -38,7 +38,8 @@ int iwp_route_reset(void* state, void* cuda_stream);
  * An expert whose logit or bias is -inf (or whose bias is NaN) is not available: not chosen, and no other is in its place,
  * so a row of fewer than top_k available experts ends in ids of -1 with weights 0.  A group with fewer than group_top
  * available experts is scored -inf.  A row with mask[t] == 0 has ids -1 and weights 0; a row that holds a NaN (or, for
- * softmax, +inf) has ids -1 and weights NaN.
+ * softmax, +inf) has ids -1 and weights NaN.  A row's ids do not depend on the other rows or on how many there are; its
+ * weights may differ in the last places between calls of fewer and of more than 24576 rows, which sum in another order.
  */
 typedef struct iwp_route_args {
   int64_t tokens;                  /* 0 <= T <= 2^30, T E <= 2^46 */

@@ -82,7 +82,8 @@ def check_route(plan, x, bias=None, mask=None, **kw):
 FORMS = [
     dict(score="softmax"), dict(score="sigmoid"), dict(score="softmax", renormalize=False, weight_scale=2.5), dict(score="sigmoid", renormalize=False),
 ]
-SIZES = [(1, 1, 1), (1, 256, 8), (7, 3, 2), (64, 8, 2), (1000, 60, 4), (257, 64, 6), (33, 257, 8), (129, 512, 10), (65, 1024, 32), (50, 37, 32), (3, 32, 32), (2500, 128, 8)]
+SIZES = [(1, 1, 1), (1, 256, 8), (7, 3, 2), (64, 8, 2), (1000, 60, 4), (257, 64, 6), (33, 257, 8), (129, 512, 10), (65, 1024, 32), (50, 37, 32), (3, 32, 32), (2500, 128, 8),
+         (700, 31, 2), (701, 24, 1), (333, 33, 4), (90, 64, 2), (91, 100, 3), (64, 300, 20), (24600, 31, 2), (24577, 33, 4), (24576, 64, 1), (24576, 20, 7)]
 
 
 @pytest.mark.parametrize("form", FORMS)
