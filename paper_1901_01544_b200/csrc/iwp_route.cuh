@@ -852,6 +852,7 @@ __global__ void __launch_bounds__(THREADS, grad_blocks_of(M)) k_route_grad(const
       }
       y = all;
     }
+    __syncwarp();  // what other lanes write has been read
     if (in && (dense || !a.accumulate))
       with_word<TYPE>(word, [&](auto vec) { store_words<TYPE, M, G, decltype(vec)::value>(v, out, g, a.E, a.accumulate); });
     __syncwarp();

@@ -87,7 +87,7 @@ class Order(NamedTuple):
 
 
 class _Made(Order):
-    """An order that a plan has made: its experts, tokens and choices, and where slots and offsets are."""
+    """An order that a plan has made: the plan, tokens and choices, and where slots and offsets are."""
 
     made = ()
 
@@ -226,7 +226,7 @@ class ExpertExchange(_Here):
         if status:
             raise IwpError(status, "iwp_order")
         order = _Made(offsets, slots, rows)
-        order.made = (self.experts, T, k, a.slots, a.offsets)
+        order.made = (self, T, k, a.slots, a.offsets)
         return order
 
     def _begin(self, a: ExchangeArgs, order: Order, x, name: str):
@@ -234,7 +234,7 @@ class ExpertExchange(_Here):
         if x.dim() != 2:
             raise ValueError(f"{name} is a matrix")
         D = x.shape[1]
-        if type(order) is _Made and order.made[0] == self.experts:
+        if type(order) is _Made and order.made[0] is self:
             _, T, k, a.slots, a.offsets = order.made
         else:
             offsets, slots, _ = order

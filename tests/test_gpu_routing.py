@@ -604,3 +604,15 @@ def test_refusals():
     # what is in range but not a slot is nobody's
     y = ex.combine(torch.ones(10, 3, device=DEV), routing.Order(o.offsets, torch.full_like(o.slots, 1000), o.rows))
     assert (y == 0).all()
+
+
+def test_order_of_another_plan():
+    """An order is taken as made by the plan that made it alone; by another it is looked at like any other tensors."""
+    one, two = routing.ExpertExchange(8), routing.ExpertExchange(8)
+    x = torch.randn(5, 4, device=DEV)
+    o = one.order(torch.randint(0, 8, (5, 2), device=DEV))
+    assert torch.equal(one.dispatch(x, o), two.dispatch(x, o))
+    other = routing._Made(*(y.cpu() for y in o))
+    other.made = o.made
+    with pytest.raises(ValueError):
+        two.dispatch(x, other)
