@@ -56,17 +56,46 @@ __device__ __forceinline__ float load(const void* p, int64_t at) {
 }
 
 // Lane g's M columns of a row, in words of VEC that the G lanes take in turn: place i holds column
-// ((i / VEC) G + g) VEC + i % VEC.  -inf outside.
+// ((i / VEC) G + g) VEC + i % VEC.  -inf outside.  (For a type of 16 bits places 2 i and 2 i + 1 are one of `two`.)
 template <int TYPE, int M, int G, int VEC>
-__device__ __forceinline__ void load_words(float (&x)[M], const typename Of<TYPE>::T* row, int g, int E, bool in) {
+__device__ __forceinline__ void load_pairs(uint32_t (&two)[M / 2], const typename Of<TYPE>::T* row, int g, int E, bool in) {
+  constexpr uint32_t NOTHING = TYPE == IWP_BF16 ? 0xFF80u : 0xFC00u;
 #pragma unroll
   for (int n = 0; n < M / VEC; n++) {
     const int first = (n * G + g) * VEC;
-    Raw<TYPE, VEC> w;
     const bool here = in && first < E;
-    if (here) w = *reinterpret_cast<const Raw<TYPE, VEC>*>(row + first);
+    if constexpr (VEC == 1) {
+      uint32_t w = NOTHING;
+      if (here) w = *reinterpret_cast<const uint16_t*>(row + first);
+      two[n / 2] = n % 2 ? two[n / 2] | w << 16 : w;
+    } else {
 #pragma unroll
-    for (int v = 0; v < VEC; v++) x[n * VEC + v] = here ? element<TYPE, VEC>(w, v) : -CUDART_INF_F;
+      for (int u = 0; u < VEC / 2; u++) two[n * VEC / 2 + u] = NOTHING << 16 | NOTHING;
+      if (here) {
+        const Raw<TYPE, VEC> w = *reinterpret_cast<const Raw<TYPE, VEC>*>(row + first);
+#pragma unroll
+        for (int u = 0; u < VEC / 2; u++) two[n * VEC / 2 + u] = reinterpret_cast<const uint32_t*>(&w)[u];
+      }
+    }
+  }
+}
+template <int TYPE, int M, int G, int VEC>
+__device__ __forceinline__ void load_words(float (&x)[M], const typename Of<TYPE>::T* row, int g, int E, bool in) {
+  if constexpr (TYPE != IWP_F32) {
+    uint32_t two[M / 2];
+    load_pairs<TYPE, M, G, VEC>(two, row, g, E, in);
+#pragma unroll
+    for (int i = 0; i < M; i++) x[i] = element<TYPE, 2>(two[i / 2], i % 2);
+  } else {
+#pragma unroll
+    for (int n = 0; n < M / VEC; n++) {
+      const int first = (n * G + g) * VEC;
+      Raw<TYPE, VEC> w;
+      const bool here = in && first < E;
+      if (here) w = *reinterpret_cast<const Raw<TYPE, VEC>*>(row + first);
+#pragma unroll
+      for (int v = 0; v < VEC; v++) x[n * VEC + v] = here ? element<TYPE, VEC>(w, v) : -CUDART_INF_F;
+    }
   }
 }
 
