@@ -90,11 +90,13 @@ __device__ __forceinline__ void load_words(float (&x)[M], const typename Of<TYPE
 #pragma unroll
     for (int n = 0; n < M / VEC; n++) {
       const int first = (n * G + g) * VEC;
-      Raw<TYPE, VEC> w;
-      const bool here = in && first < E;
-      if (here) w = *reinterpret_cast<const Raw<TYPE, VEC>*>(row + first);
 #pragma unroll
-      for (int v = 0; v < VEC; v++) x[n * VEC + v] = here ? element<TYPE, VEC>(w, v) : -CUDART_INF_F;
+      for (int v = 0; v < VEC; v++) x[n * VEC + v] = -CUDART_INF_F;
+      if (in && first < E) {
+        const Raw<TYPE, VEC> w = *reinterpret_cast<const Raw<TYPE, VEC>*>(row + first);
+#pragma unroll
+        for (int v = 0; v < VEC; v++) x[n * VEC + v] = element<TYPE, VEC>(w, v);
+      }
     }
   }
 }
@@ -130,6 +132,29 @@ __device__ __forceinline__ void with_word(int word, const F& f) {
 template <int TYPE, int M, int G>
 __device__ __forceinline__ void load_columns(float (&x)[M], const typename Of<TYPE>::T* row, int g, int E, bool in, int word) {
   with_word<TYPE>(word, [&](auto v) { load_words<TYPE, M, G, decltype(v)::value>(x, row, g, E, in); });
+}
+
+// Two neighbours' arithmetic at once.
+template <int TYPE>
+struct Pair {
+  using T = __nv_bfloat162;
+};
+template <>
+struct Pair<IWP_F16> {
+  using T = __half2;
+};
+template <int TYPE>
+__device__ __forceinline__ typename Pair<TYPE>::T pair_of(uint32_t two) {
+  return reinterpret_cast<const typename Pair<TYPE>::T&>(two);
+}
+// Each of two neighbours as 16 bits that order as the values do.
+template <int TYPE>
+__device__ __forceinline__ uint32_t ordered_pair(uint32_t two) {
+  const typename Pair<TYPE>::T zero = pair_of<TYPE>(0), sum = __hadd2_rn(pair_of<TYPE>(two), zero);  // (-0 is 0)
+  const uint32_t u = reinterpret_cast<const uint32_t&>(sum);
+  uint32_t negative;  // the halves' signs, 16 times each
+  asm("prmt.b32 %0, %1, %1, 0xBB99;" : "=r"(negative) : "r"(u));
+  return u ^ (negative | 0x80008000u);
 }
 
 // Over groups of G lanes.
@@ -433,7 +458,8 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
   extern __shared__ __align__(16) char smem[];
   using T = typename Of<TYPE>::T;
   constexpr uint32_t LOW = M - 1;  // the bits of a key that hold its place in the lane
-  constexpr bool LOSSLESS = !SCORES && TYPE != IWP_F32;
+  constexpr bool LOSSLESS = !SCORES && TYPE != IWP_F32;  // the type's own 16 bits are in a key
+  constexpr uint32_t NO_EXPERT = LOSSLESS && TYPE == IWP_F16 ? 0x03FFFFFFu : NONE;
   constexpr int ROWS = THREADS / G, AGAIN = M * G > 32 ? M * G / 32 : 1;  // columns per lane where a warp has one row
   const Shared at = shared_of(a.E, a.groups, G, M);
   const int tid = threadIdx.x, lane = tid & 31, g = lane & (G - 1), rl = tid / G, row0 = lane & ~(G - 1);
@@ -463,12 +489,26 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
     float top = -CUDART_INF_F, s = 0.f, tol = 0.f;  // of the row: largest logit, sum of exponentials below it
     {
       float x[M];
-      load_columns<TYPE, M, G>(x, row, g, a.E, on, word);
+      [[maybe_unused]] uint32_t two[M / 2];
       // rows that hold a NaN or an infinity are looked at again
-      float odd = 0.f;
+      bool odd;
+      if constexpr (LOSSLESS) {
+        with_word<TYPE>(word, [&](auto v) { load_pairs<TYPE, M, G, decltype(v)::value>(two, row, g, a.E, on); });
 #pragma unroll
-      for (int i = 0; i < M; i++) odd = fmaf(x[i], 0.f, odd);
-      if (on && odd != odd) {
+        for (int i = 0; i < M; i++) x[i] = element<TYPE, 2>(two[i / 2], i % 2);
+        const auto zero = pair_of<TYPE>(0);
+        auto sum = zero;
+#pragma unroll
+        for (int i = 0; i < M / 2; i++) sum = __hfma2(pair_of<TYPE>(two[i]), zero, sum);
+        odd = __hisnan(sum.x) || __hisnan(sum.y);
+      } else {
+        load_columns<TYPE, M, G>(x, row, g, a.E, on, word);
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < M; i++) sum = fmaf(x[i], 0.f, sum);
+        odd = sum != sum;
+      }
+      if (on && odd) {
 #pragma unroll
         for (int i = 0; i < M; i++) {
           bad |= isnan(x[i]) || (softmax && x[i] == CUDART_INF_F);
@@ -516,6 +556,13 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
 #pragma unroll
           for (int i = 0; i < M; i++)
             if (gone >> i & 1) key[i] = 0;
+        }
+      } else if constexpr (LOSSLESS) {
+#pragma unroll
+        for (int i = 0; i < M; i += 2) {
+          const uint32_t u = ordered_pair<TYPE>(two[i / 2]);
+          key[i] = (u << 16) + (LOW - i);
+          key[i + 1] = (u & 0xFFFF0000u) | (LOW - i - 1);
         }
       } else {
 #pragma unroll
@@ -662,7 +709,7 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
       return make_uint2(p.x, column(LOW - (p.x & LOW), p.y));
     };
     const uint2 mine = listed(g < a.k ? g : 0);
-    int e = mine.x > NONE && on && g < a.k ? static_cast<int>(mine.y) : -1;
+    int e = mine.x > NO_EXPERT && on && g < a.k ? static_cast<int>(mine.y) : -1;
     if (!LOSSLESS) {
       auto close = [&](uint32_t high, uint32_t low) {
         return low > NONE && (SCORES ? !apart(unordered(high & ~LOW), unordered(low | LOW), tol) : (high ^ low) <= LOW);

@@ -616,3 +616,20 @@ def test_order_of_another_plan():
     other.made = o.made
     with pytest.raises(ValueError):
         two.dispatch(x, other)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T,E,k", [(300, 24, 5), (301, 31, 2), (200, 257, 8)])
+def test_values_at_the_ends_of_the_types(T, E, k, dtype, score):
+    """Zeros of both signs (which are equal), subnormal numbers, the lowest and the largest ones, -inf; also in rows of nothing else."""
+    f = torch.finfo(dtype)
+    least = f.smallest_normal * f.eps
+    values = torch.tensor([0.0, -0.0, least, -least, 3 * least, f.smallest_normal, -f.smallest_normal, f.min, f.max if score == "sigmoid" else 1.0,
+                           f.min * (1 - f.eps), -math.inf], dtype=torch.float64, device=DEV).to(dtype)
+    g = torch.Generator(device=DEV).manual_seed(T)
+    x = values[torch.randint(0, len(values), (T, E), device=DEV, generator=g)]
+    x[:100] = values[torch.randint(0, 7, (100, E), device=DEV, generator=g)]
+    x[100:110] = values[torch.tensor([7, 10], device=DEV)[torch.randint(0, 2, (10, E), device=DEV, generator=g)]]
+    plan = routing.ExpertRouter(E, k, score=score, renormalize=False)
+    check_route(plan, x, score=score, renormalize=False)
