@@ -268,3 +268,28 @@ def test_refusals():
         plan.clip(1.0, squares=torch.ones(2, device=DEV, dtype=torch.float64))
     assert (x == 1).all()
     assert clipping.GradientClip([x, x]).norm().norms.item() == pytest.approx(math.sqrt(20), rel=1e-6)
+
+
+@pytest.mark.parametrize("into", [F32, BF, FP])
+@pytest.mark.parametrize("dtype", [F32, BF, FP])
+def test_every_alignment_of_short_and_long_runs(dtype, into):
+    """Sources and outputs that start anywhere in a word, of all lengths around one; what lies around the outputs stays."""
+    g = torch.Generator(device=DEV).manual_seed(5)
+    sizes = [*range(1, 40), 255, 1000, 4099]
+    pairs = [(a, b) for a in range(8) for b in range(8)]
+    xs, ys, outs = [], [], []
+    for i, (a, b) in enumerate(pairs):
+        n = sizes[i % len(sizes)] + (i // len(sizes))
+        xs.append(torch.randn(a + n + 8, generator=g, device=DEV).to(dtype)[a:a + n])
+        outs.append(torch.full((b + n + 8,), 7.0, device=DEV, dtype=into))
+        ys.append(outs[-1][b:b + n])
+    for a in range(8):  # long ones, by warps that start anywhere
+        n = 300007 + a
+        xs.append(torch.randn(n + 8, generator=g, device=DEV).to(dtype)[a:a + n])
+        outs.append(torch.full((n + 16,), 7.0, device=DEV, dtype=into))
+        ys.append(outs[-1][3:3 + n])
+        pairs.append((a, 3))
+    clipping.GradientClip(xs, ys).clip(math.inf, scale=0.5)
+    for x, y, out, (_, b) in zip(xs, ys, outs, pairs):
+        assert torch.equal(y, (x.float() * 0.5).to(into))
+        assert (out[:b] == 7).all() and (out[b + x.numel():] == 7).all()
