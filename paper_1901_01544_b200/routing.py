@@ -87,9 +87,17 @@ class Order(NamedTuple):
 
 
 class _Made(Order):
-    """An order that a plan has made: the plan, tokens and choices, and where slots and offsets are."""
+    """An order as a plan has made it: the plan, the shape of the slots, and where slots and offsets are.  What is made of it
+    (`_replace`, copies) is an order like any other."""
 
-    made = ()
+    made = None
+
+    @classmethod
+    def _make(cls, tensors):
+        return Order(*tensors)
+
+    def __reduce_ex__(self, protocol):
+        return Order, tuple(self)
 
 
 class _Here(_Plan):
@@ -226,7 +234,7 @@ class ExpertExchange(_Here):
         if status:
             raise IwpError(status, "iwp_order")
         order = _Made(offsets, slots, rows)
-        order.made = (self, T, k, a.slots, a.offsets)
+        order.made = self, slots.shape, (slots.data_ptr(), a.offsets)
         return order
 
     def _begin(self, a: ExchangeArgs, order: Order, x, name: str):
@@ -234,16 +242,16 @@ class ExpertExchange(_Here):
         if x.dim() != 2:
             raise ValueError(f"{name} is a matrix")
         D = x.shape[1]
-        if type(order) is _Made and order.made[0] is self:
-            _, T, k, a.slots, a.offsets = order.made
-        else:
-            offsets, slots, _ = order
+        offsets, slots, _ = order
+        at = slots.data_ptr(), offsets.data_ptr()
+        # (an order's tensors can be resized, transposed or set to other memory after it was made)
+        if type(order) is not _Made or order.made != (self, slots.shape, at) or not slots.is_contiguous():
             if slots.dim() != 2:
                 raise ValueError("slots is a matrix")
             _vector(slots, "slots", slots.numel(), self._ids[1:], self.device)
             _vector(offsets, "offsets", self.experts + 1, self._ids[1:], self.device)
-            T, k = slots.shape
-            a.slots, a.offsets = slots.data_ptr(), offsets.data_ptr()
+        T, k = slots.shape
+        a.slots, a.offsets = at
         a.tokens, a.top_k, a.dim = T, k, D
         return T, k, D
 

@@ -1,0 +1,64 @@
+"""An exchange by orders that were remade or changed after the plan made them."""
+import copy
+
+import pytest
+import torch
+
+from paper_1901_01544_b200 import routing
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+T, E, K, D = 70, 9, 3, 40
+
+
+def setting():
+    g = torch.Generator(device=DEV)
+    g.manual_seed(5)
+    ex = routing.ExpertExchange(E)
+    ids = torch.stack([torch.randperm(E, generator=g, device=DEV)[:K] for _ in range(T)])
+    x, dy, z, w = (torch.randn(*s, generator=g, device=DEV) for s in ((T, D), (T, D), (T * K, D), (T, K)))
+    return ex, ex.order(ids), x, dy, z, w
+
+
+def calls(ex, o, x, dy, z, w):
+    return [ex.dispatch(x, o), ex.combine(z, o, w), *ex.combine_grad(dy, z, o, w), ex.dispatch_grad(z, o)]
+
+
+@pytest.mark.parametrize("remade", [lambda o: o._replace(), lambda o: type(o)(*o), copy.copy, copy.deepcopy,
+                                    lambda o: torch.utils._pytree.tree_map(torch.clone, o)])
+def test_remade_orders(remade):
+    ex, o, *rows = setting()
+    assert all(torch.equal(a, b) for a, b in zip(calls(ex, remade(o), *rows), calls(ex, o, *rows)))
+
+
+def test_pairs_dropped_from_an_order():
+    """Slots of -1 are nobody's: not read, not written, no gradient."""
+    ex, o, x, dy, z, w = setting()
+    drop = torch.rand(T, K, device=DEV) < 0.3
+    less = o._replace(slots=torch.where(drop, -1, o.slots))
+    keep, slots = ~drop, o.slots.long()
+    there = torch.full((T * K, D), 7.0, device=DEV)
+    want = there.clone()
+    want[slots[keep]] = x[:, None].expand(T, K, D)[keep]
+    assert torch.equal(ex.dispatch(x, less, out=there), want)
+    y = ex.combine(z, less, w).double()
+    parts = (w.double()[:, :, None] * z.double()[slots]).masked_fill(drop[:, :, None], 0)
+    # three terms, each sum rounded (2^-24 of what it may be at most)
+    assert ((y - parts.sum(1)).abs() <= 3 * 2.0**-24 * parts.abs().sum(1)).all()
+    dz, dw = ex.combine_grad(dy, z, less, w, out=there.clone())
+    want = there.clone()
+    want[slots[keep]] = (w[:, :, None] * dy[:, None])[keep]
+    assert torch.equal(dz, want) and (dw[drop] == 0).all()
+    products = dy.double()[:, None] * z.double()[slots]
+    assert ((dw.double() - products.sum(2)).abs()[keep] <= (D + 2) * 2.0**-24 * products.abs().sum(2)[keep]).all()
+
+
+def test_an_order_moved_in_memory():
+    ex, o, *rows = setting()
+    want = calls(ex, o, *rows)
+    kept = o.slots.clone(), o.offsets.clone()
+    o.slots.data, o.offsets.data = kept
+    assert all(torch.equal(a, b) for a, b in zip(calls(ex, o, *rows), want))
+    o.slots.resize_(T + 1, K)
+    with pytest.raises(ValueError):
+        ex.dispatch(rows[0], o)
