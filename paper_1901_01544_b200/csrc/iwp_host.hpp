@@ -32,14 +32,15 @@ inline int device() {
   return cudaGetDevice(&dev) == cudaSuccess && dev < MAX_DEVICES ? dev : -1;
 }
 
-// Shared memory above the default limit is opted in to once per kernel and device.
+// Shared memory above the default limit is opted in to once per kernel and device: `most` is what any of the kernel's calls may
+// need, the same in all of them, so that threads whose first calls meet set the same limit.
 template <class Kernel>
-cudaError_t allow_shared(Kernel kernel, int bytes, std::atomic<int>* allowed) {
+cudaError_t allow_shared(Kernel kernel, int most, std::atomic<bool>* allowed) {
   const int dev = device();
   if (dev < 0) return cudaErrorInvalidDevice;
-  if (bytes <= 48 * 1024 || bytes <= allowed[dev]) return cudaSuccess;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e == cudaSuccess) allowed[dev] = bytes;
+  if (most <= 48 * 1024 || allowed[dev]) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+  if (e == cudaSuccess) allowed[dev] = true;
   return e;
 }
 

@@ -250,7 +250,7 @@ extern "C" int iwp_order(const iwp_order_args* a, void* cuda_stream) {
   r.ids_bytes = a->ids_bytes;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const int smem = 4 * X::ORDER_WARPS * r.E;
-  static std::atomic<int> allowed[MAX_DEVICES] = {};
+  static std::atomic<bool> allowed[MAX_DEVICES] = {};
   LOSS_CUDA(allow_shared(X::k_order_place<4>, 4 * X::ORDER_WARPS * X::MAX_EXPERTS, allowed));
   if (blocks > 1) LOSS_CUDA(launch(X::k_order_count, blocks, X::ORDER_THREADS, 0, 1, st, r));
   LOSS_CUDA(launch(X::k_order_place<4>, blocks, X::ORDER_THREADS, smem, 1, st, r));

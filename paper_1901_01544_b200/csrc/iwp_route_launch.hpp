@@ -46,9 +46,10 @@ template <int TYPE, int M, int G, bool SCORES>
 int launch_route_form(const Args& r, int word, cudaStream_t st) {
   using namespace iwp_host;
   const int smem = shared_of(r.E, r.groups, G, M).bytes;
+  const int most = shared_of(std::min(MAX_EXPERTS, M * G), SCORES ? MAX_GROUPS : 1, G, M).bytes;
   const auto kernel = k_route<TYPE, M, G, SCORES>;
-  static std::atomic<int> allowed[MAX_DEVICES] = {};
-  LOSS_CUDA(allow_shared(kernel, smem, allowed));
+  static std::atomic<bool> allowed[MAX_DEVICES] = {};
+  LOSS_CUDA(allow_shared(kernel, most, allowed));
   const int64_t steps = tiles_of(r.T, THREADS / G);
   LOSS_CUDA(launch(kernel, std::max<int64_t>(1, std::min<int64_t>(steps, blocks_of(M, SCORES) * SMS)), THREADS, smem, 1, st, r, word));
   return IWP_OK;
