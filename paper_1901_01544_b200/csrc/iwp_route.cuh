@@ -307,7 +307,10 @@ static __device__ __noinline__ double exact_score(float x, float top, double sum
   return softmax ? y / sum : 1. / (1. + y);
 }
 
-// The sum of a row's exponentials below `top`, off by 2^-22 of itself at most (two units in the last place of expf).
+// The sum of a row's exponentials below `top`, off by 2^-21 of itself at most.  A term is off by two units in the last place of
+// expf, 4 2^-24, and by what the rounding of its argument is, half a unit in its last place: 2^-24 from 1 to 2 below the top, 2 2^-24
+// from 2 to 4, 4 2^-24 from 4 to 8 and so on.  The further down, the less a term counts: arguments add the most where 1023 of them are 4
+// below the top, 0.95 of the sum, and 7.8 2^-24 in all.
 template <int TYPE, int M, int G>
 __device__ __noinline__ double exact_sum(const typename Of<TYPE>::T* row, int g, int E, bool on, int word, float top) {
   float x[M];
@@ -318,6 +321,20 @@ __device__ __noinline__ double exact_sum(const typename Of<TYPE>::T* row, int g,
 #pragma unroll
   for (int o = G / 2; o; o /= 2) s += __shfl_xor_sync(ALL, s, o);
   return s;
+}
+
+// Whether the error of softmax's sum may hide the order of two groups' scores in 64 bits, whose biases follow them: it is common to all
+// scores, but not to the biases, so equal sums are so with equal biases alone.  (Two scores of a group are 2 largest at most.)
+template <int G>
+__device__ __noinline__ bool groups_too_close(const double* score, int groups, int g, float largest) {
+  bool close = false;
+  for (int q = g; q < groups; q += G)
+    for (int p = 0; p < groups; p++) {
+      const double mine = score[q], other = score[p];
+      if (other > -CUDART_INF && mine > -CUDART_INF && (other != mine || score[groups + p] != score[groups + q]))
+        close |= fabs(other - mine) <= 0x1p-20 * largest;
+    }
+  return close;
 }
 
 __device__ __forceinline__ void in_order(uint32_t& a, uint32_t& b) {
@@ -368,7 +385,7 @@ __device__ __forceinline__ uint32_t key_over(uint32_t x) {
 
 // Shared memory of a block of k_route: lanes' sorted keys and a zero behind them (no two of eight lanes share a bank), rows' choices
 // (key and lane), counts, a warp's choices made again, and where there are groups a row's keys in the order of the columns and
-// the bounds of its groups' scores.
+// the bounds of its groups' scores, or these in 64 bits with the biases in them.
 constexpr int WAITING = 12;
 struct Shared {
   int waiting, list, hist, pick, row, score, bytes;  // offsets
@@ -382,7 +399,7 @@ __host__ __device__ inline Shared shared_of(int E, int groups, int G, int M) {
   s.pick = s.hist + 4 * E;
   s.row = (s.pick + 4 * THREADS + 15) / 16 * 16;
   s.score = s.row + (groups > 1 ? 4 * rows * G * M : 0);
-  s.bytes = s.score + (groups > 1 ? 8 * rows * groups : 0);
+  s.bytes = s.score + (groups > 1 ? 16 * rows * groups : 0);
   return s;
 }
 
@@ -420,6 +437,15 @@ __device__ __forceinline__ void spread_keys(const uint32_t (&key)[M], uint32_t* 
       for (int v = 0; v < VEC; v++) to[v] = key[n * VEC + v];
     }
   }
+}
+
+// And back.
+template <int M, int G, int VEC>
+__device__ __forceinline__ void gather_keys(uint32_t (&key)[M], const uint32_t* keys, int g) {
+#pragma unroll
+  for (int n = 0; n < M / VEC; n++)
+#pragma unroll
+    for (int v = 0; v < VEC; v++) key[n * VEC + v] = keys[(n * G + g) * VEC + v];
 }
 
 // Lane g's keys in groups of `size` columns that are not open become 0.
@@ -575,7 +601,7 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
     if (SCORES && a.groups > 1) {
       const int size = a.E / a.groups;
       uint32_t* const keys = reinterpret_cast<uint32_t*>(smem + at.row) + rl * G * M;
-      float* const group_score = reinterpret_cast<float*>(smem + at.score) + rl * 2 * a.groups;  // the least it may be
+      float* const group_score = reinterpret_cast<float*>(smem + at.score) + rl * 4 * a.groups;  // the least it may be
       float* const group_high = group_score + a.groups;
       with_word<TYPE>(word, [&](auto v) { spread_keys<M, G, decltype(v)::value>(key, keys, g); });
       __syncwarp();
@@ -666,6 +692,7 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
             again |= question && out > NONE && !apart(unordered(in & ~LOW), unordered(out), tol);
           }
           exact[q] = score;
+          if (a.bias && some) exact[a.groups + q] = static_cast<double>(a.bias[e1]) + (two ? a.bias[e2] : 0.f);
         }
         __syncwarp();
         if (question) open = 0;
@@ -675,14 +702,14 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
           for (int p = 0; p < a.groups; p++) {
             const double other = exact[p];
             ahead += other > mine || (other == mine && p < q);
-            // (the error of softmax's sum is common to all scores, but not to the biases)
-            if (softmax && a.bias && question && other != mine && other > -CUDART_INF && mine > -CUDART_INF) again |= fabs(other - mine) <= 0x1p-20 * scale_of_row;
           }
           if (question && ahead < a.top_groups) open |= 1u << q;
         }
+        if (softmax && a.bias && question) again |= groups_too_close<G>(exact, a.groups, g, scale_of_row);
 #pragma unroll
         for (int o = G / 2; o; o /= 2) open |= __shfl_xor_sync(ALL, open, o);
         again = (__ballot_sync(ALL, again) & of_row) != 0;
+        with_word<TYPE>(word, [&](auto v) { gather_keys<M, G, decltype(v)::value>(key, keys, g); });  // (not kept in registers meanwhile)
       }
       with_word<TYPE>(word, [&](auto v) { close_groups<M, G, decltype(v)::value>(key, open, size, a.groups, g); });
       __syncwarp();
@@ -747,13 +774,19 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
         for (int i = 0; i < n; i++) {
           const double other = __shfl_sync(ALL, i < G ? value[0] : value[1], row0 + (i & (G - 1)));
           const int its = __shfl_sync(ALL, i < G ? expert[0] : expert[1], row0 + (i & (G - 1)));
-          const float its_bias = __shfl_sync(ALL, i < G ? bias[0] : bias[1], row0 + (i & (G - 1)));
 #pragma unroll
           for (int u = 0; u < 2; u++) {
             rank[u] += other > value[u] || (other == value[u] && its < expert[u]);
-            // (the error of softmax's sum is common to all scores, but not to the biases)
-            if (exact && softmax && other != value[u] && its < MAX_EXPERTS && expert[u] < MAX_EXPERTS)
-              again |= fabs(other - value[u]) <= 0x1p-21 * fabs((other - its_bias) - (value[u] - bias[u]));
+          }
+        }
+        if (exact && softmax) {
+          // the error of softmax's sum is common to all scores, but not to the biases, which may even make values equal that are not
+          for (int i = 0; i < n; i++) {
+            const double other = __shfl_sync(ALL, i < G ? value[0] : value[1], row0 + (i & (G - 1)));
+            const float its_bias = __shfl_sync(ALL, i < G ? bias[0] : bias[1], row0 + (i & (G - 1)));
+#pragma unroll
+            for (int u = 0; u < 2; u++)
+              again |= fabs(other - value[u]) < 0x1p-21 * fabs((other - its_bias) - (value[u] - bias[u]));
           }
         }
         __syncwarp();
