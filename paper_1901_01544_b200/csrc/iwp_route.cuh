@@ -730,8 +730,8 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
         head = behind == waiting + 9 ? 0 : *behind++;
       }
     };
-    const int picks = LOSSLESS ? a.k : a.k + 1;
-    for (int j = 0; j < picks; j++) take(j);
+    int taken = LOSSLESS ? a.k : a.k + 1;
+    for (int j = 0; j < taken; j++) take(j);
     __syncwarp();
     auto listed = [&](int j) {  // (key, expert)
       const uint2 p = list[j];
@@ -746,12 +746,12 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
       const bool question = e >= 0 && !bad && close(mine.x, list[g + 1].x);
       if (__any_sync(ALL, question)) {
         // all that may be as good as the k-th, up to two per lane, in order of what the codes stand for
-        int n = picks;
-        auto more = [&] { return on && !bad && close(list[a.k - 1].x, list[n - 1].x); };
-        while (n < 2 * G && __any_sync(ALL, more())) {
-          take(n++);
+        auto more = [&] { return on && !bad && close(list[a.k - 1].x, list[taken - 1].x); };
+        while (taken < 2 * G && __any_sync(ALL, more())) {
+          take(taken++);
           __syncwarp();
         }
+        const int n = taken;
         again |= more();
         const bool exact = SCORES && a.bias;
         const double sum = exact && softmax ? exact_sum<TYPE, M, G>(row, g, a.E, on, word, top) : 1.;
@@ -799,7 +799,8 @@ __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const _
     }
     float y = e >= 0 ? static_cast<float>(row[e]) : -CUDART_INF_F;
     if (!LOSSLESS || M > 8) {
-      if (M > 8) again |= behind == waiting + 9;  // there may have been more in this lane
+      // all eight of this lane's keys were taken, and then others: there may have been more here
+      if (M > 8 && behind == waiting + 9) again |= list[taken - 1].x != waiting[7] || list[taken - 1].y != g;
       unsigned todo = __ballot_sync(ALL, again && on && !bad);
       while (todo) {
         const int who = __ffs(todo) - 1, who0 = who & ~(G - 1);

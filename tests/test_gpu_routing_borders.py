@@ -60,3 +60,70 @@ def test_many_equal_logits_below_the_top(far, groups):
         bias[at] = 0.0
         kw = dict(groups=groups, top_groups=max(1, groups // 2))
         check_route(routing.ExpertRouter(E, k, **kw), x, bias, **kw)
+
+
+def spread(E, word, lanes, columns):
+    """`columns` columns of one lane, where words of `word` neighbours go to the lanes in turn."""
+    e = torch.arange(E, device=DEV)
+    mine = e[e // word % lanes == lanes // 3]
+    assert len(mine) >= columns
+    return mine[:columns]
+
+
+@pytest.mark.parametrize("word", [1, 2, 4, 8])
+@pytest.mark.parametrize("lanes", [8, 16])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("k", [7, 8, 9, 10, 13])
+def test_the_best_of_a_row_side_by_side(k, dtype, lanes, word):
+    """Up to 16 largest logits in what one lane may hold, which sorts only eight; equal ones among them, and rows with nothing else
+    to choose.  (The words are the widest that the number of experts allows.)"""
+    E = {1: 249, 2: 250, 4: 252, 8: 256}[word]
+    for best in (7, 8, 9, 12):
+        at = spread(E, word, lanes, min(best, E // (word * lanes) * word))
+        g = torch.Generator(device=DEV).manual_seed(best)
+        x = torch.randn(6, E, generator=g, device=DEV).to(dtype)
+        x[:4, at] += 20
+        x[1, at] = 16.0
+        x[2, at[::2]] = 24.0
+        x[3] = torch.where(torch.isin(torch.arange(E, device=DEV), at), x[3].double(), -math.inf).to(dtype)
+        x[4] = 0.0
+        for kw in (dict(), dict(score="sigmoid", renormalize=False)):
+            plan = routing.ExpertRouter(E, k, **kw)
+            check_route(plan, x, **kw)
+            check_route(plan, x, 0.01 * torch.randn(E, generator=g, device=DEV), **kw)
+            check_route(plan, x, torch.zeros(E, device=DEV), **kw)
+
+
+def times(calls, reps=20):
+    """Of replays of captured calls, in turn, the shortest of each in ms."""
+    graphs = []
+    for f in calls:
+        f()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            for _ in range(8):
+                f()
+        graphs.append(g)
+    best = [math.inf] * len(graphs)
+    for _ in range(reps):
+        for i, g in enumerate(graphs):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            g.replay()
+            b.record()
+            b.synchronize()
+            best[i] = min(best[i], a.elapsed_time(b))
+    return best
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_equal_logits_take_no_longer(dtype):
+    """Rows of equal 16-bit logits (a router before its first step, padding) need no second look: their first eight experts are what one
+    lane has.  (With one, each row by a whole warp, it was five to six times as long.)"""
+    T, E, k = 65536, 256, 8
+    plan = routing.ExpertRouter(E, k)
+    equal, random = torch.zeros(T, E, device=DEV, dtype=dtype), torch.randn(T, E, device=DEV).to(dtype)
+    ids = plan.route(equal).ids
+    assert torch.equal(ids, torch.arange(k, device=DEV, dtype=torch.int32).expand(T, k))
+    slow, usual = times([lambda: plan.route(equal), lambda: plan.route(random)])
+    assert slow < 2 * usual, (slow, usual)
