@@ -431,7 +431,7 @@ def _once():
 
             @staticmethod
             def backward(ctx, *_):
-                raise RuntimeError("the losses' gradients cannot be differentiated again")
+                raise RuntimeError("these gradients come from kernels and cannot be differentiated again")
 
         _refuses = Once
     return _refuses

@@ -107,3 +107,22 @@ def test_an_order_that_no_longer_fits_is_refused():
             p._begin(a, o._replace(**bad), x, "x")
     with pytest.raises(TypeError):
         p._begin(a, o._replace(slots=o.slots.long()), x, "x")
+
+
+class Rows:
+    """A plan whose exchange leaves rows where they are."""
+
+    def dispatch(self, x, order):
+        return x.clone()
+
+    def dispatch_grad(self, dout, order):
+        return dout.clone()
+
+
+def test_the_refusal_of_a_second_derivative_names_no_other_operator():
+    x = torch.ones(T, D, requires_grad=True)
+    o = routing.Order(*(torch.zeros(1, dtype=torch.int32) for _ in range(3)))
+    (dx,) = torch.autograd.grad(routing.dispatch(Rows(), x, o).square().sum(), [x], create_graph=True)
+    with pytest.raises(RuntimeError, match="cannot be differentiated again") as refused:
+        dx.sum().backward()
+    assert "loss" not in str(refused.value)
