@@ -62,3 +62,22 @@ def test_an_order_moved_in_memory():
     o.slots.resize_(T + 1, K)
     with pytest.raises(ValueError):
         ex.dispatch(rows[0], o)
+
+
+@pytest.mark.parametrize("E", [8, 128, 1000])
+@pytest.mark.parametrize("pairs", [4095, 4096, 4097, 4110, 6144, 6147, 8190, 8193])
+def test_orders_about_where_more_blocks_take_part(pairs, E):
+    """One pair per token, three, and ids that belong to nobody; slots are those of a stable sort."""
+    for k in (1, 3):
+        ids = torch.randint(-1, E + 1, (pairs // k, k), generator=torch.Generator(device=DEV).manual_seed(pairs), device=DEV)
+        o = routing.ExpertExchange(E).order(ids)
+        flat = ids.flatten()
+        mine = (flat >= 0) & (flat < E)
+        by_slot = torch.sort(torch.where(mine, flat, E), stable=True).indices[: int(mine.sum())]
+        slots = torch.full_like(flat, -1)
+        slots[by_slot] = torch.arange(len(by_slot), device=DEV)
+        rows = torch.full_like(flat, -1)
+        rows[: len(by_slot)] = by_slot // k
+        counts = torch.bincount(flat[mine], minlength=E)
+        assert torch.equal(o.slots.flatten().long(), slots) and torch.equal(o.rows.long(), rows)
+        assert torch.equal(o.offsets.long(), torch.cat([counts.new_zeros(1), counts.cumsum(0)]))
