@@ -20,9 +20,18 @@ constexpr int64_t MAX_WARPS = int64_t(4) * SMS * K::WARPS;
 constexpr int MAX_CLUSTER = 16;
 // A part costs a warp as much time as this many elements more: its description and its first elements are waited for.
 constexpr int64_t PART_COST = 1024;
-// Up to this cost one cluster serves, in one launch.
+// Up to this cost one cluster serves, in one launch, which takes the host 2 us less.  (One launch and two, fp32 elements in one tensor, in a
+// loop of calls and in a graph: 100000 8.2 and 10.3, 6.2 and 5.8 us; 300000 8.6 and 10.3, 8.1 and 5.7; 500000 9.2 and 10.3, 8.9 and 6.0; 600000 9.9
+// and 10.4, 9.5 and 6.1; 1.2 million 11.3 and 10.4, 10.8 and 7.0.)
 constexpr int64_t SMALL_COST = int64_t(1) << 19;
 constexpr int64_t SMALL_WARPS = MAX_CLUSTER * (K::SMALL_THREADS / 32);
+
+// The sums of a single group, and of up to FEW_GROUPS that FEW_WARPS leave (of some 4 million elements), are added up by the last block
+// of the squares' launch, about 1 us a group; else by a launch of its own, 2 us on the host.  (Clipping in a loop of calls, the one and the
+// other: 25 million elements in 1 group 26 and 32 us, in 2 30 and 28, in 8 35 and 26; 4.2 million in 1 group 11.4 and 12.5, in 2 12.6 and 12.6, in 8
+// 16.9 and 12.7; 3.5 million in 2 10.6 and 12.5, in 8 15.6 and 12.5; 2 million in 2 10.5 and 12.7, in 8 12.7 and 12.8, in 12 16.2 and 12.7.)
+constexpr int FEW_GROUPS = 8;
+constexpr int64_t FEW_WARPS = 2560;
 
 int size_of(int type) { return type == IWP_F32 ? 4 : 2; }
 bool is_type(int type) { return type == IWP_F32 || type == IWP_BF16 || type == IWP_F16; }
@@ -198,6 +207,7 @@ extern "C" int iwp_clip(const iwp_clip_args* a, void* cuda_stream) {
   r.max_norm = a->max_norm;
   r.scale = a->scale;
   r.groups = a->groups;
+  r.join = a->groups == 1 || (a->groups <= FEW_GROUPS && warps <= FEW_WARPS);
   r.write = a->write != 0;
   r.have_squares = a->have_squares != 0;
   r.drop = a->drop_nonfinite != 0;
@@ -228,7 +238,7 @@ extern "C" int iwp_clip(const iwp_clip_args* a, void* cuda_stream) {
   }
   const int64_t blocks = std::max<int64_t>(1, tiles_of(warps, K::WARPS));
   if (!a->have_squares) LOSS_CUDA(launch(K::k_squares, blocks, K::THREADS, 0, 1, st, r));
-  if (a->have_squares || a->groups > K::FEW_GROUPS)
+  if (a->have_squares || !r.join)
     LOSS_CUDA(launch(K::k_groups, std::min<int64_t>(tiles_of(a->groups, K::WARPS), 8 * SMS), K::THREADS, 0, 1, st, r));
   if (a->write && warps) LOSS_CUDA(launch(K::k_scale, blocks, K::THREADS, 0, 1, st, r));
   return IWP_OK;

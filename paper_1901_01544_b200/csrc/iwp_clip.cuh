@@ -55,6 +55,7 @@ struct Args {
   float* factors;
   double max_norm, scale;
   int warps, groups, write, have_squares, drop;
+  int join;  // k_squares adds up the groups' sums
 };
 
 template <int TYPE>
@@ -330,17 +331,14 @@ __device__ __forceinline__ void finish_group(const Args& a, int group, double sq
 // 15 in bf16 with one, of which the chain of a block's start, its sum, the ticket and the last block's sum is 5.  (Parts of 16384
 // elements dealt out: 359 us, for the last round of them.)
 //
-// Few groups: the last block to finish adds up the warps' sums (up to FEW_GROUPS).  Many: a launch of
-// its own, a warp per group.
-constexpr int FEW_GROUPS = 8;
-
+// Few groups: the last block to finish adds up the warps' sums (`join`).  Many: a launch of its own, a warp per group.
 __global__ void __launch_bounds__(THREADS, 4) k_squares(const Args a) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   wait_previous();
   launch_next();  // after the wait: k_scale may read the table while this kernel runs
   const int w = blockIdx.x * WARPS + warp;
   if (w < a.warps) square_range(a, w, lane);
-  if (a.groups > FEW_GROUPS) return;
+  if (!a.join) return;
   __shared__ bool last;
   __threadfence();
   __syncthreads();
@@ -400,8 +398,7 @@ __global__ void __launch_bounds__(THREADS, 4) k_scale(const Args a) {
     wait_previous();
 }
 
-// All of it in one launch of one cluster, for little work: a launch less on the host (3 us), up to 300000 elements in about the time
-// of two (10 us).
+// All of it in one launch of one cluster, for little work.
 __global__ void __launch_bounds__(SMALL_THREADS) k_small(const Args a) {
   const int lane = threadIdx.x & 31, warps = gridDim.x * (SMALL_THREADS / 32);
   const int warp = (threadIdx.x >> 5) * gridDim.x + blockIdx.x;  // neighbouring ranges in different CTAs
