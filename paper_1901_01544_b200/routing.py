@@ -86,11 +86,14 @@ class Order(NamedTuple):
     rows: object
 
 
-class _Made(Order):
-    """An order as a plan has made it: the plan, the shape of the slots, and where slots and offsets are.  What is made of it
-    (`_replace`, copies) is an order like any other."""
+_UNKNOWN = (None,) * 6
 
-    made = None
+
+class _Made(Order):
+    """An order as a plan has made it: the plan, tokens and choices, the shape of the slots, and where slots and offsets are.  What is
+    made of it (`_replace`, copies) is an order like any other."""
+
+    made = _UNKNOWN
 
     @classmethod
     def _make(cls, tensors):
@@ -103,10 +106,15 @@ class _Made(Order):
 class _Here(_Plan):
     """A plan whose calls are refused while another device than its own is current."""
 
+    def __init__(self):
+        super().__init__()
+        self._current = self._torch._C._cuda_getDevice
+
     def _stream(self) -> int:
-        if self._torch._C._cuda_getDevice() != self._index:
+        if self._current() != self._index:
             raise ValueError(f"the plan is on {self.device}, which is not the current device")
-        return super()._stream()
+        s = self._raw_stream(self._index)
+        return s if s == self._last else super()._stream()
 
 
 class ExpertRouter(_Here):
@@ -218,12 +226,13 @@ class ExpertExchange(_Here):
         t, dev, a = self._torch, self.device, self._order_args
         if ids.dim() != 2:
             raise ValueError("ids is a matrix")
-        T, k = ids.shape
-        a.ids_ld = _rows_of(ids, "ids", (T, k), self._ids, dev)
+        T, k = shape = ids.shape
+        a.ids_ld = _rows_of(ids, "ids", shape, self._ids, dev)
         a.tokens, a.top_k, a.ids, a.ids_bytes = T, k, ids.data_ptr() or 256, ids.element_size()
         offsets = t.empty(self.experts + 1, dtype=t.int32, device=dev)
         slots, rows = t.empty(T, k, dtype=t.int32, device=dev), t.empty(T * k, dtype=t.int32, device=dev)
-        a.offsets, a.slots, a.rows = offsets.data_ptr(), slots.data_ptr() or 256, rows.data_ptr() or 256
+        offsets_at, at = offsets.data_ptr(), slots.data_ptr()
+        a.offsets, a.slots, a.rows = offsets_at, at or 256, rows.data_ptr() or 256
         stream = self._stream()
         if self._capturing():
             self._captured = True
@@ -234,25 +243,26 @@ class ExpertExchange(_Here):
         if status:
             raise IwpError(status, "iwp_order")
         order = _Made(offsets, slots, rows)
-        order.made = self, slots.shape, (slots.data_ptr(), a.offsets)
+        order.made = self, T, k, shape, at, offsets_at
         return order
 
     def _begin(self, a: ExchangeArgs, order: Order, x, name: str):
         """T, k and the width of x, a matrix, in an exchange by `order`."""
-        if x.dim() != 2:
+        shape = x.shape
+        if len(shape) != 2:
             raise ValueError(f"{name} is a matrix")
-        D = x.shape[1]
         offsets, slots, _ = order
-        at = slots.data_ptr(), offsets.data_ptr()
+        plan, T, k, of, at, offsets_at = order.made if type(order) is _Made else _UNKNOWN
         # (an order's tensors can be resized, transposed or set to other memory after it was made)
-        if type(order) is not _Made or order.made != (self, slots.shape, at) or not slots.is_contiguous():
+        if plan is not self or slots.data_ptr() != at or offsets.data_ptr() != offsets_at or slots.shape != of or not slots.is_contiguous():
             if slots.dim() != 2:
                 raise ValueError("slots is a matrix")
             _vector(slots, "slots", slots.numel(), self._ids[1:], self.device)
             _vector(offsets, "offsets", self.experts + 1, self._ids[1:], self.device)
-        T, k = slots.shape
-        a.slots, a.offsets = at
-        a.tokens, a.top_k, a.dim = T, k, D
+            T, k = slots.shape
+            at, offsets_at = slots.data_ptr(), offsets.data_ptr()
+        D = shape[1]
+        a.slots, a.offsets, a.tokens, a.top_k, a.dim = at, offsets_at, T, k, D
         return T, k, D
 
     def _end(self, a: ExchangeArgs, at: int, call, entry: str) -> None:

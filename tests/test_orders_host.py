@@ -75,7 +75,7 @@ def test_a_remade_order_does_not_hold_its_plan():
     p = plan()
     for how in REMADE.values():
         remade = how(order(p))
-        assert all(v is not p for v in getattr(remade, "__dict__", {}).values()) and not getattr(remade, "made", None)
+        assert p not in getattr(remade, "made", ())
 
 
 def test_an_order_whose_tensors_have_moved_is_taken_where_they_are():
