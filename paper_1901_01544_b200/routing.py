@@ -103,6 +103,12 @@ class _Made(Order):
         return Order, tuple(self)
 
 
+def _made(tensors, made) -> _Made:
+    order = _Made(*tensors)
+    order.made = made
+    return order
+
+
 class _Here(_Plan):
     """A plan whose calls are refused while another device than its own is current."""
 
@@ -242,17 +248,16 @@ class ExpertExchange(_Here):
         status = self._lib.iwp_order(self._order_at, stream)
         if status:
             raise IwpError(status, "iwp_order")
-        order = _Made(offsets, slots, rows)
-        order.made = self, T, k, shape, at, offsets_at
-        return order
+        return _made((offsets, slots, rows), (self, T, k, shape, at, offsets_at))
 
     def _begin(self, a: ExchangeArgs, order: Order, x, name: str):
-        """T, k and the width of x, a matrix, in an exchange by `order`."""
+        """T, k and the width of x, a matrix, in an exchange by `order`, and what makes a matrix that its slots are written to."""
         shape = x.shape
         if len(shape) != 2:
             raise ValueError(f"{name} is a matrix")
         offsets, slots, _ = order
         plan, T, k, of, at, offsets_at = order.made if type(order) is _Made else _UNKNOWN
+        new = self._torch.empty
         # (an order's tensors can be resized, transposed or set to other memory after it was made)
         if plan is not self or slots.data_ptr() != at or offsets.data_ptr() != offsets_at or slots.shape != of or not slots.is_contiguous():
             if slots.dim() != 2:
@@ -261,9 +266,10 @@ class ExpertExchange(_Here):
             _vector(offsets, "offsets", self.experts + 1, self._ids[1:], self.device)
             T, k = slots.shape
             at, offsets_at = slots.data_ptr(), offsets.data_ptr()
+            new = self._torch.zeros  # (there may be slots that no pair has)
         D = shape[1]
         a.slots, a.offsets, a.tokens, a.top_k, a.dim = at, offsets_at, T, k, D
-        return T, k, D
+        return T, k, D, new
 
     def _end(self, a: ExchangeArgs, at: int, call, entry: str) -> None:
         if a.tokens == 0 or a.dim == 0:
@@ -273,13 +279,14 @@ class ExpertExchange(_Here):
             raise IwpError(status, entry)
 
     def dispatch(self, x, order: Order, *, out=None):
-        """Rows [T k, D] in the order of the slots: x [T, D] of each slot's token; zero behind the last slot."""
+        """Rows [T k, D] in the order of the slots: x [T, D] of each slot's token; zero behind the last slot, and where pairs were
+        dropped from an order (slots set to -1), but for rows of `out` below the last slot, which are left as they are."""
         a, at, call = self._dispatch
-        T, k, D = self._begin(a, order, x, "x")
+        T, k, D, new = self._begin(a, order, x, "x")
         a.by_token_ld = _rows_of(x, "x", (T, D), self._floats, self.device)
         a.by_token, a.type = x.data_ptr(), self._codes[x.dtype]
         if out is None:
-            out = self._torch.empty(T * k, D, dtype=x.dtype, device=self.device)
+            out = new(T * k, D, dtype=x.dtype, device=self.device)
             a.by_slot_out_ld = D
         else:
             a.by_slot_out_ld = _rows_of(out, "out", (T * k, D), (x.dtype,), self.device)
@@ -290,7 +297,7 @@ class ExpertExchange(_Here):
     def combine(self, z, order: Order, weights=None, *, out=None):
         """Rows [T, D]: the sum of each token's rows of z [T k, D], times weights [T, k] float32 (1 if None)."""
         a, at, call = self._combine
-        T, k, D = self._begin(a, order, z, "z")
+        T, k, D, _ = self._begin(a, order, z, "z")
         a.by_slot_ld = _rows_of(z, "z", (T * k, D), self._floats, self.device)
         a.by_slot, a.type = z.data_ptr(), self._codes[z.dtype]
         if weights is None:
@@ -312,9 +319,10 @@ class ExpertExchange(_Here):
         return self.combine(dout, order, None, out=out)
 
     def combine_grad(self, dy, z, order: Order, weights=None, *, out=None, want=("rows", "weights")):
-        """The gradients ([T k, D] to z, [T, k] float32 to the weights) of `combine`; None where `want` leaves one out."""
+        """The gradients ([T k, D] to z, [T, k] float32 to the weights) of `combine`; None where `want` leaves one out.  Rows of
+        dropped pairs as in `dispatch`."""
         a, at, call = self._combine_grad
-        T, k, D = self._begin(a, order, dy, "dy")
+        T, k, D, new = self._begin(a, order, dy, "dy")
         a.by_token_ld = _rows_of(dy, "dy", (T, D), self._floats, self.device)
         a.by_token, a.type = dy.data_ptr(), self._codes[dy.dtype]
         if weights is None:
@@ -325,7 +333,7 @@ class ExpertExchange(_Here):
         dz = dw = a.by_slot = a.by_slot_out = a.dweights = None
         if "rows" in want:
             if out is None:
-                dz = self._torch.empty(T * k, D, dtype=dy.dtype, device=self.device)
+                dz = new(T * k, D, dtype=dy.dtype, device=self.device)
                 a.by_slot_out_ld = D
             else:
                 dz = out
@@ -370,19 +378,19 @@ def _functions():
         class Dispatch(torch.autograd.Function):
             @staticmethod
             def forward(ctx, x, plan, order):
-                ctx.plan = plan
+                ctx.plan, ctx.made = plan, getattr(order, "made", _UNKNOWN)
                 ctx.save_for_backward(*order)
                 return plan.dispatch(x, order)
 
             @staticmethod
             def backward(ctx, dout):
-                order = Order(*ctx.saved_tensors)
+                order = _made(ctx.saved_tensors, ctx.made)
                 return Once.apply(lambda: ctx.plan.dispatch_grad(dout.contiguous(), order), dout), None, None
 
         class Combine(torch.autograd.Function):
             @staticmethod
             def forward(ctx, z, weights, plan, order):
-                ctx.plan = plan
+                ctx.plan, ctx.made = plan, getattr(order, "made", _UNKNOWN)
                 ctx.save_for_backward(z, weights, *order)
                 return plan.combine(z, order, weights)
 
@@ -390,7 +398,8 @@ def _functions():
             def backward(ctx, dy):
                 z, weights, *order = ctx.saved_tensors
                 want = tuple(n for n, need in zip(("rows", "weights"), ctx.needs_input_grad) if need)
-                make = lambda: ctx.plan.combine_grad(dy.contiguous(), z, Order(*order), weights, want=want)  # noqa: E731
+                order = _made(order, ctx.made)
+                make = lambda: ctx.plan.combine_grad(dy.contiguous(), z, order, weights, want=want)  # noqa: E731
                 return *Once.apply(make, z, weights, dy), None, None
 
         _autograd = (Routing, Dispatch, Combine)

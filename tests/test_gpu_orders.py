@@ -49,6 +49,16 @@ def test_pairs_dropped_from_an_order():
     want = there.clone()
     want[slots[keep]] = (w[:, :, None] * dy[:, None])[keep]
     assert torch.equal(dz, want) and (dw[drop] == 0).all()
+    # without an output they are written to, zero
+    want = torch.zeros(T * K, D, device=DEV)
+    want[slots[keep]] = (w[:, :, None] * dy[:, None])[keep]
+    held = torch.full((T * K, D), float("nan"), device=DEV)
+    del held  # (what the next allocation may find)
+    assert torch.equal(ex.combine_grad(dy, z, less, w, want=("rows",))[0], want)
+    want[slots[keep]] = x[:, None].expand(T, K, D)[keep]
+    held = torch.full((T * K, D), float("nan"), device=DEV)
+    del held
+    assert torch.equal(ex.dispatch(x, less), want)
     products = dy.double()[:, None] * z.double()[slots]
     assert ((dw.double() - products.sum(2)).abs()[keep] <= (D + 2) * 2.0**-24 * products.abs().sum(2)[keep]).all()
 
@@ -81,3 +91,26 @@ def test_orders_about_where_more_blocks_take_part(pairs, E):
         counts = torch.bincount(flat[mine], minlength=E)
         assert torch.equal(o.slots.flatten().long(), slots) and torch.equal(o.rows.long(), rows)
         assert torch.equal(o.offsets.long(), torch.cat([counts.new_zeros(1), counts.cumsum(0)]))
+
+
+def test_gradients_with_pairs_dropped():
+    """The differentiable forms by an order that pairs were dropped from: nothing of what memory held reaches a gradient."""
+    ex, o, x, dy, z, w = setting()
+    drop = torch.rand(T, K, device=DEV) < 0.3
+    less = o._replace(slots=torch.where(drop, -1, o.slots))
+    x, w = x.requires_grad_(), w.requires_grad_()
+    gain = torch.randn(T * K, D, device=DEV).requires_grad_()
+    held = [torch.full((T * K, D), float("nan"), device=DEV) for _ in range(4)]
+    del held
+    y = routing.combine(ex, routing.dispatch(ex, x, less) * gain, less, w)
+    got = torch.autograd.grad(y, [x, w, gain], dy)
+    x64, w64, g64 = (v.detach().double().requires_grad_() for v in (x, w, gain))
+    want = (w64.masked_fill(drop, 0)[:, :, None] * g64[o.slots.long()] * x64[:, None]).sum(1)
+    ref = torch.autograd.grad(want, [x64, w64, g64], dy.double())
+    # roundings of 2^-24: two products and a sum of three terms, a product and a sum of D products, two products
+    w0, d0 = w64.detach().abs().masked_fill(drop, 0)[:, :, None], dy.double().abs()[:, None]
+    g0, x0 = g64.detach().abs()[o.slots.long()], x64.detach().abs()[:, None]
+    size = ((w0 * d0 * g0).sum(1), (d0 * g0 * x0).sum(2), torch.zeros(T * K, D, device=DEV).double().index_copy_(0, o.slots.flatten().long(), (w0 * d0 * x0).flatten(0, 1)))
+    for a, b, n, bound in zip(got, ref, (6, D + 3, 3), size):
+        assert ((a.double() - b).abs() <= n * 2.0**-24 * bound).all()
+    assert torch.equal(got[1] == 0, drop)
