@@ -86,12 +86,12 @@ class Order(NamedTuple):
     rows: object
 
 
-_UNKNOWN = (None,) * 6
+_UNKNOWN = (None,) * 7
 
 
 class _Made(Order):
-    """An order as a plan has made it: the plan, tokens and choices, the shape of the slots, and where slots and offsets are.  What is
-    made of it (`_replace`, copies) is an order like any other."""
+    """An order as a plan has made it: the plan, tokens and choices, the shape of the slots, where slots and offsets are, and the
+    slots' version (None in inference mode).  What is made of it (`_replace`, copies) is an order like any other."""
 
     made = _UNKNOWN
 
@@ -248,7 +248,7 @@ class ExpertExchange(_Here):
         status = self._lib.iwp_order(self._order_at, stream)
         if status:
             raise IwpError(status, "iwp_order")
-        return _made((offsets, slots, rows), (self, T, k, shape, at, offsets_at))
+        return _made((offsets, slots, rows), (self, T, k, shape, at, offsets_at, None if slots.is_inference() else slots._version))
 
     def _begin(self, a: ExchangeArgs, order: Order, x, name: str):
         """T, k and the width of x, a matrix, in an exchange by `order`, and what makes a matrix that its slots are written to."""
@@ -256,10 +256,11 @@ class ExpertExchange(_Here):
         if len(shape) != 2:
             raise ValueError(f"{name} is a matrix")
         offsets, slots, _ = order
-        plan, T, k, of, at, offsets_at = order.made if type(order) is _Made else _UNKNOWN
+        plan, T, k, of, at, offsets_at, version = order.made if type(order) is _Made else _UNKNOWN
         new = self._torch.empty
-        # (an order's tensors can be resized, transposed or set to other memory after it was made)
-        if plan is not self or slots.data_ptr() != at or offsets.data_ptr() != offsets_at or slots.shape != of or not slots.is_contiguous():
+        # (an order's tensors can be written to, resized, transposed or set to other memory after it was made)
+        if (plan is not self or slots.data_ptr() != at or offsets.data_ptr() != offsets_at or slots.shape != of or not slots.is_contiguous()
+                or (version is not None and slots._version != version)):
             if slots.dim() != 2:
                 raise ValueError("slots is a matrix")
             _vector(slots, "slots", slots.numel(), self._ids[1:], self.device)
@@ -280,7 +281,8 @@ class ExpertExchange(_Here):
 
     def dispatch(self, x, order: Order, *, out=None):
         """Rows [T k, D] in the order of the slots: x [T, D] of each slot's token; zero behind the last slot, and where pairs were
-        dropped from an order (slots set to -1), but for rows of `out` below the last slot, which are left as they are."""
+        dropped from an order (slots set to -1, not in place in inference mode), but for rows of `out` below the last slot, which are
+        left as they are."""
         a, at, call = self._dispatch
         T, k, D, new = self._begin(a, order, x, "x")
         a.by_token_ld = _rows_of(x, "x", (T, D), self._floats, self.device)

@@ -114,3 +114,19 @@ def test_gradients_with_pairs_dropped():
     for a, b, n, bound in zip(got, ref, (6, D + 3, 3), size):
         assert ((a.double() - b).abs() <= n * 2.0**-24 * bound).all()
     assert torch.equal(got[1] == 0, drop)
+
+
+@pytest.mark.parametrize("inference", [False, True])
+def test_pairs_dropped_in_place(inference):
+    with torch.inference_mode(inference):
+        ex, o, x, *_ = setting()
+        whole = ex.dispatch(x, o)
+        drop = torch.rand(T, K, device=DEV) < 0.3
+        slots = o.slots.long()
+        less = o if not inference else o._replace(slots=o.slots.clone())
+        less.slots.masked_fill_(drop, -1)
+        held = torch.full((T * K, D), float("nan"), device=DEV)
+        del held
+        want = whole.clone()
+        want[slots[drop]] = 0
+        assert torch.equal(ex.dispatch(x, less), want)

@@ -32,7 +32,8 @@ def plan():
 
 def order(p):
     o = p.order(torch.zeros(T, K, dtype=torch.int32))
-    o.offsets.zero_(), o.slots.copy_(torch.arange(T * K).view(T, K)), o.rows.zero_()
+    with torch.no_grad():
+        o.offsets.data.zero_(), o.slots.data.copy_(torch.arange(T * K).view(T, K)), o.rows.data.zero_()
     return o
 
 
@@ -126,3 +127,35 @@ def test_the_refusal_of_a_second_derivative_names_no_other_operator():
     with pytest.raises(RuntimeError, match="cannot be differentiated again") as refused:
         dx.sum().backward()
     assert "loss" not in str(refused.value)
+
+
+def test_what_is_written_to_is_looked_at_again():
+    """Slots that no pair has any more are made zero; a plan's own order, in inference mode too, has none."""
+    p = plan()
+    a, x = routing.ExchangeArgs(), torch.zeros(T, D)
+    for inference in (False, True):
+        with torch.inference_mode(inference):
+            o = p.order(torch.zeros(T, K, dtype=torch.int32))
+            assert p._begin(a, o, x, "x")[3] is torch.empty
+            assert p._begin(a, o._replace(slots=o.slots.clone()), x, "x")[3] is torch.zeros
+            assert p._begin(a, routing.Order(*o), x, "x")[3] is torch.zeros
+            if not inference:
+                o.slots[0, 0] = -1
+                assert p._begin(a, o, x, "x")[3] is torch.zeros
+
+
+def test_a_backward_pass_knows_its_plans_order():
+    p = plan()
+    seen = []
+    p.dispatch = lambda x, o: x.clone()
+
+    def dispatch_grad(dout, o):
+        seen.append(p._begin(routing.ExchangeArgs(), o, dout, "dout")[3])
+        return dout.clone()
+
+    p.dispatch_grad = dispatch_grad
+    x = torch.ones(T, D, requires_grad=True)
+    routing.dispatch(p, x, order(p)).sum().backward()
+    o = order(p)
+    routing.dispatch(p, x, o._replace(slots=o.slots.clone())).sum().backward()
+    assert seen == [torch.empty, torch.zeros]
