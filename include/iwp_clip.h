@@ -32,7 +32,7 @@ typedef struct iwp_clip_sizes {
   int64_t table_bytes;             /* of the table, 16-byte aligned on the device */
   int64_t workspace_bytes;         /* of every call's workspace */
   int64_t parts, warps;            /* for iwp_clip_args */
-  int64_t range;                   /* work of a warp, for iwp_clip_table() */
+  int64_t range;                   /* work of a warp, for information: iwp_clip_table() shares the work out again */
 } iwp_clip_sizes;
 
 /* Errors: IWP_ERR_INVALID (NULL, sizes, types, alignment below the type's size, groups outside [0, groups), more than 2^25
@@ -44,7 +44,7 @@ int iwp_clip_table(const iwp_clip_tensor* tensors_host, int64_t n, int32_t group
  *   squares[g] = sum x^2                        (64 bits; have_squares: read instead, e.g. added up over ranks)
  *   norms[g]   = |scale| sqrt(squares[g])
  *   factors[g] = scale * (norms[g] > max_norm ? max_norm / norms[g] : 1)
- *   out        = factors[g] * x, rounded once to the output's type     (`write`)
+ *   out        = factors[g] * x in fp32, rounded again to an output of 16 bits   (`write`; the factor as fp32 has it)
  * A group without elements has norm 0.  A group whose sum is not finite (a NaN or an infinity in a gradient) has factor
  * `scale`, or, with drop_nonfinite, 0, and its outputs are then 0 whatever the elements are.  A factor of exactly 1 leaves tensors that are clipped where
  * they are untouched. */

@@ -114,7 +114,8 @@ int iwp_order(const iwp_order_args* args, void* cuda_stream); /* also IWP_ERR_CA
  *               weights NULL: 1 (the gradient of dispatch)
  * combine_grad: by_slot_out[slot of (t, j)] = weights[t][j] by_token[t];  rows behind offsets[E] are set to zero
  *               dweights[t][j] = <by_token[t], by_slot[slot of (t, j)]>, 0 for a pair without a slot
- * Slots outside [0, T top_k) are none. */
+ * Slots outside [0, T top_k) are none.  Rows of slots below offsets[E] that no pair has (of an order that was changed by hand) are
+ * left as they are. */
 typedef struct iwp_exchange_args {
   int64_t tokens, dim;             /* T top_k <= 2^30, D <= 2^31 - 2^16, T top_k D <= 2^46 */
   const int32_t* slots;            /* [T][top_k], of iwp_order() */

@@ -149,6 +149,8 @@ __device__ __forceinline__ void square(const Part& q, int lane, double& sum) {
     square_part<IWP_F16>(q, lane, sum);
 }
 
+// The product is an fp32 one, and what 16 bits hold is made of that: once in 2^14 values (fp16; bf16 2^17) the first
+// rounding brings it to the middle of two of them and so decides.  A multiplication in fp32 and a conversion give the same.
 template <int OUT>
 __device__ __forceinline__ typename Of<OUT>::T scaled(float x, float f) {
   return static_cast<typename Of<OUT>::T>(f == 0.f ? 0.f : x * f);
@@ -327,7 +329,7 @@ __device__ __forceinline__ void finish_group(const Args& a, int group, double sq
   if (a.factors) a.factors[group] = o.factor;
 }
 
-// Squares of eight AlexNet workers (1.95 GB fp32): 298 us = 6.5 TB/s; ResNet-50's 161 tensors: 23 us in fp32 with a norm each,
+// Squares of eight AlexNet workers (1.95 GB fp32): 289 us = 6.75 TB/s; ResNet-50's 161 tensors: 23 us in fp32 with a norm each,
 // 15 in bf16 with one, of which the chain of a block's start, its sum, the ticket and the last block's sum is 5.  (Parts of 16384
 // elements dealt out: 359 us, for the last round of them.)
 //

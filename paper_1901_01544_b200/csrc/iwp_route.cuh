@@ -476,10 +476,10 @@ __host__ __device__ constexpr int blocks_of(int M, bool scores) { return M == 8 
 // SCORES: the choice goes by scores, or among groups; else by the logits alone.  k <= G: a lane has one pick at most.
 // word: elements that all rows are aligned for.
 //
-// Bound by the integer pipe, which takes a minimum or a maximum every other cycle: 131072 x 256 fp32, 8 choices, 53 us = 2.5 TB/s
+// Bound by the integer pipe, which takes a minimum or a maximum every other cycle: 131072 x 256 fp32, 8 choices, 52 us = 2.6 TB/s
 // at 260 instructions per row, half of them the sorts'.  (The largest of a lane taken k times from unsorted columns by 32 lanes per
 // row: 333 us; sorted, 32 lanes per row: 96.)  bf16 47, with
-// sigmoid scores and a bias 68 us; 16384 x 256 bf16, 8 of which 4 groups 18.5 us.  (Left out: lanes that sort four keys 3 us less, but 2 % of
+// sigmoid scores and a bias 67 us; 16384 x 256 bf16, 8 of which 4 groups 18.5 us.  (Left out: lanes that sort four keys 3 us less, but 2 % of
 // rows need more of a lane; rows fetched into the L2 ahead 1.5 less, 1 more where rows are short.)
 template <int TYPE, int M, int G, bool SCORES>
 __global__ void __launch_bounds__(THREADS, blocks_of(M, SCORES)) k_route(const __grid_constant__ Args a, int word) {

@@ -5,7 +5,8 @@ Like the rest of the binding this only marshals arguments: every step runs in th
 stream, there is no CPU fallback, and errors are `IwpError` (status codes) or `TypeError` / `ValueError` (tensors that do not
 fit the call).  Plans are used as those of `losses`: one stream and one thread at a time, made before a CUDA graph is
 captured and kept as long as the graph.  The differentiable forms can be captured with their backward pass, as torch's own
-operators can: nothing of an earlier eager backward graph of the same leaves may be left then.
+operators can: nothing of an earlier eager backward graph of the same leaves may be left then.  The plans' `check` has
+nothing to report: what cannot be chosen is in the outputs.
 """
 from __future__ import annotations
 
