@@ -28,10 +28,14 @@ constexpr int64_t SMALL_WARPS = MAX_CLUSTER * (K::SMALL_THREADS / 32);
 
 // The sums of a single group, and of up to FEW_GROUPS that FEW_WARPS leave (of some 4 million elements), are added up by the last block
 // of the squares' launch, about 1 us a group; else by a launch of its own, 2 us on the host.  (Clipping in a loop of calls, the one and the
-// other: 25 million elements in 1 group 26 and 32 us, in 2 30 and 28, in 8 35 and 26; 4.2 million in 1 group 11.4 and 12.5, in 2 12.6 and 12.6, in 8
-// 16.9 and 12.7; 3.5 million in 2 10.6 and 12.5, in 8 15.6 and 12.5; 2 million in 2 10.5 and 12.7, in 8 12.7 and 12.8, in 12 16.2 and 12.7.)
+// other: 25 million elements in 1 group 25.5 and 26 us, in 2 30.4 and 27.6, in 8 35 and 26; 4.2 million in 1 group 11.4 and 12.5, in 2 12.6 and
+// 12.6, in 8 16.9 and 12.6; 3.5 million in 2 10.6 and 12.5, in 8 15.6 and 12.5; 2 million in 2 10.5 and 12.7, in 8 12.7 and 12.8, in 12 16.2 and 12.7.)
 constexpr int FEW_GROUPS = 8;
 constexpr int64_t FEW_WARPS = 2560;
+// In that launch up to this many groups have a block each, which thousands of sums need, more a warp each.  (Norms of 25 million elements in a
+// graph, blocks and warps: 2 groups one of which has nearly all 23.1 and 28.1 us, 16 groups 21.9 and 22.4, 64 21.4 and 21.9, 161 21.7 and 21.6; of 4
+// million in 64 groups 5.6 and 5.7, in 161 6.0 and 5.7, in 500 6.3 and 5.8.)
+constexpr int BLOCK_GROUPS = 128;
 
 int size_of(int type) { return type == IWP_F32 ? 4 : 2; }
 bool is_type(int type) { return type == IWP_F32 || type == IWP_BF16 || type == IWP_F16; }
@@ -239,7 +243,8 @@ extern "C" int iwp_clip(const iwp_clip_args* a, void* cuda_stream) {
   const int64_t blocks = std::max<int64_t>(1, tiles_of(warps, K::WARPS));
   if (!a->have_squares) LOSS_CUDA(launch(K::k_squares, blocks, K::THREADS, 0, 1, st, r));
   if (a->have_squares || !r.join)
-    LOSS_CUDA(launch(K::k_groups, std::min<int64_t>(tiles_of(a->groups, K::WARPS), 8 * SMS), K::THREADS, 0, 1, st, r));
+    LOSS_CUDA(a->groups <= BLOCK_GROUPS ? launch(K::k_groups<true>, a->groups, K::THREADS, 0, 1, st, r)
+                                        : launch(K::k_groups<false>, std::min<int64_t>(tiles_of(a->groups, K::WARPS), 8 * SMS), K::THREADS, 0, 1, st, r));
   if (a->write && warps) LOSS_CUDA(launch(K::k_scale, blocks, K::THREADS, 0, 1, st, r));
   return IWP_OK;
 }

@@ -288,6 +288,23 @@ __device__ __forceinline__ double group_sum(const Args& a, int group, int lane) 
   return sum_of(s);
 }
 
+// The same by a block; the sum is thread 0's.
+__device__ __forceinline__ double group_sum_of_block(const Args& a, int group, double (&part)[WARPS]) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  double s = 0;
+  const int2 span = a.spans[group];
+#pragma unroll 16
+  for (int i = span.x + threadIdx.x; i < span.y; i += THREADS) s += __ldcg(a.sums + i);
+  s = sum_of(s);
+  if (lane == 0) part[warp] = s;
+  __syncthreads();
+  s = 0;
+  if (threadIdx.x == 0)
+    for (int w = 0; w < WARPS; w++) s += part[w];
+  __syncthreads();
+  return s;
+}
+
 // Sums of warp w's range.
 __device__ __forceinline__ void square_range(const Args& a, int w, int lane) {
   const Start start = a.starts[w];
@@ -329,7 +346,7 @@ __device__ __forceinline__ void finish_group(const Args& a, int group, double sq
   if (a.factors) a.factors[group] = o.factor;
 }
 
-// Squares of eight AlexNet workers (1.95 GB fp32): 289 us = 6.75 TB/s; ResNet-50's 161 tensors: 23 us in fp32 with a norm each,
+// Squares of eight AlexNet workers (1.95 GB fp32): 287 us = 6.8 TB/s; ResNet-50's 161 tensors: 23 us in fp32 with a norm each,
 // 15 in bf16 with one, of which the chain of a block's start, its sum, the ticket and the last block's sum is 5.  (Parts of 16384
 // elements dealt out: 359 us, for the last round of them.)
 //
@@ -350,29 +367,28 @@ __global__ void __launch_bounds__(THREADS, 4) k_squares(const Args a) {
   __threadfence();
   __shared__ double part[WARPS];
   for (int g = 0; g < a.groups; g++) {
-    double s = 0;
-    const int2 span = a.spans[g];
-#pragma unroll 16
-    for (int i = span.x + threadIdx.x; i < span.y; i += THREADS) s += __ldcg(a.sums + i);
-    s = sum_of(s);
-    if (lane == 0) part[warp] = s;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      double y = 0;
-      for (int w = 0; w < WARPS; w++) y += part[w];
-      finish_group(a, g, y);
-    }
-    __syncthreads();
+    const double s = group_sum_of_block(a, g, part);
+    if (threadIdx.x == 0) finish_group(a, g, s);
   }
 }
 
+// A block per group, which a single group of thousands of warps needs, or a warp per group.
+template <bool BLOCKS>
 __global__ void __launch_bounds__(THREADS) k_groups(const Args a) {
   const int lane = threadIdx.x & 31;
   wait_previous();
   launch_next();
-  for (int g = blockIdx.x * WARPS + threadIdx.x / 32; g < a.groups; g += gridDim.x * WARPS) {
-    const double s = group_sum(a, g, lane);
-    if (lane == 0) finish_group(a, g, s);
+  if constexpr (BLOCKS) {
+    __shared__ double part[WARPS];
+    for (int g = blockIdx.x; g < a.groups; g += gridDim.x) {
+      const double s = a.have_squares ? a.squares[g] : group_sum_of_block(a, g, part);
+      if (threadIdx.x == 0) finish_group(a, g, s);
+    }
+  } else {
+    for (int g = blockIdx.x * WARPS + threadIdx.x / 32; g < a.groups; g += gridDim.x * WARPS) {
+      const double s = group_sum(a, g, lane);
+      if (lane == 0) finish_group(a, g, s);
+    }
   }
 }
 

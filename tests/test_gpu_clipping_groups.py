@@ -33,3 +33,22 @@ def test_groups(groups, n):
         x.copy_(w)
     given = clip.clip(0.5 * float(want.min()), squares=r.squares.clone())
     assert torch.equal(given.factors, r.factors) and all(torch.equal(x, w * f) for x, w, f in zip(xs, was, r.factors))
+
+
+@pytest.mark.parametrize("groups,n", [(2, 9_000_000), (128, 5_000_000), (129, 5_000_000), (3, 5_000_000)])
+def test_groups_of_very_different_sizes(groups, n):
+    """One group has nearly all elements, one has none."""
+    g = torch.Generator(device=DEV).manual_seed(groups)
+    sizes = [n] + [(17 * i) % 300 for i in range(1, groups)]
+    sizes[-1] = 0
+    xs = [torch.randn(m, generator=g, device=DEV, dtype=torch.float32) for m in sizes]
+    clip = clipping.GradientClip(xs, groups=list(range(groups)))
+    assert clip.groups == groups
+    want = torch.stack([x.double().norm() for x in xs])
+    r = clip.norm()
+    assert ((r.norms.double() - want).abs() <= 6 * 2.0**-24 * want).all() and r.norms[-1] == 0
+    given = clip.clip(float("inf"), squares=r.squares.clone())
+    assert torch.equal(given.norms, r.norms)
+    xs[0][n // 2] = float("nan")
+    r = clip.clip(1.0, drop_nonfinite=True)
+    assert r.factors[0] == 0 and torch.isnan(r.norms[0]) and (xs[0] == 0).all() and ((r.norms[1:].double() - want[1:]).abs() <= 6 * 2.0**-24 * want[1:]).all()
