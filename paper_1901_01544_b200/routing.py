@@ -249,16 +249,18 @@ class ExpertExchange(_Here):
         status = self._lib.iwp_order(self._order_at, stream)
         if status:
             raise IwpError(status, "iwp_order")
-        return _made((offsets, slots, rows), (self, T, k, shape, at, offsets_at, None if slots.is_inference() else slots._version))
+        order = _Made(offsets, slots, rows)
+        order.made = self, T, k, shape, at, offsets_at, None if slots.is_inference() else slots._version
+        return order
 
     def _begin(self, a: ExchangeArgs, order: Order, x, name: str):
-        """T, k and the width of x, a matrix, in an exchange by `order`, and what makes a matrix that its slots are written to."""
+        """T, k and the width of x, a matrix, in an exchange by `order`, and what makes a matrix that its slots are written to, of x's type."""
         shape = x.shape
         if len(shape) != 2:
             raise ValueError(f"{name} is a matrix")
         offsets, slots, _ = order
         plan, T, k, of, at, offsets_at, version = order.made if type(order) is _Made else _UNKNOWN
-        new = self._torch.empty
+        new = x.new_empty
         # (an order's tensors can be written to, resized, transposed or set to other memory after it was made)
         if (plan is not self or slots.data_ptr() != at or offsets.data_ptr() != offsets_at or slots.shape != of or not slots.is_contiguous()
                 or (version is not None and slots._version != version)):
@@ -268,7 +270,7 @@ class ExpertExchange(_Here):
             _vector(offsets, "offsets", self.experts + 1, self._ids[1:], self.device)
             T, k = slots.shape
             at, offsets_at = slots.data_ptr(), offsets.data_ptr()
-            new = self._torch.zeros  # (there may be slots that no pair has)
+            new = x.new_zeros  # (there may be slots that no pair has)
         D = shape[1]
         a.slots, a.offsets, a.tokens, a.top_k, a.dim = at, offsets_at, T, k, D
         return T, k, D, new
@@ -289,7 +291,7 @@ class ExpertExchange(_Here):
         a.by_token_ld = _rows_of(x, "x", (T, D), self._floats, self.device)
         a.by_token, a.type = x.data_ptr(), self._codes[x.dtype]
         if out is None:
-            out = new(T * k, D, dtype=x.dtype, device=self.device)
+            out = new(T * k, D)
             a.by_slot_out_ld = D
         else:
             a.by_slot_out_ld = _rows_of(out, "out", (T * k, D), (x.dtype,), self.device)
@@ -309,7 +311,7 @@ class ExpertExchange(_Here):
             a.weights_ld = _rows_of(weights, "weights", (T, k), self._floats[:1], self.device)
             a.weights = weights.data_ptr()
         if out is None:
-            out = self._torch.empty(T, D, dtype=z.dtype, device=self.device)
+            out = z.new_empty(T, D)
             a.by_token_out_ld = D
         else:
             a.by_token_out_ld = _rows_of(out, "out", (T, D), (z.dtype,), self.device)
@@ -336,7 +338,7 @@ class ExpertExchange(_Here):
         dz = dw = a.by_slot = a.by_slot_out = a.dweights = None
         if "rows" in want:
             if out is None:
-                dz = new(T * k, D, dtype=dy.dtype, device=self.device)
+                dz = new(T * k, D)
                 a.by_slot_out_ld = D
             else:
                 dz = out

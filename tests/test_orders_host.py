@@ -136,12 +136,12 @@ def test_what_is_written_to_is_looked_at_again():
     for inference in (False, True):
         with torch.inference_mode(inference):
             o = p.order(torch.zeros(T, K, dtype=torch.int32))
-            assert p._begin(a, o, x, "x")[3] is torch.empty
-            assert p._begin(a, o._replace(slots=o.slots.clone()), x, "x")[3] is torch.zeros
-            assert p._begin(a, routing.Order(*o), x, "x")[3] is torch.zeros
+            assert p._begin(a, o, x, "x")[3].__name__ == "new_empty"
+            assert p._begin(a, o._replace(slots=o.slots.clone()), x, "x")[3].__name__ == "new_zeros"
+            assert p._begin(a, routing.Order(*o), x, "x")[3].__name__ == "new_zeros"
             if not inference:
                 o.slots[0, 0] = -1
-                assert p._begin(a, o, x, "x")[3] is torch.zeros
+                assert p._begin(a, o, x, "x")[3].__name__ == "new_zeros"
 
 
 def test_a_backward_pass_knows_its_plans_order():
@@ -150,7 +150,7 @@ def test_a_backward_pass_knows_its_plans_order():
     p.dispatch = lambda x, o: x.clone()
 
     def dispatch_grad(dout, o):
-        seen.append(p._begin(routing.ExchangeArgs(), o, dout, "dout")[3])
+        seen.append(p._begin(routing.ExchangeArgs(), o, dout, "dout")[3].__name__)
         return dout.clone()
 
     p.dispatch_grad = dispatch_grad
@@ -158,4 +158,4 @@ def test_a_backward_pass_knows_its_plans_order():
     routing.dispatch(p, x, order(p)).sum().backward()
     o = order(p)
     routing.dispatch(p, x, o._replace(slots=o.slots.clone())).sum().backward()
-    assert seen == [torch.empty, torch.zeros]
+    assert seen == ["new_empty", "new_zeros"]
